@@ -210,14 +210,22 @@ def _own_run(st):
         return qmm.mx_dequantize(case["fmt"], st["packed"], case["M"], case["K"], out=st["values"], tensor_scale=g)
     if kind == "linear":
         g, gw = (st["g"], st["w"]["g"]) if case["fmt"] == NVFP4 else (None, None)
-        return qmm.mx_linear(case["fmt"], st["x"], st["w"]["packed"], case["N"], Y=st["y"], x_scale=g, w_scale=gw)
+        if "ws" not in st:                                 # the workspace that a program keeps beside its weights
+            st["ws"] = torch.zeros(qmm.mx_linear_workspace_bytes(case["fmt"], case["M"], case["N"], case["K"]), dtype=torch.uint8, device=st["x"].device)
+        return qmm.mx_linear(case["fmt"], st["x"], st["w"]["packed"], case["N"], Y=st["y"], x_scale=g, w_scale=gw, ws=st["ws"])
     if kind == "experts":
         scales = {}
         if case["fmt"] == NVFP4:
             scales = {"x_scale": st["g"], "gate_scale": st["gate"]["g"], "up_scale": st["up"]["g"], "down_scale": st["down"]["g"], "h_scale": st["gh"]}
-        return qmm.mx_moe(case["fmt"], st["x"], st["idx"], st["w"], st["gate"]["packed"], st["up"]["packed"], st["down"]["packed"],
-                          case["I"], case["E"], out=st["y"], **scales)
-    plan = qmm.expert_sort(st["idx"], case["E"])
+        args = qmm.mx_moe_args(case["fmt"], st["x"], st["idx"], st["w"], st["gate"]["packed"], st["up"]["packed"], st["down"]["packed"],
+                               case["I"], case["E"], st["y"], **scales)
+        if "ws" not in st:
+            st["ws"] = torch.zeros(qmm.mx_moe_workspace_bytes(args), dtype=torch.uint8, device=st["x"].device)
+        qmm.mx_moe_run(args, st["ws"])
+        return st["y"]
+    if "plan" not in st:                                   # the plan's buffers; every pass sorts into them anew
+        st["plan"] = qmm.ExpertPlan(case["T"], st["idx"].shape[1], case["E"])
+    plan = qmm.expert_sort(st["idx"], case["E"], out=st["plan"])
     xs = qmm.expert_gather(st["x"], plan, out=st["xs"])
     y = qmm.expert_combine(st["ys"], plan, st["w"], out=st["y"])
     out = {"order": plan.order, "offsets": plan.offsets, "xs": xs, "y": y}
