@@ -382,6 +382,158 @@ qmm_status qmm_moe(const qmm_moe_args* args, void* ws, size_t ws_bytes, void* st
  * descriptor carries, Sec. 3.1, without giving the rule; the rule is above.)  */
 qmm_status qmm_moe_route(const qmm_moe_args* args, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- microscaled 4-bit floating point ----
+ *
+ * Matrices whose elements are 4-bit floats (e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their
+ * negatives) with one scale per block of consecutive elements along K (the number of
+ * a format is its block length), and products whose BOTH operands are held that way: the tensor cores take
+ * codes and scales as they are.  The paper's kernel library spans weight formats from 2 to 16
+ * bits (Sec. 3.3, Sec. 4.1); it does not describe these two.
+ *   QMM_MXFP4  blocks of 32, scale e8m0: 2^(b - 127) for byte b < 255, 255 = NaN.  Quantisation takes
+ *              b - 127 = floor(log2(amax)) - 2, not below -127 (amax = the block's largest magnitude);
+ *              elements above 6 times the scale saturate.
+ *   QMM_NVFP4  blocks of 16, scale e4m3 (0x7F = NaN) times one fp32 scale g per tensor.  Quantisation takes
+ *              s = rn_e4m3(min(amax / (6 g), 448)); 6 g and the quotient are rounded to fp32.
+ * A code is the e2m1 value nearest to x / D, D = scale * g rounded to fp32 (the quotient is rounded to fp32),
+ * ties to the even code, beyond 6 saturating, with the sign of x (a zero's sign is not kept).  D = 0 gives codes 0.  A block with an
+ * infinity or a NaN gets the NaN scale and codes 0: every value of it, and every output that reads it, is NaN.
+ *   tensor scales: device pointers to one float each, read when the work runs, NULL = 1.  A tensor
+ *   scale must be positive and finite.  MXFP4 takes none (QMM_ERR_INVALID_ARG if given).
+ *
+ * Packed operand (qmm_mx_bytes; weights and activations alike).  Units of 128 rows x 256 k,
+ * unit (i, j) = rows [128 i, 128 i + 128), k [256 j, 256 j + 256), at unit index
+ * i * ceil(K / 256) + j; a unit is
+ *     16384 bytes of codes: row r has 128 bytes at 128 r, element k in nibble k % 2 (low first) of byte
+ *            k / 2; the row's 16-byte chunks are permuted, chunk c sits at place c ^ (r % 8);
+ *     1024 (MXFP4) or 2048 (NVFP4) bytes of scales: four k-blocks to a group of 512 bytes; in group j
+ *            the scales of row r for blocks 4 j .. 4 j + 3 are the 4 bytes at 16 (r % 32) + 4 (r / 32).
+ * Elements and scales past K in the last unit are zero; rows past the matrix are never read as
+ * data (they may hold anything).  Any rows >= 1 and K >= 1; buffers are 16-byte aligned.  A unit is one
+ * contiguous copy into shared memory in the order the tensor cores want.
+ * Canonical form (qmm_mx_pack): codes [rows, ceil(K/B) * B / 2] bytes, element k in nibble k % 2 of byte
+ * k / 2; scales [rows, ceil(K/B)] bytes, B the block length; codes past K must be 0.
+ *
+ * Accuracy.  Products of codes and scales are exact; sums are held in 32 bits by the tensor
+ * core.  |y - y_ref| <= 2e-3 * sum_k |a_k w_k| + half an ulp of the output type.                    */
+typedef enum { QMM_MXFP4 = 32, QMM_NVFP4 = 16 } qmm_mx_format;
+typedef enum { QMM_F16 = 0, QMM_BF16 = 1, QMM_F32 = 2 } qmm_dtype;
+
+/* Bytes of the packed form of a [rows, K] matrix; 0 if the arguments are invalid.                   */
+size_t qmm_mx_bytes(qmm_mx_format fmt, int64_t rows, int64_t K);
+
+/* Canonical codes and scales -> packed operand (a checkpoint's weights, once).  All device pointers.  */
+qmm_status qmm_mx_pack(qmm_mx_format fmt, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t K,
+                       void* packed, void* stream);
+
+/* x [rows, ldx] of type `dtype`, ldx >= K in elements -> packed operand.                            */
+qmm_status qmm_mx_quantize(qmm_mx_format fmt, qmm_dtype dtype, const void* x, int64_t ldx, int64_t rows, int64_t K,
+                           const float* tensor_scale, void* packed, void* stream);
+
+/* Packed operand -> the values it stands for, code * D in fp32 rounded to `dtype`; out [rows, ldo].     */
+qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows, int64_t K, const float* tensor_scale,
+                             qmm_dtype dtype, void* out, int64_t ldo, void* stream);
+
+/* Y[m, n] = a_scale * w_scale * sum_k a[m, k] w[n, k] with both operands packed, M >= 0, N >= 1, K >= 1.
+ *   a, w  packed [M, K] and [N, K];  Y [M, ldy] of type `dtype`, ldy >= N
+ *   ws    device, 16-byte aligned, >= qmm_mx_gemm_workspace_bytes(); starts with a status word:
+ *         zero-fill it once (qmm_status_check reports a bounded wait that gave up).                 */
+size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
+qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K,
+                       const float* a_scale, const float* w_scale, qmm_dtype dtype, void* Y, int64_t ldy,
+                       void* ws, size_t ws_bytes, void* stream);
+
+/* The same product of activations as they come: X [M, ldx] of type `dtype` is quantised (as by
+ * qmm_mx_quantize with tensor scale x_scale) on the way in; Y [M, ldy] of the same type.
+ *   ws  device, 16-byte aligned, >= qmm_mx_linear_workspace_bytes(); its first 256 bytes zeroed once.  */
+size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
+qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int64_t ldx, int64_t M,
+                         const void* w, int64_t N, int64_t K, const float* x_scale, const float* w_scale,
+                         void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- tokens sorted by expert and back ----
+ *
+ * A router has given token t the experts idx[t, 0 .. topk) (pair p = t * topk + j).  These calls put the
+ * pairs in expert order, move token rows there and back, and give the gradients of both moves.
+ * A pair whose idx lies outside [0, E) is dropped: it has no row, contributes nothing, gets gradient 0.
+ *   order   [T * topk]  order[r] = pair of sorted row r, ascending by (expert, pair); -1 for the rows past the last
+ *   place   [T * topk]  place[p] = sorted row of pair p, -1 if dropped
+ *   offsets [E + 1]     first sorted row of expert e; offsets[E] = number of rows
+ *   units   [E + 1]     sum over e' < e of ceil(rows of e' / 128): where the units of expert e start in a
+ *                       packed operand whose rows are grouped by expert (every expert starts a unit)
+ * All are device arrays of int32 filled by qmm_expert_sort.  1 <= E <= 1024, 1 <= topk <= 32, T >= 0,
+ * T * topk <= 2^22.  Data rows are [rows, ld] of type `dtype`, ld >= H >= 1 in elements.  Weights are fp32 [T, topk].
+ * Sums run in fp32 in the order j = 0, 1, ...: the same bits on every call.                           */
+size_t qmm_expert_sort_workspace_bytes(int32_t T, int32_t topk, int32_t E);
+qmm_status qmm_expert_sort(const int32_t* idx, int32_t T, int32_t topk, int32_t E, int32_t* order, int32_t* place,
+                           int32_t* offsets, int32_t* units, void* ws, size_t ws_bytes, void* stream);
+
+/* xs[place[p], :] = w[p] * x[t, :] (w NULL: a copy); rows of xs past offsets[E] are set to zero.
+ * Also the gradient of qmm_expert_combine with respect to ys.                                       */
+qmm_status qmm_expert_gather(qmm_dtype dtype, const void* x, int64_t ldx, int32_t T, int32_t topk, int64_t H,
+                             const int32_t* order, const int32_t* place, const float* weights, void* xs, int64_t ldxs,
+                             void* stream);
+
+/* y[t, :] = sum_j w[t, j] * ys[place[t, j], :] (w NULL: the plain sum, which is also the gradient of
+ * qmm_expert_gather with respect to x).  A token with no row gets zeros.                              */
+qmm_status qmm_expert_combine(qmm_dtype dtype, const void* ys, int64_t ldys, int32_t T, int32_t topk, int64_t H,
+                              const int32_t* place, const float* weights, void* y, int64_t ldy, void* stream);
+
+/* Both gradients of qmm_expert_combine in one pass over dy and ys:
+ *   dys[place[p], :] = w[p] * dy[t, :] (rows past offsets[E]: zero),  dw[t, j] = sum_h dy[t, h] * ys[place[t, j], h]. */
+qmm_status qmm_expert_combine_grad(qmm_dtype dtype, const void* dy, int64_t lddy, const void* ys, int64_t ldys,
+                                   int32_t T, int32_t topk, int64_t H, const int32_t* order, const int32_t* place,
+                                   const float* weights, void* dys, int64_t lddys, float* dw, void* stream);
+
+/* ---- experts' products on microscaled operands ----
+ *
+ * Rows grouped by expert: the packed operand of qmm_mx_quantize_experts holds the rows of expert e in the
+ * units units[e] .. units[e + 1), its first row first (qmm_mx_experts_bytes is enough for any routing).
+ * Weights of E experts are E packed matrices one after the other, stride qmm_mx_bytes; their tensor
+ * scales are arrays of E floats.                                                                    */
+size_t qmm_mx_experts_bytes(qmm_mx_format fmt, int32_t T, int32_t topk, int32_t E, int64_t K);
+
+/* Token t of x [T, ldx] is quantised once and stored at the row of each of its pairs.               */
+qmm_status qmm_mx_quantize_experts(qmm_mx_format fmt, qmm_dtype dtype, const void* x, int64_t ldx, int32_t T, int32_t topk,
+                                   int32_t E, int64_t K, const int32_t* idx, const int32_t* place, const int32_t* offsets,
+                                   const int32_t* units, const float* tensor_scale, void* packed, void* stream);
+
+/* h = silu(g) * u with g = W_gate[e] x, u = W_up[e] x of every row, kept in fp32 and quantised at once (tensor
+ * scale h_scale) into the packed [rows, N] operand of the next product.  silu(g) = g / (1 + exp(-g)).
+ *   a  packed rows, K wide;  w_gate, w_up  E packed [N, K];  h  packed rows, N wide (qmm_mx_experts_bytes)
+ *   status  optional device word, zeroed once, that qmm_status_check reads                          */
+qmm_status qmm_mx_experts_gate_up(qmm_mx_format fmt, const void* a, int32_t T, int32_t topk, int32_t E,
+                                  const int32_t* offsets, const int32_t* units, const void* w_gate, const void* w_up,
+                                  int64_t N, int64_t K, const float* a_scale, const float* gate_scale, const float* up_scale,
+                                  const float* h_scale, void* h, int32_t* status, void* stream);
+
+/* Y[r, :] = W[e] a[r, :] for every sorted row r of every expert e; Y [T * topk, ldy] of type `dtype` in sorted
+ * order (rows past offsets[E] are not written).                                                     */
+qmm_status qmm_mx_experts_gemm(qmm_mx_format fmt, const void* a, int32_t T, int32_t topk, int32_t E,
+                               const int32_t* offsets, const int32_t* units, const void* w, int64_t N, int64_t K,
+                               const float* a_scale, const float* w_scale, qmm_dtype dtype, void* Y, int64_t ldy,
+                               int32_t* status, void* stream);
+
+/* The routed feed-forward layer made of the calls above:
+ *   sort; quantise x into the expert order; h = silu(Wgate x) * (Wup x); d = Wdown h rounded to `dtype`;
+ *   out[t, :] = sum_j weights[t, j] * d[place[t, j], :].                                               */
+typedef struct {
+    int32_t T, H, I, E, topk;      /* tokens, hidden, expert intermediate, experts, k      */
+    int32_t fmt, dtype;            /* qmm_mx_format of weights and activations; qmm_dtype of X and out */
+    const void* X;                 /* [T, ldx]                                             */
+    int64_t ldx;
+    const int32_t* idx;            /* [T, topk] experts of each token; outside [0, E) = dropped */
+    const float* weights;          /* [T, topk]                                            */
+    const void *w_gate, *w_up;     /* E packed [I, H] matrices each                        */
+    const void* w_down;            /* E packed [H, I] matrices                             */
+    const float *x_scale, *h_scale;                        /* tensor scales of x and h (NVFP4), one float each, or NULL */
+    const float *gate_scale, *up_scale, *down_scale;       /* [E] each (NVFP4), or NULL    */
+    void* out;                     /* [T, ldo], written                                    */
+    int64_t ldo;
+} qmm_mx_moe_args;
+size_t qmm_mx_moe_workspace_bytes(const qmm_mx_moe_args* args);          /* host pointer; only sizes are read */
+/* ws: device, 256-byte aligned, its first 256 bytes zeroed once (status word).                        */
+qmm_status qmm_mx_moe(const qmm_mx_moe_args* args, void* ws, size_t ws_bytes, void* stream);
+
 /* Waits for `stream`, then reports what the kernels that used `ws` recorded in
  * its status word since this call last cleared it: QMM_ERR_DEVICE_TIMEOUT if a
  * bounded wait gave up, QMM_ERR_BAD_WEIGHTS from qmm_packed_check, else QMM_OK.

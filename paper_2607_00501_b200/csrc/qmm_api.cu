@@ -67,10 +67,10 @@ static qmm_status check_fmt_everywhere(const char* who, int fmt)
     return QMM_OK;
 }
 
-static bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 // The kernels are built for sm_100a only; refuse any other device.
-static qmm_status check_device(const char* who)
+qmm_status check_device(const char* who)
 {
     static thread_local int cached_dev = -1;
     static thread_local int cached_ok = 0;

@@ -90,6 +90,8 @@ __host__ __device__ inline int canon_block_of(int fmt) { return fmt == QMM_Q4 ? 
 // Host-side error reporting (thread-local buffer; see qmm_api.cu).
 qmm_status fail(qmm_status code, const char* fmt, ...);
 qmm_status check_cuda(cudaError_t e, const char* what);
+qmm_status check_device(const char* who);
+bool aligned(const void* p, size_t a);
 
 // Debug knobs set through qmm_debug_config (tests and tuning sweeps force launch geometries
 // with them; none changes a result beyond the order of fp32 additions).  Plain process-wide

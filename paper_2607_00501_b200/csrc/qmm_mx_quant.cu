@@ -1,0 +1,319 @@
+// qmm_mx_quant.cu -- microscaled 4-bit floating point: canonical -> packed, quantisation (plain, and of
+// tokens into the experts' row order) and dequantisation.  All are bound by HBM: one pass over the data, a thread
+// per 32 elements.
+#include "qmm_mx.cuh"
+
+namespace qmm {
+
+using namespace mx;
+
+constexpr int kQuantThreads = 256;
+
+// Where a token's pairs go (grouped rows), or nothing (plain rows).
+struct MxRows {
+    const int *idx, *place, *offsets, *units;
+    int topk, E;
+};
+
+// 32 consecutive elements at p as fp32.  VEC: bytes per load that the row's alignment allows (32, 16, or 0: element
+// by element); n < 32 elements exist (the rest read as zero).
+template <typename T, int VEC> __device__ __forceinline__ void load32(const T* p, int n, float (&v)[32])
+{
+    constexpr int BYTES = 32 * (int)sizeof(T);
+    if (VEC >= 16 && n >= 32) {
+        uint32_t u[BYTES / 4];
+        if (VEC == 32) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) {
+                const u32x8 w = ld_stream_256(reinterpret_cast<const uint8_t*>(p) + 32 * i);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u[8 * i + k] = w.v[k];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>(p) + i);
+                u[4 * i] = w.x, u[4 * i + 1] = w.y, u[4 * i + 2] = w.z, u[4 * i + 3] = w.w;
+            }
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = Dt<T>::up2(u[i]);
+                v[2 * i] = f.x, v[2 * i + 1] = f.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = i < n ? Dt<T>::up(p[i]) : 0.0f;
+}
+
+// The two (NVFP4) or one (MXFP4) blocks of 32 elements -> 16 bytes of codes, scale bytes in `sb`.
+template <int FMT> __device__ __forceinline__ uint4 quantize32(const float (&v)[32], float g, float g6, uint32_t& sb)
+{
+    uint4 c;
+    if constexpr (FMT == QMM_MXFP4) {
+        uint32_t w[4];
+        sb = quantize_block<32>(v, g, g6, w);
+        c = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        float a[16], b[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[i] = v[i], b[i] = v[16 + i];
+        uint32_t wa[2], wb[2];
+        sb = quantize_block<16>(a, g, g6, wa);
+        sb |= quantize_block<16>(b, g, g6, wb) << 8;
+        c = make_uint4(wa[0], wa[1], wb[0], wb[1]);
+    }
+    return c;
+}
+
+// Thread = one 32-element chunk of one row; chunks run over the padded K (a multiple of 256), so the padding of the last
+// unit is written as zeros.  Consecutive lanes hold consecutive chunks of a row (a row has a multiple of 8):
+// 4 (MXFP4) or 2 (NVFP4) neighbouring lanes join their scale bytes into one 4-byte store.
+// EXPERTS: the row is a token, quantised once and stored at the row of each of its pairs.
+// 8192 x 8192 fp16 -> MXFP4 is 171 MB of traffic: see the table of measurements for the rate.
+template <int FMT, typename T, int VEC, bool EXPERTS>
+__global__ void __launch_bounds__(kQuantThreads)
+mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K, const float* __restrict__ tensor_scale,
+                   uint8_t* __restrict__ packed, const MxRows m, int early)
+{
+    if (early) pdl_launch_dependents();
+    pdl_wait();
+    const int64_t KU = k_units(K);
+    const int64_t chunks = KU * (kUnitK / 32);
+    const int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    if (id >= rows * chunks) return;                       // (whole quads: rows * chunks is a multiple of 8)
+    const int64_t row = id / chunks;
+    const int c = (int)(id - row * chunks);
+    const float g = tensor_scale ? __ldg(tensor_scale) : 1.0f;
+    const float g6 = 6.0f * g;
+    const int64_t left = K - (int64_t)c * 32;
+    float v[32];
+    load32<T, VEC>(x + row * ldx + (int64_t)c * 32, (int)(left < 0 ? 0 : left < 32 ? left : 32), v);
+    uint32_t sb;
+    uint4 codes = quantize32<FMT>(v, g, g6, sb);
+    // scale bytes of the group of four blocks, assembled in its first lane
+    constexpr int LANES = FMT == QMM_MXFP4 ? 4 : 2;
+    const uint32_t sub = (uint32_t)c & (LANES - 1);
+    const uint32_t active = __activemask();
+    uint32_t word = sb << (sub * (32 / LANES));
+    if (left <= 0) word = 0;
+#pragma unroll
+    for (int o = 1; o < LANES; o <<= 1) word |= __shfl_xor_sync(active, word, o);
+    const uint32_t group = (uint32_t)(c & 7) / LANES;
+    auto store = [&](int64_t slot) {
+        uint8_t* unit = packed + ((slot >> 7) * KU + (c >> 3)) * unit_bytes(FMT);
+        const uint32_t r = (uint32_t)(slot & 127);
+        *reinterpret_cast<uint4*>(unit + chunk_offset(r, c & 7)) = codes;
+        if (sub == 0) *reinterpret_cast<uint32_t*>(unit + scale_offset(r, group)) = word;
+    };
+    if constexpr (!EXPERTS) {
+        store(row);
+    } else {
+        for (int j = 0; j < m.topk; ++j) {
+            const int64_t p = row * m.topk + j;
+            const int r = m.place[p];
+            if (r < 0) continue;
+            const int e = m.idx[p];
+            store((int64_t)m.units[e] * 128 + (r - m.offsets[e]));
+        }
+    }
+}
+
+// Thread = one 16-byte chunk of codes -> 32 values.  D = scale * g in fp32, value = code * D in fp32 (rounded once).
+template <int FMT, typename T, int VEC>
+__global__ void __launch_bounds__(kQuantThreads)
+mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K, const float* __restrict__ tensor_scale,
+                     T* __restrict__ out, int64_t ldo)
+{
+    pdl_wait();
+    const int64_t chunks = (K + 31) / 32;
+    const int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    if (id >= rows * chunks) return;
+    const int64_t row = id / chunks;
+    const int c = (int)(id - row * chunks);
+    const float g = tensor_scale ? __ldg(tensor_scale) : 1.0f;
+    const uint8_t* unit = packed + ((row >> 7) * k_units(K) + (c >> 3)) * unit_bytes(FMT);
+    const uint32_t r = (uint32_t)(row & 127);
+    const uint4 q = __ldg(reinterpret_cast<const uint4*>(unit + chunk_offset(r, c & 7)));
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    float D[2];
+    if (FMT == QMM_MXFP4) {
+        D[0] = D[1] = e8m0_value(unit[scale_offset(r, (c & 7) >> 2) + (c & 3)]);
+    } else {
+        const uint16_t s = *reinterpret_cast<const uint16_t*>(unit + scale_offset(r, (c & 7) >> 1) + 2 * (c & 1));
+        D[0] = e4m3_value(s & 0xFFu) * g;
+        D[1] = e4m3_value(s >> 8) * g;
+    }
+    float v[32];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[i >> 2] >> (8 * (i & 3))), __NV_E2M1);
+        const float2 f = __half22float2(__half2(h));
+        v[2 * i] = f.x * D[i >> 3];
+        v[2 * i + 1] = f.y * D[i >> 3];
+    }
+    T* o = out + row * ldo + (int64_t)c * 32;
+    const int64_t left = K - (int64_t)c * 32;
+    if (VEC && left >= 32) {
+        if constexpr (sizeof(T) == 2) {
+            uint32_t u[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) u[i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(o)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 32; ++i)
+            if (i < left) o[i] = Dt<T>::down(v[i]);
+    }
+}
+
+// Canonical codes and scales -> packed.  Thread = one 16-byte chunk (and the scales of its 32 elements).
+template <int FMT>
+__global__ void __launch_bounds__(kQuantThreads)
+mx_pack_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales, int64_t rows, int64_t K, uint8_t* __restrict__ packed)
+{
+    const int64_t KU = k_units(K), chunks = KU * (kUnitK / 32);
+    const int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    if (id >= rows * chunks) return;
+    const int64_t row = id / chunks;
+    const int c = (int)(id - row * chunks);
+    const int64_t blocks = (K + FMT - 1) / FMT, pitch = blocks * (FMT / 2);
+    uint8_t* unit = packed + ((row >> 7) * KU + (c >> 3)) * unit_bytes(FMT);
+    const uint32_t r = (uint32_t)(row & 127);
+    uint32_t w[4] = {0, 0, 0, 0};
+    const uint8_t* src = codes + row * pitch + (int64_t)c * 16;
+    const int64_t left = pitch - (int64_t)c * 16;
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+        if (i < left) w[i >> 2] |= (uint32_t)src[i] << (8 * (i & 3));
+    *reinterpret_cast<uint4*>(unit + chunk_offset(r, c & 7)) = make_uint4(w[0], w[1], w[2], w[3]);
+    constexpr int PER = 32 / FMT;                          // blocks per chunk
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+        const int64_t b = (int64_t)c * PER + i;
+        const uint32_t in_unit = (uint32_t)((c & 7) * PER + i);
+        unit[scale_offset(r, in_unit >> 2) + (in_unit & 3)] = b < blocks ? scales[row * blocks + b] : (uint8_t)0;
+    }
+}
+
+// ------------------------------------------------------------ launches
+
+static qmm_status launch_grid(int64_t threads, dim3* grid)
+{
+    const int64_t blocks = (threads + kQuantThreads - 1) / kQuantThreads;
+    if (blocks > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "matrix of %lld 32-element chunks is too large for one launch", (long long)threads);
+    *grid = dim3((unsigned)blocks);
+    return QMM_OK;
+}
+
+template <typename... P, typename... A>
+static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, cudaStream_t st, const char* what, A... args)
+{
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(threads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kern, args...), what);
+}
+
+// `early`: let the next kernel in the stream start its prologue at once.  Only for activations on their way into a
+// product of the same call: that product reads its weights before it waits, and the rows quantised here could be a caller's weights.
+template <int FMT, typename T>
+static qmm_status quantize_t(const void* x, int64_t ldx, int64_t rows, int64_t K, const float* ts, void* packed, const MxRows* m, bool early, cudaStream_t st)
+{
+    dim3 grid;
+    const qmm_status s = launch_grid(rows * k_units(K) * (kUnitK / 32), &grid);
+    if (s != QMM_OK) return s;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(x) | (rows > 1 ? (uintptr_t)(ldx * (int64_t)sizeof(T)) : 0);
+    const int vec = a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : 0;
+    const MxRows none = {nullptr, nullptr, nullptr, nullptr, 0, 0};
+    auto go = [&](auto kern, const MxRows& r) {
+        return launch_pdl(kern, grid, kQuantThreads, st, "microscaled quantisation launch", (const T*)x, ldx, rows, K, ts, (uint8_t*)packed, r, (int)early);
+    };
+    if (m) {
+        if (vec == 32) return go(mx_quantize_kernel<FMT, T, 32, true>, *m);
+        if (vec == 16) return go(mx_quantize_kernel<FMT, T, 16, true>, *m);
+        return go(mx_quantize_kernel<FMT, T, 0, true>, *m);
+    }
+    if (vec == 32) return go(mx_quantize_kernel<FMT, T, 32, false>, none);
+    if (vec == 16) return go(mx_quantize_kernel<FMT, T, 16, false>, none);
+    return go(mx_quantize_kernel<FMT, T, 0, false>, none);
+}
+
+static qmm_status quantize_any(int fmt, int dtype, const void* x, int64_t ldx, int64_t rows, int64_t K, const float* ts, void* packed,
+                               const MxRows* m, bool early, cudaStream_t st)
+{
+    if (fmt == QMM_MXFP4) {
+        if (dtype == QMM_F16) return quantize_t<QMM_MXFP4, __half>(x, ldx, rows, K, ts, packed, m, early, st);
+        if (dtype == QMM_BF16) return quantize_t<QMM_MXFP4, __nv_bfloat16>(x, ldx, rows, K, ts, packed, m, early, st);
+        return quantize_t<QMM_MXFP4, float>(x, ldx, rows, K, ts, packed, m, early, st);
+    }
+    if (dtype == QMM_F16) return quantize_t<QMM_NVFP4, __half>(x, ldx, rows, K, ts, packed, m, early, st);
+    if (dtype == QMM_BF16) return quantize_t<QMM_NVFP4, __nv_bfloat16>(x, ldx, rows, K, ts, packed, m, early, st);
+    return quantize_t<QMM_NVFP4, float>(x, ldx, rows, K, ts, packed, m, early, st);
+}
+
+qmm_status launch_mx_quantize(int fmt, int dtype, const void* x, int64_t ldx, int64_t rows, int64_t K, const float* ts, void* packed,
+                              bool early, cudaStream_t st)
+{
+    return quantize_any(fmt, dtype, x, ldx, rows, K, ts, packed, nullptr, early, st);
+}
+
+qmm_status launch_mx_quantize_experts(int fmt, int dtype, const void* x, int64_t ldx, int T, int topk, int E, int64_t K, const int* idx,
+                                      const int* place, const int* offsets, const int* units, const float* ts, void* packed, bool early,
+                                      cudaStream_t st)
+{
+    const MxRows m = {idx, place, offsets, units, topk, E};
+    return quantize_any(fmt, dtype, x, ldx, T, K, ts, packed, &m, early, st);
+}
+
+template <int FMT, typename T>
+static qmm_status dequantize_t(const void* packed, int64_t rows, int64_t K, const float* ts, void* out, int64_t ldo, cudaStream_t st)
+{
+    dim3 grid;
+    const qmm_status s = launch_grid(rows * ((K + 31) / 32), &grid);
+    if (s != QMM_OK) return s;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(out) | (rows > 1 ? (uintptr_t)(ldo * (int64_t)sizeof(T)) : 0);
+    return launch_pdl(a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 1> : mx_dequantize_kernel<FMT, T, 0>, grid, kQuantThreads, st,
+                      "microscaled dequantisation launch", (const uint8_t*)packed, rows, K, ts, (T*)out, ldo);
+}
+
+qmm_status launch_mx_dequantize(int fmt, int dtype, const void* packed, int64_t rows, int64_t K, const float* ts, void* out, int64_t ldo, cudaStream_t st)
+{
+    if (fmt == QMM_MXFP4) {
+        if (dtype == QMM_F16) return dequantize_t<QMM_MXFP4, __half>(packed, rows, K, ts, out, ldo, st);
+        if (dtype == QMM_BF16) return dequantize_t<QMM_MXFP4, __nv_bfloat16>(packed, rows, K, ts, out, ldo, st);
+        return dequantize_t<QMM_MXFP4, float>(packed, rows, K, ts, out, ldo, st);
+    }
+    if (dtype == QMM_F16) return dequantize_t<QMM_NVFP4, __half>(packed, rows, K, ts, out, ldo, st);
+    if (dtype == QMM_BF16) return dequantize_t<QMM_NVFP4, __nv_bfloat16>(packed, rows, K, ts, out, ldo, st);
+    return dequantize_t<QMM_NVFP4, float>(packed, rows, K, ts, out, ldo, st);
+}
+
+qmm_status launch_mx_pack(int fmt, const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t K, void* packed, cudaStream_t st)
+{
+    dim3 grid;
+    const qmm_status s = launch_grid(rows * k_units(K) * (kUnitK / 32), &grid);
+    if (s != QMM_OK) return s;
+    if (fmt == QMM_MXFP4) mx_pack_kernel<QMM_MXFP4><<<grid, kQuantThreads, 0, st>>>(codes, scales, rows, K, (uint8_t*)packed);
+    else mx_pack_kernel<QMM_NVFP4><<<grid, kQuantThreads, 0, st>>>(codes, scales, rows, K, (uint8_t*)packed);
+    return check_cuda(cudaGetLastError(), "microscaled pack launch");
+}
+
+}  // namespace qmm

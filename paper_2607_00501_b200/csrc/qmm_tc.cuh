@@ -251,5 +251,70 @@ __device__ __forceinline__ void mma_commit_sel(uint64_t* bar, uint32_t sel)
         : "memory");
 }
 
+// ------------------------------------------- bulk copies, block-scaled MMA
+
+// Contiguous global -> shared copy of `bytes` (a multiple of 16; both addresses 16-byte aligned), completion counted
+// on an mbarrier.
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar)
+                 : "memory");
+}
+
+// Shared-memory descriptor of a 512-byte scale group (32 rows of 16 bytes, not swizzled: 8-row groups 128 bytes apart).
+__device__ __forceinline__ uint64_t smem_desc_scales(uint32_t smem_addr)
+{
+    return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
+}
+
+// One scale group, shared memory -> 4 columns of tensor memory, repeated in the four lane quarters.
+__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc, uint32_t sel)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t"
+        "}\n"
+        ::"r"(taddr), "l"(desc), "r"(sel)
+        : "memory");
+}
+
+// Instruction descriptor of the block-scaled 4-bit MMA: e2m1 A and B (K-major), fp32 D, M = 128 (or 256 over a pair of
+// SMs); scales e8m0 (one per 32 k) or e4m3 (one per 16).  Scale ids: byte of the scale word that the K = 64 step starts at.
+__host__ __device__ constexpr uint32_t idesc_fp4(bool e8m0, int m, int n, int scale_id)
+{
+    return (1u << 7) | (1u << 10) | ((uint32_t)scale_id << 4) | ((uint32_t)(n >> 3) << 17) | ((e8m0 ? 1u : 0u) << 23) |
+           ((uint32_t)(m >> 4) << 24) | ((uint32_t)scale_id << 29);
+}
+
+// D[tmem] (+)= (A[smem] * sa) * (B[smem] * sb)^T over 64 k.
+template <bool E8M0>
+__device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                        uint32_t acc, uint32_t sel)
+{
+    if (E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            : "memory");
+}
+
 }  // namespace tc
 }  // namespace qmm

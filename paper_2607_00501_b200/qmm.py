@@ -18,6 +18,11 @@ Q5 = 5
 Q6 = 6
 Q8 = 8
 
+# microscaled 4-bit floating point (the number of a format is its block length) and element types
+MXFP4 = 32
+NVFP4 = 16
+DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libqmm.so")
 _lock = threading.Lock()
@@ -36,6 +41,10 @@ EXPORTS = (
     "qmm_moe_workspace_bytes", "qmm_moe", "qmm_moe_route", "qmm_status_check", "qmm_gemv_static", "qmm_gemv_batch", "qmm_gemm_batch",
     "qmm_gemv_gate_up", "qmm_packed_check", "qmm_debug_config", "qmm_debug_wait_give_up",
     "qmm_chain_plan_bytes", "qmm_chain_workspace_bytes", "qmm_chain_build", "qmm_chain_run",
+    "qmm_mx_bytes", "qmm_mx_pack", "qmm_mx_quantize", "qmm_mx_dequantize", "qmm_mx_gemm_workspace_bytes", "qmm_mx_gemm",
+    "qmm_mx_linear_workspace_bytes", "qmm_mx_linear", "qmm_expert_sort_workspace_bytes", "qmm_expert_sort", "qmm_expert_gather",
+    "qmm_expert_combine", "qmm_expert_combine_grad", "qmm_mx_experts_bytes", "qmm_mx_quantize_experts", "qmm_mx_experts_gate_up",
+    "qmm_mx_experts_gemm", "qmm_mx_moe_workspace_bytes", "qmm_mx_moe",
 )
 
 
@@ -86,6 +95,18 @@ class MoeArgs(ctypes.Structure):
     ]
 
 
+class MxMoeArgs(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("H", ctypes.c_int32), ("I", ctypes.c_int32), ("E", ctypes.c_int32), ("topk", ctypes.c_int32),
+        ("fmt", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("idx", ctypes.c_void_p), ("weights", ctypes.c_void_p),
+        ("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p),
+        ("x_scale", ctypes.c_void_p), ("h_scale", ctypes.c_void_p), ("gate_scale", ctypes.c_void_p),
+        ("up_scale", ctypes.c_void_p), ("down_scale", ctypes.c_void_p),
+        ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64),
+    ]
+
+
 def lib() -> ctypes.CDLL:
     """Load libqmm.so (building it with nvcc first if it is not there)."""
     global _lib
@@ -126,6 +147,29 @@ def lib() -> ctypes.CDLL:
             L.qmm_chain_workspace_bytes.argtypes = [ci, ctypes.POINTER(ChainStage), ci]
             L.qmm_chain_build.argtypes = [ci, ctypes.POINTER(ChainStage), ci, vp, sz, vp, sz, ctypes.POINTER(ChainInfo), vp]
             L.qmm_chain_run.argtypes = [ctypes.POINTER(ChainInfo), vp]
+            i32 = ctypes.c_int32
+            for name in ("qmm_mx_bytes", "qmm_mx_gemm_workspace_bytes", "qmm_mx_linear_workspace_bytes", "qmm_expert_sort_workspace_bytes",
+                         "qmm_mx_experts_bytes", "qmm_mx_moe_workspace_bytes"):
+                getattr(L, name).restype = sz
+            L.qmm_mx_bytes.argtypes = [ci, i64, i64]
+            L.qmm_mx_pack.argtypes = [ci, vp, vp, i64, i64, vp, vp]
+            L.qmm_mx_quantize.argtypes = [ci, ci, vp, i64, i64, i64, vp, vp, vp]
+            L.qmm_mx_dequantize.argtypes = [ci, vp, i64, i64, vp, ci, vp, i64, vp]
+            L.qmm_mx_gemm_workspace_bytes.argtypes = [ci, i64, i64, i64]
+            L.qmm_mx_gemm.argtypes = [ci, vp, i64, vp, i64, i64, vp, vp, ci, vp, i64, vp, sz, vp]
+            L.qmm_mx_linear_workspace_bytes.argtypes = [ci, i64, i64, i64]
+            L.qmm_mx_linear.argtypes = [ci, ci, vp, i64, i64, vp, i64, i64, vp, vp, vp, i64, vp, sz, vp]
+            L.qmm_expert_sort_workspace_bytes.argtypes = [i32, i32, i32]
+            L.qmm_expert_sort.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]
+            L.qmm_expert_gather.argtypes = [ci, vp, i64, i32, i32, i64, vp, vp, vp, vp, i64, vp]
+            L.qmm_expert_combine.argtypes = [ci, vp, i64, i32, i32, i64, vp, vp, vp, i64, vp]
+            L.qmm_expert_combine_grad.argtypes = [ci, vp, i64, vp, i64, i32, i32, i64, vp, vp, vp, vp, i64, vp, vp]
+            L.qmm_mx_experts_bytes.argtypes = [ci, i32, i32, i32, i64]
+            L.qmm_mx_quantize_experts.argtypes = [ci, ci, vp, i64, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, vp]
+            L.qmm_mx_experts_gate_up.argtypes = [ci, vp, i32, i32, i32, vp, vp, vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, vp]
+            L.qmm_mx_experts_gemm.argtypes = [ci, vp, i32, i32, i32, vp, vp, vp, i64, i64, vp, vp, ci, vp, i64, vp, vp]
+            L.qmm_mx_moe_workspace_bytes.argtypes = [ctypes.POINTER(MxMoeArgs)]
+            L.qmm_mx_moe.argtypes = [ctypes.POINTER(MxMoeArgs), vp, sz, vp]
             L.qmm_packed_check.argtypes = [ci, vp, i64, i64, vp, vp]
             L.qmm_debug_config.argtypes = [ctypes.c_char_p, ctypes.c_char_p]
             L.qmm_debug_wait_give_up.argtypes = [vp, i64, vp]
@@ -356,6 +400,282 @@ class Chain:
 
     def run(self) -> None:
         _check(lib().qmm_chain_run(ctypes.byref(self.info), _stream()))
+
+
+# ---- microscaled 4-bit floating point
+
+def _rows2d(t: torch.Tensor, what: str):
+    """(pointer, row pitch, rows, columns) of a 2-D CUDA tensor whose rows are contiguous."""
+    shape, stride = t.shape, t.stride()
+    assert t.is_cuda and len(shape) == 2 and (stride[1] == 1 or shape[1] <= 1), "%s: 2-D CUDA tensor with contiguous rows" % what
+    return t.data_ptr(), max(stride[0], shape[1]) if shape[0] <= 1 else stride[0], shape[0], shape[1]
+
+
+def _scalar(t, n: int = 1) -> int:
+    """Pointer of n fp32 tensor scales (None: 0)."""
+    if t is None:
+        return 0
+    assert t.is_cuda and t.dtype == torch.float32 and t.numel() == n and t.is_contiguous()
+    return t.data_ptr()
+
+
+def _operand(t: torch.Tensor, need: int, what: str) -> int:
+    """Pointer of a packed operand of at least `need` bytes."""
+    assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()
+    if need == 0:
+        raise QmmError(1, last_error())
+    assert t.numel() >= need, "%s: %d bytes, %d needed" % (what, t.numel(), need)
+    return t.data_ptr()
+
+
+def _workspace(need: int, device, ws: torch.Tensor | None) -> torch.Tensor:
+    """ws, or a new workspace with a zeroed status word (callers on a hot path keep one)."""
+    if need == 0:
+        raise QmmError(1, last_error())
+    if ws is None:
+        ws = torch.empty(need, dtype=torch.uint8, device=device)
+        ws[:256].zero_()
+    return ws
+
+
+def mx_bytes(fmt: int, rows: int, K: int) -> int:
+    return lib().qmm_mx_bytes(fmt, rows, K)
+
+
+def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Canonical codes uint8 [rows, ceil(K/B) B/2] and scales uint8 [rows, ceil(K/B)] (B = fmt, the block length) -> packed operand."""
+    rows, blocks = codes.shape[0], -(-K // fmt)
+    assert codes.is_cuda and codes.dtype == torch.uint8 and codes.is_contiguous() and codes.shape == (rows, blocks * fmt // 2)
+    assert scales.is_cuda and scales.dtype == torch.uint8 and scales.is_contiguous() and scales.shape == (rows, blocks)
+    need = mx_bytes(fmt, rows, K)
+    if out is None:
+        out = torch.empty(need, dtype=torch.uint8, device=codes.device)
+    _check(lib().qmm_mx_pack(fmt, codes.data_ptr(), scales.data_ptr(), rows, K, _operand(out, need, "out"), _stream()))
+    return out
+
+
+def mx_quantize(fmt: int, x: torch.Tensor, out: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None) -> torch.Tensor:
+    """x [rows, K] (fp16, bf16 or fp32; any row stride) -> packed operand, uint8."""
+    ptr, ld, rows, K = _rows2d(x, "x")
+    need = lib().qmm_mx_bytes(fmt, rows, K)
+    if out is None:
+        out = torch.empty(need, dtype=torch.uint8, device=x.device)
+    dst = _operand(out, need, "out") if rows else 0
+    _check(_lib.qmm_mx_quantize(fmt, DTYPES[x.dtype], ptr, ld, rows, K, _scalar(tensor_scale), dst, _stream()))
+    return out
+
+
+def mx_dequantize(fmt: int, packed: torch.Tensor, rows: int, K: int, out: torch.Tensor | None = None,
+                  tensor_scale: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """Packed operand -> the values it stands for, [rows, K] of out's type (or `dtype`)."""
+    if out is None:
+        out = torch.empty((rows, K), dtype=dtype, device=packed.device)
+    ptr, ld, r, k = _rows2d(out, "out")
+    assert (r, k) == (rows, K)
+    src = _operand(packed, lib().qmm_mx_bytes(fmt, rows, K), "packed") if rows else 0
+    _check(lib().qmm_mx_dequantize(fmt, src, rows, K, _scalar(tensor_scale), DTYPES[out.dtype], ptr, ld, _stream()))
+    return out
+
+
+def mx_gemm_workspace_bytes(fmt: int, M: int, N: int, K: int) -> int:
+    return lib().qmm_mx_gemm_workspace_bytes(fmt, M, N, K)
+
+
+def mx_gemm(fmt: int, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int, Y: torch.Tensor | None = None,
+            a_scale: torch.Tensor | None = None, w_scale: torch.Tensor | None = None, ws: torch.Tensor | None = None,
+            dtype: torch.dtype = torch.float16) -> torch.Tensor:
+    """Y [M, N] = a w^T with both operands packed; Y's type, or `dtype` where Y is None."""
+    L = lib()
+    if Y is None:
+        Y = torch.empty((M, N), dtype=dtype, device=a.device)
+    ptr, ld, r, c = _rows2d(Y, "Y")
+    assert (r, c) == (M, N)
+    ws = _workspace(L.qmm_mx_gemm_workspace_bytes(fmt, M, N, K), a.device, ws)
+    _check(L.qmm_mx_gemm(fmt, _operand(a, L.qmm_mx_bytes(fmt, M, K), "a") if M else 0, M, _operand(w, L.qmm_mx_bytes(fmt, N, K), "w"), N, K,
+                         _scalar(a_scale), _scalar(w_scale), DTYPES[Y.dtype], ptr, ld, ws.data_ptr(), _nbytes(ws), _stream()))
+    return Y
+
+
+def mx_linear_workspace_bytes(fmt: int, M: int, N: int, K: int) -> int:
+    return lib().qmm_mx_linear_workspace_bytes(fmt, M, N, K)
+
+
+def mx_linear(fmt: int, X: torch.Tensor, w: torch.Tensor, N: int, Y: torch.Tensor | None = None, x_scale: torch.Tensor | None = None,
+              w_scale: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """Y [M, N] = quantised(X) w^T: X [M, K] as it comes (fp16, bf16 or fp32), w packed [N, K]; Y has X's type."""
+    L = lib()
+    xp, ldx, M, K = _rows2d(X, "X")
+    if Y is None:
+        Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
+    yp, ldy, r, c = _rows2d(Y, "Y")
+    assert (r, c) == (M, N) and Y.dtype == X.dtype
+    if ws is None:
+        ws = _workspace(L.qmm_mx_linear_workspace_bytes(fmt, M, N, K), X.device, ws)
+    _check(L.qmm_mx_linear(fmt, DTYPES[X.dtype], xp, ldx, M, _operand(w, L.qmm_mx_bytes(fmt, N, K), "w"), N, K, _scalar(x_scale),
+                           _scalar(w_scale), yp, ldy, ws.data_ptr(), _nbytes(ws), _stream()))
+    return Y
+
+
+# ---- tokens sorted by expert and back
+
+class ExpertPlan:
+    """Where each (token, slot) pair of a router's choice goes in expert order (qmm_expert_sort fills it; buffers are kept
+    and may be refilled).  order, place [T * topk], offsets, units [E + 1]: int32 views of one buffer."""
+
+    def __init__(self, T: int, topk: int, E: int, device="cuda"):
+        P = T * topk
+        self.T, self.topk, self.E = T, topk, E
+        self.buf = torch.empty(2 * P + 2 * (E + 1), dtype=torch.int32, device=device)
+        self.order, self.place, self.offsets, self.units = self.buf.split([P, P, E + 1, E + 1])
+        base = self.buf.data_ptr()
+        self.ptrs = (base, base + 4 * P, base + 8 * P, base + 8 * P + 4 * (E + 1))         # order, place, offsets, units
+        self.ws_bytes = lib().qmm_expert_sort_workspace_bytes(T, topk, E)
+        self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if self.ws_bytes else None
+
+
+def expert_sort(idx: torch.Tensor, E: int, out: ExpertPlan | None = None) -> ExpertPlan:
+    """idx [T, topk] int32: experts of each token, values outside [0, E) dropped -> ExpertPlan."""
+    assert idx.is_cuda and idx.dtype == torch.int32 and idx.dim() == 2 and idx.is_contiguous()
+    T, topk = idx.shape
+    if out is None:
+        out = ExpertPlan(T, topk, E, idx.device)
+    assert (out.T, out.topk, out.E) == (T, topk, E)
+    order, place, offsets, units = out.ptrs
+    _check(lib().qmm_expert_sort(idx.data_ptr(), T, topk, E, order, place, offsets, units, _dp(out.ws), out.ws_bytes, _stream()))
+    return out
+
+
+def _weights_ptr(weights, plan: ExpertPlan) -> int:
+    if weights is None:
+        return 0
+    assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == plan.T * plan.topk
+    return weights.data_ptr()
+
+
+def expert_gather(x: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """xs [T * topk, H]: row place[p] = (weights[p] *) x[p // topk]; rows past the last pair are zero."""
+    xp, ldx, T, H = _rows2d(x, "x")
+    if out is None:
+        out = torch.empty((plan.T * plan.topk, H), dtype=x.dtype, device=x.device)
+    op, ldo, r, c = _rows2d(out, "out")
+    assert T == plan.T and (r, c) == (T * plan.topk, H) and out.dtype == x.dtype
+    _check(lib().qmm_expert_gather(DTYPES[x.dtype], xp, ldx, T, plan.topk, H, plan.ptrs[0], plan.ptrs[1], _weights_ptr(weights, plan), op, ldo, _stream()))
+    return out
+
+
+def expert_combine(ys: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y [T, H] = sum over a token's pairs of (weights[p] *) ys[place[p]]."""
+    yp, ldys, P, H = _rows2d(ys, "ys")
+    if out is None:
+        out = torch.empty((plan.T, H), dtype=ys.dtype, device=ys.device)
+    op, ldo, r, c = _rows2d(out, "out")
+    assert P == plan.T * plan.topk and (r, c) == (plan.T, H) and out.dtype == ys.dtype
+    _check(lib().qmm_expert_combine(DTYPES[ys.dtype], yp, ldys, plan.T, plan.topk, H, plan.ptrs[1], _weights_ptr(weights, plan), op, ldo, _stream()))
+    return out
+
+
+def expert_combine_grad(dy: torch.Tensor, ys: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor, dys: torch.Tensor | None = None,
+                        dw: torch.Tensor | None = None):
+    """Gradients of expert_combine: (dys [T * topk, H], dw [T, topk] fp32)."""
+    dp, lddy, T, H = _rows2d(dy, "dy")
+    yp, ldys, P, H2 = _rows2d(ys, "ys")
+    if dys is None:
+        dys = torch.empty((P, H), dtype=dy.dtype, device=dy.device)
+    if dw is None:
+        dw = torch.empty((T, plan.topk), dtype=torch.float32, device=dy.device)
+    op, ldo, r, c = _rows2d(dys, "dys")
+    assert T == plan.T and P == T * plan.topk and H2 == H and (r, c) == (P, H) and ys.dtype == dy.dtype == dys.dtype
+    _check(lib().qmm_expert_combine_grad(DTYPES[dy.dtype], dp, lddy, yp, ldys, T, plan.topk, H, plan.ptrs[0], plan.ptrs[1],
+                                         _weights_ptr(weights, plan), op, ldo, _weights_ptr(dw, plan), _stream()))
+    return dys, dw
+
+
+def expert_gather_grad(dxs: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of expert_gather with respect to x: the sum over a token's pairs of (weights[p] *) dxs[place[p]]."""
+    return expert_combine(dxs, plan, weights, out)
+
+
+# ---- experts' products on microscaled operands
+
+def mx_experts_bytes(fmt: int, T: int, topk: int, E: int, K: int) -> int:
+    return lib().qmm_mx_experts_bytes(fmt, T, topk, E, K)
+
+
+def mx_quantize_experts(fmt: int, x: torch.Tensor, idx: torch.Tensor, plan: ExpertPlan, out: torch.Tensor | None = None,
+                        tensor_scale: torch.Tensor | None = None) -> torch.Tensor:
+    """x [T, K] quantised once per token and stored at the row of each of its pairs (rows grouped by expert)."""
+    xp, ldx, T, K = _rows2d(x, "x")
+    assert T == plan.T and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape == (T, plan.topk)
+    need = mx_experts_bytes(fmt, T, plan.topk, plan.E, K)
+    if out is None:
+        out = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(lib().qmm_mx_quantize_experts(fmt, DTYPES[x.dtype], xp, ldx, T, plan.topk, plan.E, K, idx.data_ptr(), plan.ptrs[1], plan.ptrs[2],
+                                         plan.ptrs[3], _scalar(tensor_scale), _operand(out, need, "out") if T else 0, _stream()))
+    return out
+
+
+def mx_experts_gate_up(fmt: int, a: torch.Tensor, plan: ExpertPlan, w_gate: torch.Tensor, w_up: torch.Tensor, N: int, K: int,
+                       h: torch.Tensor | None = None, a_scale=None, gate_scale=None, up_scale=None, h_scale=None, status=None) -> torch.Tensor:
+    """Packed rows [., K] -> packed rows [., N]: silu(W_gate[e] a) * (W_up[e] a), quantised from fp32."""
+    T, topk, E = plan.T, plan.topk, plan.E
+    each, need = E * mx_bytes(fmt, N, K), mx_experts_bytes(fmt, T, topk, E, N)
+    if h is None:
+        h = torch.empty(need, dtype=torch.uint8, device=a.device)
+    _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
+                                        _operand(w_gate, each, "w_gate"), _operand(w_up, each, "w_up"), N, K, _scalar(a_scale),
+                                        _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h"), _dp(status), _stream()))
+    return h
+
+
+def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor, N: int, K: int, Y: torch.Tensor | None = None,
+                    a_scale=None, w_scale=None, status=None, dtype: torch.dtype = torch.float16) -> torch.Tensor:
+    """Packed rows [., K] -> Y [T * topk, N] in sorted order: row r of expert e = W[e] a[r]."""
+    T, topk, E = plan.T, plan.topk, plan.E
+    if Y is None:
+        Y = torch.empty((T * topk, N), dtype=dtype, device=a.device)
+    yp, ldy, r, c = _rows2d(Y, "Y")
+    assert (r, c) == (T * topk, N)
+    _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
+                                     _operand(w, E * mx_bytes(fmt, N, K), "w"), N, K, _scalar(a_scale), _scalar(w_scale, E), DTYPES[Y.dtype],
+                                     yp, ldy, _dp(status), _stream()))
+    return Y
+
+
+def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int, out, x_scale=None, gate_scale=None, up_scale=None,
+                down_scale=None, h_scale=None) -> MxMoeArgs:
+    """Arguments of mx_moe_run: build once and reuse while the tensors stay where they are (the struct keeps them alive)."""
+    xp, ldx, T, H = _rows2d(X, "X")
+    op, ldo, r, c = _rows2d(out, "out")
+    topk = idx.shape[1]
+    assert idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape[0] == T
+    assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape == idx.shape
+    assert (r, c) == (T, H) and out.dtype == X.dtype
+    gu, dn = E * mx_bytes(fmt, I, H), E * mx_bytes(fmt, H, I)
+    a = MxMoeArgs(T, H, I, E, topk, fmt, DTYPES[X.dtype], xp, ldx, idx.data_ptr(), weights.data_ptr(), _operand(w_gate, gu, "w_gate"),
+                  _operand(w_up, gu, "w_up"), _operand(w_down, dn, "w_down"), _scalar(x_scale), _scalar(h_scale), _scalar(gate_scale, E),
+                  _scalar(up_scale, E), _scalar(down_scale, E), op, ldo)
+    a._keep = (X, idx, weights, w_gate, w_up, w_down, out, x_scale, gate_scale, up_scale, down_scale, h_scale)
+    return a
+
+
+def mx_moe_workspace_bytes(args: MxMoeArgs) -> int:
+    return lib().qmm_mx_moe_workspace_bytes(ctypes.byref(args))
+
+
+def mx_moe_run(args: MxMoeArgs, ws: torch.Tensor) -> None:
+    _check(lib().qmm_mx_moe(ctypes.byref(args), ws.data_ptr(), _nbytes(ws), _stream()))
+
+
+def mx_moe(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int, out=None, ws=None, **scales) -> torch.Tensor:
+    """A routed feed-forward layer in 4 bits: out [T, H] from X [T, H], idx / weights [T, topk] and E packed matrices of each kind
+    (scales: x_scale, h_scale, and [E] gate_scale, up_scale, down_scale for NVFP4)."""
+    if out is None:
+        out = torch.empty_like(X, memory_format=torch.contiguous_format)
+    args = mx_moe_args(fmt, X, idx, weights, w_gate, w_up, w_down, I, E, out, **scales)
+    if ws is None:
+        ws = _workspace(mx_moe_workspace_bytes(args), X.device, None)
+    mx_moe_run(args, ws)
+    return out
 
 
 def packed_check(fmt: int, packed: torch.Tensor, N: int, K: int, ws: torch.Tensor) -> None:
