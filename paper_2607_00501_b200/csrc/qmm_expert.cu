@@ -3,6 +3,7 @@
 // so that a token's row is read once however many experts it goes to.
 #include "qmm_mx.cuh"
 
+#include <atomic>
 #include <type_traits>
 
 namespace qmm {
@@ -10,18 +11,25 @@ namespace qmm {
 using namespace mx;
 
 template <typename... P, typename... A>
-static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, size_t smem, cudaStream_t st, const char* what, A... args)
+static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const char* what, A... args)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
     cfg.numAttrs = 1;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = (unsigned)cluster;
+        attr[1].val.clusterDim.y = 1;
+        attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    cfg.attrs = attr;
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, args...), what);
 }
 
@@ -29,8 +37,9 @@ static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, size_t 
 
 constexpr int kSortThreads = 1024;
 constexpr int kSortWarps = kSortThreads / 32;
-constexpr int kSortChunkItems = 4;                         // pairs per thread when several blocks share the work
-constexpr int kSortOneBlock = 8 * kSortThreads;            // up to here one block does everything (one launch)
+constexpr int kSortCluster = 16;                           // blocks of the one-launch form beyond a block's worth of pairs (a non-portable cluster)
+constexpr int kSortOneLaunch = 8 * kSortThreads * kSortCluster;   // up to here (131072 pairs) one launch does everything
+constexpr int kSortChunkItems = 4;                         // pairs per thread of the two-launch form
 
 // Expert of pair p; anything outside [0, E) and pairs past the end of the chunk's data map to the last bucket E
 // (dropped) and E + 1 (nothing).
@@ -57,31 +66,39 @@ __global__ void __launch_bounds__(kSortThreads) expert_count_kernel(const int* _
     for (int e = threadIdx.x; e <= E; e += kSortThreads) counts[(int64_t)blockIdx.x * (E + 1) + e] = hist[e];
 }
 
-// Places of the pairs of one chunk.  A warp takes ITEMS * 32 consecutive pairs, 32 at a time: lanes with the same bucket find
-// one another (match_any) and rank themselves by lane, the bucket's running count of this warp gives the rest.
-// With `chunks` > 1 the rows before this chunk and the totals come from `counts`; else this block is all there is.
+// Places of the pairs of one block's chunk.  A warp takes ITEMS * 32 consecutive pairs, 32 at a time: lanes with the same
+// bucket find one another (one ballot per bit of the bucket's number; a match instruction took three times as long) and rank
+// themselves by lane, the bucket's running count of this warp gives the rest.
+// The rows before this chunk and the totals come from the other blocks of the cluster, through distributed shared memory
+// (CLUSTER: the whole sort is one launch of up to sixteen blocks), or from `counts` (many chunks).
 // Dynamic shared memory: [kSortWarps][E + 2] running counts.
-template <int ITEMS>
+template <int ITEMS, bool CLUSTER>
 __global__ void __launch_bounds__(kSortThreads)
 expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, const int* __restrict__ counts, int* __restrict__ order,
                     int* __restrict__ place, int* __restrict__ offsets, int* __restrict__ units)
 {
     pdl_launch_dependents();
-    pdl_wait();
     extern __shared__ int run[];
-    __shared__ int base[1026];                             // first row of each bucket's pairs of this chunk
-    __shared__ int s_rows[kSortWarps], s_units[kSortWarps];
+    __shared__ int base[1026];                             // this chunk's rows per bucket, then the first row of each
+    __shared__ int local[ITEMS > 1 ? 1026 : 1];            // first place of each bucket's pairs inside the chunk
+    __shared__ int s_rows[kSortWarps], s_units[kSortWarps], s_local[kSortWarps];
     const int B = E + 2, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int i = threadIdx.x; i < kSortWarps * B; i += kSortThreads) run[i] = 0;
-    __syncthreads();
+    pdl_wait();
     const int64_t p0 = (int64_t)blockIdx.x * (kSortThreads * ITEMS) + (int64_t)warp * (32 * ITEMS);
     int bucket[ITEMS], rank[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) bucket[i] = bucket_of(idx, p0 + i * 32 + lane, P, E);
+    __syncthreads();
     int* mine = run + warp * B;
+    const int bits = 32 - __clz(E + 1);
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        const unsigned same = __match_any_sync(0xFFFFFFFFu, bucket[i]);
+        unsigned same = 0xFFFFFFFFu;                       // lanes with this lane's bucket: agreement in every bit of its number
+        for (int b = 0; b < bits; ++b) {
+            const unsigned ones = __ballot_sync(0xFFFFFFFFu, (bucket[i] >> b) & 1);
+            same &= (bucket[i] >> b) & 1 ? ones : ~ones;
+        }
         const int before = __popc(same & ((1u << lane) - 1u));
         rank[i] = mine[bucket[i]] + before;
         __syncwarp();
@@ -89,70 +106,100 @@ expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, c
         __syncwarp();
     }
     __syncthreads();
-    // counts of the warps -> rows of the bucket before each warp; totals over this chunk or over all of them
+    // counts of the warps -> rows of the bucket before each warp (thread e: expert e; the last thread: the dropped pairs)
     const int e = threadIdx.x;
+    auto over_warps = [&](int bkt) {
+        int c[kSortWarps], sum = 0;
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) c[w] = run[w * B + bkt];
+#pragma unroll
+        for (int w = 0; w < kSortWarps; ++w) {
+            run[w * B + bkt] = sum;
+            sum += c[w];
+        }
+        return sum;
+    };
     int total = 0, before_chunk = 0, dropped_before = 0;
-    if (e < E) {
-        int sum = 0;
-        for (int w = 0; w < kSortWarps; ++w) {
-            const int c = run[w * B + e];
-            run[w * B + e] = sum;
-            sum += c;
-        }
-        total = sum;
-        if (chunks > 1) {
-            total = 0;
-            for (int c = 0; c < chunks; ++c) {
-                const int v = counts[(int64_t)c * (E + 1) + e];
-                total += v;
-                if (c < (int)blockIdx.x) before_chunk += v;
+    if (e < E) base[e] = total = over_warps(e);
+    const int in_chunk = total;
+    if (threadIdx.x == kSortThreads - 1) base[E] = over_warps(E);
+    if (CLUSTER && chunks > 1) {
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+        auto others = [&](int bkt, int& before) {
+            int v[kSortCluster], all = 0;
+            const uint32_t at = (uint32_t)__cvta_generic_to_shared(&base[bkt]);
+#pragma unroll
+            for (int c = 0; c < kSortCluster; ++c) {
+                uint32_t remote;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(at), "r"(c));
+                asm volatile("ld.shared::cluster.b32 %0, [%1];" : "=r"(v[c]) : "r"(remote) : "memory");
             }
-        }
+#pragma unroll
+            for (int c = 0; c < kSortCluster; ++c) {
+                all += v[c];
+                if (c < (int)blockIdx.x) before += v[c];
+            }
+            return all;
+        };
+        if (e < E) total = others(e, before_chunk);
+        if (threadIdx.x == kSortThreads - 1) others(E, dropped_before);
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // base[] is overwritten below
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    } else if (!CLUSTER) {
+        auto others = [&](int bkt, int& before) {
+            int all = 0;
+#pragma unroll 8
+            for (int c = 0; c < chunks; ++c) {
+                const int v = __ldg(counts + (int64_t)c * (E + 1) + bkt);
+                all += v;
+                before += c < (int)blockIdx.x ? v : 0;
+            }
+            return all;
+        };
+        if (e < E) total = others(e, before_chunk);
+        if (threadIdx.x == kSortThreads - 1) others(E, dropped_before);
     }
-    if (threadIdx.x == kSortThreads - 1) {                 // the dropped pairs' bucket
-        int sum = 0;
-        for (int w = 0; w < kSortWarps; ++w) {
-            const int c = run[w * B + E];
-            run[w * B + E] = sum;
-            sum += c;
-        }
-        if (chunks > 1)
-            for (int c = 0; c < (int)blockIdx.x; ++c) dropped_before += counts[(int64_t)c * (E + 1) + E];
-    }
-    // exclusive scans over the experts of rows and of 128-row units
+    // exclusive scans over the experts of rows, of 128-row units and of this chunk's pairs
     const int nu = (total + 127) >> 7;
-    int rows = total, us = nu;
+    int rows = total, us = nu, ls = in_chunk;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int r = __shfl_up_sync(0xFFFFFFFFu, rows, o), u = __shfl_up_sync(0xFFFFFFFFu, us, o);
+        const int r = __shfl_up_sync(0xFFFFFFFFu, rows, o), u = __shfl_up_sync(0xFFFFFFFFu, us, o), l = __shfl_up_sync(0xFFFFFFFFu, ls, o);
         if (lane >= o) {
             rows += r;
             us += u;
+            ls += l;
         }
     }
     if (lane == 31) {
         s_rows[warp] = rows;
         s_units[warp] = us;
+        s_local[warp] = ls;
     }
     __syncthreads();
     if (warp == 0) {
-        int r = s_rows[lane], u = s_units[lane];
+        int r = s_rows[lane], u = s_units[lane], l = s_local[lane];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int r2 = __shfl_up_sync(0xFFFFFFFFu, r, o), u2 = __shfl_up_sync(0xFFFFFFFFu, u, o);
+            const int r2 = __shfl_up_sync(0xFFFFFFFFu, r, o), u2 = __shfl_up_sync(0xFFFFFFFFu, u, o), l2 = __shfl_up_sync(0xFFFFFFFFu, l, o);
             if (lane >= o) {
                 r += r2;
                 u += u2;
+                l += l2;
             }
         }
         s_rows[lane] = r;
         s_units[lane] = u;
+        s_local[lane] = l;
     }
     __syncthreads();
     rows += (warp ? s_rows[warp - 1] : 0) - total;
     us += (warp ? s_units[warp - 1] : 0) - nu;
+    ls += (warp ? s_local[warp - 1] : 0) - in_chunk;
     if (e < E) {
         base[e] = rows + before_chunk;
+        if (ITEMS > 1) local[e] = ls;
         if (blockIdx.x == 0) {
             offsets[e] = rows;
             units[e] = us;
@@ -162,41 +209,78 @@ expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, c
             }
         }
     }
-    if (threadIdx.x == kSortThreads - 1) base[E] = s_rows[kSortWarps - 1] + dropped_before;      // dropped pairs: past the last row
+    if (threadIdx.x == kSortThreads - 1) {
+        base[E] = s_rows[kSortWarps - 1] + dropped_before;  // dropped pairs: past the last row
+        if (ITEMS > 1) local[E] = s_local[kSortWarps - 1];
+    }
     __syncthreads();
+    // place[] is written in pair order.  order[] is written in row order: the chunk's pairs are sorted in shared memory first,
+    // so that a bucket's run is one contiguous store (65536 pairs: 12.9 us against 14.1 with scattered stores).
+    // (One pair per thread: too few for that to pay.)
+    int2* sorted = reinterpret_cast<int2*>(run + ((kSortWarps * B + 1) & ~1));
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int64_t p = p0 + i * 32 + lane;
         if (p >= P) continue;
-        const int row = base[bucket[i]] + mine[bucket[i]] + rank[i];
+        const int in_bucket = mine[bucket[i]] + rank[i], row = base[bucket[i]] + in_bucket;
         const bool kept = bucket[i] < E;
         place[p] = kept ? row : -1;
-        order[row] = kept ? (int)p : -1;
+        if (ITEMS > 1) sorted[local[bucket[i]] + in_bucket] = make_int2(row, kept ? (int)p : -1);
+        else order[row] = kept ? (int)p : -1;
+    }
+    if (ITEMS > 1) {
+        __syncthreads();
+        const int64_t left = P - (int64_t)blockIdx.x * (kSortThreads * ITEMS);
+        const int n = (int)(left < kSortThreads * ITEMS ? left : kSortThreads * ITEMS);
+        for (int q = threadIdx.x; q < n; q += kSortThreads) order[sorted[q].x] = sorted[q].y;
     }
 }
 
-static int sort_chunks(int64_t P) { return P <= kSortOneBlock ? 1 : (int)((P + kSortThreads * kSortChunkItems - 1) / (kSortThreads * kSortChunkItems)); }
+static int sort_chunks(int64_t P) { return (int)((P + kSortThreads * kSortChunkItems - 1) / (kSortThreads * kSortChunkItems)); }
 
-size_t expert_sort_workspace_bytes(int64_t P, int E) { return P <= kSortOneBlock ? 0 : (size_t)sort_chunks(P) * (size_t)(E + 1) * 4; }
+size_t expert_sort_workspace_bytes(int64_t P, int E) { return P <= kSortOneLaunch ? 0 : (size_t)sort_chunks(P) * (size_t)(E + 1) * 4; }
+
+struct SortArgs {
+    const int* idx;
+    int64_t P;
+    int E;
+    int *order, *place, *offsets, *units;
+    const int* counts;
+};
+template <int ITEMS, bool CLUSTER> static qmm_status launch_place(const SortArgs& a, int chunks, cudaStream_t st)
+{
+    auto kern = expert_place_kernel<ITEMS, CLUSTER>;
+    auto smem_of = [](int E) { return (size_t)((kSortWarps * (E + 2) + 1) & ~1) * 4 + (ITEMS > 1 ? (size_t)ITEMS * kSortThreads * 8 : 0); };
+    static std::atomic<uint64_t> configured{0};            // devices that have the attributes
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
+    const uint64_t bit = dev < 64 ? (1ull << dev) : 0;
+    if (!(configured.load(std::memory_order_relaxed) & bit)) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_of(1024));
+        if (e == cudaSuccess && CLUSTER) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return check_cuda(e, "expert sort attributes");
+        configured.fetch_or(bit, std::memory_order_relaxed);
+    }
+    return launch_pdl(kern, dim3(chunks), kSortThreads, smem_of(a.E), CLUSTER ? chunks : 1, st, "expert sort launch", a.idx, a.P, a.E, chunks, a.counts, a.order,
+                      a.place, a.offsets, a.units);
+}
 
 qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int* place, int* offsets, int* units, void* ws, cudaStream_t st)
 {
-    const size_t smem = (size_t)kSortWarps * (E + 2) * 4;
-    const int chunks = sort_chunks(P);
-    auto go = [&](auto kern) -> qmm_status {
-        if (smem > 40 * 1024) {                            // E > 318: beyond the default dynamic shared memory beside the static arrays
-            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return check_cuda(e, "expert sort shared memory size");
-        }
-        return launch_pdl(kern, dim3(chunks), kSortThreads, smem, st, "expert sort launch", idx, P, E, chunks, (const int*)ws, order, place, offsets, units);
-    };
-    if (chunks > 1) {
-        const qmm_status s = launch_pdl(expert_count_kernel, dim3(chunks), kSortThreads, 0, st, "expert count launch", idx, P, E, (int*)ws);
+    const SortArgs a = {idx, P, E, order, place, offsets, units, (const int*)ws};
+    if (P > kSortOneLaunch) {
+        const int chunks = sort_chunks(P);
+        const qmm_status s = launch_pdl(expert_count_kernel, dim3(chunks), kSortThreads, 0, 1, st, "expert count launch", idx, P, E, (int*)ws);
         if (s != QMM_OK) return s;
-        return go(expert_place_kernel<kSortChunkItems>);
+        return launch_place<kSortChunkItems, false>(a, chunks, st);
     }
-    if (P <= kSortThreads) return go(expert_place_kernel<1>);
-    return go(expert_place_kernel<8>);
+    if (P <= kSortThreads) return launch_place<1, true>(a, 1, st);
+    // sixteen blocks, as few pairs per thread as that allows (65536 pairs: 9.2 us, against 12.9 with 8 blocks)
+    const int64_t items = (P + kSortThreads * kSortCluster - 1) / (kSortThreads * kSortCluster);
+    if (items <= 1) return launch_place<1, true>(a, kSortCluster, st);
+    if (items <= 2) return launch_place<2, true>(a, kSortCluster, st);
+    if (items <= 4) return launch_place<4, true>(a, kSortCluster, st);
+    return launch_place<8, true>(a, kSortCluster, st);
 }
 
 // ------------------------------------------------------------- row moves
@@ -204,61 +288,67 @@ qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int*
 constexpr int kMoveThreads = 256;
 
 // One vector of V elements of a row: V * sizeof(T) = 16 bytes, 4 bytes, or a single element, as the rows' alignment allows.
-template <typename T, int V> struct Vec {
-    float f[V];
+// Raw<T, V> is the vector as loaded: several of them in flight cost half the registers of their fp32 form.
+template <typename T, int V> struct Raw {
+    static constexpr int B = V * (int)sizeof(T);
+    static constexpr int W = B >= 4 ? B / 4 : 1;
+    uint32_t u[W];
     __device__ __forceinline__ void load(const T* p)
     {
-        constexpr int B = V * (int)sizeof(T);
         if constexpr (B == 16) {
-            const uint4 u = __ldg(reinterpret_cast<const uint4*>(p));
-            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-            unpack(w);
-        } else if constexpr (B == 4 && sizeof(T) == 2) {
-            const uint32_t w[1] = {__ldg(reinterpret_cast<const uint32_t*>(p))};
-            unpack(w);
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(p));
+            u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
+        } else if constexpr (B == 4) {
+            u[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
         } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) f[i] = Dt<T>::up(p[i]);
-        }
-    }
-    template <int W> __device__ __forceinline__ void unpack(const uint32_t (&w)[W])
-    {
-#pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (sizeof(T) == 2) {
-                const float2 v = Dt<T>::up2(w[i]);
-                f[2 * i] = v.x, f[2 * i + 1] = v.y;
-            } else {
-                f[i] = __uint_as_float(w[i]);
-            }
+            u[0] = __ldg(reinterpret_cast<const unsigned short*>(p));
         }
     }
     __device__ __forceinline__ void store(T* p) const
     {
-        constexpr int B = V * (int)sizeof(T);
-        if constexpr (B == 16) {
-            uint32_t w[4];
+        if constexpr (B == 16) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        else if constexpr (B == 4) *reinterpret_cast<uint32_t*>(p) = u[0];
+        else *reinterpret_cast<unsigned short*>(p) = (unsigned short)u[0];
+    }
+    __device__ __forceinline__ void zero()
+    {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(T) == 2) w[i] = Dt<T>::down2(f[2 * i], f[2 * i + 1]);
-                else w[i] = __float_as_uint(f[i]);
-            }
-            *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-        } else if constexpr (B == 4 && sizeof(T) == 2) {
-            *reinterpret_cast<uint32_t*>(p) = Dt<T>::down2(f[0], f[1]);
+        for (int i = 0; i < W; ++i) u[i] = 0u;
+    }
+    __device__ __forceinline__ float get(int i) const                          // element i as fp32 (i a constant once unrolled)
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(u[i]);
         } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) p[i] = Dt<T>::down(f[i]);
+            const float2 f = Dt<T>::up2(u[i >> 1]);
+            return i & 1 ? f.y : f.x;
         }
     }
-    __device__ __forceinline__ Vec scaled(float s) const
+};
+template <typename T, int V> struct Vec {
+    float f[V];
+    __device__ __forceinline__ Raw<T, V> raw() const
     {
-        Vec r;
+        Raw<T, V> r;
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) r.f[i] = f[i] * s;
+            for (int i = 0; i < V; ++i) r.u[i] = __float_as_uint(f[i]);
+        } else if constexpr (V == 1) {
+            r.u[0] = Dt<T>::down2(f[0], 0.0f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) r.u[i] = Dt<T>::down2(f[2 * i], f[2 * i + 1]);
+        }
         return r;
     }
 };
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> scaled(const Raw<T, V>& x, float s)
+{
+    Vec<T, V> v;
+#pragma unroll
+    for (int i = 0; i < V; ++i) v.f[i] = x.get(i) * s;
+    return v.raw();
+}
 
 // Thread = one vector of one token's row: read once, written at the row of each of the token's pairs.  The rows past the
 // last (one per dropped pair) are dealt to the tokens by index and zeroed.
@@ -273,21 +363,17 @@ expert_gather_kernel(const T* __restrict__ x, int64_t ldx, int tokens, int topk,
     const int64_t t = id / nv;
     if (t >= tokens) return;
     const int64_t h = (id - t * nv) * V;
-    Vec<T, V> v;
+    Raw<T, V> v, z;
     v.load(x + t * ldx + h);
+    z.zero();
     for (int j = 0; j < topk; ++j) {
         const int64_t p = t * topk + j;
         const int r = __ldg(place + p);
         if (r >= 0) {
-            if (weights) v.scaled(__ldg(weights + p)).store(xs + r * ldxs + h);
+            if (weights) scaled(v, __ldg(weights + p)).store(xs + r * ldxs + h);
             else v.store(xs + r * ldxs + h);
         }
-        if (__ldg(order + p) < 0) {
-            Vec<T, V> z;
-#pragma unroll
-            for (int i = 0; i < V; ++i) z.f[i] = 0.0f;
-            z.store(xs + p * ldxs + h);
-        }
+        if (__ldg(order + p) < 0) z.store(xs + p * ldxs + h);
     }
 }
 
@@ -307,7 +393,7 @@ expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int to
 #pragma unroll
     for (int i = 0; i < V; ++i) acc.f[i] = 0.0f;
     for (int j0 = 0; j0 < topk; j0 += 8) {
-        Vec<T, V> v[8];
+        Raw<T, V> v[8];
         float w[8];
         int r[8];
 #pragma unroll
@@ -316,16 +402,15 @@ expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int to
             w[j] = r[j] >= 0 && weights ? __ldg(weights + t * topk + j0 + j) : 1.0f;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (r[j] >= 0) v[j].load(ys + r[j] * ldys + h);
+        for (int j = 0; j < 8; ++j) v[j].load(ys + max(r[j], 0) * ldys + h);   // no branch around a load: all are in flight together (row 0 stands in)
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (r[j] >= 0) {
+        for (int j = 0; j < 8; ++j) {
+            const bool kept = r[j] >= 0;
 #pragma unroll
-                for (int i = 0; i < V; ++i) acc.f[i] = fmaf(w[j], v[j].f[i], acc.f[i]);
-            }
+            for (int i = 0; i < V; ++i) acc.f[i] = kept ? fmaf(w[j], v[j].get(i), acc.f[i]) : acc.f[i];
+        }
     }
-    acc.store(y + t * ldy + h);
+    acc.raw().store(y + t * ldy + h);
 }
 
 // Block = one token: its row of dy against the rows of its pairs, eight pairs at a time.  A pair's dot product is
@@ -353,17 +438,16 @@ expert_combine_grad_kernel(const T* __restrict__ dy, int64_t lddy, const T* __re
         }
         for (int i = threadIdx.x; i < nv; i += blockDim.x) {
             const int64_t h = (int64_t)i * V;
-            Vec<T, V> d, v[8];
+            Raw<T, V> d, v[8];
             d.load(dy + t * lddy + h);
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (r[j] >= 0) v[j].load(ys + r[j] * ldys + h);
+            for (int j = 0; j < 8; ++j) v[j].load(ys + max(r[j], 0) * ldys + h);   // no branch around a load (row 0 stands in)
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (r[j] >= 0) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) dot[j] = fmaf(d.f[k], v[j].f[k], dot[j]);
-                    d.scaled(w[j]).store(dys + r[j] * lddys + h);
+                    for (int k = 0; k < V; ++k) dot[j] = fmaf(d.get(k), v[j].get(k), dot[j]);
+                    scaled(d, w[j]).store(dys + r[j] * lddys + h);
                 }
         }
 #pragma unroll
@@ -383,9 +467,8 @@ expert_combine_grad_kernel(const T* __restrict__ dy, int64_t lddy, const T* __re
     for (int j = 0; j < topk; ++j) {                       // rows past the last, as in the gather
         const int64_t row = t * topk + j;
         if (__ldg(order + row) >= 0) continue;
-        Vec<T, V> z;
-#pragma unroll
-        for (int i = 0; i < V; ++i) z.f[i] = 0.0f;
+        Raw<T, V> z;
+        z.zero();
         for (int i = threadIdx.x; i < nv; i += blockDim.x) z.store(dys + row * lddys + (int64_t)i * V);
     }
 }
@@ -429,7 +512,7 @@ qmm_status launch_expert_gather(int dtype, const void* x, int64_t ldx, int T, in
     if (s != QMM_OK) return s;
     return by_type(dtype, V, [&](auto type, auto v) {
         using D = decltype(type);
-        return launch_pdl(expert_gather_kernel<D, decltype(v)::value>, grid, kMoveThreads, 0, st, "expert gather launch", (const D*)x, ldx, T, topk, nv, order, place,
+        return launch_pdl(expert_gather_kernel<D, decltype(v)::value>, grid, kMoveThreads, 0, 1, st, "expert gather launch", (const D*)x, ldx, T, topk, nv, order, place,
                           weights, (D*)xs, ldxs);
     });
 }
@@ -444,7 +527,7 @@ qmm_status launch_expert_combine(int dtype, const void* ys, int64_t ldys, int T,
     if (s != QMM_OK) return s;
     return by_type(dtype, V, [&](auto type, auto v) {
         using D = decltype(type);
-        return launch_pdl(expert_combine_kernel<D, decltype(v)::value>, grid, kMoveThreads, 0, st, "expert combine launch", (const D*)ys, ldys, T, topk, nv, place,
+        return launch_pdl(expert_combine_kernel<D, decltype(v)::value>, grid, kMoveThreads, 0, 1, st, "expert combine launch", (const D*)ys, ldys, T, topk, nv, place,
                           weights, (D*)y, ldy);
     });
 }
@@ -457,7 +540,7 @@ qmm_status launch_expert_combine_grad(int dtype, const void* dy, int64_t lddy, c
     const int threads = nv <= 64 ? 64 : nv <= 128 ? 128 : kMoveThreads;
     return by_type(dtype, V, [&](auto type, auto v) {
         using D = decltype(type);
-        return launch_pdl(expert_combine_grad_kernel<D, decltype(v)::value>, dim3((unsigned)T), threads, 0, st, "expert combine gradient launch", (const D*)dy, lddy,
+        return launch_pdl(expert_combine_grad_kernel<D, decltype(v)::value>, dim3((unsigned)T), threads, 0, 1, st, "expert combine gradient launch", (const D*)dy, lddy,
                           (const D*)ys, ldys, topk, nv, order, place, weights, (D*)dys, lddys, dw);
     });
 }

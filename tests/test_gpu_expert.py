@@ -39,7 +39,7 @@ def check_plan(plan, idx, E):
 
 @pytest.mark.parametrize("kind", ["uniform", "dropped", "one", "none", "skewed"])
 @pytest.mark.parametrize("T,topk,E", [(1, 1, 1), (1, 8, 128), (4, 8, 128), (31, 1, 3), (512, 2, 16), (513, 2, 318), (1024, 8, 128), (8193, 1, 1024),
-                                      (3000, 3, 319), (20000, 6, 160), (40, 32, 1024)])
+                                      (3000, 3, 319), (8192, 8, 128), (20000, 6, 160), (40, 32, 1024), (50000, 4, 500)])
 def test_sort(qmm, kind, T, topk, E):
     idx = routing(T, topk, E, kind, T + E)
     plan = qmm.expert_sort(torch.from_numpy(idx).cuda(), E)

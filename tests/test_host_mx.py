@@ -33,7 +33,7 @@ def test_sizes(L):
         most = max(sum(-(-c // 128) for c in counts) for counts in
                    ([1] * min(E, P) + [], [P - min(E, P) + 1] + [1] * (min(E, P) - 1), [129] * min(E, P // 129), [P]) if sum(counts) <= P)
         assert qmm.mx_experts_bytes(32, T, topk, E, 256) >= most * u
-    assert L.qmm_expert_sort_workspace_bytes(1024, 8, 128) == 0 and L.qmm_expert_sort_workspace_bytes(1025, 8, 128) > 0
+    assert L.qmm_expert_sort_workspace_bytes(16384, 8, 128) == 0 and L.qmm_expert_sort_workspace_bytes(16385, 8, 128) > 0
     assert L.qmm_expert_sort_workspace_bytes(1, 33, 128) == 0 and L.qmm_expert_sort_workspace_bytes(-1, 1, 1) == 0
 
 
@@ -74,7 +74,7 @@ def test_refusals_of_the_expert_calls(L, a):
     assert L.qmm_expert_sort(None, 4, 2, 8, a, a, a, a, None, 0, None) == 1
     assert L.qmm_expert_sort(a, 4, 2, 8, a, a, None, a, None, 0, None) == 1
     assert L.qmm_expert_sort(a + 2, 4, 2, 8, a, a, a, a, None, 0, None) == 3
-    assert L.qmm_expert_sort(a, 8193, 1, 8, a, a, a, a, None, 0, None) == 4
+    assert L.qmm_expert_sort(a, 131073, 1, 8, a, a, a, a, None, 0, None) == 4
     assert L.qmm_expert_gather(0, a, 63, 4, 2, 64, a, a, None, a, 64, None) == 2
     assert L.qmm_expert_gather(0, a, 64, 4, 2, 0, a, a, None, a, 64, None) == 1
     assert L.qmm_expert_gather(9, a, 64, 4, 2, 64, a, a, None, a, 64, None) == 1
