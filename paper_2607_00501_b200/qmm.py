@@ -110,6 +110,8 @@ class MxMoeArgs(ctypes.Structure):
 def lib() -> ctypes.CDLL:
     """Load libqmm.so (building it with nvcc first if it is not there)."""
     global _lib
+    if _lib is not None:
+        return _lib
     with _lock:
         if _lib is None:
             if not os.path.exists(LIB_PATH):
@@ -186,8 +188,14 @@ def _check(status: int):
         raise QmmError(status, last_error())
 
 
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    """Handle of the current stream of the current device (without a Stream object: 0.3 us instead of 3.3 us per call)."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(torch.cuda.current_device())
 
 
 def _dp(t):
