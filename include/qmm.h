@@ -555,6 +555,7 @@ qmm_status qmm_status_check(void* ws, void* stream);
  *   "gemm_no_tail_cut" "1"             last, partly filled round of tiles left whole
  *   "gemm_no_small"    "1"             M <= 8 through the tensor-core kernel, not the few-token kernel
  *   "moe_no_fuse"      "1"             decode-sized qmm_moe as separate route / product / combine launches
+ *   "mx_pair"          "1" | "2"       microscaled products of more than 128 tokens on pairs of SMs: always | never
  */
 qmm_status qmm_debug_config(const char* name, const char* value);
 

@@ -392,6 +392,12 @@ qmm_status qmm_debug_config(const char* name, const char* value)
         g_knobs.gemm_units = got == 2 ? u : 0;
         return QMM_OK;
     }
+    if (strcmp(name, "mx_pair") == 0) {
+        if (!off && strcmp(value, "1") != 0 && strcmp(value, "2") != 0)
+            return fail(QMM_ERR_INVALID_ARG, "qmm_debug_config: mx_pair wants \"1\" (always) or \"2\" (never)");
+        g_knobs.mx_pair = off ? 0 : value[0] - '0';
+        return QMM_OK;
+    }
     int* flag = strcmp(name, "gemv_no_cluster") == 0    ? &g_knobs.gemv_no_cluster
                 : strcmp(name, "gemm_no_tail_cut") == 0 ? &g_knobs.gemm_no_tail_cut
                 : strcmp(name, "gemm_no_small") == 0    ? &g_knobs.gemm_no_small

@@ -104,6 +104,7 @@ struct DebugKnobs {
     int gemm_no_tail_cut;           // leave the tiles of the last, partly filled round whole
     int gemm_no_small;              // M <= 8 through the tensor-core prefill kernel instead of the few-token kernel
     int moe_no_fuse;                // decode-sized MoE layers as four separate launches
+    int mx_pair;                    // microscaled product on pairs of SMs: 1 whenever it can run, 2 never; 0: the plan
 };
 extern DebugKnobs g_knobs;
 

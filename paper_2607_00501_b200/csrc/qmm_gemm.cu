@@ -45,6 +45,22 @@ qmm_status make_x_map(CUtensorMap* map, const uint16_t* X, int64_t rows, int64_t
     return QMM_OK;
 }
 
+// A packed microscaled operand as rows of 128 bytes, read in boxes of box_rows whole rows (plain copies: the packed form is
+// already in the order of shared memory).
+qmm_status make_unit_map(CUtensorMap* map, const void* packed, int64_t rows128, int box_rows)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return fail(QMM_ERR_CUDA, "cuTensorMapEncodeTiled is not available from this driver");
+    const cuuint64_t gdim[2] = {128, (cuuint64_t)rows128};
+    const cuuint64_t gstride[1] = {128};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(packed), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) return fail(QMM_ERR_CUDA, "cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return QMM_OK;
+}
+
 template <int FMT, int BN, int NA, int EPI, bool DENSE>
 static qmm_status launch_t(const CUtensorMap& map, const GemmParams& p, dim3 grid, cudaStream_t st)
 {

@@ -28,6 +28,7 @@
 #include "qmm_tc.cuh"
 
 #include <atomic>
+#include <cuda.h>
 
 namespace qmm {
 
@@ -48,7 +49,7 @@ struct MxGemmParams {
     const float* h_scale;            // gate/up: tensor scale of the output operand
     void* y;                         // [rows, ldy], or the packed output operand (gate/up)
     int64_t ldy;
-    int vec;                         // 16-byte stores of Y are aligned
+    int vec;                         // widest aligned store of Y: 32, 16 or 0 (element by element)
     int* status;
 };
 
@@ -85,19 +86,32 @@ struct MxWork {
 
 __device__ __forceinline__ float silu_f32(float g) { return __fdividef(g, 1.0f + __expf(-g)); }
 
-// 32 consecutive outputs of one row; n = how many exist.
-template <typename T> __device__ __forceinline__ void store32(T* o, const float (&v)[32], int n, bool vec)
+// 32 consecutive outputs of one row; n = how many exist.  vec: widest store (bytes) that the rows' alignment allows; 32-byte
+// stores write whole sectors (a lane's neighbours in a store are other rows).
+__device__ __forceinline__ void st_global_256(void* p, const uint32_t* u)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]),
+                 "r"(u[6]), "r"(u[7])
+                 : "memory");
+}
+template <typename T> __device__ __forceinline__ void store32(T* o, const float (&v)[32], int n, int vec)
 {
     if (vec && n >= 32) {
+        constexpr int W = 8 * (int)sizeof(T);
+        uint32_t u[W];
         if constexpr (sizeof(T) == 2) {
-            uint32_t u[16];
 #pragma unroll
             for (int i = 0; i < 16; ++i) u[i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
         } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(o)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i]);
+        }
+        if (vec == 32) {
+#pragma unroll
+            for (int i = 0; i < W / 8; ++i) st_global_256(reinterpret_cast<uint8_t*>(o) + 32 * i, u + 8 * i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i) reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
         }
         return;
     }
@@ -423,7 +437,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, NB, GATEUP>::kThreads, 1) mx_gemm_
                             float f[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) f[i] = alpha * __uint_as_float(v[i]);
-                            store32<T>(reinterpret_cast<T*>(p.y) + (int64_t)(w.row0 + r) * p.ldy + n0, f, p.N - n0, p.vec != 0);
+                            store32<T>(reinterpret_cast<T*>(p.y) + (int64_t)(w.row0 + r) * p.ldy + n0, f, p.N - n0, p.vec);
                         }
                     }
                 }
@@ -480,6 +494,225 @@ __global__ void __launch_bounds__(MxGeom<FMT, NB, GATEUP>::kThreads, 1) mx_gemm_
     }
 }
 
+// ------------------------------------------------------------ many tokens: pairs of SMs
+
+// 256 x 256 tiles by two blocks on neighbouring SMs (cta_group::2).  A block holds 128 of the tile's token rows and half
+// of its weight rows; the pair's MMA (M = 256, N = 256) reads each half of the weights from the block that has it, so a
+// K step moves 16 KB + 16 KB of codes per SM for 512 cycles of tensor pipe -- half the L2 and shared-memory traffic
+// per flop of the 128 x 128 tile of one SM, which that traffic bounds at less than half of the tensor rate.
+// Every block keeps the scales of its own token rows and of all 256 weight rows in tensor memory.
+//
+// The first block's MMA warp issues for both.  The loads of both blocks complete on the first block's barrier, which tiled TMA
+// loads of a pair can do and plain bulk copies cannot (with bulk copies and a warp of the second block passing completions on,
+// the ring's round trip bounded the kernel at 40 % of this form).  tcgen05.commit frees ring slots and hands over the
+// accumulators in both blocks.  Tensor memory holds one 256-column accumulator beside two sets of scale columns: eight epilogue
+// warps take it into registers at once (128 columns each), free it, and store while the next tile's MMAs run.
+template <int FMT> struct MxPairGeom {
+    static constexpr int kSc = scale_bytes(FMT);
+    static constexpr int kA = 0, kB = unit_bytes(FMT), kSb = kB + kCodeBytes;              // A unit | B codes | scales of both B units
+    static constexpr int kStage = kSb + 2 * kSc;
+    static constexpr int kFit = (227 * 1024 - 2048) / kStage;
+    static constexpr int kStages = kFit < 6 ? kFit : 6;
+    static constexpr int kSmem = 2048 + kStages * kStage;
+    static constexpr int kGroups = kUnitK / FMT / 4;
+    static constexpr int kSf0 = 256, kSfCols = kGroups * 12;
+    static constexpr int kThreads = 12 * 32;
+    static_assert(kSf0 + 2 * kSfCols <= 512 && kStages >= 4, "tensor memory or shared memory over-subscribed");
+};
+
+struct MxPairMaps {
+    CUtensorMap a, w_codes, w_scales;                                         // boxes: a unit | a unit's codes | its scales
+};
+
+// Tile t of the pair form: token tiles in groups of eight, inside a group token tile first, so that the tiles in flight at one
+// time span about as many token tiles as weight tiles (fewest distinct units between L2 and the SMs).
+__device__ __forceinline__ void pair_tile(int t, int m_tiles, int n_tiles, int& mt, int& nt)
+{
+    const int per = 8 * n_tiles, g = t / per, in = t - g * per;
+    const int rows = min(8, m_tiles - 8 * g);
+    nt = in / rows;
+    mt = 8 * g + (in - nt * rows);
+}
+
+template <int FMT, typename T>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kThreads, 1) mx_pair_kernel(const __grid_constant__ MxPairMaps maps, const MxGemmParams p)
+{
+    using namespace tc;
+    using G = MxPairGeom<FMT>;
+    constexpr int S = G::kStages, UNIT = unit_bytes(FMT);
+
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * G::kStage);       // [S] loads of both blocks -> MMA (first block)
+    uint64_t* empty = full + S;                                               // [S] MMA -> loads
+    uint64_t* acc_full = empty + S;                                           // MMA -> epilogue
+    uint64_t* acc_empty = acc_full + 1;                                       // epilogues of both blocks -> MMA (first block)
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const uint32_t smem0 = smem_u32(smem);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t rank;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(&full[s], 1);
+            mbar_init(&empty[s], 1);
+        }
+        mbar_init(acc_full, 1);
+        mbar_init(acc_empty, 16);
+        *abort_flag = 0;
+        fence_barrier_init();
+    }
+    if (warp == 1) tmem_alloc_pair(tmem_slot, 512);
+    tc_fence_before_sync();
+    __syncthreads();
+    mx_cluster_sync();                                                        // the other block's barriers exist
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    pdl_launch_dependents();
+
+    const int a_units = (p.M + 127) >> 7, b_units = p.n_tiles;                // units of 128 rows
+    const int n_tiles = (b_units + 1) >> 1, m_tiles = (a_units + 1) >> 1, total = n_tiles * m_tiles;
+    const int pairs = (int)gridDim.x >> 1, first = (int)blockIdx.x >> 1;
+
+    if (warp == 0) {
+        // ================= loads
+        if (lane == 0) {
+            bool ok = true;
+            int g = 0, early = 0;
+            prefetch_tensormap(&maps.a);
+            prefetch_tensormap(&maps.w_codes);
+            prefetch_tensormap(&maps.w_scales);
+            constexpr int ROWS = UNIT / 128;
+            const uint32_t full0 = cluster_addr(full, 0);
+            auto load_w = [&](int s, int mt, int nt, int ku) {                // (first block: expects the stage of both) requests the weights
+                const int a0 = 2 * mt, b0 = 2 * nt, b = b0 + (int)rank;
+                const int as = a0 + 1 < a_units ? 2 : 1, bs = b0 + 1 < b_units ? 2 : 1;
+                const uint32_t dst = smem0 + s * G::kStage, bar = full0 + 8 * s;
+                if (rank == 0) mbar_arrive_expect_tx(&full[s], as * UNIT + bs * kCodeBytes + 2 * bs * G::kSc);
+                const int y = (b0 * p.KU + ku) * ROWS, next = p.KU * ROWS;
+                if (b < b_units) tma_load_2d_pair(dst + G::kB, &maps.w_codes, 0, y + (int)rank * next, bar);
+                tma_load_2d_pair(dst + G::kSb, &maps.w_scales, 0, y + 128, bar);
+                if (bs == 2) tma_load_2d_pair(dst + G::kSb + G::kSc, &maps.w_scales, 0, y + next + 128, bar);
+            };
+            int mt, nt;
+            pair_tile(first, m_tiles, n_tiles, mt, nt);
+            for (; early < S && early < p.KU; ++early) load_w(early, mt, nt, early);
+            pdl_wait();
+            for (int t = first; ok && t < total; t += pairs) {
+                pair_tile(t, m_tiles, n_tiles, mt, nt);
+                const int a = 2 * mt + (int)rank;
+                for (int ku = 0; ku < p.KU; ++ku, ++g) {
+                    const int s = g % S;
+                    if (g >= S) ok = mbar_wait(&empty[s], ((g / S) - 1) & 1, abort_flag);
+                    if (!ok) break;
+                    if (g >= early) load_w(s, mt, nt, ku);
+                    if (a < a_units) tma_load_2d_pair(smem0 + s * G::kStage, &maps.a, 0, (a * p.KU + ku) * ROWS, full0 + 8 * s);
+                }
+            }
+            if (!ok) {
+                *abort_flag = 1;
+                // let copies in flight land (both blocks' count on the first block's barriers; the second waits for it at the end)
+                for (int q = max(0, g - S); rank == 0 && q < g; ++q) {
+                    const long long t0 = clock64();
+                    while (!mbar_try_wait(&full[q % S], (q / S) & 1) && clock64() - t0 < (1LL << 22)) {}
+                }
+            }
+        }
+    } else if (warp == 1 && rank == 1) {
+        // (the second block's tensor memory was allocated by this warp; it frees it at the end)
+    } else if (warp == 1) {
+        // ================= MMA issuer for the pair
+        const uint32_t sel = elect_one() ? 1u : 0u;
+        const uint64_t desc_a = smem_desc_k_sw128(smem0 + G::kA), desc_b = smem_desc_k_sw128(smem0 + G::kB);
+        const uint64_t desc_sa = smem_desc_scales(smem0 + G::kA + kCodeBytes), desc_sb = smem_desc_scales(smem0 + G::kSb);
+        bool ok = true;
+        int g = 0, it = 0;
+        for (int t = first; ok && t < total; t += pairs, ++it) {
+            if (it > 0) {
+                ok = mbar_wait_cluster(acc_empty, (it - 1) & 1, abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after_sync();
+            }
+            for (int ku = 0; ku < p.KU; ++ku, ++g) {
+                const int s = g % S;
+                ok = mbar_wait(&full[s], (g / S) & 1, abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                tc_fence_after_sync();
+                const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
+                const uint32_t sfa = tmem_base + (uint32_t)(G::kSf0 + (g & 1) * G::kSfCols);
+                const uint32_t sfb = sfa + (uint32_t)(G::kGroups * 4);
+#pragma unroll
+                for (int j = 0; j < G::kGroups; ++j) {
+                    tmem_copy_scales_pair(sfa + 4 * j, desc_sa + at + 32 * j, sel);
+                    tmem_copy_scales_pair(sfb + 8 * j, desc_sb + at + 32 * j, sel);
+                    tmem_copy_scales_pair(sfb + 8 * j + 4, desc_sb + at + (G::kSc >> 4) + 32 * j, sel);
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int grp = FMT == QMM_MXFP4 ? k >> 1 : k, id = FMT == QMM_MXFP4 ? (k & 1) * 2 : 0;
+                    mma_fp4_pair<FMT == QMM_MXFP4>(tmem_base, desc_a + at + 2 * k, desc_b + at + 2 * k, idesc_fp4(FMT == QMM_MXFP4, 256, 256, id), sfa + 4 * grp,
+                                                   sfb + 8 * grp, ku != 0 || k != 0, sel);
+                }
+                mma_commit_pair(&empty[s], sel);
+                __syncwarp();
+            }
+            if (ok) mma_commit_pair(acc_full, sel);
+            __syncwarp();
+        }
+        if (!ok) *abort_flag = 1;
+    } else if (warp >= 4) {
+        // ================= epilogue: 32 rows x 128 columns per warp
+        const int quarter = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t d = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * 128);
+        bool ok = true;
+        int it = 0;
+        pdl_wait();
+        const float alpha = (p.a_scale ? __ldg(p.a_scale) : 1.0f) * (p.w_scale[0] ? __ldg(p.w_scale[0]) : 1.0f);
+        for (int t = first; ok && t < total; t += pairs, ++it) {
+            ok = mbar_wait(acc_full, it & 1, abort_flag);
+            ok = __all_sync(0xFFFFFFFFu, ok);
+            if (!ok) break;
+            tc_fence_after_sync();
+            uint32_t v[4][32];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) tmem_ld_32x32b_x32(d + 32 * c, v[c]);
+            tmem_wait_ld();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_remote(acc_empty, 0);
+            int mt, nt;
+            pair_tile(t, m_tiles, n_tiles, mt, nt);
+            const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
+            const int n0 = 256 * nt + 128 * half;
+            if (row < p.M) {
+                T* o = reinterpret_cast<T*>(p.y) + (int64_t)row * p.ldy + n0;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    float f[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = alpha * __uint_as_float(v[c][i]);
+                    store32<T>(o + 32 * c, f, p.N - n0 - 32 * c, p.vec);
+                }
+            }
+        }
+        if (!ok) *abort_flag = 1;
+    }
+
+    // ---- teardown
+    tc_fence_before_sync();
+    __syncthreads();
+    mx_cluster_sync();                                                        // no arrival or MMA of the other block is still to come
+    if (threadIdx.x == 0 && *abort_flag && p.status != nullptr) atomicExch(p.status, (int)QMM_ERR_DEVICE_TIMEOUT);
+    if (warp == 1) {
+        tc_fence_after_sync();
+        tmem_dealloc_pair(tmem_base, 512);
+    }
+}
+
 // ------------------------------------------------------------ launches
 
 template <int FMT, int NB, bool GATEUP, typename T, int FORM>
@@ -516,14 +749,53 @@ static qmm_status launch_t(const MxGemmParams& p, int grid, int cluster, cudaStr
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, p), "microscaled product launch");
 }
 
-template <typename T> static bool row_vec(const void* y, int64_t ldy)
+template <typename T> static int row_vec(const void* y, int64_t ldy)
 {
-    return ((reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * (int64_t)sizeof(T))) & 15) == 0;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * (int64_t)sizeof(T));
+    return a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : 0;
+}
+
+qmm_status make_unit_map(CUtensorMap* map, const void* packed, int64_t rows128, int box_rows);
+
+template <int FMT, typename T> static qmm_status launch_pair_t(const MxGemmParams& p, int tiles, cudaStream_t st)
+{
+    auto kern = mx_pair_kernel<FMT, T>;
+    constexpr int smem = MxPairGeom<FMT>::kSmem, ROWS = unit_bytes(FMT) / 128;
+    static std::atomic<uint64_t> configured{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
+    const uint64_t bit = dev < 64 ? (1ull << dev) : 0;
+    if (!(configured.load(std::memory_order_relaxed) & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e != cudaSuccess) return check_cuda(e, "microscaled pair product shared memory size");
+        configured.fetch_or(bit, std::memory_order_relaxed);
+    }
+    MxPairMaps maps;
+    const int64_t a_rows = (int64_t)((p.M + 127) / 128) * p.KU * ROWS, w_rows = (int64_t)p.n_tiles * p.KU * ROWS;
+    qmm_status s = make_unit_map(&maps.a, p.a, a_rows, ROWS);
+    if (s == QMM_OK) s = make_unit_map(&maps.w_codes, p.w[0], w_rows, 128);
+    if (s == QMM_OK) s = make_unit_map(&maps.w_scales, p.w[0], w_rows, ROWS - 128);
+    if (s != QMM_OK) return s;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(2 * (tiles < kNumSMs / 2 ? tiles : kNumSMs / 2)));
+    cfg.blockDim = dim3(MxPairGeom<FMT>::kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return check_cuda(cudaLaunchKernelEx(&cfg, kern, maps, p), "microscaled pair product launch");
 }
 
 template <int FMT, typename T> static qmm_status dense_t(MxGemmParams p, cudaStream_t st)
 {
     p.vec = row_vec<T>(p.y, p.ldy);
+    const int pair_tiles = ((p.n_tiles + 1) / 2) * ((p.M + 255) / 256);
+    // (the pair form's row coordinates are 32-bit: operands below 2^31 rows of 128 bytes)
+    const bool fits = ((int64_t)p.n_tiles + (p.M + 127) / 128) * p.KU * (unit_bytes(FMT) / 128) < (1LL << 31);
+    if (p.M > 128 && fits && g_knobs.mx_pair != 2 && (pair_tiles >= 32 || g_knobs.mx_pair == 1)) return launch_pair_t<FMT, T>(p, pair_tiles, st);
     const int64_t tiles = (int64_t)p.n_tiles * ((p.M + 127) / 128);
     int splits = 1;
     while (splits < 8 && splits * 2 <= p.KU && tiles * splits * 2 <= kNumSMs) splits *= 2;

@@ -316,5 +316,124 @@ __device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t a_desc, uint64
             : "memory");
 }
 
+// ------------------------------------------- pairs of SMs (cta_group::2)
+
+// 2-D tiled load into this block's shared memory whose completion may be counted on a barrier of either block of the pair
+// (bar: a shared::cluster address).  No multicast: every block fetches its own tile.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t smem_dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(smem_dst), "l"(map), "r"(x), "r"(y), "r"(bar)
+        : "memory");
+}
+
+// shared::cluster address of the variable at this place in block `rank`.
+__device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+
+// Wait that also sees what a thread of the other block of the pair released before its arrival.
+__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort)
+{
+    const long long t0 = clock64();
+    while (true) {
+        uint32_t ok;
+        asm volatile(
+            "{\n\t"
+            ".reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t"
+            "}\n"
+            : "=r"(ok)
+            : "r"(smem_u32(bar)), "r"(parity)
+            : "memory");
+        if (ok) return true;
+        if (*abort) return false;
+        if (clock64() - t0 > kWaitLimitCycles) return false;
+    }
+}
+
+// Arrive on the barrier at the same place in block `rank` of the cluster.
+__device__ __forceinline__ void mbar_arrive_remote(uint64_t* bar, uint32_t rank)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .b32 a;\n\t"
+        "mapa.shared::cluster.u32 a, %0, %1;\n\t"
+        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t"
+        "}\n"
+        ::"r"(smem_u32(bar)), "r"(rank)
+        : "memory");
+}
+
+__device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(slot)), "r"(cols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_dealloc_pair(uint32_t base, uint32_t cols)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
+}
+
+// The scale group at the same shared-memory place of both blocks -> each block's tensor memory.
+__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc, uint32_t sel)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t"
+        "}\n"
+        ::"r"(taddr), "l"(desc), "r"(sel)
+        : "memory");
+}
+
+// D (256 rows, 128 in each block) (+)= A (128 rows from each block) * B (half of its rows from each block)^T over 64 k.
+template <bool E8M0>
+__device__ __forceinline__ void mma_fp4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb,
+                                             uint32_t acc, uint32_t sel)
+{
+    if (E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p;\n\t"
+            "setp.ne.b32 q, %7, 0;\n\t"
+            "setp.ne.b32 p, %6, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            : "memory");
+}
+
+// Arrive on the barrier at this place in both blocks once everything the acting lane has issued so far has finished.
+__device__ __forceinline__ void mma_commit_pair(uint64_t* bar, uint32_t sel)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred q;\n\t"
+        ".reg .b16 m;\n\t"
+        "setp.ne.b32 q, %1, 0;\n\t"
+        "mov.b16 m, 3;\n\t"
+        "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t"
+        "}\n"
+        ::"r"(smem_u32(bar)), "r"(sel)
+        : "memory");
+}
+
 }  // namespace tc
 }  // namespace qmm

@@ -173,7 +173,7 @@ def check_product(Y, a, w, K, what=""):
 
 # one tile; K tails; clusters of 2, 4 and 8; several token tiles; more tiles than SMs, ragged both ways
 SHAPES = [(1, 1, 1), (1, 128, 256), (3, 100, 32), (5, 130, 272), (128, 128, 512), (17, 256, 1024), (1, 2048, 2048), (9, 512, 2304), (127, 640, 1000),
-          (129, 1000, 520), (300, 384, 768), (1, 20000, 256), (200, 10000, 300), (700, 4100, 544)]
+          (129, 1000, 520), (300, 384, 768), (1, 20000, 256), (200, 10000, 300), (700, 4100, 544), (2500, 3000, 288), (130, 129, 4000)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -188,6 +188,12 @@ def test_product(qmm, fmt, M, N, K):
         qmm.status_check(ws)
         check_product(Y, a, w, K, "M=%d N=%d K=%d fmt=%d %s" % (M, N, K, fmt, dt))
         assert torch.equal(Y, qmm.mx_gemm(fmt, ap, M, wp, N, K, a_scale=ga, w_scale=gw, ws=ws, dtype=dt)), "same bits on every call"
+        if M > 128:                                                                # both tile forms, whichever the plan took
+            for form in ("1", "2"):
+                qmm.debug_config("mx_pair", form)
+                check_product(qmm.mx_gemm(fmt, ap, M, wp, N, K, a_scale=ga, w_scale=gw, ws=ws, dtype=dt), a, w, K, "form " + form)
+                qmm.status_check(ws)
+            qmm.debug_config(None)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -209,7 +215,7 @@ def test_linear_is_quantize_then_product(qmm, fmt, M):
 
 @pytest.mark.parametrize("fmt", FMTS)
 def test_output_strides(qmm, fmt):
-    for M, N, K in ((5, 200, 512), (130, 300, 256), (260, 520, 512)):
+    for M, N, K in ((5, 200, 512), (130, 300, 256), (260, 520, 512), (513, 5000, 256)):
         (xa, a, ga), (xw, w, gw) = operands(fmt, M, N, K, 9)
         ap, wp = qmm.mx_quantize(fmt, xa.cuda(), tensor_scale=ga), qmm.mx_quantize(fmt, xw.cuda(), tensor_scale=gw)
         for dt in DTYPES.values():
@@ -224,7 +230,7 @@ def test_output_strides(qmm, fmt):
 
 @pytest.mark.parametrize("fmt", FMTS)
 def test_nan_blocks_reach_exactly_the_outputs_that_read_them(qmm, fmt):
-    for M, N, K in ((6, 256, 512), (300, 512, 512)):
+    for M, N, K in ((6, 256, 512), (300, 512, 512), (600, 4096, 512)):
         gen = torch.Generator().manual_seed(4)
         xa, xw = torch.randn(M, K, generator=gen), torch.randn(N, K, generator=gen)
         xa[2, 77], xw[130, 500] = float("nan"), float("inf")
@@ -237,7 +243,7 @@ def test_nan_blocks_reach_exactly_the_outputs_that_read_them(qmm, fmt):
 def test_rows_past_the_matrix_are_not_data(qmm):
     """The rows that pad the last unit may hold anything, NaN scales included."""
     for fmt in FMTS:
-        for M, N, K in ((5, 130, 512), (200, 300, 256), (300, 400, 512)):
+        for M, N, K in ((5, 130, 512), (200, 300, 256), (300, 400, 512), (385, 4225, 512)):
             (xa, a, ga), (xw, w, gw) = operands(fmt, M, N, K, 2)
             ap, wp = (torch.full((qmm.mx_bytes(fmt, r, K),), 0xFF, dtype=torch.uint8, device="cuda") for r in (M, N))
             qmm.mx_quantize(fmt, xa.cuda(), out=ap, tensor_scale=ga)
