@@ -336,35 +336,16 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank)
     return a;
 }
 
-// Wait that also sees what a thread of the other block of the pair released before its arrival.
-__device__ __forceinline__ bool mbar_wait_cluster(uint64_t* bar, uint32_t parity, volatile int* abort)
-{
-    const long long t0 = clock64();
-    while (true) {
-        uint32_t ok;
-        asm volatile(
-            "{\n\t"
-            ".reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t"
-            "}\n"
-            : "=r"(ok)
-            : "r"(smem_u32(bar)), "r"(parity)
-            : "memory");
-        if (ok) return true;
-        if (*abort) return false;
-        if (clock64() - t0 > kWaitLimitCycles) return false;
-    }
-}
-
-// Arrive on the barrier at the same place in block `rank` of the cluster.
+// Arrive on the barrier at the same place in block `rank` of the cluster.  It orders the arriving thread's tensor-memory reads
+// (after tcgen05.wait::ld and the fence before a thread sync), not its global stores: a release at cluster scope
+// would wait for all of those, which was measured at 2 000 cycles in an epilogue.
 __device__ __forceinline__ void mbar_arrive_remote(uint64_t* bar, uint32_t rank)
 {
     asm volatile(
         "{\n\t"
         ".reg .b32 a;\n\t"
         "mapa.shared::cluster.u32 a, %0, %1;\n\t"
-        "mbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t"
+        "mbarrier.arrive.shared::cluster.b64 _, [a];\n\t"
         "}\n"
         ::"r"(smem_u32(bar)), "r"(rank)
         : "memory");
