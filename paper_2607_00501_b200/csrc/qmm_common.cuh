@@ -148,6 +148,14 @@ __device__ __forceinline__ u32x8 ld_keep_256(const void* p)
     return r;
 }
 
+// 32-byte store of whole sectors.
+__device__ __forceinline__ void st_global_256(void* p, const uint32_t* u)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]),
+                 "r"(u[6]), "r"(u[7])
+                 : "memory");
+}
+
 __device__ __forceinline__ uint32_t ld_nc_u32(const void* p)
 {
     uint32_t r;

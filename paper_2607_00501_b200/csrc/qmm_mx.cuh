@@ -66,10 +66,53 @@ template <> struct Dt<float> {
 
 // ------------------------------------------------------- quantisation of one block
 
-// Two fp32 -> two e2m1 codes in a byte (first in the low nibble): nearest, ties to the even code, saturating at 6.
-__device__ __forceinline__ uint32_t codes2(float a, float b)
+// Eight fp32 -> eight e2m1 codes, first in the low nibble: nearest, ties to the even code, saturating at 6.
+__device__ __forceinline__ uint32_t codes8(const float2 (&v)[4])
 {
-    return (uint32_t)__nv_cvt_float2_to_fp4x2(make_float2(a, b), __NV_E2M1, cudaRoundNearest);
+    uint32_t w;
+    asm("{\n\t"
+        ".reg .b8 b0, b1, b2, b3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+        "mov.b32 %0, {b0, b1, b2, b3};\n\t"
+        "}\n"
+        : "=r"(w)
+        : "f"(v[0].x), "f"(v[0].y), "f"(v[1].x), "f"(v[1].y), "f"(v[2].x), "f"(v[2].y), "f"(v[3].x), "f"(v[3].y));
+    return w;
+}
+
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t as_u64(float2 v) { return *reinterpret_cast<uint64_t*>(&v); }
+__device__ __forceinline__ float2 as_f2(uint64_t u) { return *reinterpret_cast<float2*>(&u); }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)));
+    return as_f2(d);
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(as_u64(a)), "l"(as_u64(b)), "l"(as_u64(c)));
+    return as_f2(d);
+}
+__device__ __forceinline__ float2 both(float a) { return make_float2(a, a); }
+
+// max(m, |x|) that keeps a NaN.
+__device__ __forceinline__ float maxabs(float m, float x)
+{
+    float d;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(m), "f"(fabsf(x)));
+    return d;
+}
+template <int N> __device__ __forceinline__ float block_amax(const float (&v)[N])
+{
+    float m[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < N; ++i) m[i & 3] = maxabs(m[i & 3], v[i]);
+    return maxabs(maxabs(m[0], m[1]), maxabs(m[2], m[3]));
 }
 
 __device__ __forceinline__ float e8m0_value(uint32_t b)                       // 2^(b - 127); b = 0 is a subnormal fp32
@@ -82,76 +125,128 @@ __device__ __forceinline__ float e4m3_value(uint32_t b)
     return __half2float(__half(h));
 }
 
-// Scale byte of a block from its largest magnitude, given as fp32 bits (sign cleared; a NaN's bits exceed every
-// finite value's, so the integer maximum of the elements' bits is the right reduction for both).
-template <int FMT> __device__ __forceinline__ uint32_t block_scale(uint32_t amax_bits, float g6)
-{
-    if (FMT == QMM_MXFP4) {
-        const uint32_t e = amax_bits >> 23;                                    // 127 + floor(log2 amax); 0: zero or subnormal
-        return e == 255u ? 255u : e < 2u ? 0u : e - 2u;
+// Tensor scale g of an NVFP4 operand: 6 g in fp32 and its reciprocal (prepared once per thread).
+struct TensorScale {
+    float g, g6, r6;
+    bool plain;                                            // g6 is far from the ends of the exponent range
+    __device__ __forceinline__ explicit TensorScale(float scale) : g(scale), g6(6.0f * scale)
+    {
+        r6 = 1.0f / g6;
+        plain = g6 >= 0x1p-80f && g6 <= 0x1p80f;
     }
-    if (amax_bits >= 0x7F800000u) return 0x7Fu;
-    return (uint32_t)__nv_cvt_float_to_fp8(fminf(__uint_as_float(amax_bits) / g6, 448.0f), __NV_SATFINITE, __NV_E4M3);
+};
+
+// Correctly rounded a / b from r = rn(1 / b): q0 = a r, e = a - q0 b (exact in one FMA), q = q0 + e r (P. W. Markstein,
+// "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J. Res. Dev. 34, 1990).  Needs b and the
+// quotient away from the ends of the exponent range (a quotient that underflows is a zero code here either way).
+__device__ __forceinline__ float quotient(float a, float b, float r)
+{
+    const float q = a * r;
+    return fmaf(fmaf(-q, b, a), r, q);
+}
+__device__ __forceinline__ float2 quotient2(float2 a, float nb, float r)           // nb = -b
+{
+    const float2 q = mul2(a, both(r));
+    return fma2(fma2(q, both(nb), a), both(r), q);
 }
 
-// Codes of a block: FMT elements v -> FMT / 8 words, returns the scale byte.  g = the tensor's scale, g6 = 6 g in fp32.
+// Scale byte of a block from its largest magnitude (NaN if it holds one).
+template <int FMT> __device__ __forceinline__ uint32_t block_scale(float amax, const TensorScale& ts)
+{
+    if (FMT == QMM_MXFP4) {
+        const uint32_t e = __float_as_uint(amax) >> 23;                            // 127 + floor(log2 amax); 0: zero or subnormal
+        return e == 255u ? 255u : e < 2u ? 0u : e - 2u;
+    }
+    if (!(amax < __int_as_float(0x7F800000))) return 0x7Fu;
+    const float s = ts.plain && amax <= 0x1p40f ? quotient(amax, ts.g6, ts.r6) : amax / ts.g6;
+    return (uint32_t)__nv_cvt_float_to_fp8(fminf(s, 448.0f), __NV_SATFINITE, __NV_E4M3);
+}
+
+// Codes of a block whose largest magnitude is amax: FMT elements v -> FMT / 8 words, returns the scale byte.
 //
 // MXFP4: the quotient by a power of two is a product by its reciprocal, exactly.
 // NVFP4: x / D in fp32 has to be the correctly rounded quotient, because ties are common (D has few significant
-// bits) and a product by 1 / D would break them the wrong way.  One division per block gives r = rn(1 / D); then
-// q0 = x r, e = x - q0 D (exact in one FMA), q = q0 + e r is the correctly rounded quotient (P. W. Markstein,
-// "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J. Res. Dev. 34, 1990), three
-// operations per element.  That needs D and the quotients away from the ends of the exponent range; a block with D
-// outside [2^-80, 2^80] or a quotient beyond 2^80 takes true divisions (a quotient that underflows is code 0 either way).
-template <int FMT> __device__ __forceinline__ uint32_t quantize_block(const float (&v)[FMT], float g, float g6, uint32_t (&out)[FMT / 8])
+// bits) and a product by 1 / D would break them the wrong way: one division per block and three operations per element
+// (two elements per instruction); a block with D outside [2^-80, 2^80] or a quotient beyond 2^80 takes true divisions.
+template <int FMT> __device__ __forceinline__ uint32_t quantize_block(const float (&v)[FMT], float amax, const TensorScale& ts, uint32_t (&out)[FMT / 8])
 {
-    uint32_t amax = 0;
-#pragma unroll
-    for (int i = 0; i < FMT; ++i) amax = max(amax, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    const uint32_t sb = block_scale<FMT>(amax, g6);
+    const uint32_t sb = block_scale<FMT>(amax, ts);
     if (FMT == QMM_MXFP4) {
-        if (sb == 255u) {
-#pragma unroll
-            for (int w = 0; w < FMT / 8; ++w) out[w] = 0u;
-            return sb;
-        }
-        const float inv = __uint_as_float((254u - sb) << 23);                  // 2^(127 - sb), sb in 0 .. 252
+        const float inv = sb == 255u ? 0.0f : __uint_as_float((254u - sb) << 23);  // 2^(127 - sb), sb in 0 .. 252
 #pragma unroll
         for (int w = 0; w < FMT / 8; ++w) {
-            uint32_t c = 0;
+            float2 q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c |= codes2(v[8 * w + 2 * i] * inv, v[8 * w + 2 * i + 1] * inv) << (8 * i);
-            out[w] = c;
+            for (int i = 0; i < 4; ++i) q[i] = mul2(make_float2(v[8 * w + 2 * i], v[8 * w + 2 * i + 1]), both(inv));
+            const uint32_t c = codes8(q);
+            out[w] = sb == 255u ? 0u : c;
         }
         return sb;
     }
-    const float D = e4m3_value(sb) * g;
+    const float D = e4m3_value(sb) * ts.g;
     if (sb == 0x7Fu || !(D > 0.0f)) {
 #pragma unroll
         for (int w = 0; w < FMT / 8; ++w) out[w] = 0u;
         return sb;
     }
     const float r = 1.0f / D;
-    const bool plain = D >= 0x1p-80f && D <= 0x1p80f && __uint_as_float(amax) * r <= 0x1p80f;
+    if (D >= 0x1p-80f && D <= 0x1p80f && amax * r <= 0x1p80f) {
 #pragma unroll
-    for (int w = 0; w < FMT / 8; ++w) {
-        uint32_t c = 0;
+        for (int w = 0; w < FMT / 8; ++w) {
+            float2 q[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = v[8 * w + 2 * i], b = v[8 * w + 2 * i + 1];
-            float qa, qb;
-            if (plain) {
-                qa = a * r, qb = b * r;
-                qa = fmaf(fmaf(-qa, D, a), r, qa);
-                qb = fmaf(fmaf(-qb, D, b), r, qb);
-            } else {
-                qa = a / D, qb = b / D;
-            }
-            c |= codes2(qa, qb) << (8 * i);
+            for (int i = 0; i < 4; ++i) q[i] = quotient2(make_float2(v[8 * w + 2 * i], v[8 * w + 2 * i + 1]), -D, r);
+            out[w] = codes8(q);
         }
-        out[w] = c;
+    } else {
+#pragma unroll 1
+        for (int w = 0; w < FMT / 8; ++w) {
+            float2 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float a = 0.0f, b = 0.0f;                                          // (v stays in registers: no indexing by the loop variable)
+#pragma unroll
+                for (int k = 0; k < FMT / 8; ++k)
+                    if (k == w) a = v[8 * k + 2 * i], b = v[8 * k + 2 * i + 1];
+                q[i] = make_float2(a / D, b / D);
+            }
+            const uint32_t c = codes8(q);
+#pragma unroll
+            for (int k = 0; k < FMT / 8; ++k)
+                if (k == w) out[k] = c;
+        }
     }
     return sb;
+}
+
+// 32 elements (one MXFP4 block or two NVFP4 blocks) -> 16 bytes of codes and the scale byte(s).
+template <int FMT> __device__ __forceinline__ uint4 quantize32(const float (&v)[32], const float (&amax)[32 / FMT], const TensorScale& ts, uint32_t& sb)
+{
+    if constexpr (FMT == QMM_MXFP4) {
+        uint32_t w[4];
+        sb = quantize_block<32>(v, amax[0], ts, w);
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+        float a[16], b[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) a[i] = v[i], b[i] = v[16 + i];
+        uint32_t wa[2], wb[2];
+        sb = quantize_block<16>(a, amax[0], ts, wa);
+        sb |= quantize_block<16>(b, amax[1], ts, wb) << 8;
+        return make_uint4(wa[0], wa[1], wb[0], wb[1]);
+    }
+}
+template <int FMT> __device__ __forceinline__ uint4 quantize32(const float (&v)[32], const TensorScale& ts, uint32_t& sb)
+{
+    float m[32 / FMT];
+#pragma unroll
+    for (int b = 0; b < 32 / FMT; ++b) {
+        float part[FMT];
+#pragma unroll
+        for (int i = 0; i < FMT; ++i) part[i] = v[b * FMT + i];
+        m[b] = block_amax(part);
+    }
+    return quantize32<FMT>(v, m, ts, sb);
 }
 
 }  // namespace mx

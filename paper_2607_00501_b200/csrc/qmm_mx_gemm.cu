@@ -13,8 +13,8 @@
 // 128 x 128 x 256 step takes 256 cycles of the tensor pipe per 17 KB of weights, and HBM delivers 17 KB per SM in
 // ~750 cycles.
 //
-// Roles: warp 0 loads (one lane), warp 1 issues copies of scales and MMAs (converged, one elected lane), warps 4.. run the
-// epilogue: they take the accumulators into registers at once, free them, then work and store while the next tile's
+// Roles: warps 0 and 2 load weights and tokens, warp 1 issues copies of scales and MMAs (converged, one elected lane), warps 4.. run
+// the epilogue: they take the accumulators into registers at once, free them, then work and store while the next tile's
 // MMAs run.  The kernel is persistent over tiles, ring and barrier phases run on across them.
 // Tile t = (token tile t / n_tiles, weight tile t % n_tiles).  BN = 128, 64 or 32: few weight rows per tile where whole tiles would
 // leave SMs idle.  (A K split with sums joined through a cluster's shared memory was slower: 8.8 us against 6 for one
@@ -53,15 +53,18 @@ constexpr int kMxMaxE = 1024;
 template <int FMT, int BN, bool GATEUP, bool GROUPED> struct MxGeom {
     static constexpr int NB = GATEUP ? 2 : 1;                                   // weight matrices
     static constexpr int kUnit = unit_bytes(FMT), kSc = scale_bytes(FMT);
+    static constexpr bool kWhole = BN == 128;                                   // a tile's weights are whole units: one copy each
     static constexpr int kWin = BN < 64 ? 64 : BN;                              // columns of one matrix's MMA: a tile of 32 rows is half of a window
                                                                                 // of 64 (scale columns are addressed in pairs), the other half is idle
-    static constexpr int kCodesW = kWin * 128;                                  // codes of one matrix in a stage
-    static constexpr int kW = kUnit, kScW = kW + NB * kCodesW;                  // stage: token unit | codes | scales
-    static constexpr int kStage = kScW + NB * kSc;
+    static constexpr int kMat = kWin * 128 + kSc;                               // one matrix in a stage: codes, then the unit's scales
+    static constexpr int kW = kUnit;                                            // stage: token unit | matrix | matrix
+    static constexpr int kStage = kW + NB * kMat;
     static constexpr int kDCols = NB * kWin;
-    static constexpr int kEpiWarps = kDCols > 128 ? 8 : 4;                      // a warp holds at most 128 columns in registers
+    // columns per epilogue warp: 32 of each matrix in the gate/up form (its arithmetic wants warps), else up to 64
+    static constexpr int kCols = GATEUP ? 32 : BN < 64 ? BN : 64;
+    static constexpr int kParts = BN / kCols, kEpiWarps = 4 * kParts;
     static constexpr int kThreads = (4 + kEpiWarps) * 32;
-    static constexpr int kTail = 1024 + (GROUPED ? (kMxMaxE + 1) * 4 : 0);      // barriers, the experts' unit index
+    static constexpr int kTail = 1024 + (GROUPED ? 2 * (kMxMaxE + 32) * 4 : 0);   // barriers, the experts' first units and rows
     static constexpr int kFit = (227 * 1024 - 1024 - kTail) / kStage;
     static constexpr int kStages = kFit < 10 ? kFit : 10;
     static constexpr int kSmem = 1024 + kStages * kStage + kTail;
@@ -83,16 +86,30 @@ struct MxWork {
     int n_tile, expert;
 };
 
-__device__ __forceinline__ float silu_f32(float g) { return __fdividef(g, 1.0f + __expf(-g)); }
+// silu(g) u = g u / (1 + 2^(-g log2 e)) for two features at a time, g and u still to be multiplied by their tensor scales:
+// c = {-alpha log2 e}, both factors of the product in `ab`.  2^x and 1 / x are the hardware's approximations (relative error of a
+// few 2^-23 each); g << 0 gives 2^x = inf and the limit 0.
+__device__ __forceinline__ float ex2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float2 silu_mul2(float2 g, float2 u, float c, float ab)
+{
+    const float2 x = mul2(g, both(c));
+    const float2 den = make_float2(1.0f + ex2_approx(x.x), 1.0f + ex2_approx(x.y));
+    return mul2(mul2(mul2(g, both(ab)), u), make_float2(rcp_approx(den.x), rcp_approx(den.y)));
+}
 
 // 32 consecutive outputs of one row; n = how many exist.  vec: widest store (bytes) that the rows' alignment allows; 32-byte
 // stores write whole sectors (a lane's neighbours in a store are other rows).
-__device__ __forceinline__ void st_global_256(void* p, const uint32_t* u)
-{
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]),
-                 "r"(u[6]), "r"(u[7])
-                 : "memory");
-}
 template <typename T> __device__ __forceinline__ void store32(T* o, const float (&v)[32], int n, int vec)
 {
     if (vec && n >= 32) {
@@ -130,7 +147,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
     using namespace tc;
     using G = MxGeom<FMT, BN, GATEUP, GROUPED>;
     constexpr int S = G::kStages, AB = G::kAccBufs, NEPI = G::kEpiWarps, NB = G::NB;
-    constexpr int LOAD_WARP = 0, MMA_WARP = 1, EPI_WARP0 = 4;
+    constexpr int W_WARP = 0, MMA_WARP = 1, A_WARP = 2, EPI_WARP0 = 4;         // loads of weights and of tokens are two warps
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -140,13 +157,14 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
     uint64_t* acc_empty = acc_full + 2;                                       // [2] epilogue -> MMA
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    int* s_units = reinterpret_cast<int*>(smem + S * G::kStage + 1024);       // [E + 1] (grouped)
+    int* s_units = reinterpret_cast<int*>(smem + S * G::kStage + 1024);       // [E + 1], then INT_MAX up to a multiple of 32 (grouped)
+    int* s_first = s_units + kMxMaxE + 32;                                    // [E + 1]
     const uint32_t smem0 = smem_u32(smem);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(&full[s], 1);
+            mbar_init(&full[s], 2);
             mbar_init(&empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -162,7 +180,10 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
     }
     if (GROUPED) {
         pdl_wait();                                                           // the rows' grouping is written upstream
-        for (int e = threadIdx.x; e <= p.E; e += G::kThreads) s_units[e] = p.units[e];
+        for (int e = threadIdx.x; e < ((p.E + 32) & ~31); e += G::kThreads) {
+            s_units[e] = e <= p.E ? __ldg(p.units + e) : 0x7FFFFFFF;
+            if (e <= p.E) s_first[e] = __ldg(p.offsets + e);
+        }
     }
     tc_fence_before_sync();
     __syncthreads();
@@ -173,7 +194,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
     const int m_tiles = GROUPED ? s_units[p.E] : (p.M + 127) >> 7;
     const int total = m_tiles * p.n_tiles;
 
-    // i-th piece of work of this block (the same sequence for every role)
+    // i-th piece of work of this block (the same sequence for every role; whole converged warps)
     auto get_work = [&](int i, MxWork& w) -> bool {
         const int t = (int)blockIdx.x + i * (int)gridDim.x;
         if (t >= total) return false;
@@ -181,16 +202,15 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         w.n_tile = t - mt * p.n_tiles;
         w.m_unit = mt;
         if (GROUPED) {
-            int lo = 0, hi = p.E - 1;                                         // first e with units[e + 1] > mt
-            while (lo < hi) {
-                const int mid = (lo + hi) >> 1;
-                if (s_units[mid + 1] > mt) hi = mid;
-                else lo = mid + 1;
-            }
-            const int first = __ldg(p.offsets + lo), past = __ldg(p.offsets + lo + 1);
-            w.expert = lo;
-            w.row0 = first + 128 * (mt - s_units[lo]);
-            w.rows = min(128, past - w.row0);
+            // the expert that unit mt belongs to: the last e with units[e] <= mt.  Two rounds of 32 comparisons: which run of 32 experts,
+            // then which of them (units[] ascends; an expert without rows starts where the next one does)
+            const int runs = (p.E + 31) >> 5;
+            const unsigned in_run = __ballot_sync(0xFFFFFFFFu, lane < runs && s_units[lane * 32] <= mt);
+            const int run = 31 - __clz(in_run);
+            const unsigned in = __ballot_sync(0xFFFFFFFFu, s_units[run * 32 + lane] <= mt);
+            w.expert = run * 32 + 31 - __clz(in);
+            w.row0 = s_first[w.expert] + 128 * (mt - s_units[w.expert]);
+            w.rows = min(128, s_first[w.expert + 1] - w.row0);
         } else {
             w.expert = 0;
             w.row0 = mt * 128;
@@ -199,56 +219,68 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         return true;
     };
 
-    if (warp == LOAD_WARP) {
-        // ================= loads
-        if (lane == 0) {
-            bool ok = true;
-            int g = 0, early = 0;
-            MxWork w = {};
-            auto load_w = [&](int s, int ku) {                                // expects the whole stage, requests the weights
-                const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u, bar = smem_u32(&full[s]), dst = smem0 + s * G::kStage;
-                mbar_arrive_expect_tx(&full[s], NB * (BN * 128 + G::kSc) + rows8 * 128u + G::kSc);
-                const int r0 = w.n_tile * BN;
-                const int64_t at = w.expert * p.w_stride + ((int64_t)(r0 >> 7) * p.KU + ku) * G::kUnit;
+    if (warp == W_WARP || warp == A_WARP) {
+        // ================= loads (whole warps converged, one lane acts); each warp's part counts on the stage's barrier
+        const uint32_t sel = elect_one() ? 1u : 0u, full0 = smem_u32(full);
+        bool ok = true;
+        int g = 0, early = 0;
+        MxWork w = {};
+        auto load_w = [&](int s, int ku) {
+            const uint32_t bar = full0 + 8 * s, dst = smem0 + s * G::kStage + G::kW;
+            const int r0 = w.n_tile * BN;
+            const int64_t at = w.expert * p.w_stride + ((int64_t)(r0 >> 7) * p.KU + ku) * G::kUnit;
+            mbar_arrive_expect_tx_sel(bar, NB * (BN * 128 + G::kSc), sel);
 #pragma unroll
-                for (int b = 0; b < NB; ++b) {
-                    bulk_load(dst + G::kW + b * G::kCodesW + (r0 & (G::kWin - 1)) * 128, p.w[b] + at + (r0 & 127) * 128, BN * 128, bar);
-                    bulk_load(dst + G::kScW + b * G::kSc, p.w[b] + at + kCodeBytes, G::kSc, bar);
+            for (int b = 0; b < NB; ++b) {
+                if (G::kWhole) {
+                    bulk_load_sel(dst + b * G::kMat, p.w[b] + at, G::kUnit, bar, sel);
+                } else {
+                    bulk_load_sel(dst + b * G::kMat + (r0 & (G::kWin - 1)) * 128, p.w[b] + at + (r0 & 127) * 128, BN * 128, bar, sel);
+                    bulk_load_sel(dst + b * G::kMat + G::kWin * 128, p.w[b] + at + kCodeBytes, G::kSc, bar, sel);
                 }
-            };
-            // weights do not depend on the previous kernel: the first ring of them is requested before the wait for it
-            if (!GROUPED) {
-                if (get_work(0, w))
-                    for (; early < S && early < p.KU; ++early) load_w(early, early);
-                pdl_wait();
             }
-            for (int i = 0; ok && get_work(i, w); ++i) {
-                const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
-                for (int ku = 0; ku < p.KU; ++ku, ++g) {
-                    const int s = g % S;
-                    if (g >= S) ok = mbar_wait(&empty[s], ((g / S) - 1) & 1, abort_flag);
-                    if (!ok) break;
+        };
+        // weights do not depend on the previous kernel: the first ring of them is requested before the wait for it
+        if (!GROUPED) {
+            if (warp == W_WARP && get_work(0, w))
+                for (; early < S && early < p.KU; ++early) load_w(early, early);
+            pdl_wait();
+        }
+        for (int i = 0; ok && get_work(i, w); ++i) {
+            const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
+            const uint8_t* src = p.a + (int64_t)w.m_unit * p.KU * G::kUnit;
+            for (int ku = 0; ku < p.KU; ++ku, ++g) {
+                const int s = g % S;
+                if (g >= S) ok = mbar_wait(&empty[s], ((g / S) - 1) & 1, abort_flag);
+                ok = __all_sync(0xFFFFFFFFu, ok);
+                if (!ok) break;
+                if (warp == W_WARP) {
                     if (g >= early) load_w(s, ku);
-                    const uint8_t* src = p.a + ((int64_t)w.m_unit * p.KU + ku) * G::kUnit;
-                    const uint32_t dst = smem0 + s * G::kStage;
-                    bulk_load(dst, src, rows8 * 128u, smem_u32(&full[s]));
-                    bulk_load(dst + kCodeBytes, src + kCodeBytes, G::kSc, smem_u32(&full[s]));
+                    continue;
+                }
+                const uint32_t bar = full0 + 8 * s, dst = smem0 + s * G::kStage;
+                mbar_arrive_expect_tx_sel(bar, rows8 * 128u + G::kSc, sel);
+                if (rows8 == 128) {
+                    bulk_load_sel(dst, src + (int64_t)ku * G::kUnit, G::kUnit, bar, sel);
+                } else {
+                    bulk_load_sel(dst, src + (int64_t)ku * G::kUnit, rows8 * 128u, bar, sel);
+                    bulk_load_sel(dst + kCodeBytes, src + (int64_t)ku * G::kUnit + kCodeBytes, G::kSc, bar, sel);
                 }
             }
-            if (!ok) {
-                *abort_flag = 1;
-                // let copies in flight land before the block's shared memory is released
-                for (int q = max(0, g - S); q < g; ++q) {
-                    const long long t0 = clock64();
-                    while (!mbar_try_wait(&full[q % S], (q / S) & 1) && clock64() - t0 < (1LL << 22)) {}
-                }
+        }
+        if (!ok) {
+            *abort_flag = 1;
+            // let copies in flight land before the block's shared memory is released
+            for (int q = max(0, g - S); q < g; ++q) {
+                const long long t0 = clock64();
+                while (!mbar_try_wait(&full[q % S], (q / S) & 1) && clock64() - t0 < (1LL << 22)) {}
             }
         }
     } else if (warp == MMA_WARP) {
         // ================= MMA issuer (whole warp converged, one lane acts)
         const uint32_t sel = elect_one() ? 1u : 0u;
         const uint64_t desc_a = smem_desc_k_sw128(smem0), desc_w = smem_desc_k_sw128(smem0 + G::kW);
-        const uint64_t desc_sa = smem_desc_scales(smem0 + kCodeBytes), desc_sw = smem_desc_scales(smem0 + G::kScW);
+        const uint64_t desc_sa = smem_desc_scales(smem0 + kCodeBytes), desc_sw = smem_desc_scales(smem0 + G::kW + G::kWin * 128);
         bool ok = true;
         int g = 0;
         MxWork w;
@@ -276,18 +308,16 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
                 for (int j = 0; j < G::kGroups; ++j) {
                     tmem_copy_scales(sfa + 4 * j, desc_sa + at + 32 * j, sel);
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) tmem_copy_scales(sfw + 4 * (j * NB + b), desc_sw + at + b * (G::kSc >> 4) + 32 * j, sel);
+                    for (int b = 0; b < NB; ++b) tmem_copy_scales(sfw + 4 * (j * NB + b), desc_sw + at + b * (G::kMat >> 4) + 32 * j, sel);
                 }
-                // K = 64 steps: 32 bytes of a row's 128.  Two matrices of 128 rows are one MMA of N = 256 (their codes are adjacent,
-                // their scale columns too); of 64 or 32 rows, one MMA each.
-                constexpr int MMAS = BN < 128 ? NB : 1, MN = G::kDCols / MMAS;
+                // K = 64 steps: 32 bytes of a row's 128
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
                     const int grp = FMT == QMM_MXFP4 ? k >> 1 : k, id = FMT == QMM_MXFP4 ? (k & 1) * 2 : 0;
 #pragma unroll
-                    for (int b = 0; b < MMAS; ++b)
-                        mma_fp4<FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at + 2 * k, desc_w + at + b * (G::kCodesW >> 4) + 2 * k,
-                                                  idesc_fp4(FMT == QMM_MXFP4, 128, MN, id), sfa + 4 * grp, sfw + 4 * (grp * NB + b) + sub, ku != 0 || k != 0, sel);
+                    for (int b = 0; b < NB; ++b)
+                        mma_fp4<FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at + 2 * k, desc_w + at + b * (G::kMat >> 4) + 2 * k,
+                                                  idesc_fp4(FMT == QMM_MXFP4, 128, G::kWin, id), sfa + 4 * grp, sfw + 4 * (grp * NB + b) + sub, ku != 0 || k != 0, sel);
                 }
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
@@ -297,16 +327,16 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         }
         if (!ok) *abort_flag = 1;
     } else if (warp >= EPI_WARP0) {
-        // ================= epilogue: 32 rows per warp; all columns, or (eight warps) half of each matrix's
-        constexpr int HALVES = NEPI / 4, CW = BN / HALVES, C32 = CW / 32;     // columns per matrix and warp, in blocks of 32
-        const int quarter = warp & 3, half = (warp - EPI_WARP0) >> 2;
-        const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * CW);
-        static_assert(BN >= 64 || HALVES == 1, "a window's half is a tile");
+        // ================= epilogue: 32 rows x kCols columns of each matrix per warp
+        constexpr int CW = G::kCols, C32 = CW / 32;
+        const int quarter = warp & 3, part = (warp - EPI_WARP0) >> 2;
+        const uint32_t lanes = tmem_base + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(part * CW);
         bool ok = true;
         MxWork w;
         // every global write below comes after the previous kernel has completed (its readers of this buffer included)
         if (!GROUPED) pdl_wait();
         const float a_scale = p.a_scale ? __ldg(p.a_scale) : 1.0f;
+        const TensorScale hs(GATEUP && p.h_scale ? __ldg(p.h_scale) : 1.0f);
         for (int it = 0; ok && get_work(it, w); ++it) {
             const int buf = it % AB;
             const float alpha = a_scale * (p.w_scale[0] ? __ldg(p.w_scale[0] + w.expert) : 1.0f);
@@ -328,9 +358,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&acc_empty[buf]);                      // the accumulators may be overwritten
             if (!warp_has_rows) continue;
-            const int n0 = w.n_tile * BN + half * CW;
+            const int n0 = w.n_tile * BN + part * CW;
             if constexpr (GATEUP) {
-                const float hs = p.h_scale ? __ldg(p.h_scale) : 1.0f, h6 = 6.0f * hs;
                 const int hku = (p.N + kUnitK - 1) / kUnitK;                  // k units of the output operand
                 uint8_t* row_units = reinterpret_cast<uint8_t*>(p.y) + (int64_t)w.m_unit * hku * G::kUnit;
                 // 32 features from k (a multiple of 32): codes, and the scale byte(s) of their block(s)
@@ -341,32 +370,26 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
                     if (FMT == QMM_MXFP4) unit[scale_offset(r, c >> 2) + (c & 3)] = (uint8_t)sc;
                     else *reinterpret_cast<uint16_t*>(unit + scale_offset(r, c >> 1) + 2 * (c & 1)) = (uint16_t)sc;
                 };
+                const int left = p.N - n0;
+                const float c = alpha * -1.44269504f, ab = alpha * alpha1;
+                float h[32];
 #pragma unroll
-                for (int c = 0; c < C32; ++c) {
-                    const int k = n0 + 32 * c, left = p.N - k;
-                    float h[32];
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        h[i] = i < left ? silu_f32(alpha * __uint_as_float(v[c][i])) * (alpha1 * __uint_as_float(v[C32 + c][i])) : 0.0f;
-                    uint4 codes;
-                    uint32_t sc;
-                    if constexpr (FMT == QMM_MXFP4) {
-                        uint32_t cw[4];
-                        sc = quantize_block<32>(h, hs, h6, cw);
-                        codes = make_uint4(cw[0], cw[1], cw[2], cw[3]);
-                    } else {
-                        float h0[16], h1[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) h0[i] = h[i], h1[i] = h[16 + i];
-                        uint32_t w0[2], w1[2];
-                        sc = quantize_block<16>(h0, hs, h6, w0);
-                        sc |= quantize_block<16>(h1, hs, h6, w1) << 8;
-                        codes = make_uint4(w0[0], w0[1], w1[0], w1[1]);
-                    }
-                    if (r < w.rows) put(k, codes, sc);
+                for (int i = 0; i < 32; i += 2) {
+                    const float2 x = silu_mul2(make_float2(__uint_as_float(v[0][i]), __uint_as_float(v[0][i + 1])),
+                                               make_float2(__uint_as_float(v[1][i]), __uint_as_float(v[1][i + 1])), c, ab);
+                    h[i] = x.x, h[i + 1] = x.y;
                 }
-                if (w.n_tile == p.n_tiles - 1 && half == HALVES - 1 && r < w.rows)
-                    for (int k = p.n_tiles * BN; k < hku * kUnitK; k += 32) put(k, make_uint4(0, 0, 0, 0), 0);    // the last unit's padding
+                if (left < 32) {                                              // features past N are zeros of the operand's padding
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) h[i] = i < left ? h[i] : 0.0f;
+                }
+                uint32_t sc;
+                const uint4 codes = quantize32<FMT>(h, hs, sc);
+                if (r < w.rows) {
+                    put(n0, codes, sc);
+                    if (w.n_tile == p.n_tiles - 1 && part == G::kParts - 1)
+                        for (int k = p.n_tiles * BN; k < hku * kUnitK; k += 32) put(k, make_uint4(0, 0, 0, 0), 0);    // the rest of the last unit
+                }
             } else {
                 if (r < w.rows) {
                     T* o = reinterpret_cast<T*>(p.y) + (int64_t)(w.row0 + r) * p.ldy + n0;

@@ -52,26 +52,6 @@ template <typename T, int VEC> __device__ __forceinline__ void load32(const T* p
     for (int i = 0; i < 32; ++i) v[i] = i < n ? Dt<T>::up(p[i]) : 0.0f;
 }
 
-// The two (NVFP4) or one (MXFP4) blocks of 32 elements -> 16 bytes of codes, scale bytes in `sb`.
-template <int FMT> __device__ __forceinline__ uint4 quantize32(const float (&v)[32], float g, float g6, uint32_t& sb)
-{
-    uint4 c;
-    if constexpr (FMT == QMM_MXFP4) {
-        uint32_t w[4];
-        sb = quantize_block<32>(v, g, g6, w);
-        c = make_uint4(w[0], w[1], w[2], w[3]);
-    } else {
-        float a[16], b[16];
-#pragma unroll
-        for (int i = 0; i < 16; ++i) a[i] = v[i], b[i] = v[16 + i];
-        uint32_t wa[2], wb[2];
-        sb = quantize_block<16>(a, g, g6, wa);
-        sb |= quantize_block<16>(b, g, g6, wb) << 8;
-        c = make_uint4(wa[0], wa[1], wb[0], wb[1]);
-    }
-    return c;
-}
-
 // Thread = one 32-element chunk of one row; chunks run over the padded K (a multiple of 256), so the padding of the last
 // unit is written as zeros.  Consecutive lanes hold consecutive chunks of a row (a row has a multiple of 8):
 // 4 (MXFP4) or 2 (NVFP4) neighbouring lanes join their scale bytes into one 4-byte store.
@@ -90,13 +70,12 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
     if (id >= rows * chunks) return;                       // (whole quads: rows * chunks is a multiple of 8)
     const int64_t row = id / chunks;
     const int c = (int)(id - row * chunks);
-    const float g = tensor_scale ? __ldg(tensor_scale) : 1.0f;
-    const float g6 = 6.0f * g;
+    const TensorScale ts(tensor_scale ? __ldg(tensor_scale) : 1.0f);
     const int64_t left = K - (int64_t)c * 32;
     float v[32];
     load32<T, VEC>(x + row * ldx + (int64_t)c * 32, (int)(left < 0 ? 0 : left < 32 ? left : 32), v);
     uint32_t sb;
-    uint4 codes = quantize32<FMT>(v, g, g6, sb);
+    const uint4 codes = quantize32<FMT>(v, ts, sb);
     // scale bytes of the group of four blocks, assembled in its first lane
     constexpr int LANES = FMT == QMM_MXFP4 ? 4 : 2;
     const uint32_t sub = (uint32_t)c & (LANES - 1);
@@ -166,10 +145,25 @@ mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K
 #pragma unroll
             for (int i = 0; i < 16; ++i) u[i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+            for (int i = 0; i < 4; ++i) {
+                if (VEC == 32) {
+                    if (i < 2) st_global_256(reinterpret_cast<uint8_t*>(o) + 32 * i, u + 8 * i);
+                } else {
+                    reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+                }
+            }
         } else {
+            uint32_t u[32];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) reinterpret_cast<float4*>(o)[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (VEC == 32) {
+                    if (i < 4) st_global_256(reinterpret_cast<uint8_t*>(o) + 32 * i, u + 8 * i);
+                } else {
+                    reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+                }
+            }
         }
     } else {
 #pragma unroll
@@ -290,7 +284,7 @@ static qmm_status dequantize_t(const void* packed, int64_t rows, int64_t K, cons
     const qmm_status s = launch_grid(rows * ((K + 31) / 32), &grid);
     if (s != QMM_OK) return s;
     const uintptr_t a = reinterpret_cast<uintptr_t>(out) | (rows > 1 ? (uintptr_t)(ldo * (int64_t)sizeof(T)) : 0);
-    return launch_pdl(a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 1> : mx_dequantize_kernel<FMT, T, 0>, grid, kQuantThreads, st,
+    return launch_pdl(a % 32 == 0 ? mx_dequantize_kernel<FMT, T, 32> : a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 16> : mx_dequantize_kernel<FMT, T, 0>, grid, kQuantThreads, st,
                       "microscaled dequantisation launch", (const uint8_t*)packed, rows, K, ts, (T*)out, ldo);
 }
 

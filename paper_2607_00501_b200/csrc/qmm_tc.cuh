@@ -254,12 +254,29 @@ __device__ __forceinline__ void mma_commit_sel(uint64_t* bar, uint32_t sel)
 // ------------------------------------------- bulk copies, block-scaled MMA
 
 // Contiguous global -> shared copy of `bytes` (a multiple of 16; both addresses 16-byte aligned), completion counted
-// on an mbarrier.
-__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar)
+// on an mbarrier; from a converged warp, the lane with sel != 0 acting.  The operands are then warp-uniform values; a single
+// lane in a divergent branch needs ~190 cycles per copy to set them up, which bounded the loading warp.
+__device__ __forceinline__ void bulk_load_sel(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar, uint32_t sel)
 {
-    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+    asm volatile(
+        "{\n\t"
+        ".reg .pred q;\n\t"
+        "setp.ne.b32 q, %4, 0;\n\t"
+        "@q cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];\n\t"
+        "}\n"
+        ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar), "r"(sel)
+        : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_expect_tx_sel(uint32_t bar, uint32_t bytes, uint32_t sel)
+{
+    asm volatile(
+        "{\n\t"
+        ".reg .pred q;\n\t"
+        "setp.ne.b32 q, %2, 0;\n\t"
+        "@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t"
+        "}\n"
+        ::"r"(bar), "r"(bytes), "r"(sel)
+        : "memory");
 }
 
 // Shared-memory descriptor of a 512-byte scale group (32 rows of 16 bytes, not swizzled: 8-row groups 128 bytes apart).
