@@ -53,12 +53,13 @@ constexpr int kMxMaxE = 1024;
 template <int FMT, int BN, bool GATEUP, bool GROUPED> struct MxGeom {
     static constexpr int NB = GATEUP ? 2 : 1;                                   // weight matrices
     static constexpr int kUnit = unit_bytes(FMT), kSc = scale_bytes(FMT);
-    static constexpr bool kWhole = BN == 128;                                   // a tile's weights are whole units: one copy each
+    static constexpr bool kWhole = BN == 128;                                   // a tile's weights are whole units
     static constexpr int kWin = BN < 64 ? 64 : BN;                              // columns of one matrix's MMA: a tile of 32 rows is half of a window
                                                                                 // of 64 (scale columns are addressed in pairs), the other half is idle
-    static constexpr int kMat = kWin * 128 + kSc;                               // one matrix in a stage: codes, then the unit's scales
-    static constexpr int kW = kUnit;                                            // stage: token unit | matrix | matrix
-    static constexpr int kStage = kW + NB * kMat;
+    static constexpr int kCodes = kWin * 128;                                   // codes of one matrix in a stage
+    static constexpr int kW = kUnit, kScW = kW + NB * kCodes;                   // stage: token unit | codes of each matrix | scales of each
+    static constexpr int kStage = kScW + NB * kSc;
+    static constexpr int kCodeStep = kCodes >> 4, kScStep = kSc >> 4;           // from matrix to matrix, in descriptor units
     static constexpr int kDCols = NB * kWin;
     // columns per epilogue warp: 32 of each matrix in the gate/up form (its arithmetic wants warps), else up to 64
     static constexpr int kCols = GATEUP ? 32 : BN < 64 ? BN : 64;
@@ -232,11 +233,11 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
             mbar_arrive_expect_tx_sel(bar, NB * (BN * 128 + G::kSc), sel);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                if (G::kWhole) {
-                    bulk_load_sel(dst + b * G::kMat, p.w[b] + at, G::kUnit, bar, sel);
+                if (G::kWhole && NB == 1) {                                   // codes and scales in one copy
+                    bulk_load_sel(dst, p.w[b] + at, G::kUnit, bar, sel);
                 } else {
-                    bulk_load_sel(dst + b * G::kMat + (r0 & (G::kWin - 1)) * 128, p.w[b] + at + (r0 & 127) * 128, BN * 128, bar, sel);
-                    bulk_load_sel(dst + b * G::kMat + G::kWin * 128, p.w[b] + at + kCodeBytes, G::kSc, bar, sel);
+                    bulk_load_sel(dst + b * G::kCodes + (r0 & (G::kWin - 1)) * 128, p.w[b] + at + (r0 & 127) * 128, BN * 128, bar, sel);
+                    bulk_load_sel(dst + NB * G::kCodes + b * G::kSc, p.w[b] + at + kCodeBytes, G::kSc, bar, sel);
                 }
             }
         };
@@ -280,7 +281,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         // ================= MMA issuer (whole warp converged, one lane acts)
         const uint32_t sel = elect_one() ? 1u : 0u;
         const uint64_t desc_a = smem_desc_k_sw128(smem0), desc_w = smem_desc_k_sw128(smem0 + G::kW);
-        const uint64_t desc_sa = smem_desc_scales(smem0 + kCodeBytes), desc_sw = smem_desc_scales(smem0 + G::kW + G::kWin * 128);
+        const uint64_t desc_sa = smem_desc_scales(smem0 + kCodeBytes), desc_sw = smem_desc_scales(smem0 + G::kScW);
         bool ok = true;
         int g = 0;
         MxWork w;
@@ -304,21 +305,15 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
                 const uint32_t sfa = tmem_base + (uint32_t)(G::kSf0 + (g & 1) * G::kSfCols);
                 const uint32_t sfw = sfa + (uint32_t)(G::kGroups * 4);
+                copy_scales<1, G::kGroups>(sfa, desc_sa + at, 4, sel);
 #pragma unroll
-                for (int j = 0; j < G::kGroups; ++j) {
-                    tmem_copy_scales(sfa + 4 * j, desc_sa + at + 32 * j, sel);
+                for (int b = 0; b < NB; ++b) copy_scales<1, G::kGroups>(sfw + 4 * b, desc_sw + at + b * G::kScStep, 4 * NB, sel);
+                // two whole matrices are one MMA of N = 256 (their codes and their scale columns are adjacent), else one MMA each
+                constexpr int MMAS = G::kWhole ? 1 : NB;
 #pragma unroll
-                    for (int b = 0; b < NB; ++b) tmem_copy_scales(sfw + 4 * (j * NB + b), desc_sw + at + b * (G::kMat >> 4) + 32 * j, sel);
-                }
-                // K = 64 steps: 32 bytes of a row's 128
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int grp = FMT == QMM_MXFP4 ? k >> 1 : k, id = FMT == QMM_MXFP4 ? (k & 1) * 2 : 0;
-#pragma unroll
-                    for (int b = 0; b < NB; ++b)
-                        mma_fp4<FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at + 2 * k, desc_w + at + b * (G::kMat >> 4) + 2 * k,
-                                                  idesc_fp4(FMT == QMM_MXFP4, 128, G::kWin, id), sfa + 4 * grp, sfw + 4 * (grp * NB + b) + sub, ku != 0 || k != 0, sel);
-                }
+                for (int b = 0; b < MMAS; ++b)
+                    mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
+                                                       sfa, sfw + 4 * b + sub, 4 * NB, ku != 0, sel);
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
             }
@@ -567,18 +562,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
                 const uint32_t sfa = tmem_base + (uint32_t)(G::kSf0 + (g & 1) * G::kSfCols);
                 const uint32_t sfb = sfa + (uint32_t)(G::kGroups * 4);
-#pragma unroll
-                for (int j = 0; j < G::kGroups; ++j) {
-                    tmem_copy_scales_pair(sfa + 4 * j, desc_sa + at + 32 * j, sel);
-                    tmem_copy_scales_pair(sfb + 8 * j, desc_sb + at + 32 * j, sel);
-                    tmem_copy_scales_pair(sfb + 8 * j + 4, desc_sb + at + (G::kSc >> 4) + 32 * j, sel);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int grp = FMT == QMM_MXFP4 ? k >> 1 : k, id = FMT == QMM_MXFP4 ? (k & 1) * 2 : 0;
-                    mma_fp4_pair<FMT == QMM_MXFP4>(tmem_base, desc_a + at + 2 * k, desc_b + at + 2 * k, idesc_fp4(FMT == QMM_MXFP4, 256, 256, id), sfa + 4 * grp,
-                                                   sfb + 8 * grp, ku != 0 || k != 0, sel);
-                }
+                copy_scales<2, G::kGroups>(sfa, desc_sa + at, 4, sel);
+                copy_scales<2, G::kGroups>(sfb, desc_sb + at, 8, sel);
+                copy_scales<2, G::kGroups>(sfb + 4, desc_sb + at + (G::kSc >> 4), 8, sel);
+                mma_fp4_stage<2, FMT == QMM_MXFP4>(tmem_base, desc_a + at, desc_b + at, idesc_fp4(FMT == QMM_MXFP4, 256, 256), sfa, sfb, 8, ku != 0, sel);
                 mma_commit_pair(&empty[s], sel);
                 __syncwarp();
             }

@@ -285,51 +285,203 @@ __device__ __forceinline__ uint64_t smem_desc_scales(uint32_t smem_addr)
     return (uint64_t)((smem_addr >> 4) & 0x3FFFu) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
 }
 
-// One scale group, shared memory -> 4 columns of tensor memory, repeated in the four lane quarters.
-__device__ __forceinline__ void tmem_copy_scales(uint32_t taddr, uint64_t desc, uint32_t sel)
-{
-    asm volatile(
-        "{\n\t"
-        ".reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t"
-        "}\n"
-        ::"r"(taddr), "l"(desc), "r"(sel)
-        : "memory");
-}
-
 // Instruction descriptor of the block-scaled 4-bit MMA: e2m1 A and B (K-major), fp32 D, M = 128 (or 256 over a pair of
-// SMs); scales e8m0 (one per 32 k) or e4m3 (one per 16).  Scale ids: byte of the scale word that the K = 64 step starts at.
-__host__ __device__ constexpr uint32_t idesc_fp4(bool e8m0, int m, int n, int scale_id)
+// SMs); scales e8m0 (one per 32 k) or e4m3 (one per 16).  Bits 4 and 29 up (the byte of the scale words that a step starts at) are 0
+// here and 2 in the second step of an e8m0 group.
+__host__ __device__ constexpr uint32_t idesc_fp4(bool e8m0, int m, int n)
 {
-    return (1u << 7) | (1u << 10) | ((uint32_t)scale_id << 4) | ((uint32_t)(n >> 3) << 17) | ((e8m0 ? 1u : 0u) << 23) |
-           ((uint32_t)(m >> 4) << 24) | ((uint32_t)scale_id << 29);
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((e8m0 ? 1u : 0u) << 23) | ((uint32_t)(m >> 4) << 24);
 }
 
-// D[tmem] (+)= (A[smem] * sa) * (B[smem] * sb)^T over 64 k.
-template <bool E8M0>
-__device__ __forceinline__ void mma_fp4(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                        uint32_t acc, uint32_t sel)
+// The scale groups of one operand of a stage (GROUPS of 512 bytes) -> 4 columns of tensor memory each, `pitch` columns apart,
+// repeated in the four lane quarters.  CG = 2: of both blocks of the pair, each from its own shared memory.  One block of instructions
+// (as the MMAs below): the predicate is set up once, the operands are the first ones plus constants.
+template <int CG, int GROUPS>
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc, uint32_t pitch, uint32_t sel)
 {
-    if (E8M0)
+    static_assert(GROUPS == 2 || GROUPS == 4, "two (32 k per scale) or four (16 k per scale) groups per stage");
+    if constexpr (CG == 1 && GROUPS == 2)
         asm volatile(
             "{\n\t"
-            ".reg .pred q, p;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "setp.ne.b32 p, %6, 0;\n\t"
-            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            ".reg .pred q;\n\t"
+            ".reg .b32 t1;\n\t"
+            ".reg .b64 s1;\n\t"
+            "setp.ne.b32 q, %3, 0;\n\t"
+            "add.u32 t1, %0, %2;\n\t"
+            "add.u64 s1, %1, 32;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [t1], s1;\n\t"
             "}\n"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            ::"r"(taddr), "l"(desc), "r"(pitch), "r"(sel)
             : "memory");
-    else
+    else if constexpr (CG == 1 && GROUPS == 4)
         asm volatile(
             "{\n\t"
-            ".reg .pred q, p;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "setp.ne.b32 p, %6, 0;\n\t"
-            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
+            ".reg .pred q;\n\t"
+            ".reg .b32 t1, t2, t3;\n\t"
+            ".reg .b64 s1, s2, s3;\n\t"
+            "setp.ne.b32 q, %3, 0;\n\t"
+            "add.u32 t1, %0, %2;\n\t"
+            "add.u64 s1, %1, 32;\n\t"
+            "add.u32 t2, t1, %2;\n\t"
+            "add.u64 s2, %1, 64;\n\t"
+            "add.u32 t3, t2, %2;\n\t"
+            "add.u64 s3, %1, 96;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [t1], s1;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [t2], s2;\n\t"
+            "@q tcgen05.cp.cta_group::1.32x128b.warpx4 [t3], s3;\n\t"
             "}\n"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
+            ::"r"(taddr), "l"(desc), "r"(pitch), "r"(sel)
+            : "memory");
+    else if constexpr (CG == 2 && GROUPS == 2)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q;\n\t"
+            ".reg .b32 t1;\n\t"
+            ".reg .b64 s1;\n\t"
+            "setp.ne.b32 q, %3, 0;\n\t"
+            "add.u32 t1, %0, %2;\n\t"
+            "add.u64 s1, %1, 32;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [t1], s1;\n\t"
+            "}\n"
+            ::"r"(taddr), "l"(desc), "r"(pitch), "r"(sel)
+            : "memory");
+    else if constexpr (CG == 2 && GROUPS == 4)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q;\n\t"
+            ".reg .b32 t1, t2, t3;\n\t"
+            ".reg .b64 s1, s2, s3;\n\t"
+            "setp.ne.b32 q, %3, 0;\n\t"
+            "add.u32 t1, %0, %2;\n\t"
+            "add.u64 s1, %1, 32;\n\t"
+            "add.u32 t2, t1, %2;\n\t"
+            "add.u64 s2, %1, 64;\n\t"
+            "add.u32 t3, t2, %2;\n\t"
+            "add.u64 s3, %1, 96;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [t1], s1;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [t2], s2;\n\t"
+            "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [t3], s3;\n\t"
+            "}\n"
+            ::"r"(taddr), "l"(desc), "r"(pitch), "r"(sel)
+            : "memory");
+}
+
+// The four K = 64 steps of one stage: D[tmem] (+)= (A[smem] sa) (B[smem] sb)^T.  sa / sb: scale columns of the first group, the next
+// groups' 4 / sb_pitch columns further.  Scales e8m0 (E8M0: a group serves two steps, the second starts at byte 2 of its words)
+// or e4m3 (a group per step).  CG = 2: rows from both blocks of a pair.
+template <int CG, bool E8M0>
+__device__ __forceinline__ void mma_fp4_stage(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t sb_pitch,
+                                              uint32_t acc, uint32_t sel)
+{
+    if constexpr (CG == 1 && E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p0, pt;\n\t"
+            ".reg .b32 u1, v1, i1;\n\t"
+            ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+            "setp.ne.b32 q, %8, 0;\n\t"
+            "setp.ne.b32 p0, %7, 0;\n\t"
+            "setp.eq.b32 pt, %8, %8;\n\t"
+            "add.u64 a1, %1, 2;\n\t"
+            "add.u64 b1, %2, 2;\n\t"
+            "add.u64 a2, %1, 4;\n\t"
+            "add.u64 b2, %2, 4;\n\t"
+            "add.u64 a3, %1, 6;\n\t"
+            "add.u64 b3, %2, 6;\n\t"
+            "or.b32 i1, %3, 0x40000020;\n\t"
+            "add.u32 u1, %4, 4;\n\t"
+            "add.u32 v1, %5, %6;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a1, b1, i1, [%4], [%5], pt;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a2, b2, %3, [u1], [v1], pt;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], a3, b3, i1, [u1], [v1], pt;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(sb_pitch), "r"(acc), "r"(sel)
+            : "memory");
+    else if constexpr (CG == 1 && !E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p0, pt;\n\t"
+            ".reg .b32 u1, u2, u3, v1, v2, v3;\n\t"
+            ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+            "setp.ne.b32 q, %8, 0;\n\t"
+            "setp.ne.b32 p0, %7, 0;\n\t"
+            "setp.eq.b32 pt, %8, %8;\n\t"
+            "add.u64 a1, %1, 2;\n\t"
+            "add.u64 b1, %2, 2;\n\t"
+            "add.u64 a2, %1, 4;\n\t"
+            "add.u64 b2, %2, 4;\n\t"
+            "add.u64 a3, %1, 6;\n\t"
+            "add.u64 b3, %2, 6;\n\t"
+            "add.u32 u1, %4, 4;\n\t"
+            "add.u32 u2, %4, 8;\n\t"
+            "add.u32 u3, %4, 12;\n\t"
+            "add.u32 v1, %5, %6;\n\t"
+            "add.u32 v2, v1, %6;\n\t"
+            "add.u32 v3, v2, %6;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a1, b1, %3, [u1], [v1], pt;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a2, b2, %3, [u2], [v2], pt;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a3, b3, %3, [u3], [v3], pt;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(sb_pitch), "r"(acc), "r"(sel)
+            : "memory");
+    else if constexpr (CG == 2 && E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p0, pt;\n\t"
+            ".reg .b32 u1, v1, i1;\n\t"
+            ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+            "setp.ne.b32 q, %8, 0;\n\t"
+            "setp.ne.b32 p0, %7, 0;\n\t"
+            "setp.eq.b32 pt, %8, %8;\n\t"
+            "add.u64 a1, %1, 2;\n\t"
+            "add.u64 b1, %2, 2;\n\t"
+            "add.u64 a2, %1, 4;\n\t"
+            "add.u64 b2, %2, 4;\n\t"
+            "add.u64 a3, %1, 6;\n\t"
+            "add.u64 b3, %2, 6;\n\t"
+            "or.b32 i1, %3, 0x40000020;\n\t"
+            "add.u32 u1, %4, 4;\n\t"
+            "add.u32 v1, %5, %6;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a1, b1, i1, [%4], [%5], pt;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a2, b2, %3, [u1], [v1], pt;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], a3, b3, i1, [u1], [v1], pt;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(sb_pitch), "r"(acc), "r"(sel)
+            : "memory");
+    else if constexpr (CG == 2 && !E8M0)
+        asm volatile(
+            "{\n\t"
+            ".reg .pred q, p0, pt;\n\t"
+            ".reg .b32 u1, u2, u3, v1, v2, v3;\n\t"
+            ".reg .b64 a1, a2, a3, b1, b2, b3;\n\t"
+            "setp.ne.b32 q, %8, 0;\n\t"
+            "setp.ne.b32 p0, %7, 0;\n\t"
+            "setp.eq.b32 pt, %8, %8;\n\t"
+            "add.u64 a1, %1, 2;\n\t"
+            "add.u64 b1, %2, 2;\n\t"
+            "add.u64 a2, %1, 4;\n\t"
+            "add.u64 b2, %2, 4;\n\t"
+            "add.u64 a3, %1, 6;\n\t"
+            "add.u64 b3, %2, 6;\n\t"
+            "add.u32 u1, %4, 4;\n\t"
+            "add.u32 u2, %4, 8;\n\t"
+            "add.u32 u3, %4, 12;\n\t"
+            "add.u32 v1, %5, %6;\n\t"
+            "add.u32 v2, v1, %6;\n\t"
+            "add.u32 v3, v2, %6;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a1, b1, %3, [u1], [v1], pt;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a2, b2, %3, [u2], [v2], pt;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], a3, b3, %3, [u3], [v3], pt;\n\t"
+            "}\n"
+            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(sb_pitch), "r"(acc), "r"(sel)
             : "memory");
 }
 
@@ -376,46 +528,6 @@ __device__ __forceinline__ void tmem_alloc_pair(uint32_t* slot, uint32_t cols)
 __device__ __forceinline__ void tmem_dealloc_pair(uint32_t base, uint32_t cols)
 {
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(base), "r"(cols) : "memory");
-}
-
-// The scale group at the same shared-memory place of both blocks -> each block's tensor memory.
-__device__ __forceinline__ void tmem_copy_scales_pair(uint32_t taddr, uint64_t desc, uint32_t sel)
-{
-    asm volatile(
-        "{\n\t"
-        ".reg .pred q;\n\t"
-        "setp.ne.b32 q, %2, 0;\n\t"
-        "@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t"
-        "}\n"
-        ::"r"(taddr), "l"(desc), "r"(sel)
-        : "memory");
-}
-
-// D (256 rows, 128 in each block) (+)= A (128 rows from each block) * B (half of its rows from each block)^T over 64 k.
-template <bool E8M0>
-__device__ __forceinline__ void mma_fp4_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sa, uint32_t sb,
-                                             uint32_t acc, uint32_t sel)
-{
-    if (E8M0)
-        asm volatile(
-            "{\n\t"
-            ".reg .pred q, p;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "setp.ne.b32 p, %6, 0;\n\t"
-            "@q tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
-            "}\n"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
-            : "memory");
-    else
-        asm volatile(
-            "{\n\t"
-            ".reg .pred q, p;\n\t"
-            "setp.ne.b32 q, %7, 0;\n\t"
-            "setp.ne.b32 p, %6, 0;\n\t"
-            "@q tcgen05.mma.cta_group::2.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t"
-            "}\n"
-            ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sa), "r"(sb), "r"(acc), "r"(sel)
-            : "memory");
 }
 
 // Arrive on the barrier at this place in both blocks once everything the acting lane has issued so far has finished.
