@@ -64,6 +64,43 @@ template <> struct Dt<float> {
     static __device__ __forceinline__ float down(float v) { return v; }
 };
 
+// 32 consecutive elements at p as fp32.  VEC: bytes per load that the row's alignment allows (32, 16, or 0: element
+// by element); n < 32 elements exist (the rest read as zero).
+template <typename T, int VEC> __device__ __forceinline__ void load32(const T* p, int n, float (&v)[32])
+{
+    constexpr int BYTES = 32 * (int)sizeof(T);
+    if (VEC >= 16 && n >= 32) {
+        uint32_t u[BYTES / 4];
+        if (VEC == 32) {
+#pragma unroll
+            for (int i = 0; i < BYTES / 32; ++i) {
+                const u32x8 w = ld_stream_256(reinterpret_cast<const uint8_t*>(p) + 32 * i);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) u[8 * i + k] = w.v[k];
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < BYTES / 16; ++i) {
+                const uint4 w = __ldg(reinterpret_cast<const uint4*>(p) + i);
+                u[4 * i] = w.x, u[4 * i + 1] = w.y, u[4 * i + 2] = w.z, u[4 * i + 3] = w.w;
+            }
+        }
+        if constexpr (sizeof(T) == 2) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 f = Dt<T>::up2(u[i]);
+                v[2 * i] = f.x, v[2 * i + 1] = f.y;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(u[i]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = i < n ? Dt<T>::up(p[i]) : 0.0f;
+}
+
 // ------------------------------------------------------- quantisation of one block
 
 // Eight fp32 -> eight e2m1 codes, first in the low nibble: nearest, ties to the even code, saturating at 6.

@@ -15,6 +15,9 @@ qmm_status launch_mx_quantize_experts(int fmt, int dtype, const void* x, int64_t
 qmm_status launch_mx_dequantize(int fmt, int dtype, const void* packed, int64_t rows, int64_t K, const float* ts, void* out, int64_t ldo, cudaStream_t st);
 qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale, int dtype, void* y,
                           int64_t ldy, int* status, cudaStream_t st);
+bool mx_few_fits(int fmt, int64_t M, int64_t K);
+qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
+                         const float* w_scale, void* y, int64_t ldy, int* status, cudaStream_t st);
 int64_t mx_max_row_units(int64_t pairs, int E);
 qmm_status launch_mx_experts_gate_up(int fmt, const void* a, int64_t pairs, int E, const int* offsets, const int* units, const void* w_gate, const void* w_up,
                                      int64_t N, int64_t K, const float* a_scale, const float* gate_scale, const float* up_scale, const float* h_scale, void* h,
@@ -221,6 +224,7 @@ qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int6
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
     QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_linear_workspace_bytes(fmt, M, N, K), 16));
     QMM_TRY(check_device(who));
+    if (mx_few_fits(fmt, M, K)) return launch_mx_few(fmt, dtype, X, ldx, M, w, N, K, x_scale, w_scale, Y, ldy, (int*)ws, (cudaStream_t)stream);
     void* a = (char*)ws + kMxStatusBytes;
     QMM_TRY(launch_mx_quantize(fmt, dtype, X, ldx, M, K, x_scale, a, true, (cudaStream_t)stream));
     return launch_mx_gemm(fmt, a, M, w, N, K, x_scale, w_scale, dtype, Y, ldy, (int*)ws, (cudaStream_t)stream);

@@ -45,19 +45,27 @@ struct MxGemmParams {
     void* y;                         // [rows, ldy], or the packed output operand (gate/up)
     int64_t ldy;
     int vec;                         // widest aligned store of Y: 32, 16 or 0 (element by element)
+    const void* x;                   // few: token rows as they come, [M, ldx] of Y's type
+    int64_t ldx, K;
+    int x_vec;                       // widest aligned load of x
+    int atoms, stages;               // few: 8-row atoms per unit (1 or 2), ring depth that the resident rows leave
     int* status;
 };
 
 constexpr int kMxMaxE = 1024;
 
-template <int FMT, int BN, bool GATEUP, bool GROUPED> struct MxGeom {
+// Forms of the kernel of one SM: packed token rows; packed rows grouped by expert; a few rows as they come.
+enum MxForm { kMxDense = 0, kMxGrouped = 1, kMxFew = 2 };
+
+template <int FMT, int BN, bool GATEUP, int FORM> struct MxGeom {
     static constexpr int NB = GATEUP ? 2 : 1;                                   // weight matrices
     static constexpr int kUnit = unit_bytes(FMT), kSc = scale_bytes(FMT);
     static constexpr bool kWhole = BN == 128;                                   // a tile's weights are whole units
     static constexpr int kWin = BN < 64 ? 64 : BN;                              // columns of one matrix's MMA: a tile of 32 rows is half of a window
                                                                                 // of 64 (scale columns are addressed in pairs), the other half is idle
     static constexpr int kCodes = kWin * 128;                                   // codes of one matrix in a stage
-    static constexpr int kW = kUnit, kScW = kW + NB * kCodes;                   // stage: token unit | codes of each matrix | scales of each
+    static constexpr int kW = FORM == kMxFew ? 0 : kUnit;                       // stage: token unit (few: none) | codes of each matrix | scales of each
+    static constexpr int kScW = kW + NB * kCodes;
     static constexpr int kStage = kScW + NB * kSc;
     static constexpr int kCodeStep = kCodes >> 4, kScStep = kSc >> 4;           // from matrix to matrix, in descriptor units
     static constexpr int kDCols = NB * kWin;
@@ -65,10 +73,12 @@ template <int FMT, int BN, bool GATEUP, bool GROUPED> struct MxGeom {
     static constexpr int kCols = GATEUP ? 32 : BN < 64 ? BN : 64;
     static constexpr int kParts = BN / kCols, kEpiWarps = 4 * kParts;
     static constexpr int kThreads = (4 + kEpiWarps) * 32;
-    static constexpr int kTail = 1024 + (GROUPED ? 2 * (kMxMaxE + 32) * 4 : 0);   // barriers, the experts' first units and rows
-    static constexpr int kFit = (227 * 1024 - 1024 - kTail) / kStage;
+    static constexpr int kHead = 1024 + (FORM == kMxGrouped ? 9 * 1024 : 0);    // barriers, the experts' first units and rows
+    static constexpr int kRoom = 227 * 1024 - 1024 - kHead;                     // for the ring (few: after the resident rows)
+    static constexpr int kFit = kRoom / kStage;
     static constexpr int kStages = kFit < 10 ? kFit : 10;
-    static constexpr int kSmem = 1024 + kStages * kStage + kTail;
+    static constexpr int kSmem = FORM == kMxFew ? 227 * 1024 : 1024 + kHead + kStages * kStage;
+    static_assert(2 * (kMxMaxE + 32) * 4 <= 9 * 1024, "index area");
     // tensor memory: accumulators (two when they fit), then two sets of scale columns
     static constexpr int kAccBufs = kDCols > 128 ? 1 : 2;
     static constexpr int kGroups = kUnitK / FMT / 4;                            // scale groups per unit: 2 or 4
@@ -142,30 +152,36 @@ __device__ __forceinline__ void mx_cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-template <int FMT, int BN, bool GATEUP, typename T, bool GROUPED>
-__global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1) mx_gemm_kernel(const MxGemmParams p)
+template <int FMT, int BN, bool GATEUP, typename T, int FORM>
+__global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx_gemm_kernel(const MxGemmParams p)
 {
     using namespace tc;
-    using G = MxGeom<FMT, BN, GATEUP, GROUPED>;
-    constexpr int S = G::kStages, AB = G::kAccBufs, NEPI = G::kEpiWarps, NB = G::NB;
+    using G = MxGeom<FMT, BN, GATEUP, FORM>;
+    constexpr bool GROUPED = FORM == kMxGrouped, FEW = FORM == kMxFew;
+    constexpr int AB = G::kAccBufs, NEPI = G::kEpiWarps, NB = G::NB;
     constexpr int W_WARP = 0, MMA_WARP = 1, A_WARP = 2, EPI_WARP0 = 4;         // loads of weights and of tokens are two warps
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * G::kStage);       // [S] loads -> MMA
-    uint64_t* empty = full + S;                                               // [S] MMA -> loads
-    uint64_t* acc_full = empty + S;                                           // [2] MMA -> epilogue
+    const int S = FEW ? p.stages : G::kStages;                                // ring depth, at most 10
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem);                       // [S] loads -> MMA
+    uint64_t* empty = full + 10;                                              // [S] MMA -> loads
+    uint64_t* acc_full = empty + 10;                                          // [2] MMA -> epilogue
     uint64_t* acc_empty = acc_full + 2;                                       // [2] epilogue -> MMA
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    int* s_units = reinterpret_cast<int*>(smem + S * G::kStage + 1024);       // [E + 1], then INT_MAX up to a multiple of 32 (grouped)
+    int* s_units = reinterpret_cast<int*>(smem + 1024);                       // [E + 1], then INT_MAX up to a multiple of 32 (grouped)
     int* s_first = s_units + kMxMaxE + 32;                                    // [E + 1]
-    const uint32_t smem0 = smem_u32(smem);
+    // few: the resident token rows, atoms of 8 rows x 128 bytes (p.atoms of them per k unit), then their scales, then the ring.  The MMA reads
+    // 128 rows from a unit's first atom: the rows past its own are whatever follows (never stored), inside the block's memory.
+    uint8_t* resident = smem + G::kHead;
+    const int resident_codes = FEW ? p.KU * p.atoms * 1024 : 0;
+    const uint32_t ring0 = smem_u32(resident) + (FEW ? resident_codes + p.KU * G::kSc : 0);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(&full[s], 2);
+            mbar_init(&full[s], FEW ? 1 : 2);                                 // the loading warps (+ their bytes)
             mbar_init(&empty[s], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -220,14 +236,44 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         return true;
     };
 
-    if (warp == W_WARP || warp == A_WARP) {
+    // few: the whole block quantises the token rows once (a thread per 32 elements), into the place and order in which a unit's codes and
+    // scales would have arrived; the MMA warp goes on when everybody has
+    auto load_tokens = [&]() {
+        pdl_wait();
+        if constexpr (FEW) {
+            const TensorScale ts(p.a_scale ? __ldg(p.a_scale) : 1.0f);
+            const int chunks = p.KU * (kUnitK / 32);
+            for (int id = threadIdx.x; id < p.M * chunks; id += G::kThreads) {
+                const int r = id / chunks, c = id - r * chunks, ku = c >> 3;
+                const int64_t left = p.K - (int64_t)c * 32;
+                const int n = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+                const T* src = reinterpret_cast<const T*>(p.x) + r * p.ldx + (int64_t)c * 32;
+                float v[32];
+                if (p.x_vec == 32) load32<T, 32>(src, n, v);
+                else if (p.x_vec == 16) load32<T, 16>(src, n, v);
+                else load32<T, 0>(src, n, v);
+                uint32_t sb;
+                const uint4 codes = quantize32<FMT>(v, ts, sb);
+                *reinterpret_cast<uint4*>(resident + (ku * p.atoms + (r >> 3)) * 1024 + chunk_offset(r & 7, c & 7)) = codes;
+                uint8_t* sc = resident + resident_codes + ku * G::kSc - kCodeBytes;
+                if (FMT == QMM_MXFP4) sc[scale_offset(r, (c & 7) >> 2) + (c & 3)] = (uint8_t)sb;
+                else *reinterpret_cast<uint16_t*>(sc + scale_offset(r, (c & 7) >> 1) + 2 * (c & 1)) = (uint16_t)sb;
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // ordinary stores, read by the tensor core
+            asm volatile("bar.sync 1, %0;" ::"n"(G::kThreads) : "memory");
+        }
+    };
+
+    if (FEW && warp > A_WARP && warp < EPI_WARP0) {
+        load_tokens();
+    } else if (warp == W_WARP || warp == A_WARP) {
         // ================= loads (whole warps converged, one lane acts); each warp's part counts on the stage's barrier
         const uint32_t sel = elect_one() ? 1u : 0u, full0 = smem_u32(full);
         bool ok = true;
-        int g = 0, early = 0;
+        int s = 0, round = 0, early = 0, g = 0;
         MxWork w = {};
         auto load_w = [&](int s, int ku) {
-            const uint32_t bar = full0 + 8 * s, dst = smem0 + s * G::kStage + G::kW;
+            const uint32_t bar = full0 + 8 * s, dst = ring0 + s * G::kStage + G::kW;
             const int r0 = w.n_tile * BN;
             const int64_t at = w.expert * p.w_stride + ((int64_t)(r0 >> 7) * p.KU + ku) * G::kUnit;
             mbar_arrive_expect_tx_sel(bar, NB * (BN * 128 + G::kSc), sel);
@@ -245,21 +291,21 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         if (!GROUPED) {
             if (warp == W_WARP && get_work(0, w))
                 for (; early < S && early < p.KU; ++early) load_w(early, early);
-            pdl_wait();
+            if (!FEW) pdl_wait();
         }
-        for (int i = 0; ok && get_work(i, w); ++i) {
+        if (FEW) load_tokens();
+        for (int i = 0; (!FEW || warp == W_WARP) && ok && get_work(i, w); ++i) {
             const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
             const uint8_t* src = p.a + (int64_t)w.m_unit * p.KU * G::kUnit;
-            for (int ku = 0; ku < p.KU; ++ku, ++g) {
-                const int s = g % S;
-                if (g >= S) ok = mbar_wait(&empty[s], ((g / S) - 1) & 1, abort_flag);
+            for (int ku = 0; ku < p.KU; ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
+                if (round > 0) ok = mbar_wait(&empty[s], (round - 1) & 1, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
-                if (warp == W_WARP) {
+                if (FEW || warp == W_WARP) {
                     if (g >= early) load_w(s, ku);
                     continue;
                 }
-                const uint32_t bar = full0 + 8 * s, dst = smem0 + s * G::kStage;
+                const uint32_t bar = full0 + 8 * s, dst = ring0 + s * G::kStage;
                 mbar_arrive_expect_tx_sel(bar, rows8 * 128u + G::kSc, sel);
                 if (rows8 == 128) {
                     bulk_load_sel(dst, src + (int64_t)ku * G::kUnit, G::kUnit, bar, sel);
@@ -280,11 +326,14 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
     } else if (warp == MMA_WARP) {
         // ================= MMA issuer (whole warp converged, one lane acts)
         const uint32_t sel = elect_one() ? 1u : 0u;
-        const uint64_t desc_a = smem_desc_k_sw128(smem0), desc_w = smem_desc_k_sw128(smem0 + G::kW);
-        const uint64_t desc_sa = smem_desc_scales(smem0 + kCodeBytes), desc_sw = smem_desc_scales(smem0 + G::kScW);
+        // token operand: in the stage, or resident (then a k unit is atoms * 1024 bytes of codes and kSc of scales further)
+        const uint64_t desc_a = smem_desc_k_sw128(FEW ? smem_u32(resident) : ring0), desc_w = smem_desc_k_sw128(ring0 + G::kW);
+        const uint64_t desc_sa = smem_desc_scales(FEW ? smem_u32(resident) + resident_codes : ring0 + kCodeBytes), desc_sw = smem_desc_scales(ring0 + G::kScW);
         bool ok = true;
-        int g = 0;
+        int s = 0;
+        uint32_t par = 0, set = 0;                                            // parity of the ring's round; set of scale columns
         MxWork w;
+        if (FEW) load_tokens();
         for (int it = 0; ok && get_work(it, w); ++it) {
             const int buf = it % AB;
             if (it >= AB) {
@@ -296,23 +345,23 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
             const uint32_t d = tmem_base + (uint32_t)(buf * G::kDCols);
             // a window of 64 rows takes the scale columns of its rows out of the unit's four (32 rows each)
             const uint32_t sub = BN < 128 ? (uint32_t)((w.n_tile * BN) & 64) >> 5 : 0u;
-            for (int ku = 0; ku < p.KU; ++ku, ++g) {
-                const int s = g % S;
-                ok = mbar_wait(&full[s], (g / S) & 1, abort_flag);
+            for (int ku = 0; ku < p.KU; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
+                ok = mbar_wait(&full[s], par, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
-                const uint32_t sfa = tmem_base + (uint32_t)(G::kSf0 + (g & 1) * G::kSfCols);
+                const uint64_t at_a = FEW ? (uint64_t)(ku * p.atoms * 64) : at, at_sa = FEW ? (uint64_t)(ku * (G::kSc >> 4)) : at;
+                const uint32_t sfa = tmem_base + (uint32_t)G::kSf0 + set * (uint32_t)G::kSfCols;
                 const uint32_t sfw = sfa + (uint32_t)(G::kGroups * 4);
-                copy_scales<1, G::kGroups>(sfa, desc_sa + at, 4, sel);
+                copy_scales<1, G::kGroups>(sfa, desc_sa + at_sa, 4, sel);
 #pragma unroll
                 for (int b = 0; b < NB; ++b) copy_scales<1, G::kGroups>(sfw + 4 * b, desc_sw + at + b * G::kScStep, 4 * NB, sel);
                 // two whole matrices are one MMA of N = 256 (their codes and their scale columns are adjacent), else one MMA each
                 constexpr int MMAS = G::kWhole ? 1 : NB;
 #pragma unroll
                 for (int b = 0; b < MMAS; ++b)
-                    mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
+                    mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at_a, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
                                                        sfa, sfw + 4 * b + sub, 4 * NB, ku != 0, sel);
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
@@ -329,7 +378,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, GROUPED>::kThreads, 1)
         bool ok = true;
         MxWork w;
         // every global write below comes after the previous kernel has completed (its readers of this buffer included)
-        if (!GROUPED) pdl_wait();
+        if (FEW) load_tokens();
+        else if (!GROUPED) pdl_wait();
         const float a_scale = p.a_scale ? __ldg(p.a_scale) : 1.0f;
         const TensorScale hs(GATEUP && p.h_scale ? __ldg(p.h_scale) : 1.0f);
         for (int it = 0; ok && get_work(it, w); ++it) {
@@ -624,11 +674,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
 
 // ------------------------------------------------------------ launches
 
-template <int FMT, int BN, bool GATEUP, typename T, bool GROUPED>
+template <int FMT, int BN, bool GATEUP, typename T, int FORM>
 static qmm_status launch_t(const MxGemmParams& p, int64_t tiles, cudaStream_t st)
 {
-    auto kern = mx_gemm_kernel<FMT, BN, GATEUP, T, GROUPED>;
-    using G = MxGeom<FMT, BN, GATEUP, GROUPED>;
+    auto kern = mx_gemm_kernel<FMT, BN, GATEUP, T, FORM>;
+    using G = MxGeom<FMT, BN, GATEUP, FORM>;
     static std::atomic<uint64_t> configured{0};                               // devices that have the attribute
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
@@ -651,6 +701,9 @@ static qmm_status launch_t(const MxGemmParams& p, int64_t tiles, cudaStream_t st
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, p), "microscaled product launch");
 }
 
+// Few rows: shared memory that M token rows take over all KU units.
+static int few_resident(int fmt, int64_t M, int KU) { return KU * ((int)((M + 7) / 8) * 1024 + scale_bytes(fmt)); }
+
 // Weight rows per tile (128, 64 or 32): the fewest rounds over the SMs, a tile of BN rows taken as BN + 24 (the token rows'
 // loads, the scales -- a tile loads its unit's 128 rows of them -- and the hand-over of the accumulators).
 static int mx_tile_rows(int64_t row_tiles, int64_t N)
@@ -666,14 +719,19 @@ static int mx_tile_rows(int64_t row_tiles, int64_t N)
     return best;
 }
 
-template <int FMT, bool GATEUP, typename T, bool GROUPED> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
+template <int FMT, bool GATEUP, typename T, int FORM> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
 {
     const int bn = mx_tile_rows(row_tiles, p.N);
     p.n_tiles = (p.N + bn - 1) / bn;
     const int64_t tiles = row_tiles * p.n_tiles;
-    if (bn == 128) return launch_t<FMT, 128, GATEUP, T, GROUPED>(p, tiles, st);
-    if (bn == 64) return launch_t<FMT, 64, GATEUP, T, GROUPED>(p, tiles, st);
-    return launch_t<FMT, 32, GATEUP, T, GROUPED>(p, tiles, st);
+    if (FORM == kMxFew) {
+        const int stage = (bn < 64 ? 64 : bn) * 128 + scale_bytes(FMT);
+        const int fit = (227 * 1024 - 2048 - few_resident(FMT, p.M, p.KU)) / stage;
+        p.stages = fit < 10 ? fit : 10;
+    }
+    if (bn == 128) return launch_t<FMT, 128, GATEUP, T, FORM>(p, tiles, st);
+    if (bn == 64) return launch_t<FMT, 64, GATEUP, T, FORM>(p, tiles, st);
+    return launch_t<FMT, 32, GATEUP, T, FORM>(p, tiles, st);
 }
 
 template <typename T> static int row_vec(const void* y, int64_t ldy)
@@ -723,7 +781,7 @@ template <int FMT, typename T> static qmm_status dense_t(MxGemmParams p, cudaStr
     // (the pair form's row coordinates are 32-bit: operands below 2^31 rows of 128 bytes)
     const bool fits = ((int64_t)p.n_tiles + (p.M + 127) / 128) * p.KU * (unit_bytes(FMT) / 128) < (1LL << 31);
     if (p.M > 128 && fits && g_knobs.mx_pair != 2 && (pair_tiles >= 32 || g_knobs.mx_pair == 1)) return launch_pair_t<FMT, T>(p, pair_tiles, st);
-    return launch_tiles<FMT, false, T, false>(p, (p.M + 127) / 128, st);
+    return launch_tiles<FMT, false, T, kMxDense>(p, (p.M + 127) / 128, st);
 }
 
 qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale,
@@ -744,6 +802,39 @@ qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int6
     if (fmt == QMM_MXFP4)
         return dtype == QMM_F16 ? dense_t<QMM_MXFP4, __half>(p, st) : dtype == QMM_BF16 ? dense_t<QMM_MXFP4, __nv_bfloat16>(p, st) : dense_t<QMM_MXFP4, float>(p, st);
     return dtype == QMM_F16 ? dense_t<QMM_NVFP4, __half>(p, st) : dtype == QMM_BF16 ? dense_t<QMM_NVFP4, __nv_bfloat16>(p, st) : dense_t<QMM_NVFP4, float>(p, st);
+}
+
+// Whether the product of a few rows can take them as they come (else they are quantised by a launch of their own).  Up to 16 rows and 112 KB (half of the ring's room): every block quantises all of them, which
+// for one token and a 2048 x 2048 matrix takes a launch and 2.9 us off the product.
+bool mx_few_fits(int fmt, int64_t M, int64_t K) { return M <= 16 && !g_knobs.mx_no_few && few_resident(fmt, M, (int)k_units(K)) <= 112 * 1024; }
+
+template <int FMT, typename T> static qmm_status few_t(MxGemmParams p, cudaStream_t st)
+{
+    p.vec = row_vec<T>(p.y, p.ldy);
+    p.x_vec = row_vec<T>(p.x, p.M > 1 ? p.ldx : 0);
+    p.atoms = (p.M + 7) / 8;
+    return launch_tiles<FMT, false, T, kMxFew>(p, 1, st);
+}
+
+qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
+                         const float* w_scale, void* y, int64_t ldy, int* status, cudaStream_t st)
+{
+    MxGemmParams p = {};
+    p.x = x;
+    p.ldx = ldx;
+    p.K = K;
+    p.w[0] = (const uint8_t*)w;
+    p.M = (int)M;
+    p.N = (int)N;
+    p.KU = (int)k_units(K);
+    p.a_scale = x_scale;
+    p.w_scale[0] = w_scale;
+    p.y = y;
+    p.ldy = ldy;
+    p.status = status;
+    if (fmt == QMM_MXFP4)
+        return dtype == QMM_F16 ? few_t<QMM_MXFP4, __half>(p, st) : dtype == QMM_BF16 ? few_t<QMM_MXFP4, __nv_bfloat16>(p, st) : few_t<QMM_MXFP4, float>(p, st);
+    return dtype == QMM_F16 ? few_t<QMM_NVFP4, __half>(p, st) : dtype == QMM_BF16 ? few_t<QMM_NVFP4, __nv_bfloat16>(p, st) : few_t<QMM_NVFP4, float>(p, st);
 }
 
 // Most row units that P pairs over E experts can take.
@@ -775,14 +866,14 @@ qmm_status launch_mx_experts_gate_up(int fmt, const void* a, int64_t pairs, int 
     p.y = h;
     p.status = status;
     const int64_t row_tiles = mx_max_row_units(pairs, E);
-    if (fmt == QMM_MXFP4) return launch_tiles<QMM_MXFP4, true, __half, true>(p, row_tiles, st);
-    return launch_tiles<QMM_NVFP4, true, __half, true>(p, row_tiles, st);
+    if (fmt == QMM_MXFP4) return launch_tiles<QMM_MXFP4, true, __half, kMxGrouped>(p, row_tiles, st);
+    return launch_tiles<QMM_NVFP4, true, __half, kMxGrouped>(p, row_tiles, st);
 }
 
 template <int FMT, typename T> static qmm_status grouped_t(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
 {
     p.vec = row_vec<T>(p.y, p.ldy);
-    return launch_tiles<FMT, false, T, true>(p, row_tiles, st);
+    return launch_tiles<FMT, false, T, kMxGrouped>(p, row_tiles, st);
 }
 
 qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, const int* offsets, const int* units, const void* w, int64_t N,

@@ -205,7 +205,7 @@ def test_product(qmm, fmt, M, N, K):
 @pytest.mark.parametrize("M", [1, 2, 3, 7, 8, 9, 16, 17, 31, 33, 64, 100, 128, 130, 256, 257, 400])
 def test_linear_is_quantize_then_product(qmm, fmt, M):
     """qmm_mx_linear gives the bits of qmm_mx_quantize followed by qmm_mx_gemm, whatever form it takes."""
-    for N, K in ((384, 800), (2048, 512), (200, 4096)):
+    for N, K in ((384, 800), (2048, 512), (200, 4096), (130, 9000)):
         (xa, _, ga), (xw, _, gw) = operands(fmt, M, N, K, M + N)
         wp = qmm.mx_quantize(fmt, xw.cuda(), tensor_scale=gw)
         for dt in DTYPES.values():
@@ -216,6 +216,15 @@ def test_linear_is_quantize_then_product(qmm, fmt, M):
             codes, scale = mxref.quantize(f64(X), fmt, 0.004)
             check_product(Y, mxref.values(codes, scale, fmt, K, 0.004), mxref.values(*mxref.quantize(f64(xw), fmt, 0.0003), fmt, K, 0.0003), K)
             assert torch.equal(Y, qmm.mx_gemm(fmt, qmm.mx_quantize(fmt, X, tensor_scale=ga), M, wp, N, K, a_scale=ga, w_scale=gw, dtype=dt))
+            for pitch, off in ((K + 8, 8), (K + 3, 1)):                            # rows that allow 16-byte and element-wise loads
+                view = torch.zeros(M * pitch + off, dtype=dt, device="cuda")[off:].view(M, pitch)[:, :K]
+                view.copy_(X)
+                assert torch.equal(Y, qmm.mx_linear(fmt, view, wp, N, x_scale=ga, w_scale=gw, ws=ws))
+            for rows in ("32", "64", "128"):
+                qmm.debug_config("mx_tile", rows)
+                assert torch.equal(Y, qmm.mx_linear(fmt, X, wp, N, x_scale=ga, w_scale=gw, ws=ws))
+            qmm.debug_config(None)
+            qmm.status_check(ws)
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -297,6 +306,15 @@ def test_offsets_past_32_bits(qmm):
     assert torch.equal(out, want)
     back = qmm.mx_dequantize(fmt, qmm.mx_quantize(fmt, view, tensor_scale=ga), 4, K, out=view, tensor_scale=ga)
     assert np.array_equal(f64(back), mxref.values(*mxref.quantize(f64(xa.half()), fmt, 0.004), fmt, K, 0.004).astype(np.float32).astype(np.float16).astype(np.float64))
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_nan_token_in_a_few_rows(qmm, fmt):
+    xw = torch.randn(256, 512, generator=torch.Generator().manual_seed(1)).cuda()
+    X = torch.randn(5, 512, generator=torch.Generator().manual_seed(2)).cuda()
+    X[3, 100] = float("inf")
+    Y = qmm.mx_linear(fmt, X, qmm.mx_quantize(fmt, xw), 256)
+    assert bool(torch.isnan(Y[3]).all()) and bool(torch.isfinite(Y[[0, 1, 2, 4]]).all())
 
 
 def test_no_rows(qmm):
