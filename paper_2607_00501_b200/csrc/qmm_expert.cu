@@ -72,10 +72,10 @@ __global__ void __launch_bounds__(kSortThreads) expert_count_kernel(const int* _
 // The rows before this chunk and the totals come from the other blocks of the cluster, through distributed shared memory
 // (CLUSTER: the whole sort is one launch of up to sixteen blocks), or from `counts` (many chunks).
 // Dynamic shared memory: [kSortWarps][E + 2] running counts.
+// s_place, s_offsets, s_units (optional, shared memory of one block): copies of place, offsets and units for what follows in the kernel.
 template <int ITEMS, bool CLUSTER>
-__global__ void __launch_bounds__(kSortThreads)
-expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, const int* __restrict__ counts, int* __restrict__ order,
-                    int* __restrict__ place, int* __restrict__ offsets, int* __restrict__ units)
+__device__ __forceinline__ void place_pairs(const int* __restrict__ idx, int64_t P, int E, int chunks, const int* __restrict__ counts, int* __restrict__ order,
+                                            int* __restrict__ place, int* __restrict__ offsets, int* __restrict__ units, int* s_place, int* s_offsets, int* s_unit0)
 {
     pdl_launch_dependents();
     extern __shared__ int run[];
@@ -203,6 +203,7 @@ expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, c
         if (blockIdx.x == 0) {
             offsets[e] = rows;
             units[e] = us;
+            if (s_offsets) s_offsets[e] = rows, s_unit0[e] = us;
             if (e == E - 1) {
                 offsets[E] = rows + total;
                 units[E] = us + nu;
@@ -225,6 +226,7 @@ expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, c
         const int in_bucket = mine[bucket[i]] + rank[i], row = base[bucket[i]] + in_bucket;
         const bool kept = bucket[i] < E;
         place[p] = kept ? row : -1;
+        if (s_place) s_place[p] = kept ? row : -1;
         if (ITEMS > 1) sorted[local[bucket[i]] + in_bucket] = make_int2(row, kept ? (int)p : -1);
         else order[row] = kept ? (int)p : -1;
     }
@@ -233,6 +235,51 @@ expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, c
         const int64_t left = P - (int64_t)blockIdx.x * (kSortThreads * ITEMS);
         const int n = (int)(left < kSortThreads * ITEMS ? left : kSortThreads * ITEMS);
         for (int q = threadIdx.x; q < n; q += kSortThreads) order[sorted[q].x] = sorted[q].y;
+    }
+}
+
+template <int ITEMS, bool CLUSTER>
+__global__ void __launch_bounds__(kSortThreads)
+expert_place_kernel(const int* __restrict__ idx, int64_t P, int E, int chunks, const int* __restrict__ counts, int* __restrict__ order,
+                    int* __restrict__ place, int* __restrict__ offsets, int* __restrict__ units)
+{
+    place_pairs<ITEMS, CLUSTER>(idx, P, E, chunks, counts, order, place, offsets, units, nullptr, nullptr, nullptr);
+}
+
+// The sort of a few pairs and the quantisation of their tokens in one block: the front of a decode step's routed layer, one launch
+// where two (each about as long as its latency) would follow one another.  A thread takes 32 elements of a token at a time and stores
+// them at the row of each of the token's pairs.
+template <int FMT, typename T>
+__global__ void __launch_bounds__(kSortThreads)
+expert_place_quantize_kernel(const int* __restrict__ idx, int P, int E, int topk, int* __restrict__ order, int* __restrict__ place, int* __restrict__ offsets,
+                             int* __restrict__ units, const T* __restrict__ x, int64_t ldx, int x_vec, int64_t K, const float* __restrict__ tensor_scale,
+                             uint8_t* __restrict__ packed)
+{
+    __shared__ int s_place[kSortThreads], s_offsets[1024], s_units[1024];
+    place_pairs<1, true>(idx, P, E, 1, nullptr, order, place, offsets, units, s_place, s_offsets, s_units);
+    __syncthreads();
+    const TensorScale ts(tensor_scale ? __ldg(tensor_scale) : 1.0f);
+    const int KU = (int)k_units(K), chunks = KU * (kUnitK / 32);
+    for (int id = threadIdx.x; id < P / topk * chunks; id += kSortThreads) {
+        const int t = id / chunks, c = id - t * chunks;
+        const int64_t left = K - (int64_t)c * 32;
+        const int n = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+        const T* src = x + t * ldx + (int64_t)c * 32;
+        float v[32];
+        if (x_vec == 32) load32<T, 32>(src, n, v);
+        else if (x_vec == 16) load32<T, 16>(src, n, v);
+        else load32<T, 0>(src, n, v);
+        uint32_t sb;
+        const uint4 codes = quantize32<FMT>(v, ts, sb);
+        for (int j = 0; j < topk; ++j) {
+            const int r = s_place[t * topk + j];
+            if (r < 0) continue;
+            const int e = __ldg(idx + t * topk + j), slot = s_units[e] * 128 + r - s_offsets[e];
+            uint8_t* unit = packed + ((int64_t)(slot >> 7) * KU + (c >> 3)) * unit_bytes(FMT);
+            *reinterpret_cast<uint4*>(unit + chunk_offset(slot & 127, c & 7)) = codes;
+            if (FMT == QMM_MXFP4) unit[scale_offset(slot & 127, (c & 7) >> 2) + (c & 3)] = (uint8_t)sb;
+            else *reinterpret_cast<uint16_t*>(unit + scale_offset(slot & 127, (c & 7) >> 1) + 2 * (c & 1)) = (uint16_t)sb;
+        }
     }
 }
 
@@ -281,6 +328,43 @@ qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int*
     if (items <= 2) return launch_place<2, true>(a, kSortCluster, st);
     if (items <= 4) return launch_place<4, true>(a, kSortCluster, st);
     return launch_place<8, true>(a, kSortCluster, st);
+}
+
+// Whether sort and quantisation of a layer's tokens are one launch: one block's worth of pairs, and at most two passes of its threads over the
+// tokens' 32-element chunks.
+bool expert_sort_quantize_fits(int64_t P, int topk, int64_t K) { return P <= kSortThreads && P / topk * k_units(K) * (kUnitK / 32) <= 2 * kSortThreads; }
+
+template <int FMT, typename T> static qmm_status sort_quantize_t(const SortArgs& a, int topk, const void* x, int64_t ldx, int64_t K, const float* ts, void* packed, cudaStream_t st)
+{
+    const size_t smem = (size_t)((kSortWarps * (a.E + 2) + 1) & ~1) * 4;
+    auto kern = expert_place_quantize_kernel<FMT, T>;
+    static std::atomic<uint64_t> configured{0};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
+    const uint64_t bit = dev < 64 ? (1ull << dev) : 0;
+    if (!(configured.load(std::memory_order_relaxed) & bit)) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kSortWarps * 1026 * 4);
+        if (e != cudaSuccess) return check_cuda(e, "expert sort and quantisation attributes");
+        configured.fetch_or(bit, std::memory_order_relaxed);
+    }
+    const uintptr_t bits = reinterpret_cast<uintptr_t>(x) | (uintptr_t)(ldx * (int64_t)sizeof(T));
+    const int vec = bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : 0;
+    return launch_pdl(kern, dim3(1), kSortThreads, smem, 1, st, "expert sort and quantisation launch", a.idx, (int)a.P, a.E, topk, a.order, a.place, a.offsets, a.units,
+                      (const T*)x, ldx, vec, K, ts, (uint8_t*)packed);
+}
+
+qmm_status launch_expert_sort_quantize(int fmt, int dtype, const int* idx, int64_t P, int topk, int E, int* order, int* place, int* offsets, int* units,
+                                       const void* x, int64_t ldx, int64_t K, const float* ts, void* packed, cudaStream_t st)
+{
+    const SortArgs a = {idx, P, E, order, place, offsets, units, nullptr};
+    if (fmt == QMM_MXFP4) {
+        if (dtype == QMM_F16) return sort_quantize_t<QMM_MXFP4, __half>(a, topk, x, ldx, K, ts, packed, st);
+        if (dtype == QMM_BF16) return sort_quantize_t<QMM_MXFP4, __nv_bfloat16>(a, topk, x, ldx, K, ts, packed, st);
+        return sort_quantize_t<QMM_MXFP4, float>(a, topk, x, ldx, K, ts, packed, st);
+    }
+    if (dtype == QMM_F16) return sort_quantize_t<QMM_NVFP4, __half>(a, topk, x, ldx, K, ts, packed, st);
+    if (dtype == QMM_BF16) return sort_quantize_t<QMM_NVFP4, __nv_bfloat16>(a, topk, x, ldx, K, ts, packed, st);
+    return sort_quantize_t<QMM_NVFP4, float>(a, topk, x, ldx, K, ts, packed, st);
 }
 
 // ------------------------------------------------------------- row moves

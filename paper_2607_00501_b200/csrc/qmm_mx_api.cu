@@ -26,6 +26,9 @@ qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, 
                                   const float* a_scale, const float* w_scale, int dtype, void* y, int64_t ldy, int* status, cudaStream_t st);
 size_t expert_sort_workspace_bytes(int64_t P, int E);
 qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int* place, int* offsets, int* units, void* ws, cudaStream_t st);
+bool expert_sort_quantize_fits(int64_t P, int topk, int64_t K);
+qmm_status launch_expert_sort_quantize(int fmt, int dtype, const int* idx, int64_t P, int topk, int E, int* order, int* place, int* offsets, int* units,
+                                       const void* x, int64_t ldx, int64_t K, const float* ts, void* packed, cudaStream_t st);
 qmm_status launch_expert_gather(int dtype, const void* x, int64_t ldx, int T, int topk, int64_t H, const int* order, const int* place, const float* weights,
                                 void* xs, int64_t ldxs, cudaStream_t st);
 qmm_status launch_expert_combine(int dtype, const void* ys, int64_t ldys, int T, int topk, int64_t H, const int* place, const float* weights, void* y, int64_t ldy,
@@ -384,8 +387,13 @@ qmm_status qmm_mx_moe(const qmm_mx_moe_args* a, void* ws, size_t ws_bytes, void*
     char* base = (char*)ws;
     int *order = (int*)(base + l.order), *place = (int*)(base + l.place), *offsets = (int*)(base + l.offsets), *units = (int*)(base + l.units);
     const int64_t P = (int64_t)a->T * a->topk;
-    QMM_TRY(launch_expert_sort(a->idx, P, a->E, order, place, offsets, units, base + l.sort, st));
-    QMM_TRY(launch_mx_quantize_experts(a->fmt, a->dtype, a->X, a->ldx, a->T, a->topk, a->E, a->H, a->idx, place, offsets, units, a->x_scale, base + l.xq, true, st));
+    if (expert_sort_quantize_fits(P, a->topk, a->H)) {
+        QMM_TRY(launch_expert_sort_quantize(a->fmt, a->dtype, a->idx, P, a->topk, a->E, order, place, offsets, units, a->X, a->ldx, a->H, a->x_scale, base + l.xq, st));
+    } else {
+        QMM_TRY(launch_expert_sort(a->idx, P, a->E, order, place, offsets, units, base + l.sort, st));
+        QMM_TRY(launch_mx_quantize_experts(a->fmt, a->dtype, a->X, a->ldx, a->T, a->topk, a->E, a->H, a->idx, place, offsets, units, a->x_scale, base + l.xq, true,
+                                           st));
+    }
     QMM_TRY(launch_mx_experts_gate_up(a->fmt, base + l.xq, P, a->E, offsets, units, a->w_gate, a->w_up, a->I, a->H, a->x_scale, a->gate_scale, a->up_scale,
                                       a->h_scale, base + l.h, (int*)ws, st));
     QMM_TRY(launch_mx_experts_gemm(a->fmt, base + l.h, P, a->E, offsets, units, a->w_down, a->H, a->I, a->h_scale, a->down_scale, a->dtype, base + l.d, a->H,

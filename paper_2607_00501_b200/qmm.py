@@ -414,9 +414,18 @@ class Chain:
 
 def _rows2d(t: torch.Tensor, what: str):
     """(pointer, row pitch, rows, columns) of a 2-D CUDA tensor whose rows are contiguous."""
-    shape, stride = t.shape, t.stride()
-    assert t.is_cuda and len(shape) == 2 and (stride[1] == 1 or shape[1] <= 1), "%s: 2-D CUDA tensor with contiguous rows" % what
-    return t.data_ptr(), max(stride[0], shape[1]) if shape[0] <= 1 else stride[0], shape[0], shape[1]
+    assert t.is_cuda and t.dim() == 2, "%s: 2-D CUDA tensor" % what
+    rows, cols = t.shape
+    ld, inner = t.stride()
+    assert inner == 1 or cols <= 1, "%s: rows must be contiguous" % what
+    return t.data_ptr(), ld if rows > 1 or ld > cols else cols, rows, cols
+
+
+def _mx_need(fmt: int, rows: int, K: int) -> int:
+    """mx_bytes, for the two formats without a call into the library: the size that a packed argument has to have."""
+    if fmt != MXFP4 and fmt != NVFP4:
+        return lib().qmm_mx_bytes(fmt, rows, K)
+    return ((rows + 127) >> 7) * ((K + 255) >> 8) * (16384 + 32768 // fmt)
 
 
 def _scalar(t, n: int = 1) -> int:
@@ -465,11 +474,11 @@ def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: to
 def mx_quantize(fmt: int, x: torch.Tensor, out: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None) -> torch.Tensor:
     """x [rows, K] (fp16, bf16 or fp32; any row stride) -> packed operand, uint8."""
     ptr, ld, rows, K = _rows2d(x, "x")
-    need = lib().qmm_mx_bytes(fmt, rows, K)
+    L = lib()
     if out is None:
-        out = torch.empty(need, dtype=torch.uint8, device=x.device)
-    dst = _operand(out, need, "out") if rows else 0
-    _check(_lib.qmm_mx_quantize(fmt, DTYPES[x.dtype], ptr, ld, rows, K, _scalar(tensor_scale), dst, _stream()))
+        out = torch.empty(L.qmm_mx_bytes(fmt, rows, K), dtype=torch.uint8, device=x.device)
+    dst = _operand(out, _mx_need(fmt, rows, K), "out") if rows else 0
+    _check(L.qmm_mx_quantize(fmt, DTYPES[x.dtype], ptr, ld, rows, K, _scalar(tensor_scale), dst, _stream()))
     return out
 
 
@@ -480,7 +489,7 @@ def mx_dequantize(fmt: int, packed: torch.Tensor, rows: int, K: int, out: torch.
         out = torch.empty((rows, K), dtype=dtype, device=packed.device)
     ptr, ld, r, k = _rows2d(out, "out")
     assert (r, k) == (rows, K)
-    src = _operand(packed, lib().qmm_mx_bytes(fmt, rows, K), "packed") if rows else 0
+    src = _operand(packed, _mx_need(fmt, rows, K), "packed") if rows else 0
     _check(lib().qmm_mx_dequantize(fmt, src, rows, K, _scalar(tensor_scale), DTYPES[out.dtype], ptr, ld, _stream()))
     return out
 
@@ -499,7 +508,7 @@ def mx_gemm(fmt: int, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int, 
     ptr, ld, r, c = _rows2d(Y, "Y")
     assert (r, c) == (M, N)
     ws = _workspace(L.qmm_mx_gemm_workspace_bytes(fmt, M, N, K), a.device, ws)
-    _check(L.qmm_mx_gemm(fmt, _operand(a, L.qmm_mx_bytes(fmt, M, K), "a") if M else 0, M, _operand(w, L.qmm_mx_bytes(fmt, N, K), "w"), N, K,
+    _check(L.qmm_mx_gemm(fmt, _operand(a, _mx_need(fmt, M, K), "a") if M else 0, M, _operand(w, _mx_need(fmt, N, K), "w"), N, K,
                          _scalar(a_scale), _scalar(w_scale), DTYPES[Y.dtype], ptr, ld, ws.data_ptr(), _nbytes(ws), _stream()))
     return Y
 
@@ -519,8 +528,8 @@ def mx_linear(fmt: int, X: torch.Tensor, w: torch.Tensor, N: int, Y: torch.Tenso
     assert (r, c) == (M, N) and Y.dtype == X.dtype
     if ws is None:
         ws = _workspace(L.qmm_mx_linear_workspace_bytes(fmt, M, N, K), X.device, ws)
-    _check(L.qmm_mx_linear(fmt, DTYPES[X.dtype], xp, ldx, M, _operand(w, L.qmm_mx_bytes(fmt, N, K), "w"), N, K, _scalar(x_scale),
-                           _scalar(w_scale), yp, ldy, ws.data_ptr(), _nbytes(ws), _stream()))
+    _check(L.qmm_mx_linear(fmt, DTYPES[X.dtype], xp, ldx, M, _operand(w, _mx_need(fmt, N, K), "w"), N, K, _scalar(x_scale),
+                           _scalar(w_scale), yp, ldy, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
     return Y
 
 
@@ -658,7 +667,7 @@ def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int,
     assert idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape[0] == T
     assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape == idx.shape
     assert (r, c) == (T, H) and out.dtype == X.dtype
-    gu, dn = E * mx_bytes(fmt, I, H), E * mx_bytes(fmt, H, I)
+    gu, dn = E * _mx_need(fmt, I, H), E * _mx_need(fmt, H, I)
     a = MxMoeArgs(T, H, I, E, topk, fmt, DTYPES[X.dtype], xp, ldx, idx.data_ptr(), weights.data_ptr(), _operand(w_gate, gu, "w_gate"),
                   _operand(w_up, gu, "w_up"), _operand(w_down, dn, "w_down"), _scalar(x_scale), _scalar(h_scale), _scalar(gate_scale, E),
                   _scalar(up_scale, E), _scalar(down_scale, E), op, ldo)
