@@ -557,7 +557,7 @@ qmm_status qmm_status_check(void* ws, void* stream);
  *   "moe_no_fuse"      "1"             decode-sized qmm_moe as separate route / product / combine launches
  *   "mx_pair"          "1" | "2"       microscaled products of more than 128 tokens on pairs of SMs: always | never
  *   "mx_no_few"        "1"             qmm_mx_linear of few rows through a quantisation launch of its own
- *   "mx_tile"          "32|64|128"     weight rows per tile of the other microscaled products
+ *   "mx_tile"          "64" | "128"    weight rows per matrix and tile of the microscaled gate/up product
  */
 qmm_status qmm_debug_config(const char* name, const char* value);
 

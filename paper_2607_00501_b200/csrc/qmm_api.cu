@@ -399,9 +399,9 @@ qmm_status qmm_debug_config(const char* name, const char* value)
         return QMM_OK;
     }
     if (strcmp(name, "mx_tile") == 0) {
-        if (!off && strcmp(value, "32") != 0 && strcmp(value, "64") != 0 && strcmp(value, "128") != 0)
-            return fail(QMM_ERR_INVALID_ARG, "qmm_debug_config: mx_tile wants 32, 64 or 128");
-        g_knobs.mx_tile = off ? 0 : (value[0] == '3' ? 32 : value[0] == '6' ? 64 : 128);
+        if (!off && strcmp(value, "64") != 0 && strcmp(value, "128") != 0)
+            return fail(QMM_ERR_INVALID_ARG, "qmm_debug_config: mx_tile wants 64 or 128");
+        g_knobs.mx_tile = off ? 0 : (value[0] == '6' ? 64 : 128);
         return QMM_OK;
     }
     int* flag = strcmp(name, "gemv_no_cluster") == 0    ? &g_knobs.gemv_no_cluster

@@ -16,8 +16,7 @@
 // Roles: warps 0 and 2 load weights and tokens, warp 1 issues copies of scales and MMAs (converged, one elected lane), warps 4.. run
 // the epilogue: they take the accumulators into registers at once, free them, then work and store while the next tile's
 // MMAs run.  The kernel is persistent over tiles, ring and barrier phases run on across them.
-// Tile t = (token tile t / n_tiles, weight tile t % n_tiles).  BN = 128, 64 or 32: few weight rows per tile where whole tiles would
-// leave SMs idle.  (A K split with sums joined through a cluster's shared memory was slower: 8.8 us against 6 for one
+// Tile t = (token tile t / n_tiles, weight tile t % n_tiles).  BN = 128; 64 in the gate/up form of few rows.  (A K split with sums joined through a cluster's shared memory was slower: 8.8 us against 6 for one
 // token and a 2048 x 2048 matrix -- clusters of eight do not all fit the GPU at once, and their launch costs 3 us.)
 // Grouped: token tiles of the experts' rows, from the device arrays units[] / offsets[].
 // Every mbarrier wait is bounded; on give-up the block records QMM_ERR_DEVICE_TIMEOUT, waits (bounded) for its copies
@@ -44,11 +43,12 @@ struct MxGemmParams {
     const float* h_scale;            // gate/up: tensor scale of the output operand
     void* y;                         // [rows, ldy], or the packed output operand (gate/up)
     int64_t ldy;
-    int vec;                         // widest aligned store of Y: 32, 16 or 0 (element by element)
+    int vec;                         // widest aligned store of Y: 32, 16, 4 or 2 bytes
     const void* x;                   // few: token rows as they come, [M, ldx] of Y's type
     int64_t ldx, K;
     int x_vec;                       // widest aligned load of x
-    int atoms, stages;               // few: 8-row atoms per unit (1 or 2), ring depth that the resident rows leave
+    int atoms;                       // few: 8-row atoms per unit (1 or 2)
+    int stages;                      // ring depth (what resident rows or staging leave)
     int* status;
 };
 
@@ -57,27 +57,29 @@ constexpr int kMxMaxE = 1024;
 // Forms of the kernel of one SM: packed token rows; packed rows grouped by expert; a few rows as they come.
 enum MxForm { kMxDense = 0, kMxGrouped = 1, kMxFew = 2 };
 
+// Shared memory of an epilogue warp that writes rows of any alignment: 32 rows of 32 words, one word apart.
+constexpr int kRowStaging = 32 * 33 * 4;
+
 template <int FMT, int BN, bool GATEUP, int FORM> struct MxGeom {
     static constexpr int NB = GATEUP ? 2 : 1;                                   // weight matrices
     static constexpr int kUnit = unit_bytes(FMT), kSc = scale_bytes(FMT);
     static constexpr bool kWhole = BN == 128;                                   // a tile's weights are whole units
-    static constexpr int kWin = BN < 64 ? 64 : BN;                              // columns of one matrix's MMA: a tile of 32 rows is half of a window
-                                                                                // of 64 (scale columns are addressed in pairs), the other half is idle
-    static constexpr int kCodes = kWin * 128;                                   // codes of one matrix in a stage
+    static constexpr int kCodes = BN * 128;                                     // codes of one matrix in a stage
     static constexpr int kW = FORM == kMxFew ? 0 : kUnit;                       // stage: token unit (few: none) | codes of each matrix | scales of each
     static constexpr int kScW = kW + NB * kCodes;
     static constexpr int kStage = kScW + NB * kSc;
     static constexpr int kCodeStep = kCodes >> 4, kScStep = kSc >> 4;           // from matrix to matrix, in descriptor units
-    static constexpr int kDCols = NB * kWin;
+    static constexpr int kDCols = NB * BN;
     // columns per epilogue warp: 32 of each matrix in the gate/up form (its arithmetic wants warps), else up to 64
-    static constexpr int kCols = GATEUP ? 32 : BN < 64 ? BN : 64;
+    static constexpr int kCols = GATEUP ? 32 : 64;
     static constexpr int kParts = BN / kCols, kEpiWarps = 4 * kParts;
     static constexpr int kThreads = (4 + kEpiWarps) * 32;
     static constexpr int kHead = 1024 + (FORM == kMxGrouped ? 9 * 1024 : 0);    // barriers, the experts' first units and rows
+    static constexpr int kStaging = GATEUP ? 0 : kEpiWarps * kRowStaging;       // after the ring, for rows that 16-byte stores cannot reach
     static constexpr int kRoom = 227 * 1024 - 1024 - kHead;                     // for the ring (few: after the resident rows)
     static constexpr int kFit = kRoom / kStage;
     static constexpr int kStages = kFit < 10 ? kFit : 10;
-    static constexpr int kSmem = FORM == kMxFew ? 227 * 1024 : 1024 + kHead + kStages * kStage;
+    static constexpr int kSmem = GATEUP ? 1024 + kHead + kStages * kStage : 227 * 1024;
     static_assert(2 * (kMxMaxE + 32) * 4 <= 9 * 1024, "index area");
     // tensor memory: accumulators (two when they fit), then two sets of scale columns
     static constexpr int kAccBufs = kDCols > 128 ? 1 : 2;
@@ -119,11 +121,11 @@ __device__ __forceinline__ float2 silu_mul2(float2 g, float2 u, float c, float a
     return mul2(mul2(mul2(g, both(ab)), u), make_float2(rcp_approx(den.x), rcp_approx(den.y)));
 }
 
-// 32 consecutive outputs of one row; n = how many exist.  vec: widest store (bytes) that the rows' alignment allows; 32-byte
-// stores write whole sectors (a lane's neighbours in a store are other rows).
+// 32 consecutive outputs of one row; n = how many exist.  vec: 32 or 16 byte stores (32 writes whole sectors: a lane's neighbours in a
+// store are other rows).
 template <typename T> __device__ __forceinline__ void store32(T* o, const float (&v)[32], int n, int vec)
 {
-    if (vec && n >= 32) {
+    if (n >= 32) {
         constexpr int W = 8 * (int)sizeof(T);
         uint32_t u[W];
         if constexpr (sizeof(T) == 2) {
@@ -147,6 +149,33 @@ template <typename T> __device__ __forceinline__ void store32(T* o, const float 
         if (i < n) o[i] = Dt<T>::down(v[i]);
 }
 
+// 32 rows (a lane each, `rows` of them exist; y: row 0) x 32 columns from n0 of a matrix whose rows start anywhere: through shared memory, so that
+// a store instruction writes consecutive elements of one row.  (Element by element from the row's own lane, 128 x 300 took 20 us, so 3.)
+template <typename T>
+__device__ __forceinline__ void store_rows_any(uint32_t* staging, T* y, int64_t ldy, const uint32_t (&v)[32], float alpha, int lane, int rows, int n0, int N, int vec)
+{
+    __syncwarp();                                                             // (the previous columns have been read)
+    constexpr int W = 8 * (int)sizeof(T);                                     // words of a row
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (sizeof(T) == 2) staging[lane * 33 + i] = Dt<T>::down2(alpha * __uint_as_float(v[2 * i]), alpha * __uint_as_float(v[2 * i + 1]));
+        else staging[lane * 33 + i] = __float_as_uint(alpha * __uint_as_float(v[i]));
+    }
+    __syncwarp();
+    const int left = min(32, N - n0);
+    if (sizeof(T) == 2 && vec >= 4) {                                         // two elements per lane, two rows per instruction
+        const int c = 2 * (lane & 15);
+        for (int r = lane >> 4; r < rows; r += 2) {
+            const uint32_t u = staging[r * 33 + (lane & 15)];
+            T* o = y + r * ldy + n0 + c;
+            if (c + 2 <= left) *reinterpret_cast<uint32_t*>(o) = u;
+            else if (c < left) *reinterpret_cast<unsigned short*>(o) = (unsigned short)u;
+        }
+    } else if (lane < left) {
+        for (int r = 0; r < rows; ++r) y[r * ldy + n0 + lane] = reinterpret_cast<const T*>(staging + r * 33)[lane];
+    }
+}
+
 __device__ __forceinline__ void mx_cluster_sync()
 {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -163,7 +192,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    const int S = FEW ? p.stages : G::kStages;                                // ring depth, at most 10
+    const int S = p.stages;                                                   // ring depth, at most 10
     uint64_t* full = reinterpret_cast<uint64_t*>(smem);                       // [S] loads -> MMA
     uint64_t* empty = full + 10;                                              // [S] MMA -> loads
     uint64_t* acc_full = empty + 10;                                          // [2] MMA -> epilogue
@@ -276,13 +305,13 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             const uint32_t bar = full0 + 8 * s, dst = ring0 + s * G::kStage + G::kW;
             const int r0 = w.n_tile * BN;
             const int64_t at = w.expert * p.w_stride + ((int64_t)(r0 >> 7) * p.KU + ku) * G::kUnit;
-            mbar_arrive_expect_tx_sel(bar, NB * (BN * 128 + G::kSc), sel);
+            mbar_arrive_expect_tx_sel(bar, NB * (G::kCodes + G::kSc), sel);
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if (G::kWhole && NB == 1) {                                   // codes and scales in one copy
                     bulk_load_sel(dst, p.w[b] + at, G::kUnit, bar, sel);
                 } else {
-                    bulk_load_sel(dst + b * G::kCodes + (r0 & (G::kWin - 1)) * 128, p.w[b] + at + (r0 & 127) * 128, BN * 128, bar, sel);
+                    bulk_load_sel(dst + b * G::kCodes, p.w[b] + at + (r0 & 127) * 128, G::kCodes, bar, sel);
                     bulk_load_sel(dst + NB * G::kCodes + b * G::kSc, p.w[b] + at + kCodeBytes, G::kSc, bar, sel);
                 }
             }
@@ -343,7 +372,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                 tc_fence_after_sync();
             }
             const uint32_t d = tmem_base + (uint32_t)(buf * G::kDCols);
-            // a window of 64 rows takes the scale columns of its rows out of the unit's four (32 rows each)
+            // a tile of 64 rows takes the scale columns of its rows out of the unit's four (32 rows each)
             const uint32_t sub = BN < 128 ? (uint32_t)((w.n_tile * BN) & 64) >> 5 : 0u;
             for (int ku = 0; ku < p.KU; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
                 ok = mbar_wait(&full[s], par, abort_flag);
@@ -361,7 +390,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                 constexpr int MMAS = G::kWhole ? 1 : NB;
 #pragma unroll
                 for (int b = 0; b < MMAS; ++b)
-                    mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * G::kWin, desc_a + at_a, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
+                    mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * BN, desc_a + at_a, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
                                                        sfa, sfw + 4 * b + sub, 4 * NB, ku != 0, sel);
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
@@ -396,7 +425,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             if (warp_has_rows) {
 #pragma unroll
                 for (int c = 0; c < NB * C32; ++c)
-                    tmem_ld_32x32b_x32(lanes + (uint32_t)(buf * G::kDCols + (c / C32) * G::kWin + (c % C32) * 32 + (w.n_tile * BN & (G::kWin - 1))), v[c]);
+                    tmem_ld_32x32b_x32(lanes + (uint32_t)(buf * G::kDCols + (c / C32) * BN + (c % C32) * 32), v[c]);
                 tmem_wait_ld();
             }
             tc_fence_before_sync();
@@ -436,7 +465,13 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                         for (int k = p.n_tiles * BN; k < hku * kUnitK; k += 32) put(k, make_uint4(0, 0, 0, 0), 0);    // the rest of the last unit
                 }
             } else {
-                if (r < w.rows) {
+                if (p.vec < 16) {
+                    uint32_t* staging = reinterpret_cast<uint32_t*>(smem_raw + G::kSmem - G::kStaging + (warp - EPI_WARP0) * kRowStaging);
+#pragma unroll
+                    for (int c = 0; c < C32; ++c)
+                        store_rows_any(staging, reinterpret_cast<T*>(p.y) + (int64_t)(w.row0 + quarter * 32) * p.ldy, p.ldy, v[c], alpha, lane,
+                                       min(32, w.rows - quarter * 32), n0 + 32 * c, p.N, p.vec);
+                } else if (r < w.rows) {
                     T* o = reinterpret_cast<T*>(p.y) + (int64_t)(w.row0 + r) * p.ldy + n0;
 #pragma unroll
                     for (int c = 0; c < C32; ++c) {
@@ -478,13 +513,17 @@ template <int FMT> struct MxPairGeom {
     static constexpr int kSc = scale_bytes(FMT);
     static constexpr int kA = 0, kB = unit_bytes(FMT), kSb = kB + kCodeBytes;              // A unit | B codes | scales of both B units
     static constexpr int kStage = kSb + 2 * kSc;
-    static constexpr int kFit = (227 * 1024 - 2048) / kStage;
-    static constexpr int kStages = kFit < 6 ? kFit : 6;
-    static constexpr int kSmem = 2048 + kStages * kStage;
+    static constexpr int kStaging = 8 * kRowStaging;                                       // at the end, for rows that 16-byte stores cannot reach
+    static constexpr int kSmem = 227 * 1024;
+    static constexpr int stages(bool staging)
+    {
+        const int fit = (kSmem - 2048 - (staging ? kStaging : 0)) / kStage;
+        return fit < 6 ? fit : 6;
+    }
     static constexpr int kGroups = kUnitK / FMT / 4;
     static constexpr int kSf0 = 256, kSfCols = kGroups * 12;
     static constexpr int kThreads = 12 * 32;
-    static_assert(kSf0 + 2 * kSfCols <= 512 && kStages >= 4, "tensor memory or shared memory over-subscribed");
+    static_assert(kSf0 + 2 * kSfCols <= 512 && stages(true) >= 4, "tensor memory or shared memory over-subscribed");
 };
 
 struct MxPairMaps {
@@ -506,17 +545,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
 {
     using namespace tc;
     using G = MxPairGeom<FMT>;
-    constexpr int S = G::kStages, UNIT = unit_bytes(FMT);
+    constexpr int UNIT = unit_bytes(FMT);
+    const int S = p.stages;                                                   // ring depth, at most 6
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* full = reinterpret_cast<uint64_t*>(smem + S * G::kStage);       // [S] loads of both blocks -> MMA (first block)
-    uint64_t* empty = full + S;                                               // [S] MMA -> loads
-    uint64_t* acc_full = empty + S;                                           // MMA -> epilogue
+    uint64_t* full = reinterpret_cast<uint64_t*>(smem);                       // [S] loads of both blocks -> MMA (first block)
+    uint64_t* empty = full + 6;                                               // [S] MMA -> loads
+    uint64_t* acc_full = empty + 6;                                           // MMA -> epilogue
     uint64_t* acc_empty = acc_full + 1;                                       // epilogues of both blocks -> MMA (first block)
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    const uint32_t smem0 = smem_u32(smem);
+    const uint32_t smem0 = smem_u32(smem) + 1024;                             // the ring
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
@@ -547,7 +587,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
         // ================= loads
         if (lane == 0) {
             bool ok = true;
-            int g = 0, early = 0;
+            int g = 0, s = 0, round = 0, early = 0;
             prefetch_tensormap(&maps.a);
             prefetch_tensormap(&maps.w_codes);
             prefetch_tensormap(&maps.w_scales);
@@ -570,9 +610,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
             for (int t = first; ok && t < total; t += pairs) {
                 pair_tile(t, m_tiles, n_tiles, mt, nt);
                 const int a = 2 * mt + (int)rank;
-                for (int ku = 0; ku < p.KU; ++ku, ++g) {
-                    const int s = g % S;
-                    if (g >= S) ok = mbar_wait(&empty[s], ((g / S) - 1) & 1, abort_flag);
+                for (int ku = 0; ku < p.KU; ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
+                    if (round > 0) ok = mbar_wait(&empty[s], (round - 1) & 1, abort_flag);
                     if (!ok) break;
                     if (g >= early) load_w(s, mt, nt, ku);
                     if (a < a_units) tma_load_2d_pair(smem0 + s * G::kStage, &maps.a, 0, (a * p.KU + ku) * ROWS, full0 + 8 * s);
@@ -595,7 +634,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
         const uint64_t desc_a = smem_desc_k_sw128(smem0 + G::kA), desc_b = smem_desc_k_sw128(smem0 + G::kB);
         const uint64_t desc_sa = smem_desc_scales(smem0 + G::kA + kCodeBytes), desc_sb = smem_desc_scales(smem0 + G::kSb);
         bool ok = true;
-        int g = 0, it = 0;
+        int s = 0, it = 0;
+        uint32_t par = 0, set = 0;                                            // parity of the ring's round; set of scale columns
         for (int t = first; ok && t < total; t += pairs, ++it) {
             if (it > 0) {
                 ok = mbar_wait(acc_empty, (it - 1) & 1, abort_flag);
@@ -603,14 +643,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
                 if (!ok) break;
                 tc_fence_after_sync();
             }
-            for (int ku = 0; ku < p.KU; ++ku, ++g) {
-                const int s = g % S;
-                ok = mbar_wait(&full[s], (g / S) & 1, abort_flag);
+            for (int ku = 0; ku < p.KU; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
+                ok = mbar_wait(&full[s], par, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
-                const uint32_t sfa = tmem_base + (uint32_t)(G::kSf0 + (g & 1) * G::kSfCols);
+                const uint32_t sfa = tmem_base + (uint32_t)G::kSf0 + set * (uint32_t)G::kSfCols;
                 const uint32_t sfb = sfa + (uint32_t)(G::kGroups * 4);
                 copy_scales<2, G::kGroups>(sfa, desc_sa + at, 4, sel);
                 copy_scales<2, G::kGroups>(sfb, desc_sb + at, 8, sel);
@@ -647,7 +686,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
             pair_tile(t, m_tiles, n_tiles, mt, nt);
             const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
             const int n0 = 256 * nt + 128 * half;
-            if (row < p.M) {
+            if (p.vec < 16) {
+                uint32_t* staging = reinterpret_cast<uint32_t*>(smem_raw + G::kSmem - G::kStaging + (warp - 4) * kRowStaging);
+                const int row0 = row - lane;
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    store_rows_any(staging, reinterpret_cast<T*>(p.y) + (int64_t)row0 * p.ldy, p.ldy, v[c], alpha, lane, min(32, p.M - row0), n0 + 32 * c, p.N, p.vec);
+            } else if (row < p.M) {
                 T* o = reinterpret_cast<T*>(p.y) + (int64_t)row * p.ldy + n0;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -701,49 +746,45 @@ static qmm_status launch_t(const MxGemmParams& p, int64_t tiles, cudaStream_t st
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, p), "microscaled product launch");
 }
 
-// Few rows: shared memory that M token rows take over all KU units.
-static int few_resident(int fmt, int64_t M, int KU) { return KU * ((int)((M + 7) / 8) * 1024 + scale_bytes(fmt)); }
-
-// Weight rows per tile (128, 64 or 32): the fewest rounds over the SMs, a tile of BN rows taken as BN + 24 (the token rows'
-// loads, the scales -- a tile loads its unit's 128 rows of them -- and the hand-over of the accumulators).
-static int mx_tile_rows(int64_t row_tiles, int64_t N)
-{
-    if (g_knobs.mx_tile) return g_knobs.mx_tile;
-    int best = 128;
-    int64_t cost = -1;
-    for (int bn = 128; bn >= 32; bn /= 2) {
-        const int64_t rounds = (row_tiles * ((N + bn - 1) / bn) + kNumSMs - 1) / kNumSMs;
-        const int64_t c = rounds * (bn + 24);
-        if (cost < 0 || c < cost) cost = c, best = bn;
-    }
-    return best;
-}
-
-template <int FMT, bool GATEUP, typename T, int FORM> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
-{
-    const int bn = mx_tile_rows(row_tiles, p.N);
-    p.n_tiles = (p.N + bn - 1) / bn;
-    const int64_t tiles = row_tiles * p.n_tiles;
-    if (FORM == kMxFew) {
-        const int stage = (bn < 64 ? 64 : bn) * 128 + scale_bytes(FMT);
-        const int fit = (227 * 1024 - 2048 - few_resident(FMT, p.M, p.KU)) / stage;
-        p.stages = fit < 10 ? fit : 10;
-    }
-    if (bn == 128) return launch_t<FMT, 128, GATEUP, T, FORM>(p, tiles, st);
-    if (bn == 64) return launch_t<FMT, 64, GATEUP, T, FORM>(p, tiles, st);
-    return launch_t<FMT, 32, GATEUP, T, FORM>(p, tiles, st);
-}
-
+// Widest access (bytes) that every row's start allows.
 template <typename T> static int row_vec(const void* y, int64_t ldy)
 {
     const uintptr_t a = reinterpret_cast<uintptr_t>(y) | (uintptr_t)(ldy * (int64_t)sizeof(T));
-    return a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : 0;
+    return a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : a % 4 == 0 ? 4 : 2;
+}
+
+// Few rows: shared memory that M token rows take over all KU units.
+static int few_resident(int fmt, int64_t M, int KU) { return KU * ((int)((M + 7) / 8) * 1024 + scale_bytes(fmt)); }
+
+template <int FMT, typename T, int FORM> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
+{
+    using G = MxGeom<FMT, 128, false, FORM>;
+    p.vec = row_vec<T>(p.y, p.ldy);
+    const int room = G::kRoom - (FORM == kMxFew ? few_resident(FMT, p.M, p.KU) : 0) - (p.vec < 16 ? G::kStaging : 0);
+    p.stages = room / G::kStage < 10 ? room / G::kStage : 10;
+    return launch_t<FMT, 128, false, T, FORM>(p, row_tiles * p.n_tiles, st);
+}
+
+// Gate/up: tiles of 64 + 64 weight rows spread a decode step better over the SMs, tiles of 128 + 128 move fewer token rows: 128 experts of
+// 768 x 2048, 8 per token, 64 / 128: 4 tokens 14.3 / 16.2 us, 1024 tokens 40.8 / 45.3, 2048 tokens (128 rows an expert) 55.0 / 52.3.
+template <int FMT> static qmm_status launch_gate_up(MxGemmParams p, int64_t pairs, int64_t row_tiles, cudaStream_t st)
+{
+    const int bn = g_knobs.mx_tile ? g_knobs.mx_tile : pairs >= 96LL * p.E ? 128 : 64;
+    p.n_tiles = (p.N + bn - 1) / bn;
+    if (bn == 128) {
+        p.stages = MxGeom<FMT, 128, true, kMxGrouped>::kStages;
+        return launch_t<FMT, 128, true, __half, kMxGrouped>(p, row_tiles * p.n_tiles, st);
+    }
+    p.stages = MxGeom<FMT, 64, true, kMxGrouped>::kStages;
+    return launch_t<FMT, 64, true, __half, kMxGrouped>(p, row_tiles * p.n_tiles, st);
 }
 
 qmm_status make_unit_map(CUtensorMap* map, const void* packed, int64_t rows128, int box_rows);
 
-template <int FMT, typename T> static qmm_status launch_pair_t(const MxGemmParams& p, int tiles, cudaStream_t st)
+template <int FMT, typename T> static qmm_status launch_pair_t(MxGemmParams p, int tiles, cudaStream_t st)
 {
+    p.vec = row_vec<T>(p.y, p.ldy);
+    p.stages = MxPairGeom<FMT>::stages(p.vec < 16);
     auto kern = mx_pair_kernel<FMT, T>;
     constexpr int smem = MxPairGeom<FMT>::kSmem, ROWS = unit_bytes(FMT) / 128;
     static std::atomic<uint64_t> configured{0};
@@ -774,14 +815,25 @@ template <int FMT, typename T> static qmm_status launch_pair_t(const MxGemmParam
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, maps, p), "microscaled pair product launch");
 }
 
+// Whether 256 x 256 tiles on pairs of SMs beat 128 x 128 tiles on single ones: estimated ns of each, rounds of tiles times (k units, with the
+// hand-over; at least the time to store a tile) and a constant.  Measured (us, pairs / singles): 2048 x 8192 x 8192 49 / 58, x 2048 17.7 / 19.7,
+// x 768 13.5 / 12.8; 1024 x 2048 x 8192 15.2 / 11.9; 2048 x 2048 x 8192 17.0 / 19.6, x 2048 9.2 / 8.1.
+static bool pairs_pay(const MxGemmParams& p, int64_t pair_tiles)
+{
+    if (g_knobs.mx_pair) return g_knobs.mx_pair == 1;
+    auto most = [](int64_t a, int64_t b) { return a > b ? a : b; };
+    const int64_t singles = (int64_t)p.n_tiles * ((p.M + 127) / 128);
+    const int64_t rounds2 = (pair_tiles + kNumSMs / 2 - 1) / (kNumSMs / 2), rounds1 = (singles + kNumSMs - 1) / kNumSMs;
+    return 4600 + rounds2 * most(1900, 300 * p.KU + 1100) < 2000 + rounds1 * most(1250, 240 * p.KU + 600);
+}
+
 template <int FMT, typename T> static qmm_status dense_t(MxGemmParams p, cudaStream_t st)
 {
-    p.vec = row_vec<T>(p.y, p.ldy);
     const int pair_tiles = ((p.n_tiles + 1) / 2) * ((p.M + 255) / 256);
     // (the pair form's row coordinates are 32-bit: operands below 2^31 rows of 128 bytes)
     const bool fits = ((int64_t)p.n_tiles + (p.M + 127) / 128) * p.KU * (unit_bytes(FMT) / 128) < (1LL << 31);
-    if (p.M > 128 && fits && g_knobs.mx_pair != 2 && (pair_tiles >= 32 || g_knobs.mx_pair == 1)) return launch_pair_t<FMT, T>(p, pair_tiles, st);
-    return launch_tiles<FMT, false, T, kMxDense>(p, (p.M + 127) / 128, st);
+    if (p.M > 128 && pairs_pay(p, pair_tiles) && fits) return launch_pair_t<FMT, T>(p, pair_tiles, st);
+    return launch_tiles<FMT, T, kMxDense>(p, (p.M + 127) / 128, st);
 }
 
 qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale,
@@ -804,16 +856,20 @@ qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int6
     return dtype == QMM_F16 ? dense_t<QMM_NVFP4, __half>(p, st) : dtype == QMM_BF16 ? dense_t<QMM_NVFP4, __nv_bfloat16>(p, st) : dense_t<QMM_NVFP4, float>(p, st);
 }
 
-// Whether the product of a few rows can take them as they come (else they are quantised by a launch of their own).  Up to 16 rows and 112 KB (half of the ring's room): every block quantises all of them, which
-// for one token and a 2048 x 2048 matrix takes a launch and 2.9 us off the product.
-bool mx_few_fits(int fmt, int64_t M, int64_t K) { return M <= 16 && !g_knobs.mx_no_few && few_resident(fmt, M, (int)k_units(K)) <= 112 * 1024; }
+// Whether the product of a few rows takes them as they come (else they are quantised by a launch of their own).  Every block quantises all of them:
+// up to 16 rows of 2048 that costs 1.4 us and saves a launch (one token, 2048 x 2048: 8.8 -> 4.1 us), 8 rows of 8192 cost 3 to 5 us.  They may take
+// 112 KB, half of the shared memory.
+bool mx_few_fits(int fmt, int64_t M, int64_t K)
+{
+    return M <= 16 && M * K <= 32768 && few_resident(fmt, M, (int)k_units(K)) <= 112 * 1024 && !g_knobs.mx_no_few;
+}
 
 template <int FMT, typename T> static qmm_status few_t(MxGemmParams p, cudaStream_t st)
 {
-    p.vec = row_vec<T>(p.y, p.ldy);
-    p.x_vec = row_vec<T>(p.x, p.M > 1 ? p.ldx : 0);
+    const int x_vec = row_vec<T>(p.x, p.M > 1 ? p.ldx : 0);
+    p.x_vec = x_vec < 16 ? 0 : x_vec;
     p.atoms = (p.M + 7) / 8;
-    return launch_tiles<FMT, false, T, kMxFew>(p, 1, st);
+    return launch_tiles<FMT, T, kMxFew>(p, 1, st);
 }
 
 qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
@@ -827,6 +883,7 @@ qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t
     p.M = (int)M;
     p.N = (int)N;
     p.KU = (int)k_units(K);
+    p.n_tiles = (int)((N + 127) / 128);
     p.a_scale = x_scale;
     p.w_scale[0] = w_scale;
     p.y = y;
@@ -866,14 +923,13 @@ qmm_status launch_mx_experts_gate_up(int fmt, const void* a, int64_t pairs, int 
     p.y = h;
     p.status = status;
     const int64_t row_tiles = mx_max_row_units(pairs, E);
-    if (fmt == QMM_MXFP4) return launch_tiles<QMM_MXFP4, true, __half, kMxGrouped>(p, row_tiles, st);
-    return launch_tiles<QMM_NVFP4, true, __half, kMxGrouped>(p, row_tiles, st);
+    if (fmt == QMM_MXFP4) return launch_gate_up<QMM_MXFP4>(p, pairs, row_tiles, st);
+    return launch_gate_up<QMM_NVFP4>(p, pairs, row_tiles, st);
 }
 
 template <int FMT, typename T> static qmm_status grouped_t(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
 {
-    p.vec = row_vec<T>(p.y, p.ldy);
-    return launch_tiles<FMT, false, T, kMxGrouped>(p, row_tiles, st);
+    return launch_tiles<FMT, T, kMxGrouped>(p, row_tiles, st);
 }
 
 qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, const int* offsets, const int* units, const void* w, int64_t N,

@@ -15,6 +15,86 @@ struct MxRows {
     int topk, E;
 };
 
+// Rows that 16-byte accesses cannot reach: the warp's 32 chunks are read or written one after the other through shared memory, 4 bytes per
+// lane (VEC 4: 16-bit elements two chunks at a time) or one element (VEC 2) -- an access then covers consecutive elements of a row instead
+// of one element of each of 32 places.  Shared memory of a warp: a chunk per row, rows of W words one word apart.
+template <typename T> struct AnyRows {
+    static constexpr int W = 8 * (int)sizeof(T);
+    uint32_t w[kQuantThreads / 32][32 * (W + 1)];
+};
+template <typename T> __device__ __forceinline__ T* shfl_ptr(T* p, int lane)
+{
+    return reinterpret_cast<T*>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(p), lane));
+}
+template <typename T, int VEC> __device__ __forceinline__ void load32_any(AnyRows<T>& sm, const T* src, int n, float (&v)[32])
+{
+    constexpr int W = AnyRows<T>::W;
+    const int lane = threadIdx.x & 31;
+    uint32_t* rows = sm.w[threadIdx.x >> 5];
+    if constexpr (sizeof(T) == 2 && VEC == 4) {
+        const int l = lane & 15;
+#pragma unroll 8
+        for (int i = 0; i < 16; ++i) {
+            const int j = 2 * i + (lane >> 4);
+            const T* p = shfl_ptr(src, j);
+            const int nj = __shfl_sync(0xFFFFFFFFu, n, j);
+            uint32_t u = 0;
+            if (2 * l + 1 < nj) u = __ldg(reinterpret_cast<const uint32_t*>(p) + l);
+            else if (2 * l < nj) u = __ldg(reinterpret_cast<const unsigned short*>(p) + 2 * l);
+            rows[j * (W + 1) + l] = u;
+        }
+    } else
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+        const T* p = shfl_ptr(src, j);
+        const int nj = __shfl_sync(0xFFFFFFFFu, n, j);
+        T e = T(0.0f);
+        if (lane < nj) e = p[lane];
+        reinterpret_cast<T*>(rows + j * (W + 1))[lane] = e;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        const uint32_t u = rows[lane * (W + 1) + i];
+        if constexpr (sizeof(T) == 2) {
+            const float2 f = Dt<T>::up2(u);
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        } else {
+            v[i] = __uint_as_float(u);
+        }
+    }
+}
+template <typename T, int VEC> __device__ __forceinline__ void store32_any(AnyRows<T>& sm, T* dst, int n, const float (&v)[32])
+{
+    constexpr int W = AnyRows<T>::W;
+    const int lane = threadIdx.x & 31;
+    uint32_t* rows = sm.w[threadIdx.x >> 5];
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+        if constexpr (sizeof(T) == 2) rows[lane * (W + 1) + i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
+        else rows[lane * (W + 1) + i] = __float_as_uint(v[i]);
+    }
+    __syncwarp();
+    if constexpr (sizeof(T) == 2 && VEC == 4) {
+        const int l = lane & 15;
+#pragma unroll 8
+        for (int i = 0; i < 16; ++i) {
+            const int j = 2 * i + (lane >> 4);
+            T* p = shfl_ptr(dst, j);
+            const int nj = __shfl_sync(0xFFFFFFFFu, n, j);
+            const uint32_t u = rows[j * (W + 1) + l];
+            if (2 * l + 1 < nj) reinterpret_cast<uint32_t*>(p)[l] = u;
+            else if (2 * l < nj) reinterpret_cast<unsigned short*>(p)[2 * l] = (unsigned short)u;
+        }
+    } else
+#pragma unroll 8
+    for (int j = 0; j < 32; ++j) {
+        T* p = shfl_ptr(dst, j);
+        const int nj = __shfl_sync(0xFFFFFFFFu, n, j);
+        if (lane < nj) p[lane] = reinterpret_cast<const T*>(rows + j * (W + 1))[lane];
+    }
+}
+
 // Thread = one 32-element chunk of one row; chunks run over the padded K (a multiple of 256), so the padding of the last
 // unit is written as zeros.  Consecutive lanes hold consecutive chunks of a row (a row has a multiple of 8):
 // 4 (MXFP4) or 2 (NVFP4) neighbouring lanes join their scale bytes into one 4-byte store.
@@ -29,14 +109,24 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
     pdl_wait();
     const int64_t KU = k_units(K);
     const int64_t chunks = KU * (kUnitK / 32);
-    const int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
-    if (id >= rows * chunks) return;                       // (whole quads: rows * chunks is a multiple of 8)
+    int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    const bool live = id < rows * chunks;                  // (whole quads: rows * chunks is a multiple of 8)
+    if (VEC >= 16 && !live) return;
+    if (!live) id = 0;
     const int64_t row = id / chunks;
     const int c = (int)(id - row * chunks);
     const TensorScale ts(tensor_scale ? __ldg(tensor_scale) : 1.0f);
     const int64_t left = K - (int64_t)c * 32;
+    const T* src = x + row * ldx + (int64_t)c * 32;
+    const int n = (int)(left < 0 ? 0 : left < 32 ? left : 32);
     float v[32];
-    load32<T, VEC>(x + row * ldx + (int64_t)c * 32, (int)(left < 0 ? 0 : left < 32 ? left : 32), v);
+    if constexpr (VEC >= 16) {
+        load32<T, VEC>(src, n, v);
+    } else {
+        __shared__ AnyRows<T> sm;
+        load32_any<T, VEC>(sm, src, live ? n : 0, v);
+        if (!live) return;
+    }
     uint32_t sb;
     const uint4 codes = quantize32<FMT>(v, ts, sb);
     // scale bytes of the group of four blocks, assembled in its first lane
@@ -75,8 +165,10 @@ mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K
 {
     pdl_wait();
     const int64_t chunks = (K + 31) / 32;
-    const int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
-    if (id >= rows * chunks) return;
+    int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
+    const bool live = id < rows * chunks;
+    if (VEC >= 16 && !live) return;
+    if (!live) id = 0;
     const int64_t row = id / chunks;
     const int c = (int)(id - row * chunks);
     const float g = tensor_scale ? __ldg(tensor_scale) : 1.0f;
@@ -102,7 +194,7 @@ mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K
     }
     T* o = out + row * ldo + (int64_t)c * 32;
     const int64_t left = K - (int64_t)c * 32;
-    if (VEC && left >= 32) {
+    if (VEC >= 16 && left >= 32) {
         if constexpr (sizeof(T) == 2) {
             uint32_t u[16];
 #pragma unroll
@@ -128,10 +220,13 @@ mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K
                 }
             }
         }
-    } else {
+    } else if constexpr (VEC >= 16) {
 #pragma unroll
         for (int i = 0; i < 32; ++i)
             if (i < left) o[i] = Dt<T>::down(v[i]);
+    } else {
+        __shared__ AnyRows<T> sm;
+        store32_any<T, VEC>(sm, o, live ? (int)(left < 32 ? left : 32) : 0, v);
     }
 }
 
@@ -198,7 +293,7 @@ static qmm_status quantize_t(const void* x, int64_t ldx, int64_t rows, int64_t K
     const qmm_status s = launch_grid(rows * k_units(K) * (kUnitK / 32), &grid);
     if (s != QMM_OK) return s;
     const uintptr_t a = reinterpret_cast<uintptr_t>(x) | (rows > 1 ? (uintptr_t)(ldx * (int64_t)sizeof(T)) : 0);
-    const int vec = a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : 0;
+    const int vec = a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : a % 4 == 0 ? 4 : 2;     // (fp32 rows: 4 at least)
     const MxRows none = {nullptr, nullptr, nullptr, nullptr, 0, 0};
     auto go = [&](auto kern, const MxRows& r) {
         return launch_pdl(kern, grid, kQuantThreads, st, "microscaled quantisation launch", (const T*)x, ldx, rows, K, ts, (uint8_t*)packed, r, (int)early);
@@ -206,11 +301,11 @@ static qmm_status quantize_t(const void* x, int64_t ldx, int64_t rows, int64_t K
     if (m) {
         if (vec == 32) return go(mx_quantize_kernel<FMT, T, 32, true>, *m);
         if (vec == 16) return go(mx_quantize_kernel<FMT, T, 16, true>, *m);
-        return go(mx_quantize_kernel<FMT, T, 0, true>, *m);
+        return vec == 4 ? go(mx_quantize_kernel<FMT, T, 4, true>, *m) : go(mx_quantize_kernel<FMT, T, 2, true>, *m);
     }
     if (vec == 32) return go(mx_quantize_kernel<FMT, T, 32, false>, none);
     if (vec == 16) return go(mx_quantize_kernel<FMT, T, 16, false>, none);
-    return go(mx_quantize_kernel<FMT, T, 0, false>, none);
+    return vec == 4 ? go(mx_quantize_kernel<FMT, T, 4, false>, none) : go(mx_quantize_kernel<FMT, T, 2, false>, none);
 }
 
 static qmm_status quantize_any(int fmt, int dtype, const void* x, int64_t ldx, int64_t rows, int64_t K, const float* ts, void* packed,
@@ -247,7 +342,8 @@ static qmm_status dequantize_t(const void* packed, int64_t rows, int64_t K, cons
     const qmm_status s = launch_grid(rows * ((K + 31) / 32), &grid);
     if (s != QMM_OK) return s;
     const uintptr_t a = reinterpret_cast<uintptr_t>(out) | (rows > 1 ? (uintptr_t)(ldo * (int64_t)sizeof(T)) : 0);
-    return launch_pdl(a % 32 == 0 ? mx_dequantize_kernel<FMT, T, 32> : a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 16> : mx_dequantize_kernel<FMT, T, 0>, grid, kQuantThreads, st,
+    return launch_pdl(a % 32 == 0 ? mx_dequantize_kernel<FMT, T, 32> : a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 16> : a % 4 == 0 ? mx_dequantize_kernel<FMT, T, 4> : mx_dequantize_kernel<FMT, T, 2>,
+                      grid, kQuantThreads, st,
                       "microscaled dequantisation launch", (const uint8_t*)packed, rows, K, ts, (T*)out, ldo);
 }
 
