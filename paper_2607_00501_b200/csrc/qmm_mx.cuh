@@ -13,6 +13,7 @@
 
 #include "qmm_common.cuh"
 #include <cuda_bf16.h>
+#include <type_traits>
 
 namespace qmm {
 namespace mx {
@@ -169,13 +170,14 @@ struct TensorScale {
     __device__ __forceinline__ explicit TensorScale(float scale) : g(scale), g6(6.0f * scale)
     {
         r6 = 1.0f / g6;
-        plain = g6 >= 0x1p-80f && g6 <= 0x1p80f;
+        plain = g6 >= 0x1p-40f && g6 <= 0x1p40f;
     }
 };
 
-// Correctly rounded a / b from r = rn(1 / b): q0 = a r, e = a - q0 b (exact in one FMA), q = q0 + e r (P. W. Markstein,
-// "Computation of elementary functions on the IBM RISC System/6000 processor", IBM J. Res. Dev. 34, 1990).  Needs b and the
-// quotient away from the ends of the exponent range (a quotient that underflows is a zero code here either way).
+// Correctly rounded a / b from r = rn(1 / b): q0 = a r, e = a - q0 b (exact in one FMA), q = q0 + e r; and rn(1 / b) itself from an
+// approximation within an ulp, by one such step, unless b's significand is all ones (P. W. Markstein, "Computation of elementary
+// functions on the IBM RISC System/6000 processor", IBM J. Res. Dev. 34, 1990).  Need b and the quotient away from the ends of the
+// exponent range (a quotient that underflows is a zero code here either way).
 __device__ __forceinline__ float quotient(float a, float b, float r)
 {
     const float q = a * r;
@@ -186,29 +188,26 @@ __device__ __forceinline__ float2 quotient2(float2 a, float nb, float r)        
     const float2 q = mul2(a, both(r));
     return fma2(fma2(q, both(nb), a), both(r), q);
 }
-
-// Scale byte of a block from its largest magnitude (NaN if it holds one).
-template <int FMT> __device__ __forceinline__ uint32_t block_scale(float amax, const TensorScale& ts)
+__device__ __forceinline__ float reciprocal(float b)
 {
-    if (FMT == QMM_MXFP4) {
-        const uint32_t e = __float_as_uint(amax) >> 23;                            // 127 + floor(log2 amax); 0: zero or subnormal
-        return e == 255u ? 255u : e < 2u ? 0u : e - 2u;
-    }
-    if (!(amax < __int_as_float(0x7F800000))) return 0x7Fu;
-    const float s = ts.plain && amax <= 0x1p40f ? quotient(amax, ts.g6, ts.r6) : amax / ts.g6;
-    return (uint32_t)__nv_cvt_float_to_fp8(fminf(s, 448.0f), __NV_SATFINITE, __NV_E4M3);
+    if ((__float_as_uint(b) & 0x007FFFFFu) == 0x007FFFFFu) return 1.0f / b;
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(b));
+    return fmaf(fmaf(-b, r, 1.0f), r, r);
 }
 
-// Codes of a block whose largest magnitude is amax: FMT elements v -> FMT / 8 words, returns the scale byte.
+// Codes of a block whose largest magnitude is amax (NaN if it holds one): FMT elements v -> FMT / 8 words, returns the scale byte.
 //
 // MXFP4: the quotient by a power of two is a product by its reciprocal, exactly.
 // NVFP4: x / D in fp32 has to be the correctly rounded quotient, because ties are common (D has few significant
-// bits) and a product by 1 / D would break them the wrong way: one division per block and three operations per element
-// (two elements per instruction); a block with D outside [2^-80, 2^80] or a quotient beyond 2^80 takes true divisions.
+// bits) and a product by 1 / D would break them the wrong way: three operations per element, two elements per instruction.  With
+// 2^-40 <= 6 g <= 2^40 and amax <= 2^40 nothing comes near the ends of the exponent range (2^-52 <= D <= 2^47 or D = 0); every other
+// block takes true divisions.  8192 x 8192 bf16: 35 us, against 37.4 with a division per block and 27.8 for MXFP4.
 template <int FMT> __device__ __forceinline__ uint32_t quantize_block(const float (&v)[FMT], float amax, const TensorScale& ts, uint32_t (&out)[FMT / 8])
 {
-    const uint32_t sb = block_scale<FMT>(amax, ts);
     if (FMT == QMM_MXFP4) {
+        const uint32_t e = __float_as_uint(amax) >> 23;                            // 127 + floor(log2 amax); 0: zero or subnormal
+        const uint32_t sb = e == 255u ? 255u : e < 2u ? 0u : e - 2u;
         const float inv = sb == 255u ? 0.0f : __uint_as_float((254u - sb) << 23);  // 2^(127 - sb), sb in 0 .. 252
 #pragma unroll
         for (int w = 0; w < FMT / 8; ++w) {
@@ -220,14 +219,10 @@ template <int FMT> __device__ __forceinline__ uint32_t quantize_block(const floa
         }
         return sb;
     }
-    const float D = e4m3_value(sb) * ts.g;
-    if (sb == 0x7Fu || !(D > 0.0f)) {
-#pragma unroll
-        for (int w = 0; w < FMT / 8; ++w) out[w] = 0u;
-        return sb;
-    }
-    const float r = 1.0f / D;
-    if (D >= 0x1p-80f && D <= 0x1p80f && amax * r <= 0x1p80f) {
+    if (ts.plain && amax <= 0x1p40f) {
+        const uint32_t sb = (uint32_t)__nv_cvt_float_to_fp8(fminf(quotient(amax, ts.g6, ts.r6), 448.0f), __NV_SATFINITE, __NV_E4M3);
+        const float D = e4m3_value(sb) * ts.g;
+        const float r = D > 0.0f ? reciprocal(D) : 0.0f;                           // (D = 0: codes 0)
 #pragma unroll
         for (int w = 0; w < FMT / 8; ++w) {
             float2 q[4];
@@ -235,23 +230,26 @@ template <int FMT> __device__ __forceinline__ uint32_t quantize_block(const floa
             for (int i = 0; i < 4; ++i) q[i] = quotient2(make_float2(v[8 * w + 2 * i], v[8 * w + 2 * i + 1]), -D, r);
             out[w] = codes8(q);
         }
-    } else {
+        return sb;
+    }
+    const bool finite = amax < __int_as_float(0x7F800000);
+    const uint32_t sb = finite ? (uint32_t)__nv_cvt_float_to_fp8(fminf(amax / ts.g6, 448.0f), __NV_SATFINITE, __NV_E4M3) : 0x7Fu;
+    const float D = e4m3_value(sb) * ts.g;
 #pragma unroll 1
-        for (int w = 0; w < FMT / 8; ++w) {
-            float2 q[4];
+    for (int w = 0; w < FMT / 8; ++w) {
+        float2 q[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float a = 0.0f, b = 0.0f;                                          // (v stays in registers: no indexing by the loop variable)
-#pragma unroll
-                for (int k = 0; k < FMT / 8; ++k)
-                    if (k == w) a = v[8 * k + 2 * i], b = v[8 * k + 2 * i + 1];
-                q[i] = make_float2(a / D, b / D);
-            }
-            const uint32_t c = codes8(q);
+        for (int i = 0; i < 4; ++i) {
+            float a = 0.0f, b = 0.0f;                                              // (v stays in registers: no indexing by the loop variable)
 #pragma unroll
             for (int k = 0; k < FMT / 8; ++k)
-                if (k == w) out[k] = c;
+                if (k == w) a = v[8 * k + 2 * i], b = v[8 * k + 2 * i + 1];
+            q[i] = finite && D > 0.0f ? make_float2(a / D, b / D) : make_float2(0.0f, 0.0f);
         }
+        const uint32_t c = codes8(q);
+#pragma unroll
+        for (int k = 0; k < FMT / 8; ++k)
+            if (k == w) out[k] = c;
     }
     return sb;
 }
