@@ -1,15 +1,18 @@
-"""Build libqmm.so in-tree with nvcc for sm_100a (no other target is built)."""
+"""Build libqmm.so in-tree with nvcc for sm_100a (no other target is built), and beside it the CPython extension
+that marshals the arguments of its hot-path calls."""
 from __future__ import annotations
 
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libqmm.so")
+EXT = os.path.join(HERE, "_qmm_py.so")
 SOURCES = ("qmm_api.cu", "qmm_pack.cu", "qmm_gemv.cu", "qmm_gemm.cu", "qmm_gemm_small.cu", "qmm_moe.cu", "qmm_chain.cu",
            "qmm_mx_api.cu", "qmm_mx_quant.cu", "qmm_mx_gemm.cu", "qmm_expert.cu")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -31,7 +34,7 @@ def _deps_mtime() -> float:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile every .cu under csrc/ and link libqmm.so beside this file."""
-    if not force and os.path.exists(LIB) and os.path.getmtime(LIB) >= _deps_mtime():
+    if not force and os.path.exists(LIB) and os.path.exists(EXT) and min(os.path.getmtime(LIB), os.path.getmtime(EXT)) >= _deps_mtime():
         return LIB
     os.makedirs(BUILD, exist_ok=True)
     nvcc = _nvcc()
@@ -57,6 +60,12 @@ def build(force: bool = False, verbose: bool = False) -> str:
     cmd = [nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
+    # the extension finds libqmm.so beside itself
+    tmp = EXT + ".tmp.%d" % os.getpid()
+    cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "qmm_py.c"), "-o", tmp,
+           "-L", HERE, "-l:libqmm.so", "-Wl,-rpath,$ORIGIN"]
+    subprocess.run(cmd, check=True)
+    os.replace(tmp, EXT)
     return LIB
 
 

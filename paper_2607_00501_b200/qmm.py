@@ -1,7 +1,7 @@
 """Thin ctypes binding of libqmm.so (the C ABI declared in include/qmm.h).
 
-Argument marshalling only: every step of every product runs in the CUDA
-kernels of the library.  PyTorch is used for device memory and streams.  There
+Argument marshalling only (of the shortest hot-path calls in the extension csrc/qmm_py.c,
+of the others here): every step of every product runs in the CUDA kernels of the library.  PyTorch is used for device memory and streams.  There
 is no CPU fallback: if the shared library cannot be loaded, or a call fails,
 an exception is raised.
 """
@@ -114,7 +114,7 @@ def lib() -> ctypes.CDLL:
         return _lib
     with _lock:
         if _lib is None:
-            if not os.path.exists(LIB_PATH):
+            if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_qmm_py.so")):
                 from . import _build
                 _build.build()
             L = ctypes.CDLL(LIB_PATH)
@@ -177,6 +177,19 @@ def lib() -> ctypes.CDLL:
             L.qmm_debug_wait_give_up.argtypes = [vp, i64, vp]
             _lib = L
     return _lib
+
+
+_ext = None
+
+
+def _native():
+    """The extension that marshals the shortest calls (0.5 us instead of 3 us of a call)."""
+    global _ext
+    if _ext is None:
+        lib()
+        from . import _qmm_py
+        _ext = _qmm_py
+    return _ext
 
 
 def last_error() -> str:
@@ -473,12 +486,9 @@ def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: to
 
 def mx_quantize(fmt: int, x: torch.Tensor, out: torch.Tensor | None = None, tensor_scale: torch.Tensor | None = None) -> torch.Tensor:
     """x [rows, K] (fp16, bf16 or fp32; any row stride) -> packed operand, uint8."""
-    ptr, ld, rows, K = _rows2d(x, "x")
-    L = lib()
     if out is None:
-        out = torch.empty(L.qmm_mx_bytes(fmt, rows, K), dtype=torch.uint8, device=x.device)
-    dst = _operand(out, _mx_need(fmt, rows, K), "out") if rows else 0
-    _check(L.qmm_mx_quantize(fmt, DTYPES[x.dtype], ptr, ld, rows, K, _scalar(tensor_scale), dst, _stream()))
+        out = torch.empty(lib().qmm_mx_bytes(fmt, x.shape[0], x.shape[1]), dtype=torch.uint8, device=x.device)
+    _check((_ext or _native()).mx_quantize(fmt, x, out, tensor_scale))
     return out
 
 
@@ -487,10 +497,8 @@ def mx_dequantize(fmt: int, packed: torch.Tensor, rows: int, K: int, out: torch.
     """Packed operand -> the values it stands for, [rows, K] of out's type (or `dtype`)."""
     if out is None:
         out = torch.empty((rows, K), dtype=dtype, device=packed.device)
-    ptr, ld, r, k = _rows2d(out, "out")
-    assert (r, k) == (rows, K)
-    src = _operand(packed, _mx_need(fmt, rows, K), "packed") if rows else 0
-    _check(lib().qmm_mx_dequantize(fmt, src, rows, K, _scalar(tensor_scale), DTYPES[out.dtype], ptr, ld, _stream()))
+    assert out.shape == (rows, K)
+    _check((_ext or _native()).mx_dequantize(fmt, packed, out, tensor_scale))
     return out
 
 
@@ -520,16 +528,11 @@ def mx_linear_workspace_bytes(fmt: int, M: int, N: int, K: int) -> int:
 def mx_linear(fmt: int, X: torch.Tensor, w: torch.Tensor, N: int, Y: torch.Tensor | None = None, x_scale: torch.Tensor | None = None,
               w_scale: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
     """Y [M, N] = quantised(X) w^T: X [M, K] as it comes (fp16, bf16 or fp32), w packed [N, K]; Y has X's type."""
-    L = lib()
-    xp, ldx, M, K = _rows2d(X, "X")
     if Y is None:
-        Y = torch.empty((M, N), dtype=X.dtype, device=X.device)
-    yp, ldy, r, c = _rows2d(Y, "Y")
-    assert (r, c) == (M, N) and Y.dtype == X.dtype
+        Y = torch.empty((X.shape[0], N), dtype=X.dtype, device=X.device)
     if ws is None:
-        ws = _workspace(L.qmm_mx_linear_workspace_bytes(fmt, M, N, K), X.device, ws)
-    _check(L.qmm_mx_linear(fmt, DTYPES[X.dtype], xp, ldx, M, _operand(w, _mx_need(fmt, N, K), "w"), N, K, _scalar(x_scale),
-                           _scalar(w_scale), yp, ldy, ws.data_ptr(), ws.numel() * ws.element_size(), _stream()))
+        ws = _workspace(lib().qmm_mx_linear_workspace_bytes(fmt, X.shape[0], N, X.shape[1]), X.device, ws)
+    _check((_ext or _native()).mx_linear(fmt, X, w, N, Y, x_scale, w_scale, ws))
     return Y
 
 
@@ -548,62 +551,44 @@ class ExpertPlan:
         self.ptrs = (base, base + 4 * P, base + 8 * P, base + 8 * P + 4 * (E + 1))         # order, place, offsets, units
         self.ws_bytes = lib().qmm_expert_sort_workspace_bytes(T, topk, E)
         self.ws = torch.empty(self.ws_bytes, dtype=torch.uint8, device=device) if self.ws_bytes else None
+        self.ws_ptr = _dp(self.ws)
 
 
 def expert_sort(idx: torch.Tensor, E: int, out: ExpertPlan | None = None) -> ExpertPlan:
     """idx [T, topk] int32: experts of each token, values outside [0, E) dropped -> ExpertPlan."""
-    assert idx.is_cuda and idx.dtype == torch.int32 and idx.dim() == 2 and idx.is_contiguous()
     T, topk = idx.shape
     if out is None:
         out = ExpertPlan(T, topk, E, idx.device)
-    assert (out.T, out.topk, out.E) == (T, topk, E)
+    assert out.T == T and out.topk == topk and out.E == E
     order, place, offsets, units = out.ptrs
-    _check(lib().qmm_expert_sort(idx.data_ptr(), T, topk, E, order, place, offsets, units, _dp(out.ws), out.ws_bytes, _stream()))
+    _check((_ext or _native()).expert_sort(idx, E, order, place, offsets, units, out.ws_ptr, out.ws_bytes))
     return out
-
-
-def _weights_ptr(weights, plan: ExpertPlan) -> int:
-    if weights is None:
-        return 0
-    assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.numel() == plan.T * plan.topk
-    return weights.data_ptr()
 
 
 def expert_gather(x: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """xs [T * topk, H]: row place[p] = (weights[p] *) x[p // topk]; rows past the last pair are zero."""
-    xp, ldx, T, H = _rows2d(x, "x")
     if out is None:
-        out = torch.empty((plan.T * plan.topk, H), dtype=x.dtype, device=x.device)
-    op, ldo, r, c = _rows2d(out, "out")
-    assert T == plan.T and (r, c) == (T * plan.topk, H) and out.dtype == x.dtype
-    _check(lib().qmm_expert_gather(DTYPES[x.dtype], xp, ldx, T, plan.topk, H, plan.ptrs[0], plan.ptrs[1], _weights_ptr(weights, plan), op, ldo, _stream()))
+        out = torch.empty((plan.T * plan.topk, x.shape[1]), dtype=x.dtype, device=x.device)
+    _check((_ext or _native()).expert_gather(x, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], weights, out))
     return out
 
 
 def expert_combine(ys: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | None = None, out: torch.Tensor | None = None) -> torch.Tensor:
     """y [T, H] = sum over a token's pairs of (weights[p] *) ys[place[p]]."""
-    yp, ldys, P, H = _rows2d(ys, "ys")
     if out is None:
-        out = torch.empty((plan.T, H), dtype=ys.dtype, device=ys.device)
-    op, ldo, r, c = _rows2d(out, "out")
-    assert P == plan.T * plan.topk and (r, c) == (plan.T, H) and out.dtype == ys.dtype
-    _check(lib().qmm_expert_combine(DTYPES[ys.dtype], yp, ldys, plan.T, plan.topk, H, plan.ptrs[1], _weights_ptr(weights, plan), op, ldo, _stream()))
+        out = torch.empty((plan.T, ys.shape[1]), dtype=ys.dtype, device=ys.device)
+    _check((_ext or _native()).expert_combine(ys, plan.T, plan.topk, plan.ptrs[1], weights, out))
     return out
 
 
 def expert_combine_grad(dy: torch.Tensor, ys: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor, dys: torch.Tensor | None = None,
                         dw: torch.Tensor | None = None):
     """Gradients of expert_combine: (dys [T * topk, H], dw [T, topk] fp32)."""
-    dp, lddy, T, H = _rows2d(dy, "dy")
-    yp, ldys, P, H2 = _rows2d(ys, "ys")
     if dys is None:
-        dys = torch.empty((P, H), dtype=dy.dtype, device=dy.device)
+        dys = torch.empty((plan.T * plan.topk, dy.shape[1]), dtype=dy.dtype, device=dy.device)
     if dw is None:
-        dw = torch.empty((T, plan.topk), dtype=torch.float32, device=dy.device)
-    op, ldo, r, c = _rows2d(dys, "dys")
-    assert T == plan.T and P == T * plan.topk and H2 == H and (r, c) == (P, H) and ys.dtype == dy.dtype == dys.dtype
-    _check(lib().qmm_expert_combine_grad(DTYPES[dy.dtype], dp, lddy, yp, ldys, T, plan.topk, H, plan.ptrs[0], plan.ptrs[1],
-                                         _weights_ptr(weights, plan), op, ldo, _weights_ptr(dw, plan), _stream()))
+        dw = torch.empty((plan.T, plan.topk), dtype=torch.float32, device=dy.device)
+    _check((_ext or _native()).expert_combine_grad(dy, ys, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], weights, dys, dw))
     return dys, dw
 
 
