@@ -251,6 +251,21 @@ def test_layer_with_strided_bf16_rows(qmm):
     assert torch.equal(buf[:, :H], want) and bool((buf[:, H:] == 7).all())
 
 
+@pytest.mark.parametrize("fmt", ["mxfp4", "nvfp4"])
+def test_example_layer(qmm, fmt):
+    """The example serves a layer and trains through the moves.  Two 4-bit operands per product, each off by a relative rms of about
+    0.12 (the e2m1 grid under one scale per block): sqrt(2) * 0.12 per product, two products in sequence and the product g u in between
+    leave about 0.35 (0.45 with the spread of a single token); the gradients differ by the order of fp32 sums."""
+    import importlib.util
+    import os
+    spec = importlib.util.spec_from_file_location("mx_moe_layer", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "mx_moe_layer.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    for tokens in (1, 64, 300):
+        served, trained = example.main(["--tokens", str(tokens), "--fmt", fmt])
+        assert 0 < served < 0.45 and trained < 1e-5
+
+
 def test_offsets_past_32_bits(qmm):
     T, topk, H = 4, 1, 64
     pitch = (1 << 30) + 8
