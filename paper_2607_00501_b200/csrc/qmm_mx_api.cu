@@ -23,7 +23,7 @@ qmm_status launch_mx_experts_gate_up(int fmt, const void* a, int64_t pairs, int 
                                      int64_t N, int64_t K, const float* a_scale, const float* gate_scale, const float* up_scale, const float* h_scale, void* h,
                                      int* status, cudaStream_t st);
 qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, const int* offsets, const int* units, const void* w, int64_t N, int64_t K,
-                                  const float* a_scale, const float* w_scale, int dtype, void* y, int64_t ldy, int* status, cudaStream_t st);
+                                  const float* a_scale, const float* w_scale, int dtype, void* y, int64_t ldy, bool list_ready, int* status, cudaStream_t st);
 size_t expert_sort_workspace_bytes(int64_t P, int E);
 qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int* place, int* offsets, int* units, void* ws, cudaStream_t st);
 bool expert_sort_quantize_fits(int64_t P, int topk, int64_t K);
@@ -358,7 +358,7 @@ qmm_status qmm_mx_experts_gemm(qmm_mx_format fmt, const void* a, int32_t T, int3
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
     if (!offsets || !units) return fail(QMM_ERR_INVALID_ARG, "%s: offsets or units is null", who);
     QMM_TRY(check_device(who));
-    return launch_mx_experts_gemm(fmt, a, (int64_t)T * topk, E, offsets, units, w, N, K, a_scale, w_scale, dtype, Y, ldy, status, (cudaStream_t)stream);
+    return launch_mx_experts_gemm(fmt, a, (int64_t)T * topk, E, offsets, units, w, N, K, a_scale, w_scale, dtype, Y, ldy, false, status, (cudaStream_t)stream);
 }
 
 size_t qmm_mx_moe_workspace_bytes(const qmm_mx_moe_args* args)
@@ -397,7 +397,7 @@ qmm_status qmm_mx_moe(const qmm_mx_moe_args* a, void* ws, size_t ws_bytes, void*
     QMM_TRY(launch_mx_experts_gate_up(a->fmt, base + l.xq, P, a->E, offsets, units, a->w_gate, a->w_up, a->I, a->H, a->x_scale, a->gate_scale, a->up_scale,
                                       a->h_scale, base + l.h, (int*)ws, st));
     QMM_TRY(launch_mx_experts_gemm(a->fmt, base + l.h, P, a->E, offsets, units, a->w_down, a->H, a->I, a->h_scale, a->down_scale, a->dtype, base + l.d, a->H,
-                                   (int*)ws, st));
+                                   true, (int*)ws, st));                                 // gate/up waited for the sort before it let this one go
     return launch_expert_combine(a->dtype, base + l.d, a->H, a->T, a->topk, a->H, place, a->weights, a->out, a->ldo, st);
 }
 

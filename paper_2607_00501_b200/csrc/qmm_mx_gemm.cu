@@ -38,6 +38,8 @@ struct MxGemmParams {
     int n_tiles;                     // weight tiles of BN rows (pair form: of 128)
     const int *offsets, *units;      // grouped: [E + 1] each
     int E;
+    int list_ready;                  // grouped: units[] and offsets[] were complete before this kernel could start (the kernel upstream lets its
+                                     // dependents go only after its own wait for the sort): weights are requested while that kernel still runs
     const float* a_scale;            // tensor scales, null = 1
     const float* w_scale[2];         // grouped: [E]
     const float* h_scale;            // gate/up: tensor scale of the output operand
@@ -224,8 +226,9 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         tmem_alloc(tmem_slot, G::kTmemCols);
         tmem_relinquish();
     }
+    const bool waited = GROUPED && !p.list_ready;
+    if (waited) pdl_wait();                                                   // the rows' grouping is written upstream
     if (GROUPED) {
-        pdl_wait();                                                           // the rows' grouping is written upstream
         for (int e = threadIdx.x; e < ((p.E + 32) & ~31); e += G::kThreads) {
             s_units[e] = e <= p.E ? __ldg(p.units + e) : 0x7FFFFFFF;
             if (e <= p.E) s_first[e] = __ldg(p.offsets + e);
@@ -320,9 +323,9 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         if (!GROUPED) {
             if (warp == W_WARP && get_work(0, w))
                 for (; early < S && early < p.KU; ++early) load_w(early, early);
-            if (!FEW) pdl_wait();
         }
         if (FEW) load_tokens();
+        else if (!waited && warp == A_WARP) pdl_wait();                       // weights go on; token rows are the previous kernel's
         for (int i = 0; (!FEW || warp == W_WARP) && ok && get_work(i, w); ++i) {
             const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
             const uint8_t* src = p.a + (int64_t)w.m_unit * p.KU * G::kUnit;
@@ -408,7 +411,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         MxWork w;
         // every global write below comes after the previous kernel has completed (its readers of this buffer included)
         if (FEW) load_tokens();
-        else if (!GROUPED) pdl_wait();
+        else if (!waited) pdl_wait();
         const float a_scale = p.a_scale ? __ldg(p.a_scale) : 1.0f;
         const TensorScale hs(GATEUP && p.h_scale ? __ldg(p.h_scale) : 1.0f);
         for (int it = 0; ok && get_work(it, w); ++it) {
@@ -933,7 +936,8 @@ template <int FMT, typename T> static qmm_status grouped_t(MxGemmParams p, int64
 }
 
 qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, const int* offsets, const int* units, const void* w, int64_t N,
-                                  int64_t K, const float* a_scale, const float* w_scale, int dtype, void* y, int64_t ldy, int* status, cudaStream_t st)
+                                  int64_t K, const float* a_scale, const float* w_scale, int dtype, void* y, int64_t ldy, bool list_ready, int* status,
+                                  cudaStream_t st)
 {
     MxGemmParams p = {};
     p.a = (const uint8_t*)a;
@@ -945,6 +949,7 @@ qmm_status launch_mx_experts_gemm(int fmt, const void* a, int64_t pairs, int E, 
     p.offsets = offsets;
     p.units = units;
     p.E = E;
+    p.list_ready = list_ready;
     p.a_scale = a_scale;
     p.w_scale[0] = w_scale;
     p.y = y;
