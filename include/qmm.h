@@ -435,8 +435,9 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
 
 /* Y[m, n] = a_scale * w_scale * sum_k a[m, k] w[n, k] with both operands packed, M >= 0, N >= 1, K >= 1.
  *   a, w  packed [M, K] and [N, K];  Y [M, ldy] of type `dtype`, ldy >= N
- *   ws    device, 16-byte aligned, >= qmm_mx_gemm_workspace_bytes(); starts with a status word:
- *         zero-fill it once (qmm_status_check reports a bounded wait that gave up).                 */
+ *   ws    device, 256-byte aligned, >= qmm_mx_gemm_workspace_bytes(); starts with a status word (qmm_status_check
+ *         reports a bounded wait that gave up) and counters that every complete call leaves at zero: zero-fill its first
+ *         1024 bytes once, and again after a call on it was reported as failed.                      */
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
 qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K,
                        const float* a_scale, const float* w_scale, qmm_dtype dtype, void* Y, int64_t ldy,
@@ -444,7 +445,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
 
 /* The same product of activations as they come: X [M, ldx] of type `dtype` is quantised (as by
  * qmm_mx_quantize with tensor scale x_scale) on the way in; Y [M, ldy] of the same type.
- *   ws  device, 16-byte aligned, >= qmm_mx_linear_workspace_bytes(); its first 256 bytes zeroed once.  */
+ *   ws  device, 256-byte aligned, >= qmm_mx_linear_workspace_bytes(); its first 1024 bytes zeroed once, as above. */
 size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
 qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int64_t ldx, int64_t M,
                          const void* w, int64_t N, int64_t K, const float* x_scale, const float* w_scale,
@@ -556,6 +557,7 @@ qmm_status qmm_status_check(void* ws, void* stream);
  *   "gemm_no_small"    "1"             M <= 8 through the tensor-core kernel, not the few-token kernel
  *   "moe_no_fuse"      "1"             decode-sized qmm_moe as separate route / product / combine launches
  *   "mx_pair"          "1" | "2"       microscaled products of more than 128 tokens on pairs of SMs: always | never
+ *   "mx_no_split"      "1"             microscaled products without blocks that share a tile's K
  *   "mx_no_few"        "1"             qmm_mx_linear of few rows through a quantisation launch of its own
  *   "mx_tile"          "64" | "128"    weight rows per matrix and tile of the microscaled gate/up product
  */

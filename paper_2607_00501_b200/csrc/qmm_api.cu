@@ -409,6 +409,7 @@ qmm_status qmm_debug_config(const char* name, const char* value)
                 : strcmp(name, "gemm_no_small") == 0    ? &g_knobs.gemm_no_small
                 : strcmp(name, "moe_no_fuse") == 0      ? &g_knobs.moe_no_fuse
                 : strcmp(name, "mx_no_few") == 0        ? &g_knobs.mx_no_few
+                : strcmp(name, "mx_no_split") == 0      ? &g_knobs.mx_no_split
                                                         : nullptr;
     if (!flag) return fail(QMM_ERR_INVALID_ARG, "qmm_debug_config: unknown knob \"%s\"", name);
     *flag = off ? 0 : 1;

@@ -105,6 +105,7 @@ struct DebugKnobs {
     int gemm_no_small;              // M <= 8 through the tensor-core prefill kernel instead of the few-token kernel
     int moe_no_fuse;                // decode-sized MoE layers as four separate launches
     int mx_pair;                    // microscaled product on pairs of SMs: 1 whenever it can run, 2 never; 0: the plan
+    int mx_no_split;                // microscaled products whose tiles are never shared between blocks
     int mx_no_few;                  // qmm_mx_linear of few rows through a quantisation launch
     int mx_tile;                    // weight rows per matrix and tile of the microscaled gate/up product (64, 128); 0: the plan
 };

@@ -22,6 +22,10 @@ constexpr int kUnitRows = 128;
 constexpr int kUnitK = 256;
 constexpr int kCodeBytes = kUnitRows * kUnitK / 2;
 
+// Workspace of a product: status word, counters of tiles whose K is shared between blocks (two blocks per tile at least, so at most 74), then
+// partial sums.  The header is zero between calls.
+constexpr int kMxCounters = 256, kMxHeader = 1024;
+
 __host__ __device__ constexpr int scale_bytes(int fmt) { return kUnitRows * kUnitK / fmt; }      // fmt = block length
 __host__ __device__ constexpr int unit_bytes(int fmt) { return kCodeBytes + scale_bytes(fmt); }
 __host__ __device__ inline int64_t k_units(int64_t K) { return (K + kUnitK - 1) / kUnitK; }

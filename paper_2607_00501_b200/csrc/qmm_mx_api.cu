@@ -15,7 +15,8 @@ qmm_status launch_mx_quantize_experts(int fmt, int dtype, const void* x, int64_t
 qmm_status launch_mx_dequantize(int fmt, int dtype, const void* packed, int64_t rows, int64_t K, const float* ts, void* out, int64_t ldo, cudaStream_t st);
 qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale, int dtype, void* y,
                           int64_t ldy, int* status, cudaStream_t st);
-bool mx_few_fits(int fmt, int64_t M, int64_t K);
+bool mx_few_fits(int fmt, int64_t M, int64_t N, int64_t K);
+size_t mx_gemm_partial_bytes(int64_t M, int64_t N, int64_t K);
 qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
                          const float* w_scale, void* y, int64_t ldy, int* status, cudaStream_t st);
 int64_t mx_max_row_units(int64_t pairs, int E);
@@ -185,7 +186,7 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
     if (check_mx("qmm_mx_gemm_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_gemm_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
-    return kMxStatusBytes;
+    return kMxHeader + mx_gemm_partial_bytes(M, N, K);
 }
 
 qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale, qmm_dtype dtype,
@@ -201,7 +202,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
     QMM_TRY(check_packed(who, "a", a));
     QMM_TRY(check_packed(who, "w", w));
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
-    QMM_TRY(check_ws(who, ws, ws_bytes, kMxStatusBytes, 16));
+    QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_gemm_workspace_bytes(fmt, M, N, K), 256));
     QMM_TRY(check_device(who));
     return launch_mx_gemm(fmt, a, M, w, N, K, a_scale, w_scale, dtype, Y, ldy, (int*)ws, (cudaStream_t)stream);
 }
@@ -209,7 +210,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
 size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
     if (check_mx("qmm_mx_linear_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_linear_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
-    return kMxStatusBytes + mx_bytes(fmt, (M + 127) / 128, K);
+    return kMxHeader + mx_gemm_partial_bytes(M, N, K) + mx_bytes(fmt, (M + 127) / 128, K);
 }
 
 qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
@@ -225,10 +226,10 @@ qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int6
     QMM_TRY(check_rows(who, "X", dtype, X, ldx, K));
     QMM_TRY(check_packed(who, "w", w));
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
-    QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_linear_workspace_bytes(fmt, M, N, K), 16));
+    QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_linear_workspace_bytes(fmt, M, N, K), 256));
     QMM_TRY(check_device(who));
-    if (mx_few_fits(fmt, M, K)) return launch_mx_few(fmt, dtype, X, ldx, M, w, N, K, x_scale, w_scale, Y, ldy, (int*)ws, (cudaStream_t)stream);
-    void* a = (char*)ws + kMxStatusBytes;
+    if (mx_few_fits(fmt, M, N, K)) return launch_mx_few(fmt, dtype, X, ldx, M, w, N, K, x_scale, w_scale, Y, ldy, (int*)ws, (cudaStream_t)stream);
+    void* a = (char*)ws + kMxHeader + mx_gemm_partial_bytes(M, N, K);
     QMM_TRY(launch_mx_quantize(fmt, dtype, X, ldx, M, K, x_scale, a, true, (cudaStream_t)stream));
     return launch_mx_gemm(fmt, a, M, w, N, K, x_scale, w_scale, dtype, Y, ldy, (int*)ws, (cudaStream_t)stream);
 }

@@ -50,6 +50,9 @@ struct MxGemmParams {
     int64_t ldx, K;
     int x_vec;                       // widest aligned load of x
     int atoms;                       // few: 8-row atoms per unit (1 or 2)
+    int splits;                      // dense, few: blocks that share a tile's K (1: none); then every block has one piece of work, and
+    float* partial;                  // partial sums go here, [tile][split][rows, a multiple of 32][128 columns],
+    int* counters;                   // per tile, zero between calls: the block that comes last adds the partial sums
     int stages;                      // ring depth (what resident rows or staging leave)
     int* status;
 };
@@ -99,6 +102,7 @@ struct MxWork {
     int rows;                        // token rows in it (1 .. 128)
     int row0;                        // first row of Y
     int n_tile, expert;
+    int k0, k1;                      // k units
 };
 
 // silu(g) u = g u / (1 + 2^(-g log2 e)) for two features at a time, g and u still to be multiplied by their tensor scales:
@@ -183,7 +187,21 @@ __device__ __forceinline__ void mx_cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-template <int FMT, int BN, bool GATEUP, typename T, int FORM>
+// The epilogue's warps meet: whether all / any of their threads said so.
+template <int THREADS> __device__ __forceinline__ bool epilogue_all(bool x)
+{
+    int r;
+    asm volatile("{.reg .pred p, q; setp.ne.s32 p, %1, 0; barrier.cta.red.and.pred q, 2, %2, p; selp.s32 %0, 1, 0, q;}" : "=r"(r) : "r"((int)x), "n"(THREADS) : "memory");
+    return r != 0;
+}
+template <int THREADS> __device__ __forceinline__ bool epilogue_any(bool x)
+{
+    int r;
+    asm volatile("{.reg .pred p, q; setp.ne.s32 p, %1, 0; barrier.cta.red.or.pred q, 2, %2, p; selp.s32 %0, 1, 0, q;}" : "=r"(r) : "r"((int)x), "n"(THREADS) : "memory");
+    return r != 0;
+}
+
+template <int FMT, int BN, bool GATEUP, typename T, int FORM, bool SPLIT>
 __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx_gemm_kernel(const MxGemmParams p)
 {
     using namespace tc;
@@ -206,8 +224,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
     // few: the resident token rows, atoms of 8 rows x 128 bytes (p.atoms of them per k unit), then their scales, then the ring.  The MMA reads
     // 128 rows from a unit's first atom: the rows past its own are whatever follows (never stored), inside the block's memory.
     uint8_t* resident = smem + G::kHead;
-    const int resident_codes = FEW ? p.KU * p.atoms * 1024 : 0;
-    const uint32_t ring0 = smem_u32(resident) + (FEW ? resident_codes + p.KU * G::kSc : 0);
+    const int resident_units = !FEW ? 0 : SPLIT ? (p.KU + p.splits - 1) / p.splits : p.KU, resident_codes = resident_units * p.atoms * 1024;
+    const uint32_t ring0 = smem_u32(resident) + resident_codes + resident_units * G::kSc;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -245,7 +263,16 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
 
     // i-th piece of work of this block (the same sequence for every role; whole converged warps)
     auto get_work = [&](int i, MxWork& w) -> bool {
-        const int t = (int)blockIdx.x + i * (int)gridDim.x;
+        int t = (int)blockIdx.x + i * (int)gridDim.x;
+        w.k0 = 0;
+        w.k1 = p.KU;
+        if (SPLIT) {
+            if (i > 0) return false;
+            const int q = t % p.splits;
+            t /= p.splits;
+            w.k0 = p.KU * q / p.splits;
+            w.k1 = p.KU * (q + 1) / p.splits;
+        }
         if (t >= total) return false;
         const int mt = t / p.n_tiles;
         w.n_tile = t - mt * p.n_tiles;
@@ -274,12 +301,15 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         pdl_wait();
         if constexpr (FEW) {
             const TensorScale ts(p.a_scale ? __ldg(p.a_scale) : 1.0f);
-            const int chunks = p.KU * (kUnitK / 32);
+            const int q = SPLIT ? (int)blockIdx.x % p.splits : 0;             // the block's units of K
+            const int k0 = SPLIT ? p.KU * q / p.splits : 0, chunks = (SPLIT ? p.KU * (q + 1) / p.splits - k0 : p.KU) * (kUnitK / 32);
+            const T* x = reinterpret_cast<const T*>(p.x) + (SPLIT ? k0 * kUnitK : 0);
+            const int64_t K = SPLIT ? p.K - k0 * kUnitK : p.K;
             for (int id = threadIdx.x; id < p.M * chunks; id += G::kThreads) {
                 const int r = id / chunks, c = id - r * chunks, ku = c >> 3;
-                const int64_t left = p.K - (int64_t)c * 32;
+                const int64_t left = K - (int64_t)c * 32;
                 const int n = (int)(left < 0 ? 0 : left < 32 ? left : 32);
-                const T* src = reinterpret_cast<const T*>(p.x) + r * p.ldx + (int64_t)c * 32;
+                const T* src = x + r * p.ldx + (int64_t)c * 32;
                 float v[32];
                 if (p.x_vec == 32) load32<T, 32>(src, n, v);
                 else if (p.x_vec == 16) load32<T, 16>(src, n, v);
@@ -322,14 +352,14 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         // weights do not depend on the previous kernel: the first ring of them is requested before the wait for it
         if (!GROUPED) {
             if (warp == W_WARP && get_work(0, w))
-                for (; early < S && early < p.KU; ++early) load_w(early, early);
+                for (; early < S && early < w.k1 - w.k0; ++early) load_w(early, w.k0 + early);
         }
         if (FEW) load_tokens();
         else if (!waited && warp == A_WARP) pdl_wait();                       // weights go on; token rows are the previous kernel's
         for (int i = 0; (!FEW || warp == W_WARP) && ok && get_work(i, w); ++i) {
             const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
             const uint8_t* src = p.a + (int64_t)w.m_unit * p.KU * G::kUnit;
-            for (int ku = 0; ku < p.KU; ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
+            for (int ku = w.k0; ku < w.k1; ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
                 if (round > 0) ok = mbar_wait(&empty[s], (round - 1) & 1, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
@@ -377,13 +407,13 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             const uint32_t d = tmem_base + (uint32_t)(buf * G::kDCols);
             // a tile of 64 rows takes the scale columns of its rows out of the unit's four (32 rows each)
             const uint32_t sub = BN < 128 ? (uint32_t)((w.n_tile * BN) & 64) >> 5 : 0u;
-            for (int ku = 0; ku < p.KU; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
+            for (int ku = w.k0; ku < w.k1; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
                 ok = mbar_wait(&full[s], par, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
-                const uint64_t at_a = FEW ? (uint64_t)(ku * p.atoms * 64) : at, at_sa = FEW ? (uint64_t)(ku * (G::kSc >> 4)) : at;
+                const uint64_t at_a = FEW ? (uint64_t)((ku - w.k0) * p.atoms * 64) : at, at_sa = FEW ? (uint64_t)((ku - w.k0) * (G::kSc >> 4)) : at;
                 const uint32_t sfa = tmem_base + (uint32_t)G::kSf0 + set * (uint32_t)G::kSfCols;
                 const uint32_t sfw = sfa + (uint32_t)(G::kGroups * 4);
                 copy_scales<1, G::kGroups>(sfa, desc_sa + at_sa, 4, sel);
@@ -394,7 +424,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
 #pragma unroll
                 for (int b = 0; b < MMAS; ++b)
                     mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * BN, desc_a + at_a, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
-                                                       sfa, sfw + 4 * b + sub, 4 * NB, ku != 0, sel);
+                                                       sfa, sfw + 4 * b + sub, 4 * NB, ku != w.k0, sel);
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
             }
@@ -420,10 +450,10 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             const float alpha1 = GATEUP ? a_scale * (p.w_scale[1] ? __ldg(p.w_scale[1] + w.expert) : 1.0f) : 0.0f;
             ok = mbar_wait(&acc_full[buf], (it / AB) & 1, abort_flag);
             ok = __all_sync(0xFFFFFFFFu, ok);
-            if (!ok) break;
+            if (!ok && !SPLIT) break;                                         // (split: the epilogue's warps meet below, whatever became of the wait)
             tc_fence_after_sync();
             const int r = quarter * 32 + lane;                                // token row of the tile
-            const bool warp_has_rows = quarter * 32 < w.rows;
+            const bool warp_has_rows = ok && quarter * 32 < w.rows;
             uint32_t v[NB * C32][32];
             if (warp_has_rows) {
 #pragma unroll
@@ -434,7 +464,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive(&acc_empty[buf]);                      // the accumulators may be overwritten
-            if (!warp_has_rows) continue;
+            if (!SPLIT && !warp_has_rows) continue;
             const int n0 = w.n_tile * BN + part * CW;
             if constexpr (GATEUP) {
                 const int hku = (p.N + kUnitK - 1) / kUnitK;                  // k units of the output operand
@@ -466,6 +496,54 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                     put(n0, codes, sc);
                     if (w.n_tile == p.n_tiles - 1 && part == G::kParts - 1)
                         for (int k = p.n_tiles * BN; k < hku * kUnitK; k += 32) put(k, make_uint4(0, 0, 0, 0), 0);    // the rest of the last unit
+                }
+            } else if constexpr (SPLIT) {
+                // Partial sums to memory; the block that finds the others' there already adds them in the order of K (same bits on every
+                // call), all its epilogue warps sharing the tile, and stores.  Nobody waits for another block.
+                const int tile = (int)blockIdx.x / p.splits, span = (min(p.M, 128) + 31) / 32 * 32 * BN;     // span: a tile's partial sums
+                float* slots = p.partial + (int64_t)tile * p.splits * span;
+                if (ok && r < w.rows) {
+                    float* o = slots + ((int)blockIdx.x % p.splits) * span + r * BN + part * CW;
+#pragma unroll
+                    for (int c = 0; c < C32; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st_global_256(o + 32 * c + 8 * i, &v[c][8 * i]);
+                }
+                __threadfence();
+                bool last = false;
+                const int e0 = (int)threadIdx.x - EPI_WARP0 * 32;
+                if (epilogue_all<32 * G::kEpiWarps>(ok) && e0 == 0) {
+                    __threadfence();
+                    last = atomicAdd(p.counters + tile, 1) == p.splits - 1;
+                    if (last) p.counters[tile] = 0;
+                }
+                if (!epilogue_any<32 * G::kEpiWarps>(last)) break;
+                __threadfence();
+                T* y = reinterpret_cast<T*>(p.y) + (int64_t)w.row0 * p.ldy + w.n_tile * BN;
+                for (int e = 4 * e0; e < w.rows * BN; e += 128 * G::kEpiWarps) {       // four columns of a row: every split's in flight at once
+                    float4 v4[8];
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < p.splits) v4[q] = __ldcg(reinterpret_cast<const float4*>(slots + q * span + e));
+                    float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int q = 0; q < 8; ++q)
+                        if (q < p.splits) {
+                            sum[0] += v4[q].x;
+                            sum[1] += v4[q].y;
+                            sum[2] += v4[q].z;
+                            sum[3] += v4[q].w;
+                        }
+                    const int c = e % BN, left = p.N - w.n_tile * BN - c;
+                    T* o = y + (e / BN) * p.ldy + c;
+                    if (sizeof(T) == 2 && p.vec >= 16 && left >= 4) {
+                        if constexpr (sizeof(T) == 2)
+                            *reinterpret_cast<uint2*>(o) = make_uint2(Dt<T>::down2(alpha * sum[0], alpha * sum[1]), Dt<T>::down2(alpha * sum[2], alpha * sum[3]));
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (k < left) o[k] = Dt<T>::down(alpha * sum[k]);
+                    }
                 }
             } else {
                 if (p.vec < 16) {
@@ -722,10 +800,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
 
 // ------------------------------------------------------------ launches
 
-template <int FMT, int BN, bool GATEUP, typename T, int FORM>
+template <int FMT, int BN, bool GATEUP, typename T, int FORM, bool SPLIT = false>
 static qmm_status launch_t(const MxGemmParams& p, int64_t tiles, cudaStream_t st)
 {
-    auto kern = mx_gemm_kernel<FMT, BN, GATEUP, T, FORM>;
+    auto kern = mx_gemm_kernel<FMT, BN, GATEUP, T, FORM, SPLIT>;
     using G = MxGeom<FMT, BN, GATEUP, FORM>;
     static std::atomic<uint64_t> configured{0};                               // devices that have the attribute
     int dev = 0;
@@ -756,16 +834,46 @@ template <typename T> static int row_vec(const void* y, int64_t ldy)
     return a % 32 == 0 ? 32 : a % 16 == 0 ? 16 : a % 4 == 0 ? 4 : 2;
 }
 
-// Few rows: shared memory that M token rows take over all KU units.
+// Few rows: shared memory that M token rows take over KU units.
 static int few_resident(int fmt, int64_t M, int KU) { return KU * ((int)((M + 7) / 8) * 1024 + scale_bytes(fmt)); }
+
+// Blocks that share a tile's K, where the tiles leave most SMs idle: 2 to 8, of at least four units of K each.  A unit is 0.3 us of a block's
+// time; meeting costs about 2 us, and adding up 1 us more for 8 rows (every block's sums are written and read once).  So a share has to save
+// 12 units, and half a unit more for every row past 16.  Shared / whole, MXFP4, N = 2048: one token, K = 4096 5.2 / 6.1 us, 8192 5.8 / 9.8, 16384
+// 7.3 / 20.7; 16 tokens 6.9 / 8.0, 7.7 / 12.2; 64 tokens 10.6 / 8.4, 13.6 / 12.5, 15.1 / 20.7; 128 tokens, 16384 21.5 / 22.0; and two blocks a
+// tile, N = 8192: one token, K = 4096 7.0 / 6.6, 8192 10.2 / 10.7.
+static int mx_splits(int64_t M, int64_t N, int KU)
+{
+    const int64_t most = kNumSMs / ((N + 127) / 128), by_k = KU / 4;
+    int64_t s = most < by_k ? most : by_k;
+    if (s > 8) s = 8;
+    if (M > 128 || s < 2 || g_knobs.mx_no_split) return 1;
+    return KU - KU / s >= 12 + (M > 16 ? (M - 16) / 2 : 0) ? (int)s : 1;
+}
+
+// Workspace of a product behind the status word: counters (zero between calls) at kMxCounters, partial sums at kMxHeader.
+size_t mx_gemm_partial_bytes(int64_t M, int64_t N, int64_t K)
+{
+    const int splits = mx_splits(M, N, (int)k_units(K));
+    return splits > 1 ? (size_t)((N + 127) / 128 * splits) * ((M + 31) / 32 * 32) * 128 * sizeof(float) : 0;
+}
 
 template <int FMT, typename T, int FORM> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
 {
     using G = MxGeom<FMT, 128, false, FORM>;
     p.vec = row_vec<T>(p.y, p.ldy);
-    const int room = G::kRoom - (FORM == kMxFew ? few_resident(FMT, p.M, p.KU) : 0) - (p.vec < 16 ? G::kStaging : 0);
+    const int64_t tiles = row_tiles * p.n_tiles;
+    p.splits = 1;
+    if (FORM != kMxGrouped) {
+        p.splits = mx_splits(p.M, p.N, p.KU);
+        p.counters = p.status + kMxCounters / 4;
+        p.partial = reinterpret_cast<float*>(reinterpret_cast<char*>(p.status) + kMxHeader);
+    }
+    const int room = G::kRoom - (FORM == kMxFew ? few_resident(FMT, p.M, (p.KU + p.splits - 1) / p.splits) : 0) - (p.vec < 16 && p.splits == 1 ? G::kStaging : 0);
     p.stages = room / G::kStage < 10 ? room / G::kStage : 10;
-    return launch_t<FMT, 128, false, T, FORM>(p, row_tiles * p.n_tiles, st);
+    if constexpr (FORM != kMxGrouped)
+        if (p.splits > 1) return launch_t<FMT, 128, false, T, FORM, true>(p, tiles * p.splits, st);
+    return launch_t<FMT, 128, false, T, FORM>(p, tiles, st);
 }
 
 // Gate/up: tiles of 64 + 64 weight rows spread a decode step better over the SMs, tiles of 128 + 128 move fewer token rows: 128 experts of
@@ -860,11 +968,12 @@ qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int6
 }
 
 // Whether the product of a few rows takes them as they come (else they are quantised by a launch of their own).  Every block quantises all of them:
-// up to 16 rows of 2048 that costs 1.4 us and saves a launch (one token, 2048 x 2048: 8.8 -> 4.1 us), 8 rows of 8192 cost 3 to 5 us.  They may take
-// 112 KB, half of the shared memory.
-bool mx_few_fits(int fmt, int64_t M, int64_t K)
+// up to 16 rows of 2048 that costs 1.4 us and saves a launch (one token, 2048 x 2048: 8.8 -> 4.1 us), 8 rows of 8192 would cost 3 to 5 us (where
+// blocks share K, each takes its part only).  They may take 112 KB, half of the shared memory.
+bool mx_few_fits(int fmt, int64_t M, int64_t N, int64_t K)
 {
-    return M <= 16 && M * K <= 32768 && few_resident(fmt, M, (int)k_units(K)) <= 112 * 1024 && !g_knobs.mx_no_few;
+    const int KU = (int)k_units(K), splits = mx_splits(M, N, KU);
+    return M <= 16 && M * K <= 32768 * splits && few_resident(fmt, M, (KU + splits - 1) / splits) <= 112 * 1024 && !g_knobs.mx_no_few;
 }
 
 template <int FMT, typename T> static qmm_status few_t(MxGemmParams p, cudaStream_t st)

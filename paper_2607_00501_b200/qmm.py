@@ -459,12 +459,12 @@ def _operand(t: torch.Tensor, need: int, what: str) -> int:
 
 
 def _workspace(need: int, device, ws: torch.Tensor | None) -> torch.Tensor:
-    """ws, or a new workspace with a zeroed status word (callers on a hot path keep one)."""
+    """ws, or a new workspace with its header zeroed (callers on a hot path keep one)."""
     if need == 0:
         raise QmmError(1, last_error())
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=device)
-        ws[:256].zero_()
+        ws[:1024].zero_()
     return ws
 
 

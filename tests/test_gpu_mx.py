@@ -173,7 +173,7 @@ def check_product(Y, a, w, K, what=""):
 
 # one tile; K tails; few and many weight tiles; several token tiles; more tiles than SMs, ragged both ways
 SHAPES = [(1, 1, 1), (1, 128, 256), (3, 100, 32), (5, 130, 272), (128, 128, 512), (17, 256, 1024), (1, 2048, 2048), (9, 512, 2304), (127, 640, 1000),
-          (129, 1000, 520), (300, 384, 768), (1, 20000, 256), (200, 10000, 300), (700, 4100, 544), (2500, 3000, 288), (130, 129, 4000), (300, 301, 600), (1500, 2051, 300), (513, 998, 256)]
+          (129, 1000, 520), (300, 384, 768), (1, 20000, 256), (200, 10000, 300), (700, 4100, 544), (2500, 3000, 288), (130, 129, 4000), (300, 301, 600), (1500, 2051, 300), (513, 998, 256), (1, 2048, 8192), (40, 300, 5000), (128, 129, 4096), (200, 777, 6000), (14, 1900, 7000), (50, 515, 16384)]
 
 
 @pytest.mark.parametrize("fmt", FMTS)
@@ -194,13 +194,18 @@ def test_product(qmm, fmt, M, N, K):
                 check_product(qmm.mx_gemm(fmt, ap, M, wp, N, K, a_scale=ga, w_scale=gw, ws=ws, dtype=dt), a, w, K, "form " + form)
                 qmm.status_check(ws)
         qmm.debug_config(None)
+        if K >= 4096:                                                              # without blocks that share a tile's K
+            qmm.debug_config("mx_no_split", "1")
+            check_product(qmm.mx_gemm(fmt, ap, M, wp, N, K, a_scale=ga, w_scale=gw, ws=ws, dtype=dt), a, w, K, "whole K")
+            qmm.debug_config(None)
+            assert not ws[256:1024].any(), "the counters are zero between calls"
 
 
 @pytest.mark.parametrize("fmt", FMTS)
 @pytest.mark.parametrize("M", [1, 2, 3, 7, 8, 9, 16, 17, 31, 33, 64, 100, 128, 130, 256, 257, 400])
 def test_linear_is_quantize_then_product(qmm, fmt, M):
     """qmm_mx_linear gives the bits of qmm_mx_quantize followed by qmm_mx_gemm, whatever form it takes."""
-    for N, K in ((384, 800), (2048, 512), (200, 4096), (130, 9000)):
+    for N, K in ((384, 800), (2048, 512), (200, 4096), (130, 9000), (1100, 5000)):
         (xa, _, ga), (xw, _, gw) = operands(fmt, M, N, K, M + N)
         wp = qmm.mx_quantize(fmt, xw.cuda(), tensor_scale=gw)
         for dt in DTYPES.values():

@@ -26,7 +26,8 @@ def test_sizes(L):
     assert qmm.mx_bytes(32, 128, 256) == 16384 + 1024 and qmm.mx_bytes(16, 128, 256) == 16384 + 2048
     assert qmm.mx_bytes(32, 129, 257) == 4 * qmm.mx_bytes(32, 1, 1)
     assert qmm.mx_bytes(32, 0, 256) == 0 and qmm.mx_bytes(8, 128, 256) == 0 and qmm.mx_bytes(32, -1, 256) == 0 and qmm.mx_bytes(16, 1, 0) == 0
-    assert qmm.mx_linear_workspace_bytes(32, 130, 64, 512) == 256 + qmm.mx_bytes(32, 130, 512)
+    assert qmm.mx_linear_workspace_bytes(32, 130, 64, 512) == 1024 + qmm.mx_bytes(32, 130, 512)
+    assert qmm.mx_gemm_workspace_bytes(32, 1, 64, 512) == 1024 and qmm.mx_gemm_workspace_bytes(32, 1, 2048, 8192) > 1024       # partial sums
     # any routing fits: rows spread over the experts so that as many units as possible are begun
     for T, topk, E in ((1, 1, 1), (4, 8, 128), (100, 3, 2), (4096, 8, 128), (129, 1, 1)):
         P, u = T * topk, 17408
@@ -57,7 +58,8 @@ def test_refusals_of_the_microscaled_calls(L, a):
     assert L.qmm_mx_pack(32, a, a, 1, 256, a + 8, None) == 3
     assert L.qmm_mx_gemm(32, a, 1, a, 0, 256, None, None, 0, a, 256, a, 4096, None) == 1
     assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, None, None, 0, a, 63, a, 4096, None) == 2
-    assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, None, None, 0, a, 64, a, 100, None) == 4
+    assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, None, None, 0, a, 64, a, 1023, None) == 4
+    assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, None, None, 0, a, 64, a + 16, 8192, None) == 3
     assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, None, None, 0, a, 64, None, 0, None) == 4
     assert L.qmm_mx_gemm(32, a, 1, a + 8, 64, 256, None, None, 0, a, 64, a, 4096, None) == 3
     assert L.qmm_mx_gemm(32, a, 1, a, 64, 256, a, None, 0, a, 64, a, 4096, None) == 1
