@@ -99,7 +99,8 @@ template <typename T, int VEC> __device__ __forceinline__ void store32_any(AnyRo
 // unit is written as zeros.  Consecutive lanes hold consecutive chunks of a row (a row has a multiple of 8):
 // 4 (MXFP4) or 2 (NVFP4) neighbouring lanes join their scale bytes into one 4-byte store.
 // EXPERTS: the row is a token, quantised once and stored at the row of each of its pairs.
-// 8192 x 8192 fp16 -> MXFP4 is 171 MB of traffic: see the table of measurements for the rate.
+// 8192 x 8192 -> MXFP4: fp16 24 us, bf16 26, fp32 49 (6.2 to 7.2 TB/s, part of the codes still in L2: bound by HBM); -> NVFP4: 35, 35, 51 (16-bit values:
+// 4.9 TB/s, bound by instruction issue -- the quotients' correct rounding).
 template <int FMT, typename T, int VEC, bool EXPERTS>
 __global__ void __launch_bounds__(kQuantThreads)
 mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K, const float* __restrict__ tensor_scale,
@@ -157,76 +158,77 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
     }
 }
 
-// Thread = one 16-byte chunk of codes -> 32 values.  D = scale * g in fp32, value = code * D in fp32 (rounded once).
+// Elements per thread of the dequantisation, for rows of VEC-byte alignment.
+template <typename T> __host__ __device__ constexpr int dequantize_elements(int vec) { return vec == 32 && sizeof(T) == 4 ? 8 : 32; }
+
+// value = code * D in fp32 (rounded once), D = scale * g in fp32.  Thread = one 16-byte chunk of codes, 32 values.  Rows of fp32 that 32-byte
+// stores reach: thread = one such store, 8 values, so that a warp's store covers whole lines (8192 x 8192 MXFP4 51.7 us, 5.9 TB/s, against 63.2;
+// 16-bit values gain nothing from it: 30.3 against 29.9 us, 5.7 TB/s).  Bound by the writes.
 template <int FMT, typename T, int VEC>
 __global__ void __launch_bounds__(kQuantThreads)
 mx_dequantize_kernel(const uint8_t* __restrict__ packed, int64_t rows, int64_t K, const float* __restrict__ tensor_scale,
                      T* __restrict__ out, int64_t ldo)
 {
     pdl_wait();
-    const int64_t chunks = (K + 31) / 32;
+    constexpr int V = dequantize_elements<T>(VEC);
+    const int64_t pieces = (K + V - 1) / V;
     int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
-    const bool live = id < rows * chunks;
+    const bool live = id < rows * pieces;
     if (VEC >= 16 && !live) return;
     if (!live) id = 0;
-    const int64_t row = id / chunks;
-    const int c = (int)(id - row * chunks);
+    const int64_t row = (uint64_t)(rows * pieces) >> 32 ? id / pieces : (int64_t)((uint32_t)id / (uint32_t)pieces);
+    const int64_t k = (id - row * pieces) * V;
     const float g = tensor_scale ? __ldg(tensor_scale) : 1.0f;
-    const uint8_t* unit = packed + ((row >> 7) * k_units(K) + (c >> 3)) * unit_bytes(FMT);
-    const uint32_t r = (uint32_t)(row & 127);
-    const uint4 q = __ldg(reinterpret_cast<const uint4*>(unit + chunk_offset(r, c & 7)));
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-    float D[2];
-    if (FMT == QMM_MXFP4) {
-        D[0] = D[1] = e8m0_value(unit[scale_offset(r, (c & 7) >> 2) + (c & 3)]);
+    const uint8_t* unit = packed + ((row >> 7) * k_units(K) + k / kUnitK) * unit_bytes(FMT);
+    const uint32_t r = (uint32_t)(row & 127), in = (uint32_t)(k & (kUnitK - 1));
+    const uint8_t* codes = unit + chunk_offset(r, in >> 5) + ((in & 31) >> 1);
+    uint32_t w[V / 8];
+    if constexpr (V == 32) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(codes));
+        w[0] = q.x, w[1] = q.y, w[2] = q.z, w[3] = q.w;
     } else {
-        const uint16_t s = *reinterpret_cast<const uint16_t*>(unit + scale_offset(r, (c & 7) >> 1) + 2 * (c & 1));
-        D[0] = e4m3_value(s & 0xFFu) * g;
-        D[1] = e4m3_value(s >> 8) * g;
+        w[0] = __ldg(reinterpret_cast<const uint32_t*>(codes));
     }
-    float v[32];
+    constexpr int BLOCKS = V > FMT ? V / FMT : 1;
+    float D[BLOCKS];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < BLOCKS; ++i) {
+        const uint32_t b = in / FMT + i;
+        const uint8_t s = __ldg(unit + scale_offset(r, b >> 2) + (b & 3));
+        D[i] = FMT == QMM_MXFP4 ? e8m0_value(s) : e4m3_value(s) * g;
+    }
+    float v[V];
+#pragma unroll
+    for (int i = 0; i < V / 2; ++i) {
         const __half2_raw h = __nv_cvt_fp4x2_to_halfraw2((__nv_fp4x2_storage_t)(w[i >> 2] >> (8 * (i & 3))), __NV_E2M1);
         const float2 f = __half22float2(__half2(h));
-        v[2 * i] = f.x * D[i >> 3];
-        v[2 * i + 1] = f.y * D[i >> 3];
+        v[2 * i] = f.x * D[2 * i / (V / BLOCKS)];
+        v[2 * i + 1] = f.y * D[2 * i / (V / BLOCKS)];
     }
-    T* o = out + row * ldo + (int64_t)c * 32;
-    const int64_t left = K - (int64_t)c * 32;
-    if (VEC >= 16 && left >= 32) {
-        if constexpr (sizeof(T) == 2) {
-            uint32_t u[16];
-#pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (VEC == 32) {
-                    if (i < 2) st_global_256(reinterpret_cast<uint8_t*>(o) + 32 * i, u + 8 * i);
-                } else {
-                    reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-                }
-            }
-        } else {
-            uint32_t u[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) u[i] = __float_as_uint(v[i]);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (VEC == 32) {
-                    if (i < 4) st_global_256(reinterpret_cast<uint8_t*>(o) + 32 * i, u + 8 * i);
-                } else {
-                    reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
-                }
-            }
-        }
-    } else if constexpr (VEC >= 16) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < left) o[i] = Dt<T>::down(v[i]);
-    } else {
+    T* o = out + row * ldo + k;
+    const int64_t left = K - k;
+    if constexpr (VEC < 16) {
         __shared__ AnyRows<T> sm;
         store32_any<T, VEC>(sm, o, live ? (int)(left < 32 ? left : 32) : 0, v);
+    } else if (left >= V) {
+        constexpr int W = V * (int)sizeof(T) / 4;
+        uint32_t u[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(T) == 2) u[i] = Dt<T>::down2(v[2 * i], v[2 * i + 1]);
+            else u[i] = __float_as_uint(v[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < W / 4; ++i)
+            if (VEC == 32) {
+                if (i % 2 == 0) st_global_256(reinterpret_cast<uint4*>(o) + i, u + 4 * i);
+            } else {
+                reinterpret_cast<uint4*>(o)[i] = make_uint4(u[4 * i], u[4 * i + 1], u[4 * i + 2], u[4 * i + 3]);
+            }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < left) o[i] = Dt<T>::down(v[i]);
     }
 }
 
@@ -338,10 +340,11 @@ qmm_status launch_mx_quantize_experts(int fmt, int dtype, const void* x, int64_t
 template <int FMT, typename T>
 static qmm_status dequantize_t(const void* packed, int64_t rows, int64_t K, const float* ts, void* out, int64_t ldo, cudaStream_t st)
 {
-    dim3 grid;
-    const qmm_status s = launch_grid(rows * ((K + 31) / 32), &grid);
-    if (s != QMM_OK) return s;
     const uintptr_t a = reinterpret_cast<uintptr_t>(out) | (rows > 1 ? (uintptr_t)(ldo * (int64_t)sizeof(T)) : 0);
+    const int per = dequantize_elements<T>(a % 32 == 0 ? 32 : 2);
+    dim3 grid;
+    const qmm_status s = launch_grid(rows * ((K + per - 1) / per), &grid);
+    if (s != QMM_OK) return s;
     return launch_pdl(a % 32 == 0 ? mx_dequantize_kernel<FMT, T, 32> : a % 16 == 0 ? mx_dequantize_kernel<FMT, T, 16> : a % 4 == 0 ? mx_dequantize_kernel<FMT, T, 4> : mx_dequantize_kernel<FMT, T, 2>,
                       grid, kQuantThreads, st,
                       "microscaled dequantisation launch", (const uint8_t*)packed, rows, K, ts, (T*)out, ldo);
