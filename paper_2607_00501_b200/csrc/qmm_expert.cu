@@ -436,6 +436,8 @@ template <typename T, int V> __device__ __forceinline__ Raw<T, V> scaled(const R
 
 // Thread = one vector of one token's row: read once, written at the row of each of the token's pairs.  The rows past the
 // last (one per dropped pair) are dealt to the tokens by index and zeroed.
+// Bound by HBM (one row read, topk written): 8192 tokens x 8, 2048 bf16 48.6 us, 6.2 TB/s (50.0 with weights); fp32 94.9, 6.4.
+// 61 tokens: 2.6 us, a launch.
 template <typename T, int V>
 __global__ void __launch_bounds__(kMoveThreads)
 expert_gather_kernel(const T* __restrict__ x, int64_t ldx, int tokens, int topk, int nv, const int* __restrict__ order, const int* __restrict__ place,
@@ -461,7 +463,8 @@ expert_gather_kernel(const T* __restrict__ x, int64_t ldx, int tokens, int topk,
     }
 }
 
-// Thread = one vector of one token's row; the rows of up to eight pairs are in flight at once, added in order.
+// Thread = one vector of one token's row; the rows of up to eight pairs are in flight at once, added in order (fp32).
+// Bound by HBM (topk rows read, one written): 8192 tokens x 8, 2048 bf16 48.6 us, 6.2 TB/s; fp32 93.4, 6.5.  61 tokens: 2.0 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kMoveThreads)
 expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int topk, int nv, const int* __restrict__ place,
@@ -499,6 +502,7 @@ expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int to
 
 // Block = one token: its row of dy against the rows of its pairs, eight pairs at a time.  A pair's dot product is
 // added over the thread's vectors, the warp (shuffles) and the warps in a fixed order.
+// Bound by HBM (dy and topk rows read, topk written): 8192 tokens x 8, 2048 bf16 93.0 us, 6.1 TB/s; fp32 174.9, 6.5.  61 tokens: 3.4 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(kMoveThreads)
 expert_combine_grad_kernel(const T* __restrict__ dy, int64_t lddy, const T* __restrict__ ys, int64_t ldys, int topk, int nv,

@@ -16,8 +16,13 @@
 // Roles: warps 0 and 2 load weights and tokens, warp 1 issues copies of scales and MMAs (converged, one elected lane), warps 4.. run
 // the epilogue: they take the accumulators into registers at once, free them, then work and store while the next tile's
 // MMAs run.  The kernel is persistent over tiles, ring and barrier phases run on across them.
-// Tile t = (token tile t / n_tiles, weight tile t % n_tiles).  BN = 128; 64 in the gate/up form of few rows.  (A K split with sums joined through a cluster's shared memory was slower: 8.8 us against 6 for one
-// token and a 2048 x 2048 matrix -- clusters of eight do not all fit the GPU at once, and their launch costs 3 us.)
+// Tile t = (token tile t / n_tiles, weight tile t % n_tiles).  BN = 128; 64 in the gate/up form of few rows.
+// Few rows, few tiles, long K: blocks share a tile's K (mx_splits) and meet through memory.  (Meeting through the shared memory of a cluster
+// was slower: 8.8 us against 6 unshared for one token and a 2048 x 2048 matrix -- clusters of eight do not all fit the GPU at once, and their
+// launch costs 3 us.)
+// What bounds it: one token, 128256 x 2048 25 us (MXFP4; 140 MB, 5.6 TB/s), 2048 x 2048 4.1 us (launch, first loads, 1.4 us of quantising the row
+// in every block); one token, 2048 x 8192 5.8 us.  Gate/up of 128 experts x 768 x 2048, 16384 pairs: 53 us, DRAM 56 % and tensor pipe 35 % busy:
+// the 128-row tiles of one SM take 17 KB per 256 cycles each of tokens and weights from L2.
 // Grouped: token tiles of the experts' rows, from the device arrays units[] / offsets[].
 // Every mbarrier wait is bounded; on give-up the block records QMM_ERR_DEVICE_TIMEOUT, waits (bounded) for its copies
 // in flight, frees its tensor memory and returns.
@@ -590,6 +595,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
 // the ring's round trip bounded the kernel at 40 % of this form).  tcgen05.commit frees ring slots and hands over the
 // accumulators in both blocks.  Tensor memory holds one 256-column accumulator beside two sets of scale columns: eight epilogue
 // warps take it into registers at once (128 columns each), free it, and store while the next tile's MMAs run.
+// Bound by the tensor pipe, and that by the power limit: NVFP4 8192 x 8192 x 8192 199 us (5.5 PFLOP/s, the pipe 74 % busy) after a pause, 226 to 234
+// back to back, 158 on constant data.
 template <int FMT> struct MxPairGeom {
     static constexpr int kSc = scale_bytes(FMT);
     static constexpr int kA = 0, kB = unit_bytes(FMT), kSb = kB + kCodeBytes;              // A unit | B codes | scales of both B units
