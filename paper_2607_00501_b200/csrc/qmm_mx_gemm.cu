@@ -55,11 +55,11 @@ struct MxGemmParams {
     int64_t ldx, K;
     int x_vec;                       // widest aligned load of x
     int atoms;                       // few: 8-row atoms per unit (1 or 2)
+    int stages;                      // ring depth (what resident rows or staging leave)
+    int* status;
     int splits;                      // dense, few: blocks that share a tile's K (1: none); then every block has one piece of work, and
     float* partial;                  // partial sums go here, [tile][split][rows, a multiple of 32][128 columns],
     int* counters;                   // per tile, zero between calls: the block that comes last adds the partial sums
-    int stages;                      // ring depth (what resident rows or staging leave)
-    int* status;
 };
 
 constexpr int kMxMaxE = 1024;
@@ -107,7 +107,7 @@ struct MxWork {
     int rows;                        // token rows in it (1 .. 128)
     int row0;                        // first row of Y
     int n_tile, expert;
-    int k0, k1;                      // k units
+    int k0, k1;                      // k units (K shared between blocks)
 };
 
 // silu(g) u = g u / (1 + 2^(-g log2 e)) for two features at a time, g and u still to be multiplied by their tensor scales:
@@ -266,11 +266,12 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
     const int m_tiles = GROUPED ? s_units[p.E] : (p.M + 127) >> 7;
     const int total = m_tiles * p.n_tiles;
 
+    // the units of K of a piece of work
+    auto K0 = [&](const MxWork& w) { return SPLIT ? w.k0 : 0; };
+    auto K1 = [&](const MxWork& w) { return SPLIT ? w.k1 : p.KU; };
     // i-th piece of work of this block (the same sequence for every role; whole converged warps)
     auto get_work = [&](int i, MxWork& w) -> bool {
         int t = (int)blockIdx.x + i * (int)gridDim.x;
-        w.k0 = 0;
-        w.k1 = p.KU;
         if (SPLIT) {
             if (i > 0) return false;
             const int q = t % p.splits;
@@ -357,14 +358,14 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         // weights do not depend on the previous kernel: the first ring of them is requested before the wait for it
         if (!GROUPED) {
             if (warp == W_WARP && get_work(0, w))
-                for (; early < S && early < w.k1 - w.k0; ++early) load_w(early, w.k0 + early);
+                for (; early < S && early < K1(w) - K0(w); ++early) load_w(early, K0(w) + early);
         }
         if (FEW) load_tokens();
         else if (!waited && warp == A_WARP) pdl_wait();                       // weights go on; token rows are the previous kernel's
         for (int i = 0; (!FEW || warp == W_WARP) && ok && get_work(i, w); ++i) {
             const uint32_t rows8 = (uint32_t)(w.rows + 7) & ~7u;
             const uint8_t* src = p.a + (int64_t)w.m_unit * p.KU * G::kUnit;
-            for (int ku = w.k0; ku < w.k1; ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
+            for (int ku = K0(w); ku < K1(w); ++ku, ++g, s + 1 == S ? (s = 0, ++round) : ++s) {
                 if (round > 0) ok = mbar_wait(&empty[s], (round - 1) & 1, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
@@ -412,13 +413,13 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             const uint32_t d = tmem_base + (uint32_t)(buf * G::kDCols);
             // a tile of 64 rows takes the scale columns of its rows out of the unit's four (32 rows each)
             const uint32_t sub = BN < 128 ? (uint32_t)((w.n_tile * BN) & 64) >> 5 : 0u;
-            for (int ku = w.k0; ku < w.k1; ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
+            for (int ku = K0(w); ku < K1(w); ++ku, set ^= 1, s + 1 == S ? (s = 0, par ^= 1) : ++s) {
                 ok = mbar_wait(&full[s], par, abort_flag);
                 ok = __all_sync(0xFFFFFFFFu, ok);
                 if (!ok) break;
                 tc_fence_after_sync();
                 const uint64_t at = (uint64_t)(s * (G::kStage >> 4));
-                const uint64_t at_a = FEW ? (uint64_t)((ku - w.k0) * p.atoms * 64) : at, at_sa = FEW ? (uint64_t)((ku - w.k0) * (G::kSc >> 4)) : at;
+                const uint64_t at_a = FEW ? (uint64_t)((ku - K0(w)) * p.atoms * 64) : at, at_sa = FEW ? (uint64_t)((ku - K0(w)) * (G::kSc >> 4)) : at;
                 const uint32_t sfa = tmem_base + (uint32_t)G::kSf0 + set * (uint32_t)G::kSfCols;
                 const uint32_t sfw = sfa + (uint32_t)(G::kGroups * 4);
                 copy_scales<1, G::kGroups>(sfa, desc_sa + at_sa, 4, sel);
@@ -429,7 +430,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
 #pragma unroll
                 for (int b = 0; b < MMAS; ++b)
                     mma_fp4_stage<1, FMT == QMM_MXFP4>(d + b * BN, desc_a + at_a, desc_w + at + b * G::kCodeStep, idesc_fp4(FMT == QMM_MXFP4, 128, G::kDCols / MMAS),
-                                                       sfa, sfw + 4 * b + sub, 4 * NB, ku != w.k0, sel);
+                                                       sfa, sfw + 4 * b + sub, 4 * NB, ku != K0(w), sel);
                 mma_commit_sel(&empty[s], sel);
                 __syncwarp();
             }
@@ -458,7 +459,7 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             if (!ok && !SPLIT) break;                                         // (split: the epilogue's warps meet below, whatever became of the wait)
             tc_fence_after_sync();
             const int r = quarter * 32 + lane;                                // token row of the tile
-            const bool warp_has_rows = ok && quarter * 32 < w.rows;
+            const bool warp_has_rows = (!SPLIT || ok) && quarter * 32 < w.rows;
             uint32_t v[NB * C32][32];
             if (warp_has_rows) {
 #pragma unroll
