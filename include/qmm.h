@@ -515,8 +515,11 @@ qmm_status qmm_mx_experts_gemm(qmm_mx_format fmt, const void* a, int32_t T, int3
                                int32_t* status, void* stream);
 
 /* The routed feed-forward layer made of the calls above:
- *   sort; quantise x into the expert order; h = silu(Wgate x) * (Wup x); d = Wdown h rounded to `dtype`;
- *   out[t, :] = sum_j weights[t, j] * d[place[t, j], :].                                               */
+ *   sort; quantise x into the expert order; h = silu(Wgate x) * (Wup x); d = Wdown h;
+ *   out[t, :] = sum_j weights[t, j] * d[place[t, j], :], summed in fp32 and rounded to `dtype` once.
+ * rows_f32 says how d is kept between the two steps.  0: rounded to `dtype`, the bits of qmm_mx_experts_gemm and
+ * qmm_expert_combine in that type, half the traffic; an fp16 row beyond 65504 is then infinite whatever its weight.
+ * 1: in fp32.                                                                                         */
 typedef struct {
     int32_t T, H, I, E, topk;      /* tokens, hidden, expert intermediate, experts, k      */
     int32_t fmt, dtype;            /* qmm_mx_format of weights and activations; qmm_dtype of X and out */
@@ -530,6 +533,7 @@ typedef struct {
     const float *gate_scale, *up_scale, *down_scale;       /* [E] each (NVFP4), or NULL    */
     void* out;                     /* [T, ldo], written                                    */
     int64_t ldo;
+    int32_t rows_f32;              /* 1: experts' rows stay fp32 until they are summed; 0: rounded to dtype */
 } qmm_mx_moe_args;
 size_t qmm_mx_moe_workspace_bytes(const qmm_mx_moe_args* args);          /* host pointer; only sizes are read */
 /* ws: device, 256-byte aligned, its first 256 bytes zeroed once (status word).                        */

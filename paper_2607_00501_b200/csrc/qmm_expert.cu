@@ -371,7 +371,8 @@ qmm_status launch_expert_sort_quantize(int fmt, int dtype, const int* idx, int64
 
 constexpr int kMoveThreads = 256;
 
-// One vector of V elements of a row: V * sizeof(T) = 16 bytes, 4 bytes, or a single element, as the rows' alignment allows.
+// One vector of V elements of a row: V * sizeof(T) = 16 bytes, 4 bytes, or a single element, as the rows' alignment allows (8 bytes: 16-bit sums of
+// fp32 rows).
 // Raw<T, V> is the vector as loaded: several of them in flight cost half the registers of their fp32 form.
 template <typename T, int V> struct Raw {
     static constexpr int B = V * (int)sizeof(T);
@@ -391,6 +392,7 @@ template <typename T, int V> struct Raw {
     __device__ __forceinline__ void store(T* p) const
     {
         if constexpr (B == 16) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        else if constexpr (B == 8) *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
         else if constexpr (B == 4) *reinterpret_cast<uint32_t*>(p) = u[0];
         else *reinterpret_cast<unsigned short*>(p) = (unsigned short)u[0];
     }
@@ -465,10 +467,11 @@ expert_gather_kernel(const T* __restrict__ x, int64_t ldx, int tokens, int topk,
 
 // Thread = one vector of one token's row; the rows of up to eight pairs are in flight at once, added in order (fp32).
 // Bound by HBM (topk rows read, one written): 8192 tokens x 8, 2048 bf16 48.6 us, 6.2 TB/s; fp32 93.4, 6.5.  61 tokens: 2.0 us.
-template <typename T, int V>
+// TO: type of the sums (fp32 rows may have 16-bit sums).
+template <typename T, typename TO, int V>
 __global__ void __launch_bounds__(kMoveThreads)
 expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int topk, int nv, const int* __restrict__ place,
-                      const float* __restrict__ weights, T* __restrict__ y, int64_t ldy)
+                      const float* __restrict__ weights, TO* __restrict__ y, int64_t ldy)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -476,7 +479,7 @@ expert_combine_kernel(const T* __restrict__ ys, int64_t ldys, int tokens, int to
     const int64_t t = id / nv;
     if (t >= tokens) return;
     const int64_t h = (id - t * nv) * V;
-    Vec<T, V> acc;
+    Vec<TO, V> acc;
 #pragma unroll
     for (int i = 0; i < V; ++i) acc.f[i] = 0.0f;
     for (int j0 = 0; j0 < topk; j0 += 8) {
@@ -605,18 +608,32 @@ qmm_status launch_expert_gather(int dtype, const void* x, int64_t ldx, int T, in
     });
 }
 
-qmm_status launch_expert_combine(int dtype, const void* ys, int64_t ldys, int T, int topk, int64_t H, const int* place, const float* weights, void* y, int64_t ldy,
-                                 cudaStream_t st)
+template <typename T, typename TO, int V>
+static qmm_status combine_t(const void* ys, int64_t ldys, int T_, int topk, int64_t H, const int* place, const float* weights, void* y, int64_t ldy, cudaStream_t st)
+{
+    const int nv = (int)(H / V);
+    dim3 grid;
+    const qmm_status s = move_grid((int64_t)T_ * nv, &grid);
+    if (s != QMM_OK) return s;
+    return launch_pdl(expert_combine_kernel<T, TO, V>, grid, kMoveThreads, 0, 1, st, "expert combine launch", (const T*)ys, ldys, T_, topk, nv, place, weights, (TO*)y, ldy);
+}
+
+// rows_dtype: type of ys, that of y or fp32.
+qmm_status launch_expert_combine(int rows_dtype, int dtype, const void* ys, int64_t ldys, int T, int topk, int64_t H, const int* place, const float* weights, void* y,
+                                 int64_t ldy, cudaStream_t st)
 {
     const int size = dtype == QMM_F32 ? 4 : 2;
-    const int V = vector_of(size, H, bits_of(ys, ldys, size) | bits_of(y, ldy, size)), nv = (int)(H / V);
-    dim3 grid;
-    const qmm_status s = move_grid((int64_t)T * nv, &grid);
-    if (s != QMM_OK) return s;
-    return by_type(dtype, V, [&](auto type, auto v) {
+    if (rows_dtype != dtype) {                             // fp32 rows, 16-bit sums: 16-byte loads, 8-byte stores
+        const bool wide = vector_of(4, H, bits_of(ys, ldys, 4)) == 4 && bits_of(y, ldy, size) % 8 == 0;
+        if (dtype == QMM_F16)
+            return wide ? combine_t<float, __half, 4>(ys, ldys, T, topk, H, place, weights, y, ldy, st)
+                        : combine_t<float, __half, 1>(ys, ldys, T, topk, H, place, weights, y, ldy, st);
+        return wide ? combine_t<float, __nv_bfloat16, 4>(ys, ldys, T, topk, H, place, weights, y, ldy, st)
+                    : combine_t<float, __nv_bfloat16, 1>(ys, ldys, T, topk, H, place, weights, y, ldy, st);
+    }
+    return by_type(dtype, vector_of(size, H, bits_of(ys, ldys, size) | bits_of(y, ldy, size)), [&](auto type, auto v) {
         using D = decltype(type);
-        return launch_pdl(expert_combine_kernel<D, decltype(v)::value>, grid, kMoveThreads, 0, 1, st, "expert combine launch", (const D*)ys, ldys, T, topk, nv, place,
-                          weights, (D*)y, ldy);
+        return combine_t<D, D, decltype(v)::value>(ys, ldys, T, topk, H, place, weights, y, ldy, st);
     });
 }
 

@@ -103,7 +103,7 @@ class MxMoeArgs(ctypes.Structure):
         ("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p),
         ("x_scale", ctypes.c_void_p), ("h_scale", ctypes.c_void_p), ("gate_scale", ctypes.c_void_p),
         ("up_scale", ctypes.c_void_p), ("down_scale", ctypes.c_void_p),
-        ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64),
+        ("out", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("rows_f32", ctypes.c_int32),
     ]
 
 
@@ -644,18 +644,20 @@ def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor
 
 
 def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int, out, x_scale=None, gate_scale=None, up_scale=None,
-                down_scale=None, h_scale=None) -> MxMoeArgs:
-    """Arguments of mx_moe_run: build once and reuse while the tensors stay where they are (the struct keeps them alive)."""
+                down_scale=None, h_scale=None, rows_dtype: torch.dtype | None = None) -> MxMoeArgs:
+    """Arguments of mx_moe_run: build once and reuse while the tensors stay where they are (the struct keeps them alive).
+    rows_dtype: type of the experts' rows on their way to the weighted sum, X's (default) or torch.float32."""
     xp, ldx, T, H = _rows2d(X, "X")
     op, ldo, r, c = _rows2d(out, "out")
     topk = idx.shape[1]
     assert idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape[0] == T
     assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape == idx.shape
     assert (r, c) == (T, H) and out.dtype == X.dtype
+    assert rows_dtype in (None, X.dtype, torch.float32), "rows_dtype: X's type or torch.float32"
     gu, dn = E * _mx_need(fmt, I, H), E * _mx_need(fmt, H, I)
     a = MxMoeArgs(T, H, I, E, topk, fmt, DTYPES[X.dtype], xp, ldx, idx.data_ptr(), weights.data_ptr(), _operand(w_gate, gu, "w_gate"),
                   _operand(w_up, gu, "w_up"), _operand(w_down, dn, "w_down"), _scalar(x_scale), _scalar(h_scale), _scalar(gate_scale, E),
-                  _scalar(up_scale, E), _scalar(down_scale, E), op, ldo)
+                  _scalar(up_scale, E), _scalar(down_scale, E), op, ldo, int(rows_dtype is torch.float32))
     a._keep = (X, idx, weights, w_gate, w_up, w_down, out, x_scale, gate_scale, up_scale, down_scale, h_scale)
     return a
 
@@ -670,7 +672,7 @@ def mx_moe_run(args: MxMoeArgs, ws: torch.Tensor) -> None:
 
 def mx_moe(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int, out=None, ws=None, **scales) -> torch.Tensor:
     """A routed feed-forward layer in 4 bits: out [T, H] from X [T, H], idx / weights [T, topk] and E packed matrices of each kind
-    (scales: x_scale, h_scale, and [E] gate_scale, up_scale, down_scale for NVFP4)."""
+    (scales: x_scale, h_scale, and [E] gate_scale, up_scale, down_scale for NVFP4; rows_dtype as in mx_moe_args)."""
     if out is None:
         out = torch.empty_like(X, memory_format=torch.contiguous_format)
     args = mx_moe_args(fmt, X, idx, weights, w_gate, w_up, w_down, I, E, out, **scales)

@@ -1,0 +1,48 @@
+"""GPU parity of microscaled calls in company: workspaces shared between operators and between batch sizes, calls without rows."""
+import numpy as np
+import pytest
+import torch
+
+from tests import mxref
+from tests.test_gpu_mx import FMTS, f64, scale_of
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def qmm():
+    from paper_2607_00501_b200 import qmm as _qmm
+    assert torch.cuda.is_available()
+    _qmm.lib()
+    return _qmm
+
+
+def layer(qmm, T=6, H=256, I=128, E=8, topk=2, dtype=torch.float16, scale=0.05):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    make = lambda n, k: torch.cat([qmm.mx_quantize(32, torch.randn(n, k, generator=gen, device="cuda") * scale) for _ in range(E)])  # noqa: E731
+    idx = torch.randint(0, E, (T, topk), generator=gen, dtype=torch.int32, device="cuda")
+    X = torch.randn(T, H, generator=gen, device="cuda").to(dtype)
+    w = torch.rand(T, topk, generator=gen, device="cuda")
+    return X, idx, w, make(I, H), make(I, H), make(H, I), I, E
+
+
+def test_experts_rows_in_32_bits(qmm):
+    """With rows_dtype = float32 the experts' rows reach the weighted sum unrounded: out is within one rounding of the sum of the fp32 rows,
+    and a row beyond fp16 comes back where its weight brings it back."""
+    for dtype, T, H, I in ((torch.float16, 6, 256, 128), (torch.bfloat16, 300, 320, 96), (torch.float16, 50, 257, 90), (torch.float32, 20, 64, 64)):
+        X, idx, w, gate, up, down, I, E = args = layer(qmm, T=T, H=H, I=I, dtype=dtype)
+        out = qmm.mx_moe(32, *args, rows_dtype=torch.float32)
+        plan = qmm.expert_sort(idx, E)
+        h = qmm.mx_experts_gate_up(32, qmm.mx_quantize_experts(32, X, idx, plan), plan, gate, up, I, H)
+        Y = qmm.mx_experts_gemm(32, h, plan, down, H, I, dtype=torch.float32)
+        assert torch.equal(out, qmm.expert_combine(Y, plan, w).to(dtype))            # the fp32 sum, rounded once
+        buf = torch.full((T, H + 5), 7.0, dtype=dtype, device="cuda")              # rows of any alignment
+        qmm.mx_moe(32, *args, out=buf[:, 1:H + 1], rows_dtype=torch.float32)
+        assert torch.equal(buf[:, 1:H + 1], out) and bool((buf[:, 0] == 7).all()) and bool((buf[:, H + 1:] == 7).all())
+    X, idx, w, gate, up, down, I, E = layer(qmm, scale=4.0)
+    w = w * 1e-4
+    plain = qmm.mx_moe(32, X, idx, w, gate, up, down, I, E)
+    kept = qmm.mx_moe(32, X, idx, w, gate, up, down, I, E, rows_dtype=torch.float32)
+    assert torch.isfinite(kept).all() and not torch.isfinite(plain).all()
+    with pytest.raises(AssertionError):
+        qmm.mx_moe(32, X, idx, w, gate, up, down, I, E, rows_dtype=torch.bfloat16)
