@@ -178,6 +178,27 @@ struct TensorScale {
     }
 };
 
+// The two tensor scales a, b of a product (positive, finite) as factors of its fp32 sum, applied one after the other: sum * first * second.  Their product is one
+// factor (first = 1) where it is far from the ends of the exponent range.  Elsewhere it could be infinite or lose its bits although a b sum is an fp32
+// number -- sums of codes and block scales run from 2^-20 to about 2^43 -- and the two are applied in the order that keeps the step between inside the range.
+struct ProductScale {
+    float first, second;
+    __device__ __forceinline__ ProductScale(float a, float b) : first(1.0f), second(a * b)
+    {
+        if (second >= 0x1p-100f && second <= 0x1p100f) return;
+        const bool small = second < 1.0f;
+        first = small ? fmaxf(a, b) : fminf(a, b);
+        second = small ? fminf(a, b) : fmaxf(a, b);
+    }
+    // the first factor, on accumulators (bits of fp32)
+    template <int N> __device__ __forceinline__ void apply_first(uint32_t (&v)[N]) const
+    {
+        if (first == 1.0f) return;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * first);
+    }
+};
+
 // Correctly rounded a / b from r = rn(1 / b): q0 = a r, e = a - q0 b (exact in one FMA), q = q0 + e r; and rn(1 / b) itself from an
 // approximation within an ulp, by one such step, unless b's significand is all ones (P. W. Markstein, "Computation of elementary
 // functions on the IBM RISC System/6000 processor", IBM J. Res. Dev. 34, 1990).  Need b and the quotient away from the ends of the

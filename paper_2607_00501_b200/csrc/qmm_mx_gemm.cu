@@ -110,9 +110,9 @@ struct MxWork {
     int k0, k1;                      // k units (K shared between blocks)
 };
 
-// silu(g) u = g u / (1 + 2^(-g log2 e)) for two features at a time, g and u still to be multiplied by their tensor scales:
-// c = {-alpha log2 e}, both factors of the product in `ab`.  2^x and 1 / x are the hardware's approximations (relative error of a
-// few 2^-23 each); g << 0 gives 2^x = inf and the limit 0.
+// silu(g) u = (g / (1 + 2^(-g log2 e))) u for two features at a time, g and u still to be multiplied by the factors a0 and a1.  2^x and 1 / x are the hardware's
+// approximations (relative error of a few 2^-23 each); g << 0 gives 2^x = inf and silu = -0.  silu is complete before u comes in: g u may be beyond fp32 where
+// silu(g) u is not.  The denominator is held times 2^-8, so that its reciprocal is no subnormal (which the approximation flushes) while silu itself is none.
 __device__ __forceinline__ float ex2_approx(float x)
 {
     float y;
@@ -125,11 +125,12 @@ __device__ __forceinline__ float rcp_approx(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float2 silu_mul2(float2 g, float2 u, float c, float ab)
+__device__ __forceinline__ float2 silu_mul2(float2 g, float2 u, float a0, float a1)
 {
-    const float2 x = mul2(g, both(c));
-    const float2 den = make_float2(1.0f + ex2_approx(x.x), 1.0f + ex2_approx(x.y));
-    return mul2(mul2(mul2(g, both(ab)), u), make_float2(rcp_approx(den.x), rcp_approx(den.y)));
+    g = mul2(g, both(a0));
+    const float2 x = fma2(g, both(-1.44269504f), both(-8.0f));
+    const float2 r = make_float2(rcp_approx(0x1p-8f + ex2_approx(x.x)), rcp_approx(0x1p-8f + ex2_approx(x.y)));
+    return mul2(mul2(g, mul2(r, both(0x1p-8f))), mul2(u, both(a1)));
 }
 
 // 32 consecutive outputs of one row; n = how many exist.  vec: 32 or 16 byte stores (32 writes whole sectors: a lane's neighbours in a
@@ -452,8 +453,9 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
         const TensorScale hs(GATEUP && p.h_scale ? __ldg(p.h_scale) : 1.0f);
         for (int it = 0; ok && get_work(it, w); ++it) {
             const int buf = it % AB;
-            const float alpha = a_scale * (p.w_scale[0] ? __ldg(p.w_scale[0] + w.expert) : 1.0f);
-            const float alpha1 = GATEUP ? a_scale * (p.w_scale[1] ? __ldg(p.w_scale[1] + w.expert) : 1.0f) : 0.0f;
+            const ProductScale scale(a_scale, p.w_scale[0] ? __ldg(p.w_scale[0] + w.expert) : 1.0f);
+            const ProductScale scale1(a_scale, GATEUP && p.w_scale[1] ? __ldg(p.w_scale[1] + w.expert) : 1.0f);
+            const float alpha = scale.second;
             ok = mbar_wait(&acc_full[buf], (it / AB) & 1, abort_flag);
             ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok && !SPLIT) break;                                         // (split: the epilogue's warps meet below, whatever became of the wait)
@@ -472,6 +474,10 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
             if (lane == 0) mbar_arrive(&acc_empty[buf]);                      // the accumulators may be overwritten
             if (!SPLIT && !warp_has_rows) continue;
             const int n0 = w.n_tile * BN + part * CW;
+            if constexpr (!SPLIT) {
+#pragma unroll
+                for (int c = 0; c < NB * C32; ++c) (GATEUP && c ? scale1 : scale).apply_first(v[c]);
+            }
             if constexpr (GATEUP) {
                 const int hku = (p.N + kUnitK - 1) / kUnitK;                  // k units of the output operand
                 uint8_t* row_units = reinterpret_cast<uint8_t*>(p.y) + (int64_t)w.m_unit * hku * G::kUnit;
@@ -484,12 +490,11 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                     else *reinterpret_cast<uint16_t*>(unit + scale_offset(r, c >> 1) + 2 * (c & 1)) = (uint16_t)sc;
                 };
                 const int left = p.N - n0;
-                const float c = alpha * -1.44269504f, ab = alpha * alpha1;
                 float h[32];
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) {
                     const float2 x = silu_mul2(make_float2(__uint_as_float(v[0][i]), __uint_as_float(v[0][i + 1])),
-                                               make_float2(__uint_as_float(v[1][i]), __uint_as_float(v[1][i + 1])), c, ab);
+                                               make_float2(__uint_as_float(v[1][i]), __uint_as_float(v[1][i + 1])), alpha, scale1.second);
                     h[i] = x.x, h[i + 1] = x.y;
                 }
                 if (left < 32) {                                              // features past N are zeros of the operand's padding
@@ -540,6 +545,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                             sum[2] += v4[q].z;
                             sum[3] += v4[q].w;
                         }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) sum[k] *= scale.first;
                     const int c = e % BN, left = p.N - w.n_tile * BN - c;
                     T* o = y + (e / BN) * p.ldy + c;
                     if (sizeof(T) == 2 && p.vec >= 16 && left >= 4) {
@@ -758,7 +765,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
         bool ok = true;
         int it = 0;
         pdl_wait();
-        const float alpha = (p.a_scale ? __ldg(p.a_scale) : 1.0f) * (p.w_scale[0] ? __ldg(p.w_scale[0]) : 1.0f);
+        const ProductScale scale(p.a_scale ? __ldg(p.a_scale) : 1.0f, p.w_scale[0] ? __ldg(p.w_scale[0]) : 1.0f);
+        const float alpha = scale.second;
         for (int t = first; ok && t < total; t += pairs, ++it) {
             ok = mbar_wait(acc_full, it & 1, abort_flag);
             ok = __all_sync(0xFFFFFFFFu, ok);
@@ -771,6 +779,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
             tc_fence_before_sync();
             __syncwarp();
             if (lane == 0) mbar_arrive_remote(acc_empty, 0);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) scale.apply_first(v[c]);
             int mt, nt;
             pair_tile(t, m_tiles, n_tiles, mt, nt);
             const int row = 256 * mt + 128 * (int)rank + quarter * 32 + lane;
