@@ -33,6 +33,10 @@
  *     keeps counters in its workspace that every complete call leaves at zero:
  *     zero-fill a workspace once after allocating it, and again after a call on
  *     it was reported as failed (qmm_status_check) or was abandoned midway.
+ *   - A workspace that starts with a status word has data from byte 256 on.  One such buffer may
+ *     serve calls of several operators and shapes one after the other in one stream (the largest of
+ *     their sizes), but not qmm_moe among them, which keeps counters in that data area: its
+ *     workspace belongs to it alone.
  *   - Packed weights are read before the product kernels wait for the work
  *     that precedes them in the stream (their loads overlap the tail of the
  *     previous kernel).  A packed buffer must therefore be complete when a
@@ -436,8 +440,8 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
 /* Y[m, n] = a_scale * w_scale * sum_k a[m, k] w[n, k] with both operands packed, M >= 0, N >= 1, K >= 1.
  *   a, w  packed [M, K] and [N, K];  Y [M, ldy] of type `dtype`, ldy >= N
  *   ws    device, 256-byte aligned, >= qmm_mx_gemm_workspace_bytes(); starts with a status word (qmm_status_check
- *         reports a bounded wait that gave up) and counters that every complete call leaves at zero: zero-fill its first
- *         1024 bytes once, and again after a call on it was reported as failed.                      */
+ *         reports a bounded wait that gave up) and counters beside it that every complete call leaves at zero: zero-fill
+ *         its first 1024 bytes once, and again after a call on it was reported as failed.            */
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
 qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K,
                        const float* a_scale, const float* w_scale, qmm_dtype dtype, void* Y, int64_t ldy,

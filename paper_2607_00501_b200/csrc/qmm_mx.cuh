@@ -22,9 +22,11 @@ constexpr int kUnitRows = 128;
 constexpr int kUnitK = 256;
 constexpr int kCodeBytes = kUnitRows * kUnitK / 2;
 
-// Workspace of a product: status word, counters of tiles whose K is shared between blocks (two blocks per tile at least, so at most 74), then
-// partial sums.  The header is zero between calls.
-constexpr int kMxCounters = 256, kMxHeader = 1024;
+// Workspace of a product: status word; counters of tiles whose K is shared between blocks (two blocks per tile at least, so at most 74), 16 bits each; from kMxHeader
+// partial sums.  The header is zero between calls.  The counters lie in the 256 bytes that every workspace with a status word keeps for it: the data of another
+// operator that has used the same workspace begins behind them.
+constexpr int kMxCounters = 64, kMxHeader = 1024;
+static_assert(kMxCounters + 2 * (kNumSMs / 2) <= 256, "the counters share the status word's 256 bytes");
 
 __host__ __device__ constexpr int scale_bytes(int fmt) { return kUnitRows * kUnitK / fmt; }      // fmt = block length
 __host__ __device__ constexpr int unit_bytes(int fmt) { return kCodeBytes + scale_bytes(fmt); }

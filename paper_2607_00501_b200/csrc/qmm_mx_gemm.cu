@@ -59,7 +59,7 @@ struct MxGemmParams {
     int* status;
     int splits;                      // dense, few: blocks that share a tile's K (1: none); then every block has one piece of work, and
     float* partial;                  // partial sums go here, [tile][split][rows, a multiple of 32][128 columns],
-    int* counters;                   // per tile, zero between calls: the block that comes last adds the partial sums
+    int* counters;                   // 16 bits per tile, zero between calls: the block that comes last adds the partial sums
 };
 
 constexpr int kMxMaxE = 1024;
@@ -525,8 +525,10 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                 const int e0 = (int)threadIdx.x - EPI_WARP0 * 32;
                 if (epilogue_all<32 * G::kEpiWarps>(ok) && e0 == 0) {
                     __threadfence();
-                    last = atomicAdd(p.counters + tile, 1) == p.splits - 1;
-                    if (last) p.counters[tile] = 0;
+                    int* word = p.counters + (tile >> 1);                     // (at most eight blocks a tile: no carry into the other half)
+                    const int shift = 16 * (tile & 1);
+                    last = ((unsigned)atomicAdd(word, 1 << shift) >> shift & 0xFFFFu) == (unsigned)(p.splits - 1);
+                    if (last) atomicSub(word, p.splits << shift);
                 }
                 if (!epilogue_any<32 * G::kEpiWarps>(last)) break;
                 __threadfence();

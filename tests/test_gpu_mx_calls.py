@@ -46,3 +46,33 @@ def test_experts_rows_in_32_bits(qmm):
     assert torch.isfinite(kept).all() and not torch.isfinite(plain).all()
     with pytest.raises(AssertionError):
         qmm.mx_moe(32, X, idx, w, gate, up, down, I, E, rows_dtype=torch.bfloat16)
+
+
+def test_one_workspace_for_layers_and_products(qmm):
+    """A product that shares a tile's K keeps counters in its workspace's header; another operator's data there must not count."""
+    args = layer(qmm)
+    out = torch.empty_like(args[0])
+    a = qmm.mx_moe_args(32, *args, out)
+    ws = torch.zeros(max(qmm.mx_moe_workspace_bytes(a), 1 << 24), dtype=torch.uint8, device="cuda")
+    want_layer = qmm.mx_moe(32, *args)
+    canon = torch.zeros(qmm.canonical_bytes(qmm.Q4, 512, 4096), dtype=torch.uint8, device="cuda")
+    q4, Xg = qmm.pack(qmm.Q4, canon, 512, 4096), torch.randn(100, 4096, device="cuda").half()
+    for M, N, K in ((1, 2048, 8192), (16, 512, 8192), (40, 300, 5000)):
+        X, w = torch.randn(M, K, device="cuda").half(), qmm.mx_quantize(32, torch.randn(N, K, device="cuda"))
+        want = qmm.mx_linear(32, X, w, N)
+        xq = qmm.mx_quantize(32, X)
+        for other in (lambda: qmm.mx_moe_run(a, ws), lambda: qmm.gemm(qmm.Q4, q4, 512, 4096, Xg, ws=ws)):
+            for _ in range(2):
+                other()
+                Y = torch.full_like(want, 7.0)
+                qmm.mx_linear(32, X, w, N, Y=Y, ws=ws)
+                assert torch.equal(Y, want)
+                other()
+                Y = torch.full_like(want, 7.0)
+                qmm.mx_gemm(32, xq, M, w, N, K, Y=Y, ws=ws)
+                assert torch.equal(Y, want)
+                out.fill_(7.0)
+                qmm.mx_moe_run(a, ws)
+                assert torch.equal(out, want_layer)
+        qmm.status_check(ws)
+        assert not ws[:256].any(), "status word and counters are zero between calls"
