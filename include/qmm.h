@@ -441,7 +441,8 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
  *   a, w  packed [M, K] and [N, K];  Y [M, ldy] of type `dtype`, ldy >= N
  *   ws    device, 256-byte aligned, >= qmm_mx_gemm_workspace_bytes(); starts with a status word (qmm_status_check
  *         reports a bounded wait that gave up) and counters beside it that every complete call leaves at zero: zero-fill
- *         its first 1024 bytes once, and again after a call on it was reported as failed.            */
+ *         its first 1024 bytes once, and again after a call on it was reported as failed.  The size asked for M rows
+ *         serves every smaller M of the same N and K.                                                */
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
 qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K,
                        const float* a_scale, const float* w_scale, qmm_dtype dtype, void* Y, int64_t ldy,
@@ -449,7 +450,8 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
 
 /* The same product of activations as they come: X [M, ldx] of type `dtype` is quantised (as by
  * qmm_mx_quantize with tensor scale x_scale) on the way in; Y [M, ldy] of the same type.
- *   ws  device, 256-byte aligned, >= qmm_mx_linear_workspace_bytes(); its first 1024 bytes zeroed once, as above. */
+ *   ws  device, 256-byte aligned, >= qmm_mx_linear_workspace_bytes(); its first 1024 bytes zeroed once, and
+ *       its size enough for fewer rows, as above.                                                    */
 size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K);
 qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int64_t ldx, int64_t M,
                          const void* w, int64_t N, int64_t K, const float* x_scale, const float* w_scale,

@@ -17,6 +17,7 @@ qmm_status launch_mx_gemm(int fmt, const void* a, int64_t M, const void* w, int6
                           int64_t ldy, int* status, cudaStream_t st);
 bool mx_few_fits(int fmt, int64_t M, int64_t N, int64_t K);
 size_t mx_gemm_partial_bytes(int64_t M, int64_t N, int64_t K);
+size_t mx_gemm_partial_bytes_up_to(int64_t M, int64_t N, int64_t K);
 qmm_status launch_mx_few(int fmt, int dtype, const void* x, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
                          const float* w_scale, void* y, int64_t ldy, int* status, cudaStream_t st);
 int64_t mx_max_row_units(int64_t pairs, int E);
@@ -191,7 +192,7 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
     if (check_mx("qmm_mx_gemm_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_gemm_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
-    return kMxHeader + mx_gemm_partial_bytes(M, N, K);
+    return kMxHeader + mx_gemm_partial_bytes_up_to(M, N, K);
 }
 
 qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* w, int64_t N, int64_t K, const float* a_scale, const float* w_scale, qmm_dtype dtype,
@@ -207,7 +208,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
     QMM_TRY(check_packed(who, "a", a));
     QMM_TRY(check_packed(who, "w", w));
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
-    QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_gemm_workspace_bytes(fmt, M, N, K), 256));
+    QMM_TRY(check_ws(who, ws, ws_bytes, kMxHeader + mx_gemm_partial_bytes(M, N, K), 256));
     QMM_TRY(check_device(who));
     return launch_mx_gemm(fmt, a, M, w, N, K, a_scale, w_scale, dtype, Y, ldy, (int*)ws, (cudaStream_t)stream);
 }
@@ -215,7 +216,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
 size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
     if (check_mx("qmm_mx_linear_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_linear_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
-    return kMxHeader + mx_gemm_partial_bytes(M, N, K) + mx_bytes(fmt, (M + 127) / 128, K);
+    return kMxHeader + mx_gemm_partial_bytes_up_to(M, N, K) + mx_bytes(fmt, (M + 127) / 128, K);
 }
 
 qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int64_t ldx, int64_t M, const void* w, int64_t N, int64_t K, const float* x_scale,
@@ -231,10 +232,12 @@ qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int6
     QMM_TRY(check_rows(who, "X", dtype, X, ldx, K));
     QMM_TRY(check_packed(who, "w", w));
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
-    QMM_TRY(check_ws(who, ws, ws_bytes, qmm_mx_linear_workspace_bytes(fmt, M, N, K), 256));
+    const size_t before_a = kMxHeader + mx_gemm_partial_bytes(M, N, K);        // status word, counters, partial sums; then the quantised rows
+    const bool few = mx_few_fits(fmt, M, N, K);
+    QMM_TRY(check_ws(who, ws, ws_bytes, before_a + (few ? 0 : mx_bytes(fmt, (M + 127) / 128, K)), 256));
     QMM_TRY(check_device(who));
-    if (mx_few_fits(fmt, M, N, K)) return launch_mx_few(fmt, dtype, X, ldx, M, w, N, K, x_scale, w_scale, Y, ldy, (int*)ws, (cudaStream_t)stream);
-    void* a = (char*)ws + kMxHeader + mx_gemm_partial_bytes(M, N, K);
+    if (few) return launch_mx_few(fmt, dtype, X, ldx, M, w, N, K, x_scale, w_scale, Y, ldy, (int*)ws, (cudaStream_t)stream);
+    void* a = (char*)ws + before_a;
     QMM_TRY(launch_mx_quantize(fmt, dtype, X, ldx, M, K, x_scale, a, true, (cudaStream_t)stream));
     return launch_mx_gemm(fmt, a, M, w, N, K, x_scale, w_scale, dtype, Y, ldy, (int*)ws, (cudaStream_t)stream);
 }

@@ -878,6 +878,17 @@ size_t mx_gemm_partial_bytes(int64_t M, int64_t N, int64_t K)
     return splits > 1 ? (size_t)((N + 127) / 128 * splits) * ((M + 31) / 32 * 32) * 128 * sizeof(float) : 0;
 }
 
+// The most of it that any product of up to M rows takes (more rows may share less): what a size query answers, so that a workspace serves smaller batches too.
+size_t mx_gemm_partial_bytes_up_to(int64_t M, int64_t N, int64_t K)
+{
+    size_t most = 0;
+    for (int64_t m = 1; m <= M && m <= 128; ++m) {
+        const size_t bytes = mx_gemm_partial_bytes(m, N, K);
+        if (bytes > most) most = bytes;
+    }
+    return most;
+}
+
 template <int FMT, typename T, int FORM> static qmm_status launch_tiles(MxGemmParams p, int64_t row_tiles, cudaStream_t st)
 {
     using G = MxGeom<FMT, 128, false, FORM>;

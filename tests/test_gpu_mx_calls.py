@@ -76,3 +76,18 @@ def test_one_workspace_for_layers_and_products(qmm):
                 assert torch.equal(out, want_layer)
         qmm.status_check(ws)
         assert not ws[:256].any(), "status word and counters are zero between calls"
+
+
+@pytest.mark.parametrize("fmt", FMTS)
+def test_workspace_of_the_largest_batch_serves_smaller_ones(qmm, fmt):
+    N, K = 2048, 8192
+    w = qmm.mx_quantize(fmt, torch.randn(N, K, device="cuda") * 0.05)
+    ws = torch.zeros(qmm.mx_linear_workspace_bytes(fmt, 256, N, K), dtype=torch.uint8, device="cuda")
+    wg = torch.zeros(qmm.mx_gemm_workspace_bytes(fmt, 256, N, K), dtype=torch.uint8, device="cuda")
+    for M in (256, 1, 33, 16, 64, 128, 17, 200):
+        X = torch.randn(M, K, device="cuda").half()
+        want = qmm.mx_linear(fmt, X, w, N)
+        assert torch.equal(qmm.mx_linear(fmt, X, w, N, ws=ws), want)
+        assert torch.equal(qmm.mx_gemm(fmt, qmm.mx_quantize(fmt, X), M, w, N, K, ws=wg), want)
+    qmm.status_check(ws)
+    qmm.status_check(wg)

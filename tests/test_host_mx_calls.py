@@ -28,3 +28,18 @@ def test_type_of_the_experts_rows(L, a):
     assert L.qmm_mx_moe(ctypes.byref(args), a, need, None) == 4
     args.rows_f32 = 2
     assert L.qmm_mx_moe_workspace_bytes(ctypes.byref(args)) == 0 and "rows_f32" in qmm.last_error()
+
+
+@pytest.mark.parametrize("query", ["qmm_mx_linear_workspace_bytes", "qmm_mx_gemm_workspace_bytes"])
+def test_workspace_sizes_do_not_fall_with_the_batch(L, query):
+    """A workspace sized for the largest batch serves every smaller one."""
+    for fmt in (32, 16):
+        for N, K in ((2048, 8192), (512, 16384), (8192, 8192), (130, 5000), (128256, 2048), (2048, 2048)):
+            sizes = [getattr(L, query)(fmt, M, N, K) for M in [*range(0, 300), 512, 1000, 4096]]
+            assert all(a <= b for a, b in zip(sizes, sizes[1:])), (fmt, N, K)
+
+
+def test_a_call_asks_for_no_more_workspace_than_it_uses(L, a):
+    """64 rows of 2048 x 8192 share nothing, one row does: the header is enough for the first.  (Without a GPU the call goes on to the device check.)"""
+    assert L.qmm_mx_gemm(32, a, 1, a, 2048, 8192, None, None, 0, a, 2048, a, 1024, None) == 4
+    assert L.qmm_mx_gemm(32, a, 128, a, 2048, 8192, None, None, 0, a, 2048, a, 1023, None) == 4
