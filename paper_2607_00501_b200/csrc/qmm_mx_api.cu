@@ -92,6 +92,15 @@ static qmm_status check_pairs(const char* who, int32_t T, int32_t topk, int32_t 
     return QMM_OK;
 }
 
+// Operands of a dense product: M rows against N >= 1 weight rows.
+static qmm_status check_product(const char* who, int fmt, int64_t M, int64_t N, int64_t K)
+{
+    const qmm_status s = check_mx(who, fmt, M, K);
+    if (s != QMM_OK) return s;
+    if (N == 0) return fail(QMM_ERR_INVALID_ARG, "%s: N must be positive", who);
+    return check_mx(who, fmt, N, K);
+}
+
 static size_t mx_bytes(int fmt, int64_t row_units, int64_t K) { return (size_t)row_units * (size_t)k_units(K) * (size_t)unit_bytes(fmt); }
 
 #define QMM_TRY(call)                    \
@@ -191,7 +200,7 @@ qmm_status qmm_mx_dequantize(qmm_mx_format fmt, const void* packed, int64_t rows
 
 size_t qmm_mx_gemm_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
-    if (check_mx("qmm_mx_gemm_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_gemm_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
+    if (check_product("qmm_mx_gemm_workspace_bytes", fmt, M, N, K) != QMM_OK) return 0;
     return kMxHeader + mx_gemm_partial_bytes_up_to(M, N, K);
 }
 
@@ -199,9 +208,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
                        void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream)
 {
     const char* who = "qmm_mx_gemm";
-    QMM_TRY(check_mx(who, fmt, M, K));
-    QMM_TRY(check_mx(who, fmt, N, K));
-    if (N == 0) return fail(QMM_ERR_INVALID_ARG, "%s: N must be positive", who);
+    QMM_TRY(check_product(who, fmt, M, N, K));
     QMM_TRY(check_scale(who, fmt, a_scale));
     QMM_TRY(check_scale(who, fmt, w_scale));
     if (M == 0) return QMM_OK;
@@ -215,7 +222,7 @@ qmm_status qmm_mx_gemm(qmm_mx_format fmt, const void* a, int64_t M, const void* 
 
 size_t qmm_mx_linear_workspace_bytes(qmm_mx_format fmt, int64_t M, int64_t N, int64_t K)
 {
-    if (check_mx("qmm_mx_linear_workspace_bytes", fmt, M, K) != QMM_OK || check_mx("qmm_mx_linear_workspace_bytes", fmt, N, K) != QMM_OK) return 0;
+    if (check_product("qmm_mx_linear_workspace_bytes", fmt, M, N, K) != QMM_OK) return 0;
     return kMxHeader + mx_gemm_partial_bytes_up_to(M, N, K) + mx_bytes(fmt, (M + 127) / 128, K);
 }
 
@@ -223,9 +230,7 @@ qmm_status qmm_mx_linear(qmm_mx_format fmt, qmm_dtype dtype, const void* X, int6
                          const float* w_scale, void* Y, int64_t ldy, void* ws, size_t ws_bytes, void* stream)
 {
     const char* who = "qmm_mx_linear";
-    QMM_TRY(check_mx(who, fmt, M, K));
-    QMM_TRY(check_mx(who, fmt, N, K));
-    if (N == 0) return fail(QMM_ERR_INVALID_ARG, "%s: N must be positive", who);
+    QMM_TRY(check_product(who, fmt, M, N, K));
     QMM_TRY(check_scale(who, fmt, x_scale));
     QMM_TRY(check_scale(who, fmt, w_scale));
     if (M == 0) return QMM_OK;

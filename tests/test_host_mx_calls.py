@@ -43,3 +43,14 @@ def test_a_call_asks_for_no_more_workspace_than_it_uses(L, a):
     """64 rows of 2048 x 8192 share nothing, one row does: the header is enough for the first.  (Without a GPU the call goes on to the device check.)"""
     assert L.qmm_mx_gemm(32, a, 1, a, 2048, 8192, None, None, 0, a, 2048, a, 1024, None) == 4
     assert L.qmm_mx_gemm(32, a, 128, a, 2048, 8192, None, None, 0, a, 2048, a, 1023, None) == 4
+
+
+def test_workspace_sizes_without_weight_rows(L):
+    """N = 0 is refused like any other argument out of range (in a process of its own: it once ended in a division by zero)."""
+    import subprocess
+    import sys
+    code = ("from paper_2607_00501_b200 import qmm\n"
+            "for q in (qmm.mx_gemm_workspace_bytes, qmm.mx_linear_workspace_bytes):\n"
+            "    for M in (0, 1, 200):\n"
+            "        assert q(32, M, 0, 8192) == 0 and 'N must be positive' in qmm.last_error()\n")
+    assert subprocess.run([sys.executable, "-c", code]).returncode == 0
