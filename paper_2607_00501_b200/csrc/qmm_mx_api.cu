@@ -332,6 +332,8 @@ qmm_status qmm_mx_quantize_experts(qmm_mx_format fmt, qmm_dtype dtype, const voi
     QMM_TRY(check_rows(who, "x", dtype, x, ldx, K));
     QMM_TRY(check_packed(who, "packed", packed));
     if (!idx || !place || !offsets || !units) return fail(QMM_ERR_INVALID_ARG, "%s: idx, place, offsets or units is null", who);
+    if (!aligned(idx, 4) || !aligned(place, 4) || !aligned(offsets, 4) || !aligned(units, 4))
+        return fail(QMM_ERR_ALIGNMENT, "%s: index arrays must be 4-byte aligned", who);
     QMM_TRY(check_device(who));
     return launch_mx_quantize_experts(fmt, dtype, x, ldx, T, topk, E, K, idx, place, offsets, units, tensor_scale, packed, false, (cudaStream_t)stream);
 }
@@ -351,6 +353,8 @@ qmm_status qmm_mx_experts_gate_up(qmm_mx_format fmt, const void* a, int32_t T, i
     QMM_TRY(check_packed(who, "w_up", w_up));
     QMM_TRY(check_packed(who, "h", h));
     if (!offsets || !units) return fail(QMM_ERR_INVALID_ARG, "%s: offsets or units is null", who);
+    if (!aligned(offsets, 4) || !aligned(units, 4) || !aligned(status, 4))
+        return fail(QMM_ERR_ALIGNMENT, "%s: offsets, units and status must be 4-byte aligned", who);
     QMM_TRY(check_device(who));
     return launch_mx_experts_gate_up(fmt, a, (int64_t)T * topk, E, offsets, units, w_gate, w_up, N, K, a_scale, gate_scale, up_scale, h_scale, h, status,
                                      (cudaStream_t)stream);
@@ -371,6 +375,8 @@ qmm_status qmm_mx_experts_gemm(qmm_mx_format fmt, const void* a, int32_t T, int3
     QMM_TRY(check_packed(who, "w", w));
     QMM_TRY(check_rows(who, "Y", dtype, Y, ldy, N));
     if (!offsets || !units) return fail(QMM_ERR_INVALID_ARG, "%s: offsets or units is null", who);
+    if (!aligned(offsets, 4) || !aligned(units, 4) || !aligned(status, 4))
+        return fail(QMM_ERR_ALIGNMENT, "%s: offsets, units and status must be 4-byte aligned", who);
     QMM_TRY(check_device(who));
     return launch_mx_experts_gemm(fmt, a, (int64_t)T * topk, E, offsets, units, w, N, K, a_scale, w_scale, dtype, Y, ldy, false, status, (cudaStream_t)stream);
 }

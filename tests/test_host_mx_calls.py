@@ -54,3 +54,14 @@ def test_workspace_sizes_without_weight_rows(L):
             "    for M in (0, 1, 200):\n"
             "        assert q(32, M, 0, 8192) == 0 and 'N must be positive' in qmm.last_error()\n")
     assert subprocess.run([sys.executable, "-c", code]).returncode == 0
+
+
+def test_index_arrays_of_the_experts_calls_are_aligned(L, a):
+    """Misaligned index arrays and status words are refused on the host (a kernel would fault on them)."""
+    good = [a, a, a, a]
+    for i in range(4):
+        bad = [p + 2 * (i == j) for j, p in enumerate(good)]
+        assert L.qmm_mx_quantize_experts(32, 0, a, 64, 4, 2, 8, 64, *bad, None, a, None) == 3, i
+    for off, units, status in ((a + 2, a, None), (a, a + 1, None), (a, a, a + 2)):
+        assert L.qmm_mx_experts_gate_up(32, a, 4, 2, 8, off, units, a, a, 64, 64, None, None, None, None, a, status, None) == 3
+        assert L.qmm_mx_experts_gemm(32, a, 4, 2, 8, off, units, a, 64, 64, None, None, 0, a, 64, status, None) == 3
