@@ -499,7 +499,8 @@ qmm_status qmm_expert_combine_grad(qmm_dtype dtype, const void* dy, int64_t lddy
  * scales are arrays of E floats.                                                                    */
 size_t qmm_mx_experts_bytes(qmm_mx_format fmt, int32_t T, int32_t topk, int32_t E, int64_t K);
 
-/* Token t of x [T, ldx] is quantised once and stored at the row of each of its pairs.               */
+/* Token t of x [T, ldx] is quantised once and stored at the row of each of its pairs.  idx: what was sorted (a pair whose
+ * expert is another one by now is not stored).                                                      */
 qmm_status qmm_mx_quantize_experts(qmm_mx_format fmt, qmm_dtype dtype, const void* x, int64_t ldx, int32_t T, int32_t topk,
                                    int32_t E, int64_t K, const int32_t* idx, const int32_t* place, const int32_t* offsets,
                                    const int32_t* units, const float* tensor_scale, void* packed, void* stream);

@@ -153,7 +153,10 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
             const int r = m.place[p];
             if (r < 0) continue;
             const int e = m.idx[p];
-            store((int64_t)m.units[e] * 128 + (r - m.offsets[e]));
+            if ((unsigned)e >= (unsigned)m.E) continue;    // idx is the caller's: no row where it is not what was sorted
+            const int first = m.offsets[e];
+            if (r < first || r >= m.offsets[e + 1]) continue;
+            store((int64_t)m.units[e] * 128 + (r - first));
         }
     }
 }

@@ -91,3 +91,26 @@ def test_workspace_of_the_largest_batch_serves_smaller_ones(qmm, fmt):
         assert torch.equal(qmm.mx_gemm(fmt, qmm.mx_quantize(fmt, X), M, w, N, K, ws=wg), want)
     qmm.status_check(ws)
     qmm.status_check(wg)
+
+
+def test_experts_rows_of_another_routing_are_not_stored(qmm):
+    """mx_quantize_experts on an idx that is not the sorted one stores the pairs that agree and writes nowhere else."""
+    T, topk, E, K = 70, 3, 5, 300
+    rng = np.random.default_rng(3)
+    idx = rng.integers(0, E, (T, topk)).astype(np.int32)
+    plan = qmm.expert_sort(torch.from_numpy(idx).cuda(), E)
+    x = torch.randn(T, K, device="cuda").half()
+    other = np.where(rng.random((T, topk)) < 0.5, idx, rng.choice([-1, E, 2**30, -2**31, 0, E - 1], (T, topk))).astype(np.int32)
+    need = qmm.mx_experts_bytes(32, T, topk, E, K)
+    want = qmm.mx_quantize_experts(32, x, torch.from_numpy(idx).cuda(), plan).cpu().numpy()
+    buf = torch.full((need + 8192,), 0xAB, dtype=torch.uint8, device="cuda")
+    qmm.mx_quantize_experts(32, x, torch.from_numpy(other).cuda(), plan, out=buf[4096: 4096 + need])
+    got = buf.cpu().numpy()
+    assert (got[:4096] == 0xAB).all() and (got[4096 + need:] == 0xAB).all()
+    order, place, offsets, units = mxref.sort(idx, E)
+    for e in range(E):
+        n = int(offsets[e + 1] - offsets[e])
+        (c, s), (cw, sw) = (mxref.unpack(b, 32, n, K, int(units[e])) for b in (got[4096: 4096 + need], want))
+        stored = other.reshape(-1)[order[offsets[e]: offsets[e + 1]]] == e
+        assert np.array_equal(c[stored], cw[stored]) and np.array_equal(s[stored], sw[stored])
+        assert (s[~stored] == 0xAB).all() and (c[~stored][:, 0::2] == 0xB).all()
