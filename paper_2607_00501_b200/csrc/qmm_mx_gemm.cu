@@ -384,9 +384,11 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
                 }
             }
         }
+        // the MMA's last arrivals (one per stage of the last round) have come before the block's shared memory is released
+        for (int q = max(0, g - S); ok && warp == W_WARP && q < g; ++q) ok = __all_sync(0xFFFFFFFFu, mbar_wait(&empty[q % S], (q / S) & 1, abort_flag));
         if (!ok) {
             *abort_flag = 1;
-            // let copies in flight land before the block's shared memory is released
+            // let copies in flight land, too
             for (int q = max(0, g - S); q < g; ++q) {
                 const long long t0 = clock64();
                 while (!mbar_try_wait(&full[q % S], (q / S) & 1) && clock64() - t0 < (1LL << 22)) {}
@@ -715,6 +717,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MxPairGeom<FMT>::kTh
                     if (a < a_units) tma_load_2d_pair(smem0 + s * G::kStage, &maps.a, 0, (a * p.KU + ku) * ROWS, full0 + 8 * s);
                 }
             }
+            // the MMA's last arrivals, which come from the first block to both, before the block's shared memory is released
+            for (int q = max(0, g - S); ok && q < g; ++q) ok = mbar_wait(&empty[q % S], (q / S) & 1, abort_flag);
             if (!ok) {
                 *abort_flag = 1;
                 // let copies in flight land (both blocks' count on the first block's barriers; the second waits for it at the end)
