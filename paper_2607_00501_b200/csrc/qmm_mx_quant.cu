@@ -133,11 +133,11 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
     // scale bytes of the group of four blocks, assembled in its first lane
     constexpr int LANES = FMT == QMM_MXFP4 ? 4 : 2;
     const uint32_t sub = (uint32_t)c & (LANES - 1);
-    const uint32_t active = __activemask();
+    const uint32_t mine = ((1u << LANES) - 1u) << ((threadIdx.x & 31) & ~(LANES - 1));      // these lanes: whole and live, whatever branches they came by
     uint32_t word = sb << (sub * (32 / LANES));
     if (left <= 0) word = 0;
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) word |= __shfl_xor_sync(active, word, o);
+    for (int o = 1; o < LANES; o <<= 1) word |= __shfl_xor_sync(mine, word, o);
     const uint32_t group = (uint32_t)(c & 7) / LANES;
     auto store = [&](int64_t slot) {
         uint8_t* unit = packed + ((slot >> 7) * KU + (c >> 3)) * unit_bytes(FMT);

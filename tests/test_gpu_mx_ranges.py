@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests import mxref
-from tests.test_gpu_mx import FMTS, f64, scale_of
+from tests.test_gpu_mx import DTYPES, FMTS, check_quantized, f64, scale_of
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +149,21 @@ def test_experts_product_far_tensor_scales(qmm):
         Y = qmm.mx_experts_gemm(16, a, plan, qmm.mx_quantize(16, W, tensor_scale=scale_of(16, gw)), N, K, a_scale=scale_of(16, ga), w_scale=scale_of(16, gw), dtype=torch.float32)
         want = (6 * 448.0) ** 2 * K * float(np.float32(ga)) * float(np.float32(gw))
         assert (np.abs(f64(Y) - want) <= 2.0**-18 * want).all(), (ga, gw, float(Y[0, 0]), want)
+
+
+# ---- quantisation
+
+@pytest.mark.parametrize("dt", ["f16", "bf16", "f32"])
+@pytest.mark.parametrize("fmt", FMTS)
+def test_scales_of_lanes_that_took_different_branches(qmm, fmt, dt):
+    """Four neighbouring blocks of a row share a word of scales: here a row's end, blocks beyond 2^40 (true divisions), zeros and infinities meet in it."""
+    dtype = DTYPES[dt]
+    for rows, K in ((40, 40), (33, 296), (64, 264), (9, 1000), (5, 2024)):
+        x = torch.randn(rows, K, generator=torch.Generator().manual_seed(rows))
+        b = torch.arange(K) // fmt
+        r = torch.arange(rows)[:, None]
+        x = x * torch.where((b + r) % 3 == 0, 2.0**41 if dt != "f16" else 2.0**10, 1.0)
+        x = torch.where((b + r) % 7 == 3, torch.zeros(()), x)
+        x = torch.where(((b + 2 * r) % 11 == 5) & (torch.arange(K) % fmt == 1), torch.full((), float("inf")), x).to(dtype)
+        for g in ((1.0,) if fmt == mxref.MXFP4 else (0.01, 2.0**-41)):
+            check_quantized(qmm.mx_quantize(fmt, x.cuda(), tensor_scale=scale_of(fmt, g)), f64(x), fmt, g)
