@@ -4,14 +4,15 @@
  * converting its arguments in Python and ctypes took 3 us beside a launch of 2.6.  These wrappers read the tensors' attributes
  * and call the C ABI directly (0.5 us).  They only check and convert: every step of every operator runs in libqmm's kernels.
  * Each returns the qmm_status; wrong tensors raise AssertionError, like the asserts of the other wrappers.
- * The stream is the current one of the first tensor's device.                                                        */
+ * A kernel runs on the current device, in its current stream: tensors of another device are refused.                     */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include "../../include/qmm.h"
 
-static PyObject *s_is_cuda, *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_numel, *s_is_contiguous, *s_get_device;
-static PyObject *raw_stream, *dt[3], *dt_u8, *dt_i32;                 /* torch._C._cuda_getCurrentRawStream; dtype objects */
+static PyObject *s_shape, *s_stride, *s_dtype, *s_data_ptr, *s_numel, *s_is_contiguous, *s_get_device;
+static PyObject *device_count, *current_device, *raw_stream;         /* torch._C._cuda_getDeviceCount, _cuda_getDevice, _cuda_getCurrentRawStream */
+static PyObject *dt[3], *dt_u8, *dt_i32;                              /* dtype objects */
 
 static int fail_assert(const char* what, const char* why)
 {
@@ -19,10 +20,9 @@ static int fail_assert(const char* what, const char* why)
     return -1;
 }
 
-/* attribute `name` of t is True / method `name` of t returns True */
-static int flag(PyObject* t, PyObject* name, int method)
+static int is_contiguous(PyObject* t)
 {
-    PyObject* v = method ? PyObject_CallMethodNoArgs(t, name) : PyObject_GetAttr(t, name);
+    PyObject* v = PyObject_CallMethodNoArgs(t, s_is_contiguous);
     if (!v) return 0;
     const int yes = v == Py_True;
     Py_DECREF(v);
@@ -55,6 +55,14 @@ static int pair(PyObject* tuple, int64_t* a, int64_t* b)              /* a tuple
     return ok ? 0 : -1;
 }
 
+/* All tensors (and the plan) of a call are on one device: *dev, -1 before the first. */
+static int on_device(int64_t d, const char* what, int64_t* dev)
+{
+    if (d < 0) return fail_assert(what, "a CUDA tensor is wanted");
+    if (*dev < 0) *dev = d;
+    return d == *dev ? 0 : fail_assert(what, "on another device than the tensors before it");
+}
+
 typedef struct {
     void* ptr;
     int64_t ld, rows, cols;
@@ -62,10 +70,10 @@ typedef struct {
 } rows_t;
 
 /* A 2-D CUDA tensor with contiguous rows of fp16, bf16 or fp32. */
-static int get_rows(PyObject* t, const char* what, rows_t* r)
+static int get_rows(PyObject* t, const char* what, rows_t* r, int64_t* dev)
 {
     int64_t inner;
-    if (!flag(t, s_is_cuda, 0)) return fail_assert(what, "a CUDA tensor is wanted");
+    if (on_device(number(t, s_get_device), what, dev)) return -1;    /* (-1: a CPU tensor) */
     if (pair(PyObject_GetAttr(t, s_shape), &r->rows, &r->cols) || pair(PyObject_CallMethodNoArgs(t, s_stride), &r->ld, &inner))
         return fail_assert(what, "a 2-D tensor is wanted");
     if (inner != 1 && r->cols > 1) return fail_assert(what, "rows must be contiguous");
@@ -80,11 +88,12 @@ static int get_rows(PyObject* t, const char* what, rows_t* r)
 }
 
 /* A contiguous CUDA tensor of type `type` with exactly (exact) or at least n elements; None gives a null pointer where `optional`. */
-static int get_flat(PyObject* t, const char* what, PyObject* type, int64_t n, int exact, int optional, void** ptr)
+static int get_flat(PyObject* t, const char* what, PyObject* type, int64_t n, int exact, int optional, void** ptr, int64_t* dev)
 {
     *ptr = NULL;
     if (t == Py_None) return optional ? 0 : fail_assert(what, "a tensor is wanted");
-    if (!flag(t, s_is_cuda, 0) || !is_dtype(t, type) || !flag(t, s_is_contiguous, 1)) return fail_assert(what, "a contiguous CUDA tensor of the right type is wanted");
+    if (on_device(number(t, s_get_device), what, dev)) return -1;
+    if (!is_dtype(t, type) || !is_contiguous(t)) return fail_assert(what, "a contiguous CUDA tensor of the right type is wanted");
     const int64_t have = number(t, s_numel);
     if (exact ? have != n : have < n) {
         if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "%s: %lld elements, %lld needed", what, (long long)have, (long long)n);
@@ -94,15 +103,32 @@ static int get_flat(PyObject* t, const char* what, PyObject* type, int64_t n, in
     return PyErr_Occurred() ? -1 : 0;
 }
 
-static int get_stream(PyObject* t, void** stream)
+/* Current stream of device `dev`, which has to be the current device (with one GPU there is no other: asking takes 0.2 us). */
+static int get_stream(int64_t dev, void** stream)
 {
-    PyObject* dev = PyObject_CallMethodNoArgs(t, s_get_device);
-    if (!dev) return -1;
-    PyObject* s = PyObject_CallOneArg(raw_stream, dev);
-    Py_DECREF(dev);
-    if (!s) return -1;
-    *stream = (void*)PyLong_AsUnsignedLongLongMask(s);
-    Py_DECREF(s);
+    static int gpus = 0;
+    PyObject* v;
+    if (gpus == 0) {
+        if (!(v = PyObject_CallNoArgs(device_count))) return -1;
+        gpus = (int)PyLong_AsLong(v);
+        Py_DECREF(v);
+    }
+    if (gpus != 1) {
+        if (!(v = PyObject_CallNoArgs(current_device))) return -1;
+        const long long now = PyLong_AsLongLong(v);
+        Py_DECREF(v);
+        if (now != dev) {
+            if (!PyErr_Occurred()) PyErr_Format(PyExc_AssertionError, "the tensors are on device %lld, the current device is %lld", (long long)dev, now);
+            return -1;
+        }
+    }
+    PyObject* d = PyLong_FromLongLong(dev);
+    if (!d) return -1;
+    v = PyObject_CallOneArg(raw_stream, d);
+    Py_DECREF(d);
+    if (!v) return -1;
+    *stream = (void*)PyLong_AsUnsignedLongLongMask(v);
+    Py_DECREF(v);
     return 0;
 }
 
@@ -132,87 +158,87 @@ static int64_t packed_need(int64_t fmt, int64_t rows, int64_t K) { return rows >
 /* (fmt, x, out, tensor_scale) */
 static PyObject* py_mx_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t fmt;
+    int64_t fmt, dev = -1;
     rows_t x;
     void *out, *scale, *stream;
-    TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[1], "x", &x));
-    TRY(get_flat(a[2], "out", dt_u8, packed_need(fmt, x.rows, x.cols), 0, 0, &out) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale) || get_stream(a[1], &stream));
+    TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[1], "x", &x, &dev));
+    TRY(get_flat(a[2], "out", dt_u8, packed_need(fmt, x.rows, x.cols), 0, 0, &out, &dev) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale, &dev) || get_stream(dev, &stream));
     return PyLong_FromLong(qmm_mx_quantize((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, x.cols, scale, out, stream));
 }
 
 /* (fmt, packed, out, tensor_scale) */
 static PyObject* py_mx_dequantize(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t fmt;
+    int64_t fmt, dev = -1;
     rows_t o;
     void *packed, *scale, *stream;
-    TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[2], "out", &o));
-    TRY(get_flat(a[1], "packed", dt_u8, packed_need(fmt, o.rows, o.cols), 0, 0, &packed) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale) || get_stream(a[2], &stream));
+    TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[2], "out", &o, &dev));
+    TRY(get_flat(a[1], "packed", dt_u8, packed_need(fmt, o.rows, o.cols), 0, 0, &packed, &dev) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale, &dev) || get_stream(dev, &stream));
     return PyLong_FromLong(qmm_mx_dequantize((qmm_mx_format)fmt, packed, o.rows, o.cols, scale, (qmm_dtype)o.dtype, o.ptr, o.ld, stream));
 }
 
 /* (fmt, X, w, N, Y, x_scale, w_scale, ws) */
 static PyObject* py_mx_linear(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t fmt, N;
+    int64_t fmt, N, dev = -1;
     rows_t x, y;
     void *w, *xs, *wsc, *ws, *stream;
-    TRY(arity(n, 8) || get_ints(a, 1, &fmt) || get_ints(a + 3, 1, &N) || get_rows(a[1], "X", &x) || get_rows(a[4], "Y", &y));
+    TRY(arity(n, 8) || get_ints(a, 1, &fmt) || get_ints(a + 3, 1, &N) || get_rows(a[1], "X", &x, &dev) || get_rows(a[4], "Y", &y, &dev));
     UNLESS(y.rows == x.rows && y.cols == N && y.dtype == x.dtype, "Y", "[M, N] of X's type is wanted");
-    TRY(get_flat(a[2], "w", dt_u8, packed_need(fmt, N, x.cols), 0, 0, &w) || get_flat(a[5], "x_scale", dt[2], 1, 1, 1, &xs) ||
-        get_flat(a[6], "w_scale", dt[2], 1, 1, 1, &wsc) || get_flat(a[7], "ws", dt_u8, 0, 0, 0, &ws) || get_stream(a[1], &stream));
+    TRY(get_flat(a[2], "w", dt_u8, packed_need(fmt, N, x.cols), 0, 0, &w, &dev) || get_flat(a[5], "x_scale", dt[2], 1, 1, 1, &xs, &dev) ||
+        get_flat(a[6], "w_scale", dt[2], 1, 1, 1, &wsc, &dev) || get_flat(a[7], "ws", dt_u8, 0, 0, 0, &ws, &dev) || get_stream(dev, &stream));
     const int64_t ws_bytes = number(a[7], s_numel);
     return PyLong_FromLong(qmm_mx_linear((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, w, N, x.cols, xs, wsc, y.ptr, y.ld, ws, (size_t)ws_bytes, stream));
 }
 
-/* (idx, E, order, place, offsets, units, ws, ws_bytes): the plan's arrays as addresses */
+/* (idx, E, order, place, offsets, units, ws, ws_bytes, device): the plan's arrays as addresses, and their device */
 static PyObject* py_expert_sort(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t v[7], T, topk;
+    int64_t v[8], T, topk, dev = -1;
     void *idx, *stream;
-    TRY(arity(n, 8) || get_ints(a + 1, 7, v));
-    TRY(get_flat(a[0], "idx", dt_i32, 0, 0, 0, &idx));
+    TRY(arity(n, 9) || get_ints(a + 1, 8, v) || on_device(v[7], "plan", &dev));
+    TRY(get_flat(a[0], "idx", dt_i32, 0, 0, 0, &idx, &dev));
     if (pair(PyObject_GetAttr(a[0], s_shape), &T, &topk)) return fail_assert("idx", "[T, topk] is wanted"), NULL;
-    TRY(get_stream(a[0], &stream));
+    TRY(get_stream(dev, &stream));
     return PyLong_FromLong(qmm_expert_sort(idx, (int32_t)T, (int32_t)topk, (int32_t)v[0], (int32_t*)v[1], (int32_t*)v[2], (int32_t*)v[3], (int32_t*)v[4], (void*)v[5],
                                            (size_t)v[6], stream));
 }
 
-/* (x, T, topk, order, place, weights, xs) */
+/* (x, T, topk, order, place, device, weights, xs) */
 static PyObject* py_expert_gather(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t v[4];
+    int64_t v[5], dev = -1;
     rows_t x, o;
     void *w, *stream;
-    TRY(arity(n, 7) || get_ints(a + 1, 4, v) || get_rows(a[0], "x", &x) || get_rows(a[6], "out", &o));
+    TRY(arity(n, 8) || get_ints(a + 1, 5, v) || on_device(v[4], "plan", &dev) || get_rows(a[0], "x", &x, &dev) || get_rows(a[7], "out", &o, &dev));
     UNLESS(x.rows == v[0] && o.rows == v[0] * v[1] && o.cols == x.cols && o.dtype == x.dtype, "out", "x [T, H] and out [T * topk, H] of one type are wanted");
-    TRY(get_flat(a[5], "weights", dt[2], v[0] * v[1], 1, 1, &w) || get_stream(a[0], &stream));
+    TRY(get_flat(a[6], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_stream(dev, &stream));
     return PyLong_FromLong(qmm_expert_gather((qmm_dtype)x.dtype, x.ptr, x.ld, (int32_t)v[0], (int32_t)v[1], x.cols, (const int32_t*)v[2], (const int32_t*)v[3], w, o.ptr,
                                              o.ld, stream));
 }
 
-/* (ys, T, topk, place, weights, y) */
+/* (ys, T, topk, place, device, weights, y) */
 static PyObject* py_expert_combine(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t v[3];
+    int64_t v[4], dev = -1;
     rows_t y, o;
     void *w, *stream;
-    TRY(arity(n, 6) || get_ints(a + 1, 3, v) || get_rows(a[0], "ys", &y) || get_rows(a[5], "out", &o));
+    TRY(arity(n, 7) || get_ints(a + 1, 4, v) || on_device(v[3], "plan", &dev) || get_rows(a[0], "ys", &y, &dev) || get_rows(a[6], "out", &o, &dev));
     UNLESS(y.rows == v[0] * v[1] && o.rows == v[0] && o.cols == y.cols && o.dtype == y.dtype, "out", "ys [T * topk, H] and out [T, H] of one type are wanted");
-    TRY(get_flat(a[4], "weights", dt[2], v[0] * v[1], 1, 1, &w) || get_stream(a[0], &stream));
+    TRY(get_flat(a[5], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_stream(dev, &stream));
     return PyLong_FromLong(qmm_expert_combine((qmm_dtype)y.dtype, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], y.cols, (const int32_t*)v[2], w, o.ptr, o.ld, stream));
 }
 
-/* (dy, ys, T, topk, order, place, weights, dys, dw) */
+/* (dy, ys, T, topk, order, place, device, weights, dys, dw) */
 static PyObject* py_expert_combine_grad(PyObject* self, PyObject* const* a, Py_ssize_t n)
 {
-    int64_t v[4];
+    int64_t v[5], dev = -1;
     rows_t d, y, o;
     void *w, *dw, *stream;
-    TRY(arity(n, 9) || get_ints(a + 2, 4, v) || get_rows(a[0], "dy", &d) || get_rows(a[1], "ys", &y) || get_rows(a[7], "dys", &o));
+    TRY(arity(n, 10) || get_ints(a + 2, 5, v) || on_device(v[4], "plan", &dev) || get_rows(a[0], "dy", &d, &dev) || get_rows(a[1], "ys", &y, &dev) || get_rows(a[8], "dys", &o, &dev));
     UNLESS(d.rows == v[0] && y.rows == v[0] * v[1] && o.rows == y.rows && y.cols == d.cols && o.cols == d.cols && y.dtype == d.dtype && o.dtype == d.dtype, "dys",
            "dy [T, H], ys and dys [T * topk, H] of one type are wanted");
-    TRY(get_flat(a[6], "weights", dt[2], v[0] * v[1], 1, 1, &w) || get_flat(a[8], "dw", dt[2], v[0] * v[1], 1, 0, &dw) || get_stream(a[0], &stream));
+    TRY(get_flat(a[7], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_flat(a[9], "dw", dt[2], v[0] * v[1], 1, 0, &dw, &dev) || get_stream(dev, &stream));
     return PyLong_FromLong(qmm_expert_combine_grad((qmm_dtype)d.dtype, d.ptr, d.ld, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], d.cols, (const int32_t*)v[2],
                                                    (const int32_t*)v[3], w, o.ptr, o.ld, dw, stream));
 }
@@ -227,7 +253,6 @@ PyMODINIT_FUNC PyInit__qmm_py(void)
     PyObject* torch = PyImport_ImportModule("torch");
     PyObject* c = PyImport_ImportModule("torch._C");
     if (!torch || !c) return NULL;
-    s_is_cuda = PyUnicode_InternFromString("is_cuda");
     s_shape = PyUnicode_InternFromString("shape");
     s_stride = PyUnicode_InternFromString("stride");
     s_dtype = PyUnicode_InternFromString("dtype");
@@ -235,6 +260,8 @@ PyMODINIT_FUNC PyInit__qmm_py(void)
     s_numel = PyUnicode_InternFromString("numel");
     s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
     s_get_device = PyUnicode_InternFromString("get_device");
+    device_count = PyObject_GetAttrString(c, "_cuda_getDeviceCount");
+    current_device = PyObject_GetAttrString(c, "_cuda_getDevice");
     raw_stream = PyObject_GetAttrString(c, "_cuda_getCurrentRawStream");
     dt[0] = PyObject_GetAttrString(torch, "float16");
     dt[1] = PyObject_GetAttrString(torch, "bfloat16");

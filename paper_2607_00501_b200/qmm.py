@@ -434,6 +434,21 @@ def _rows2d(t: torch.Tensor, what: str):
     return t.data_ptr(), ld if rows > 1 or ld > cols else cols, rows, cols
 
 
+_one_gpu = None
+
+
+def _on_current_device(*tensors) -> None:
+    """A kernel runs on the current device: CUDA tensors of another one are refused (None is skipped; with one GPU there is no other)."""
+    global _one_gpu
+    if _one_gpu is None:
+        _one_gpu = torch.cuda.device_count() == 1
+    if _one_gpu:
+        return
+    now = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == now, "tensor on device %d, the current device is %d" % (t.get_device(), now)
+
+
 def _mx_need(fmt: int, rows: int, K: int) -> int:
     """mx_bytes, for the two formats without a call into the library: the size that a packed argument has to have."""
     if fmt != MXFP4 and fmt != NVFP4:
@@ -480,6 +495,7 @@ def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: to
     need = mx_bytes(fmt, rows, K)
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=codes.device)
+    _on_current_device(codes, scales, out)
     _check(lib().qmm_mx_pack(fmt, codes.data_ptr(), scales.data_ptr(), rows, K, _operand(out, need, "out"), _stream()))
     return out
 
@@ -516,6 +532,7 @@ def mx_gemm(fmt: int, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int, 
     ptr, ld, r, c = _rows2d(Y, "Y")
     assert (r, c) == (M, N)
     ws = _workspace(L.qmm_mx_gemm_workspace_bytes(fmt, M, N, K), a.device, ws)
+    _on_current_device(a, w, Y, a_scale, w_scale, ws)
     _check(L.qmm_mx_gemm(fmt, _operand(a, _mx_need(fmt, M, K), "a") if M else 0, M, _operand(w, _mx_need(fmt, N, K), "w"), N, K,
                          _scalar(a_scale), _scalar(w_scale), DTYPES[Y.dtype], ptr, ld, ws.data_ptr(), _nbytes(ws), _stream()))
     return Y
@@ -546,6 +563,7 @@ class ExpertPlan:
         P = T * topk
         self.T, self.topk, self.E = T, topk, E
         self.buf = torch.empty(2 * P + 2 * (E + 1), dtype=torch.int32, device=device)
+        self.device = self.buf.get_device()
         self.order, self.place, self.offsets, self.units = self.buf.split([P, P, E + 1, E + 1])
         base = self.buf.data_ptr()
         self.ptrs = (base, base + 4 * P, base + 8 * P, base + 8 * P + 4 * (E + 1))         # order, place, offsets, units
@@ -561,7 +579,7 @@ def expert_sort(idx: torch.Tensor, E: int, out: ExpertPlan | None = None) -> Exp
         out = ExpertPlan(T, topk, E, idx.device)
     assert out.T == T and out.topk == topk and out.E == E
     order, place, offsets, units = out.ptrs
-    _check((_ext or _native()).expert_sort(idx, E, order, place, offsets, units, out.ws_ptr, out.ws_bytes))
+    _check((_ext or _native()).expert_sort(idx, E, order, place, offsets, units, out.ws_ptr, out.ws_bytes, out.device))
     return out
 
 
@@ -569,7 +587,7 @@ def expert_gather(x: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | Non
     """xs [T * topk, H]: row place[p] = (weights[p] *) x[p // topk]; rows past the last pair are zero."""
     if out is None:
         out = torch.empty((plan.T * plan.topk, x.shape[1]), dtype=x.dtype, device=x.device)
-    _check((_ext or _native()).expert_gather(x, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], weights, out))
+    _check((_ext or _native()).expert_gather(x, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], plan.device, weights, out))
     return out
 
 
@@ -577,7 +595,7 @@ def expert_combine(ys: torch.Tensor, plan: ExpertPlan, weights: torch.Tensor | N
     """y [T, H] = sum over a token's pairs of (weights[p] *) ys[place[p]]."""
     if out is None:
         out = torch.empty((plan.T, ys.shape[1]), dtype=ys.dtype, device=ys.device)
-    _check((_ext or _native()).expert_combine(ys, plan.T, plan.topk, plan.ptrs[1], weights, out))
+    _check((_ext or _native()).expert_combine(ys, plan.T, plan.topk, plan.ptrs[1], plan.device, weights, out))
     return out
 
 
@@ -588,7 +606,7 @@ def expert_combine_grad(dy: torch.Tensor, ys: torch.Tensor, plan: ExpertPlan, we
         dys = torch.empty((plan.T * plan.topk, dy.shape[1]), dtype=dy.dtype, device=dy.device)
     if dw is None:
         dw = torch.empty((plan.T, plan.topk), dtype=torch.float32, device=dy.device)
-    _check((_ext or _native()).expert_combine_grad(dy, ys, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], weights, dys, dw))
+    _check((_ext or _native()).expert_combine_grad(dy, ys, plan.T, plan.topk, plan.ptrs[0], plan.ptrs[1], plan.device, weights, dys, dw))
     return dys, dw
 
 
@@ -611,6 +629,7 @@ def mx_quantize_experts(fmt: int, x: torch.Tensor, idx: torch.Tensor, plan: Expe
     need = mx_experts_bytes(fmt, T, plan.topk, plan.E, K)
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _on_current_device(x, idx, plan.buf, out, tensor_scale)
     _check(lib().qmm_mx_quantize_experts(fmt, DTYPES[x.dtype], xp, ldx, T, plan.topk, plan.E, K, idx.data_ptr(), plan.ptrs[1], plan.ptrs[2],
                                          plan.ptrs[3], _scalar(tensor_scale), _operand(out, need, "out") if T else 0, _stream()))
     return out
@@ -623,6 +642,7 @@ def mx_experts_gate_up(fmt: int, a: torch.Tensor, plan: ExpertPlan, w_gate: torc
     each, need = E * mx_bytes(fmt, N, K), mx_experts_bytes(fmt, T, topk, E, N)
     if h is None:
         h = torch.empty(need, dtype=torch.uint8, device=a.device)
+    _on_current_device(a, plan.buf, w_gate, w_up, h, a_scale, gate_scale, up_scale, h_scale, status)
     _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                         _operand(w_gate, each, "w_gate"), _operand(w_up, each, "w_up"), N, K, _scalar(a_scale),
                                         _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h"), _dp(status), _stream()))
@@ -637,6 +657,7 @@ def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor
         Y = torch.empty((T * topk, N), dtype=dtype, device=a.device)
     yp, ldy, r, c = _rows2d(Y, "Y")
     assert (r, c) == (T * topk, N)
+    _on_current_device(a, plan.buf, w, Y, a_scale, w_scale, status)
     _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                      _operand(w, E * mx_bytes(fmt, N, K), "w"), N, K, _scalar(a_scale), _scalar(w_scale, E), DTYPES[Y.dtype],
                                      yp, ldy, _dp(status), _stream()))
@@ -659,6 +680,7 @@ def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int,
                   _operand(w_up, gu, "w_up"), _operand(w_down, dn, "w_down"), _scalar(x_scale), _scalar(h_scale), _scalar(gate_scale, E),
                   _scalar(up_scale, E), _scalar(down_scale, E), op, ldo, int(rows_dtype is torch.float32))
     a._keep = (X, idx, weights, w_gate, w_up, w_down, out, x_scale, gate_scale, up_scale, down_scale, h_scale)
+    _on_current_device(*a._keep)
     return a
 
 
@@ -667,6 +689,7 @@ def mx_moe_workspace_bytes(args: MxMoeArgs) -> int:
 
 
 def mx_moe_run(args: MxMoeArgs, ws: torch.Tensor) -> None:
+    _on_current_device(ws, *getattr(args, "_keep", ())[:1])
     _check(lib().qmm_mx_moe(ctypes.byref(args), ws.data_ptr(), _nbytes(ws), _stream()))
 
 

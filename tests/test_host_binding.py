@@ -1,0 +1,210 @@
+"""The binding without a GPU: the extension's checks and calls, on a stand-in for libqmm and for the tensors.
+
+The extension is compiled together with C functions of the library's names that record their call and, where told, wait; the
+tensors are objects with the attributes that it reads."""
+import importlib.machinery
+import importlib.util
+import os
+import subprocess
+import sys
+import sysconfig
+import threading
+import time
+
+import pytest
+import torch
+
+from paper_2607_00501_b200 import _build
+
+STUB = r"""
+#include <unistd.h>
+#include "qmm.h"
+int calls = 0, naps_us = 0;
+static qmm_status called(void) { __atomic_add_fetch(&calls, 1, __ATOMIC_SEQ_CST); if (naps_us) usleep(naps_us); return QMM_OK; }
+size_t qmm_mx_bytes(qmm_mx_format fmt, int64_t rows, int64_t K) { return (size_t)((rows + 127) / 128 * ((K + 255) / 256) * (16384 + 32768 / (int)fmt)); }
+qmm_status qmm_mx_quantize(qmm_mx_format f, qmm_dtype d, const void* x, int64_t l, int64_t r, int64_t K, const float* t, void* p, void* s) { return called(); }
+qmm_status qmm_mx_dequantize(qmm_mx_format f, const void* p, int64_t r, int64_t K, const float* t, qmm_dtype d, void* o, int64_t l, void* s) { return called(); }
+qmm_status qmm_mx_linear(qmm_mx_format f, qmm_dtype d, const void* X, int64_t l, int64_t M, const void* w, int64_t N, int64_t K, const float* xs, const float* ws, void* Y,
+                         int64_t ly, void* k, size_t kb, void* s) { return called(); }
+qmm_status qmm_expert_sort(const int32_t* i, int32_t T, int32_t k, int32_t E, int32_t* o, int32_t* p, int32_t* f, int32_t* u, void* w, size_t b, void* s) { return called(); }
+qmm_status qmm_expert_gather(qmm_dtype d, const void* x, int64_t l, int32_t T, int32_t k, int64_t H, const int32_t* o, const int32_t* p, const float* w, void* xs, int64_t lx,
+                             void* s) { return called(); }
+qmm_status qmm_expert_combine(qmm_dtype d, const void* y, int64_t l, int32_t T, int32_t k, int64_t H, const int32_t* p, const float* w, void* o, int64_t lo, void* s) { return called(); }
+qmm_status qmm_expert_combine_grad(qmm_dtype d, const void* dy, int64_t l, const void* y, int64_t ly, int32_t T, int32_t k, int64_t H, const int32_t* o, const int32_t* p,
+                                   const float* w, void* dys, int64_t ld, float* dw, void* s) { return called(); }
+"""
+
+
+class Tensor:
+    """What the extension reads of a CUDA tensor."""
+
+    def __init__(self, *shape, dtype=torch.float16, device=0):
+        self.shape, self.dtype, self.is_cuda, self.device = tuple(shape), dtype, True, device
+
+    def stride(self):
+        return tuple(self.shape[1:]) + (1,)
+
+    def dim(self):
+        return len(self.shape)
+
+    def numel(self):
+        n = 1
+        for s in self.shape:
+            n *= s
+        return n
+
+    def element_size(self):
+        return self.dtype.itemsize
+
+    def data_ptr(self):
+        return 4096
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self.device
+
+
+@pytest.fixture(scope="module")
+def ext(tmp_path_factory):
+    """The extension over the stand-in; device 0 of two is current, streams are handle 0."""
+    import ctypes
+    at = tmp_path_factory.mktemp("binding")
+    (at / "stub.c").write_text(STUB)
+    so = str(at / ("_qmm_py" + sysconfig.get_config_var("EXT_SUFFIX")))
+    root = os.path.dirname(_build.HERE)
+    subprocess.run(["gcc", "-O1", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], "-I", os.path.join(root, "include"), os.path.join(_build.CSRC, "qmm_py.c"),
+                    str(at / "stub.c"), "-o", so], check=True)
+    kept = {n: getattr(torch._C, n) for n in ("_cuda_getCurrentRawStream", "_cuda_getDevice", "_cuda_getDeviceCount")}
+    torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice, torch._C._cuda_getDeviceCount = (lambda device: 0), (lambda: 0), (lambda: 2)
+    try:
+        loader = importlib.machinery.ExtensionFileLoader("_qmm_py", so)
+        module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_qmm_py", loader))
+        loader.exec_module(module)
+    finally:
+        for n, f in kept.items():
+            setattr(torch._C, n, f)
+        sys.modules.pop("_qmm_py", None)
+    lib = ctypes.CDLL(so)
+    module_calls = lambda: ctypes.c_int.in_dll(lib, "calls").value                 # noqa: E731
+    naps = ctypes.c_int.in_dll(lib, "naps_us")
+    return module, module_calls, naps
+
+
+def every_call(device=lambda i: 0):
+    """(name, arguments) of a good call of every entry; device(i) places its i-th tensor.  The plan's arrays are addresses."""
+    u8, f32, i32 = torch.uint8, torch.float32, torch.int32
+    T, k, H = 4, 2, 64
+    calls = [
+        ("mx_quantize", [32, (5, 256), ((17408,), u8), None]),
+        ("mx_quantize", [16, (5, 256), ((18432,), u8), ((1,), f32)]),
+        ("mx_dequantize", [16, ((18432,), u8), (5, 256), ((1,), f32)]),
+        ("mx_linear", [16, (5, 256), ((18432,), u8), 100, (5, 100), ((1,), f32), ((1,), f32), ((4096,), u8)]),
+        ("expert_sort", [((T, k), i32), 8, 4096, 4096, 4096, 4096, 0, 0, 0]),
+        ("expert_gather", [(T, H), T, k, 4096, 4096, 0, ((T, k), f32), (T * k, H)]),
+        ("expert_combine", [(T * k, H), T, k, 4096, 0, ((T, k), f32), (T, H)]),
+        ("expert_combine_grad", [(T, H), (T * k, H), T, k, 4096, 4096, 0, ((T, k), f32), (T * k, H), ((T, k), f32)]),
+    ]
+    out = []
+    for name, args in calls:
+        made, i = [], 0
+        for a in args:
+            if isinstance(a, tuple):
+                shape, dtype = a if isinstance(a[0], tuple) else (a, torch.float16)
+                made.append(Tensor(*shape, dtype=dtype, device=device(i)))
+                i += 1
+            else:
+                made.append(a)
+        out.append((name, made, i))
+    return out
+
+
+def test_good_calls_reach_the_library(ext):
+    module, calls, _ = ext
+    for name, args, _ in every_call():
+        before = calls()
+        assert getattr(module, name)(*args) == 0 and calls() == before + 1
+
+
+def test_tensors_of_another_gpu_are_refused(ext):
+    """A kernel runs on the current device: a tensor of another one, or tensors of two, never reach the library."""
+    module, calls, _ = ext
+    for n, (name, _, tensors) in enumerate(every_call()):
+        for odd in [None, *range(tensors)]:
+            args = every_call(lambda i: 1 if odd is None or i == odd else 0)[n][1]
+            before = calls()
+            with pytest.raises(AssertionError, match="device"):
+                getattr(module, name)(*args)
+            assert calls() == before
+
+
+def test_wrappers_refuse_tensors_of_another_gpu(monkeypatch):
+    """The same for the calls that go through ctypes (over a stand-in whose launches are only counted)."""
+    from types import SimpleNamespace
+
+    from paper_2607_00501_b200 import qmm
+    _build.build()
+    real, launched = qmm.lib(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith(("_bytes", "_error")) else lambda *a: launched.append(name) or 0
+    monkeypatch.setattr(qmm, "lib", Lib)
+    monkeypatch.setattr(qmm, "_stream", lambda: 0)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(qmm, "_one_gpu", False)
+    T, k, E, H = 4, 2, 8, 256
+    u8, i32, f32 = torch.uint8, torch.int32, torch.float32
+    unit, rows = qmm.mx_bytes(16, 1, 256), qmm.mx_experts_bytes(16, T, k, E, H)
+    plan = SimpleNamespace(T=T, topk=k, E=E, ptrs=(4096,) * 4, buf=None)
+    wrappers = [
+        lambda t: qmm.mx_pack(16, t(5, 128, dtype=u8), t(5, 16, dtype=u8), H, out=t(unit, dtype=u8)),
+        lambda t: qmm.mx_gemm(16, t(unit, dtype=u8), 5, t(unit, dtype=u8), 100, H, Y=t(5, 100), a_scale=t(1, dtype=f32), w_scale=t(1, dtype=f32), ws=t(1024, dtype=u8)),
+        lambda t: qmm.mx_quantize_experts(16, t(T, H), t(T, k, dtype=i32), plan, out=t(rows, dtype=u8), tensor_scale=t(1, dtype=f32)),
+        lambda t: qmm.mx_experts_gate_up(16, t(rows, dtype=u8), plan, t(E * unit, dtype=u8), t(E * unit, dtype=u8), 100, H, h=t(rows, dtype=u8), a_scale=t(1, dtype=f32),
+                                         gate_scale=t(E, dtype=f32), up_scale=t(E, dtype=f32), h_scale=t(1, dtype=f32)),
+        lambda t: qmm.mx_experts_gemm(16, t(rows, dtype=u8), plan, t(E * unit, dtype=u8), 100, H, Y=t(T * k, 100), a_scale=t(1, dtype=f32), w_scale=t(E, dtype=f32)),
+        lambda t: qmm.mx_moe_run(qmm.mx_moe_args(16, t(T, H), t(T, k, dtype=i32), t(T, k, dtype=f32), t(E * unit, dtype=u8), t(E * unit, dtype=u8), t(2 * E * unit, dtype=u8), 100, E,
+                                                 t(T, H), x_scale=t(1, dtype=f32), gate_scale=t(E, dtype=f32)), t(1 << 20, dtype=u8)),
+    ]
+    for call in wrappers:
+        made = []
+        call(lambda *shape, dtype=torch.float16: made.append(Tensor(*shape, dtype=dtype)) or made[-1])
+        count = len(made)
+        assert len(launched) == 1
+        for odd in range(count):
+            i = iter(range(count))
+            with pytest.raises(AssertionError, match="device"):
+                call(lambda *shape, dtype=torch.float16: Tensor(*shape, dtype=dtype, device=int(next(i) == odd)))
+        assert len(launched) == 1
+        launched.clear()
+
+
+def test_plan_of_another_gpu_is_refused(ext, monkeypatch):
+    """The plan's arrays go through the extension as addresses, with their device beside them."""
+    from paper_2607_00501_b200 import qmm
+    module, calls, _ = ext
+    monkeypatch.setattr(qmm, "_ext", module)
+    plan = qmm.ExpertPlan.__new__(qmm.ExpertPlan)
+    plan.T, plan.topk, plan.E, plan.ptrs, plan.ws_ptr, plan.ws_bytes = 4, 2, 8, (4096,) * 4, 0, 0
+    x, ys, w, idx = Tensor(4, 64), Tensor(8, 64), Tensor(4, 2, dtype=torch.float32), Tensor(4, 2, dtype=torch.int32)
+    for call in (lambda: qmm.expert_sort(idx, 8, out=plan), lambda: qmm.expert_gather(x, plan, out=ys), lambda: qmm.expert_combine(ys, plan, out=x),
+                 lambda: qmm.expert_gather_grad(ys, plan, out=x), lambda: qmm.expert_combine_grad(x, ys, plan, w, dys=ys, dw=w)):
+        plan.device, before = 0, calls()
+        call()
+        assert calls() == before + 1
+        plan.device = 1
+        with pytest.raises(AssertionError, match="device"):
+            call()
+        assert calls() == before + 1
+
+
+def test_cpu_tensors_are_refused(ext):
+    module, calls, _ = ext
+    before = calls()
+    for n, (name, _, tensors) in enumerate(every_call()):
+        for odd in range(tensors):
+            with pytest.raises(AssertionError):
+                getattr(module, name)(*every_call(lambda i: -1 if i == odd else 0)[n][1])
+    assert calls() == before
