@@ -112,32 +112,30 @@ mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K
     const int64_t chunks = KU * (kUnitK / 32);
     int64_t id = (int64_t)blockIdx.x * kQuantThreads + threadIdx.x;
     const bool live = id < rows * chunks;                  // (whole quads: rows * chunks is a multiple of 8)
-    if (VEC >= 16 && !live) return;
-    if (!live) id = 0;
+    if (!live) id = 0;                                     // (stays: whole warps meet below)
     const int64_t row = id / chunks;
     const int c = (int)(id - row * chunks);
     const TensorScale ts(tensor_scale ? __ldg(tensor_scale) : 1.0f);
     const int64_t left = K - (int64_t)c * 32;
     const T* src = x + row * ldx + (int64_t)c * 32;
-    const int n = (int)(left < 0 ? 0 : left < 32 ? left : 32);
+    const int n = (int)(left < 0 || !live ? 0 : left < 32 ? left : 32);
     float v[32];
     if constexpr (VEC >= 16) {
         load32<T, VEC>(src, n, v);
     } else {
         __shared__ AnyRows<T> sm;
-        load32_any<T, VEC>(sm, src, live ? n : 0, v);
-        if (!live) return;
+        load32_any<T, VEC>(sm, src, n, v);
     }
     uint32_t sb;
     const uint4 codes = quantize32<FMT>(v, ts, sb);
     // scale bytes of the group of four blocks, assembled in its first lane
     constexpr int LANES = FMT == QMM_MXFP4 ? 4 : 2;
     const uint32_t sub = (uint32_t)c & (LANES - 1);
-    const uint32_t mine = ((1u << LANES) - 1u) << ((threadIdx.x & 31) & ~(LANES - 1));      // these lanes: whole and live, whatever branches they came by
     uint32_t word = sb << (sub * (32 / LANES));
     if (left <= 0) word = 0;
 #pragma unroll
-    for (int o = 1; o < LANES; o <<= 1) word |= __shfl_xor_sync(mine, word, o);
+    for (int o = 1; o < LANES; o <<= 1) word |= __shfl_xor_sync(0xFFFFFFFFu, word, o);       // whole warps, whatever branches their lanes came by
+    if (!live) return;
     const uint32_t group = (uint32_t)(c & 7) / LANES;
     auto store = [&](int64_t slot) {
         uint8_t* unit = packed + ((slot >> 7) * KU + (c >> 3)) * unit_bytes(FMT);
