@@ -147,6 +147,16 @@ static int arity(Py_ssize_t have, Py_ssize_t want)
     return -1;
 }
 
+/* The library's call, its status the result.  Other Python threads run meanwhile: a launch waits where the launch queue is full, and the stream before it may wait
+ * for a host function that needs the interpreter. */
+#define CALL(expr)                      \
+    do {                                \
+        qmm_status status_;             \
+        Py_BEGIN_ALLOW_THREADS          \
+        status_ = expr;                 \
+        Py_END_ALLOW_THREADS            \
+        return PyLong_FromLong(status_); \
+    } while (0)
 #define TRY(x) \
     if (x) return NULL
 #define UNLESS(cond, what, why) \
@@ -163,7 +173,7 @@ static PyObject* py_mx_quantize(PyObject* self, PyObject* const* a, Py_ssize_t n
     void *out, *scale, *stream;
     TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[1], "x", &x, &dev));
     TRY(get_flat(a[2], "out", dt_u8, packed_need(fmt, x.rows, x.cols), 0, 0, &out, &dev) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale, &dev) || get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_mx_quantize((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, x.cols, scale, out, stream));
+    CALL(qmm_mx_quantize((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, x.cols, scale, out, stream));
 }
 
 /* (fmt, packed, out, tensor_scale) */
@@ -174,7 +184,7 @@ static PyObject* py_mx_dequantize(PyObject* self, PyObject* const* a, Py_ssize_t
     void *packed, *scale, *stream;
     TRY(arity(n, 4) || get_ints(a, 1, &fmt) || get_rows(a[2], "out", &o, &dev));
     TRY(get_flat(a[1], "packed", dt_u8, packed_need(fmt, o.rows, o.cols), 0, 0, &packed, &dev) || get_flat(a[3], "tensor_scale", dt[2], 1, 1, 1, &scale, &dev) || get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_mx_dequantize((qmm_mx_format)fmt, packed, o.rows, o.cols, scale, (qmm_dtype)o.dtype, o.ptr, o.ld, stream));
+    CALL(qmm_mx_dequantize((qmm_mx_format)fmt, packed, o.rows, o.cols, scale, (qmm_dtype)o.dtype, o.ptr, o.ld, stream));
 }
 
 /* (fmt, X, w, N, Y, x_scale, w_scale, ws) */
@@ -188,7 +198,7 @@ static PyObject* py_mx_linear(PyObject* self, PyObject* const* a, Py_ssize_t n)
     TRY(get_flat(a[2], "w", dt_u8, packed_need(fmt, N, x.cols), 0, 0, &w, &dev) || get_flat(a[5], "x_scale", dt[2], 1, 1, 1, &xs, &dev) ||
         get_flat(a[6], "w_scale", dt[2], 1, 1, 1, &wsc, &dev) || get_flat(a[7], "ws", dt_u8, 0, 0, 0, &ws, &dev) || get_stream(dev, &stream));
     const int64_t ws_bytes = number(a[7], s_numel);
-    return PyLong_FromLong(qmm_mx_linear((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, w, N, x.cols, xs, wsc, y.ptr, y.ld, ws, (size_t)ws_bytes, stream));
+    CALL(qmm_mx_linear((qmm_mx_format)fmt, (qmm_dtype)x.dtype, x.ptr, x.ld, x.rows, w, N, x.cols, xs, wsc, y.ptr, y.ld, ws, (size_t)ws_bytes, stream));
 }
 
 /* (idx, E, order, place, offsets, units, ws, ws_bytes, device): the plan's arrays as addresses, and their device */
@@ -200,7 +210,7 @@ static PyObject* py_expert_sort(PyObject* self, PyObject* const* a, Py_ssize_t n
     TRY(get_flat(a[0], "idx", dt_i32, 0, 0, 0, &idx, &dev));
     if (pair(PyObject_GetAttr(a[0], s_shape), &T, &topk)) return fail_assert("idx", "[T, topk] is wanted"), NULL;
     TRY(get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_expert_sort(idx, (int32_t)T, (int32_t)topk, (int32_t)v[0], (int32_t*)v[1], (int32_t*)v[2], (int32_t*)v[3], (int32_t*)v[4], (void*)v[5],
+    CALL(qmm_expert_sort(idx, (int32_t)T, (int32_t)topk, (int32_t)v[0], (int32_t*)v[1], (int32_t*)v[2], (int32_t*)v[3], (int32_t*)v[4], (void*)v[5],
                                            (size_t)v[6], stream));
 }
 
@@ -213,7 +223,7 @@ static PyObject* py_expert_gather(PyObject* self, PyObject* const* a, Py_ssize_t
     TRY(arity(n, 8) || get_ints(a + 1, 5, v) || on_device(v[4], "plan", &dev) || get_rows(a[0], "x", &x, &dev) || get_rows(a[7], "out", &o, &dev));
     UNLESS(x.rows == v[0] && o.rows == v[0] * v[1] && o.cols == x.cols && o.dtype == x.dtype, "out", "x [T, H] and out [T * topk, H] of one type are wanted");
     TRY(get_flat(a[6], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_expert_gather((qmm_dtype)x.dtype, x.ptr, x.ld, (int32_t)v[0], (int32_t)v[1], x.cols, (const int32_t*)v[2], (const int32_t*)v[3], w, o.ptr,
+    CALL(qmm_expert_gather((qmm_dtype)x.dtype, x.ptr, x.ld, (int32_t)v[0], (int32_t)v[1], x.cols, (const int32_t*)v[2], (const int32_t*)v[3], w, o.ptr,
                                              o.ld, stream));
 }
 
@@ -226,7 +236,7 @@ static PyObject* py_expert_combine(PyObject* self, PyObject* const* a, Py_ssize_
     TRY(arity(n, 7) || get_ints(a + 1, 4, v) || on_device(v[3], "plan", &dev) || get_rows(a[0], "ys", &y, &dev) || get_rows(a[6], "out", &o, &dev));
     UNLESS(y.rows == v[0] * v[1] && o.rows == v[0] && o.cols == y.cols && o.dtype == y.dtype, "out", "ys [T * topk, H] and out [T, H] of one type are wanted");
     TRY(get_flat(a[5], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_expert_combine((qmm_dtype)y.dtype, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], y.cols, (const int32_t*)v[2], w, o.ptr, o.ld, stream));
+    CALL(qmm_expert_combine((qmm_dtype)y.dtype, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], y.cols, (const int32_t*)v[2], w, o.ptr, o.ld, stream));
 }
 
 /* (dy, ys, T, topk, order, place, device, weights, dys, dw) */
@@ -239,7 +249,7 @@ static PyObject* py_expert_combine_grad(PyObject* self, PyObject* const* a, Py_s
     UNLESS(d.rows == v[0] && y.rows == v[0] * v[1] && o.rows == y.rows && y.cols == d.cols && o.cols == d.cols && y.dtype == d.dtype && o.dtype == d.dtype, "dys",
            "dy [T, H], ys and dys [T * topk, H] of one type are wanted");
     TRY(get_flat(a[7], "weights", dt[2], v[0] * v[1], 1, 1, &w, &dev) || get_flat(a[9], "dw", dt[2], v[0] * v[1], 1, 0, &dw, &dev) || get_stream(dev, &stream));
-    return PyLong_FromLong(qmm_expert_combine_grad((qmm_dtype)d.dtype, d.ptr, d.ld, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], d.cols, (const int32_t*)v[2],
+    CALL(qmm_expert_combine_grad((qmm_dtype)d.dtype, d.ptr, d.ld, y.ptr, y.ld, (int32_t)v[0], (int32_t)v[1], d.cols, (const int32_t*)v[2],
                                                    (const int32_t*)v[3], w, o.ptr, o.ld, dw, stream));
 }
 

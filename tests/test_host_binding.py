@@ -208,3 +208,28 @@ def test_cpu_tensors_are_refused(ext):
             with pytest.raises(AssertionError):
                 getattr(module, name)(*every_call(lambda i: -1 if i == odd else 0)[n][1])
     assert calls() == before
+
+
+def test_calls_let_other_threads_run(ext):
+    """While a call waits in the library (a launch queue may be full), other Python threads go on."""
+    module, _, naps = ext
+    naps.value = 200000
+    try:
+        for name, args, _ in every_call():
+            ticks, stop = [0], threading.Event()
+
+            def tick():
+                while not stop.is_set():
+                    ticks[0] += 1
+                    time.sleep(0.001)
+            t = threading.Thread(target=tick)
+            t.start()
+            time.sleep(0.02)
+            before = ticks[0]
+            assert getattr(module, name)(*args) == 0
+            during = ticks[0] - before
+            stop.set()
+            t.join()
+            assert during >= 10, "%s: %d ticks in 200 ms" % (name, during)
+    finally:
+        naps.value = 0
