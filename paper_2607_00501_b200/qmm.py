@@ -434,6 +434,11 @@ def _rows2d(t: torch.Tensor, what: str):
     return t.data_ptr(), ld if rows > 1 or ld > cols else cols, rows, cols
 
 
+def _counts(*n) -> None:
+    """Counts are 32-bit in the library (ctypes would cut larger ones)."""
+    assert max(n) < 1 << 31 and min(n) >= -(1 << 31), "a count past 32 bits: %s" % (n,)
+
+
 _one_gpu = None
 
 
@@ -560,6 +565,7 @@ class ExpertPlan:
     and may be refilled).  order, place [T * topk], offsets, units [E + 1]: int32 views of one buffer."""
 
     def __init__(self, T: int, topk: int, E: int, device="cuda"):
+        _counts(T, topk, E, T * topk)
         P = T * topk
         self.T, self.topk, self.E = T, topk, E
         self.buf = torch.empty(2 * P + 2 * (E + 1), dtype=torch.int32, device=device)
@@ -618,6 +624,7 @@ def expert_gather_grad(dxs: torch.Tensor, plan: ExpertPlan, weights: torch.Tenso
 # ---- experts' products on microscaled operands
 
 def mx_experts_bytes(fmt: int, T: int, topk: int, E: int, K: int) -> int:
+    _counts(fmt, T, topk, E)
     return lib().qmm_mx_experts_bytes(fmt, T, topk, E, K)
 
 
@@ -671,6 +678,7 @@ def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int,
     xp, ldx, T, H = _rows2d(X, "X")
     op, ldo, r, c = _rows2d(out, "out")
     topk = idx.shape[1]
+    _counts(T, H, I, E, topk)
     assert idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape[0] == T
     assert weights.is_cuda and weights.dtype == torch.float32 and weights.is_contiguous() and weights.shape == idx.shape
     assert (r, c) == (T, H) and out.dtype == X.dtype

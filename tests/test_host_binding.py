@@ -233,3 +233,31 @@ def test_calls_let_other_threads_run(ext):
             assert during >= 10, "%s: %d ticks in 200 ms" % (name, during)
     finally:
         naps.value = 0
+
+
+def test_sizes_past_32_bits_are_refused(ext):
+    """Token counts are 32-bit in the library: larger ones are refused, not cut."""
+    module, calls, _ = ext
+    before = calls()
+    with pytest.raises(AssertionError):
+        module.expert_sort(Tensor(2**32 + 4, 2, dtype=torch.int32), 8, 4096, 4096, 4096, 4096, 0, 0, 0)
+    with pytest.raises(AssertionError):
+        module.expert_sort(Tensor(4, 2, dtype=torch.int32), 2**32 + 8, 4096, 4096, 4096, 4096, 0, 0, 0)
+    with pytest.raises(AssertionError):
+        module.expert_gather(Tensor(2**32 + 4, 8), 2**32 + 4, 1, 4096, 4096, 0, None, Tensor(2**32 + 4, 8))
+    with pytest.raises(AssertionError):
+        module.mx_quantize(2**32 + 32, Tensor(5, 256), Tensor(17408, dtype=torch.uint8), None)
+    assert calls() == before
+    with pytest.raises(AssertionError):
+        module.mx_quantize(10**30, Tensor(5, 256), Tensor(17408, dtype=torch.uint8), None)
+    from paper_2607_00501_b200 import qmm
+    _build.build()
+    for T, k, E in ((2**32 + 4, 2, 8), (4, 2**32 + 2, 8), (4, 2, 2**32 + 8)):
+        with pytest.raises(AssertionError):
+            qmm.ExpertPlan(T, k, E, device="cpu")
+        with pytest.raises(AssertionError):
+            qmm.mx_experts_bytes(32, T, k, E, 256)
+    with pytest.raises(AssertionError):
+        qmm.mx_moe_args(32, Tensor(2**32 + 4, 256), Tensor(2**32 + 4, 2, dtype=torch.int32), Tensor(2**32 + 4, 2, dtype=torch.float32), None, None, None, 128, 8,
+                        Tensor(2**32 + 4, 256))
+    assert calls() == before
