@@ -1,5 +1,5 @@
 """Build libqmm.so in-tree with nvcc for sm_100a (no other target is built), and beside it the CPython extension
-that marshals the arguments of its hot-path calls."""
+that marshals the arguments of its hot-path calls.  The two are separate: the library serves every other call without the extension."""
 from __future__ import annotations
 
 import os
@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libqmm.so")
-EXT = os.path.join(HERE, "_qmm_py.so")
+EXT = os.path.join(HERE, "_qmm_py" + sysconfig.get_config_var("EXT_SUFFIX"))      # (another CPython does not load it)
 SOURCES = ("qmm_api.cu", "qmm_pack.cu", "qmm_gemv.cu", "qmm_gemm.cu", "qmm_gemm_small.cu", "qmm_moe.cu", "qmm_chain.cu",
            "qmm_mx_api.cu", "qmm_mx_quant.cu", "qmm_mx_gemm.cu", "qmm_expert.cu")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
@@ -26,15 +26,22 @@ def _nvcc() -> str:
     return "nvcc"
 
 
-def _deps_mtime() -> float:
-    files = [os.path.join(CSRC, f) for f in os.listdir(CSRC)]
-    files.append(os.path.join(os.path.dirname(HERE), "include", "qmm.h"))
-    return max(os.path.getmtime(f) for f in files)
+def _stale(target: str, sources) -> bool:
+    """Whether the target is missing or older than the C header or one of these files of csrc/."""
+    files = [os.path.join(CSRC, f) for f in sources] + [os.path.join(os.path.dirname(HERE), "include", "qmm.h")]
+    return not os.path.exists(target) or os.path.getmtime(target) < max(os.path.getmtime(f) for f in files)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """Compile every .cu under csrc/ and link libqmm.so beside this file."""
-    if not force and os.path.exists(LIB) and os.path.exists(EXT) and min(os.path.getmtime(LIB), os.path.getmtime(EXT)) >= _deps_mtime():
+    """libqmm.so and the extension, beside this file."""
+    build_library(force, verbose)
+    build_extension(force)
+    return LIB
+
+
+def build_library(force: bool = False, verbose: bool = False) -> str:
+    """Compile every .cu under csrc/ and link libqmm.so."""
+    if not force and not _stale(LIB, [f for f in os.listdir(CSRC) if f.endswith((".cu", ".cuh"))]):
         return LIB
     os.makedirs(BUILD, exist_ok=True)
     nvcc = _nvcc()
@@ -60,13 +67,19 @@ def build(force: bool = False, verbose: bool = False) -> str:
     cmd = [nvcc, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, LIB)
-    # the extension finds libqmm.so beside itself
+    return LIB
+
+
+def build_extension(force: bool = False) -> str:
+    """Compile csrc/qmm_py.c; the extension finds libqmm.so beside itself."""
+    if not force and not _stale(EXT, ["qmm_py.c"]):
+        return EXT
     tmp = EXT + ".tmp.%d" % os.getpid()
     cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "qmm_py.c"), "-o", tmp,
            "-L", HERE, "-l:libqmm.so", "-Wl,-rpath,$ORIGIN"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, EXT)
-    return LIB
+    return EXT
 
 
 if __name__ == "__main__":

@@ -114,9 +114,9 @@ def lib() -> ctypes.CDLL:
         return _lib
     with _lock:
         if _lib is None:
-            if not os.path.exists(LIB_PATH) or not os.path.exists(os.path.join(_HERE, "_qmm_py.so")):
+            if not os.path.exists(LIB_PATH):
                 from . import _build
-                _build.build()
+                _build.build_library()
             L = ctypes.CDLL(LIB_PATH)
             i64, vp, ci, sz = ctypes.c_int64, ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
             L.qmm_last_error.restype = ctypes.c_char_p
@@ -183,10 +183,14 @@ _ext = None
 
 
 def _native():
-    """The extension that marshals the shortest calls (0.5 us instead of 3 us of a call)."""
+    """The extension that marshals the shortest calls (0.5 us instead of 3 us of a call), built first if it is not there."""
     global _ext
     if _ext is None:
         lib()
+        from . import _build
+        with _lock:
+            if not os.path.exists(_build.EXT):
+                _build.build_extension()
         from . import _qmm_py
         _ext = _qmm_py
     return _ext

@@ -261,3 +261,51 @@ def test_sizes_past_32_bits_are_refused(ext):
         qmm.mx_moe_args(32, Tensor(2**32 + 4, 256), Tensor(2**32 + 4, 2, dtype=torch.int32), Tensor(2**32 + 4, 2, dtype=torch.float32), None, None, None, 128, 8,
                         Tensor(2**32 + 4, 256))
     assert calls() == before
+
+
+OLDER_CALLS = r"""
+import os, sys
+sys.path.insert(0, sys.argv[1])
+from paper_2607_00501_b200 import _build, qmm
+assert os.path.dirname(_build.HERE) == sys.argv[1]
+def run(*a, **k):
+    raise RuntimeError("no compiler on this machine")
+_build.subprocess.run = run
+assert qmm.version() > 0 and qmm.packed_bytes(qmm.Q4, 128, 256) > 0 and qmm.mx_bytes(32, 128, 256) > 0
+try:
+    qmm.mx_quantize(32, None, out=None if len(sys.argv) < 3 else sys.argv[2])
+except RuntimeError as e:
+    assert "no compiler" in str(e)
+else:
+    raise SystemExit("the extension came from nowhere")
+"""
+
+
+def shipped(tmp_path, foreign):
+    """A copy of the package with its library and without the extension (foreign: with one of another interpreter)."""
+    import shutil
+    _build.build()
+    to = tmp_path / os.path.basename(_build.HERE)
+    to.mkdir()
+    for f in os.listdir(_build.HERE):
+        if f.endswith(".py") or f == "libqmm.so":
+            shutil.copy(os.path.join(_build.HERE, f), to / f)
+    if foreign:
+        (to / "_qmm_py.cpython-38-x86_64-linux-gnu.so").write_bytes(b"built for another interpreter")
+    return str(tmp_path)
+
+
+@pytest.mark.parametrize("foreign", [False, True])
+def test_calls_without_the_extension_need_no_compiler(tmp_path, foreign):
+    """A machine with the built library alone serves every call that does not go through the extension."""
+    at = shipped(tmp_path, foreign)
+    r = subprocess.run([sys.executable, "-c", OLDER_CALLS, at, "x"], cwd=at, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
+
+
+def test_extension_is_named_for_its_interpreter(tmp_path):
+    """An extension of one CPython is not loaded by another; the module's place and name are the import system's."""
+    assert _build.EXT.endswith(sysconfig.get_config_var("EXT_SUFFIX"))
+    _build.build()
+    from paper_2607_00501_b200 import qmm
+    assert os.path.samefile(qmm._native().__file__, _build.EXT)
