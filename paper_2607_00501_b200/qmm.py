@@ -473,8 +473,10 @@ def _scalar(t, n: int = 1) -> int:
     return t.data_ptr()
 
 
-def _operand(t: torch.Tensor, need: int, what: str) -> int:
-    """Pointer of a packed operand of at least `need` bytes."""
+def _operand(t: torch.Tensor, need: int, what: str, rows: int = 1) -> int:
+    """Pointer of a packed operand of at least `need` bytes (without rows nothing is touched)."""
+    if rows == 0:
+        return 0
     assert t.is_cuda and t.dtype == torch.uint8 and t.is_contiguous()
     if need == 0:
         raise QmmError(1, last_error())
@@ -505,7 +507,7 @@ def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: to
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=codes.device)
     _on_current_device(codes, scales, out)
-    _check(lib().qmm_mx_pack(fmt, codes.data_ptr(), scales.data_ptr(), rows, K, _operand(out, need, "out"), _stream()))
+    _check(lib().qmm_mx_pack(fmt, codes.data_ptr(), scales.data_ptr(), rows, K, _operand(out, need, "out", rows), _stream()))
     return out
 
 
@@ -542,7 +544,7 @@ def mx_gemm(fmt: int, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int, 
     assert (r, c) == (M, N)
     ws = _workspace(L.qmm_mx_gemm_workspace_bytes(fmt, M, N, K), a.device, ws)
     _on_current_device(a, w, Y, a_scale, w_scale, ws)
-    _check(L.qmm_mx_gemm(fmt, _operand(a, _mx_need(fmt, M, K), "a") if M else 0, M, _operand(w, _mx_need(fmt, N, K), "w"), N, K,
+    _check(L.qmm_mx_gemm(fmt, _operand(a, _mx_need(fmt, M, K), "a", M), M, _operand(w, _mx_need(fmt, N, K), "w"), N, K,
                          _scalar(a_scale), _scalar(w_scale), DTYPES[Y.dtype], ptr, ld, ws.data_ptr(), _nbytes(ws), _stream()))
     return Y
 
@@ -642,7 +644,7 @@ def mx_quantize_experts(fmt: int, x: torch.Tensor, idx: torch.Tensor, plan: Expe
         out = torch.empty(need, dtype=torch.uint8, device=x.device)
     _on_current_device(x, idx, plan.buf, out, tensor_scale)
     _check(lib().qmm_mx_quantize_experts(fmt, DTYPES[x.dtype], xp, ldx, T, plan.topk, plan.E, K, idx.data_ptr(), plan.ptrs[1], plan.ptrs[2],
-                                         plan.ptrs[3], _scalar(tensor_scale), _operand(out, need, "out") if T else 0, _stream()))
+                                         plan.ptrs[3], _scalar(tensor_scale), _operand(out, need, "out", T), _stream()))
     return out
 
 
@@ -654,9 +656,9 @@ def mx_experts_gate_up(fmt: int, a: torch.Tensor, plan: ExpertPlan, w_gate: torc
     if h is None:
         h = torch.empty(need, dtype=torch.uint8, device=a.device)
     _on_current_device(a, plan.buf, w_gate, w_up, h, a_scale, gate_scale, up_scale, h_scale, status)
-    _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
+    _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                         _operand(w_gate, each, "w_gate"), _operand(w_up, each, "w_up"), N, K, _scalar(a_scale),
-                                        _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h"), _dp(status), _stream()))
+                                        _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h", T), _dp(status), _stream()))
     return h
 
 
@@ -669,7 +671,7 @@ def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor
     yp, ldy, r, c = _rows2d(Y, "Y")
     assert (r, c) == (T * topk, N)
     _on_current_device(a, plan.buf, w, Y, a_scale, w_scale, status)
-    _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a"), T, topk, E, plan.ptrs[2], plan.ptrs[3],
+    _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                      _operand(w, E * mx_bytes(fmt, N, K), "w"), N, K, _scalar(a_scale), _scalar(w_scale, E), DTYPES[Y.dtype],
                                      yp, ldy, _dp(status), _stream()))
     return Y

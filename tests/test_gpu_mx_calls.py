@@ -114,3 +114,23 @@ def test_experts_rows_of_another_routing_are_not_stored(qmm):
         stored = other.reshape(-1)[order[offsets[e]: offsets[e + 1]]] == e
         assert np.array_equal(c[stored], cw[stored]) and np.array_equal(s[stored], sw[stored])
         assert (s[~stored] == 0xAB).all() and (c[~stored][:, 0::2] == 0xB).all()
+
+
+def test_no_tokens(qmm):
+    """Calls without rows return empty results, whichever wrapper they go through."""
+    E, H, I = 4, 256, 128
+    idx = torch.empty(0, 2, dtype=torch.int32, device="cuda")
+    plan = qmm.expert_sort(idx, E)
+    gu, dn = torch.zeros(E * qmm.mx_bytes(32, I, H), dtype=torch.uint8, device="cuda"), torch.zeros(E * qmm.mx_bytes(32, H, I), dtype=torch.uint8, device="cuda")
+    x = torch.empty(0, H, dtype=torch.float16, device="cuda")
+    a = qmm.mx_quantize_experts(32, x, idx, plan)
+    h = qmm.mx_experts_gate_up(32, a, plan, gu, gu, I, H)
+    assert a.numel() == 0 and h.numel() == 0
+    assert qmm.mx_experts_gemm(32, h, plan, dn, H, I).shape == (0, H)
+    assert qmm.mx_moe(32, x, idx, torch.empty(0, 2, device="cuda"), gu, gu, dn, I, E).shape == (0, H)
+    assert qmm.mx_pack(32, torch.empty(0, 128, dtype=torch.uint8, device="cuda"), torch.empty(0, 8, dtype=torch.uint8, device="cuda"), 256).numel() == 0
+    assert qmm.mx_dequantize(32, a, 0, H).shape == (0, H)
+    assert qmm.mx_gemm(32, a, 0, gu, I, H).shape == (0, I)
+    assert qmm.expert_gather(x, plan).shape == (0, H) and qmm.expert_combine(x, plan).shape == (0, H)
+    with pytest.raises(qmm.QmmError):
+        qmm.mx_experts_gate_up(8, a, plan, gu, gu, I, H)                           # (an unknown format is still refused)
