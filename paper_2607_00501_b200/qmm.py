@@ -491,7 +491,16 @@ def _workspace(need: int, device, ws: torch.Tensor | None) -> torch.Tensor:
     if ws is None:
         ws = torch.empty(need, dtype=torch.uint8, device=device)
         ws[:1024].zero_()
+    assert ws.is_cuda and ws.is_contiguous(), "workspace: a contiguous CUDA tensor is wanted"
     return ws
+
+
+def _status(t) -> int:
+    """Pointer of a status word in device memory (None: 0)."""
+    if t is None:
+        return 0
+    assert t.is_cuda and t.is_contiguous() and _nbytes(t) >= 4, "status: a word in CUDA memory is wanted"
+    return t.data_ptr()
 
 
 def mx_bytes(fmt: int, rows: int, K: int) -> int:
@@ -638,7 +647,7 @@ def mx_quantize_experts(fmt: int, x: torch.Tensor, idx: torch.Tensor, plan: Expe
                         tensor_scale: torch.Tensor | None = None) -> torch.Tensor:
     """x [T, K] quantised once per token and stored at the row of each of its pairs (rows grouped by expert)."""
     xp, ldx, T, K = _rows2d(x, "x")
-    assert T == plan.T and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape == (T, plan.topk)
+    assert T == plan.T and idx.is_cuda and idx.dtype == torch.int32 and idx.is_contiguous() and idx.shape == (T, plan.topk)
     need = mx_experts_bytes(fmt, T, plan.topk, plan.E, K)
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=x.device)
@@ -658,7 +667,7 @@ def mx_experts_gate_up(fmt: int, a: torch.Tensor, plan: ExpertPlan, w_gate: torc
     _on_current_device(a, plan.buf, w_gate, w_up, h, a_scale, gate_scale, up_scale, h_scale, status)
     _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                         _operand(w_gate, each, "w_gate"), _operand(w_up, each, "w_up"), N, K, _scalar(a_scale),
-                                        _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h", T), _dp(status), _stream()))
+                                        _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h", T), _status(status), _stream()))
     return h
 
 
@@ -673,7 +682,7 @@ def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor
     _on_current_device(a, plan.buf, w, Y, a_scale, w_scale, status)
     _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                      _operand(w, E * mx_bytes(fmt, N, K), "w"), N, K, _scalar(a_scale), _scalar(w_scale, E), DTYPES[Y.dtype],
-                                     yp, ldy, _dp(status), _stream()))
+                                     yp, ldy, _status(status), _stream()))
     return Y
 
 
@@ -703,6 +712,7 @@ def mx_moe_workspace_bytes(args: MxMoeArgs) -> int:
 
 
 def mx_moe_run(args: MxMoeArgs, ws: torch.Tensor) -> None:
+    assert ws.is_cuda and ws.is_contiguous(), "workspace: a contiguous CUDA tensor is wanted"
     _on_current_device(ws, *getattr(args, "_keep", ())[:1])
     _check(lib().qmm_mx_moe(ctypes.byref(args), ws.data_ptr(), _nbytes(ws), _stream()))
 

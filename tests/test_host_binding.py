@@ -181,6 +181,46 @@ def test_wrappers_refuse_tensors_of_another_gpu(monkeypatch):
         launched.clear()
 
 
+def test_host_memory_is_refused_by_the_wrappers(monkeypatch):
+    """Index arrays, workspaces and status words in host memory never reach a kernel (over the same stand-in)."""
+    from types import SimpleNamespace
+
+    from paper_2607_00501_b200 import qmm
+    _build.build()
+    real, launched = qmm.lib(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith(("_bytes", "_error")) else lambda *a: launched.append(name) or 0
+    monkeypatch.setattr(qmm, "lib", Lib)
+    monkeypatch.setattr(qmm, "_stream", lambda: 0)
+    monkeypatch.setattr(qmm, "_one_gpu", True)
+    T, k, E, H, u8, i32 = 4, 2, 8, 256, torch.uint8, torch.int32
+    unit, rows = qmm.mx_bytes(32, 1, 256), qmm.mx_experts_bytes(32, T, k, E, H)
+    plan = SimpleNamespace(T=T, topk=k, E=E, ptrs=(4096,) * 4, buf=None)
+    w = Tensor(E * unit, dtype=u8)
+
+    def host(t, contiguous=True):
+        t.is_cuda, t.is_contiguous = not contiguous, lambda: contiguous
+        return t
+    calls = [lambda idx: qmm.mx_quantize_experts(32, Tensor(T, H), idx, plan, out=Tensor(rows, dtype=u8)),
+             lambda ws: qmm.mx_gemm(32, Tensor(unit, dtype=u8), 5, Tensor(unit, dtype=u8), 100, H, Y=Tensor(5, 100), ws=ws),
+             lambda ws: qmm.mx_moe_run(qmm.MxMoeArgs(), ws),
+             lambda word: qmm.mx_experts_gate_up(32, Tensor(rows, dtype=u8), plan, w, w, 100, H, h=Tensor(rows, dtype=u8), status=word),
+             lambda word: qmm.mx_experts_gemm(32, Tensor(rows, dtype=u8), plan, w, 100, H, Y=Tensor(T * k, 100), status=word)]
+    good = [lambda: Tensor(T, k, dtype=i32), lambda: Tensor(4096, dtype=u8), lambda: Tensor(4096, dtype=u8), lambda: Tensor(1, dtype=i32), lambda: Tensor(1, dtype=i32)]
+    for call, make in zip(calls, good):
+        call(make())
+        for bad in (host(make()), host(make(), contiguous=False)):
+            with pytest.raises(AssertionError):
+                call(bad)
+        assert len(launched) == 1
+        launched.clear()
+    for call in calls[3:]:
+        with pytest.raises(AssertionError):
+            call(Tensor(2, dtype=u8))                                              # not a whole word
+
+
 def test_plan_of_another_gpu_is_refused(ext, monkeypatch):
     """The plan's arrays go through the extension as addresses, with their device beside them."""
     from paper_2607_00501_b200 import qmm
