@@ -396,7 +396,7 @@ qmm_status qmm_moe_route(const qmm_moe_args* args, void* ws, size_t ws_bytes, vo
  *   QMM_MXFP4  blocks of 32, scale e8m0: 2^(b - 127) for byte b < 255, 255 = NaN.  Quantisation takes
  *              b - 127 = floor(log2(amax)) - 2, not below -127 (amax = the block's largest magnitude);
  *              elements above 6 times the scale saturate.
- *   QMM_NVFP4  blocks of 16, scale e4m3 (0x7F = NaN) times one fp32 scale g per tensor.  Quantisation takes
+ *   QMM_NVFP4  blocks of 16, scale e4m3 (sign bit 0; 0x7F = NaN) times one fp32 scale g per tensor.  Quantisation takes
  *              s = rn_e4m3(min(amax / (6 g), 448)); 6 g and the quotient are rounded to fp32.
  * A code is the e2m1 value nearest to x / D, D = scale * g rounded to fp32 (the quotient is rounded to fp32),
  * ties to the even code, beyond 6 saturating, with the sign of x (a zero's sign is not kept).  D = 0 gives codes 0.  A block with an

@@ -100,7 +100,7 @@ template <typename T, int VEC> __device__ __forceinline__ void store32_any(AnyRo
 // 4 (MXFP4) or 2 (NVFP4) neighbouring lanes join their scale bytes into one 4-byte store.
 // EXPERTS: the row is a token, quantised once and stored at the row of each of its pairs.
 // 8192 x 8192 -> MXFP4: fp16 24 us, bf16 26, fp32 49 (6.2 to 7.2 TB/s, part of the codes still in L2: bound by HBM); -> NVFP4: 35, 35, 51 (16-bit values:
-// 4.9 TB/s, bound by instruction issue -- the quotients' correct rounding).
+// 4.9 TB/s, bound by instruction issue -- the quotients' correct rounding, beside the 64-bit division for a chunk's place that every form issues).
 template <int FMT, typename T, int VEC, bool EXPERTS>
 __global__ void __launch_bounds__(kQuantThreads)
 mx_quantize_kernel(const T* __restrict__ x, int64_t ldx, int64_t rows, int64_t K, const float* __restrict__ tensor_scale,
