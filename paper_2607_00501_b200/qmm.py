@@ -446,16 +446,17 @@ def _counts(*n) -> None:
 _one_gpu = None
 
 
-def _on_current_device(*tensors) -> None:
-    """A kernel runs on the current device: CUDA tensors of another one are refused (None is skipped; with one GPU there is no other)."""
+def _on_device(now, *tensors) -> None:
+    """CUDA tensors of another device than `now` (None: the current one, where a kernel runs) are refused.  A tensor may be None; with one GPU there is no other."""
     global _one_gpu
     if _one_gpu is None:
         _one_gpu = torch.cuda.device_count() == 1
     if _one_gpu:
         return
-    now = torch.cuda.current_device()
+    if now is None:
+        now = torch.cuda.current_device()
     for t in tensors:
-        assert t is None or t.get_device() == now, "tensor on device %d, the current device is %d" % (t.get_device(), now)
+        assert t is None or t.get_device() == now, "tensor on device %d, device %d is wanted" % (t.get_device(), now)
 
 
 def _mx_need(fmt: int, rows: int, K: int) -> int:
@@ -515,7 +516,7 @@ def mx_pack(fmt: int, codes: torch.Tensor, scales: torch.Tensor, K: int, out: to
     need = mx_bytes(fmt, rows, K)
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=codes.device)
-    _on_current_device(codes, scales, out)
+    _on_device(None, codes, scales, out)
     _check(lib().qmm_mx_pack(fmt, codes.data_ptr(), scales.data_ptr(), rows, K, _operand(out, need, "out", rows), _stream()))
     return out
 
@@ -552,7 +553,7 @@ def mx_gemm(fmt: int, a: torch.Tensor, M: int, w: torch.Tensor, N: int, K: int, 
     ptr, ld, r, c = _rows2d(Y, "Y")
     assert (r, c) == (M, N)
     ws = _workspace(L.qmm_mx_gemm_workspace_bytes(fmt, M, N, K), a.device, ws)
-    _on_current_device(a, w, Y, a_scale, w_scale, ws)
+    _on_device(None, a, w, Y, a_scale, w_scale, ws)
     _check(L.qmm_mx_gemm(fmt, _operand(a, _mx_need(fmt, M, K), "a", M), M, _operand(w, _mx_need(fmt, N, K), "w"), N, K,
                          _scalar(a_scale), _scalar(w_scale), DTYPES[Y.dtype], ptr, ld, ws.data_ptr(), _nbytes(ws), _stream()))
     return Y
@@ -651,7 +652,7 @@ def mx_quantize_experts(fmt: int, x: torch.Tensor, idx: torch.Tensor, plan: Expe
     need = mx_experts_bytes(fmt, T, plan.topk, plan.E, K)
     if out is None:
         out = torch.empty(need, dtype=torch.uint8, device=x.device)
-    _on_current_device(x, idx, plan.buf, out, tensor_scale)
+    _on_device(None, x, idx, plan.buf, out, tensor_scale)
     _check(lib().qmm_mx_quantize_experts(fmt, DTYPES[x.dtype], xp, ldx, T, plan.topk, plan.E, K, idx.data_ptr(), plan.ptrs[1], plan.ptrs[2],
                                          plan.ptrs[3], _scalar(tensor_scale), _operand(out, need, "out", T), _stream()))
     return out
@@ -664,7 +665,7 @@ def mx_experts_gate_up(fmt: int, a: torch.Tensor, plan: ExpertPlan, w_gate: torc
     each, need = E * mx_bytes(fmt, N, K), mx_experts_bytes(fmt, T, topk, E, N)
     if h is None:
         h = torch.empty(need, dtype=torch.uint8, device=a.device)
-    _on_current_device(a, plan.buf, w_gate, w_up, h, a_scale, gate_scale, up_scale, h_scale, status)
+    _on_device(None, a, plan.buf, w_gate, w_up, h, a_scale, gate_scale, up_scale, h_scale, status)
     _check(lib().qmm_mx_experts_gate_up(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                         _operand(w_gate, each, "w_gate"), _operand(w_up, each, "w_up"), N, K, _scalar(a_scale),
                                         _scalar(gate_scale, E), _scalar(up_scale, E), _scalar(h_scale), _operand(h, need, "h", T), _status(status), _stream()))
@@ -679,7 +680,7 @@ def mx_experts_gemm(fmt: int, a: torch.Tensor, plan: ExpertPlan, w: torch.Tensor
         Y = torch.empty((T * topk, N), dtype=dtype, device=a.device)
     yp, ldy, r, c = _rows2d(Y, "Y")
     assert (r, c) == (T * topk, N)
-    _on_current_device(a, plan.buf, w, Y, a_scale, w_scale, status)
+    _on_device(None, a, plan.buf, w, Y, a_scale, w_scale, status)
     _check(lib().qmm_mx_experts_gemm(fmt, _operand(a, mx_experts_bytes(fmt, T, topk, E, K), "a", T), T, topk, E, plan.ptrs[2], plan.ptrs[3],
                                      _operand(w, E * mx_bytes(fmt, N, K), "w"), N, K, _scalar(a_scale), _scalar(w_scale, E), DTYPES[Y.dtype],
                                      yp, ldy, _status(status), _stream()))
@@ -703,7 +704,7 @@ def mx_moe_args(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int,
                   _operand(w_up, gu, "w_up"), _operand(w_down, dn, "w_down"), _scalar(x_scale), _scalar(h_scale), _scalar(gate_scale, E),
                   _scalar(up_scale, E), _scalar(down_scale, E), op, ldo, int(rows_dtype is torch.float32))
     a._keep = (X, idx, weights, w_gate, w_up, w_down, out, x_scale, gate_scale, up_scale, down_scale, h_scale)
-    _on_current_device(*a._keep)
+    _on_device(X.get_device(), *a._keep)
     return a
 
 
@@ -713,7 +714,7 @@ def mx_moe_workspace_bytes(args: MxMoeArgs) -> int:
 
 def mx_moe_run(args: MxMoeArgs, ws: torch.Tensor) -> None:
     assert ws.is_cuda and ws.is_contiguous(), "workspace: a contiguous CUDA tensor is wanted"
-    _on_current_device(ws, *getattr(args, "_keep", ())[:1])
+    _on_device(None, ws, *getattr(args, "_keep", ())[:1])
     _check(lib().qmm_mx_moe(ctypes.byref(args), ws.data_ptr(), _nbytes(ws), _stream()))
 
 

@@ -181,6 +181,31 @@ def test_wrappers_refuse_tensors_of_another_gpu(monkeypatch):
         launched.clear()
 
 
+def test_arguments_of_a_layer_may_be_built_anywhere(monkeypatch):
+    """mx_moe_args only wants its tensors together; the run is where the current device counts."""
+    from paper_2607_00501_b200 import qmm
+    _build.build()
+    monkeypatch.setattr(qmm, "_one_gpu", False)
+    now = [0]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    u8, i32, f32 = torch.uint8, torch.int32, torch.float32
+    t = lambda *shape, dtype=torch.float16: Tensor(*shape, dtype=dtype, device=1)  # noqa: E731
+    w = t(8 * qmm.mx_bytes(32, 256, 256), dtype=u8)
+    args = qmm.mx_moe_args(32, t(4, 256), t(4, 2, dtype=i32), t(4, 2, dtype=f32), w, w, w, 128, 8, t(4, 256))
+    real, launched = qmm.lib(), []
+
+    class Lib:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith(("_bytes", "_error")) else lambda *a: launched.append(name) or 0
+    monkeypatch.setattr(qmm, "lib", Lib)
+    monkeypatch.setattr(qmm, "_stream", lambda: 0)
+    with pytest.raises(AssertionError, match="device"):
+        qmm.mx_moe_run(args, t(1 << 20, dtype=u8))
+    now[0] = 1
+    qmm.mx_moe_run(args, t(1 << 20, dtype=u8))
+    assert launched == ["qmm_mx_moe"]
+
+
 def test_host_memory_is_refused_by_the_wrappers(monkeypatch):
     """Index arrays, workspaces and status words in host memory never reach a kernel (over the same stand-in)."""
     from types import SimpleNamespace
