@@ -578,15 +578,19 @@ def mx_linear(fmt: int, X: torch.Tensor, w: torch.Tensor, N: int, Y: torch.Tenso
 
 class ExpertPlan:
     """Where each (token, slot) pair of a router's choice goes in expert order (qmm_expert_sort fills it; buffers are kept
-    and may be refilled).  order, place [T * topk], offsets, units [E + 1]: int32 views of one buffer."""
+    and may be refilled; before the first sort every pair counts as dropped).  order, place [T * topk], offsets, units [E + 1]:
+    int32 views of one buffer."""
 
-    def __init__(self, T: int, topk: int, E: int, device="cuda"):
+    def __init__(self, T: int, topk: int, E: int, device="cuda", fill: bool = True):
         _counts(T, topk, E, T * topk)
         P = T * topk
         self.T, self.topk, self.E = T, topk, E
         self.buf = torch.empty(2 * P + 2 * (E + 1), dtype=torch.int32, device=device)
         self.device = self.buf.get_device()
         self.order, self.place, self.offsets, self.units = self.buf.split([P, P, E + 1, E + 1])
+        if fill:                                           # (a sort follows at once otherwise)
+            self.buf[: 2 * P].fill_(-1)
+            self.buf[2 * P:].zero_()
         base = self.buf.data_ptr()
         self.ptrs = (base, base + 4 * P, base + 8 * P, base + 8 * P + 4 * (E + 1))         # order, place, offsets, units
         self.ws_bytes = lib().qmm_expert_sort_workspace_bytes(T, topk, E)
@@ -598,7 +602,7 @@ def expert_sort(idx: torch.Tensor, E: int, out: ExpertPlan | None = None) -> Exp
     """idx [T, topk] int32: experts of each token, values outside [0, E) dropped -> ExpertPlan."""
     T, topk = idx.shape
     if out is None:
-        out = ExpertPlan(T, topk, E, idx.device)
+        out = ExpertPlan(T, topk, E, idx.device, fill=False)
     assert out.T == T and out.topk == topk and out.E == E
     order, place, offsets, units = out.ptrs
     _check((_ext or _native()).expert_sort(idx, E, order, place, offsets, units, out.ws_ptr, out.ws_bytes, out.device))

@@ -134,3 +134,22 @@ def test_no_tokens(qmm):
     assert qmm.expert_gather(x, plan).shape == (0, H) and qmm.expert_combine(x, plan).shape == (0, H)
     with pytest.raises(qmm.QmmError):
         qmm.mx_experts_gate_up(8, a, plan, gu, gu, I, H)                           # (an unknown format is still refused)
+
+
+def test_plan_before_its_first_sort(qmm):
+    """A plan that has not been sorted into drops every pair; its arrays never hold places that are none."""
+    T, topk, E, H = 9, 3, 5, 300
+    for _ in range(3):                                                             # (memory that others have used)
+        torch.full((1 << 20,), 0x7F, dtype=torch.uint8, device="cuda")
+    plan = qmm.ExpertPlan(T, topk, E)
+    x, ys, w = torch.randn(T, H, device="cuda"), torch.randn(T * topk, H, device="cuda"), torch.rand(T, topk, device="cuda")
+    assert bool((plan.order == -1).all()) and bool((plan.place == -1).all()) and not plan.offsets.any() and not plan.units.any()
+    assert not qmm.expert_gather(x, plan).any() and not qmm.expert_combine(ys, plan, w).any()
+    dys, dw = qmm.expert_combine_grad(x, ys, plan, w)
+    assert not dys.any() and not dw.any()
+    idx = torch.zeros(T, topk, dtype=torch.int32, device="cuda")
+    a = torch.full((qmm.mx_experts_bytes(32, T, topk, E, H),), 0xAB, dtype=torch.uint8, device="cuda")
+    qmm.mx_quantize_experts(32, x, idx, plan, out=a)
+    Y = torch.full((T * topk, 64), 7.0, device="cuda")
+    qmm.mx_experts_gemm(32, a, plan, torch.zeros(E * qmm.mx_bytes(32, 64, H), dtype=torch.uint8, device="cuda"), 64, H, Y=Y)
+    assert bool((a == 0xAB).all()) and bool((Y == 7).all())
