@@ -256,8 +256,8 @@ __global__ void __launch_bounds__(MxGeom<FMT, BN, GATEUP, FORM>::kThreads, 1) mx
     if (waited) pdl_wait();                                                   // the rows' grouping is written upstream
     if (GROUPED) {
         for (int e = threadIdx.x; e < ((p.E + 32) & ~31); e += G::kThreads) {
-            s_units[e] = e <= p.E ? __ldg(p.units + e) : 0x7FFFFFFF;
-            if (e <= p.E) s_first[e] = __ldg(p.offsets + e);
+            s_units[e] = e <= p.E ? __ldcg(p.units + e) : 0x7FFFFFFF;         // (from L2: with list_ready no wait of this kernel stands before the read)
+            if (e <= p.E) s_first[e] = __ldcg(p.offsets + e);
         }
     }
     tc_fence_before_sync();
