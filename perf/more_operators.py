@@ -161,8 +161,8 @@ def _own_run(st):
         if case["rows"] == "same":
             y, h = qmm.rms_norm(st["x"], st["weight"], EPS, residual=st["residual"], h=st["h"], y=st["y"])
         else:
-            codes, scales, h = qmm.rms_norm_rows8(st["x"], st["weight"], EPS, residual=st["residual"], h=st["h"], codes=st["codes"], scales=st["scales"])
-            y = qmm.rows8_dequantize(codes, scales, out=st["y"])
+            codes, scales, h = qmm.rms_norm_rows(st["x"], st["weight"], EPS, residual=st["residual"], h=st["h"], codes=st["codes"], scales=st["scales"])
+            y = qmm.rows_dequantize(codes, scales, out=st["y"])
         out = {"y": y}
         if case["residual"]:
             out["h"] = h
