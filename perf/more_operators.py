@@ -256,7 +256,7 @@ def _norm_plain(st):
         top = _TOP[case["rows"]]
         t = hf * w
         amax = t.abs().amax(1, keepdim=True)
-        q = (t * (top / amax)).clamp(-top, top)
+        q = (t * (torch.full_like(amax, top) / amax)).clamp(-top, top)          # (a number / a tensor is a reciprocal and a product: two roundings)
         codes = q.to(torch.float8_e4m3fn).float() if case["rows"] == "e4m3" else torch.round(q)
         out = {"y": (codes * (amax / top * rstd)).to(dt)}
     if case["residual"]:
