@@ -491,6 +491,103 @@ qmm_status qmm_expert_combine_grad(qmm_dtype dtype, const void* dy, int64_t lddy
                                    int32_t T, int32_t topk, int64_t H, const int32_t* order, const int32_t* place,
                                    const float* weights, void* dys, int64_t lddys, float* dw, void* stream);
 
+/* ---- a router's choice ----
+ *
+ * Logits [T, ld] of type `dtype`, ld >= E -> the experts of each token, idx [T, topk], and their weights fp32 [T, topk]: what the
+ * calls above take.  Per token
+ *   s = softmax(l) over all experts, or sigmoid(l);   c = s + bias (bias fp32 [E], NULL: none)
+ *   the E experts form `groups` groups of E / groups consecutive ones, valued by the sum of their group_top (1 or 2)
+ *   largest c (a missing second counts 0); the top_groups best stay, equal ones by lower group
+ *   idx = the topk experts of the largest c among them, larger first, equal ones by lower expert
+ *   weights = scale * s[idx], with `renormalize` divided by the sum of the chosen s before
+ * Scores are compared as they are in 64 bits; without a bias experts are compared by their logits.  An expert whose
+ * logit or bias is -inf or NaN is never chosen: slots for which nothing is left have idx -1 (dropped by the
+ * calls above) and weight 0.  A logit of +inf counts as the largest finite fp32.
+ * 1 <= topk <= min(E, 32), E <= 1024, 1 <= groups <= 32, groups divides E, 1 <= top_groups <= groups.          */
+typedef enum { QMM_SOFTMAX = 0, QMM_SIGMOID = 1 } qmm_scores;
+qmm_status qmm_expert_route(qmm_dtype dtype, const void* logits, int64_t ld, int32_t T, int32_t E, int32_t topk, qmm_scores scores, const float* bias,
+                            int32_t groups, int32_t top_groups, int32_t group_top, int32_t renormalize, float scale, int32_t* idx, float* weights,
+                            void* stream);
+
+/* Gradient of the weights with respect to the logits, at the choice idx (which is constant; so is the bias):
+ * dlogits [T, ldd] of type `dtype` is written whole.  dweights fp32 [T, topk]; what stands at dropped slots is not read
+ * into the result.  dlogits may be logits.                                                            */
+qmm_status qmm_expert_route_grad(qmm_dtype dtype, const float* dweights, const void* logits, int64_t ld, const int32_t* idx, int32_t T, int32_t E,
+                                 int32_t topk, qmm_scores scores, int32_t renormalize, float scale, void* dlogits, int64_t ldd, void* stream);
+
+/* ---- root-mean-square norm, rows of 8 bits ----
+ *
+ * h = x + residual (rounded to `dtype`; residual NULL: h = x),  rstd = 1 / sqrt(mean(h^2) + eps),  y = h * rstd * weight.
+ * x, residual, h, y [rows, ld] of type `dtype`, weight [K] of the same type or NULL (ones), 1 <= K <= 32768, eps > 0.  Statistics
+ * in fp32 (rows whose squares leave its range are formed again with scaled elements).  h, y and codes are
+ * each optional (NULL), y or codes is wanted; h may be x or residual, y may be x, residual or h.
+ * Rows of 8 bits: codes [rows, ldc] bytes and one fp32 scale per row, value = code * scale:
+ *   t = fp32(h * weight), amax = max |t|, code = rn(fp32(t * fp32(L / amax))), scale = amax / L * rstd
+ *   QMM_ROW_E4M3: L = 448, codes are e4m3;  QMM_ROW_INT8: L = 127, codes are int8 (ties to even in both).
+ * amax below 2^-118 counts as zero (codes and scale 0); a row with an infinity or NaN has codes 0 and scale NaN.   */
+typedef enum { QMM_ROW_E4M3 = 0, QMM_ROW_INT8 = 1 } qmm_row_format;
+qmm_status qmm_rms_norm(qmm_dtype dtype, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight, float eps, int64_t rows, int64_t K,
+                        void* h, int64_t ldh, void* y, int64_t ldy, qmm_row_format fmt, void* codes, int64_t ldc, float* scales, void* stream);
+
+/* Gradients for dy at y (an 8-bit output counts as y) and, where dh is given, dh at h from elsewhere:
+ *   xhat = h * rstd,  dx = rstd * (weight dy - xhat * mean(weight dy xhat)) + dh   (of x and of the residual alike)
+ *   dweight = sum over rows of dy * xhat, fp32 [K], added in an order that does not change
+ * dx [rows, lddx] of type `dtype`, may be dy or dh; dx or dweight may be NULL.
+ *   ws  device, 16-byte aligned, >= qmm_rms_norm_grad_workspace_bytes() where dweight is wanted; holds nothing between calls     */
+size_t qmm_rms_norm_grad_workspace_bytes(int64_t rows, int64_t K);
+qmm_status qmm_rms_norm_grad(qmm_dtype dtype, const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* weight, float eps, int64_t rows, int64_t K,
+                             const void* dh, int64_t lddh, void* dx, int64_t lddx, float* dweight, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows as they come -> rows of 8 bits (t = x, rstd = 1 above), and back: out = code * scale rounded to `dtype`.         */
+qmm_status qmm_rows_quantize(qmm_dtype dtype, const void* x, int64_t ldx, int64_t rows, int64_t K, qmm_row_format fmt, void* codes, int64_t ldc,
+                              float* scales, void* stream);
+qmm_status qmm_rows_dequantize(qmm_row_format fmt, const void* codes, int64_t ldc, const float* scales, int64_t rows, int64_t K, qmm_dtype dtype, void* out,
+                                int64_t ldo, void* stream);
+
+/* ---- low-rank adapters beside a shared projection ----
+ *
+ * Row t of X [T, K] belongs to adapter a = idx[t] of n (outside [0, n): to none).  Adapters lie one after the other, A [n, r, K]
+ * and B [n, N, r], of X's type (QMM_F16 or QMM_BF16); r is 8, 16, 32, 64 or 128 (pad with zeros).
+ *   qmm_lora       S[t] = A[a] x[t] (fp32),  Y[t] = Y0[t] + scale[a] * B[a] S[t]
+ *   qmm_lora_grad  dS[t] = scale[a] * B[a]^T dY[t],  dX[t] = dX0[t] + A[a]^T dS[t],
+ *                  dA[a] = sum_t dS[t] x[t]^T,  dB[a] = scale[a] * sum_t dY[t] S[t]^T   (sums over the adapter's rows; fp32, in a fixed order)
+ * A row without an adapter has Y = Y0 and dX = dX0, its row of S is neither written nor read; an adapter without rows has gradients 0.
+ * X may be rows of 8 bits (x_format, x_scale as qmm_rms_norm and qmm_rows_quantize leave them), in the forward pass, in dA, or in both.
+ * Accuracy: sums in fp32; S and dS enter the second products as two 16-bit parts (off by 2^-16 of the row's largest element at most).
+ *   order, offsets, units  of qmm_expert_sort(idx, T, 1, n), for callers that use one sort for many projections; NULL: the call
+ *                          sorts in its workspace (rows up to 256 of a forward pass need no sort)
+ *   Y0 may be Y, dX0 may be dX (in place); NULL counts as zeros.  Otherwise no output may overlap an input.
+ *   S [T, r] is optional in qmm_lora, needed for dB in qmm_lora_grad.  dX, dA and dB are each optional in qmm_lora_grad (dX0 goes with dX).
+ *   ws  device, 256-byte aligned, >= qmm_lora_workspace_bytes(); holds nothing between calls.                        */
+typedef struct {
+    int32_t T, n, r;
+    int32_t dtype;                 /* of X (where x_scale is NULL), A, B, Y and dX      */
+    int32_t x_format;              /* qmm_row_format, where x_scale is given            */
+    int64_t K, N;
+    const void* X;                 /* [T, ldx]                                          */
+    int64_t ldx;
+    const float* x_scale;          /* [T]: X is rows of 8 bits;  NULL: of type dtype    */
+    const int32_t* idx;            /* [T]                                               */
+    const int32_t *order, *offsets, *units;                /* optional plan             */
+    const void *A, *B;
+    const float* scale;            /* [n], NULL: 1                                      */
+    float* S;                      /* [T, r]                                            */
+    const void* Y0;                /* forward: [T, ldy0] in, [T, ldy] out               */
+    int64_t ldy0;
+    void* Y;
+    int64_t ldy;
+    const void* dY;                /* backward: [T, lddy]                               */
+    int64_t lddy;
+    const void* dX0;               /* [T, lddx0] in, [T, lddx] out                      */
+    int64_t lddx0;
+    void* dX;
+    int64_t lddx;
+    float *dA, *dB;                /* [n, r, K], [n, N, r]                              */
+} qmm_lora_args;
+size_t qmm_lora_workspace_bytes(int32_t T, int32_t n, int32_t r);
+qmm_status qmm_lora(const qmm_lora_args* args, void* ws, size_t ws_bytes, void* stream);
+qmm_status qmm_lora_grad(const qmm_lora_args* args, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- experts' products on microscaled operands ----
  *
  * Rows grouped by expert: the packed operand of qmm_mx_quantize_experts holds the rows of expert e in the

@@ -1,5 +1,5 @@
-"""Build libqmm.so in-tree with nvcc for sm_100a (no other target is built), and beside it the CPython extension
-that marshals the arguments of its hot-path calls.  The two are separate: the library serves every other call without the extension."""
+"""Build libqmm.so in-tree with nvcc for sm_100a (no other target is built), and beside it the CPython extensions
+that marshal the arguments of its hot-path calls.  They are separate: the library serves every other call without an extension."""
 from __future__ import annotations
 
 import os
@@ -13,8 +13,10 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "build")
 LIB = os.path.join(HERE, "libqmm.so")
 EXT = os.path.join(HERE, "_qmm_py" + sysconfig.get_config_var("EXT_SUFFIX"))      # (another CPython does not load it)
+LAYER_EXT = os.path.join(HERE, "_qmm_layer_py" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ("qmm_api.cu", "qmm_pack.cu", "qmm_gemv.cu", "qmm_gemm.cu", "qmm_gemm_small.cu", "qmm_moe.cu", "qmm_chain.cu",
-           "qmm_mx_api.cu", "qmm_mx_quant.cu", "qmm_mx_gemm.cu", "qmm_expert.cu")
+           "qmm_mx_api.cu", "qmm_mx_quant.cu", "qmm_mx_gemm.cu", "qmm_expert.cu", "qmm_layer_api.cu", "qmm_router.cu", "qmm_norm.cu", "qmm_lora_f16.cu",
+           "qmm_lora_bf16.cu", "qmm_lora_grad_f16.cu", "qmm_lora_grad_bf16.cu")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-DQMM_BUILD"]
 
@@ -33,7 +35,7 @@ def _stale(target: str, sources) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
-    """libqmm.so and the extension, beside this file."""
+    """libqmm.so and the extensions, beside this file."""
     build_library(force, verbose)
     build_extension(force)
     return LIB
@@ -71,14 +73,15 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
 
 
 def build_extension(force: bool = False) -> str:
-    """Compile csrc/qmm_py.c; the extension finds libqmm.so beside itself."""
-    if not force and not _stale(EXT, ["qmm_py.c"]):
-        return EXT
-    tmp = EXT + ".tmp.%d" % os.getpid()
-    cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "qmm_py.c"), "-o", tmp,
-           "-L", HERE, "-l:libqmm.so", "-Wl,-rpath,$ORIGIN"]
-    subprocess.run(cmd, check=True)
-    os.replace(tmp, EXT)
+    """Compile csrc/qmm_py.c and csrc/qmm_layer_py.c; the extensions find libqmm.so beside themselves."""
+    for target, source in ((EXT, "qmm_py.c"), (LAYER_EXT, "qmm_layer_py.c")):
+        if not force and not _stale(target, [source, "qmm_py.h"]):
+            continue
+        tmp = target + ".tmp.%d" % os.getpid()
+        cmd = ["gcc", "-O2", "-Wall", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, source), "-o", tmp,
+               "-L", HERE, "-l:libqmm.so", "-Wl,-rpath,$ORIGIN"]
+        subprocess.run(cmd, check=True)
+        os.replace(tmp, target)
     return EXT
 
 

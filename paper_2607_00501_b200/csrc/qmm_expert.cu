@@ -1,6 +1,7 @@
 // qmm_expert.cu -- tokens sorted by expert and back: the stable counting sort of a router's choices, the row moves it
 // implies, and their gradients.  The sort is bound by latency, the moves by HBM: they work from the token's side,
 // so that a token's row is read once however many experts it goes to.
+#include "qmm_launch.cuh"
 #include "qmm_mx.cuh"
 
 #include <atomic>
@@ -9,29 +10,6 @@
 namespace qmm {
 
 using namespace mx;
-
-template <typename... P, typename... A>
-static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, size_t smem, int cluster, cudaStream_t st, const char* what, A... args)
-{
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3(threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.numAttrs = 1;
-    if (cluster > 1) {
-        attr[1].id = cudaLaunchAttributeClusterDimension;
-        attr[1].val.clusterDim.x = (unsigned)cluster;
-        attr[1].val.clusterDim.y = 1;
-        attr[1].val.clusterDim.z = 1;
-        cfg.numAttrs = 2;
-    }
-    cfg.attrs = attr;
-    return check_cuda(cudaLaunchKernelEx(&cfg, kern, args...), what);
-}
 
 // ------------------------------------------------------------------ sort
 

@@ -1,0 +1,1091 @@
+// qmm_lora.cuh -- low-rank adapters beside a shared projection: rows of any mixture of adapters, forward and backward.
+//
+//   forward   s = A[a] x,        y  = y0  + scale[a] * B[a] s          A [n, r, K], B [n, N, r], a = idx[row]
+//   backward  ds = scale[a] * B[a]^T dy,  dx = dx0 + A[a]^T ds,  dA[a] = sum ds x^T,  dB[a] = scale[a] * sum dy s^T
+//
+// The forward pass and dx are the same two products, a narrowing one over a row's K elements and a widening one over its N outputs, on weights laid out with either
+// axis contiguous ("LAY" below).  All of them move far more bytes than the tensor cores have work (r = 16: 16 multiply-adds per element read), so what counts is that x and
+// y pass through once, in wide accesses.  They therefore go from global memory straight into the fragments of mma.sync: which k (n) stands at which place of a
+// fragment is free as long as both operands agree, and with the orders below a lane's share of a row is one 16-byte access, without shared memory or
+// transposition.  (tcgen05 would take x through shared memory and y through tensor memory for no gain: the products are 2 to 30 % of the time that the bytes take.)
+//
+// Sums are fp32.  s enters the widening product and the weight gradients as the sum of two 16-bit numbers (high and low part), so that no bits of it are
+// lost that matter beside fp32 sums; for fp16 the rows of s are scaled by a power of two first, or the product is one of tf32 halves (weight gradients), so that fp16's range
+// does not bound s.
+#pragma once
+
+#include "qmm_launch.cuh"
+#include "qmm_mx.cuh"
+
+namespace qmm {
+namespace lora {
+
+using namespace mx;
+
+constexpr int kThreads = 256;
+constexpr int kWarps = kThreads / 32;
+constexpr int kSmallRows = 256;                            // up to here a row's cluster finds its adapter's rows by itself
+constexpr int kTileRows = 64;                              // rows of a tile of the two-launch form (half a unit of the sort)
+
+// ---------------------------------------------------------------- products of fragments
+
+template <typename T> __device__ __forceinline__ void mma16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma8_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t tf32(float v)
+{
+    uint32_t u;
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(u) : "f"(v));
+    return u;
+}
+// The halves of two registers that hold elements i and i + 1 of two rows: element (i & 1) of both, the first row's in the low half.
+__device__ __forceinline__ uint32_t pair_of(uint32_t first, uint32_t second, int odd) { return __byte_perm(first, second, odd ? 0x7632 : 0x5410); }
+
+// (hi, lo) 16-bit parts of two fp32 values.
+template <typename T> __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo)
+{
+    hi = Dt<T>::down2(a, b);
+    const float2 f = Dt<T>::up2(hi);
+    lo = Dt<T>::down2(a - f.x, b - f.y);
+}
+
+// Three bf16 parts of two fp32 values: all 24 bits.
+__device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t& mid, uint32_t& lo)
+{
+    hi = Dt<__nv_bfloat16>::down2(a, b);
+    const float2 f = Dt<__nv_bfloat16>::up2(hi);
+    split2<__nv_bfloat16>(a - f.x, b - f.y, mid, lo);
+}
+
+// ------------------------------------------------------------------ loads
+
+// Eight consecutive elements of a row as four registers of T pairs; elements from `left` on are zero.  VEC: one access (left is then 0 or at least 8).
+// NC: nobody writes the row meanwhile (y0 may be y).
+template <typename T, bool VEC, bool NC = true> __device__ __forceinline__ void load8(const T* p, int left, uint32_t (&u)[4])
+{
+    if (VEC) {
+        if (left > 0) {
+            const uint4 q = NC ? __ldg(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
+            u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
+        } else {
+            u[0] = u[1] = u[2] = u[3] = 0u;
+        }
+    } else {
+        const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t a = 0u, b = 0u;
+            if (2 * i < left) a = NC ? __ldg(s + 2 * i) : s[2 * i];
+            if (2 * i + 1 < left) b = NC ? __ldg(s + 2 * i + 1) : s[2 * i + 1];
+            u[i] = a | (b << 16);
+        }
+    }
+}
+// R8 consecutive elements (1, 2, 4, 8 or 16) of a weight row of r contiguous ones; (R8 + 1) / 2 registers, a single element in the low half.
+template <typename T, int R8, bool VEC> __device__ __forceinline__ void load_r(const T* p, bool there, uint32_t (&u)[(R8 + 1) / 2])
+{
+#pragma unroll
+    for (int i = 0; i < (R8 + 1) / 2; ++i) u[i] = 0u;
+    if (!there) return;
+    const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+    if constexpr (R8 == 1) {
+        u[0] = __ldg(s);
+    } else if (!VEC) {
+#pragma unroll
+        for (int i = 0; i < R8 / 2; ++i) u[i] = (uint32_t)__ldg(s + 2 * i) | ((uint32_t)__ldg(s + 2 * i + 1) << 16);
+    } else if constexpr (R8 == 2) {
+        u[0] = __ldg(reinterpret_cast<const uint32_t*>(p));
+    } else if constexpr (R8 == 4) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(p));
+        u[0] = q.x, u[1] = q.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < R8 / 8; ++i) {
+            const uint4 q = __ldg(reinterpret_cast<const uint4*>(p) + i);
+            u[4 * i] = q.x, u[4 * i + 1] = q.y, u[4 * i + 2] = q.z, u[4 * i + 3] = q.w;
+        }
+    }
+}
+
+// Four codes of a row of 8 bits as two registers of T pairs: exact in both types.
+template <typename T> __device__ __forceinline__ void values4(uint32_t w, int int8, uint32_t& lo, uint32_t& hi)
+{
+    __half2 a, b;
+    if (int8) {
+        __half2 q[2];
+        q8_word_to_h2(w ^ 0x80808080u, q);
+        a = q[0], b = q[1];
+    } else {
+        uint32_t x, y;
+        asm("{\n\t.reg .b16 p, q;\n\tmov.b32 {p, q}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, p;\n\tcvt.rn.f16x2.e4m3x2 %1, q;\n\t}" : "=r"(x), "=r"(y) : "r"(w));
+        a = as_h2(x), b = as_h2(y);
+    }
+    if constexpr (std::is_same<T, __half>::value) {
+        lo = as_u32(a), hi = as_u32(b);
+    } else {
+        const float2 f = __half22float2(a), g = __half22float2(b);
+        lo = Dt<T>::down2(f.x, f.y), hi = Dt<T>::down2(g.x, g.y);
+    }
+}
+// A lane's eight elements of x as loaded: 16-bit pairs, or eight codes.
+template <typename T, bool X8, bool VEC> struct XPiece {
+    uint32_t u[X8 ? 2 : 4];
+    __device__ __forceinline__ void load(const void* row, int64_t k, int left)                // row: null reads as zero
+    {
+        if (!row) left = 0;
+        if constexpr (!X8) {
+            load8<T, VEC>((const T*)row + k, left, u);
+        } else if (VEC) {
+            const uint2 q = left > 0 ? __ldg(reinterpret_cast<const uint2*>((const uint8_t*)row + k)) : make_uint2(0u, 0u);
+            u[0] = q.x, u[1] = q.y;
+        } else {
+            const uint8_t* s = (const uint8_t*)row + k;
+            u[0] = u[1] = 0u;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < left) u[i >> 2] |= (uint32_t)__ldg(s + i) << (8 * (i & 3));
+        }
+    }
+    __device__ __forceinline__ void pairs(int int8, uint32_t (&v)[4]) const
+    {
+        if constexpr (X8) {
+            values4<T>(u[0], int8, v[0], v[1]);
+            values4<T>(u[1], int8, v[2], v[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = u[i];
+        }
+    }
+};
+
+// ------------------------------------------------------------------ the narrowing product
+
+// acc += rows . w1 over the chunks c0, c0 + step, ... < c1 of 32 elements, for MW tiles of 16 rows.  Lane (g, t) = (lane / 4, lane % 4) holds elements 8 t .. 8 t + 7 of
+// a chunk for rows g and g + 8 of each tile: two k-steps of the MMA.
+//   LAY 0: w1 [R, K], column c of accumulator tile i = rank 8 i + c;  LAY 1: w1 [K, R], rank c (R / 8) + i
+// row[m][h]: row g + 8 h of tile m, or null.
+template <typename T, bool X8, int R, int LAY, bool VEC, int MW>
+__device__ __forceinline__ void narrow(float (&acc)[MW][R / 8][4], const void* const (&row)[MW][2], const T* __restrict__ w1, int K, int int8, int c0, int c1, int step,
+                                       int lane)
+{
+    constexpr int R8 = R / 8;
+    constexpr int U = MW == 1 ? 4 : 2;                     // chunks in flight
+    const int g = lane >> 2, t = lane & 3;
+    for (int c = c0; c < c1; c += step * U) {
+        XPiece<T, X8, VEC> x[U][MW][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = (c + u * step) * 32 + 8 * t;
+            const int left = c + u * step < c1 ? K - k : 0;
+#pragma unroll
+            for (int m = 0; m < MW; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) x[u][m][h].load(row[m][h], k, left);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int k = (c + u * step) * 32 + 8 * t;
+            const int left = c + u * step < c1 ? K - k : 0;
+            uint32_t a[MW][2][4];
+#pragma unroll
+            for (int m = 0; m < MW; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) x[u][m][h].pairs(int8, a[m][h]);
+            if constexpr (LAY == 0) {
+#pragma unroll
+                for (int i = 0; i < R8; ++i) {
+                    uint32_t w[4];
+                    load8<T, VEC>(w1 + (int64_t)(8 * i + g) * K + k, left, w);
+#pragma unroll
+                    for (int m = 0; m < MW; ++m)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t f[4] = {a[m][0][2 * j], a[m][1][2 * j], a[m][0][2 * j + 1], a[m][1][2 * j + 1]};
+                            mma16<T>(acc[m][i], f, w[2 * j], w[2 * j + 1]);
+                        }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t w[4][(R8 + 1) / 2];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) load_r<T, R8, VEC>(w1 + (int64_t)(k + 4 * j + q) * R + g * R8, 4 * j + q < left, w[q]);
+#pragma unroll
+                    for (int i = 0; i < R8; ++i) {
+                        const uint32_t b0 = pair_of(w[0][i >> 1], w[1][i >> 1], i & 1), b1 = pair_of(w[2][i >> 1], w[3][i >> 1], i & 1);
+#pragma unroll
+                        for (int m = 0; m < MW; ++m) {
+                            const uint32_t f[4] = {a[m][0][2 * j], a[m][1][2 * j], a[m][0][2 * j + 1], a[m][1][2 * j + 1]};
+                            mma16<T>(acc[m][i], f, b0, b1);
+                        }
+                    }
+                }
+            }
+        }
+    }
+}
+// The accumulators of one tile into shared memory [16][R].
+template <int R, int LAY> __device__ __forceinline__ void put_narrow(const float (&acc)[R / 8][4], float* out, int lane)
+{
+    const int g = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int i = 0; i < R / 8; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            const int j = LAY == 0 ? 8 * i + 2 * t + c : (2 * t + c) * (R / 8) + i;
+            out[g * R + j] = acc[i][c];
+            out[(g + 8) * R + j] = acc[i][2 + c];
+        }
+}
+
+// ------------------------------------------------------------------ the widening product
+
+// Rows of u = scale * s as two 16-bit parts in shared memory, for the fragments below: [rows][R] each, rows padded by 16 bytes.
+template <int R> constexpr int u_pitch = 2 * R + 16;
+
+// One row's share of four ranks j .. j + 3 (R / 4 neighbouring lanes hold a row): parts into shared memory, the row's factor into `back`.
+// fp16: the row is scaled by a power of two so that its largest element lies in [1, 2).  bf16 has fp32's range.
+template <typename T, int R> __device__ __forceinline__ void put_u(const float (&v)[4], uint8_t* hi, uint8_t* lo, float* back, int row, int j)
+{
+    float f[4] = {v[0], v[1], v[2], v[3]};
+    if constexpr (std::is_same<T, __half>::value) {
+        float m = fmaxf(fmaxf(fabsf(f[0]), fabsf(f[1])), fmaxf(fabsf(f[2]), fabsf(f[3])));
+#pragma unroll
+        for (int o = 1; o < R / 4; o <<= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, o));
+        const int e = min(max((int)(__float_as_uint(m) >> 23), 2), 252);                      // biased exponent, so that both factors are ordinary numbers
+        const float down = __uint_as_float((uint32_t)(254 - e) << 23);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] *= down;
+        if (j == 0) back[row] = __uint_as_float((uint32_t)e << 23);
+    } else if (j == 0) {
+        back[row] = 1.0f;
+    }
+    uint2 h, l;
+    split2<T>(f[0], f[1], h.x, l.x);
+    split2<T>(f[2], f[3], h.y, l.y);
+    *reinterpret_cast<uint2*>(hi + row * u_pitch<R> + 2 * j) = h;
+    *reinterpret_cast<uint2*>(lo + row * u_pitch<R> + 2 * j) = l;
+}
+
+// Fragments of u for k-step ks (16 ranks) of tile m.  LAY 0: lane t holds ranks 4 t .. 4 t + 3 of the step (R >= 32: of 8 t .. 8 t + 7 of two steps, the first four in the
+// even one); LAY 1: ranks 2 t, 2 t + 1 and 2 t + 8, 2 t + 9.  R = 8: the missing ranks are zero.
+template <int R, int LAY> __device__ __forceinline__ void get_u(const uint8_t* part, int m, int ks, int lane, uint32_t (&a)[4])
+{
+    const int g = lane >> 2, t = lane & 3;
+    const uint8_t* r0 = part + (m * 16 + g) * u_pitch<R>;
+    const uint8_t* r1 = r0 + 8 * u_pitch<R>;
+    if constexpr (LAY == 0) {
+        int at = 16 * ks + 4 * t;
+        if (R >= 32) at = 32 * (ks >> 1) + 8 * t + 4 * (ks & 1);
+        if (R == 8) {
+            const bool in = t < 2;
+            const uint2 p = in ? *reinterpret_cast<const uint2*>(r0 + 2 * at) : make_uint2(0u, 0u);
+            const uint2 q = in ? *reinterpret_cast<const uint2*>(r1 + 2 * at) : make_uint2(0u, 0u);
+            a[0] = p.x, a[2] = p.y, a[1] = q.x, a[3] = q.y;
+        } else {
+            const uint2 p = *reinterpret_cast<const uint2*>(r0 + 2 * at), q = *reinterpret_cast<const uint2*>(r1 + 2 * at);
+            a[0] = p.x, a[2] = p.y, a[1] = q.x, a[3] = q.y;
+        }
+    } else {
+        a[0] = *reinterpret_cast<const uint32_t*>(r0 + 2 * (16 * ks + 2 * t));
+        a[1] = *reinterpret_cast<const uint32_t*>(r1 + 2 * (16 * ks + 2 * t));
+        a[2] = R == 8 ? 0u : *reinterpret_cast<const uint32_t*>(r0 + 2 * (16 * ks + 2 * t + 8));
+        a[3] = R == 8 ? 0u : *reinterpret_cast<const uint32_t*>(r1 + 2 * (16 * ks + 2 * t + 8));
+    }
+}
+
+// Column groups of the widening product: 32 (LAY 0) or 64 (LAY 1) columns.  A lane ends up with OWN consecutive columns of a row, from OWN t on.
+//   LAY 0: w2 [N, R]; column c of tile i (of 4) = 8 (c / 2) + 2 i + c % 2;   LAY 1: w2 [R, N]; column c of tile i (of 8) = 8 c + i
+template <int LAY> struct Wide {
+    static constexpr int cols = LAY == 0 ? 32 : 64;
+    static constexpr int tiles = LAY == 0 ? 4 : 8;
+    static constexpr int own = cols / 4;
+};
+
+template <typename T, int R, int LAY, bool VEC> struct WideWeights {
+    static constexpr int steps = R < 16 ? 1 : R / 16;
+    uint32_t b[steps][Wide<LAY>::tiles][2];
+    // column group from column n0; w2 of the adapter, N columns
+    __device__ __forceinline__ void load(const T* __restrict__ w2, int n0, int N, int lane, int s0 = 0, int s1 = steps)
+    {
+        const int g = lane >> 2, t = lane & 3;
+        if constexpr (LAY == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int n = n0 + 8 * (g >> 1) + 2 * i + (g & 1);
+                const T* p = w2 + (int64_t)n * R;
+                const bool there = n < N;
+                if constexpr (R >= 32) {
+#pragma unroll
+                    for (int q = 0; q < R / 32; ++q) {
+                        uint32_t u[4];
+                        load8<T, VEC>(p + 32 * q + 8 * t, there ? 8 : 0, u);
+                        b[2 * q][i][0] = u[0], b[2 * q][i][1] = u[1];
+                        b[2 * q + 1][i][0] = u[2], b[2 * q + 1][i][1] = u[3];
+                    }
+                } else {
+                    uint32_t u[2];
+                    load_r<T, 4, VEC>(p + 4 * t, there && (R == 16 || t < 2), u);
+                    b[0][i][0] = u[0], b[0][i][1] = u[1];
+                }
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < steps; ++s) {
+                uint32_t u[4][4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int j = 16 * s + 2 * t + (q & 1) + 8 * (q >> 1);
+                    const int left = j < R ? N - (n0 + 8 * g) : 0;
+                    load8<T, VEC>(w2 + (int64_t)j * N + n0 + 8 * g, left, u[q]);
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    b[s][i][0] = pair_of(u[0][i >> 1], u[1][i >> 1], i & 1);
+                    b[s][i][1] = pair_of(u[2][i >> 1], u[3][i >> 1], i & 1);
+                }
+            }
+        }
+    }
+};
+
+// A lane's share of two rows (g, g + 8) of y0 as loaded.
+template <typename T, int LAY, bool VEC> struct YPiece {
+    static constexpr int regs = Wide<LAY>::own / 2;
+    uint32_t u[2][regs];
+    __device__ __forceinline__ void load(const T* y0, int64_t ld, const int (&row)[2], int n, int N)           // n: first column of the lane
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < regs; i += 4) {
+                uint32_t v[4];
+                load8<T, VEC, false>(y0 + row[h] * ld + n + 2 * i, y0 && row[h] >= 0 ? N - (n + 2 * i) : 0, v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) u[h][i + k] = v[k];
+            }
+    }
+};
+template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int left, const uint32_t (&u)[4])
+{
+    if (VEC) {
+        if (left > 0) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+    } else {
+        unsigned short* s = reinterpret_cast<unsigned short*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) s[i] = (unsigned short)(u[i >> 1] >> (16 * (i & 1)));
+    }
+}
+
+// y = rn(y0 + back * (u . w2)) for the 16 rows of tile m and one column group.
+template <typename T, int R, int LAY, bool VEC>
+__device__ __forceinline__ void widen(const WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
+                                      T* y, int64_t ld, const int (&row)[2], int n, int N, int lane)
+{
+    constexpr int tiles = Wide<LAY>::tiles, steps = WideWeights<T, R, LAY, VEC>::steps;
+    float acc[tiles][4];
+#pragma unroll
+    for (int i = 0; i < tiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < steps; ++s) {
+        uint32_t a[4];
+        get_u<R, LAY>(lo, m, s, lane, a);
+#pragma unroll
+        for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, w.b[s][i][0], w.b[s][i][1]);
+        get_u<R, LAY>(hi, m, s, lane, a);
+#pragma unroll
+        for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, w.b[s][i][0], w.b[s][i][1]);
+    }
+    const int g = lane >> 2;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float f = back[m * 16 + g + 8 * h];
+        if (row[h] < 0) continue;
+#pragma unroll
+        for (int i = 0; i < YPiece<T, LAY, VEC>::regs; i += 4) {
+            uint32_t o[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 b = Dt<T>::up2(y0.u[h][i + k]);
+                // columns 2 (i + k), 2 (i + k) + 1 of the lane's share
+                float c0, c1;
+                if constexpr (LAY == 0) c0 = acc[k][2 * h], c1 = acc[k][2 * h + 1];
+                else c0 = acc[2 * k][2 * h + (i >> 2)], c1 = acc[2 * k + 1][2 * h + (i >> 2)];
+                o[k] = Dt<T>::down2(fmaf(f, c0, b.x), fmaf(f, c1, b.y));
+            }
+            store8<T, VEC>(y + row[h] * ld + n + 2 * i, N - (n + 2 * i), o);
+        }
+    }
+}
+
+// ------------------------------------------------------------------ kernels
+
+struct LoraP {
+    const void* x;
+    int64_t ldx;
+    const float* x_scale;                                  // of rows of 8 bits, null: x has type T
+    int int8;
+    const int *idx, *order, *offsets, *units;
+    int T, n, K, N;
+    const void *w1, *w2;
+    const float* scale;                                    // [n] or null
+    const void* y0;                                        // null: zeros
+    int64_t ldy0;
+    void* y;
+    int64_t ldy;
+    float* s;                                              // [T, R]
+    int s_scaled;                                          // what s keeps: 0 the narrowing product, 1 that times scale
+    int rest;                                              // rows without an adapter get y0 (0: they have it already)
+};
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_size()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ float4 remote4(const float* p, int rank)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(there) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ float remote1(const float* p, int rank)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    return v;
+}
+
+// Part `rank` of `size` of n things: [first, last).
+__device__ __forceinline__ void share_of(int n, int rank, int size, int& first, int& last)
+{
+    first = (int)((int64_t)n * rank / size);
+    last = (int)((int64_t)n * (rank + 1) / size);
+}
+
+// Copies columns [n0, n1) of a row of y0 (null: zeros) to y, by one warp.
+template <typename T, bool VEC> __device__ __forceinline__ void copy_row(const LoraP& p, int row, int n0, int n1, int lane)
+{
+    for (int n = n0 + 8 * lane; n < n1; n += 256) {
+        uint32_t u[4];
+        load8<T, VEC, false>((const T*)p.y0 + row * p.ldy0 + n, p.y0 ? n1 - n : 0, u);
+        store8<T, VEC>((T*)p.y + row * p.ldy + n, n1 - n, u);
+    }
+}
+
+// Both products of up to 16 rows of one adapter by a cluster of blocks: each takes a share of K, the shares' sums meet through distributed shared memory, and each takes
+// a share of N.  One launch: for a decode step two would cost as much as all their work.  Cluster b is there for row b: it does something if row b is
+// the first, 17th, ... of its adapter's rows, and then takes 16 of them.
+template <typename T, bool X8, int R, int LAY, bool VEC>
+__global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* part = reinterpret_cast<float*>(smem);          // [kWarps][16][R]
+    float* sum = part + kWarps * 16 * R;                   // [16][R]: this block's share
+    uint8_t* hi = reinterpret_cast<uint8_t*>(sum + 16 * R);
+    uint8_t* lo = hi + 16 * u_pitch<R>;
+    __shared__ float back[16];
+    __shared__ int rows[16], before[kWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster_rank(), size = (int)cluster_size();
+    const int b = blockIdx.x / size;
+    int n0, n1;
+    constexpr int G = Wide<LAY>::cols;
+    share_of((p.N + G - 1) / G, rank, size, n0, n1);
+    if (!p.y) n1 = n0;                                     // s alone is wanted
+    const int a = __ldg(p.idx + b), other = tid < p.T ? __ldg(p.idx + tid) : -1;
+    if (a < 0 || a >= p.n) {                               // (the whole cluster)
+        if (p.rest)
+            for (int c = n0 + warp; c < n1; c += kWarps) copy_row<T, VEC>(p, b, c * G, min(c * G + G, p.N), lane);
+        return;
+    }
+    // this row's place among its adapter's rows
+    const unsigned same = __ballot_sync(0xFFFFFFFFu, other == a);
+    if (tid < 16) rows[tid] = -1;
+    if (lane == 0) before[warp] = __popc(same);
+    __syncthreads();
+    int mine = __popc(same & ((1u << lane) - 1u)), first = 0;
+#pragma unroll
+    for (int w = 0; w < kWarps; ++w) {
+        if (w < warp) mine += before[w];
+        if (w < (b >> 5)) first += before[w];
+    }
+    // rows of warp b / 32 before row b
+    __shared__ unsigned mask;
+    if (warp == (b >> 5) && lane == 0) mask = same;
+    __syncthreads();
+    first += __popc(mask & ((1u << (b & 31)) - 1u));
+    if (first & 15) return;                                // (the whole cluster)
+    if (other == a && mine >= first && mine < first + 16) rows[mine - first] = tid;
+    __syncthreads();
+
+    const int g = lane >> 2, t = lane & 3;
+    const int row[2] = {rows[g], rows[g + 8]};
+    const T* w1 = (const T*)p.w1 + (int64_t)a * R * p.K;
+    const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
+    int c0, c1;
+    share_of((p.K + 31) / 32, rank, size, c0, c1);
+    const char* xb = (const char*)p.x;
+    const int xs = X8 ? 1 : 2;
+    const void* const xr[1][2] = {{row[0] >= 0 ? xb + row[0] * p.ldx * xs : nullptr, row[1] >= 0 ? xb + row[1] * p.ldx * xs : nullptr}};
+    float acc[1][R / 8][4];
+#pragma unroll
+    for (int i = 0; i < R / 8; ++i) acc[0][i][0] = acc[0][i][1] = acc[0][i][2] = acc[0][i][3] = 0.0f;
+    narrow<T, X8, R, LAY, VEC, 1>(acc, xr, w1, p.K, p.int8, c0 + warp, c1, kWarps, lane);
+    // the first column group is on its way while the shares meet
+    WideWeights<T, R, LAY, VEC> w;
+    YPiece<T, LAY, VEC> y0;
+    const int own = Wide<LAY>::own * t;
+    int c = n0 + warp;
+    if (c < n1) {
+        if (R <= 32) w.load(w2, c * G, p.N, lane);
+        y0.load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
+    }
+    put_narrow<R, LAY>(acc[0], part + warp * 16 * R, lane);
+    __syncthreads();
+    for (int i = tid; i < 16 * R / 4; i += kThreads) {
+        float4 v = reinterpret_cast<float4*>(part)[i];
+#pragma unroll
+        for (int k = 1; k < kWarps; ++k) {
+            const float4 q = reinterpret_cast<float4*>(part + k * 16 * R)[i];
+            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        }
+        reinterpret_cast<float4*>(sum)[i] = v;
+    }
+    cluster_arrive();
+    cluster_wait();
+    const float sc = p.scale ? __ldg(p.scale + a) : 1.0f;
+    constexpr int rounds = 16 * R / 4 < kThreads ? 1 : 16 * R / 4 / kThreads;
+#pragma unroll
+    for (int q = 0; q < rounds; ++q) {
+        const int i = tid + q * kThreads;
+        if (16 * R / 4 >= kThreads || warp < (16 * R / 4 + 31) / 32) {        // whole warps: put_u shuffles
+            float4 v = remote4(sum + 4 * i, 0);
+            for (int k = 1; k < size; ++k) {
+                const float4 r = remote4(sum + 4 * i, k);
+                v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
+            }
+            const int m = 4 * i / R, j = 4 * i % R, to = rows[m];
+            float f[4] = {v.x, v.y, v.z, v.w};
+            if (X8 && to >= 0) {
+                const float xsc = __ldg(p.x_scale + to);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] *= xsc;
+            }
+            const float4 raw = make_float4(f[0], f[1], f[2], f[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] *= sc;
+            if (p.s && to >= 0 && rank == 0)
+                *reinterpret_cast<float4*>(p.s + (int64_t)to * R + j) = p.s_scaled ? make_float4(f[0], f[1], f[2], f[3]) : raw;
+            put_u<T, R>(f, hi, lo, back, m, j);
+        }
+    }
+    cluster_arrive();                                      // this block has read the others' shares
+    __syncthreads();
+    while (c < n1) {
+        if (R > 32) w.load(w2, c * G, p.N, lane);
+        widen<T, R, LAY, VEC>(w, y0, hi, lo, back, 0, (T*)p.y, p.ldy, row, c * G + own, p.N, lane);
+        c += kWarps;
+        if (c < n1) {
+            if (R <= 32) w.load(w2, c * G, p.N, lane);
+            y0.load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
+        }
+    }
+    cluster_wait();                                        // nobody reads this block's share any more
+}
+
+// Which adapter a tile belongs to: the last a with starts[a] <= v, of n + 1 ascending numbers, by a warp.
+__device__ __forceinline__ int find_part(const int* __restrict__ starts, int n, int v, int lane)
+{
+    // 32 samples, then the 32 (at most 33) numbers from the last sample that is not above v
+    const int stride = (n + 32) / 32;
+    const int at = min(lane * stride, n);
+    const unsigned below = __ballot_sync(0xFFFFFFFFu, __ldg(starts + at) <= v);
+    const int from = (31 - __clz(below | 1u)) * stride;
+    int found = from;
+    for (int o = 0; o < stride; o += 32) {
+        const int i = from + o + lane;
+        const unsigned m = __ballot_sync(0xFFFFFFFFu, i < n && o + lane < stride && __ldg(starts + min(i, n)) <= v);
+        if (m) found = from + o + 31 - __clz(m);
+    }
+    return found;
+}
+
+// Rows of tile `tile` (64 of a unit of 128 of the sort): adapter, first sorted row, number of rows; false if there are none.
+__device__ __forceinline__ bool tile_rows(const LoraP& p, int tile, int lane, int& a, int& first, int& count)
+{
+    a = find_part(p.units, p.n, tile >> 1, lane);
+    first = __ldg(p.offsets + a) + 128 * ((tile >> 1) - __ldg(p.units + a)) + kTileRows * (tile & 1);
+    const int end = min(__ldg(p.offsets + a + 1), p.T);
+    count = min(end - first, kTileRows);
+    return count > 0;
+}
+
+// The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
+// Bound by HBM (x once); w1 comes from L1 and L2.
+template <typename T, bool X8, int R, int LAY, bool VEC>
+__global__ void __launch_bounds__(kThreads, 2) lora_narrow_kernel(const LoraP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr int MW = R <= 64 ? 2 : 1;                    // row tiles of a warp
+    constexpr int RG = kTileRows / 16 / MW, KP = kWarps / RG;                  // row groups x shares of the block's K
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* part = reinterpret_cast<float*>(smem);          // [KP][64][R]; share 0 holds the block's sum in the end
+    __shared__ int rows[kTileRows];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int rank = (int)cluster_rank(), size = (int)cluster_size();
+    int a, first, count;
+    if (blockIdx.x / size >= 2 * __ldg(p.units + p.n)) return;                // (the whole cluster)
+    if (!tile_rows(p, blockIdx.x / size, lane, a, first, count)) return;
+    if (tid < kTileRows) {
+        const int r = tid < count ? __ldg(p.order + first + tid) : -1;
+        rows[tid] = r >= 0 && r < p.T ? r : -1;
+    }
+    __syncthreads();
+    const int g = lane >> 2, rg = warp % RG, kp = warp / RG;
+    const char* xb = (const char*)p.x;
+    const void* xr[MW][2];
+#pragma unroll
+    for (int m = 0; m < MW; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int r = rows[(rg * MW + m) * 16 + g + 8 * h];
+            xr[m][h] = r >= 0 ? xb + r * p.ldx * (X8 ? 1 : 2) : nullptr;
+        }
+    int c0, c1;
+    share_of((p.K + 31) / 32, rank, size, c0, c1);
+    float acc[MW][R / 8][4];
+#pragma unroll
+    for (int m = 0; m < MW; ++m)
+#pragma unroll
+        for (int i = 0; i < R / 8; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
+    if ((rg * MW) * 16 < count)
+        narrow<T, X8, R, LAY, VEC, MW>(acc, *reinterpret_cast<const void* const(*)[MW][2]>(&xr), (const T*)p.w1 + (int64_t)a * R * p.K, p.K, p.int8, c0 + kp, c1, KP, lane);
+#pragma unroll
+    for (int m = 0; m < MW; ++m) put_narrow<R, LAY>(acc[m], part + (kp * kTileRows + (rg * MW + m) * 16) * R, lane);
+    __syncthreads();
+    for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
+        float4 v = reinterpret_cast<float4*>(part)[i];
+#pragma unroll
+        for (int k = 1; k < KP; ++k) {
+            const float4 q = reinterpret_cast<float4*>(part + k * kTileRows * R)[i];
+            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        }
+        reinterpret_cast<float4*>(part)[i] = v;
+    }
+    cluster_arrive();
+    cluster_wait();
+    const float sc = p.s_scaled && p.scale ? __ldg(p.scale + a) : 1.0f;
+    int i0, i1;
+    share_of(kTileRows * R / 4, rank, size, i0, i1);       // each block adds and stores its share of the tile's sums
+    for (int i = i0 + tid; i < i1; i += kThreads) {
+        const int to = rows[4 * i / R];
+        float4 v = remote4(part + 4 * i, 0);
+        for (int k = 1; k < size; ++k) {
+            const float4 r = remote4(part + 4 * i, k);
+            v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
+        }
+        if (to < 0) continue;
+        const float f = X8 ? __ldg(p.x_scale + to) : 1.0f;
+        if (X8) v.x *= f, v.y *= f, v.z *= f, v.w *= f;
+        if (p.s_scaled) v.x *= sc, v.y *= sc, v.z *= sc, v.w *= sc;
+        *reinterpret_cast<float4*>(p.s + (int64_t)to * R + 4 * i % R) = v;
+    }
+    cluster_arrive();                                      // (a block's shared memory stays until the others have read it)
+    cluster_wait();
+}
+
+// The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
+template <typename T, int R, int LAY, bool VEC>
+__global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ __align__(16) uint8_t hi[kTileRows * u_pitch<R>], lo[kTileRows * u_pitch<R>];
+    __shared__ float back[kTileRows];
+    __shared__ int rows[kTileRows];
+    constexpr int G = Wide<LAY>::cols;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int groups = (p.N + G - 1) / G;
+    if ((int)blockIdx.x >= tile_blocks) {                  // rows without an adapter among 64, the columns of a span
+        const int id = (int)blockIdx.x - tile_blocks, t0 = id / spans * kTileRows, n0 = (id - id / spans * spans) * per_span * G;
+        if (tid < kTileRows) {
+            const int e = t0 + tid < p.T ? __ldg(p.idx + t0 + tid) : 0;
+            rows[tid] = e < 0 || e >= p.n;
+        }
+        __syncthreads();
+        const int n1 = min(n0 + per_span * G, p.N);
+        for (int r = warp; r < kTileRows; r += kWarps)
+            if (rows[r]) copy_row<T, VEC>(p, t0 + r, n0, n1, lane);
+        return;
+    }
+    const int tile = blockIdx.x / spans, span = blockIdx.x - tile * spans;
+    int a, first, count;
+    if (tile >= 2 * __ldg(p.units + p.n)) return;
+    if (!tile_rows(p, tile, lane, a, first, count)) return;
+    if (tid < kTileRows) {
+        const int r = tid < count ? __ldg(p.order + first + tid) : -1;
+        rows[tid] = r >= 0 && r < p.T ? r : -1;
+    }
+    __syncthreads();
+    const float sc = !p.s_scaled && p.scale ? __ldg(p.scale + a) : 1.0f;
+    for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
+        const int m = 4 * i / R, j = 4 * i % R, from = rows[m];
+        const float4 v = from >= 0 ? *reinterpret_cast<const float4*>(p.s + (int64_t)from * R + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        const float f[4] = {v.x * sc, v.y * sc, v.z * sc, v.w * sc};
+        put_u<T, R>(f, hi, lo, back, m, j);
+    }
+    __syncthreads();
+    const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
+    const int g = lane >> 2, t = lane & 3, own = Wide<LAY>::own * t;
+    const int last = min((span + 1) * per_span, groups);
+    for (int c = span * per_span + warp; c < last; c += kWarps) {
+        WideWeights<T, R, LAY, VEC> w;
+        YPiece<T, LAY, VEC> y0[4];
+        int row[4][2];
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+            row[m][0] = rows[m * 16 + g], row[m][1] = rows[m * 16 + g + 8];
+            y0[m].load((const T*)p.y0, p.ldy0, row[m], c * G + own, p.N);
+        }
+        w.load(w2, c * G, p.N, lane);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+            if (m * 16 < count) widen<T, R, LAY, VEC>(w, y0[m], hi, lo, back, m, (T*)p.y, p.ldy, row[m], c * G + own, p.N, lane);
+    }
+}
+
+// ------------------------------------------------------------------ weight gradients
+
+struct WgradP {
+    const void* v;                                         // rows [T, ldv] of W elements: x for dA, dy for dB
+    int64_t ldv;
+    const float* v_scale;                                  // of rows of 8 bits
+    int int8;
+    const float* s;                                        // [T, R]: ds for dA, s for dB
+    const float* scale;                                    // [n] or null, applied to s
+    const int *order, *offsets;
+    int T, n, W;
+    float* out;                                            // [n, R, W] or, TRANS, [n, W, R]
+};
+
+// out[a] = sum over the adapter's rows of s (R) x v (W).  A cluster takes 64 columns of one adapter, its blocks and their warps share the rows, 16 at a time: lane (g, t)
+// loads columns 8 g .. 8 g + 7 of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9 (a whole 128-byte line per row), pairs of rows become the MMA's k, and its tile i has column 8 c + i
+// at place c.  The parts are added in a fixed order: warps, then blocks.
+//   bf16 products of three parts of s (all of its bits: with two, dA is off by 1.5e-6 beside an fp32 sum's 3e-7); fp16 rows: tf32 products of two parts, whose exponent
+//   holds any s (a gradient's 1e-7 is below fp16's normal numbers).
+template <typename T, bool X8, int R, bool TRANS, bool VEC>
+__global__ void __launch_bounds__(kThreads, R >= 64 ? 1 : 2) lora_wgrad_kernel(const WgradP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    constexpr bool TF32 = std::is_same<T, __half>::value && !X8;
+    using M = typename std::conditional<TF32, __half, __nv_bfloat16>::type;   // 16-bit type of the loaded pairs
+    constexpr int MT = R <= 32 ? 1 : 2;                    // tiles of 16 ranks per warp
+    constexpr int JG = R <= 16 ? 1 : R / (16 * MT);        // groups of ranks: warps that read the same rows (from L1)
+    constexpr int TG = kWarps / JG;                        // warps that share the rows
+    constexpr int RT = R < 16 ? 16 : R;
+    extern __shared__ __align__(16) uint8_t smem[];
+    float* part = reinterpret_cast<float*>(smem);          // [TG][RT][64]; share 0 holds the block's sum in the end
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int rank = (int)cluster_rank(), size = (int)cluster_size();
+    const int chunks = (p.W + 63) / 64;
+    const int64_t id = blockIdx.x / size;
+    const int a = (int)(id / chunks), col0 = (int)(id - (int64_t)a * chunks) * 64;
+    const int first = __ldg(p.offsets + a), end = min(__ldg(p.offsets + a + 1), p.T);
+    const int jg = warp % JG, tg = warp / JG;
+    const float sc = p.scale ? __ldg(p.scale + a) : 1.0f;
+    float acc[MT][8][4];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
+    // lane's ranks: 2 MT consecutive ones (R = 8: one); row c of tile m is rank of lane (c % 8), the (2 m + c / 8)-th
+    constexpr int JN = R == 8 ? 1 : 2 * MT;
+    const int j0 = R == 8 ? g : jg * 16 * MT + g * JN;
+    const int left = p.W - (col0 + 8 * g);
+    for (int r0 = first + 16 * (rank * TG + tg); r0 < end; r0 += 16 * size * TG) {
+        const int mine = r0 + (lane & 15) < end ? __ldg(p.order + r0 + (lane & 15)) : -1;
+        XPiece<M, X8, VEC> v[4];
+        float s[4][JN];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            int row = __shfl_sync(0xFFFFFFFFu, mine, 2 * t + (q & 1) + 8 * (q >> 1));
+            if (row >= p.T) row = -1;
+            v[q].load(row >= 0 ? (const char*)p.v + row * p.ldv * (X8 ? 1 : 2) : nullptr, col0 + 8 * g, left);
+            const float* sp = p.s + (int64_t)max(row, 0) * R + j0;
+            if constexpr (JN == 4) {
+                const float4 f = *reinterpret_cast<const float4*>(sp);
+                s[q][0] = f.x, s[q][1] = f.y, s[q][2] = f.z, s[q][3] = f.w;
+            } else if constexpr (JN == 2) {
+                const float2 f = *reinterpret_cast<const float2*>(sp);
+                s[q][0] = f.x, s[q][1] = f.y;
+            } else {
+                s[q][0] = *sp;
+            }
+            const float f = row < 0 ? 0.0f : X8 ? sc * __ldg(p.v_scale + row) : sc;
+#pragma unroll
+            for (int k = 0; k < JN; ++k) s[q][k] = row < 0 ? 0.0f : s[q][k] * f;
+        }
+        uint32_t x[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q].pairs(p.int8, x[q]);
+        if constexpr (TF32) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {                  // rows 2 t + 8 h and 2 t + 1 + 8 h: k = t and t + 4
+                uint32_t ah[MT][4], al[MT][4];
+#pragma unroll
+                for (int m = 0; m < MT; ++m)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {          // e: rank half (e & 1), row (e >> 1)
+                        const float f = R == 8 ? (e & 1 ? 0.0f : s[2 * h + (e >> 1)][0]) : s[2 * h + (e >> 1)][2 * m + (e & 1) < JN ? 2 * m + (e & 1) : 0];
+                        ah[m][e] = tf32(f);
+                        al[m][e] = tf32(f - __uint_as_float(ah[m][e]));
+                    }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float2 f0 = Dt<M>::up2(x[2 * h][i >> 1]), f1 = Dt<M>::up2(x[2 * h + 1][i >> 1]);
+                    const uint32_t b0 = __float_as_uint(i & 1 ? f0.y : f0.x), b1 = __float_as_uint(i & 1 ? f1.y : f1.x);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        mma8_tf32(acc[m][i], al[m], b0, b1);
+                        mma8_tf32(acc[m][i], ah[m], b0, b1);
+                    }
+                }
+            }
+        } else {
+            uint32_t ah[MT][4], am[MT][4], al[MT][4];
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {              // e: rank half (e & 1), rows 2 t + 8 (e >> 1) and the next
+                    const int k = R == 8 ? 0 : 2 * m + (e & 1) < JN ? 2 * m + (e & 1) : 0;
+                    if (R == 8 && (e & 1)) ah[m][e] = am[m][e] = al[m][e] = 0u;
+                    else split3(s[2 * (e >> 1)][k], s[2 * (e >> 1) + 1][k], ah[m][e], am[m][e], al[m][e]);
+                }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t b0 = pair_of(x[0][i >> 1], x[1][i >> 1], i & 1), b1 = pair_of(x[2][i >> 1], x[3][i >> 1], i & 1);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                    mma16<__nv_bfloat16>(acc[m][i], al[m], b0, b1);
+                    mma16<__nv_bfloat16>(acc[m][i], am[m], b0, b1);
+                    mma16<__nv_bfloat16>(acc[m][i], ah[m], b0, b1);
+                }
+            }
+        }
+    }
+    // parts into shared memory, [rank][column]
+    float* mypart = part + tg * RT * 64;
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {                      // rank half
+            if (R == 8 && e) continue;
+            const int j = R == 8 ? g : j0 + 2 * m + e;
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                const float4 lo4 = make_float4(acc[m][0][2 * e + c], acc[m][1][2 * e + c], acc[m][2][2 * e + c], acc[m][3][2 * e + c]);
+                const float4 hi4 = make_float4(acc[m][4][2 * e + c], acc[m][5][2 * e + c], acc[m][6][2 * e + c], acc[m][7][2 * e + c]);
+                float4* to = reinterpret_cast<float4*>(mypart + j * 64 + 8 * (2 * t + c));
+                to[0] = lo4;
+                to[1] = hi4;
+            }
+        }
+    __syncthreads();
+    for (int i = tid; i < R * 16; i += kThreads) {
+        float4 v = reinterpret_cast<float4*>(part)[i];
+#pragma unroll
+        for (int k = 1; k < TG; ++k) {
+            const float4 q = reinterpret_cast<float4*>(part + k * RT * 64)[i];
+            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        }
+        reinterpret_cast<float4*>(part)[i] = v;
+    }
+    if (size > 1) {
+        cluster_arrive();
+        cluster_wait();
+    } else {
+        __syncthreads();
+    }
+    int i0, i1;
+    share_of(R * 16, rank, size, i0, i1);                  // each block adds and stores its share of the sums
+    for (int i = i0 + tid; i < i1; i += kThreads) {
+        if constexpr (TRANS) {                             // four ranks of one column
+            const int c = i / (R / 4), j = 4 * (i % (R / 4));
+            float f[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) f[k] = size > 1 ? remote1(part + (j + k) * 64 + c, 0) : part[(j + k) * 64 + c];
+            for (int b = 1; b < size; ++b)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) f[k] += remote1(part + (j + k) * 64 + c, b);
+            if (col0 + c < p.W) *reinterpret_cast<float4*>(p.out + ((int64_t)a * p.W + col0 + c) * R + j) = make_float4(f[0], f[1], f[2], f[3]);
+        } else {                                           // four columns of one rank
+            float4 v = size > 1 ? remote4(part + 4 * i, 0) : reinterpret_cast<float4*>(part)[i];
+            for (int b = 1; b < size; ++b) {
+                const float4 r = remote4(part + 4 * i, b);
+                v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
+            }
+            const int j = i / 16, c = col0 + 4 * (i % 16);
+            float* out = p.out + ((int64_t)a * R + j) * p.W + c;
+            const float f[4] = {v.x, v.y, v.z, v.w};
+            if (VEC) {
+                if (c < p.W) *reinterpret_cast<float4*>(out) = v;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (c + k < p.W) out[k] = f[k];
+            }
+        }
+    }
+    if (size > 1) {
+        cluster_arrive();                                  // (a block's shared memory stays until the others have read it)
+        cluster_wait();
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+template <typename F> static qmm_status by_rank(int r, F f)
+{
+    switch (r) {
+    case 8: return f(std::integral_constant<int, 8>());
+    case 16: return f(std::integral_constant<int, 16>());
+    case 32: return f(std::integral_constant<int, 32>());
+    case 64: return f(std::integral_constant<int, 64>());
+    default: return f(std::integral_constant<int, 128>());
+    }
+}
+
+// Blocks of a cluster that share a length of `parts` pieces: a power of two up to `most`, each with at least one piece.
+static int cluster_for(int64_t parts, int most)
+{
+    int c = 1;
+    while (c < most && 2 * c <= parts) c *= 2;
+    return c;
+}
+
+// Tiles that any distribution of T rows over n adapters can need.
+static int64_t most_tiles(int64_t T, int64_t n)
+{
+    const int64_t used = T < n ? T : n;
+    return 2 * ((T + 127 * used) / 128);
+}
+
+template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const LoraP& p, int r, bool x8, cudaStream_t st)
+{
+    return by_rank(r, [&](auto rank) {
+        constexpr int R = decltype(rank)::value;
+        constexpr int G = Wide<LAY>::cols;
+        auto narrowed = [&](auto e8) {
+            constexpr bool X8 = decltype(e8)::value;
+            if (p.T <= kSmallRows) {
+                constexpr int smem = (kWarps + 1) * 16 * R * 4 + 2 * 16 * u_pitch<R>;
+                static std::atomic<uint64_t> configured{0};
+                auto kern = lora_small_kernel<T, X8, R, LAY, VEC>;
+                const qmm_status s = configure_once(configured, kern, smem, true, "adapter attributes");
+                if (s != QMM_OK) return s;
+                // a block for every 256 elements of K or N, eight at most; sixteen where that leaves most of the GPU idle
+                const int64_t pieces = (p.K > p.N ? p.K : p.N) / 256;
+                const int size = cluster_for(pieces, p.T <= 4 ? 16 : 8);
+                return launch_pdl(kern, dim3((unsigned)(p.T * size)), kThreads, smem, size, st, "adapter launch", p);
+            }
+            constexpr int MW = R <= 64 ? 2 : 1, KP = kWarps / (kTileRows / 16 / MW);
+            constexpr int smem = KP * kTileRows * R * 4;
+            static std::atomic<uint64_t> configured{0};
+            auto kern = lora_narrow_kernel<T, X8, R, LAY, VEC>;
+            const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
+            if (s != QMM_OK) return s;
+            const int64_t tiles = (p.T + kTileRows - 1) / kTileRows;
+            int size = 1;                                  // blocks that share a tile's K: two per SM in all, 256 elements each at least
+            while (size < 8 && tiles * size < 2 * kNumSMs && p.K / (2 * size) >= 256) size *= 2;
+            return launch_pdl(kern, dim3((unsigned)(most_tiles(p.T, p.n) * size)), kThreads, smem, size, st, "adapter narrowing launch", p);
+        };
+        qmm_status s;
+        if constexpr (LAY == 0) s = x8 ? narrowed(std::true_type()) : narrowed(std::false_type());
+        else s = narrowed(std::false_type());
+        if (s != QMM_OK || p.T <= kSmallRows || !p.y) return s;
+        const int groups = (p.N + G - 1) / G;
+        const int per_span = groups < 4 * kWarps ? ((groups + kWarps - 1) / kWarps) * kWarps : 4 * kWarps;
+        const int spans = (groups + per_span - 1) / per_span;
+        const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
+        if (blocks + rest > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapters: %lld blocks are too many for one launch", (long long)(blocks + rest));
+        return launch_pdl(lora_widen_kernel<T, R, LAY, VEC>, dim3((unsigned)(blocks + rest)), kThreads, 0, 1, st, "adapter widening launch", p, spans, per_span, (int)blocks);
+    });
+}
+
+template <typename T, bool TRANS, bool VEC> static qmm_status launch_wgrad(const WgradP& p, int r, bool x8, cudaStream_t st)
+{
+    return by_rank(r, [&](auto rank) {
+        constexpr int R = decltype(rank)::value;
+        auto go = [&](auto e8) {
+            constexpr bool X8 = decltype(e8)::value;
+            constexpr int MT = R <= 32 ? 1 : 2, JG = R <= 16 ? 1 : R / (16 * MT), TG = kWarps / JG, RT = R < 16 ? 16 : R;
+            constexpr int smem = TG * RT * 64 * 4;
+            static std::atomic<uint64_t> configured{0};
+            auto kern = lora_wgrad_kernel<T, X8, R, TRANS, VEC>;
+            const qmm_status s = configure_once(configured, kern, smem, false, "adapter gradient attributes");
+            if (s != QMM_OK) return s;
+            const int64_t columns = (int64_t)p.n * ((p.W + 63) / 64);
+            // blocks that share a column's rows: as many as have 128 rows each if one adapter had them all, while the launch stays a few waves
+            int size = 1;
+            while (size < 8 && columns * size < 8 * kNumSMs && (int64_t)p.T >= 256 * size) size *= 2;
+            if (columns * size > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapter gradients: %lld blocks are too many for one launch", (long long)(columns * size));
+            return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", p);
+        };
+        if constexpr (!TRANS)
+            return x8 ? go(std::true_type()) : go(std::false_type());
+        else
+            return go(std::false_type());
+    });
+}
+
+}  // namespace lora
+
+// forward: both products of x with (A, B); backward: of dy with (B, A)
+#define QMM_LORA_TYPE(NAME, TYPE)                                                                                                                          \
+    qmm_status launch_lora_##NAME(const lora::LoraP& p, int r, bool x8, bool back, bool vec, cudaStream_t st)                                              \
+    {                                                                                                                                                      \
+        if (back) return vec ? lora::launch_pair<TYPE, 1, true>(p, r, false, st) : lora::launch_pair<TYPE, 1, false>(p, r, false, st);                     \
+        return vec ? lora::launch_pair<TYPE, 0, true>(p, r, x8, st) : lora::launch_pair<TYPE, 0, false>(p, r, x8, st);                                     \
+    }
+#define QMM_LORA_WGRAD_TYPE(NAME, TYPE)                                                                                                                    \
+    qmm_status launch_lora_wgrad_##NAME(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st)                                      \
+    {                                                                                                                                                      \
+        if (trans) return vec ? lora::launch_wgrad<TYPE, true, true>(p, r, false, st) : lora::launch_wgrad<TYPE, true, false>(p, r, false, st);            \
+        return vec ? lora::launch_wgrad<TYPE, false, true>(p, r, x8, st) : lora::launch_wgrad<TYPE, false, false>(p, r, x8, st);                           \
+    }
+
+}  // namespace qmm

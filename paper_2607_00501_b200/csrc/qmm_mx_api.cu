@@ -1,6 +1,7 @@
 // qmm_mx_api.cu -- C ABI of the microscaled 4-bit operators and of the expert sort: argument checks and dispatch.
 // The same rules as in qmm_api.cu: everything is checked on the host before anything is enqueued, nothing
 // allocates, errors go through the thread-local buffer.
+#include "qmm_checks.cuh"
 #include "qmm_mx.cuh"
 
 namespace qmm {
@@ -41,25 +42,12 @@ qmm_status launch_expert_combine_grad(int dtype, const void* dy, int64_t lddy, c
 constexpr size_t kMxStatusBytes = 256;
 
 static bool mx_fmt_ok(int fmt) { return fmt == QMM_MXFP4 || fmt == QMM_NVFP4; }
-static bool dtype_ok(int dt) { return dt == QMM_F16 || dt == QMM_BF16 || dt == QMM_F32; }
-static int dtype_size(int dt) { return dt == QMM_F32 ? 4 : 2; }
 
 static qmm_status check_mx(const char* who, int fmt, int64_t rows, int64_t K)
 {
     if (!mx_fmt_ok(fmt)) return fail(QMM_ERR_INVALID_ARG, "%s: unknown microscaled format %d (expected 32 or 16)", who, fmt);
     if (rows < 0 || K <= 0) return fail(QMM_ERR_INVALID_ARG, "%s: rows=%lld is negative or K=%lld not positive", who, (long long)rows, (long long)K);
     if (rows > (1 << 24) || K > (1 << 20)) return fail(QMM_ERR_UNSUPPORTED, "%s: %lld rows > 2^24 or K=%lld > 2^20", who, (long long)rows, (long long)K);
-    return QMM_OK;
-}
-
-// A matrix of plain elements: type, row pitch, element alignment.
-static qmm_status check_rows(const char* who, const char* name, int dtype, const void* p, int64_t ld, int64_t width)
-{
-    if (!dtype_ok(dtype)) return fail(QMM_ERR_INVALID_ARG, "%s: unknown data type %d (expected 0, 1 or 2)", who, dtype);
-    if (!p) return fail(QMM_ERR_INVALID_ARG, "%s: %s is null", who, name);
-    if (ld < width) return fail(QMM_ERR_SHAPE, "%s: row pitch %lld of %s is below its width %lld", who, (long long)ld, name, (long long)width);
-    if (ld > (1LL << 40)) return fail(QMM_ERR_UNSUPPORTED, "%s: row pitch %lld of %s > 2^40", who, (long long)ld, name);
-    if (!aligned(p, (size_t)dtype_size(dtype))) return fail(QMM_ERR_ALIGNMENT, "%s: %s is not aligned to its element type", who, name);
     return QMM_OK;
 }
 
@@ -77,21 +65,6 @@ static qmm_status check_scale(const char* who, int fmt, const float* s)
     return QMM_OK;
 }
 
-static qmm_status check_ws(const char* who, const void* ws, size_t given, size_t need, size_t align)
-{
-    if (!ws || given < need) return fail(QMM_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, ws ? given : (size_t)0);
-    if (!aligned(ws, align)) return fail(QMM_ERR_ALIGNMENT, "%s: workspace must be %zu-byte aligned", who, align);
-    return QMM_OK;
-}
-
-static qmm_status check_pairs(const char* who, int32_t T, int32_t topk, int32_t E)
-{
-    if (T < 0 || topk <= 0 || E <= 0) return fail(QMM_ERR_INVALID_ARG, "%s: T=%d topk=%d E=%d out of range", who, T, topk, E);
-    if (E > 1024 || topk > 32) return fail(QMM_ERR_UNSUPPORTED, "%s: E=%d > 1024 or topk=%d > 32", who, E, topk);
-    if ((int64_t)T * topk > (1 << 22)) return fail(QMM_ERR_UNSUPPORTED, "%s: T*topk=%lld > 2^22", who, (long long)T * topk);
-    return QMM_OK;
-}
-
 // Operands of a dense product: M rows against N >= 1 weight rows.
 static qmm_status check_product(const char* who, int fmt, int64_t M, int64_t N, int64_t K)
 {
@@ -102,12 +75,6 @@ static qmm_status check_product(const char* who, int fmt, int64_t M, int64_t N, 
 }
 
 static size_t mx_bytes(int fmt, int64_t row_units, int64_t K) { return (size_t)row_units * (size_t)k_units(K) * (size_t)unit_bytes(fmt); }
-
-#define QMM_TRY(call)                    \
-    do {                                 \
-        const qmm_status s_ = (call);    \
-        if (s_ != QMM_OK) return s_;     \
-    } while (0)
 
 // Type of the experts' rows on their way to the weighted sum.  Rounding them to the output's 16 bits halves their traffic and adds half an ulp to each term of the
 // sum; which one it is is the caller's choice (128 experts x 768 x 2048, 8 per token, fp16: 2048 tokens 121 us, 153 with fp32 rows; 4 tokens 31.1, 31.4).

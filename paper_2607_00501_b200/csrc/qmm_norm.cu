@@ -1,0 +1,547 @@
+// qmm_norm.cu -- root-mean-square norm with the residual's addition, into rows of the input's type and / or rows of 8 bits with a scale
+// each, its gradient, and the 8-bit rows by themselves.
+//
+//   h = rn(x + residual);  rstd = (mean h^2 + eps)^-1/2;  y = h * rstd * w
+//   8 bits: t = fp32(h * w), amax = max |t|, code = rn8(fp32(t * fp32(L / amax))), scale = amax * rstd / L, L = 448 (e4m3) or 127 (int8)
+//
+// The codes are those of t, not of y: rstd is one factor of the whole row, so it cancels in t / amax, and a code does not depend on the order in
+// which the squares were added.  Every element is read once and written once: a row lives in the registers of its threads.
+#include "qmm_launch.cuh"
+#include "qmm_mx.cuh"
+
+#include <float.h>
+
+namespace qmm {
+
+using namespace mx;
+
+// V elements of a row as loaded.
+template <typename T, int V> struct Piece {
+    static constexpr int B = V * (int)sizeof(T);
+    static constexpr int W = B >= 4 ? B / 4 : 1;
+    uint32_t u[W];
+    __device__ __forceinline__ void load(const T* p)
+    {
+        if constexpr (B == 16) {
+            const uint4 q = *reinterpret_cast<const uint4*>(p);
+            u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
+        } else if constexpr (B == 4) {
+            u[0] = *reinterpret_cast<const uint32_t*>(p);
+        } else {
+            u[0] = *reinterpret_cast<const unsigned short*>(p);
+        }
+    }
+    __device__ __forceinline__ void store(T* p) const
+    {
+        if constexpr (B == 16) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        else if constexpr (B == 4) *reinterpret_cast<uint32_t*>(p) = u[0];
+        else *reinterpret_cast<unsigned short*>(p) = (unsigned short)u[0];
+    }
+    __device__ __forceinline__ void fill(uint32_t v)
+    {
+#pragma unroll
+        for (int i = 0; i < W; ++i) u[i] = v;
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(u[i]);
+        } else {
+            const float2 f = Dt<T>::up2(u[i >> 1]);
+            return i & 1 ? f.y : f.x;
+        }
+    }
+    __device__ __forceinline__ void set(const float (&f)[V])
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) u[i] = __float_as_uint(f[i]);
+        } else if constexpr (V == 1) {
+            u[0] = Dt<T>::down2(f[0], 0.0f);
+        } else {
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) u[i] = Dt<T>::down2(f[2 * i], f[2 * i + 1]);
+        }
+    }
+};
+
+// Sum of a and largest magnitude of b (a NaN stays) over the `threads` threads of a row; the same value, added in the same order, on each.  `red`: two floats per warp.
+__device__ __forceinline__ void row_reduce(float& a, float& b, int threads, int barrier, int tid, float* red)
+{
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        b = maxabs(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+    }
+    if (threads == 32) return;
+    const int warps = threads >> 5;
+    if ((tid & 31) == 0) {
+        red[2 * (tid >> 5)] = a;
+        red[2 * (tid >> 5) + 1] = b;
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");
+    const int at = (tid & 31) < warps ? tid & 31 : 0;
+    a = (tid & 31) < warps ? red[2 * at] : 0.0f;
+    b = red[2 * at + 1];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        b = maxabs(b, __shfl_xor_sync(0xFFFFFFFFu, b, o));
+    }
+    asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");      // red may be written again
+}
+
+// 1 / sqrt(mean + eps) of a sum of squares; 64 bits where the squares were scaled by f^2 = 2^-128 or 2^128 to stay in fp32's range.
+__device__ __forceinline__ float rstd_of(float ss, int K, float eps) { return 1.0f / sqrtf(ss / (float)K + eps); }
+__device__ __forceinline__ float rstd_scaled(float ss, int K, float eps, bool small)
+{
+    return (float)(1.0 / sqrt((double)ss / K * (small ? 0x1p-128 : 0x1p128) + (double)eps));
+}
+// Sums of squares outside this range have lost values to fp32's ends and are formed again with scaled elements.
+__device__ __forceinline__ bool off_range(float ss) { return !(ss < FLT_MAX) || ss < 0x1p-90f; }
+
+struct NormP {
+    int64_t rows, ldx, ldr, ldh, ldy, ldc;
+    int K, nv, tpr;                                        // nv: vectors per row; tpr: threads per row
+    const void *x, *res, *w;                               // w null: 1
+    void *h, *y;                                           // optional
+    uint8_t* codes;                                        // optional
+    float* scales;
+    int int8, norm;                                        // norm 0: rstd = 1
+    float eps;
+};
+
+__device__ __forceinline__ uint32_t code8(float a, int int8)
+{
+    if (int8) return (uint32_t)__float2int_rn(fminf(fmaxf(a, -127.0f), 127.0f)) & 0xFFu;
+    return (uint32_t)__nv_cvt_float_to_fp8(a, __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ uint32_t code8x2(float a, float b, int int8)
+{
+    if (int8) return code8(a, 1) | (code8(b, 1) << 8);
+    return (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+}
+
+// A row by p.tpr threads, NV vectors of V elements each; blocks of several rows where a row needs fewer than the block's threads.
+template <typename T, int V, int NV>
+__global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ float red[64];
+    const int tpr = p.tpr, group = threadIdx.x / tpr, tid = threadIdx.x - group * tpr;
+    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / tpr) + group;
+    if (row >= p.rows) return;                             // (a whole row group leaves: its barrier is its own)
+    const T* x = (const T*)p.x + row * p.ldx;
+    const T* res = p.res ? (const T*)p.res + row * p.ldr : nullptr;
+    Piece<T, V> h[NV], w[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        h[i].fill(0u);
+        w[i].fill(0u);
+        const int v = tid + i * tpr;
+        if (v < p.nv) h[i].load(x + v * V);
+    }
+    if (res) {
+        Piece<T, V> r[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            r[i].fill(0u);
+            const int v = tid + i * tpr;
+            if (v < p.nv) r[i].load(res + v * V);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            float f[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) f[k] = h[i].get(k) + r[i].get(k);
+            h[i].set(f);
+        }
+    }
+    if (p.w) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            if (v < p.nv) w[i].load((const T*)p.w + v * V);
+        }
+    } else {
+        float one[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) one[k] = 1.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) w[i].set(one);
+    }
+    if (p.h) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            if (v < p.nv) h[i].store((T*)p.h + row * p.ldh + v * V);
+        }
+    }
+    float ss = 0.0f, amax = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float f = h[i].get(k);
+            ss = fmaf(f, f, ss);
+            if (p.codes) amax = maxabs(amax, f * w[i].get(k));
+        }
+    row_reduce(ss, amax, tpr, 1 + group, tid, red + 2 * (group * (tpr >> 5)));
+    float rstd = 1.0f;
+    if (p.norm) {
+        rstd = rstd_of(ss, p.K, p.eps);
+        if (off_range(ss)) {                               // (the same on every thread of the row)
+            const bool small = ss < 1.0f;
+            const float f = small ? 0x1p64f : 0x1p-64f;
+            float again = 0.0f, none = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float e = h[i].get(k) * f;
+                    again = fmaf(e, e, again);
+                }
+            row_reduce(again, none, tpr, 1 + group, tid, red + 2 * (group * (tpr >> 5)));
+            rstd = rstd_scaled(again, p.K, p.eps, small);
+        }
+    }
+    if (p.y) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            float f[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) f[k] = h[i].get(k) * rstd * w[i].get(k);
+            Piece<T, V> o;
+            o.set(f);
+            if (v < p.nv) o.store((T*)p.y + row * p.ldy + v * V);
+        }
+    }
+    if (p.codes) {
+        const float top = p.int8 ? 127.0f : 448.0f;
+        const bool fine = amax < INFINITY, zero = amax < 0x1p-118f;         // (a NaN is neither)
+        const float inv = fine && !zero ? top / amax : 0.0f;
+        if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7FC00000) : zero ? 0.0f : amax / top * rstd;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            if (v >= p.nv) continue;
+            uint8_t* o = p.codes + row * p.ldc + v * V;
+            uint32_t c[V > 4 ? 2 : 1] = {};
+            if (fine && !zero) {
+                if constexpr (V == 1) c[0] = code8(h[i].get(0) * w[i].get(0) * inv, p.int8);
+                else {
+#pragma unroll
+                    for (int k = 0; k < V; k += 2)
+                        c[k >> 2] |= code8x2(h[i].get(k) * w[i].get(k) * inv, h[i].get(k + 1) * w[i].get(k + 1) * inv, p.int8) << (8 * (k & 2));
+                }
+            }
+            if constexpr (V == 8) *reinterpret_cast<uint2*>(o) = make_uint2(c[0], c[1]);
+            else if constexpr (V == 4) *reinterpret_cast<uint32_t*>(o) = c[0];
+            else *o = (uint8_t)c[0];
+        }
+    }
+}
+
+// ------------------------------------------------------------------ gradient
+//
+//   xhat = h * rstd;  dx = rstd * (w dy - xhat * mean(w dy xhat)) (+ dh);  dw = sum over rows of dy * xhat
+//
+// One pass over h and dy.  A block takes every gridDim-th row and keeps its part of dw in registers, which it writes once; the parts are added by a second launch in
+// block order: the same bits on every call.
+
+struct NormGradP {
+    int64_t rows, lddy, ldh, lddh, lddx;
+    int K, nv;
+    const void *dy, *h, *w, *dh;                           // w null: 1; dh optional
+    void* dx;                                              // optional
+    float* part;                                           // [gridDim, K], null: dw is not wanted
+    float eps;
+};
+
+template <typename T, int V, int NV>
+__global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(const NormGradP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ float red[2][64];
+    const int tpr = blockDim.x, tid = threadIdx.x;
+    Piece<T, V> w[NV];
+    float dw[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int v = tid + i * tpr;
+        float one[V];
+#pragma unroll
+        for (int k = 0; k < V; ++k) one[k] = 1.0f, dw[i][k] = 0.0f;
+        w[i].set(one);
+        if (p.w && v < p.nv) w[i].load((const T*)p.w + v * V);
+    }
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        Piece<T, V> h[NV], dy[NV], dh[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            h[i].fill(0u);
+            dy[i].fill(0u);
+            dh[i].fill(0u);
+            const int v = tid + i * tpr;
+            if (v < p.nv) {
+                h[i].load((const T*)p.h + row * p.ldh + v * V);
+                dy[i].load((const T*)p.dy + row * p.lddy + v * V);
+                if (p.dh) dh[i].load((const T*)p.dh + row * p.lddh + v * V);
+            }
+        }
+        float ss = 0.0f, dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float f = h[i].get(k);
+                ss = fmaf(f, f, ss);
+                dot = fmaf(w[i].get(k) * dy[i].get(k), f, dot);
+            }
+        auto reduce2 = [&](float& a, float& b) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+                b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+            }
+            if (tpr == 32) return;
+            __syncthreads();                               // the sums of the row before have been read
+            if ((tid & 31) == 0) red[0][tid >> 5] = a, red[1][tid >> 5] = b;
+            __syncthreads();
+            const bool mine = (tid & 31) < (tpr >> 5);
+            a = mine ? red[0][tid & 31] : 0.0f;
+            b = mine ? red[1][tid & 31] : 0.0f;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+                b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+            }
+        };
+        reduce2(ss, dot);
+        float rstd = rstd_of(ss, p.K, p.eps), c = rstd * (rstd * dot / (float)p.K);        // rstd * mean(w dy xhat)
+        if (off_range(ss)) {                               // (the same on every thread)
+            const bool small = ss < 1.0f;
+            const float f = small ? 0x1p64f : 0x1p-64f;
+            float again = 0.0f, dot2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float e = h[i].get(k) * f;
+                    again = fmaf(e, e, again);
+                    dot2 = fmaf(w[i].get(k) * dy[i].get(k), e, dot2);
+                }
+            reduce2(again, dot2);
+            rstd = rstd_scaled(again, p.K, p.eps, small);
+            c = rstd * (rstd / f * dot2 / (float)p.K);
+        }
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            float f[V];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float xhat = h[i].get(k) * rstd;
+                f[k] = fmaf(rstd, w[i].get(k) * dy[i].get(k), fmaf(-c, xhat, dh[i].get(k)));
+                dw[i][k] = fmaf(dy[i].get(k), xhat, dw[i][k]);
+            }
+            Piece<T, V> o;
+            o.set(f);
+            if (p.dx && v < p.nv) o.store((T*)p.dx + row * p.lddx + v * V);
+        }
+    }
+    if (p.part) {
+        float* part = p.part + (int64_t)blockIdx.x * p.K;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int v = tid + i * tpr;
+            if (v >= p.nv) continue;
+            if constexpr (V >= 4) {
+#pragma unroll
+                for (int k = 0; k < V; k += 4) *reinterpret_cast<float4*>(part + v * V + k) = make_float4(dw[i][k], dw[i][k + 1], dw[i][k + 2], dw[i][k + 3]);
+            } else {
+                part[v] = dw[i][0];
+            }
+        }
+    }
+}
+
+constexpr int kColThreads = 256;                           // 32 columns x 8 shares of the parts
+__global__ void __launch_bounds__(kColThreads) rms_norm_dw_kernel(const float* __restrict__ part, int parts, int K, float* __restrict__ dw)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    __shared__ float red[8][32];
+    const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
+    float s = 0.0f;
+    if (k < K) {
+#pragma unroll 8
+        for (int i = share; i < parts; i += 8) s += part[(int64_t)i * K + k];
+    }
+    red[share][lane] = s;
+    __syncthreads();
+    if (share == 0 && k < K) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += red[i][lane];
+        dw[k] = sum;
+    }
+}
+
+// ------------------------------------------------------- 8-bit rows back to values
+
+// Thread = V codes of a row.
+template <typename T, int V>
+__global__ void __launch_bounds__(256) rows8_dequantize_kernel(const uint8_t* __restrict__ codes, int64_t ldc, const float* __restrict__ scales, int int8, int64_t rows, int nv,
+                                                               T* __restrict__ out, int64_t ldo)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = id / nv;
+    if (row >= rows) return;
+    const int64_t k = (id - row * nv) * V;
+    const uint8_t* c = codes + row * ldc + k;
+    uint32_t u[V >= 4 ? V / 4 : 1];
+    if constexpr (V == 16) {
+        const uint4 q = __ldg(reinterpret_cast<const uint4*>(c));
+        u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
+    } else if constexpr (V == 8) {
+        const uint2 q = __ldg(reinterpret_cast<const uint2*>(c));
+        u[0] = q.x, u[1] = q.y;
+    } else {
+        u[0] = __ldg(c);
+    }
+    const float s = __ldg(scales + row);
+    float f[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const uint32_t b = u[i >> 2] >> (8 * (i & 3)) & 0xFFu;
+        f[i] = s * (int8 ? (float)(int8_t)b : __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)b, __NV_E4M3))));
+    }
+    constexpr int S = V * (int)sizeof(T) >= 16 ? 16 / (int)sizeof(T) : V;     // elements per store
+#pragma unroll
+    for (int i = 0; i < V; i += S) {
+        Piece<T, S> o;
+        float g[S];
+#pragma unroll
+        for (int j = 0; j < S; ++j) g[j] = f[i + j];
+        o.set(g);
+        o.store(out + row * ldo + k + i);
+    }
+}
+
+// ------------------------------------------------------------------ launches
+
+static uintptr_t norm_bits(const void* p, int64_t ld, int size) { return p ? reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size) : 0; }
+
+// Threads per row and vectors per thread of a row of nv vectors.  Many rows: four vectors a thread keep more bytes in flight per warp and meet in fewer barriers;
+// few rows (less than a warp per scheduler): one vector a thread, for latency.
+struct NormShape {
+    int tpr, per;
+};
+static NormShape norm_shape(int nv, int64_t rows, int most_threads)
+{
+    int per = rows * ((nv + 127) / 128) >= 4 * kNumSMs ? 4 : 1;
+    while (per < 4 && (nv + per - 1) / per > most_threads) per *= 2;
+    while (per < 32 && (nv + per - 1) / per > 1024) per *= 2;
+    int tpr = 32;
+    while (tpr * per < nv) tpr *= 2;
+    while (per > 1 && tpr * (per / 2) >= nv) per /= 2;
+    return {tpr, per};
+}
+
+template <typename F> static qmm_status norm_by_shape(int dtype, bool vec, int per, F f)
+{
+    auto by_per = [&](auto type, auto v) {
+        if (per <= 1) return f(type, v, std::integral_constant<int, 1>());
+        if (per <= 2) return f(type, v, std::integral_constant<int, 2>());
+        if (per <= 4) return f(type, v, std::integral_constant<int, 4>());
+        if constexpr (decltype(v)::value > 1) {            // 1024 threads of 8 vectors cover 32768 elements of either size
+            return f(type, v, std::integral_constant<int, 8>());
+        } else {
+            if (per <= 8) return f(type, v, std::integral_constant<int, 8>());
+            return f(type, v, std::integral_constant<int, 32>());
+        }
+    };
+    if (dtype == QMM_F32) return vec ? by_per(float(), std::integral_constant<int, 4>()) : by_per(float(), std::integral_constant<int, 1>());
+    if (dtype == QMM_F16) return vec ? by_per(__half(), std::integral_constant<int, 8>()) : by_per(__half(), std::integral_constant<int, 1>());
+    return vec ? by_per(__nv_bfloat16(), std::integral_constant<int, 8>()) : by_per(__nv_bfloat16(), std::integral_constant<int, 1>());
+}
+
+qmm_status launch_rms_norm(int dtype, const void* x, int64_t ldx, const void* res, int64_t ldr, const void* w, float eps, int64_t rows, int K, void* h, int64_t ldh,
+                           void* y, int64_t ldy, int row8, void* codes, int64_t ldc, float* scales, int norm, cudaStream_t st)
+{
+    const int size = dtype == QMM_F32 ? 4 : 2, V = 16 / size;
+    const uintptr_t bits = norm_bits(x, ldx, size) | norm_bits(res, ldr, size) | norm_bits(w, 0, size) | norm_bits(h, ldh, size) | norm_bits(y, ldy, size);
+    const bool vec = K % V == 0 && bits % 16 == 0 && norm_bits(codes, ldc, 1) % V == 0;
+    const int nv = vec ? K / V : K;
+    const NormShape s = norm_shape(nv, rows, 1024);
+    NormP p = {rows, ldx, ldr, ldh, ldy, ldc, K, nv, s.tpr, x, res, w, h, y, (uint8_t*)codes, scales, row8, norm, eps};
+    const int threads = s.tpr < 128 ? 128 : s.tpr;
+    const int per_block = threads / s.tpr;
+    const dim3 grid((unsigned)((rows + per_block - 1) / per_block));
+    return norm_by_shape(dtype, vec, s.per, [&](auto type, auto v, auto n) {
+        return launch_pdl(rms_norm_kernel<decltype(type), decltype(v)::value, decltype(n)::value>, grid, threads, 0, 1, st, "root-mean-square norm launch", p);
+    });
+}
+
+// Blocks of the gradient: about as many as run at once, each keeps a part of dw.
+static int norm_grad_blocks(int64_t rows, int tpr)
+{
+    const int64_t most = (int64_t)kNumSMs * (tpr >= 1024 ? 1 : 1024 / tpr < 8 ? 1024 / tpr : 8);
+    return (int)(rows < most ? rows : most);
+}
+size_t rms_norm_grad_workspace_bytes(int64_t rows, int K)
+{
+    const int64_t most = (int64_t)kNumSMs * 8;
+    return (size_t)(rows < most ? rows : most) * (size_t)K * 4;
+}
+
+qmm_status launch_rms_norm_grad(int dtype, const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* w, float eps, int64_t rows, int K, const void* dh,
+                                int64_t lddh, void* dx, int64_t lddx, float* dw, void* ws, cudaStream_t st)
+{
+    const int size = dtype == QMM_F32 ? 4 : 2, V = 16 / size;
+    const uintptr_t bits = norm_bits(dy, lddy, size) | norm_bits(h, ldh, size) | norm_bits(w, 0, size) | norm_bits(dh, lddh, size) | norm_bits(dx, lddx, size);
+    const bool vec = K % V == 0 && bits % 16 == 0;
+    const int nv = vec ? K / V : K;
+    NormShape s = norm_shape(nv, rows, 512);               // (the kernels of up to four vectors are built for 512 threads)
+    if (s.per <= 4 && s.tpr > 512) s.per = 8;
+    const int blocks = norm_grad_blocks(rows, s.tpr);
+    NormGradP p = {rows, lddy, ldh, lddh, lddx, K, nv, dy, h, w, dh, dx, dw ? (float*)ws : nullptr, eps};
+    const qmm_status e = norm_by_shape(dtype, vec, s.per, [&](auto type, auto v, auto n) {
+        return launch_pdl(rms_norm_grad_kernel<decltype(type), decltype(v)::value, decltype(n)::value>, dim3((unsigned)blocks), s.tpr, 0, 1, st,
+                          "root-mean-square norm gradient launch", p);
+    });
+    if (e != QMM_OK || !dw) return e;
+    return launch_pdl(rms_norm_dw_kernel, dim3((unsigned)((K + 31) / 32)), kColThreads, 0, 1, st, "norm weight gradient launch", (const float*)ws, blocks, K, dw);
+}
+
+template <typename T, int V>
+static qmm_status dequantize_t(const void* codes, int64_t ldc, const float* scales, int int8, int64_t rows, int K, void* out, int64_t ldo, cudaStream_t st)
+{
+    const int nv = K / V;
+    const int64_t blocks = (rows * nv + 255) / 256;
+    if (blocks > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "%lld row vectors are too many for one launch", (long long)(rows * nv));
+    return launch_pdl(rows8_dequantize_kernel<T, V>, dim3((unsigned)blocks), 256, 0, 1, st, "8-bit rows launch", (const uint8_t*)codes, ldc, scales, int8, rows, nv, (T*)out,
+                      ldo);
+}
+template <typename T> static qmm_status dequantize_v(const void* codes, int64_t ldc, const float* scales, int int8, int64_t rows, int K, void* out, int64_t ldo, cudaStream_t st)
+{
+    const bool wide = norm_bits(out, ldo, (int)sizeof(T)) % 16 == 0;
+    const uintptr_t bits = norm_bits(codes, ldc, 1) | (uintptr_t)K;
+    if (wide && bits % 16 == 0) return dequantize_t<T, 16>(codes, ldc, scales, int8, rows, K, out, ldo, st);
+    if (wide && bits % 8 == 0) return dequantize_t<T, 8>(codes, ldc, scales, int8, rows, K, out, ldo, st);
+    return dequantize_t<T, 1>(codes, ldc, scales, int8, rows, K, out, ldo, st);
+}
+qmm_status launch_rows8_dequantize(int row8, const void* codes, int64_t ldc, const float* scales, int64_t rows, int K, int dtype, void* out, int64_t ldo, cudaStream_t st)
+{
+    if (dtype == QMM_F16) return dequantize_v<__half>(codes, ldc, scales, row8, rows, K, out, ldo, st);
+    if (dtype == QMM_BF16) return dequantize_v<__nv_bfloat16>(codes, ldc, scales, row8, rows, K, out, ldo, st);
+    return dequantize_v<float>(codes, ldc, scales, row8, rows, K, out, ldo, st);
+}
+
+}  // namespace qmm

@@ -18,6 +18,10 @@ Q5 = 5
 Q6 = 6
 Q8 = 8
 
+# scores of a router
+SOFTMAX = 0
+SIGMOID = 1
+
 # microscaled 4-bit floating point (the number of a format is its block length) and element types
 MXFP4 = 32
 NVFP4 = 16
@@ -45,6 +49,8 @@ EXPORTS = (
     "qmm_mx_linear_workspace_bytes", "qmm_mx_linear", "qmm_expert_sort_workspace_bytes", "qmm_expert_sort", "qmm_expert_gather",
     "qmm_expert_combine", "qmm_expert_combine_grad", "qmm_mx_experts_bytes", "qmm_mx_quantize_experts", "qmm_mx_experts_gate_up",
     "qmm_mx_experts_gemm", "qmm_mx_moe_workspace_bytes", "qmm_mx_moe",
+    "qmm_expert_route", "qmm_expert_route_grad", "qmm_rms_norm", "qmm_rms_norm_grad_workspace_bytes", "qmm_rms_norm_grad",
+    "qmm_rows_quantize", "qmm_rows_dequantize", "qmm_lora_workspace_bytes", "qmm_lora", "qmm_lora_grad",
 )
 
 
@@ -107,6 +113,18 @@ class MxMoeArgs(ctypes.Structure):
     ]
 
 
+class LoraArgs(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("n", ctypes.c_int32), ("r", ctypes.c_int32), ("dtype", ctypes.c_int32), ("x_format", ctypes.c_int32),
+        ("K", ctypes.c_int64), ("N", ctypes.c_int64), ("X", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("x_scale", ctypes.c_void_p),
+        ("idx", ctypes.c_void_p), ("order", ctypes.c_void_p), ("offsets", ctypes.c_void_p), ("units", ctypes.c_void_p),
+        ("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("S", ctypes.c_void_p),
+        ("Y0", ctypes.c_void_p), ("ldy0", ctypes.c_int64), ("Y", ctypes.c_void_p), ("ldy", ctypes.c_int64),
+        ("dY", ctypes.c_void_p), ("lddy", ctypes.c_int64), ("dX0", ctypes.c_void_p), ("lddx0", ctypes.c_int64),
+        ("dX", ctypes.c_void_p), ("lddx", ctypes.c_int64), ("dA", ctypes.c_void_p), ("dB", ctypes.c_void_p),
+    ]
+
+
 def lib() -> ctypes.CDLL:
     """Load libqmm.so (building it with nvcc first if it is not there)."""
     global _lib
@@ -151,7 +169,7 @@ def lib() -> ctypes.CDLL:
             L.qmm_chain_run.argtypes = [ctypes.POINTER(ChainInfo), vp]
             i32 = ctypes.c_int32
             for name in ("qmm_mx_bytes", "qmm_mx_gemm_workspace_bytes", "qmm_mx_linear_workspace_bytes", "qmm_expert_sort_workspace_bytes",
-                         "qmm_mx_experts_bytes", "qmm_mx_moe_workspace_bytes"):
+                         "qmm_mx_experts_bytes", "qmm_mx_moe_workspace_bytes", "qmm_rms_norm_grad_workspace_bytes", "qmm_lora_workspace_bytes"):
                 getattr(L, name).restype = sz
             L.qmm_mx_bytes.argtypes = [ci, i64, i64]
             L.qmm_mx_pack.argtypes = [ci, vp, vp, i64, i64, vp, vp]
@@ -172,6 +190,16 @@ def lib() -> ctypes.CDLL:
             L.qmm_mx_experts_gemm.argtypes = [ci, vp, i32, i32, i32, vp, vp, vp, i64, i64, vp, vp, ci, vp, i64, vp, vp]
             L.qmm_mx_moe_workspace_bytes.argtypes = [ctypes.POINTER(MxMoeArgs)]
             L.qmm_mx_moe.argtypes = [ctypes.POINTER(MxMoeArgs), vp, sz, vp]
+            L.qmm_expert_route.argtypes = [ci, vp, i64, i32, i32, i32, ci, vp, i32, i32, i32, i32, ctypes.c_float, vp, vp, vp]
+            L.qmm_expert_route_grad.argtypes = [ci, vp, vp, i64, vp, i32, i32, i32, ci, i32, ctypes.c_float, vp, i64, vp]
+            L.qmm_rms_norm.argtypes = [ci, vp, i64, vp, i64, vp, ctypes.c_float, i64, i64, vp, i64, vp, i64, ci, vp, i64, vp, vp]
+            L.qmm_rms_norm_grad_workspace_bytes.argtypes = [i64, i64]
+            L.qmm_rms_norm_grad.argtypes = [ci, vp, i64, vp, i64, vp, ctypes.c_float, i64, i64, vp, i64, vp, i64, vp, vp, sz, vp]
+            L.qmm_rows_quantize.argtypes = [ci, vp, i64, i64, i64, ci, vp, i64, vp, vp]
+            L.qmm_rows_dequantize.argtypes = [ci, vp, i64, vp, i64, i64, ci, vp, i64, vp]
+            L.qmm_lora_workspace_bytes.argtypes = [i32, i32, i32]
+            L.qmm_lora.argtypes = [ctypes.POINTER(LoraArgs), vp, sz, vp]
+            L.qmm_lora_grad.argtypes = [ctypes.POINTER(LoraArgs), vp, sz, vp]
             L.qmm_packed_check.argtypes = [ci, vp, i64, i64, vp, vp]
             L.qmm_debug_config.argtypes = [ctypes.c_char_p, ctypes.c_char_p]
             L.qmm_debug_wait_give_up.argtypes = [vp, i64, vp]
@@ -194,6 +222,23 @@ def _native():
         from . import _qmm_py
         _ext = _qmm_py
     return _ext
+
+
+_layer_ext = None
+
+
+def _layer():
+    """The same for the router, the norm and the adapters."""
+    global _layer_ext
+    if _layer_ext is None:
+        lib()
+        from . import _build
+        with _lock:
+            if not os.path.exists(_build.LAYER_EXT):
+                _build.build_extension()
+        from . import _qmm_layer_py
+        _layer_ext = _qmm_layer_py
+    return _layer_ext
 
 
 def last_error() -> str:
@@ -732,6 +777,146 @@ def mx_moe(fmt: int, X, idx, weights, w_gate, w_up, w_down, I: int, E: int, out=
         ws = _workspace(mx_moe_workspace_bytes(args), X.device, None)
     mx_moe_run(args, ws)
     return out
+
+
+# ---- a router's choice
+
+def expert_route(logits: torch.Tensor, topk: int, scores: int = SOFTMAX, bias: torch.Tensor | None = None, groups: int = 1, top_groups: int | None = None,
+                 group_top: int = 1, renormalize: bool = True, scale: float = 1.0, idx: torch.Tensor | None = None, weights: torch.Tensor | None = None):
+    """logits [T, E] (fp16, bf16 or fp32) -> (idx [T, topk] int32, weights [T, topk] fp32): what expert_sort, expert_combine and mx_moe take.
+    scores SOFTMAX or SIGMOID; bias [E] fp32 counts for the choice alone; of `groups` groups of experts, valued by their group_top (1 or 2) best, top_groups
+    (default: all) are open.  Experts whose logit is -inf are not chosen: slots left over have idx -1 and weight 0."""
+    T, E = logits.shape
+    if idx is None:
+        idx = torch.empty((T, topk), dtype=torch.int32, device=logits.device)
+    if weights is None:
+        weights = torch.empty((T, topk), dtype=torch.float32, device=logits.device)
+    assert idx.shape == (T, topk) and weights.shape == (T, topk), "idx and weights: [T, topk]"
+    _check((_layer_ext or _layer()).expert_route(logits, topk, scores, bias, groups, groups if top_groups is None else top_groups, group_top, 1 if renormalize else 0, scale,
+                                                 idx, weights))
+    return idx, weights
+
+
+def expert_route_grad(dweights: torch.Tensor, logits: torch.Tensor, idx: torch.Tensor, scores: int = SOFTMAX, renormalize: bool = True, scale: float = 1.0,
+                      out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of expert_route's weights with respect to the logits: dweights [T, topk] (as expert_combine_grad gives it) -> [T, E] of the logits' type."""
+    if out is None:
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    T, topk = idx.shape
+    assert logits.shape[0] == T and dweights.shape == (T, topk), "dweights and idx [T, topk], logits [T, E]"
+    _check((_layer_ext or _layer()).expert_route_grad(dweights, logits, idx, topk, scores, 1 if renormalize else 0, scale, out))
+    return out
+
+
+# ---- root-mean-square norm, rows of 8 bits
+
+def rms_norm(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-6, residual: torch.Tensor | None = None, h: torch.Tensor | None = None,
+             y: torch.Tensor | None = None):
+    """(y, h): h = x + residual (x itself without one), y = h / sqrt(mean(h^2) + eps) * weight, all [rows, K] of one type; any row strides.  h may be x or residual."""
+    if y is None:
+        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    if h is None and residual is not None:
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    _check((_layer_ext or _layer()).rms_norm(x, weight, eps, residual, h, y, None, None))
+    return y, x if h is None else h
+
+
+def rms_norm_rows(x: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-6, residual: torch.Tensor | None = None, h: torch.Tensor | None = None,
+                  codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, y: torch.Tensor | None = None, dtype: torch.dtype = torch.float8_e4m3fn):
+    """(codes, scales, h): the same norm into rows of 8 bits (torch.float8_e4m3fn or torch.int8) with one fp32 scale per row; also into y where it is given."""
+    if codes is None:
+        codes = torch.empty(x.shape, dtype=dtype, device=x.device)
+    if scales is None:
+        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    if h is None and residual is not None:
+        h = torch.empty_like(x, memory_format=torch.contiguous_format)
+    _check((_layer_ext or _layer()).rms_norm(x, weight, eps, residual, h, y, codes, scales))
+    return codes, scales, x if h is None else h
+
+
+def rms_norm_grad_workspace_bytes(rows: int, K: int) -> int:
+    return lib().qmm_rms_norm_grad_workspace_bytes(rows, K)
+
+
+def rms_norm_grad(dy: torch.Tensor, h: torch.Tensor, weight: torch.Tensor | None = None, eps: float = 1e-6, dh: torch.Tensor | None = None, dx: torch.Tensor | None = None,
+                  dweight: torch.Tensor | None = None, ws: torch.Tensor | None = None, want_dweight: bool = True):
+    """(dx, dweight fp32 [K]): gradients of rms_norm for dy at y and dh (optional) at h; dx is that of x and of the residual."""
+    if dx is None:
+        dx = torch.empty_like(h, memory_format=torch.contiguous_format)
+    if dweight is None and want_dweight:
+        dweight = torch.empty(h.shape[1], dtype=torch.float32, device=h.device)
+    if ws is None and dweight is not None:
+        ws = torch.empty(rms_norm_grad_workspace_bytes(*h.shape), dtype=torch.uint8, device=h.device)
+    _check((_layer_ext or _layer()).rms_norm_grad(dy, h, weight, eps, dh, dx, dweight, ws))
+    return dx, dweight
+
+
+def rows_quantize(x: torch.Tensor, codes: torch.Tensor | None = None, scales: torch.Tensor | None = None, dtype: torch.dtype = torch.float8_e4m3fn):
+    """x [rows, K] -> (codes of 8 bits [rows, K], scales fp32 [rows]): what lora takes as x, and what a training program keeps of x for lora_grad."""
+    if codes is None:
+        codes = torch.empty(x.shape, dtype=dtype, device=x.device)
+    if scales is None:
+        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    _check((_layer_ext or _layer()).rows_quantize(x, codes, scales))
+    return codes, scales
+
+
+def rows_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor | None = None, dtype: torch.dtype = torch.float32) -> torch.Tensor:
+    """Rows of 8 bits -> the values that they stand for, of out's type (or `dtype`)."""
+    if out is None:
+        out = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    _check((_layer_ext or _layer()).rows_dequantize(codes, scales, out))
+    return out
+
+
+# ---- low-rank adapters beside a shared projection
+
+def lora_workspace_bytes(T: int, n: int, r: int) -> int:
+    _counts(T, n, r)
+    need = lib().qmm_lora_workspace_bytes(T, n, r)
+    if need == 0:
+        raise QmmError(1, last_error())
+    return need
+
+
+def _lora_plan(plan: ExpertPlan | None, T: int, n: int):
+    """Addresses of a plan's order, offsets and units, and its device; zeros without one."""
+    if plan is None:
+        return 0, 0, 0, 0
+    assert plan.T == T and plan.topk == 1 and plan.E == n, "plan: of idx [T, 1] and n adapters"
+    return plan.ptrs[0], plan.ptrs[2], plan.ptrs[3], plan.device
+
+
+def lora(x: torch.Tensor, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, y0: torch.Tensor | None, scale: torch.Tensor | None = None,
+         x_scale: torch.Tensor | None = None, s: torch.Tensor | None = None, plan: ExpertPlan | None = None, ws: torch.Tensor | None = None,
+         out: torch.Tensor | None = None) -> torch.Tensor:
+    """out [T, N] = y0 + scale[idx] * b[idx] (a[idx] x): adapters a [n, r, K], b [n, N, r] beside a projection's output y0 (None: zeros; out may be y0).
+    x [T, K] of the adapters' type, or rows of 8 bits with x_scale.  idx [T] int32, outside [0, n): no adapter.  s [T, r] fp32 receives a[idx] x, which lora_grad takes.
+    plan: expert_sort(idx.view(-1, 1), n), for programs that use one for many projections."""
+    T = x.shape[0]
+    if out is None:
+        out = torch.empty((T, b.shape[1]), dtype=b.dtype, device=x.device)
+    if ws is None and T > 256:
+        ws = torch.empty(lora_workspace_bytes(T, a.shape[0], a.shape[1]), dtype=torch.uint8, device=x.device)
+    _check((_layer_ext or _layer()).lora(x, x_scale, idx, a, b, scale, *_lora_plan(plan, T, a.shape[0]), s, y0, out, ws))
+    return out
+
+
+def lora_grad(dy: torch.Tensor, x: torch.Tensor | None, s: torch.Tensor | None, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, dx0: torch.Tensor | None = None,
+              scale: torch.Tensor | None = None, x_scale: torch.Tensor | None = None, plan: ExpertPlan | None = None, ws: torch.Tensor | None = None,
+              dx: torch.Tensor | None = None, da: torch.Tensor | None = None, db: torch.Tensor | None = None):
+    """(dx, da, db): dx [T, K] = dx0 (None: zeros) + the adapters' part, of dy's type; da, db fp32 in a's and b's shapes.  x: as in lora, 16-bit or 8-bit rows."""
+    T, n, r = dy.shape[0], a.shape[0], a.shape[1]
+    if dx is None:
+        dx = torch.empty((T, a.shape[2]), dtype=dy.dtype, device=dy.device)
+    if da is None:
+        da = torch.empty(a.shape, dtype=torch.float32, device=dy.device)
+    if db is None:
+        db = torch.empty(b.shape, dtype=torch.float32, device=dy.device)
+    if ws is None:
+        ws = torch.empty(lora_workspace_bytes(T, n, r), dtype=torch.uint8, device=dy.device)
+    _check((_layer_ext or _layer()).lora_grad(x, x_scale, idx, a, b, scale, *_lora_plan(plan, T, n), s, dy, dx0, dx, da, db, ws))
+    return dx, da, db
 
 
 def packed_check(fmt: int, packed: torch.Tensor, N: int, K: int, ws: torch.Tensor) -> None:
