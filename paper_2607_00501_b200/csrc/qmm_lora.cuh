@@ -73,26 +73,45 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t& hi, uint32_t&
 
 // ------------------------------------------------------------------ loads
 
-// Eight consecutive elements of a row as four registers of T pairs; elements from `left` on are zero.  VEC: one access (left is then 0 or at least 8).
-// NC: nobody writes the row meanwhile (y0 may be y).
-template <typename T, bool VEC, bool NC = true> __device__ __forceinline__ void load8(const T* p, int left, uint32_t (&u)[4])
+template <bool NC> __device__ __forceinline__ uint32_t ld32(const void* p)
 {
+    return NC ? __ldg(reinterpret_cast<const uint32_t*>(p)) : *reinterpret_cast<const uint32_t*>(p);
+}
+// Eight consecutive elements of a row, from element `at` on, as four registers of T pairs; elements from `left` on are zero.  VEC: rows are 16-byte aligned and a
+// multiple of 8 long, one access.  Otherwise rows start at any element: whole words with a shift by half a word where that stays inside the row, else (its ends) element by
+// element.  NC: nobody writes the row meanwhile (y0 may be y).
+template <typename T, bool VEC, bool NC = true> __device__ __forceinline__ void load8(const T* row, int64_t at, int left, uint32_t (&u)[4])
+{
+    const T* p = row + at;
+    u[0] = u[1] = u[2] = u[3] = 0u;
     if (VEC) {
         if (left > 0) {
             const uint4 q = NC ? __ldg(reinterpret_cast<const uint4*>(p)) : *reinterpret_cast<const uint4*>(p);
             u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
-        } else {
-            u[0] = u[1] = u[2] = u[3] = 0u;
         }
-    } else {
-        const unsigned short* s = reinterpret_cast<const unsigned short*>(p);
+        return;
+    }
+    if (left <= 0) return;
+    const bool odd = reinterpret_cast<uintptr_t>(p) & 2;
+    if (left > 8 || (left == 8 && !odd)) {
+        if (!odd || at > 0) {
+            const uint32_t* w = reinterpret_cast<const uint32_t*>(p - (odd ? 1 : 0));
+            uint32_t v[5];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t a = 0u, b = 0u;
-            if (2 * i < left) a = NC ? __ldg(s + 2 * i) : s[2 * i];
-            if (2 * i + 1 < left) b = NC ? __ldg(s + 2 * i + 1) : s[2 * i + 1];
-            u[i] = a | (b << 16);
+            for (int i = 0; i < 4; ++i) v[i] = ld32<NC>(w + i);
+            v[4] = odd ? ld32<NC>(w + 4) : 0u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) u[i] = __funnelshift_r(v[i], v[i + 1], odd ? 16 : 0);
+            return;
         }
+    }
+    const unsigned short* e = reinterpret_cast<const unsigned short*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t a = 0u, b = 0u;
+        if (2 * i < left) a = NC ? __ldg(e + 2 * i) : e[2 * i];
+        if (2 * i + 1 < left) b = NC ? __ldg(e + 2 * i + 1) : e[2 * i + 1];
+        u[i] = a | (b << 16);
     }
 }
 // R8 consecutive elements (1, 2, 4, 8 or 16) of a weight row of r contiguous ones; (R8 + 1) / 2 registers, a single element in the low half.
@@ -148,16 +167,23 @@ template <typename T, bool X8, bool VEC> struct XPiece {
     {
         if (!row) left = 0;
         if constexpr (!X8) {
-            load8<T, VEC>((const T*)row + k, left, u);
+            load8<T, VEC>((const T*)row, k, left, u);
         } else if (VEC) {
             const uint2 q = left > 0 ? __ldg(reinterpret_cast<const uint2*>((const uint8_t*)row + k)) : make_uint2(0u, 0u);
             u[0] = q.x, u[1] = q.y;
         } else {
-            const uint8_t* s = (const uint8_t*)row + k;
+            const uint8_t* e = (const uint8_t*)row + k;
+            const int off = (int)(reinterpret_cast<uintptr_t>(e) & 3);
             u[0] = u[1] = 0u;
+            if (off == 0 ? left >= 8 : left >= 12 && k >= 4) {                 // words that lie inside the row
+                const uint32_t* w = reinterpret_cast<const uint32_t*>(e - off);
+                const uint32_t v[3] = {ld32<true>(w), ld32<true>(w + 1), off ? ld32<true>(w + 2) : 0u};
+                u[0] = __funnelshift_r(v[0], v[1], 8 * off), u[1] = __funnelshift_r(v[1], v[2], 8 * off);
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < left) u[i >> 2] |= (uint32_t)__ldg(s + i) << (8 * (i & 3));
+                for (int i = 0; i < 8; ++i)
+                    if (i < left) u[i >> 2] |= (uint32_t)__ldg(e + i) << (8 * (i & 3));
+            }
         }
     }
     __device__ __forceinline__ void pairs(int int8, uint32_t (&v)[4]) const
@@ -183,10 +209,11 @@ __device__ __forceinline__ void narrow(float (&acc)[MW][R / 8][4], const void* c
                                        int lane)
 {
     constexpr int R8 = R / 8;
-    constexpr int U = MW == 1 ? 4 : 2;                     // chunks in flight
+    // chunks a round; the next round's are on their way during the products of this one
+    constexpr int U = MW == 1 ? (R <= 64 ? 4 : 2) : (R <= 32 ? 2 : 1);
     const int g = lane >> 2, t = lane & 3;
-    for (int c = c0; c < c1; c += step * U) {
-        XPiece<T, X8, VEC> x[U][MW][2];
+    XPiece<T, X8, VEC> x[U][MW][2];
+    auto fetch = [&](int c) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = (c + u * step) * 32 + 8 * t;
@@ -196,6 +223,17 @@ __device__ __forceinline__ void narrow(float (&acc)[MW][R / 8][4], const void* c
 #pragma unroll
                 for (int h = 0; h < 2; ++h) x[u][m][h].load(row[m][h], k, left);
         }
+    };
+    fetch(c0);
+    for (int c = c0; c < c1; c += step * U) {
+        XPiece<T, X8, VEC> now[U][MW][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int m = 0; m < MW; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) now[u][m][h] = x[u][m][h];
+        fetch(c + step * U);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int k = (c + u * step) * 32 + 8 * t;
@@ -204,12 +242,12 @@ __device__ __forceinline__ void narrow(float (&acc)[MW][R / 8][4], const void* c
 #pragma unroll
             for (int m = 0; m < MW; ++m)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) x[u][m][h].pairs(int8, a[m][h]);
+                for (int h = 0; h < 2; ++h) now[u][m][h].pairs(int8, a[m][h]);
             if constexpr (LAY == 0) {
 #pragma unroll
                 for (int i = 0; i < R8; ++i) {
                     uint32_t w[4];
-                    load8<T, VEC>(w1 + (int64_t)(8 * i + g) * K + k, left, w);
+                    load8<T, VEC>(w1 + (int64_t)(8 * i + g) * K, k, left, w);
 #pragma unroll
                     for (int m = 0; m < MW; ++m)
 #pragma unroll
@@ -316,11 +354,13 @@ template <int LAY> struct Wide {
     static constexpr int own = cols / 4;
 };
 
-template <typename T, int R, int LAY, bool VEC> struct WideWeights {
-    static constexpr int steps = R < 16 ? 1 : R / 16;
+// Weights of a column group for one block of ranks: two k-steps (LAY 0, R >= 32) or one.
+template <typename T, int R, int LAY, bool VEC> struct WideBlock {
+    static constexpr int steps = LAY == 0 && R >= 32 ? 2 : 1;
+    static constexpr int blocks = (R < 16 ? 16 : R) / 16 / steps;
     uint32_t b[steps][Wide<LAY>::tiles][2];
-    // column group from column n0; w2 of the adapter, N columns
-    __device__ __forceinline__ void load(const T* __restrict__ w2, int n0, int N, int lane, int s0 = 0, int s1 = steps)
+    // column group from column n0; w2 of the adapter, N columns; q: which block
+    __device__ __forceinline__ void load(const T* __restrict__ w2, int n0, int N, int q, int lane)
     {
         const int g = lane >> 2, t = lane & 3;
         if constexpr (LAY == 0) {
@@ -330,13 +370,10 @@ template <typename T, int R, int LAY, bool VEC> struct WideWeights {
                 const T* p = w2 + (int64_t)n * R;
                 const bool there = n < N;
                 if constexpr (R >= 32) {
-#pragma unroll
-                    for (int q = 0; q < R / 32; ++q) {
-                        uint32_t u[4];
-                        load8<T, VEC>(p + 32 * q + 8 * t, there ? 8 : 0, u);
-                        b[2 * q][i][0] = u[0], b[2 * q][i][1] = u[1];
-                        b[2 * q + 1][i][0] = u[2], b[2 * q + 1][i][1] = u[3];
-                    }
+                    uint32_t u[4];
+                    load8<T, VEC>(p, 32 * q + 8 * t, there ? R - (32 * q + 8 * t) : 0, u);
+                    b[0][i][0] = u[0], b[0][i][1] = u[1];
+                    b[1][i][0] = u[2], b[1][i][1] = u[3];
                 } else {
                     uint32_t u[2];
                     load_r<T, 4, VEC>(p + 4 * t, there && (R == 16 || t < 2), u);
@@ -344,21 +381,34 @@ template <typename T, int R, int LAY, bool VEC> struct WideWeights {
                 }
             }
         } else {
+            uint32_t u[4][4];
 #pragma unroll
-            for (int s = 0; s < steps; ++s) {
-                uint32_t u[4][4];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int j = 16 * s + 2 * t + (q & 1) + 8 * (q >> 1);
-                    const int left = j < R ? N - (n0 + 8 * g) : 0;
-                    load8<T, VEC>(w2 + (int64_t)j * N + n0 + 8 * g, left, u[q]);
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    b[s][i][0] = pair_of(u[0][i >> 1], u[1][i >> 1], i & 1);
-                    b[s][i][1] = pair_of(u[2][i >> 1], u[3][i >> 1], i & 1);
-                }
+            for (int k = 0; k < 4; ++k) {
+                const int j = 16 * q + 2 * t + (k & 1) + 8 * (k >> 1);
+                const int left = j < R ? N - (n0 + 8 * g) : 0;
+                load8<T, VEC>(w2 + (int64_t)j * N, n0 + 8 * g, left, u[k]);
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                b[0][i][0] = pair_of(u[0][i >> 1], u[1][i >> 1], i & 1);
+                b[0][i][1] = pair_of(u[2][i >> 1], u[3][i >> 1], i & 1);
+            }
+        }
+    }
+};
+// All of a group's weights in registers, or, for high ranks, none of them: each row tile reads them again (from L1) block by block.
+template <typename T, int R, int LAY, bool VEC> struct WideWeights {
+    using Block = WideBlock<T, R, LAY, VEC>;
+    static constexpr bool held = LAY == 0 ? R <= 64 : R <= 32;
+    Block block[held ? Block::blocks : 1];
+    const T* w2;
+    int n0, N;
+    __device__ __forceinline__ void load(const T* __restrict__ w, int first, int width, int lane)
+    {
+        w2 = w, n0 = first, N = width;
+        if constexpr (held) {
+#pragma unroll
+            for (int q = 0; q < Block::blocks; ++q) block[q].load(w, first, width, q, lane);
         }
     }
 };
@@ -374,7 +424,7 @@ template <typename T, int LAY, bool VEC> struct YPiece {
 #pragma unroll
             for (int i = 0; i < regs; i += 4) {
                 uint32_t v[4];
-                load8<T, VEC, false>(y0 + row[h] * ld + n + 2 * i, y0 && row[h] >= 0 ? N - (n + 2 * i) : 0, v);
+                load8<T, VEC, false>(y0 + row[h] * ld, n + 2 * i, y0 && row[h] >= 0 ? N - (n + 2 * i) : 0, v);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) u[h][i + k] = v[k];
             }
@@ -384,8 +434,18 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
 {
     if (VEC) {
         if (left > 0) *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+        return;
+    }
+    unsigned short* s = reinterpret_cast<unsigned short*>(p);
+    if (left >= 8 && !(reinterpret_cast<uintptr_t>(p) & 2)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = u[i];
+    } else if (left >= 8) {                                // an element, three words, an element
+        s[0] = (unsigned short)u[0];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) *reinterpret_cast<uint32_t*>(s + 1 + 2 * i) = __funnelshift_r(u[i], u[i + 1], 16);
+        s[7] = (unsigned short)(u[3] >> 16);
     } else {
-        unsigned short* s = reinterpret_cast<unsigned short*>(p);
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if (i < left) s[i] = (unsigned short)(u[i >> 1] >> (16 * (i & 1)));
@@ -394,22 +454,35 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
 
 // y = rn(y0 + back * (u . w2)) for the 16 rows of tile m and one column group.
 template <typename T, int R, int LAY, bool VEC>
-__device__ __forceinline__ void widen(const WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
+__device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
                                       T* y, int64_t ld, const int (&row)[2], int n, int N, int lane)
 {
-    constexpr int tiles = Wide<LAY>::tiles, steps = WideWeights<T, R, LAY, VEC>::steps;
+    using W = WideWeights<T, R, LAY, VEC>;
+    constexpr int tiles = Wide<LAY>::tiles, steps = W::Block::steps;
     float acc[tiles][4];
 #pragma unroll
     for (int i = 0; i < tiles; ++i) acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.0f;
+    auto product = [&](const typename W::Block& b, int q) {
 #pragma unroll
-    for (int s = 0; s < steps; ++s) {
-        uint32_t a[4];
-        get_u<R, LAY>(lo, m, s, lane, a);
+        for (int s = 0; s < steps; ++s) {
+            uint32_t a[4];
+            get_u<R, LAY>(lo, m, q * steps + s, lane, a);
 #pragma unroll
-        for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, w.b[s][i][0], w.b[s][i][1]);
-        get_u<R, LAY>(hi, m, s, lane, a);
+            for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, b.b[s][i][0], b.b[s][i][1]);
+            get_u<R, LAY>(hi, m, q * steps + s, lane, a);
 #pragma unroll
-        for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, w.b[s][i][0], w.b[s][i][1]);
+            for (int i = 0; i < tiles; ++i) mma16<T>(acc[i], a, b.b[s][i][0], b.b[s][i][1]);
+        }
+    };
+    if constexpr (W::held) {
+#pragma unroll
+        for (int q = 0; q < W::Block::blocks; ++q) product(w.block[q], q);
+    } else {
+#pragma unroll 1
+        for (int q = 0; q < W::Block::blocks; ++q) {
+            w.block[0].load(w.w2, w.n0, w.N, q, lane);
+            product(w.block[0], q);
+        }
     }
     const int g = lane >> 2;
 #pragma unroll
@@ -476,12 +549,37 @@ __device__ __forceinline__ float4 remote4(const float* p, int rank)
     return v;
 }
 
-__device__ __forceinline__ float remote1(const float* p, int rank)
+// The blocks' four numbers at p (shared memory), added in block order; up to 16 blocks, the loads of eight in flight at once.
+__device__ __forceinline__ float4 cluster_sum4(const float* p, int size)
 {
-    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), there;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(there) : "memory");
+    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+        if (8 * half >= size) break;
+        float4 r[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) r[k] = 8 * half + k < size ? remote4(p, 8 * half + k) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v.x += r[k].x, v.y += r[k].y, v.z += r[k].z, v.w += r[k].w;
+    }
+    return v;
+}
+
+__device__ __forceinline__ float cluster_sum1(const float* p, int size)
+{
+    const uint32_t at = (uint32_t)__cvta_generic_to_shared(p);
+    float r[8], v = 0.0f;                                  // (weight gradients: eight blocks at most)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        r[k] = 0.0f;
+        if (k < size) {
+            uint32_t there;
+            asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(k));
+            asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(r[k]) : "r"(there) : "memory");
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v += r[k];
     return v;
 }
 
@@ -497,7 +595,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void copy_row(const L
 {
     for (int n = n0 + 8 * lane; n < n1; n += 256) {
         uint32_t u[4];
-        load8<T, VEC, false>((const T*)p.y0 + row * p.ldy0 + n, p.y0 ? n1 - n : 0, u);
+        load8<T, VEC, false>((const T*)p.y0 + row * p.ldy0, n, p.y0 ? n1 - n : 0, u);
         store8<T, VEC>((T*)p.y + row * p.ldy + n, n1 - n, u);
     }
 }
@@ -591,11 +689,7 @@ __global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
     for (int q = 0; q < rounds; ++q) {
         const int i = tid + q * kThreads;
         if (16 * R / 4 >= kThreads || warp < (16 * R / 4 + 31) / 32) {        // whole warps: put_u shuffles
-            float4 v = remote4(sum + 4 * i, 0);
-            for (int k = 1; k < size; ++k) {
-                const float4 r = remote4(sum + 4 * i, k);
-                v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
-            }
+            const float4 v = cluster_sum4(sum + 4 * i, size);
             const int m = 4 * i / R, j = 4 * i % R, to = rows[m];
             float f[4] = {v.x, v.y, v.z, v.w};
             if (X8 && to >= 0) {
@@ -712,11 +806,7 @@ __global__ void __launch_bounds__(kThreads, 2) lora_narrow_kernel(const LoraP p)
     share_of(kTileRows * R / 4, rank, size, i0, i1);       // each block adds and stores its share of the tile's sums
     for (int i = i0 + tid; i < i1; i += kThreads) {
         const int to = rows[4 * i / R];
-        float4 v = remote4(part + 4 * i, 0);
-        for (int k = 1; k < size; ++k) {
-            const float4 r = remote4(part + 4 * i, k);
-            v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
-        }
+        float4 v = cluster_sum4(part + 4 * i, size);
         if (to < 0) continue;
         const float f = X8 ? __ldg(p.x_scale + to) : 1.0f;
         if (X8) v.x *= f, v.y *= f, v.z *= f, v.w *= f;
@@ -771,19 +861,39 @@ __global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, 
     const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
     const int g = lane >> 2, t = lane & 3, own = Wide<LAY>::own * t;
     const int last = min((span + 1) * per_span, groups);
-    for (int c = span * per_span + warp; c < last; c += kWarps) {
-        WideWeights<T, R, LAY, VEC> w;
-        YPiece<T, LAY, VEC> y0[4];
-        int row[4][2];
+    // a column group in phases of HM row tiles; the next phase's y0 (and the next group's weights, where registers allow) is on its way during the products of this one
+    constexpr int HM = LAY == 0 ? 2 : 1, PH = 4 / HM;
+    constexpr bool AHEAD = LAY == 0 ? R <= 32 : R <= 16;
+    using W = WideWeights<T, R, LAY, VEC>;
+    YPiece<T, LAY, VEC> y0[2][HM];
+    W w;
+    auto load_y = [&](int c, int ph, YPiece<T, LAY, VEC> (&y)[HM]) {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            row[m][0] = rows[m * 16 + g], row[m][1] = rows[m * 16 + g + 8];
-            y0[m].load((const T*)p.y0, p.ldy0, row[m], c * G + own, p.N);
+        for (int m = 0; m < HM; ++m) {
+            const int at = (ph * HM + m) * 16 + g, row[2] = {c < last ? rows[at] : -1, c < last ? rows[at + 8] : -1};
+            y[m].load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
         }
-        w.load(w2, c * G, p.N, lane);
+    };
+    int c = span * per_span + warp;
+    load_y(c, 0, y0[0]);
+    if (AHEAD && c < last) w.load(w2, c * G, p.N, lane);
+    for (; c < last; c += kWarps) {
+        if (!AHEAD) w.load(w2, c * G, p.N, lane);
+        W next;
 #pragma unroll
-        for (int m = 0; m < 4; ++m)
-            if (m * 16 < count) widen<T, R, LAY, VEC>(w, y0[m], hi, lo, back, m, (T*)p.y, p.ldy, row[m], c * G + own, p.N, lane);
+        for (int ph = 0; ph < PH; ++ph) {
+            if (ph + 1 < PH) load_y(c, ph + 1, y0[(ph + 1) & 1]);
+            else load_y(c + kWarps, 0, y0[(ph + 1) & 1]);
+            if (AHEAD && ph == PH - 1 && c + kWarps < last) next.load(w2, (c + kWarps) * G, p.N, lane);
+#pragma unroll
+            for (int m = 0; m < HM; ++m) {
+                const int mt = ph * HM + m;
+                if (mt * 16 >= count) continue;
+                const int row[2] = {rows[mt * 16 + g], rows[mt * 16 + g + 8]};
+                widen<T, R, LAY, VEC>(w, y0[ph & 1][m], hi, lo, back, mt, (T*)p.y, p.ldy, row, c * G + own, p.N, lane);
+            }
+        }
+        if (AHEAD) w = next;
     }
 }
 
@@ -801,138 +911,294 @@ struct WgradP {
     float* out;                                            // [n, R, W] or, TRANS, [n, W, R]
 };
 
-// out[a] = sum over the adapter's rows of s (R) x v (W).  A cluster takes 64 columns of one adapter, its blocks and their warps share the rows, 16 at a time: lane (g, t)
-// loads columns 8 g .. 8 g + 7 of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9 (a whole 128-byte line per row), pairs of rows become the MMA's k, and its tile i has column 8 c + i
-// at place c.  The parts are added in a fixed order: warps, then blocks.
+__device__ __forceinline__ void async16(uint32_t to, const void* from, int bytes)            // bytes < 16: the rest becomes zero
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void async4(uint32_t to, const void* from, int bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+
+// out[a] = sum over the adapter's rows of s (R) x v (W).  A block takes 128 columns of one adapter and 64 rows a stage, two or three stages in flight (cp.async); the blocks of a
+// cluster share the rows.  A warp has all R ranks of 64, 32 or 16 columns (R x columns = 2048 where R >= 32: 64 accumulators a lane), the warps of a column group share the stage's
+// rows.  k of the products is the row: v comes out of shared memory transposed (ldmatrix.trans; codes of 8 bits by words and byte permutes), s is brought into
+// [rank][row] once per stage, split into 16-bit or tf32 parts:
 //   bf16 products of three parts of s (all of its bits: with two, dA is off by 1.5e-6 beside an fp32 sum's 3e-7); fp16 rows: tf32 products of two parts, whose exponent
 //   holds any s (a gradient's 1e-7 is below fp16's normal numbers).
+// The parts of a sum are added in a fixed order: warps, then blocks.
+// Bound by HBM where R <= 16; from R = 32 on by the warp-level tensor products of the parts (3 or 4 of them for each of s).
+template <typename T, bool X8, int R> struct WgradShape {
+    static constexpr bool tf32 = std::is_same<T, __half>::value && !X8;
+    static constexpr int cols = 128, rows = 64, stages = R == 64 ? 2 : 3;      // (two blocks per SM up to R = 64)
+    static constexpr int RT = R < 16 ? 16 : R;             // ranks, as whole tiles of 16
+    static constexpr int MT = RT / 16;
+    static constexpr int WC = R <= 32 ? 64 : R == 64 ? 32 : 16;               // columns of a warp
+    static constexpr int CG = cols / WC, RG = kWarps / CG, NT = WC / 8;
+    static constexpr int vpitch = X8 ? cols : 2 * cols;
+    static constexpr int vbytes = rows * vpitch, sbytes = rows * R * 4;
+    static constexpr int part = tf32 ? RT * rows * 4 : RT * rows * 2;
+    static constexpr int parts = tf32 ? 2 : 3;
+    static constexpr int stage = vbytes + sbytes;
+    static constexpr int sums = RG * RT * cols * 4;
+    static constexpr int front = stages * stage > sums ? stages * stage : sums;
+    static constexpr int smem = front + parts * part + stages * rows * 4;
+};
+
 template <typename T, bool X8, int R, bool TRANS, bool VEC>
-__global__ void __launch_bounds__(kThreads, R >= 64 ? 1 : 2) lora_wgrad_kernel(const WgradP p)
+__global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(const WgradP p)
 {
     pdl_launch_dependents();
     pdl_wait();
-    constexpr bool TF32 = std::is_same<T, __half>::value && !X8;
-    using M = typename std::conditional<TF32, __half, __nv_bfloat16>::type;   // 16-bit type of the loaded pairs
-    constexpr int MT = R <= 32 ? 1 : 2;                    // tiles of 16 ranks per warp
-    constexpr int JG = R <= 16 ? 1 : R / (16 * MT);        // groups of ranks: warps that read the same rows (from L1)
-    constexpr int TG = kWarps / JG;                        // warps that share the rows
-    constexpr int RT = R < 16 ? 16 : R;
+    using S = WgradShape<T, X8, R>;
+    constexpr int MT = S::MT, NT = S::NT, WC = S::WC, RG = S::RG, RT = S::RT;
     extern __shared__ __align__(16) uint8_t smem[];
-    float* part = reinterpret_cast<float*>(smem);          // [TG][RT][64]; share 0 holds the block's sum in the end
+    uint8_t* s_part = smem + S::front;
+    float* s_scale = reinterpret_cast<float*>(s_part + S::parts * S::part);
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem), part0 = base + S::front;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int rank = (int)cluster_rank(), size = (int)cluster_size();
-    const int chunks = (p.W + 63) / 64;
+    const int chunks = (p.W + S::cols - 1) / S::cols;
     const int64_t id = blockIdx.x / size;
-    const int a = (int)(id / chunks), col0 = (int)(id - (int64_t)a * chunks) * 64;
-    const int first = __ldg(p.offsets + a), end = min(__ldg(p.offsets + a + 1), p.T);
-    const int jg = warp % JG, tg = warp / JG;
+    const int a = (int)(id / chunks), col0 = (int)(id - (int64_t)a * chunks) * S::cols;
+    const int first = max(__ldg(p.offsets + a), 0), end = min(__ldg(p.offsets + a + 1), p.T);
+    const int total = end > first ? (end - first + S::rows - 1) / S::rows : 0;               // stages of the adapter
+    int st0, st1;
+    share_of(total, rank, size, st0, st1);
+    const int cg = warp / RG, rg = warp % RG;
     const float sc = p.scale ? __ldg(p.scale + a) : 1.0f;
-    float acc[MT][8][4];
+    const int es = X8 ? 1 : 2;
+
+    // this thread's part of a stage: VN pieces of 16 bytes of v, rows vr + q VS; SN pieces of s, rows sr + q SS
+    constexpr int VPR = S::vpitch / 16, VS = kThreads / VPR, VN = S::rows / VS;              // pieces per row
+    constexpr int SPR = R * 4 / 16, SS = kThreads / SPR >= S::rows ? S::rows : kThreads / SPR, SN = S::rows / SS;
+    const int vr = tid / VPR, vc = tid % VPR, sr = tid / SPR, sp = tid % SPR;
+    const bool s_mine = tid < SS * SPR;
+    const int vcol = col0 + vc * 16 / es, vleft = p.W - vcol;
+    int vrow[VN], srow[SN], xrow = -1;
+    auto rows_of = [&](int stage) {                        // order of the stage's rows that this thread loads
+        const int r0 = first + stage * S::rows;
+        const int n = stage < st1 ? end - r0 : 0;
+        auto at = [&](int i) {
+            const int r = i < n ? __ldg(p.order + r0 + i) : -1;
+            return r < p.T ? r : -1;
+        };
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+        for (int q = 0; q < VN; ++q) vrow[q] = at(vr + q * VS);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
-    // lane's ranks: 2 MT consecutive ones (R = 8: one); row c of tile m is rank of lane (c % 8), the (2 m + c / 8)-th
-    constexpr int JN = R == 8 ? 1 : 2 * MT;
-    const int j0 = R == 8 ? g : jg * 16 * MT + g * JN;
-    const int left = p.W - (col0 + 8 * g);
-    for (int r0 = first + 16 * (rank * TG + tg); r0 < end; r0 += 16 * size * TG) {
-        const int mine = r0 + (lane & 15) < end ? __ldg(p.order + r0 + (lane & 15)) : -1;
-        XPiece<M, X8, VEC> v[4];
-        float s[4][JN];
+        for (int q = 0; q < SN; ++q) srow[q] = s_mine ? at(sr + q * SS) : -1;
+        if (X8 && tid < S::rows) xrow = at(tid);
+    };
+    auto v_place = [&](int r, int c) -> uint32_t {         // of 16-byte piece c of row r
+        return (uint32_t)(r * S::vpitch) + (uint32_t)(X8 ? c ^ (((r >> 1) & 3) << 1) : c ^ (r & 7)) * 16u;
+    };
+    uint32_t held[VEC ? 1 : VN][4];                        // rows that are not 16-byte aligned come through registers
+    auto fetch = [&](int buf) {
+        const uint32_t to = base + buf * S::stage;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            int row = __shfl_sync(0xFFFFFFFFu, mine, 2 * t + (q & 1) + 8 * (q >> 1));
-            if (row >= p.T) row = -1;
-            v[q].load(row >= 0 ? (const char*)p.v + row * p.ldv * (X8 ? 1 : 2) : nullptr, col0 + 8 * g, left);
-            const float* sp = p.s + (int64_t)max(row, 0) * R + j0;
-            if constexpr (JN == 4) {
-                const float4 f = *reinterpret_cast<const float4*>(sp);
-                s[q][0] = f.x, s[q][1] = f.y, s[q][2] = f.z, s[q][3] = f.w;
-            } else if constexpr (JN == 2) {
-                const float2 f = *reinterpret_cast<const float2*>(sp);
-                s[q][0] = f.x, s[q][1] = f.y;
+        for (int q = 0; q < VN; ++q) {
+            const char* row = vrow[q] >= 0 ? (const char*)p.v + vrow[q] * p.ldv * es : nullptr;
+            if constexpr (VEC) {
+                const int bytes = row ? min(max(vleft * es, 0), 16) : 0;
+                async16(to + v_place(vr + q * VS, vc), bytes ? row + (int64_t)vcol * es : p.v, bytes);
+            } else if constexpr (!X8) {
+                load8<T, false>((const T*)row, vcol, row ? vleft : 0, held[q]);
             } else {
-                s[q][0] = *sp;
-            }
-            const float f = row < 0 ? 0.0f : X8 ? sc * __ldg(p.v_scale + row) : sc;
-#pragma unroll
-            for (int k = 0; k < JN; ++k) s[q][k] = row < 0 ? 0.0f : s[q][k] * f;
-        }
-        uint32_t x[4][4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q].pairs(p.int8, x[q]);
-        if constexpr (TF32) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {                  // rows 2 t + 8 h and 2 t + 1 + 8 h: k = t and t + 4
-                uint32_t ah[MT][4], al[MT][4];
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {          // e: rank half (e & 1), row (e >> 1)
-                        const float f = R == 8 ? (e & 1 ? 0.0f : s[2 * h + (e >> 1)][0]) : s[2 * h + (e >> 1)][2 * m + (e & 1) < JN ? 2 * m + (e & 1) : 0];
-                        ah[m][e] = tf32(f);
-                        al[m][e] = tf32(f - __uint_as_float(ah[m][e]));
-                    }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float2 f0 = Dt<M>::up2(x[2 * h][i >> 1]), f1 = Dt<M>::up2(x[2 * h + 1][i >> 1]);
-                    const uint32_t b0 = __float_as_uint(i & 1 ? f0.y : f0.x), b1 = __float_as_uint(i & 1 ? f1.y : f1.x);
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        mma8_tf32(acc[m][i], al[m], b0, b1);
-                        mma8_tf32(acc[m][i], ah[m], b0, b1);
-                    }
-                }
-            }
-        } else {
-            uint32_t ah[MT][4], am[MT][4], al[MT][4];
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {              // e: rank half (e & 1), rows 2 t + 8 (e >> 1) and the next
-                    const int k = R == 8 ? 0 : 2 * m + (e & 1) < JN ? 2 * m + (e & 1) : 0;
-                    if (R == 8 && (e & 1)) ah[m][e] = am[m][e] = al[m][e] = 0u;
-                    else split3(s[2 * (e >> 1)][k], s[2 * (e >> 1) + 1][k], ah[m][e], am[m][e], al[m][e]);
-                }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t b0 = pair_of(x[0][i >> 1], x[1][i >> 1], i & 1), b1 = pair_of(x[2][i >> 1], x[3][i >> 1], i & 1);
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    mma16<__nv_bfloat16>(acc[m][i], al[m], b0, b1);
-                    mma16<__nv_bfloat16>(acc[m][i], am[m], b0, b1);
-                    mma16<__nv_bfloat16>(acc[m][i], ah[m], b0, b1);
-                }
+                XPiece<T, true, false> lo, hi;
+                lo.load(row, vcol, vleft);
+                hi.load(row, vcol + 8, vleft - 8);
+                held[q][0] = lo.u[0], held[q][1] = lo.u[1], held[q][2] = hi.u[0], held[q][3] = hi.u[1];
             }
         }
-    }
-    // parts into shared memory, [rank][column]
-    float* mypart = part + tg * RT * 64;
+        if (s_mine) {
+#pragma unroll
+            for (int q = 0; q < SN; ++q)
+                async16(to + S::vbytes + (sr + q * SS) * (R * 4) + sp * 16, srow[q] >= 0 ? p.s + (int64_t)srow[q] * R + sp * 4 : p.s, srow[q] >= 0 ? 16 : 0);
+        }
+        if (X8 && tid < S::rows)
+            async4((uint32_t)__cvta_generic_to_shared(s_scale + buf * S::rows + tid), xrow >= 0 ? p.v_scale + xrow : p.v_scale, xrow >= 0 ? 4 : 0);
+    };
+    auto put_held = [&](int buf) {
+        if constexpr (!VEC) {
+#pragma unroll
+            for (int q = 0; q < VN; ++q)
+                *reinterpret_cast<uint4*>(smem + buf * S::stage + v_place(vr + q * VS, vc)) = make_uint4(held[q][0], held[q][1], held[q][2], held[q][3]);
+        }
+    };
+
+    float acc[MT][NT][4];
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {                      // rank half
-            if (R == 8 && e) continue;
-            const int j = R == 8 ? g : j0 + 2 * m + e;
+        for (int i = 0; i < NT; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
+    if (R == 8)                                            // ranks 8 .. 15 of the tile
+        for (int i = tid; i < S::parts * S::part / 4; i += kThreads) reinterpret_cast<uint32_t*>(s_part)[i] = 0u;
+    rows_of(st0);
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                const float4 lo4 = make_float4(acc[m][0][2 * e + c], acc[m][1][2 * e + c], acc[m][2][2 * e + c], acc[m][3][2 * e + c]);
-                const float4 hi4 = make_float4(acc[m][4][2 * e + c], acc[m][5][2 * e + c], acc[m][6][2 * e + c], acc[m][7][2 * e + c]);
-                float4* to = reinterpret_cast<float4*>(mypart + j * 64 + 8 * (2 * t + c));
-                to[0] = lo4;
-                to[1] = hi4;
+    for (int i = 0; i < S::stages - 1; ++i) {
+        if (st0 + i < st1) fetch(i);
+        async_commit();
+        if (st0 + i < st1) put_held(i);
+        rows_of(st0 + i + 1);
+    }
+    int buf = 0;
+    for (int st = st0; st < st1; ++st) {
+        async_wait<S::stages - 2>();
+        __syncthreads();                                   // the stage is there; the one before it and the parts are free
+        const int next = buf == 0 ? S::stages - 1 : buf - 1;
+        const bool more = st + S::stages - 1 < st1;
+        if (more) fetch(next);
+        async_commit();
+        rows_of(st + S::stages);
+        // s of the stage into [rank][row] parts: eight rows of a rank per thread
+        const float* ss = reinterpret_cast<const float*>(smem + buf * S::stage + S::vbytes);
+        for (int i = tid; i < 8 * R; i += kThreads) {
+            const int j = i % R, c = i / R;
+            float f[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                f[k] = ss[(8 * c + k) * R + j] * sc;
+                if (X8) f[k] *= s_scale[buf * S::rows + 8 * c + k];
+            }
+            if constexpr (S::tf32) {
+                uint32_t h[8], l[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    h[k] = tf32(f[k]);
+                    l[k] = tf32(f[k] - __uint_as_float(h[k]));
+                }
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    uint8_t* to = s_part + j * 256 + (((2 * c + q) ^ ((j & 7) << 1)) << 4);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
+                    *reinterpret_cast<uint4*>(to + S::part) = make_uint4(l[4 * q], l[4 * q + 1], l[4 * q + 2], l[4 * q + 3]);
+                }
+            } else {
+                uint4 h, m, l;
+                split3(f[0], f[1], h.x, m.x, l.x);
+                split3(f[2], f[3], h.y, m.y, l.y);
+                split3(f[4], f[5], h.z, m.z, l.z);
+                split3(f[6], f[7], h.w, m.w, l.w);
+                uint8_t* to = s_part + j * 128 + ((c ^ (j & 7)) << 4);
+                *reinterpret_cast<uint4*>(to) = h;
+                *reinterpret_cast<uint4*>(to + S::part) = m;
+                *reinterpret_cast<uint4*>(to + 2 * S::part) = l;
             }
         }
-    __syncthreads();
-    for (int i = tid; i < R * 16; i += kThreads) {
-        float4 v = reinterpret_cast<float4*>(part)[i];
+        __syncthreads();
+        const uint32_t vb = base + buf * S::stage;
 #pragma unroll
-        for (int k = 1; k < TG; ++k) {
-            const float4 q = reinterpret_cast<float4*>(part + k * RT * 64)[i];
-            v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+        for (int k0 = 0; k0 < S::rows / RG; k0 += 16) {
+            const int r0 = rg * (S::rows / RG) + k0;       // 16 rows of the stage
+            uint32_t b[NT][2];                             // pairs of rows (2 t, 2 t + 1) and (2 t + 8, 2 t + 9) of column g of the tile
+            if constexpr (!X8) {
+#pragma unroll
+                for (int i = 0; i < NT; i += 2) {
+                    uint32_t q[4];
+                    const int r = r0 + (lane & 15);
+                    ldmatrix4t(q, vb + v_place(r, cg * (WC / 8) + i + (lane >> 4)));
+                    b[i][0] = q[0], b[i][1] = q[1], b[i + 1][0] = q[2], b[i + 1][1] = q[3];
+                }
+            } else {                                       // tile i has column NT g + i at place g: NT codes of a row per lane
+                uint32_t x[4][(NT + 1) / 2];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int r = r0 + 2 * t + (q & 1) + 8 * (q >> 1), at = cg * WC + NT * g;
+                    const uint8_t* c = smem + buf * S::stage + v_place(r, at >> 4) + (at & 15);
+                    uint32_t w[2] = {0u, 0u};
+                    if constexpr (NT == 8) {
+                        const uint2 z = *reinterpret_cast<const uint2*>(c);
+                        w[0] = z.x, w[1] = z.y;
+                    } else if constexpr (NT == 4) {
+                        w[0] = *reinterpret_cast<const uint32_t*>(c);
+                    } else {
+                        w[0] = *reinterpret_cast<const unsigned short*>(c);
+                    }
+                    uint32_t lo, hi;
+                    values4<__nv_bfloat16>(w[0], p.int8, lo, hi);
+                    x[q][0] = lo;
+                    if constexpr (NT >= 4) x[q][1] = hi;
+                    if constexpr (NT == 8) {
+                        values4<__nv_bfloat16>(w[1], p.int8, lo, hi);
+                        x[q][2] = lo, x[q][3] = hi;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < NT; ++i) {
+                    b[i][0] = pair_of(x[0][i >> 1], x[1][i >> 1], i & 1);
+                    b[i][1] = pair_of(x[2][i >> 1], x[3][i >> 1], i & 1);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                if constexpr (S::tf32) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {          // rows 2 t + 8 h and the next: k = t and t + 4
+                        uint32_t f[2][4];
+#pragma unroll
+                        for (int q = 0; q < 2; ++q)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const int j = 16 * m + g + 8 * e, r = r0 + 2 * t + 8 * h;
+                                const uint2 z = *reinterpret_cast<const uint2*>(s_part + q * S::part + j * 256 + (((r >> 2) ^ ((j & 7) << 1)) << 4) + (r & 3) * 4);
+                                f[q][e] = z.x, f[q][2 + e] = z.y;
+                            }
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) {
+                            const float2 x = Dt<__half>::up2(b[i][h]);
+                            mma8_tf32(acc[m][i], f[1], __float_as_uint(x.x), __float_as_uint(x.y));
+                            mma8_tf32(acc[m][i], f[0], __float_as_uint(x.x), __float_as_uint(x.y));
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int q = 2; q >= 0; --q) {         // smallest part first
+                        uint32_t f[4];
+                        const int j = 16 * m + (lane & 15), c = (r0 >> 3) + (lane >> 4);
+                        ldmatrix4(f, part0 + q * S::part + j * 128 + ((c ^ (j & 7)) << 4));
+#pragma unroll
+                        for (int i = 0; i < NT; ++i) mma16<__nv_bfloat16>(acc[m][i], f, b[i][0], b[i][1]);
+                    }
+                }
+            }
         }
-        reinterpret_cast<float4*>(part)[i] = v;
+        if (more) put_held(next);
+        buf = buf == S::stages - 1 ? 0 : buf + 1;
+    }
+    async_wait<0>();
+    __syncthreads();
+    // the warps' sums into shared memory [row group][rank][column], over the stages
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = 16 * m + g + 8 * (e >> 1), c = cg * WC + (X8 ? NT * (2 * t + (e & 1)) + i : 8 * i + 2 * t + (e & 1));
+                sums[(rg * RT + j) * S::cols + c] = acc[m][i][e];
+            }
+    __syncthreads();
+    if (RG > 1) {
+        for (int i = tid; i < R * S::cols / 4; i += kThreads) {
+            float4 v = reinterpret_cast<float4*>(sums)[i];
+#pragma unroll
+            for (int k = 1; k < RG; ++k) {
+                const float4 q = reinterpret_cast<float4*>(sums + k * RT * S::cols)[i];
+                v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
+            }
+            reinterpret_cast<float4*>(sums)[i] = v;
+        }
     }
     if (size > 1) {
         cluster_arrive();
@@ -940,25 +1206,21 @@ __global__ void __launch_bounds__(kThreads, R >= 64 ? 1 : 2) lora_wgrad_kernel(c
     } else {
         __syncthreads();
     }
+    // each block adds and stores its share of the sums
     int i0, i1;
-    share_of(R * 16, rank, size, i0, i1);                  // each block adds and stores its share of the sums
-    for (int i = i0 + tid; i < i1; i += kThreads) {
-        if constexpr (TRANS) {                             // four ranks of one column
+    share_of(R * S::cols / 4, rank, size, i0, i1);
+    if constexpr (TRANS) {                                 // [column][rank]
+        for (int i = i0 + tid; i < i1; i += kThreads) {    // four ranks of one column
             const int c = i / (R / 4), j = 4 * (i % (R / 4));
             float f[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) f[k] = size > 1 ? remote1(part + (j + k) * 64 + c, 0) : part[(j + k) * 64 + c];
-            for (int b = 1; b < size; ++b)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) f[k] += remote1(part + (j + k) * 64 + c, b);
+            for (int k = 0; k < 4; ++k) f[k] = size > 1 ? cluster_sum1(sums + (j + k) * S::cols + c, size) : sums[(j + k) * S::cols + c];
             if (col0 + c < p.W) *reinterpret_cast<float4*>(p.out + ((int64_t)a * p.W + col0 + c) * R + j) = make_float4(f[0], f[1], f[2], f[3]);
-        } else {                                           // four columns of one rank
-            float4 v = size > 1 ? remote4(part + 4 * i, 0) : reinterpret_cast<float4*>(part)[i];
-            for (int b = 1; b < size; ++b) {
-                const float4 r = remote4(part + 4 * i, b);
-                v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
-            }
-            const int j = i / 16, c = col0 + 4 * (i % 16);
+        }
+    } else {
+        for (int i = i0 + tid; i < i1; i += kThreads) {    // four columns of one rank
+            const float4 v = size > 1 ? cluster_sum4(sums + 4 * i, size) : reinterpret_cast<float4*>(sums)[i];
+            const int j = i / (S::cols / 4), c = col0 + 4 * (i % (S::cols / 4));
             float* out = p.out + ((int64_t)a * R + j) * p.W + c;
             const float f[4] = {v.x, v.y, v.z, v.w};
             if (VEC) {
@@ -1052,16 +1314,16 @@ template <typename T, bool TRANS, bool VEC> static qmm_status launch_wgrad(const
         constexpr int R = decltype(rank)::value;
         auto go = [&](auto e8) {
             constexpr bool X8 = decltype(e8)::value;
-            constexpr int MT = R <= 32 ? 1 : 2, JG = R <= 16 ? 1 : R / (16 * MT), TG = kWarps / JG, RT = R < 16 ? 16 : R;
-            constexpr int smem = TG * RT * 64 * 4;
+            using S = WgradShape<T, X8, R>;
+            constexpr int smem = S::smem;
             static std::atomic<uint64_t> configured{0};
             auto kern = lora_wgrad_kernel<T, X8, R, TRANS, VEC>;
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter gradient attributes");
             if (s != QMM_OK) return s;
-            const int64_t columns = (int64_t)p.n * ((p.W + 63) / 64);
-            // blocks that share a column's rows: as many as have 128 rows each if one adapter had them all, while the launch stays a few waves
+            const int64_t columns = (int64_t)p.n * ((p.W + S::cols - 1) / S::cols);
+            // blocks that share a column's rows: 128 rows each at least if one adapter had them all, while the launch stays a few waves
             int size = 1;
-            while (size < 8 && columns * size < 8 * kNumSMs && (int64_t)p.T >= 256 * size) size *= 2;
+            while (size < 8 && columns * size < 4 * kNumSMs && (int64_t)p.T >= 256 * size) size *= 2;
             if (columns * size > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapter gradients: %lld blocks are too many for one launch", (long long)(columns * size));
             return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", p);
         };
