@@ -30,7 +30,7 @@ static qmm_status launch_pdl(void (*kern)(P...), dim3 grid, int threads, size_t 
     return check_cuda(cudaLaunchKernelEx(&cfg, kern, args...), what);
 }
 
-// Sets a kernel's attributes once per device: dynamic shared memory beyond 48 KB, clusters of more than eight blocks.
+// Sets a kernel's attributes once per device: dynamic shared memory that may pass 48 KB together with static arrays, clusters of more than eight blocks.
 // `configured`: one bit per device, a static of the caller's instantiation.
 template <typename K> static qmm_status configure_once(std::atomic<uint64_t>& configured, K kern, size_t smem, bool wide_cluster, const char* what)
 {
@@ -38,7 +38,7 @@ template <typename K> static qmm_status configure_once(std::atomic<uint64_t>& co
     if (cudaGetDevice(&dev) != cudaSuccess) dev = 0;
     const uint64_t bit = dev < 64 ? (1ull << dev) : 0;
     if (configured.load(std::memory_order_relaxed) & bit) return QMM_OK;
-    cudaError_t e = smem > 48 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+    cudaError_t e = smem > 32 * 1024 ? cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
     if (e == cudaSuccess && wide_cluster) e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return check_cuda(e, what);
     configured.fetch_or(bit, std::memory_order_relaxed);

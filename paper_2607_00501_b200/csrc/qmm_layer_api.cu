@@ -254,7 +254,7 @@ qmm_status qmm_lora(const qmm_lora_args* a, void* ws, size_t ws_bytes, void* str
     const int *order = nullptr, *offsets = nullptr, *units = nullptr;
     if (!small) QMM_TRY(lora_plan(a, l, (char*)ws, &order, &offsets, &units, st));
     const bool x8 = a->x_scale != nullptr, same = a->Y0 == a->Y && a->ldy0 == a->ldy;
-    const uintptr_t bits = (x8 ? pitch_bits(a->X, a->ldx, 1) * 2 : pitch_bits(a->X, a->ldx, 2)) | pitch_bits(a->A, a->K, 2) | pitch_bits(a->B, a->r, 2) |
+    const uintptr_t bits = pitch_bits(a->X, a->ldx, x8 ? 1 : 2) | pitch_bits(a->A, a->K, 2) | pitch_bits(a->B, a->r, 2) |
                            pitch_bits(a->Y0, a->ldy0, 2) | pitch_bits(a->Y, a->ldy, 2) | (uintptr_t)(a->N * 2);
     const lora::LoraP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, a->idx, order, offsets, units, a->T, a->n, (int)a->K, (int)a->N, a->A, a->B, a->scale,
                            a->Y0, a->ldy0, a->Y, a->ldy, a->S ? a->S : small ? nullptr : (float*)((char*)ws + l.s), 0, !same};

@@ -430,6 +430,10 @@ template <typename T, int LAY, bool VEC> struct YPiece {
             }
     }
 };
+// A stage of y0 in shared memory: 64 rows of kStageCols columns; 16-byte piece c of row r lies at place c ^ 4 (r % 2), so that two rows' shares of a column group do not meet in a bank.
+constexpr int kStageCols = 128, kStageBytes = kTileRows * kStageCols * 2;
+__device__ __forceinline__ uint32_t stage_place(int r, int c) { return (uint32_t)(r * (kStageCols * 2) + ((c ^ ((r & 1) << 2)) << 4)); }
+
 template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int left, const uint32_t (&u)[4])
 {
     if (VEC) {
@@ -452,10 +456,10 @@ template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int
     }
 }
 
-// y = rn(y0 + back * (u . w2)) for the 16 rows of tile m and one column group.
+// y = rn(y0 + back * (u . w2)) for the 16 rows of tile m and one column group; to: the lane's columns of rows g and g + 8 of the tile (null: none), `left` columns from there.
 template <typename T, int R, int LAY, bool VEC>
-__device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
-                                      T* y, int64_t ld, const int (&row)[2], int n, int N, int lane)
+__device__ __forceinline__ void widen_at(WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
+                                         T* const (&to)[2], int left, int lane)
 {
     using W = WideWeights<T, R, LAY, VEC>;
     constexpr int tiles = Wide<LAY>::tiles, steps = W::Block::steps;
@@ -488,7 +492,7 @@ __device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPie
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const float f = back[m * 16 + g + 8 * h];
-        if (row[h] < 0) continue;
+        if (!to[h]) continue;
 #pragma unroll
         for (int i = 0; i < YPiece<T, LAY, VEC>::regs; i += 4) {
             uint32_t o[4];
@@ -501,9 +505,37 @@ __device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPie
                 else c0 = acc[2 * k][2 * h + (i >> 2)], c1 = acc[2 * k + 1][2 * h + (i >> 2)];
                 o[k] = Dt<T>::down2(fmaf(f, c0, b.x), fmaf(f, c1, b.y));
             }
-            store8<T, VEC>(y + row[h] * ld + n + 2 * i, N - (n + 2 * i), o);
+            store8<T, VEC>(to[h] + 2 * i, left - 2 * i, o);
         }
     }
+}
+template <typename T, int R, int LAY, bool VEC>
+__device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPiece<T, LAY, VEC>& y0, const uint8_t* hi, const uint8_t* lo, const float* back, int m,
+                                      T* y, int64_t ld, const int (&row)[2], int n, int N, int lane)
+{
+    T* const to[2] = {row[0] >= 0 ? y + row[0] * ld + n : nullptr, row[1] >= 0 ? y + row[1] * ld + n : nullptr};
+    widen_at<T, R, LAY, VEC>(w, y0, hi, lo, back, m, to, N - n, lane);
+}
+
+// ------------------------------------------------------------------ copies into shared memory
+
+__device__ __forceinline__ void async16(uint32_t to, const void* from, int bytes)            // bytes < 16: the rest becomes zero
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void async4(uint32_t to, const void* from, int bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t at)
+{
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
 }
 
 // ------------------------------------------------------------------ kernels
@@ -746,17 +778,155 @@ __device__ __forceinline__ bool tile_rows(const LoraP& p, int tile, int lane, in
     return count > 0;
 }
 
+// Shapes of the narrowing product of a tile of 64 rows.  VEC: x and w1 come in stages of 128 elements of K.
+template <bool X8, int R, int LAY, bool VEC> struct NarrowShape {
+    static constexpr int MW = R <= 64 ? 2 : 1;             // row tiles of a warp
+    static constexpr int RG = kTileRows / 16 / MW, KP = kWarps / RG;          // row groups x shares of K
+    static constexpr int K = 128, chunks = K / 32 / KP;    // elements of a stage; 32-element chunks of a warp
+    static constexpr int xbytes = kTileRows * K * (X8 ? 1 : 2), wbytes = K * R * 2, stage = xbytes + wbytes;
+    static constexpr int stages = R <= 64 ? 3 : 2;
+    static constexpr int sums = KP * kTileRows * R * 4;
+    static constexpr int smem = VEC && stages * stage > sums ? stages * stage : sums;
+    static constexpr int blocks = R <= 32 ? 3 : 2;         // per SM, as registers and shared memory allow
+};
+
+// Places of 16-byte pieces in a stage: conflict-free both for eight rows' pieces at one k (ldmatrix) and for two rows' four neighbouring ones.
+__device__ __forceinline__ uint32_t piece_in_row(int r, int c) { return (uint32_t)((c ^ (((r & 1) << 2) | ((r >> 1) & 3))) << 4); }
+template <int R> __device__ __forceinline__ uint32_t piece_of_k(int k, int c)                 // row k of w1 [K, R]
+{
+    const int f = R >= 64 ? k & 7 : R == 32 ? (k >> 1) & 3 : R == 16 ? (k >> 2) & 1 : 0;
+    return (uint32_t)(k * 2 * R + ((c ^ f) << 4));
+}
+
+// acc += tile . w1 over the stages [st0, st1) of K, rows[64] in shared memory.
+template <typename T, bool X8, int R, int LAY>
+__device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R, LAY, true>::MW][R / 8][4], const LoraP& p, const T* __restrict__ w1, const int* rows, uint8_t* smem,
+                                              int st0, int st1)
+{
+    using S = NarrowShape<X8, R, LAY, true>;
+    constexpr int MW = S::MW;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int rg = warp % S::RG, kp = warp / S::RG;
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem);
+    constexpr int XP = X8 ? 8 : 16, XN = kTileRows * XP / kThreads, WN = 16 * R / kThreads ? 16 * R / kThreads : 1;      // pieces of a row of x; pieces of a thread
+    const int xr = tid / XP, xc = tid % XP;
+    const char* from[XN];
+#pragma unroll
+    for (int q = 0; q < XN; ++q) {
+        const int r = rows[xr + q * (kThreads / XP)];
+        from[q] = r >= 0 ? (const char*)p.x + (int64_t)r * p.ldx * (X8 ? 1 : 2) + 16 * xc : nullptr;
+    }
+    auto fetch = [&](int st, int buf) {
+        if (st < st1) {
+            const uint32_t to = base + buf * S::stage;
+            const int left = (p.K - st * S::K) * (X8 ? 1 : 2) - 16 * xc, bytes = min(max(left, 0), 16);
+#pragma unroll
+            for (int q = 0; q < XN; ++q) {
+                const int r = xr + q * (kThreads / XP);
+                const int n = from[q] ? bytes : 0;
+                const uint32_t at = X8 ? (uint32_t)(r * S::K + ((xc ^ ((r & 3) << 1)) << 4)) : (uint32_t)(r * 2 * S::K) + piece_in_row(r, xc);
+                async16(to + at, n ? from[q] + (int64_t)st * (S::K * (X8 ? 1 : 2)) : (const char*)p.x, n);
+            }
+#pragma unroll
+            for (int q = 0; q < WN; ++q) {
+                const int i = tid + q * kThreads;
+                if (16 * R < kThreads && i >= 16 * R) break;
+                if constexpr (LAY == 0) {
+                    const int r = i / 16, c = i % 16, k = st * S::K + 8 * c;
+                    const int n = k < p.K ? 16 : 0;
+                    async16(to + S::xbytes + r * 2 * S::K + piece_in_row(r, c), n ? w1 + (int64_t)r * p.K + k : w1, n);
+                } else {
+                    constexpr int C = R / 8;
+                    const int r = i / C, c = i % C, k = st * S::K + r;
+                    const int n = k < p.K ? 16 : 0;
+                    async16(to + S::xbytes + piece_of_k<R>(r, c), n ? w1 + (int64_t)k * R + 8 * c : w1, n);
+                }
+            }
+        }
+        async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S::stages - 1; ++i) fetch(st0 + i, i);
+    int buf = 0;
+    for (int st = st0; st < st1; ++st) {
+        async_wait<S::stages - 2>();
+        __syncthreads();                                   // the stage is there; the one before it is free
+        fetch(st + S::stages - 1, buf == 0 ? S::stages - 1 : buf - 1);
+        const uint8_t* xs = smem + buf * S::stage;
+        const uint32_t xb = base + buf * S::stage, wb = xb + S::xbytes;
+#pragma unroll
+        for (int ch = 0; ch < S::chunks; ++ch) {
+            const int c32 = kp * S::chunks + ch;           // 32 elements: pieces 4 c32 .. 4 c32 + 3 of a 16-bit row
+            if constexpr (LAY == 0) {                      // lane's elements 8 t .. 8 t + 7 of the chunk, as in narrow()
+                uint32_t a[MW][2][4];
+#pragma unroll
+                for (int m = 0; m < MW; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int r = (rg * MW + m) * 16 + g + 8 * h;
+                        if constexpr (X8) {
+                            XPiece<T, true, true> x;
+                            const uint2 q = *reinterpret_cast<const uint2*>(xs + r * S::K + (((2 * c32 + (t >> 1)) ^ ((r & 3) << 1)) << 4) + 8 * (t & 1));
+                            x.u[0] = q.x, x.u[1] = q.y;
+                            x.pairs(p.int8, a[m][h]);
+                        } else {
+                            const uint4 q = *reinterpret_cast<const uint4*>(xs + r * 2 * S::K + piece_in_row(r, 4 * c32 + t));
+                            a[m][h][0] = q.x, a[m][h][1] = q.y, a[m][h][2] = q.z, a[m][h][3] = q.w;
+                        }
+                    }
+#pragma unroll
+                for (int i = 0; i < R / 8; ++i) {
+                    const int r = 8 * i + g;
+                    const uint4 q = *reinterpret_cast<const uint4*>(xs + S::xbytes + r * 2 * S::K + piece_in_row(r, 4 * c32 + t));
+                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int m = 0; m < MW; ++m)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            const uint32_t f[4] = {a[m][0][2 * j], a[m][1][2 * j], a[m][0][2 * j + 1], a[m][1][2 * j + 1]};
+                            mma16<T>(acc[m][i], f, w[2 * j], w[2 * j + 1]);
+                        }
+                }
+            } else {                                       // fragments in the MMA's own order; accumulator tile i has ranks 8 i .. 8 i + 7
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    uint32_t a[MW][4];
+#pragma unroll
+                    for (int m = 0; m < MW; ++m) {
+                        const int r = (rg * MW + m) * 16 + (lane & 15);
+                        ldmatrix4(a[m], xb + r * 2 * S::K + piece_in_row(r, 4 * c32 + 2 * j + (lane >> 4)));
+                    }
+                    const int k = 32 * c32 + 16 * j + (lane & 15);
+#pragma unroll
+                    for (int i = 0; i < R / 8; i += 2) {
+                        uint32_t b[4];
+                        ldmatrix4t(b, wb + piece_of_k<R>(k, R == 8 ? 0 : i + (lane >> 4)));
+#pragma unroll
+                        for (int m = 0; m < MW; ++m) {
+                            mma16<T>(acc[m][i], a[m], b[0], b[1]);
+                            if constexpr (R > 8) mma16<T>(acc[m][i + 1], a[m], b[2], b[3]);
+                        }
+                    }
+                }
+            }
+        }
+        buf = buf == S::stages - 1 ? 0 : buf + 1;
+    }
+    async_wait<0>();
+    __syncthreads();
+}
+
 // The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
-// Bound by HBM (x once); w1 comes from L1 and L2.
+// Bound by HBM (x once); w1 comes from L2.
 template <typename T, bool X8, int R, int LAY, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) lora_narrow_kernel(const LoraP p)
+__global__ void __launch_bounds__(kThreads, NarrowShape<X8, R, LAY, VEC>::blocks) lora_narrow_kernel(const LoraP p)
 {
     pdl_launch_dependents();
     pdl_wait();
-    constexpr int MW = R <= 64 ? 2 : 1;                    // row tiles of a warp
-    constexpr int RG = kTileRows / 16 / MW, KP = kWarps / RG;                  // row groups x shares of the block's K
+    using S = NarrowShape<X8, R, LAY, VEC>;
+    constexpr int MW = S::MW, RG = S::RG, KP = S::KP;
     extern __shared__ __align__(16) uint8_t smem[];
-    float* part = reinterpret_cast<float*>(smem);          // [KP][64][R]; share 0 holds the block's sum in the end
+    float* part = reinterpret_cast<float*>(smem);          // [KP][64][R], over the stages; share 0 holds the block's sum in the end
     __shared__ int rows[kTileRows];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_rank(), size = (int)cluster_size();
@@ -769,26 +939,34 @@ __global__ void __launch_bounds__(kThreads, 2) lora_narrow_kernel(const LoraP p)
     }
     __syncthreads();
     const int g = lane >> 2, rg = warp % RG, kp = warp / RG;
-    const char* xb = (const char*)p.x;
-    const void* xr[MW][2];
-#pragma unroll
-    for (int m = 0; m < MW; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int r = rows[(rg * MW + m) * 16 + g + 8 * h];
-            xr[m][h] = r >= 0 ? xb + r * p.ldx * (X8 ? 1 : 2) : nullptr;
-        }
-    int c0, c1;
-    share_of((p.K + 31) / 32, rank, size, c0, c1);
+    const T* w1 = (const T*)p.w1 + (int64_t)a * R * p.K;
     float acc[MW][R / 8][4];
 #pragma unroll
     for (int m = 0; m < MW; ++m)
 #pragma unroll
         for (int i = 0; i < R / 8; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
-    if ((rg * MW) * 16 < count)
-        narrow<T, X8, R, LAY, VEC, MW>(acc, *reinterpret_cast<const void* const(*)[MW][2]>(&xr), (const T*)p.w1 + (int64_t)a * R * p.K, p.K, p.int8, c0 + kp, c1, KP, lane);
+    int c0, c1;
+    if constexpr (VEC) {
+        share_of((p.K + S::K - 1) / S::K, rank, size, c0, c1);
+        narrow_stages<T, X8, R, LAY>(acc, p, w1, rows, smem, c0, c1);
+    } else {
+        const char* xb = (const char*)p.x;
+        const void* xr[MW][2];
 #pragma unroll
-    for (int m = 0; m < MW; ++m) put_narrow<R, LAY>(acc[m], part + (kp * kTileRows + (rg * MW + m) * 16) * R, lane);
+        for (int m = 0; m < MW; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = rows[(rg * MW + m) * 16 + g + 8 * h];
+                xr[m][h] = r >= 0 ? xb + r * p.ldx * (X8 ? 1 : 2) : nullptr;
+            }
+        share_of((p.K + 31) / 32, rank, size, c0, c1);
+        if ((rg * MW) * 16 < count)
+            narrow<T, X8, R, LAY, VEC, MW>(acc, *reinterpret_cast<const void* const(*)[MW][2]>(&xr), w1, p.K, p.int8, c0 + kp, c1, KP, lane);
+    }
+    // accumulator columns: as narrow() has them, or, from stages with LAY 1, plain
+    constexpr int ORDER = VEC ? 0 : LAY;
+#pragma unroll
+    for (int m = 0; m < MW; ++m) put_narrow<R, ORDER>(acc[m], part + (kp * kTileRows + (rg * MW + m) * 16) * R, lane);
     __syncthreads();
     for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
         float4 v = reinterpret_cast<float4*>(part)[i];
@@ -823,7 +1001,8 @@ __global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, 
 {
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ __align__(16) uint8_t hi[kTileRows * u_pitch<R>], lo[kTileRows * u_pitch<R>];
+    extern __shared__ __align__(16) uint8_t smem[];
+    uint8_t *hi = smem, *lo = smem + kTileRows * u_pitch<R>, *stages = smem + 2 * kTileRows * u_pitch<R>;        // (stages: VEC alone)
     __shared__ float back[kTileRows];
     __shared__ int rows[kTileRows];
     constexpr int G = Wide<LAY>::cols;
@@ -861,39 +1040,96 @@ __global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, 
     const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
     const int g = lane >> 2, t = lane & 3, own = Wide<LAY>::own * t;
     const int last = min((span + 1) * per_span, groups);
-    // a column group in phases of HM row tiles; the next phase's y0 (and the next group's weights, where registers allow) is on its way during the products of this one
-    constexpr int HM = LAY == 0 ? 2 : 1, PH = 4 / HM;
-    constexpr bool AHEAD = LAY == 0 ? R <= 32 : R <= 16;
     using W = WideWeights<T, R, LAY, VEC>;
-    YPiece<T, LAY, VEC> y0[2][HM];
-    W w;
-    auto load_y = [&](int c, int ph, YPiece<T, LAY, VEC> (&y)[HM]) {
-#pragma unroll
-        for (int m = 0; m < HM; ++m) {
-            const int at = (ph * HM + m) * 16 + g, row[2] = {c < last ? rows[at] : -1, c < last ? rows[at + 8] : -1};
-            y[m].load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
-        }
-    };
-    int c = span * per_span + warp;
-    load_y(c, 0, y0[0]);
-    if (AHEAD && c < last) w.load(w2, c * G, p.N, lane);
-    for (; c < last; c += kWarps) {
-        if (!AHEAD) w.load(w2, c * G, p.N, lane);
-        W next;
-#pragma unroll
-        for (int ph = 0; ph < PH; ++ph) {
-            if (ph + 1 < PH) load_y(c, ph + 1, y0[(ph + 1) & 1]);
-            else load_y(c + kWarps, 0, y0[(ph + 1) & 1]);
-            if (AHEAD && ph == PH - 1 && c + kWarps < last) next.load(w2, (c + kWarps) * G, p.N, lane);
+    if constexpr (!VEC) {
+        // a column group in phases of HM row tiles; the next phase's y0 is on its way during the products of this one
+        constexpr int HM = LAY == 0 ? 2 : 1, PH = 4 / HM;
+        YPiece<T, LAY, VEC> y0[2][HM];
+        W w;
+        auto load_y = [&](int c, int ph, YPiece<T, LAY, VEC> (&y)[HM]) {
 #pragma unroll
             for (int m = 0; m < HM; ++m) {
-                const int mt = ph * HM + m;
-                if (mt * 16 >= count) continue;
-                const int row[2] = {rows[mt * 16 + g], rows[mt * 16 + g + 8]};
-                widen<T, R, LAY, VEC>(w, y0[ph & 1][m], hi, lo, back, mt, (T*)p.y, p.ldy, row, c * G + own, p.N, lane);
+                const int at = (ph * HM + m) * 16 + g, row[2] = {c < last ? rows[at] : -1, c < last ? rows[at + 8] : -1};
+                y[m].load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
+            }
+        };
+        int c = span * per_span + warp;
+        load_y(c, 0, y0[0]);
+        for (; c < last; c += kWarps) {
+            w.load(w2, c * G, p.N, lane);
+#pragma unroll
+            for (int ph = 0; ph < PH; ++ph) {
+                if (ph + 1 < PH) load_y(c, ph + 1, y0[(ph + 1) & 1]);
+                else load_y(c + kWarps, 0, y0[(ph + 1) & 1]);
+#pragma unroll
+                for (int m = 0; m < HM; ++m) {
+                    const int mt = ph * HM + m;
+                    if (mt * 16 >= count) continue;
+                    const int row[2] = {rows[mt * 16 + g], rows[mt * 16 + g + 8]};
+                    widen<T, R, LAY, VEC>(w, y0[ph & 1][m], hi, lo, back, mt, (T*)p.y, p.ldy, row, c * G + own, p.N, lane);
+                }
             }
         }
-        if (AHEAD) w = next;
+    } else {
+        // y0 comes in stages of 64 rows x 128 columns, three in flight (cp.async: whole 256-byte pieces of rows); a warp takes one column group of a stage and MU of its row tiles
+        constexpr int GS = kStageCols / G, MU = GS * 4 / kWarps;               // groups of a stage; row tiles of a warp
+        const int cw = warp % GS, m0 = warp / GS * MU;
+        const int s0 = span * per_span / GS, s1 = (last + GS - 1) / GS;       // (per_span is a multiple of GS)
+        const int fr = tid >> 4, fc = tid & 15;            // piece fc of rows fr + 16 q
+        const T* from[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int r = rows[fr + 16 * q];
+            from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 + 8 * fc : nullptr;
+        }
+        T* to[MU][2];
+#pragma unroll
+        for (int m = 0; m < MU; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = rows[(m0 + m) * 16 + g + 8 * h];
+                to[m][h] = r >= 0 ? (T*)p.y + (int64_t)r * p.ldy + cw * G + own : nullptr;
+            }
+        const uint32_t base = (uint32_t)__cvta_generic_to_shared(stages);
+        auto fetch = [&](int st, int buf) {
+            if (st < s1) {
+                const bool there = st * kStageCols + 8 * fc < p.N;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bool in = there && from[q];
+                    async16(base + buf * kStageBytes + stage_place(fr + 16 * q, fc), in ? (const void*)(from[q] + (int64_t)st * kStageCols) : p.w2, in ? 16 : 0);
+                }
+            }
+            async_commit();
+        };
+        fetch(s0, 0);
+        fetch(s0 + 1, 1);
+        W w, next;
+        next.load(w2, s0 * kStageCols + cw * G, p.N, lane);
+        int buf = 0;
+        for (int st = s0; st < s1; ++st) {
+            w = next;
+            if (st + 1 < s1) next.load(w2, (st + 1) * kStageCols + cw * G, p.N, lane);
+            async_wait<1>();
+            __syncthreads();                               // the stage is there; the one before it is free
+            fetch(st + 2, buf == 0 ? 2 : buf - 1);
+            const int n = st * kStageCols + cw * G + own;
+#pragma unroll
+            for (int m = 0; m < MU; ++m) {
+                if ((m0 + m) * 16 >= count) continue;
+                YPiece<T, LAY, VEC> y0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < YPiece<T, LAY, VEC>::regs; i += 4) {
+                        const uint4 q = *reinterpret_cast<const uint4*>(stages + buf * kStageBytes + stage_place((m0 + m) * 16 + g + 8 * h, (cw * G + own) / 8 + i / 4));
+                        y0.u[h][i] = q.x, y0.u[h][i + 1] = q.y, y0.u[h][i + 2] = q.z, y0.u[h][i + 3] = q.w;
+                    }
+                T* const at[2] = {to[m][0] ? to[m][0] + (int64_t)st * kStageCols : nullptr, to[m][1] ? to[m][1] + (int64_t)st * kStageCols : nullptr};
+                widen_at<T, R, LAY, VEC>(w, y0, hi, lo, back, m0 + m, at, p.N - n, lane);
+            }
+            buf = buf == 2 ? 0 : buf + 1;
+        }
     }
 }
 
@@ -910,25 +1146,6 @@ struct WgradP {
     int T, n, W;
     float* out;                                            // [n, R, W] or, TRANS, [n, W, R]
 };
-
-__device__ __forceinline__ void async16(uint32_t to, const void* from, int bytes)            // bytes < 16: the rest becomes zero
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void async4(uint32_t to, const void* from, int bytes)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void ldmatrix4t(uint32_t (&r)[4], uint32_t at)
-{
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
 
 // out[a] = sum over the adapter's rows of s (R) x v (W).  A block takes 128 columns of one adapter and 64 rows a stage, two or three stages in flight (cp.async); the blocks of a
 // cluster share the rows.  A warp has all R ranks of 64, 32 or 16 columns (R x columns = 2048 where R >= 32: 64 accumulators a lane), the warps of a column group share the stage's
@@ -1284,8 +1501,7 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
                 const int size = cluster_for(pieces, p.T <= 4 ? 16 : 8);
                 return launch_pdl(kern, dim3((unsigned)(p.T * size)), kThreads, smem, size, st, "adapter launch", p);
             }
-            constexpr int MW = R <= 64 ? 2 : 1, KP = kWarps / (kTileRows / 16 / MW);
-            constexpr int smem = KP * kTileRows * R * 4;
+            constexpr int smem = NarrowShape<X8, R, LAY, VEC>::smem;
             static std::atomic<uint64_t> configured{0};
             auto kern = lora_narrow_kernel<T, X8, R, LAY, VEC>;
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
@@ -1300,11 +1516,18 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
         else s = narrowed(std::false_type());
         if (s != QMM_OK || p.T <= kSmallRows || !p.y) return s;
         const int groups = (p.N + G - 1) / G;
-        const int per_span = groups < 4 * kWarps ? ((groups + kWarps - 1) / kWarps) * kWarps : 4 * kWarps;
+        // column groups of a block: 1024 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns)
+        int per_span = 1024 / G;
+        while (per_span > 256 / G && (int64_t)((p.T + kTileRows - 1) / kTileRows) * ((groups + per_span - 1) / per_span) < 2 * kNumSMs) per_span /= 2;
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
         if (blocks + rest > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapters: %lld blocks are too many for one launch", (long long)(blocks + rest));
-        return launch_pdl(lora_widen_kernel<T, R, LAY, VEC>, dim3((unsigned)(blocks + rest)), kThreads, 0, 1, st, "adapter widening launch", p, spans, per_span, (int)blocks);
+        constexpr int smem = 2 * kTileRows * u_pitch<R> + (VEC ? 3 * kStageBytes : 0);
+        static std::atomic<uint64_t> configured{0};
+        auto kern = lora_widen_kernel<T, R, LAY, VEC>;
+        s = configure_once(configured, kern, smem, false, "adapter attributes");
+        if (s != QMM_OK) return s;
+        return launch_pdl(kern, dim3((unsigned)(blocks + rest)), kThreads, smem, 1, st, "adapter widening launch", p, spans, per_span, (int)blocks);
     });
 }
 
