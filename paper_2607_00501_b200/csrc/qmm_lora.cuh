@@ -40,6 +40,18 @@ template <typename T> __device__ __forceinline__ void mma16(float (&d)[4], const
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+// d = a . b
+template <typename T> __device__ __forceinline__ void mma16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if constexpr (std::is_same<T, __half>::value)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                     : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                     : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ void mma8_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -430,10 +442,6 @@ template <typename T, int LAY, bool VEC> struct YPiece {
             }
     }
 };
-// A stage of y0 in shared memory: 64 rows of kStageCols columns; 16-byte piece c of row r lies at place c ^ 4 (r % 2), so that two rows' shares of a column group do not meet in a bank.
-constexpr int kStageCols = 128, kStageBytes = kTileRows * kStageCols * 2;
-__device__ __forceinline__ uint32_t stage_place(int r, int c) { return (uint32_t)(r * (kStageCols * 2) + ((c ^ ((r & 1) << 2)) << 4)); }
-
 template <typename T, bool VEC> __device__ __forceinline__ void store8(T* p, int left, const uint32_t (&u)[4])
 {
     if (VEC) {
@@ -757,9 +765,10 @@ __device__ __forceinline__ int find_part(const int* __restrict__ starts, int n, 
     // 32 samples, then the 32 (at most 33) numbers from the last sample that is not above v
     const int stride = (n + 32) / 32;
     const int at = min(lane * stride, n);
-    const unsigned below = __ballot_sync(0xFFFFFFFFu, __ldg(starts + at) <= v);
+    const unsigned below = __ballot_sync(0xFFFFFFFFu, __ldg(starts + at) <= v && lane * stride < n);
     const int from = (31 - __clz(below | 1u)) * stride;
     int found = from;
+    if (stride == 1) return found;
     for (int o = 0; o < stride; o += 32) {
         const int i = from + o + lane;
         const unsigned m = __ballot_sync(0xFFFFFFFFu, i < n && o + lane < stride && __ldg(starts + min(i, n)) <= v);
@@ -995,9 +1004,161 @@ __global__ void __launch_bounds__(kThreads, NarrowShape<X8, R, LAY, VEC>::blocks
     cluster_wait();
 }
 
+// Stages of the widening product: 64 rows x 128 columns of y0 and the weights of these columns.
+template <int R, int LAY> struct WideShape {
+    static constexpr int cols = 128;
+    static constexpr int ybytes = kTileRows * cols * 2, wbytes = cols * R * 2, stage = ybytes + wbytes;
+    static constexpr int stages = R <= 16 ? 3 : 2;
+    static constexpr int blocks = R <= 32 ? 3 : R <= 64 ? 2 : 1;              // per SM
+};
+// 16-byte piece c of row r of y0 lies at place c ^ 4 (r % 2), so that two rows' shares of a column group do not meet in a bank.
+__device__ __forceinline__ uint32_t y_place(int r, int c) { return (uint32_t)(r * 256 + ((c ^ ((r & 1) << 2)) << 4)); }
+
+// y = rn(y0 + back * (u . w2)) over the stages [s0, s1) of 128 columns.  y0 and w2 come by cp.async in whole pieces of rows; a warp takes one column group of a stage and MU of its
+// row tiles, and stores y from its fragments.
+template <typename T, int R, int LAY>
+__device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict__ w2, const int* rows, const uint8_t* hi, const uint8_t* lo, const float* back, uint8_t* stages,
+                                             int count, int s0, int s1)
+{
+    using S = WideShape<R, LAY>;
+    constexpr int G = Wide<LAY>::cols, GS = S::cols / G, MU = GS * 4 / kWarps, tiles = Wide<LAY>::tiles, steps = R < 16 ? 1 : R / 16;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
+    const int cw = warp % GS, m0 = warp / GS * MU;
+    const int fr = tid >> 4, fc = tid & 15;                // piece fc of rows fr + 16 q of y0
+    const T* from[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = rows[fr + 16 * q];
+        from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 + 8 * fc : nullptr;
+    }
+    T* to[MU][2];
+    float factor[MU][2];
+#pragma unroll
+    for (int m = 0; m < MU; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = (m0 + m) * 16 + g + 8 * h, r = rows[at];
+            to[m][h] = r >= 0 ? (T*)p.y + (int64_t)r * p.ldy + cw * G + Wide<LAY>::own * t : nullptr;
+            factor[m][h] = back[at];
+        }
+    const uint32_t base = (uint32_t)__cvta_generic_to_shared(stages);
+    auto fetch = [&](int st, int buf) {
+        if (st < s1) {
+            const uint32_t at = base + buf * S::stage;
+            const int n0 = st * S::cols;
+            const bool there = n0 + 8 * fc < p.N;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const bool in = there && from[q];
+                async16(at + y_place(fr + 16 * q, fc), in ? (const void*)(from[q] + n0) : w2, in ? 16 : 0);
+            }
+            constexpr int WN = 16 * R / kThreads ? 16 * R / kThreads : 1;     // pieces of w2 of a thread
+#pragma unroll
+            for (int q = 0; q < WN; ++q) {
+                const int i = tid + q * kThreads;
+                if (16 * R < kThreads && i >= 16 * R) break;
+                if constexpr (LAY == 0) {                  // row n of 2 R bytes, at the row that its fragment has: column c of tile i of a group at 8 i + c
+                    constexpr int C = R / 8;
+                    const int n = i / C, c = i % C, at_row = (n & ~31) + ((n & 6) << 2) + ((n >> 3 & 3) << 1) + (n & 1);
+                    const bool in = n0 + n < p.N;
+                    async16(at + S::ybytes + piece_of_k<R>(at_row, c), in ? w2 + (int64_t)(n0 + n) * R + 8 * c : w2, in ? 16 : 0);
+                } else {                                   // rank j, 128 columns
+                    const int j = i / 16, c = i % 16;
+                    const bool in = n0 + 8 * c < p.N;
+                    async16(at + S::ybytes + j * 256 + ((c ^ (((j >> 1) & 3) << 1)) << 4), in ? w2 + (int64_t)j * p.N + n0 + 8 * c : w2, in ? 16 : 0);
+                }
+            }
+        }
+        async_commit();
+    };
+#pragma unroll
+    for (int i = 0; i < S::stages - 1; ++i) fetch(s0 + i, i);
+    int buf = 0;
+    for (int st = s0; st < s1; ++st) {
+        async_wait<S::stages - 2>();
+        __syncthreads();                                   // the stage is there; the one before it is free
+        fetch(st + S::stages - 1, buf == 0 ? S::stages - 1 : buf - 1);
+        const uint8_t* ys = stages + buf * S::stage;
+        const uint32_t ws = base + buf * S::stage + S::ybytes;
+        float acc[MU][tiles][4];
+#pragma unroll
+        for (int s = 0; s < steps; ++s) {
+            uint32_t b[tiles][2];
+            if constexpr (LAY == 0 && R == 8) {            // one piece per row: two tiles' rows at a time, their missing ranks zero
+#pragma unroll
+                for (int i = 0; i < 4; i += 4) {
+                    uint32_t q[4];
+                    ldmatrix4(q, ws + piece_of_k<8>(32 * cw + lane, 0));
+                    b[0][0] = q[0], b[1][0] = q[1], b[2][0] = q[2], b[3][0] = q[3];
+                    b[0][1] = b[1][1] = b[2][1] = b[3][1] = 0u;
+                }
+            } else if constexpr (LAY == 0) {
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    uint32_t q[4];
+                    ldmatrix4(q, ws + piece_of_k<R>(32 * cw + 8 * i + (lane & 7) + 8 * (lane >> 4), 2 * s + ((lane >> 3) & 1)));
+                    b[i][0] = q[0], b[i][1] = q[1], b[i + 1][0] = q[2], b[i + 1][1] = q[3];
+                }
+            } else {
+                uint32_t u[4][4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = 16 * s + 2 * t + (k & 1) + 8 * (k >> 1);
+                    uint4 q = make_uint4(0u, 0u, 0u, 0u);
+                    if (R >= 16 || k < 2) q = *reinterpret_cast<const uint4*>(ys + S::ybytes + j * 256 + (((8 * cw + g) ^ (((j >> 1) & 3) << 1)) << 4));
+                    u[k][0] = q.x, u[k][1] = q.y, u[k][2] = q.z, u[k][3] = q.w;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    b[i][0] = pair_of(u[0][i >> 1], u[1][i >> 1], i & 1);
+                    b[i][1] = pair_of(u[2][i >> 1], u[3][i >> 1], i & 1);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < MU; ++m) {
+                if ((m0 + m) * 16 >= count) continue;
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {     // the low part first
+                    uint32_t a[4];
+                    get_u<R, 1>(part ? hi : lo, m0 + m, s, lane, a);          // (ranks in the MMA's own order)
+#pragma unroll
+                    for (int i = 0; i < tiles; ++i) {
+                        if (s == 0 && part == 0) mma16_first<T>(acc[m][i], a, b[i][0], b[i][1]);
+                        else mma16<T>(acc[m][i], a, b[i][0], b[i][1]);
+                    }
+                }
+            }
+        }
+        const int n0 = st * S::cols, left = p.N - (n0 + cw * G + Wide<LAY>::own * t);
+#pragma unroll
+        for (int m = 0; m < MU; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!to[m][h]) continue;
+                const float2 f = both(factor[m][h]);
+#pragma unroll
+                for (int v = 0; v < Wide<LAY>::own; v += 8) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(ys + y_place((m0 + m) * 16 + g + 8 * h, (cw * G + Wide<LAY>::own * t + v) >> 3));
+                    const uint32_t y0[4] = {q.x, q.y, q.z, q.w};
+                    uint32_t o[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        float2 c;
+                        if constexpr (LAY == 0) c = make_float2(acc[m][k][2 * h], acc[m][k][2 * h + 1]);
+                        else c = make_float2(acc[m][2 * k][2 * h + (v >> 3)], acc[m][2 * k + 1][2 * h + (v >> 3)]);
+                        const float2 r = fma2(f, c, Dt<T>::up2(y0[k]));
+                        o[k] = Dt<T>::down2(r.x, r.y);
+                    }
+                    if (left > v) *reinterpret_cast<uint4*>(to[m][h] + n0 + v) = make_uint4(o[0], o[1], o[2], o[3]);
+                }
+            }
+        buf = buf == S::stages - 1 ? 0 : buf + 1;
+    }
+}
+
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
 template <typename T, int R, int LAY, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
+__global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : 2) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -1071,65 +1232,7 @@ __global__ void __launch_bounds__(kThreads, 2) lora_widen_kernel(const LoraP p, 
             }
         }
     } else {
-        // y0 comes in stages of 64 rows x 128 columns, three in flight (cp.async: whole 256-byte pieces of rows); a warp takes one column group of a stage and MU of its row tiles
-        constexpr int GS = kStageCols / G, MU = GS * 4 / kWarps;               // groups of a stage; row tiles of a warp
-        const int cw = warp % GS, m0 = warp / GS * MU;
-        const int s0 = span * per_span / GS, s1 = (last + GS - 1) / GS;       // (per_span is a multiple of GS)
-        const int fr = tid >> 4, fc = tid & 15;            // piece fc of rows fr + 16 q
-        const T* from[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int r = rows[fr + 16 * q];
-            from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 + 8 * fc : nullptr;
-        }
-        T* to[MU][2];
-#pragma unroll
-        for (int m = 0; m < MU; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rows[(m0 + m) * 16 + g + 8 * h];
-                to[m][h] = r >= 0 ? (T*)p.y + (int64_t)r * p.ldy + cw * G + own : nullptr;
-            }
-        const uint32_t base = (uint32_t)__cvta_generic_to_shared(stages);
-        auto fetch = [&](int st, int buf) {
-            if (st < s1) {
-                const bool there = st * kStageCols + 8 * fc < p.N;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const bool in = there && from[q];
-                    async16(base + buf * kStageBytes + stage_place(fr + 16 * q, fc), in ? (const void*)(from[q] + (int64_t)st * kStageCols) : p.w2, in ? 16 : 0);
-                }
-            }
-            async_commit();
-        };
-        fetch(s0, 0);
-        fetch(s0 + 1, 1);
-        W w, next;
-        next.load(w2, s0 * kStageCols + cw * G, p.N, lane);
-        int buf = 0;
-        for (int st = s0; st < s1; ++st) {
-            w = next;
-            if (st + 1 < s1) next.load(w2, (st + 1) * kStageCols + cw * G, p.N, lane);
-            async_wait<1>();
-            __syncthreads();                               // the stage is there; the one before it is free
-            fetch(st + 2, buf == 0 ? 2 : buf - 1);
-            const int n = st * kStageCols + cw * G + own;
-#pragma unroll
-            for (int m = 0; m < MU; ++m) {
-                if ((m0 + m) * 16 >= count) continue;
-                YPiece<T, LAY, VEC> y0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < YPiece<T, LAY, VEC>::regs; i += 4) {
-                        const uint4 q = *reinterpret_cast<const uint4*>(stages + buf * kStageBytes + stage_place((m0 + m) * 16 + g + 8 * h, (cw * G + own) / 8 + i / 4));
-                        y0.u[h][i] = q.x, y0.u[h][i + 1] = q.y, y0.u[h][i + 2] = q.z, y0.u[h][i + 3] = q.w;
-                    }
-                T* const at[2] = {to[m][0] ? to[m][0] + (int64_t)st * kStageCols : nullptr, to[m][1] ? to[m][1] + (int64_t)st * kStageCols : nullptr};
-                widen_at<T, R, LAY, VEC>(w, y0, hi, lo, back, m0 + m, at, p.N - n, lane);
-            }
-            buf = buf == 2 ? 0 : buf + 1;
-        }
+        widen_stages<T, R, LAY>(p, w2, rows, hi, lo, back, stages, count, span * per_span / (WideShape<R, LAY>::cols / G), (last * G + WideShape<R, LAY>::cols - 1) / WideShape<R, LAY>::cols);
     }
 }
 
@@ -1522,7 +1625,7 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
         if (blocks + rest > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapters: %lld blocks are too many for one launch", (long long)(blocks + rest));
-        constexpr int smem = 2 * kTileRows * u_pitch<R> + (VEC ? 3 * kStageBytes : 0);
+        constexpr int smem = 2 * kTileRows * u_pitch<R> + (VEC ? WideShape<R, LAY>::stages * WideShape<R, LAY>::stage : 0);
         static std::atomic<uint64_t> configured{0};
         auto kern = lora_widen_kernel<T, R, LAY, VEC>;
         s = configure_once(configured, kern, smem, false, "adapter attributes");
@@ -1544,9 +1647,9 @@ template <typename T, bool TRANS, bool VEC> static qmm_status launch_wgrad(const
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter gradient attributes");
             if (s != QMM_OK) return s;
             const int64_t columns = (int64_t)p.n * ((p.W + S::cols - 1) / S::cols);
-            // blocks that share a column's rows: 128 rows each at least if one adapter had them all, while the launch stays a few waves
+            // blocks that share a column's rows: as many as make about two per SM in all, 128 rows each at least if one adapter had them all
             int size = 1;
-            while (size < 8 && columns * size < 4 * kNumSMs && (int64_t)p.T >= 256 * size) size *= 2;
+            while (size < 8 && columns * size < 3 * kNumSMs / 2 && (int64_t)p.T >= 256 * size) size *= 2;
             if (columns * size > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapter gradients: %lld blocks are too many for one launch", (long long)(columns * size));
             return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", p);
         };
