@@ -14,6 +14,7 @@
 // does not bound s.
 #pragma once
 
+#include "qmm_async.cuh"
 #include "qmm_launch.cuh"
 #include "qmm_mx.cuh"
 
@@ -527,16 +528,6 @@ __device__ __forceinline__ void widen(WideWeights<T, R, LAY, VEC>& w, const YPie
 
 // ------------------------------------------------------------------ copies into shared memory
 
-__device__ __forceinline__ void async16(uint32_t to, const void* from, int bytes)            // bytes < 16: the rest becomes zero
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void async4(uint32_t to, const void* from, int bytes)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(to), "l"(from), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldmatrix4(uint32_t (&r)[4], uint32_t at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");

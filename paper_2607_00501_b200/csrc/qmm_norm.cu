@@ -6,6 +6,7 @@
 //
 // The codes are those of t, not of y: rstd is one factor of the whole row, so it cancels in t / amax, and a code does not depend on the order in
 // which the squares were added.  Every element is read once and written once: a row lives in the registers of its threads.
+#include "qmm_async.cuh"
 #include "qmm_launch.cuh"
 #include "qmm_mx.cuh"
 
@@ -260,11 +261,37 @@ struct NormGradP {
     float eps;
 };
 
-template <typename T, int V, int NV>
+// Sums of a and b over the block, the same on every thread, added in a fixed order.
+__device__ __forceinline__ void block_sum2(float& a, float& b, float (*red)[64])
+{
+    const int tid = threadIdx.x, warps = blockDim.x >> 5;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+    }
+    if (warps == 1) return;
+    __syncthreads();                                       // the sums before these have been read
+    if ((tid & 31) == 0) red[0][tid >> 5] = a, red[1][tid >> 5] = b;
+    __syncthreads();
+    const bool mine = (tid & 31) < warps;
+    a = mine ? red[0][tid & 31] : 0.0f;
+    b = mine ? red[1][tid & 31] : 0.0f;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
+        b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
+    }
+}
+
+// RING > 0: the rows of h, dy and dh come through shared memory, RING rows in flight (cp.async; a thread reads what it copied itself, so the rows need no
+// barrier).  RING 0: straight into registers, for rows that are not 16-byte aligned or too long for that.
+template <typename T, int V, int NV, int RING>
 __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(const NormGradP p)
 {
     pdl_launch_dependents();
     pdl_wait();
+    extern __shared__ __align__(16) uint8_t ring[];        // [RING][h, dy, dh][NV][threads] pieces of 16 bytes
     __shared__ float red[2][64];
     const int tpr = blockDim.x, tid = threadIdx.x;
     Piece<T, V> w[NV];
@@ -278,18 +305,46 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
         w[i].set(one);
         if (p.w && v < p.nv) w[i].load((const T*)p.w + v * V);
     }
-    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
-        Piece<T, V> h[NV], dy[NV], dh[NV];
+    const int parts = p.dh ? 3 : 2;
+    auto place = [&](int slot, int which, int i) { return ((slot * parts + which) * NV + i) * tpr * 16 + tid * 16; };
+    auto fetch = [&](int64_t row, int slot) {
+        if constexpr (RING > 0) {
+            if (row < p.rows) {
+                const uint32_t base = (uint32_t)__cvta_generic_to_shared(ring);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            h[i].fill(0u);
-            dy[i].fill(0u);
-            dh[i].fill(0u);
-            const int v = tid + i * tpr;
-            if (v < p.nv) {
-                h[i].load((const T*)p.h + row * p.ldh + v * V);
-                dy[i].load((const T*)p.dy + row * p.lddy + v * V);
-                if (p.dh) dh[i].load((const T*)p.dh + row * p.lddh + v * V);
+                for (int i = 0; i < NV; ++i) {
+                    const int v = tid + i * tpr, n = v < p.nv ? 16 : 0, at = v < p.nv ? v * V : 0;
+                    async16(base + place(slot, 0, i), (const T*)p.h + row * p.ldh + at, n);
+                    async16(base + place(slot, 1, i), (const T*)p.dy + row * p.lddy + at, n);
+                    if (p.dh) async16(base + place(slot, 2, i), (const T*)p.dh + row * p.lddh + at, n);
+                }
+            }
+            async_commit();
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) fetch(blockIdx.x + (int64_t)i * gridDim.x, i);
+    int slot = 0;
+    for (int64_t row = blockIdx.x; row < p.rows; row += gridDim.x) {
+        Piece<T, V> h[NV], dy[NV];
+        if constexpr (RING > 0) {
+            fetch(row + (int64_t)(RING - 1) * gridDim.x, slot == 0 ? RING - 1 : slot - 1);
+            async_wait<RING - 1>();
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                h[i].load(reinterpret_cast<const T*>(ring + place(slot, 0, i)));
+                dy[i].load(reinterpret_cast<const T*>(ring + place(slot, 1, i)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                h[i].fill(0u);
+                dy[i].fill(0u);
+                const int v = tid + i * tpr;
+                if (v < p.nv) {
+                    h[i].load((const T*)p.h + row * p.ldh + v * V);
+                    dy[i].load((const T*)p.dy + row * p.lddy + v * V);
+                }
             }
         }
         float ss = 0.0f, dot = 0.0f;
@@ -301,26 +356,7 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
                 ss = fmaf(f, f, ss);
                 dot = fmaf(w[i].get(k) * dy[i].get(k), f, dot);
             }
-        auto reduce2 = [&](float& a, float& b) {
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-                b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-            }
-            if (tpr == 32) return;
-            __syncthreads();                               // the sums of the row before have been read
-            if ((tid & 31) == 0) red[0][tid >> 5] = a, red[1][tid >> 5] = b;
-            __syncthreads();
-            const bool mine = (tid & 31) < (tpr >> 5);
-            a = mine ? red[0][tid & 31] : 0.0f;
-            b = mine ? red[1][tid & 31] : 0.0f;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                a += __shfl_xor_sync(0xFFFFFFFFu, a, o);
-                b += __shfl_xor_sync(0xFFFFFFFFu, b, o);
-            }
-        };
-        reduce2(ss, dot);
+        block_sum2(ss, dot, red);
         float rstd = rstd_of(ss, p.K, p.eps), c = rstd * (rstd * dot / (float)p.K);        // rstd * mean(w dy xhat)
         if (off_range(ss)) {                               // (the same on every thread)
             const bool small = ss < 1.0f;
@@ -334,25 +370,34 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
                     again = fmaf(e, e, again);
                     dot2 = fmaf(w[i].get(k) * dy[i].get(k), e, dot2);
                 }
-            reduce2(again, dot2);
+            block_sum2(again, dot2, red);
             rstd = rstd_scaled(again, p.K, p.eps, small);
             c = rstd * (rstd / f * dot2 / (float)p.K);
         }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = tid + i * tpr;
+            Piece<T, V> dh;
+            dh.fill(0u);
+            if constexpr (RING > 0) {
+                if (p.dh) dh.load(reinterpret_cast<const T*>(ring + place(slot, 2, i)));
+            } else {
+                if (p.dh && v < p.nv) dh.load((const T*)p.dh + row * p.lddh + v * V);
+            }
             float f[V];
 #pragma unroll
             for (int k = 0; k < V; ++k) {
                 const float xhat = h[i].get(k) * rstd;
-                f[k] = fmaf(rstd, w[i].get(k) * dy[i].get(k), fmaf(-c, xhat, dh[i].get(k)));
+                f[k] = fmaf(rstd, w[i].get(k) * dy[i].get(k), fmaf(-c, xhat, dh.get(k)));
                 dw[i][k] = fmaf(dy[i].get(k), xhat, dw[i][k]);
             }
             Piece<T, V> o;
             o.set(f);
             if (p.dx && v < p.nv) o.store((T*)p.dx + row * p.lddx + v * V);
         }
+        if (RING > 0) slot = slot == RING - 1 ? 0 : slot + 1;
     }
+    if (RING > 0) async_wait<0>();
     if (p.part) {
         float* part = p.part + (int64_t)blockIdx.x * p.K;
 #pragma unroll
@@ -369,26 +414,25 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
     }
 }
 
-constexpr int kColThreads = 256;                           // 32 columns x 8 shares of the parts
+// The blocks' parts of dw in block order: 32 columns by 32 shares of the parts per block (all of a share's loads are in flight at once up to 512 parts).
+constexpr int kColThreads = 1024;
 __global__ void __launch_bounds__(kColThreads) rms_norm_dw_kernel(const float* __restrict__ part, int parts, int K, float* __restrict__ dw)
 {
     pdl_launch_dependents();
     pdl_wait();
-    __shared__ float red[8][32];
+    __shared__ float red[32][33];
     const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
     float s = 0.0f;
     if (k < K) {
-#pragma unroll 8
-        for (int i = share; i < parts; i += 8) s += part[(int64_t)i * K + k];
+#pragma unroll 16
+        for (int i = share; i < parts; i += 32) s += part[(int64_t)i * K + k];
     }
     red[share][lane] = s;
     __syncthreads();
-    if (share == 0 && k < K) {
-        float sum = 0.0f;
+    s = red[lane][share];                                  // warp `share`: column `share` of the block
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += red[i][lane];
-        dw[k] = sum;
-    }
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+    if (lane == 0 && blockIdx.x * 32 + share < K) dw[blockIdx.x * 32 + share] = s;
 }
 
 // ------------------------------------------------------- 8-bit rows back to values
@@ -489,17 +533,15 @@ qmm_status launch_rms_norm(int dtype, const void* x, int64_t ldx, const void* re
     });
 }
 
-// Blocks of the gradient: about as many as run at once, each keeps a part of dw.
+// Blocks of the gradient: as many as run at once (two per SM of up to 512 threads, four of up to 256); each writes a part of dw.  (500 rows of 1001: a block for each 5 us
+// and 5 for the sum of the parts; 148 blocks 9.7 and 5.)
+constexpr int kGradBlocks = 4 * kNumSMs;
 static int norm_grad_blocks(int64_t rows, int tpr)
 {
-    const int64_t most = (int64_t)kNumSMs * (tpr >= 1024 ? 1 : 1024 / tpr < 8 ? 1024 / tpr : 8);
+    const int64_t most = tpr > 512 ? kNumSMs : tpr > 256 ? 2 * kNumSMs : kGradBlocks;
     return (int)(rows < most ? rows : most);
 }
-size_t rms_norm_grad_workspace_bytes(int64_t rows, int K)
-{
-    const int64_t most = (int64_t)kNumSMs * 8;
-    return (size_t)(rows < most ? rows : most) * (size_t)K * 4;
-}
+size_t rms_norm_grad_workspace_bytes(int64_t rows, int K) { return (size_t)(rows < kGradBlocks ? rows : kGradBlocks) * (size_t)K * 4; }
 
 qmm_status launch_rms_norm_grad(int dtype, const void* dy, int64_t lddy, const void* h, int64_t ldh, const void* w, float eps, int64_t rows, int K, const void* dh,
                                 int64_t lddh, void* dx, int64_t lddx, float* dw, void* ws, cudaStream_t st)
@@ -508,13 +550,38 @@ qmm_status launch_rms_norm_grad(int dtype, const void* dy, int64_t lddy, const v
     const uintptr_t bits = norm_bits(dy, lddy, size) | norm_bits(h, ldh, size) | norm_bits(w, 0, size) | norm_bits(dh, lddh, size) | norm_bits(dx, lddx, size);
     const bool vec = K % V == 0 && bits % 16 == 0;
     const int nv = vec ? K / V : K;
-    NormShape s = norm_shape(nv, rows, 512);               // (the kernels of up to four vectors are built for 512 threads)
-    if (s.per <= 4 && s.tpr > 512) s.per = 8;
+    // vectors per thread: two with rows in a ring (few registers, many threads), as in the forward pass without
+    const int stage = (dh ? 3 : 2) * 16;                   // bytes of a row in the ring, per vector
+    int tpr = 32, per = 2;
+    while (tpr < 512 && 2 * tpr < nv) tpr *= 2;
+    if (2 * tpr < nv) per = 4;
+    bool in_ring = vec && per * tpr >= nv && (size_t)per * tpr * stage * 2 <= 200 * 1024;
+    NormShape s = {tpr, per};
+    if (!in_ring) {
+        s = norm_shape(nv, rows, 512);                     // (the kernels of up to four vectors are built for 512 threads)
+        if (s.per <= 4 && s.tpr > 512) s.per = 8;
+    }
     const int blocks = norm_grad_blocks(rows, s.tpr);
     NormGradP p = {rows, lddy, ldh, lddh, lddx, K, nv, dy, h, w, dh, dx, dw ? (float*)ws : nullptr, eps};
+    const size_t row_bytes = (size_t)s.per * s.tpr * stage;
+    const bool three = row_bytes * 3 <= 72 * 1024 || (row_bytes * 3 <= 200 * 1024 && s.tpr > 256);
     const qmm_status e = norm_by_shape(dtype, vec, s.per, [&](auto type, auto v, auto n) {
-        return launch_pdl(rms_norm_grad_kernel<decltype(type), decltype(v)::value, decltype(n)::value>, dim3((unsigned)blocks), s.tpr, 0, 1, st,
-                          "root-mean-square norm gradient launch", p);
+        using D = decltype(type);
+        constexpr int VV = decltype(v)::value, NV = decltype(n)::value;
+        if constexpr (VV > 1 && (NV == 2 || NV == 4)) {
+            if (in_ring) {
+                auto go = [&](auto rows_in_flight) {
+                    constexpr int RING = decltype(rows_in_flight)::value;
+                    auto kern = rms_norm_grad_kernel<D, VV, NV, RING>;
+                    static std::atomic<uint64_t> configured{0};
+                    const qmm_status c = configure_once(configured, kern, 200 * 1024, false, "norm gradient attributes");
+                    if (c != QMM_OK) return c;
+                    return launch_pdl(kern, dim3((unsigned)blocks), s.tpr, row_bytes * RING, 1, st, "root-mean-square norm gradient launch", p);
+                };
+                return three ? go(std::integral_constant<int, 3>()) : go(std::integral_constant<int, 2>());
+            }
+        }
+        return launch_pdl(rms_norm_grad_kernel<D, VV, NV, 0>, dim3((unsigned)blocks), s.tpr, 0, 1, st, "root-mean-square norm gradient launch", p);
     });
     if (e != QMM_OK || !dw) return e;
     return launch_pdl(rms_norm_dw_kernel, dim3((unsigned)((K + 31) / 32)), kColThreads, 0, 1, st, "norm weight gradient launch", (const float*)ws, blocks, K, dw);
