@@ -423,9 +423,12 @@ __global__ void __launch_bounds__(kColThreads) rms_norm_dw_kernel(const float* _
     __shared__ float red[32][33];
     const int lane = threadIdx.x & 31, share = threadIdx.x >> 5, k = blockIdx.x * 32 + lane;
     float s = 0.0f;
-    if (k < K) {
-#pragma unroll 16
-        for (int i = share; i < parts; i += 32) s += part[(int64_t)i * K + k];
+    for (int i0 = share; i0 < parts; i0 += 512) {
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = k < K && i0 + 32 * i < parts ? part[(int64_t)(i0 + 32 * i) * K + k] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s += v[i];
     }
     red[share][lane] = s;
     __syncthreads();

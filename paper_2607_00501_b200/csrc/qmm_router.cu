@@ -21,8 +21,10 @@ constexpr int kRouteWarps = 4;
 
 struct RouteP {
     int T, E, topk, sigmoid, groups, top_groups, group_top, renorm, vec;      // vec: P logits of a lane are one or more 16-byte loads
+    int per, share, per_inverse;                           // experts of a group; 2^share lanes look through one; ceil(2^20 / per)
     int64_t ld;
     const float* bias;
+    int bias_vec;
     float scale;
     int* idx;
     float* w;
@@ -72,6 +74,23 @@ template <typename T, int P> __device__ __forceinline__ void load_logits(const T
     }
 }
 
+// P consecutive numbers of fp32 per lane, zeros from E on; vec: 16-byte loads.
+template <int P> __device__ __forceinline__ void load_floats(const float* __restrict__ from, int E, int lane, int vec, float (&v)[P])
+{
+    if constexpr (P >= 4) {
+        if (vec) {
+#pragma unroll
+            for (int i = 0; i < P; i += 4) {
+                const float4 q = lane * P + i < E ? __ldg(reinterpret_cast<const float4*>(from + lane * P + i)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                v[i] = q.x, v[i + 1] = q.y, v[i + 2] = q.z, v[i + 3] = q.w;
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < P; ++i) v[i] = lane * P + i < E ? __ldg(from + lane * P + i) : 0.0f;
+}
+
 __device__ __forceinline__ float warp_max(float v) { return route_unkey(__reduce_max_sync(0xFFFFFFFFu, route_key(v))); }
 template <typename F> __device__ __forceinline__ F warp_sum(F v)
 {
@@ -82,7 +101,9 @@ template <typename F> __device__ __forceinline__ F warp_sum(F v)
 
 // Largest magnitude beyond which exp(-l) of a sigmoid leaves fp32's range: there sigmoid(l) = exp(l) to the last bit.
 constexpr float kSigmoidEnd = -80.0f;
-__device__ __forceinline__ float sigmoid_f(float l) { return l < kSigmoidEnd ? expf(l) : 1.0f / (1.0f + expf(-l)); }
+__device__ __forceinline__ float sigmoid_f(float l) { return l < kSigmoidEnd ? expf(l) : __fdividef(1.0f, 1.0f + expf(-l)); }          // (a reciprocal off by 1 ulp)
+// The same for comparisons: below -87 it is 0, which is nearer than they look.
+__device__ __forceinline__ float sigmoid_score(float l) { return __fdividef(1.0f, 1.0f + expf(-l)); }
 
 // Order of fp64 values as unsigned numbers, as route_key; 0 is left for "none".
 __device__ __forceinline__ unsigned long long key_of(double v)
@@ -90,9 +111,7 @@ __device__ __forceinline__ unsigned long long key_of(double v)
     const unsigned long long u = (unsigned long long)__double_as_longlong(v + 0.0);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
-__device__ __forceinline__ unsigned key_of(float v) { return route_key(v); }
-// The largest key of the warp, and among the lanes that hold it the lowest expert.  In two words: the upper ones first.
-__device__ __forceinline__ unsigned top_key(unsigned k) { return __reduce_max_sync(0xFFFFFFFFu, k); }
+// The largest key of the warp, in two words: the upper ones first.
 __device__ __forceinline__ unsigned long long top_key(unsigned long long k)
 {
     const unsigned hi = __reduce_max_sync(0xFFFFFFFFu, (unsigned)(k >> 32));
@@ -100,20 +119,30 @@ __device__ __forceinline__ unsigned long long top_key(unsigned long long k)
     return (unsigned long long)hi << 32 | lo;
 }
 
-// The groups that stay open, a bit for each: values are the sums of a group's group_top largest c (shared memory, -inf: not to be chosen).  32 / groups lanes, as a power of two,
+// The groups that stay open, a bit for each: values are the sums of a group's group_top largest c (-inf: not to be chosen).  32 / groups lanes, as a power of two,
 // look through each group.  near: whether the last group that stays and the first that does not are within `tie` of one another (fp32).
-template <typename F> __device__ __forceinline__ unsigned open_groups(const F* sc, const RouteP& p, int lane, F tie, bool& near)
+// Where the lanes' P consecutive experts make up whole groups (inside) they are looked through in registers, c, else in shared memory, sc (stored: they are there).
+template <typename F, int P> __device__ __forceinline__ unsigned open_groups(const F (&c)[P], F* sc, const RouteP& p, int lane, F tie, bool& near, bool stored = false)
 {
     const F none = (F)-INFINITY;
-    const int per = p.E / p.groups;
-    const int share = 31 - __clz(32 / p.groups), L = 1 << share, g = lane >> share;
+    const int per = p.per, share = p.share, L = 1 << share, g = lane >> share;
     F a = none, b = none;
-    if (g < p.groups)
-        for (int i = lane & (L - 1); i < per; i += L) {
-            const F v = sc[g * per + i];
-            b = v < a ? (v > b ? v : b) : a;
-            a = v > a ? v : a;
-        }
+    auto take = [&](F v) {
+        b = v < a ? (v > b ? v : b) : a;
+        a = v > a ? v : a;
+    };
+    if (!stored && per == P << share) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) take(c[i]);
+    } else {
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+            if (!stored && lane * P + i < p.E) sc[lane * P + i] = c[i];
+        __syncwarp();
+        if (g < p.groups)
+            for (int i = lane & (L - 1); i < per; i += L) take(sc[g * per + i]);
+    }
     for (int o = 1; o < L; o <<= 1) {
         const F a2 = __shfl_xor_sync(0xFFFFFFFFu, a, o), b2 = __shfl_xor_sync(0xFFFFFFFFu, b, o);
         const F low = a < a2 ? a : a2, high = b > b2 ? b : b2;
@@ -135,101 +164,195 @@ template <typename F> __device__ __forceinline__ unsigned open_groups(const F* s
     return __ballot_sync(0xFFFFFFFFu, (lane & (L - 1)) == 0 && stays);        // bit g << share
 }
 
-// One pass of a choice: the largest key left and its expert; that key is taken out.  false: nothing left.
-template <int P, typename K> __device__ __forceinline__ bool take_top(K (&key)[P], int lane, K& top, int& e)
+// Takes out the keys of closed groups (open: bit group << share).
+template <int P, typename K> __device__ __forceinline__ void close_groups(K (&key)[P], unsigned open, const RouteP& p, int lane)
 {
-    K best = 0;
-    int best_i = 0;
+    if (p.per == P << p.share) {                           // a lane's experts belong to one group
+        const bool stays = open >> (lane >> p.share << p.share) & 1u;
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-        if (key[i] > best) {
-            best = key[i];
-            best_i = i;
+        for (int i = 0; i < P; ++i) key[i] = stays ? key[i] : 0;
+    } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const int g = (lane * P + i) * p.per_inverse >> 20;                // e / per: e < 1024, so the product's error stays below 1 / per
+            if (!(open >> ((g << p.share) & 31) & 1u)) key[i] = 0;
         }
-    top = top_key(best);
-    if (top == 0) return false;
-    e = (int)__reduce_min_sync(0xFFFFFFFFu, best == top ? (unsigned)(lane * P + best_i) : 0x7FFFFFFFu);
+    }
+}
+
+// A lane's own numbers, largest first (odd-even merge sort; P a power of two).
+template <int P> __device__ __forceinline__ void sort_down(unsigned (&v)[P])
+{
 #pragma unroll
-    for (int i = 0; i < P; ++i)
-        if (lane * P + i == e) key[i] = 0;                 // (constant indices: the array stays in registers)
+    for (int p = 1; p < P; p *= 2)
+#pragma unroll
+        for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+            for (int j = k % p; j + k < P; j += 2 * k)
+#pragma unroll
+                for (int i = 0; i < k; ++i)
+                    if (i + j + k < P && (i + j) / (2 * p) == (i + j + k) / (2 * p)) {
+                        const unsigned hi = max(v[i + j], v[i + j + k]), lo = min(v[i + j], v[i + j + k]);
+                        v[i + j] = hi;
+                        v[i + j + k] = lo;
+                    }
+}
+
+// What turns a logit into its score in 64 bits: the largest logit and the sum of a softmax.
+struct Score64 {
+    double m, z;
+};
+template <typename T> __device__ __forceinline__ Score64 score64_of(const T* __restrict__ row, const RouteP& p, int lane)
+{
+    Score64 q = {0.0, 1.0};
+    if (!p.sigmoid) {
+        float top = -INFINITY;
+        for (int e = lane; e < p.E; e += 32) top = fmaxf(top, route_logit(Dt<T>::up(row[e])));
+        q.m = (double)warp_max(top);
+        q.z = 0.0;
+#pragma unroll 1
+        for (int e = lane; e < p.E; e += 32) {
+            const float l = route_logit(Dt<T>::up(row[e]));
+            q.z += l > -INFINITY ? exp((double)l - q.m) : 0.0;
+        }
+        q.z = warp_sum(q.z);
+    }
+    return q;
+}
+// Score and bias of expert e, -inf if it is not to be chosen.
+template <typename T> __device__ __forceinline__ double value64(const T* __restrict__ row, int e, const Score64& q, const RouteP& p)
+{
+    const double l = (double)route_logit(Dt<T>::up(row[e]));
+    const double v = exp(p.sigmoid ? -l : l - q.m);
+    double c = p.sigmoid ? 1.0 / (1.0 + v) : v / q.z;
+    if (p.bias) c += (double)__ldg(p.bias + e);
+    return l > -INFINITY && c == c ? c : -INFINITY;
+}
+
+// The three places below take over where fp32 leaves something open, about one token in a thousand.  Their code is cold: what it takes is mostly its way into the instruction
+// cache, so loops stay rolled.
+
+// Open groups in 64 bits: sc holds the scores of 32 bits (shared memory).  false: a group's second and third are too near to one another as well.
+template <typename T> __device__ __noinline__ bool open_groups_exactly(const T* __restrict__ row, const float* sc, const RouteP& p, int lane, float tie, unsigned& open)
+{
+    const Score64 q = score64_of(row, p, lane);
+    double value = -INFINITY;
+    bool near = false;
+    if (lane < p.groups) {
+        float a = -INFINITY, b = -INFINITY, c = -INFINITY; // the group's three largest, and where the first two are
+        int ea = -1, eb = -1;
+#pragma unroll 1
+        for (int e = lane * p.per; e < (lane + 1) * p.per; ++e) {
+            const float v = sc[e];
+            if (v > a) c = b, b = a, eb = ea, a = v, ea = e;
+            else if (v > b) c = b, b = v, eb = e;
+            else if (v > c) c = v;
+        }
+        const float last = p.group_top == 2 ? b : a, next = p.group_top == 2 ? c : b;
+        near = next > -INFINITY && !(last - next > tie);
+        double sum = 0.0;
+#pragma unroll 1
+        for (int k = 0; k < p.group_top; ++k) {
+            const int e = k ? eb : ea;
+            if (e >= 0) sum += value64(row, e, q, p);
+        }
+        if (ea >= 0) value = sum;
+    }
+    if (__any_sync(0xFFFFFFFFu, near)) return false;
+    int rank = 0;
+#pragma unroll 1
+    for (int k = 0; k < p.groups; ++k) {
+        const double v = __shfl_sync(0xFFFFFFFFu, value, k);
+        rank += v > value || (v == value && k < lane);
+    }
+    const unsigned stay = __ballot_sync(0xFFFFFFFFu, lane < p.groups && rank < p.top_groups);
+    open = 0u;                                             // bit g << share
+#pragma unroll 1
+    for (int k = 0; k < p.groups; ++k) open |= (stay >> k & 1u) << (k << p.share);
     return true;
 }
 
-// The choice in 64 bits, for a token whose fp32 scores leave it open.  l: the token's logits; sd: E fp64 numbers of shared memory where there are groups (over the logits, which
-// the caller restores).  Lane j < topk returns its expert, -1 if none.
-template <int P> __device__ __noinline__ int route_exactly(const float (&l)[P], double* sd, const RouteP& p, int lane)
+// The topk best of the candidates that the lanes hold (mine: the key's upper bits, and in the bits `low` what the expert leaves of them; 0: none), compared in 64 bits.  rest: the largest key that no lane holds.
+// Lane j < topk returns its expert; false: an expert that no lane holds may belong among them.
+template <typename T> __device__ __noinline__ bool refine(const T* __restrict__ row, unsigned mine, unsigned rest, unsigned low, const RouteP& p, int lane, float tie, int& sel)
 {
-    double c[P], m = 0.0, z = 1.0;
-    if (!p.sigmoid) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < P; ++i) top = fmaxf(top, l[i]);
-        m = (double)warp_max(top);
+    const Score64 q = score64_of(row, p, lane);
+    const int e = mine ? (int)(low - (mine & low)) : 0x7FFFFFFF;
+    double v = -INFINITY;
+    if (mine) v = value64(row, e, q, p);
+    int rank = 0;
+    const int held = __popc(__ballot_sync(0xFFFFFFFFu, mine != 0u));           // (the first lanes)
+#pragma unroll 1
+    for (int k = 0; k < held; ++k) {
+        const double o = __shfl_sync(0xFFFFFFFFu, v, k);
+        const int oe = __shfl_sync(0xFFFFFFFFu, e, k);
+        rank += o > v || (o == v && oe < e);
     }
-#pragma unroll
-    for (int i = 0; i < P; ++i) c[i] = l[i] > -INFINITY ? exp(p.sigmoid ? -(double)l[i] : (double)l[i] - m) : 0.0;
-    if (!p.sigmoid) {
-        z = 0.0;
-#pragma unroll
-        for (int i = 0; i < P; ++i) z += c[i];
-        z = warp_sum(z);
-    }
-    unsigned long long key[P];
-#pragma unroll
-    for (int i = 0; i < P; ++i) {
-        const int e = lane * P + i;
-        const double s = p.sigmoid ? 1.0 / (1.0 + c[i]) : c[i] / z;
-        c[i] = p.bias && e < p.E ? s + (double)__ldg(p.bias + e) : s;
-        if (!(l[i] > -INFINITY) || !(c[i] == c[i])) c[i] = -INFINITY;
-        key[i] = c[i] > -INFINITY ? key_of(p.bias ? c[i] : (double)l[i]) : 0;      // without a bias: the scores' order is that of the logits
-    }
-    if (p.groups > 1) {
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (lane * P + i < p.E) sd[lane * P + i] = c[i];
-        __syncwarp();
-        bool near;
-        const unsigned open = open_groups<double>(sd, p, lane, 0.0, near);
-        const int per = p.E / p.groups, share = 31 - __clz(32 / p.groups);
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (!(open >> (((lane * P + i) / per << share) & 31) & 1u)) key[i] = 0;
-    }
-    int mine = -1;
+    sel = -1;
+    double last = INFINITY;                                // the last one chosen
+#pragma unroll 1
     for (int j = 0; j < p.topk; ++j) {
-        unsigned long long top;
-        int e;
-        if (!take_top(key, lane, top, e)) break;
-        if (lane == j) mine = e;
+        const unsigned who = __ballot_sync(0xFFFFFFFFu, mine && rank == j);
+        if (!who) break;
+        const int from = __ffs(who) - 1, ej = __shfl_sync(0xFFFFFFFFu, e, from);
+        last = __shfl_sync(0xFFFFFFFFu, v, from);
+        if (lane == j) sel = ej;
     }
+    return rest == 0u || last > (double)route_unkey(rest | low) + (double)tie;
+}
+
+// The whole choice in 64 bits.  sd: E fp64 numbers of shared memory.  Lane j < topk returns its expert, -1 if none.
+template <typename T> __device__ __noinline__ int route_exactly(const T* __restrict__ row, double* sd, const RouteP& p, int lane)
+{
+    const double none = -INFINITY;
+    const Score64 q = score64_of(row, p, lane);
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 32) sd[e] = value64(row, e, q, p);
+    __syncwarp();
+    if (p.groups > 1) {
+        const double unused[1] = {none};
+        bool near;
+        const unsigned open = open_groups<double, 1>(unused, sd, p, lane, 0.0, near, true);
+#pragma unroll 1
+        for (int e = lane; e < p.E; e += 32)
+            if (!(open >> (((e * p.per_inverse >> 20) << p.share) & 31) & 1u)) sd[e] = none;
+    }
+    if (!p.bias)                                           // the scores' order is that of the logits
+#pragma unroll 1
+        for (int e = lane; e < p.E; e += 32)
+            if (sd[e] > none) sd[e] = (double)route_logit(Dt<T>::up(row[e]));
+    int mine = -1;
+#pragma unroll 1
+    for (int j = 0; j < p.topk; ++j) {                     // a lane's experts lie 32 apart: lower ones first
+        double best = none;
+        int at = 0x7FFFFFFF;
+#pragma unroll 4
+        for (int e = lane; e < p.E; e += 32) {
+            const double v = sd[e];
+            if (v > best) {
+                best = v;
+                at = e;
+            }
+        }
+        const unsigned long long key = best > none ? key_of(best) : 0ull, top = top_key(key);
+        if (top == 0) break;
+        at = (int)__reduce_min_sync(0xFFFFFFFFu, key == top ? (unsigned)at : 0x7FFFFFFFu);
+        if ((at & 31) == lane) sd[at] = none;
+        if (lane == j) mine = at;
+    }
+    __syncwarp();
     return mine;
 }
 
 // Two fp32 scores that differ by less than this (plus the roundings of the bias's addition) are compared in 64 bits.  sigmoid: expf off by 2 ulp moves 1 / (1 + e) by
-// 6e-8 at most, the sum and the division add 1.2e-7: two of them 4e-7.  softmax, relative to the token's largest score: 2 ulp of expf, |l - m| e^-|l - m| 2^-24 of its argument,
+// 6e-8 at most, the sum and the reciprocal (1 ulp) add 1.8e-7: two of them 4.8e-7.  softmax, relative to the token's largest score: 2 ulp of expf, |l - m| e^-|l - m| 2^-24 of its argument,
 // a rounding, for both, and the denominator's 37 additions, which scale both alike: 3e-6.
 constexpr float kTieSigmoid = 6e-7f, kTieSoftmax = 4e-6f;
 
 template <typename T, int P>
-__global__ void __launch_bounds__(32 * kRouteWarps) expert_route_kernel(const T* __restrict__ logits, const RouteP p)
+__device__ __forceinline__ void route_one(const T* __restrict__ row, int64_t t, const float (&l)[P], const float (&bias)[P], double* sd, const RouteP& p, int lane)
 {
-    pdl_launch_dependents();
-    pdl_wait();
-    extern __shared__ __align__(16) float s_row[];         // per warp: E logits, and E scores where there are groups
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int t = blockIdx.x * kRouteWarps + warp;
-    if (t >= p.T) return;
-    float* sl = s_row + warp * p.E * (p.groups > 1 ? 2 : 1);
-    float l[P], c[P];
-    load_logits<T, P>(logits + t * p.ld, p.E, lane, p.vec, l);
-    auto keep_logits = [&] {
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (lane * P + i < p.E) sl[lane * P + i] = l[i];
-        __syncwarp();
-    };
-    keep_logits();
+    float c[P];
     const bool scored = p.bias || (p.groups > 1 && p.group_top == 2);        // whether scores are compared, not logits alone
     float m = -INFINITY, z = 1.0f;
     if (!p.sigmoid && (scored || !p.renorm)) {
@@ -251,11 +374,12 @@ __global__ void __launch_bounds__(32 * kRouteWarps) expert_route_kernel(const T*
         float most = 0.0f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const int e = lane * P + i;
-            const float s = p.sigmoid ? sigmoid_f(l[i]) : c[i] * per_z;
-            c[i] = p.bias && e < p.E ? s + __ldg(p.bias + e) : s;
-            c[i] = l[i] > -INFINITY && c[i] == c[i] ? c[i] : -INFINITY;
-            if (c[i] > -INFINITY) most = fmaxf(most, fabsf(c[i]));
+            const float s = p.sigmoid ? sigmoid_score(l[i]) : c[i] * per_z;
+            c[i] = p.bias ? s + bias[i] : s;
+            c[i] = l[i] > -INFINITY ? c[i] : -INFINITY;
+            const bool live = c[i] > -INFINITY;            // (a NaN is not)
+            c[i] = live ? c[i] : -INFINITY;
+            most = fmaxf(most, live ? fabsf(c[i]) : 0.0f);
         }
         tie = fmaf(warp_max(most), 2.4e-7f, p.sigmoid ? kTieSigmoid : kTieSoftmax * per_z);          // (the largest softmax is 1 / z)
     } else {
@@ -266,54 +390,89 @@ __global__ void __launch_bounds__(32 * kRouteWarps) expert_route_kernel(const T*
 #pragma unroll
     for (int i = 0; i < P; ++i) key[i] = c[i] > -INFINITY ? route_key(scored && !p.bias ? l[i] : c[i]) : 0u;
     if (p.groups > 1) {
-        float* sc = sl + p.E;
-#pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (lane * P + i < p.E) sc[lane * P + i] = c[i];
-        __syncwarp();
         bool near = false;
-        const unsigned stay = open_groups<float>(sc, p, lane, 2.0f * tie, near);
-        if (scored) open = near;
-        const int per = p.E / p.groups, share = 31 - __clz(32 / p.groups);
+        float* sc = reinterpret_cast<float*>(sd);
+        unsigned stay = open_groups<float, P>(c, sc, p, lane, 2.0f * tie, near);
+        if (scored && near) {
+            __syncwarp();
 #pragma unroll
-        for (int i = 0; i < P; ++i)
-            if (!(stay >> (((lane * P + i) / per << share) & 31) & 1u)) key[i] = 0u;
-    }
-    // the topk largest keys, and one more where neighbours are compared
-    const int passes = p.bias ? p.topk + 1 : p.topk;
-    int sel = -1, after = -1;
-    unsigned sel_key = 0u, after_key = 0u;                 // lane j: the j-th choice; after: what follows the last one
-    for (int j = 0; j < passes; ++j) {
-        unsigned top;
-        int e;
-        if (!take_top(key, lane, top, e)) break;
-        if (j == p.topk) {
-            after = e;
-            after_key = top;
-        } else if (lane == j) {
-            sel = e;
-            sel_key = top;
+            for (int i = 0; i < P; ++i)
+                if (lane * P + i < p.E) sc[lane * P + i] = c[i];
+            __syncwarp();
+            open = !open_groups_exactly<T>(row, sc, p, lane, tie, stay);
         }
+        close_groups(key, stay, p, lane);
     }
-    if (p.bias) {
-        // lane j against what follows it; equal logits and biases give equal scores in 64 bits too
-        const int next_lane = lane + 1 < 32 ? lane + 1 : 31;
-        int next = __shfl_sync(0xFFFFFFFFu, sel, next_lane);
-        unsigned next_key = __shfl_sync(0xFFFFFFFFu, sel_key, next_lane);
-        if (lane == p.topk - 1) next = after, next_key = after_key;
+    // The topk largest, and one more to see what follows: by the keys' upper 22 to 27 bits with the expert in the lower ones.  That is one number to compare, so a lane keeps its own
+    // in order and a pass is one reduction and one step down in the lane that won.
+    int sel = -1;
+    float v = -INFINITY;
+    if (!open) {
+        constexpr unsigned low = 32 * P - 1;               // bits of an expert's number
+        unsigned packed[P], mine = 0u;                     // lane j: the j-th largest
+#pragma unroll
+        for (int i = 0; i < P; ++i) packed[i] = key[i] ? (key[i] & ~low) | (low - (unsigned)(lane * P + i)) : 0u;
+        sort_down(packed);
+        auto pass = [&](int j) {                           // (0: nothing left, and nothing changes)
+            const unsigned top = __reduce_max_sync(0xFFFFFFFFu, packed[0]);
+            const bool won = packed[0] == top;
+            mine = lane == j ? top : mine;
+#pragma unroll
+            for (int i = 0; i + 1 < P; ++i) packed[i] = won ? packed[i + 1] : packed[i];
+            packed[P - 1] = won ? 0u : packed[P - 1];
+        };
+        const int passes = p.topk < 32 ? p.topk + 1 : 32;
+#pragma unroll 2
+        for (int j = 0; j < passes; ++j) pass(j);
+        unsigned follow = __shfl_down_sync(0xFFFFFFFFu, mine, 1);
+        if (p.topk == 32) {
+            const unsigned rest = __reduce_max_sync(0xFFFFFFFFu, packed[0]);
+            if (lane == 31) follow = rest;
+        }
+        sel = lane < p.topk && mine ? (int)(low - (mine & low)) : -1;
+        const int next = lane < p.topk && follow ? (int)(low - (follow & low)) : -1;
+        if (sel >= 0) v = route_logit(Dt<T>::up(row[sel]));
+        // Neighbours that agree in these bits (for 16-bit logits without a bias: are equal, and in order), or whose scores of 32 bits are nearer than these are exact, are
+        // compared as logits, or in 64 bits, with eight that follow.  Equal logits and biases give equal scores there too.
         bool near = false;
-        if (lane < p.topk && sel >= 0 && next >= 0)
-            near = !(route_unkey(sel_key) - route_unkey(next_key) > tie) && !(sl[sel] == sl[next] && __ldg(p.bias + sel) == __ldg(p.bias + next));
-        open = open || __any_sync(0xFFFFFFFFu, near);
+        if (next >= 0) {
+            near = !(sizeof(T) == 2 && !p.bias) && (mine & ~low) == (follow & ~low);
+            if (p.bias) {
+                const float l2 = route_logit(Dt<T>::up(row[next])), b1 = __ldg(p.bias + sel), b2 = __ldg(p.bias + next);
+                const float s1 = p.sigmoid ? sigmoid_score(v) : expf(v - m) * per_z, s2 = p.sigmoid ? sigmoid_score(l2) : expf(l2 - m) * per_z;
+                near = (near || !((s1 + b1) - (s2 + b2) > tie)) && !(v == l2 && b1 == b2);
+            }
+        }
+        if (__any_sync(0xFFFFFFFFu, near)) {
+            unsigned rest;
+            if (!p.bias) {                                 // the logits themselves decide: neighbours change places until they are in order
+                int e = mine ? (int)(low - (mine & low)) : 0x7FFFFFFF;
+                float own = mine ? route_logit(Dt<T>::up(row[e])) : -INFINITY;
+#pragma unroll 1
+                for (int r = 0; r < passes; ++r) {
+                    const int with = r & 1 ? ((lane + 1) ^ 1) - 1 : lane ^ 1;
+                    const float o = __shfl_sync(0xFFFFFFFFu, own, with & 31);
+                    const int oe = __shfl_sync(0xFFFFFFFFu, e, with & 31);
+                    const bool behind = with > lane ? o > own || (o == own && oe < e) : own > o || (own == o && e < oe);
+                    if (behind && with >= 0 && with < passes && lane < passes) own = o, e = oe;
+                }
+                rest = __reduce_max_sync(0xFFFFFFFFu, packed[0]);              // the largest that no lane holds
+                const unsigned lowest = __shfl_sync(0xFFFFFFFFu, mine, passes - 1);
+                open = rest != 0u && (rest & ~low) == (lowest & ~low);
+                sel = lane < p.topk && e < p.E ? e : -1;
+            } else {
+#pragma unroll 1
+                for (int j = passes; j < 32 && j < passes + 8; ++j) pass(j);
+                rest = __reduce_max_sync(0xFFFFFFFFu, packed[0]);
+                open = !refine<T>(row, mine, rest, low, p, lane, tie, sel);
+            }
+            v = sel >= 0 ? route_logit(Dt<T>::up(row[sel])) : -INFINITY;
+        }
     }
     if (open) {
-        sel = route_exactly<P>(l, reinterpret_cast<double*>(sl), p, lane);
-        if (p.groups > 1) {
-            __syncwarp();
-            keep_logits();
-        }
+        sel = route_exactly<T>(row, sd, p, lane);
+        v = sel >= 0 ? route_logit(Dt<T>::up(row[sel])) : -INFINITY;
     }
-    const float v = sel >= 0 ? sl[sel] : -INFINITY;
     float w = 0.0f;
     if (!p.renorm) {
         if (sel >= 0) w = p.sigmoid ? sigmoid_f(v) : expf(v - m) * per_z;
@@ -328,6 +487,20 @@ __global__ void __launch_bounds__(32 * kRouteWarps) expert_route_kernel(const T*
         p.idx[(int64_t)t * p.topk + lane] = sel;
         p.w[(int64_t)t * p.topk + lane] = sel >= 0 ? p.scale * w : 0.0f;
     }
+}
+
+template <typename T, int P> __global__ void __launch_bounds__(32 * kRouteWarps, P <= 4 ? 8 : P == 8 ? 6 : 4) expert_route_kernel(const T* __restrict__ logits, const RouteP p)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    extern __shared__ __align__(16) double s_row[];        // per warp: E scores
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int t = blockIdx.x * kRouteWarps + warp;
+    if (t >= p.T) return;
+    float l[P], bias[P];
+    load_logits<T, P>(logits + t * p.ld, p.E, lane, p.vec, l);
+    if (p.bias) load_floats<P>(p.bias, p.E, lane, p.bias_vec, bias);
+    route_one<T, P>(logits + t * p.ld, t, l, bias, s_row + warp * p.E, p, lane);
 }
 
 // ------------------------------------------------------------------ gradient
@@ -463,12 +636,16 @@ template <typename F> static qmm_status route_by_type(int dtype, int E, F f)
 qmm_status launch_expert_route(int dtype, const void* logits, int64_t ld, int T, int E, int topk, int sigmoid, const float* bias, int groups, int top_groups,
                                int group_top, int renorm, float scale, int* idx, float* w, cudaStream_t st)
 {
-    RouteP p = {T, E, topk, sigmoid, groups, top_groups, group_top, renorm, 0, ld, bias, scale, idx, w};
+    const int per_group = E / groups;
+    int share = 0;                                         // the largest power of two of lanes that all groups can have
+    while ((2 << share) * groups <= 32) ++share;
+    RouteP p = {T, E, topk, sigmoid, groups, top_groups, group_top, renorm, 0, per_group, share, ((1 << 20) + per_group - 1) / per_group, ld, bias,
+                E % 4 == 0 && aligned(bias, 16), scale, idx, w};
     return route_by_type(dtype, E, [&](auto type, auto per) {
         using D = decltype(type);
         constexpr int P = decltype(per)::value;
         p.vec = route_vec(logits, ld, E, P, (int)sizeof(D));
-        const size_t smem = (size_t)kRouteWarps * E * (groups > 1 ? 2 : 1) * 4;               // 32 KB at most
+        const size_t smem = (size_t)kRouteWarps * E * 8;                                       // 32 KB at most
         return launch_pdl(expert_route_kernel<D, P>, dim3((unsigned)((T + kRouteWarps - 1) / kRouteWarps)), 32 * kRouteWarps, smem, 1, st, "expert route launch",
                           (const D*)logits, p);
     });
