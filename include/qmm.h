@@ -555,7 +555,7 @@ qmm_status qmm_rows_dequantize(qmm_row_format fmt, const void* codes, int64_t ld
  * X may be rows of 8 bits (x_format, x_scale as qmm_rms_norm and qmm_rows_quantize leave them), in the forward pass, in dA, or in both.
  * Accuracy: sums in fp32; S and dS enter the second products as two 16-bit parts (off by 2^-16 of the row's largest element at most).
  *   order, offsets, units  of qmm_expert_sort(idx, T, 1, n), for callers that use one sort for many projections; NULL: the call
- *                          sorts in its workspace (rows up to 256 of a forward pass need no sort)
+ *                          sorts in its workspace (up to 512 rows a forward pass needs none)
  *   Y0 may be Y, dX0 may be dX (in place); NULL counts as zeros.  Otherwise no output may overlap an input.
  *   S [T, r] is optional in qmm_lora, needed for dB in qmm_lora_grad.  dX, dA and dB are each optional in qmm_lora_grad (dX0 goes with dX).
  *   ws  device, 256-byte aligned, >= qmm_lora_workspace_bytes(); holds nothing between calls.                        */

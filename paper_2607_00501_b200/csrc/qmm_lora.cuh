@@ -25,7 +25,8 @@ using namespace mx;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kSmallRows = 256;                            // up to here a row's cluster finds its adapter's rows by itself
+constexpr int kSmallRows = 512;                            // up to here the one-launch form finds an adapter's rows by itself
+constexpr int kSmallBlocks = 8;                            // blocks of its clusters at most
 constexpr int kTileRows = 64;                              // rows of a tile of the two-launch form (half a unit of the sort)
 
 // ---------------------------------------------------------------- products of fragments
@@ -580,6 +581,13 @@ __device__ __forceinline__ float4 remote4(const float* p, int rank)
     return v;
 }
 
+__device__ __forceinline__ void send4(float* p, int rank, float4 v)
+{
+    uint32_t at = (uint32_t)__cvta_generic_to_shared(p), there;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(there) : "r"(at), "r"(rank));
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(there), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+
 // The blocks' four numbers at p (shared memory), added in block order; up to 16 blocks, the loads of eight in flight at once.
 __device__ __forceinline__ float4 cluster_sum4(const float* p, int size)
 {
@@ -632,51 +640,118 @@ template <typename T, bool VEC> __device__ __forceinline__ void copy_row(const L
 }
 
 // Both products of up to 16 rows of one adapter by a cluster of blocks: each takes a share of K, the shares' sums meet through distributed shared memory, and each takes
-// a share of N.  One launch: for a decode step two would cost as much as all their work.  Cluster b is there for row b: it does something if row b is
-// the first, 17th, ... of its adapter's rows, and then takes 16 of them.
+// a share of N.  One launch: for a decode step two, and a sort before them, would cost as much as all their work.
+//   groups 0: cluster b is there for row b; it does something if row b is the first, 17th, ... of its adapter's rows, and then takes 16 of them
+//   groups > 0 (so many clusters, fewer than rows): cluster c takes the c-th group of 16 rows in the order of the adapters, which it counts
 template <typename T, bool X8, int R, int LAY, bool VEC>
-__global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
+__global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p, int groups)
 {
     pdl_launch_dependents();
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
     float* part = reinterpret_cast<float*>(smem);          // [kWarps][16][R]
-    float* sum = part + kWarps * 16 * R;                   // [16][R]: this block's share
-    uint8_t* hi = reinterpret_cast<uint8_t*>(sum + 16 * R);
+    float* shares = part + kWarps * 16 * R;                // [kSmallBlocks][16][R]: the blocks' sums over their shares of K
+    uint8_t* hi = reinterpret_cast<uint8_t*>(shares + kSmallBlocks * 16 * R);
     uint8_t* lo = hi + 16 * u_pitch<R>;
+    constexpr int Q = kSmallRows / kThreads;               // rows of a thread: tid + q kThreads
     __shared__ float back[16];
-    __shared__ int rows[16], before[kWarps];
+    __shared__ int rows[16], before[Q * kWarps], first_of, adapter;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_rank(), size = (int)cluster_size();
     const int b = blockIdx.x / size;
+    cluster_arrive();                                      // (the others' shared memory may be written once they have all begun)
     int n0, n1;
     constexpr int G = Wide<LAY>::cols;
     share_of((p.N + G - 1) / G, rank, size, n0, n1);
     if (!p.y) n1 = n0;                                     // s alone is wanted
-    const int a = __ldg(p.idx + b), other = tid < p.T ? __ldg(p.idx + tid) : -1;
-    if (a < 0 || a >= p.n) {                               // (the whole cluster)
-        if (p.rest)
-            for (int c = n0 + warp; c < n1; c += kWarps) copy_row<T, VEC>(p, b, c * G, min(c * G + G, p.N), lane);
-        return;
-    }
-    // this row's place among its adapter's rows
-    const unsigned same = __ballot_sync(0xFFFFFFFFu, other == a);
-    if (tid < 16) rows[tid] = -1;
-    if (lane == 0) before[warp] = __popc(same);
-    __syncthreads();
-    int mine = __popc(same & ((1u << lane) - 1u)), first = 0;
+    int id[Q], a = -1, first = 0;
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w < warp) mine += before[w];
-        if (w < (b >> 5)) first += before[w];
+    for (int q = 0; q < Q; ++q) {
+        id[q] = tid + q * kThreads < p.T ? __ldg(p.idx + tid + q * kThreads) : -1;
+        if (id[q] >= p.n) id[q] = -1;
     }
-    // rows of warp b / 32 before row b
-    __shared__ unsigned mask;
-    if (warp == (b >> 5) && lane == 0) mask = same;
+    if (tid < 16) rows[tid] = -1;
+    if (groups == 0) {
+        a = __ldg(p.idx + b);
+        if (a < 0 || a >= p.n) {                           // (the whole cluster)
+            if (p.rest)
+                for (int c = n0 + warp; c < n1; c += kWarps) copy_row<T, VEC>(p, b, c * G, min(c * G + G, p.N), lane);
+            cluster_wait();
+            return;
+        }
+    } else {
+        int* count = reinterpret_cast<int*>(smem);         // rows of each adapter (4 KB, over the parts)
+        for (int i = tid; i < 1024; i += kThreads) count[i] = 0;
+        if (tid == 0) adapter = -1;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (id[q] >= 0) atomicAdd(&count[id[q]], 1);   // (a count: order does not matter)
+        __syncthreads();
+        const int4 c = reinterpret_cast<const int4*>(count)[tid];
+        const int g0 = (c.x + 15) >> 4, g1 = g0 + ((c.y + 15) >> 4), g2 = g1 + ((c.z + 15) >> 4), g3 = g2 + ((c.w + 15) >> 4);
+        int end = g3;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xFFFFFFFFu, end, o);
+            if (lane >= o) end += v;
+        }
+        if (lane == 31) before[warp] = end;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w)
+            if (w < warp) end += before[w];
+        const int at = b - (end - g3);                     // group b among this thread's
+        if (at >= 0 && at < g3) {
+            const int k = at < g0 ? 0 : at < g1 ? 1 : at < g2 ? 2 : 3;
+            adapter = 4 * tid + k;
+            first_of = 16 * (at - (k == 0 ? 0 : k == 1 ? g0 : k == 2 ? g1 : g2));
+        }
+        if (p.rest) {                                      // the rows without an adapter, dealt to the clusters
+            for (int r = b; r < p.T; r += groups) {
+                const int e = __ldg(p.idx + r);
+                if (e < 0 || e >= p.n)
+                    for (int cc = n0 + warp; cc < n1; cc += kWarps) copy_row<T, VEC>(p, r, cc * G, min(cc * G + G, p.N), lane);
+            }
+        }
+        __syncthreads();
+        a = adapter;
+        if (a < 0) {                                       // (the whole cluster)
+            cluster_wait();
+            return;
+        }
+        first = first_of;
+    }
+    // the rows' places among their adapter's
+    int mine[Q];
+    unsigned same[Q];
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        same[q] = __ballot_sync(0xFFFFFFFFu, id[q] == a);
+        if (lane == 0) before[q * kWarps + warp] = __popc(same[q]);
+    }
     __syncthreads();
-    first += __popc(mask & ((1u << (b & 31)) - 1u));
-    if (first & 15) return;                                // (the whole cluster)
-    if (other == a && mine >= first && mine < first + 16) rows[mine - first] = tid;
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        mine[q] = __popc(same[q] & ((1u << lane) - 1u));
+#pragma unroll
+        for (int w = 0; w < Q * kWarps; ++w)
+            if (w < q * kWarps + warp) mine[q] += before[w];
+    }
+    if (groups == 0) {
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+            if (tid + q * kThreads == b) first_of = mine[q];
+        __syncthreads();
+        first = first_of;
+        if (first & 15) {                                  // (the whole cluster)
+            cluster_wait();
+            return;
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < Q; ++q)
+        if (id[q] == a && mine[q] >= first && mine[q] < first + 16) rows[mine[q] - first] = tid + q * kThreads;
     __syncthreads();
 
     const int g = lane >> 2, t = lane & 3;
@@ -703,24 +778,29 @@ __global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
     }
     put_narrow<R, LAY>(acc[0], part + warp * 16 * R, lane);
     __syncthreads();
-    for (int i = tid; i < 16 * R / 4; i += kThreads) {
+    cluster_wait();
+    for (int i = tid; i < 16 * R / 4; i += kThreads) {     // this block's sum goes to every block of the cluster
         float4 v = reinterpret_cast<float4*>(part)[i];
 #pragma unroll
         for (int k = 1; k < kWarps; ++k) {
             const float4 q = reinterpret_cast<float4*>(part + k * 16 * R)[i];
             v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
         }
-        reinterpret_cast<float4*>(sum)[i] = v;
+        for (int k = 0; k < size; ++k) send4(shares + rank * 16 * R + 4 * i, k, v);
     }
     cluster_arrive();
-    cluster_wait();
+    cluster_wait();                                        // (the last that the blocks have to do with one another)
     const float sc = p.scale ? __ldg(p.scale + a) : 1.0f;
     constexpr int rounds = 16 * R / 4 < kThreads ? 1 : 16 * R / 4 / kThreads;
 #pragma unroll
     for (int q = 0; q < rounds; ++q) {
         const int i = tid + q * kThreads;
         if (16 * R / 4 >= kThreads || warp < (16 * R / 4 + 31) / 32) {        // whole warps: put_u shuffles
-            const float4 v = cluster_sum4(sum + 4 * i, size);
+            float4 v = reinterpret_cast<const float4*>(shares)[i];
+            for (int k = 1; k < size; ++k) {
+                const float4 r = reinterpret_cast<const float4*>(shares + k * 16 * R)[i];
+                v.x += r.x, v.y += r.y, v.z += r.z, v.w += r.w;
+            }
             const int m = 4 * i / R, j = 4 * i % R, to = rows[m];
             float f[4] = {v.x, v.y, v.z, v.w};
             if (X8 && to >= 0) {
@@ -736,7 +816,6 @@ __global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
             put_u<T, R>(f, hi, lo, back, m, j);
         }
     }
-    cluster_arrive();                                      // this block has read the others' shares
     __syncthreads();
     while (c < n1) {
         if (R > 32) w.load(w2, c * G, p.N, lane);
@@ -747,7 +826,6 @@ __global__ void __launch_bounds__(kThreads) lora_small_kernel(const LoraP p)
             y0.load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
         }
     }
-    cluster_wait();                                        // nobody reads this block's share any more
 }
 
 // Which adapter a tile belongs to: the last a with starts[a] <= v, of n + 1 ascending numbers, by a warp.
@@ -1585,15 +1663,19 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
         auto narrowed = [&](auto e8) {
             constexpr bool X8 = decltype(e8)::value;
             if (p.T <= kSmallRows) {
-                constexpr int smem = (kWarps + 1) * 16 * R * 4 + 2 * 16 * u_pitch<R>;
+                constexpr int smem = (kWarps + kSmallBlocks) * 16 * R * 4 + 2 * 16 * u_pitch<R>;              // (at least the 4 KB of the counts)
                 static std::atomic<uint64_t> configured{0};
                 auto kern = lora_small_kernel<T, X8, R, LAY, VEC>;
-                const qmm_status s = configure_once(configured, kern, smem, true, "adapter attributes");
+                const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
                 if (s != QMM_OK) return s;
-                // a block for every 256 elements of K or N, eight at most; sixteen where that leaves most of the GPU idle
-                const int64_t pieces = (p.K > p.N ? p.K : p.N) / 256;
-                const int size = cluster_for(pieces, p.T <= 4 ? 16 : 8);
-                return launch_pdl(kern, dim3((unsigned)(p.T * size)), kThreads, smem, size, st, "adapter launch", p);
+                // groups of 16 rows that any distribution can need, where they are fewer than the rows; blocks of 256 elements of K or N each, of 64 where that
+                // leaves SMs without one (clusters of 16 were slower: 16 x 8192 x 2048 8.8 us against 7.0)
+                const int64_t need = (p.T + 15 * (int64_t)(p.T < p.n ? p.T : p.n)) / 16, clusters = need < p.T ? need : p.T;
+                const int64_t longest = p.K > p.N ? p.K : p.N;
+                const bool grouped = need < p.T && p.T > 16;                  // (up to 16 rows a cluster for each runs at once)
+                int size = cluster_for(longest / 256, kSmallBlocks);
+                while (size < kSmallBlocks && 2 * size <= longest / 64 && clusters * size * 2 <= 2 * kNumSMs) size *= 2;
+                return launch_pdl(kern, dim3((unsigned)((grouped ? clusters : p.T) * size)), kThreads, smem, size, st, "adapter launch", p, (int)(grouped ? need : 0));
             }
             constexpr int smem = NarrowShape<X8, R, LAY, VEC>::smem;
             static std::atomic<uint64_t> configured{0};
@@ -1601,8 +1683,8 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
             if (s != QMM_OK) return s;
             const int64_t tiles = (p.T + kTileRows - 1) / kTileRows;
-            int size = 1;                                  // blocks that share a tile's K: two per SM in all, 256 elements each at least
-            while (size < 8 && tiles * size < 2 * kNumSMs && p.K / (2 * size) >= 256) size *= 2;
+            int size = 1;                                  // blocks that share a tile's K: two per SM in all, 128 elements each at least
+            while (size < 8 && tiles * size < 2 * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
             return launch_pdl(kern, dim3((unsigned)(most_tiles(p.T, p.n) * size)), kThreads, smem, size, st, "adapter narrowing launch", p);
         };
         qmm_status s;

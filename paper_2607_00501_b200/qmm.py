@@ -896,7 +896,7 @@ def lora(x: torch.Tensor, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, y
     T = x.shape[0]
     if out is None:
         out = torch.empty((T, b.shape[1]), dtype=b.dtype, device=x.device)
-    if ws is None and T > 256:
+    if ws is None and T > 512:
         ws = torch.empty(lora_workspace_bytes(T, a.shape[0], a.shape[1]), dtype=torch.uint8, device=x.device)
     _check((_layer_ext or _layer()).lora(x, x_scale, idx, a, b, scale, *_lora_plan(plan, T, a.shape[0]), s, y0, out, ws))
     return out
