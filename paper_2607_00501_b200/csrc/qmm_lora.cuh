@@ -1339,9 +1339,11 @@ template <typename T, bool X8, int R> struct WgradShape {
     static constexpr int part = tf32 ? RT * rows * 4 : RT * rows * 2;
     static constexpr int parts = tf32 ? 2 : 3;
     static constexpr int stage = vbytes + sbytes;
-    static constexpr int sums = RG * RT * cols * 4;
+    static constexpr int ahead = R <= 32 ? 2 : 1;          // sets of parts: with two, a stage's s is split during the products of the one before
+    static constexpr int pitch = cols + 8;                 // floats of a row of the sums (8 apart: no bank conflicts)
+    static constexpr int sums = RG * RT * pitch * 4;
     static constexpr int front = stages * stage > sums ? stages * stage : sums;
-    static constexpr int smem = front + parts * part + stages * rows * 4;
+    static constexpr int smem = front + ahead * parts * part + stages * rows * 4;
 };
 
 template <typename T, bool X8, int R, bool TRANS, bool VEC>
@@ -1353,7 +1355,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
     constexpr int MT = S::MT, NT = S::NT, WC = S::WC, RG = S::RG, RT = S::RT;
     extern __shared__ __align__(16) uint8_t smem[];
     uint8_t* s_part = smem + S::front;
-    float* s_scale = reinterpret_cast<float*>(s_part + S::parts * S::part);
+    float* s_scale = reinterpret_cast<float*>(s_part + S::ahead * S::parts * S::part);
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem), part0 = base + S::front;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int rank = (int)cluster_rank(), size = (int)cluster_size();
@@ -1431,26 +1433,11 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
 #pragma unroll
         for (int i = 0; i < NT; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
     if (R == 8)                                            // ranks 8 .. 15 of the tile
-        for (int i = tid; i < S::parts * S::part / 4; i += kThreads) reinterpret_cast<uint32_t*>(s_part)[i] = 0u;
-    rows_of(st0);
-#pragma unroll
-    for (int i = 0; i < S::stages - 1; ++i) {
-        if (st0 + i < st1) fetch(i);
-        async_commit();
-        if (st0 + i < st1) put_held(i);
-        rows_of(st0 + i + 1);
-    }
-    int buf = 0;
-    for (int st = st0; st < st1; ++st) {
-        async_wait<S::stages - 2>();
-        __syncthreads();                                   // the stage is there; the one before it and the parts are free
-        const int next = buf == 0 ? S::stages - 1 : buf - 1;
-        const bool more = st + S::stages - 1 < st1;
-        if (more) fetch(next);
-        async_commit();
-        rows_of(st + S::stages);
-        // s of the stage into [rank][row] parts: eight rows of a rank per thread
+        for (int i = tid; i < S::ahead * S::parts * S::part / 4; i += kThreads) reinterpret_cast<uint32_t*>(s_part)[i] = 0u;
+    // s of a stage into [rank][row] parts: eight rows of a rank per thread
+    auto split = [&](int buf, int set) {
         const float* ss = reinterpret_cast<const float*>(smem + buf * S::stage + S::vbytes);
+        uint8_t* pt = s_part + set * S::parts * S::part;
         for (int i = tid; i < 8 * R; i += kThreads) {
             const int j = i % R, c = i / R;
             float f[8];
@@ -1468,7 +1455,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
                 }
 #pragma unroll
                 for (int q = 0; q < 2; ++q) {
-                    uint8_t* to = s_part + j * 256 + (((2 * c + q) ^ ((j & 7) << 1)) << 4);
+                    uint8_t* to = pt + j * 256 + (((2 * c + q) ^ ((j & 7) << 1)) << 4);
                     *reinterpret_cast<uint4*>(to) = make_uint4(h[4 * q], h[4 * q + 1], h[4 * q + 2], h[4 * q + 3]);
                     *reinterpret_cast<uint4*>(to + S::part) = make_uint4(l[4 * q], l[4 * q + 1], l[4 * q + 2], l[4 * q + 3]);
                 }
@@ -1478,14 +1465,16 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
                 split3(f[2], f[3], h.y, m.y, l.y);
                 split3(f[4], f[5], h.z, m.z, l.z);
                 split3(f[6], f[7], h.w, m.w, l.w);
-                uint8_t* to = s_part + j * 128 + ((c ^ (j & 7)) << 4);
+                uint8_t* to = pt + j * 128 + ((c ^ (j & 7)) << 4);
                 *reinterpret_cast<uint4*>(to) = h;
                 *reinterpret_cast<uint4*>(to + S::part) = m;
                 *reinterpret_cast<uint4*>(to + 2 * S::part) = l;
             }
         }
-        __syncthreads();
+    };
+    auto product = [&](int buf, int set) {
         const uint32_t vb = base + buf * S::stage;
+        const uint8_t* pt = s_part + set * S::parts * S::part;
 #pragma unroll
         for (int k0 = 0; k0 < S::rows / RG; k0 += 16) {
             const int r0 = rg * (S::rows / RG) + k0;       // 16 rows of the stage
@@ -1539,7 +1528,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 const int j = 16 * m + g + 8 * e, r = r0 + 2 * t + 8 * h;
-                                const uint2 z = *reinterpret_cast<const uint2*>(s_part + q * S::part + j * 256 + (((r >> 2) ^ ((j & 7) << 1)) << 4) + (r & 3) * 4);
+                                const uint2 z = *reinterpret_cast<const uint2*>(pt + q * S::part + j * 256 + (((r >> 2) ^ ((j & 7) << 1)) << 4) + (r & 3) * 4);
                                 f[q][e] = z.x, f[q][2 + e] = z.y;
                             }
 #pragma unroll
@@ -1554,15 +1543,58 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
                     for (int q = 2; q >= 0; --q) {         // smallest part first
                         uint32_t f[4];
                         const int j = 16 * m + (lane & 15), c = (r0 >> 3) + (lane >> 4);
-                        ldmatrix4(f, part0 + q * S::part + j * 128 + ((c ^ (j & 7)) << 4));
+                        ldmatrix4(f, part0 + set * S::parts * S::part + q * S::part + j * 128 + ((c ^ (j & 7)) << 4));
 #pragma unroll
                         for (int i = 0; i < NT; ++i) mma16<__nv_bfloat16>(acc[m][i], f, b[i][0], b[i][1]);
                     }
                 }
             }
         }
-        if (more) put_held(next);
-        buf = buf == S::stages - 1 ? 0 : buf + 1;
+    };
+    rows_of(st0);
+#pragma unroll
+    for (int i = 0; i < S::stages - 1; ++i) {
+        if (st0 + i < st1) fetch(i);
+        async_commit();
+        if (st0 + i < st1) put_held(i);
+        rows_of(st0 + i + 1);
+    }
+    int buf = 0;
+    if constexpr (S::ahead == 2) {
+        static_assert(S::stages == 3, "a stage in use, one being split, one on its way");
+        async_wait<1>();
+        __syncthreads();
+        if (st0 < st1) split(0, 0);
+        for (int st = st0; st < st1; ++st) {
+            const int set = (st - st0) & 1, after = buf == 2 ? 0 : buf + 1, next = buf == 0 ? 2 : buf - 1;
+            async_wait<0>();
+            __syncthreads();                               // the next stage is there and this one is split; the one before it is free
+            const bool more = st + 2 < st1;
+            if (more) fetch(next);
+            async_commit();
+            rows_of(st + 3);
+            // half of the warps of a scheduler begin with the products
+            if (!(warp & 4) && st + 1 < st1) split(after, set ^ 1);
+            product(buf, set);
+            if ((warp & 4) && st + 1 < st1) split(after, set ^ 1);
+            if (more) put_held(next);
+            buf = after;
+        }
+    } else {
+        for (int st = st0; st < st1; ++st) {
+            async_wait<S::stages - 2>();
+            __syncthreads();                               // the stage is there; the one before it and the parts are free
+            const int next = buf == 0 ? S::stages - 1 : buf - 1;
+            const bool more = st + S::stages - 1 < st1;
+            if (more) fetch(next);
+            async_commit();
+            rows_of(st + S::stages);
+            split(buf, 0);
+            __syncthreads();
+            product(buf, 0);
+            if (more) put_held(next);
+            buf = buf == S::stages - 1 ? 0 : buf + 1;
+        }
     }
     async_wait<0>();
     __syncthreads();
@@ -1571,22 +1603,30 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+        for (int h = 0; h < 2; ++h) {
+            float* to = sums + (rg * RT + 16 * m + g + 8 * h) * S::pitch + cg * WC;
+            if constexpr (X8) {                            // NT consecutive columns
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = 16 * m + g + 8 * (e >> 1), c = cg * WC + (X8 ? NT * (2 * t + (e & 1)) + i : 8 * i + 2 * t + (e & 1));
-                sums[(rg * RT + j) * S::cols + c] = acc[m][i][e];
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int i = 0; i < NT; i += 2) *reinterpret_cast<float2*>(to + NT * (2 * t + c) + i) = make_float2(acc[m][i][2 * h + c], acc[m][i + 1][2 * h + c]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < NT; ++i) *reinterpret_cast<float2*>(to + 8 * i + 2 * t) = make_float2(acc[m][i][2 * h], acc[m][i][2 * h + 1]);
             }
+        }
     __syncthreads();
+    constexpr int Q = S::cols / 4;                         // pieces of a rank's columns
     if (RG > 1) {
-        for (int i = tid; i < R * S::cols / 4; i += kThreads) {
-            float4 v = reinterpret_cast<float4*>(sums)[i];
+        for (int i = tid; i < R * Q; i += kThreads) {
+            float* at = sums + i / Q * S::pitch + i % Q * 4;
+            float4 v = *reinterpret_cast<float4*>(at);
 #pragma unroll
             for (int k = 1; k < RG; ++k) {
-                const float4 q = reinterpret_cast<float4*>(sums + k * RT * S::cols)[i];
+                const float4 q = *reinterpret_cast<const float4*>(at + k * RT * S::pitch);
                 v.x += q.x, v.y += q.y, v.z += q.z, v.w += q.w;
             }
-            reinterpret_cast<float4*>(sums)[i] = v;
+            *reinterpret_cast<float4*>(at) = v;
         }
     }
     if (size > 1) {
@@ -1603,13 +1643,14 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
             const int c = i / (R / 4), j = 4 * (i % (R / 4));
             float f[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) f[k] = size > 1 ? cluster_sum1(sums + (j + k) * S::cols + c, size) : sums[(j + k) * S::cols + c];
+            for (int k = 0; k < 4; ++k) f[k] = size > 1 ? cluster_sum1(sums + (j + k) * S::pitch + c, size) : sums[(j + k) * S::pitch + c];
             if (col0 + c < p.W) *reinterpret_cast<float4*>(p.out + ((int64_t)a * p.W + col0 + c) * R + j) = make_float4(f[0], f[1], f[2], f[3]);
         }
     } else {
         for (int i = i0 + tid; i < i1; i += kThreads) {    // four columns of one rank
-            const float4 v = size > 1 ? cluster_sum4(sums + 4 * i, size) : reinterpret_cast<float4*>(sums)[i];
-            const int j = i / (S::cols / 4), c = col0 + 4 * (i % (S::cols / 4));
+            const int j = i / Q, c = col0 + 4 * (i % Q);
+            float* at = sums + j * S::pitch + 4 * (i % Q);
+            const float4 v = size > 1 ? cluster_sum4(at, size) : *reinterpret_cast<float4*>(at);
             float* out = p.out + ((int64_t)a * R + j) * p.W + c;
             const float f[4] = {v.x, v.y, v.z, v.w};
             if (VEC) {
@@ -1683,8 +1724,10 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
             if (s != QMM_OK) return s;
             const int64_t tiles = (p.T + kTileRows - 1) / kTileRows;
-            int size = 1;                                  // blocks that share a tile's K: two per SM in all, 128 elements each at least
-            while (size < 8 && tiles * size < 2 * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
+            int size = 1;                                  // blocks that share a tile's K: as many as run at once in all, 128 elements each at least
+            // (528 blocks where 264 run at once: 24 us against 18.5 for 6000 x 2048 at r = 64)
+            const int64_t most = tiles + (p.T < p.n ? p.T : p.n) / 2;
+            while (size < 8 && 2 * most * size <= NarrowShape<X8, R, LAY, VEC>::blocks * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
             return launch_pdl(kern, dim3((unsigned)(most_tiles(p.T, p.n) * size)), kThreads, smem, size, st, "adapter narrowing launch", p);
         };
         qmm_status s;
