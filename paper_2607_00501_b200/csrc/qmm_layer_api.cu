@@ -297,13 +297,13 @@ qmm_status qmm_lora_grad(const qmm_lora_args* a, void* ws, size_t ws_bytes, void
         QMM_TRY(half ? launch_lora_f16(p, a->r, false, true, bits % 16 == 0, st) : launch_lora_bf16(p, a->r, false, true, bits % 16 == 0, st));
     }
     if (a->dB) {
-        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, a->T, a->n, (int)a->N, a->dB};
+        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, a->T, a->n, (int)a->N, a->dB, 0};
         const bool vec = (pitch_bits(a->dY, a->lddy, 2) | (uintptr_t)(a->N * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, false, true, vec, st) : launch_lora_wgrad_bf16(p, a->r, false, true, vec, st));
     }
     if (a->dA) {
         const bool x8 = a->x_scale != nullptr;
-        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, a->T, a->n, (int)a->K, a->dA};
+        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, a->T, a->n, (int)a->K, a->dA, a->dB != nullptr};
         const bool vec = (pitch_bits(a->X, a->ldx, x8 ? 1 : 2) | (uintptr_t)(a->K * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, x8, false, vec, st) : launch_lora_wgrad_bf16(p, a->r, x8, false, vec, st));
     }

@@ -1317,6 +1317,7 @@ struct WgradP {
     const int *order, *offsets;
     int T, n, W;
     float* out;                                            // [n, R, W] or, TRANS, [n, W, R]
+    int beside;                                            // this launch needs nothing of the one before it, which is the other weight gradient of the same call
 };
 
 // out[a] = sum over the adapter's rows of s (R) x v (W).  A block takes 128 columns of one adapter and 64 rows a stage, two or three stages in flight (cp.async); the blocks of a
@@ -1349,8 +1350,10 @@ template <typename T, bool X8, int R> struct WgradShape {
 template <typename T, bool X8, int R, bool TRANS, bool VEC>
 __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(const WgradP p)
 {
+    // The next launch may begin once everything before this one is complete: the second weight gradient then runs beside the first, without waiting for it at its
+    // beginning, but at its end, so that what comes after it comes after both.
+    if (!p.beside) pdl_wait();
     pdl_launch_dependents();
-    pdl_wait();
     using S = WgradShape<T, X8, R>;
     constexpr int MT = S::MT, NT = S::NT, WC = S::WC, RG = S::RG, RT = S::RT;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -1666,6 +1669,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
         cluster_arrive();                                  // (a block's shared memory stays until the others have read it)
         cluster_wait();
     }
+    if (p.beside) pdl_wait();
 }
 
 // ------------------------------------------------------------------ launches
