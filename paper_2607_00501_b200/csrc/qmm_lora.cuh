@@ -856,16 +856,16 @@ __device__ __forceinline__ bool tile_rows(const LoraP& p, int tile, int lane, in
     return count > 0;
 }
 
-// Shapes of the narrowing product of a tile of 64 rows.  VEC: x and w1 come in stages of 128 elements of K.
-template <bool X8, int R, int LAY, bool VEC> struct NarrowShape {
+// Shapes of the narrowing product of a tile of 64 rows: x and w1 come in stages of 128 elements of K.
+template <bool X8, int R> struct NarrowShape {
     static constexpr int MW = R <= 64 ? 2 : 1;             // row tiles of a warp
     static constexpr int RG = kTileRows / 16 / MW, KP = kWarps / RG;          // row groups x shares of K
     static constexpr int K = 128, chunks = K / 32 / KP;    // elements of a stage; 32-element chunks of a warp
     static constexpr int xbytes = kTileRows * K * (X8 ? 1 : 2), wbytes = K * R * 2, stage = xbytes + wbytes;
     static constexpr int stages = R <= 64 ? 3 : 2;
     static constexpr int sums = KP * kTileRows * R * 4;
-    static constexpr int smem = VEC && stages * stage > sums ? stages * stage : sums;
-    static constexpr int blocks = R <= 32 ? 3 : 2;         // per SM, as registers and shared memory allow
+    static constexpr int smem = stages * stage > sums ? stages * stage : sums;
+    static constexpr int blocks = R <= 32 ? 3 : 2;         // per SM, as shared memory allows
 };
 
 // Places of 16-byte pieces in a stage: conflict-free both for eight rows' pieces at one k (ldmatrix) and for two rows' four neighbouring ones.
@@ -876,12 +876,13 @@ template <int R> __device__ __forceinline__ uint32_t piece_of_k(int k, int c)   
     return (uint32_t)(k * 2 * R + ((c ^ f) << 4));
 }
 
-// acc += tile . w1 over the stages [st0, st1) of K, rows[64] in shared memory.
-template <typename T, bool X8, int R, int LAY>
-__device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R, LAY, true>::MW][R / 8][4], const LoraP& p, const T* __restrict__ w1, const int* rows, uint8_t* smem,
-                                              int st0, int st1)
+// acc += tile . w1 over the stages [st0, st1) of K, rows[64] in shared memory.  VEC: whole pieces of 16 bytes, copied asynchronously; otherwise rows begin anywhere, and a
+// stage's pieces are put together in registers, which wait there during the products of the stage that is there.
+template <typename T, bool X8, int R, int LAY, bool VEC>
+__device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::MW][R / 8][4], const LoraP& p, const T* __restrict__ w1, const int* rows, uint8_t* smem, int st0,
+                                              int st1)
 {
-    using S = NarrowShape<X8, R, LAY, true>;
+    using S = NarrowShape<X8, R>;
     constexpr int MW = S::MW;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int rg = warp % S::RG, kp = warp / S::RG;
@@ -892,44 +893,79 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R, LA
 #pragma unroll
     for (int q = 0; q < XN; ++q) {
         const int r = rows[xr + q * (kThreads / XP)];
-        from[q] = r >= 0 ? (const char*)p.x + (int64_t)r * p.ldx * (X8 ? 1 : 2) + 16 * xc : nullptr;
+        from[q] = r >= 0 ? (const char*)p.x + (int64_t)r * p.ldx * (X8 ? 1 : 2) : nullptr;
     }
+    auto x_at = [&](int q) -> uint32_t {
+        const int r = xr + q * (kThreads / XP);
+        return X8 ? (uint32_t)(r * S::K + ((xc ^ ((r & 3) << 1)) << 4)) : (uint32_t)(r * 2 * S::K) + piece_in_row(r, xc);
+    };
+    // piece i of w1: LAY 0 rank i / 16, elements 8 (i % 16) of the stage; LAY 1 element i / (R / 8) of the stage, ranks 8 (i % (R / 8))
+    auto w_at = [&](int i) -> uint32_t { return S::xbytes + (LAY == 0 ? (uint32_t)(i / 16 * 2 * S::K) + piece_in_row(i / 16, i % 16) : piece_of_k<R>(i / (R / 8), i % (R / 8))); };
+    uint4 held_x[VEC ? 1 : XN], held_w[VEC ? 1 : WN];
     auto fetch = [&](int st, int buf) {
         if (st < st1) {
             const uint32_t to = base + buf * S::stage;
-            const int left = (p.K - st * S::K) * (X8 ? 1 : 2) - 16 * xc, bytes = min(max(left, 0), 16);
+            const int k0 = st * S::K, kx = k0 + 16 * xc / (X8 ? 1 : 2), left = p.K - kx;                                 // first element of this thread's pieces of x
 #pragma unroll
             for (int q = 0; q < XN; ++q) {
-                const int r = xr + q * (kThreads / XP);
-                const int n = from[q] ? bytes : 0;
-                const uint32_t at = X8 ? (uint32_t)(r * S::K + ((xc ^ ((r & 3) << 1)) << 4)) : (uint32_t)(r * 2 * S::K) + piece_in_row(r, xc);
-                async16(to + at, n ? from[q] + (int64_t)st * (S::K * (X8 ? 1 : 2)) : (const char*)p.x, n);
+                if constexpr (VEC) {
+                    const int n = from[q] ? min(max(left * (X8 ? 1 : 2), 0), 16) : 0;
+                    async16(to + x_at(q), n ? from[q] + (int64_t)kx * (X8 ? 1 : 2) : (const char*)p.x, n);
+                } else if constexpr (X8) {
+                    XPiece<T, true, false> a, b;
+                    a.load(from[q], kx, left);
+                    b.load(from[q], kx + 8, left - 8);
+                    held_x[q] = make_uint4(a.u[0], a.u[1], b.u[0], b.u[1]);
+                } else {
+                    uint32_t u[4];
+                    load8<T, false>((const T*)from[q], kx, from[q] ? left : 0, u);
+                    held_x[q] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
             }
 #pragma unroll
             for (int q = 0; q < WN; ++q) {
                 const int i = tid + q * kThreads;
                 if (16 * R < kThreads && i >= 16 * R) break;
-                if constexpr (LAY == 0) {
-                    const int r = i / 16, c = i % 16, k = st * S::K + 8 * c;
+                const int k = k0 + (LAY == 0 ? i % 16 * 8 : i / (R / 8));
+                const T* row = LAY == 0 ? w1 + (int64_t)(i / 16) * p.K : w1 + (int64_t)k * R;
+                const int at = LAY == 0 ? k : i % (R / 8) * 8;
+                if constexpr (VEC) {
                     const int n = k < p.K ? 16 : 0;
-                    async16(to + S::xbytes + r * 2 * S::K + piece_in_row(r, c), n ? w1 + (int64_t)r * p.K + k : w1, n);
+                    async16(to + w_at(i), n ? row + at : w1, n);
                 } else {
-                    constexpr int C = R / 8;
-                    const int r = i / C, c = i % C, k = st * S::K + r;
-                    const int n = k < p.K ? 16 : 0;
-                    async16(to + S::xbytes + piece_of_k<R>(r, c), n ? w1 + (int64_t)k * R + 8 * c : w1, n);
+                    uint32_t u[4];
+                    load8<T, false>(row, at, k < p.K ? (LAY == 0 ? p.K : R) - at : 0, u);
+                    held_w[q] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             }
         }
         async_commit();
     };
+    auto put = [&](int st, int buf) {
+        if constexpr (!VEC) {
+            if (st >= st1) return;
+            uint8_t* to = smem + buf * S::stage;
 #pragma unroll
-    for (int i = 0; i < S::stages - 1; ++i) fetch(st0 + i, i);
+            for (int q = 0; q < XN; ++q) *reinterpret_cast<uint4*>(to + x_at(q)) = held_x[q];
+#pragma unroll
+            for (int q = 0; q < WN; ++q) {
+                const int i = tid + q * kThreads;
+                if (16 * R < kThreads && i >= 16 * R) break;
+                *reinterpret_cast<uint4*>(to + w_at(i)) = held_w[q];
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < S::stages - 1; ++i) {
+        fetch(st0 + i, i);
+        put(st0 + i, i);
+    }
     int buf = 0;
     for (int st = st0; st < st1; ++st) {
         async_wait<S::stages - 2>();
         __syncthreads();                                   // the stage is there; the one before it is free
-        fetch(st + S::stages - 1, buf == 0 ? S::stages - 1 : buf - 1);
+        const int next = buf == 0 ? S::stages - 1 : buf - 1;
+        fetch(st + S::stages - 1, next);
         const uint8_t* xs = smem + buf * S::stage;
         const uint32_t xb = base + buf * S::stage, wb = xb + S::xbytes;
 #pragma unroll
@@ -988,6 +1024,7 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R, LA
                 }
             }
         }
+        put(st + S::stages - 1, next);
         buf = buf == S::stages - 1 ? 0 : buf + 1;
     }
     async_wait<0>();
@@ -997,11 +1034,11 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R, LA
 // The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
 // Bound by HBM (x once); w1 comes from L2.
 template <typename T, bool X8, int R, int LAY, bool VEC>
-__global__ void __launch_bounds__(kThreads, NarrowShape<X8, R, LAY, VEC>::blocks) lora_narrow_kernel(const LoraP p)
+__global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2) lora_narrow_kernel(const LoraP p)
 {
     pdl_launch_dependents();
     pdl_wait();
-    using S = NarrowShape<X8, R, LAY, VEC>;
+    using S = NarrowShape<X8, R>;
     constexpr int MW = S::MW, RG = S::RG, KP = S::KP;
     extern __shared__ __align__(16) uint8_t smem[];
     float* part = reinterpret_cast<float*>(smem);          // [KP][64][R], over the stages; share 0 holds the block's sum in the end
@@ -1016,7 +1053,7 @@ __global__ void __launch_bounds__(kThreads, NarrowShape<X8, R, LAY, VEC>::blocks
         rows[tid] = r >= 0 && r < p.T ? r : -1;
     }
     __syncthreads();
-    const int g = lane >> 2, rg = warp % RG, kp = warp / RG;
+    const int rg = warp % RG, kp = warp / RG;
     const T* w1 = (const T*)p.w1 + (int64_t)a * R * p.K;
     float acc[MW][R / 8][4];
 #pragma unroll
@@ -1024,27 +1061,10 @@ __global__ void __launch_bounds__(kThreads, NarrowShape<X8, R, LAY, VEC>::blocks
 #pragma unroll
         for (int i = 0; i < R / 8; ++i) acc[m][i][0] = acc[m][i][1] = acc[m][i][2] = acc[m][i][3] = 0.0f;
     int c0, c1;
-    if constexpr (VEC) {
-        share_of((p.K + S::K - 1) / S::K, rank, size, c0, c1);
-        narrow_stages<T, X8, R, LAY>(acc, p, w1, rows, smem, c0, c1);
-    } else {
-        const char* xb = (const char*)p.x;
-        const void* xr[MW][2];
+    share_of((p.K + S::K - 1) / S::K, rank, size, c0, c1);
+    narrow_stages<T, X8, R, LAY, VEC>(acc, p, w1, rows, smem, c0, c1);
 #pragma unroll
-        for (int m = 0; m < MW; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = rows[(rg * MW + m) * 16 + g + 8 * h];
-                xr[m][h] = r >= 0 ? xb + r * p.ldx * (X8 ? 1 : 2) : nullptr;
-            }
-        share_of((p.K + 31) / 32, rank, size, c0, c1);
-        if ((rg * MW) * 16 < count)
-            narrow<T, X8, R, LAY, VEC, MW>(acc, *reinterpret_cast<const void* const(*)[MW][2]>(&xr), w1, p.K, p.int8, c0 + kp, c1, KP, lane);
-    }
-    // accumulator columns: as narrow() has them, or, from stages with LAY 1, plain
-    constexpr int ORDER = VEC ? 0 : LAY;
-#pragma unroll
-    for (int m = 0; m < MW; ++m) put_narrow<R, ORDER>(acc[m], part + (kp * kTileRows + (rg * MW + m) * 16) * R, lane);
+    for (int m = 0; m < MW; ++m) put_narrow<R, 0>(acc[m], part + (kp * kTileRows + (rg * MW + m) * 16) * R, lane);
     __syncthreads();
     for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
         float4 v = reinterpret_cast<float4*>(part)[i];
@@ -1085,7 +1105,7 @@ __device__ __forceinline__ uint32_t y_place(int r, int c) { return (uint32_t)(r 
 
 // y = rn(y0 + back * (u . w2)) over the stages [s0, s1) of 128 columns.  y0 and w2 come by cp.async in whole pieces of rows; a warp takes one column group of a stage and MU of its
 // row tiles, and stores y from its fragments.
-template <typename T, int R, int LAY>
+template <typename T, int R, int LAY, bool VEC>
 __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict__ w2, const int* rows, const uint8_t* hi, const uint8_t* lo, const float* back, uint8_t* stages,
                                              int count, int s0, int s1)
 {
@@ -1098,7 +1118,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int r = rows[fr + 16 * q];
-        from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 + 8 * fc : nullptr;
+        from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 : nullptr;
     }
     T* to[MU][2];
     float factor[MU][2];
@@ -1111,42 +1131,75 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
             factor[m][h] = back[at];
         }
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(stages);
+    constexpr int WN = 16 * R / kThreads ? 16 * R / kThreads : 1;             // pieces of w2 of a thread
+    // piece i of w2.  LAY 0: row n = i / (R / 8) of 2 R bytes, at the row that its fragment has: column c of tile t of a group at 8 t + c.  LAY 1: rank i / 16, columns 8 (i % 16)
+    auto w_at = [&](int i) -> uint32_t {
+        if (LAY == 0) {
+            const int n = i / (R / 8), at_row = (n & ~31) + ((n & 6) << 2) + ((n >> 3 & 3) << 1) + (n & 1);
+            return S::ybytes + piece_of_k<R>(at_row, i % (R / 8));
+        }
+        const int j = i / 16;
+        return S::ybytes + j * 256 + ((i % 16 ^ (((j >> 1) & 3) << 1)) << 4);
+    };
+    uint4 held_y[VEC ? 1 : 4], held_w[VEC ? 1 : WN];       // as in narrow_stages
     auto fetch = [&](int st, int buf) {
         if (st < s1) {
             const uint32_t at = base + buf * S::stage;
-            const int n0 = st * S::cols;
-            const bool there = n0 + 8 * fc < p.N;
+            const int n0 = st * S::cols, left = p.N - (n0 + 8 * fc);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const bool in = there && from[q];
-                async16(at + y_place(fr + 16 * q, fc), in ? (const void*)(from[q] + n0) : w2, in ? 16 : 0);
+                if constexpr (VEC) {
+                    const bool in = left > 0 && from[q];
+                    async16(at + y_place(fr + 16 * q, fc), in ? from[q] + n0 + 8 * fc : w2, in ? 16 : 0);
+                } else {
+                    uint32_t u[4];
+                    load8<T, false, false>(from[q], n0 + 8 * fc, from[q] ? left : 0, u);
+                    held_y[q] = make_uint4(u[0], u[1], u[2], u[3]);
+                }
             }
-            constexpr int WN = 16 * R / kThreads ? 16 * R / kThreads : 1;     // pieces of w2 of a thread
 #pragma unroll
             for (int q = 0; q < WN; ++q) {
                 const int i = tid + q * kThreads;
                 if (16 * R < kThreads && i >= 16 * R) break;
-                if constexpr (LAY == 0) {                  // row n of 2 R bytes, at the row that its fragment has: column c of tile i of a group at 8 i + c
-                    constexpr int C = R / 8;
-                    const int n = i / C, c = i % C, at_row = (n & ~31) + ((n & 6) << 2) + ((n >> 3 & 3) << 1) + (n & 1);
-                    const bool in = n0 + n < p.N;
-                    async16(at + S::ybytes + piece_of_k<R>(at_row, c), in ? w2 + (int64_t)(n0 + n) * R + 8 * c : w2, in ? 16 : 0);
-                } else {                                   // rank j, 128 columns
-                    const int j = i / 16, c = i % 16;
-                    const bool in = n0 + 8 * c < p.N;
-                    async16(at + S::ybytes + j * 256 + ((c ^ (((j >> 1) & 3) << 1)) << 4), in ? w2 + (int64_t)j * p.N + n0 + 8 * c : w2, in ? 16 : 0);
+                const int n = n0 + (LAY == 0 ? i / (R / 8) : i % 16 * 8), col = LAY == 0 ? i % (R / 8) * 8 : n;
+                const T* row = LAY == 0 ? w2 + (int64_t)n * R : w2 + (int64_t)(i / 16) * p.N;
+                if constexpr (VEC) {
+                    const bool in = n < p.N;
+                    async16(at + w_at(i), in ? row + col : w2, in ? 16 : 0);
+                } else {
+                    uint32_t u[4];
+                    load8<T, false>(row, col, n < p.N ? (LAY == 0 ? R : p.N) - col : 0, u);
+                    held_w[q] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             }
         }
         async_commit();
     };
+    auto put = [&](int st, int buf) {
+        if constexpr (!VEC) {
+            if (st >= s1) return;
+            uint8_t* at = stages + buf * S::stage;
 #pragma unroll
-    for (int i = 0; i < S::stages - 1; ++i) fetch(s0 + i, i);
+            for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(at + y_place(fr + 16 * q, fc)) = held_y[q];
+#pragma unroll
+            for (int q = 0; q < WN; ++q) {
+                const int i = tid + q * kThreads;
+                if (16 * R < kThreads && i >= 16 * R) break;
+                *reinterpret_cast<uint4*>(at + w_at(i)) = held_w[q];
+            }
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < S::stages - 1; ++i) {
+        fetch(s0 + i, i);
+        put(s0 + i, i);
+    }
     int buf = 0;
     for (int st = s0; st < s1; ++st) {
         async_wait<S::stages - 2>();
         __syncthreads();                                   // the stage is there; the one before it is free
-        fetch(st + S::stages - 1, buf == 0 ? S::stages - 1 : buf - 1);
+        const int next = buf == 0 ? S::stages - 1 : buf - 1;
+        fetch(st + S::stages - 1, next);
         const uint8_t* ys = stages + buf * S::stage;
         const uint32_t ws = base + buf * S::stage + S::ybytes;
         float acc[MU][tiles][4];
@@ -1218,21 +1271,22 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
                         const float2 r = fma2(f, c, Dt<T>::up2(y0[k]));
                         o[k] = Dt<T>::down2(r.x, r.y);
                     }
-                    if (left > v) *reinterpret_cast<uint4*>(to[m][h] + n0 + v) = make_uint4(o[0], o[1], o[2], o[3]);
+                    store8<T, VEC>(to[m][h] + n0 + v, left - v, o);
                 }
             }
+        put(st + S::stages - 1, next);
         buf = buf == S::stages - 1 ? 0 : buf + 1;
     }
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
 template <typename T, int R, int LAY, bool VEC>
-__global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : 2) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
+__global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
 {
     pdl_launch_dependents();
     pdl_wait();
     extern __shared__ __align__(16) uint8_t smem[];
-    uint8_t *hi = smem, *lo = smem + kTileRows * u_pitch<R>, *stages = smem + 2 * kTileRows * u_pitch<R>;        // (stages: VEC alone)
+    uint8_t *hi = smem, *lo = smem + kTileRows * u_pitch<R>, *stages = smem + 2 * kTileRows * u_pitch<R>;
     __shared__ float back[kTileRows];
     __shared__ int rows[kTileRows];
     constexpr int G = Wide<LAY>::cols;
@@ -1268,41 +1322,9 @@ __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : 2)
     }
     __syncthreads();
     const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
-    const int g = lane >> 2, t = lane & 3, own = Wide<LAY>::own * t;
     const int last = min((span + 1) * per_span, groups);
-    using W = WideWeights<T, R, LAY, VEC>;
-    if constexpr (!VEC) {
-        // a column group in phases of HM row tiles; the next phase's y0 is on its way during the products of this one
-        constexpr int HM = LAY == 0 ? 2 : 1, PH = 4 / HM;
-        YPiece<T, LAY, VEC> y0[2][HM];
-        W w;
-        auto load_y = [&](int c, int ph, YPiece<T, LAY, VEC> (&y)[HM]) {
-#pragma unroll
-            for (int m = 0; m < HM; ++m) {
-                const int at = (ph * HM + m) * 16 + g, row[2] = {c < last ? rows[at] : -1, c < last ? rows[at + 8] : -1};
-                y[m].load((const T*)p.y0, p.ldy0, row, c * G + own, p.N);
-            }
-        };
-        int c = span * per_span + warp;
-        load_y(c, 0, y0[0]);
-        for (; c < last; c += kWarps) {
-            w.load(w2, c * G, p.N, lane);
-#pragma unroll
-            for (int ph = 0; ph < PH; ++ph) {
-                if (ph + 1 < PH) load_y(c, ph + 1, y0[(ph + 1) & 1]);
-                else load_y(c + kWarps, 0, y0[(ph + 1) & 1]);
-#pragma unroll
-                for (int m = 0; m < HM; ++m) {
-                    const int mt = ph * HM + m;
-                    if (mt * 16 >= count) continue;
-                    const int row[2] = {rows[mt * 16 + g], rows[mt * 16 + g + 8]};
-                    widen<T, R, LAY, VEC>(w, y0[ph & 1][m], hi, lo, back, mt, (T*)p.y, p.ldy, row, c * G + own, p.N, lane);
-                }
-            }
-        }
-    } else {
-        widen_stages<T, R, LAY>(p, w2, rows, hi, lo, back, stages, count, span * per_span / (WideShape<R, LAY>::cols / G), (last * G + WideShape<R, LAY>::cols - 1) / WideShape<R, LAY>::cols);
-    }
+    constexpr int per_stage = WideShape<R, LAY>::cols / G;
+    widen_stages<T, R, LAY, VEC>(p, w2, rows, hi, lo, back, stages, count, span * per_span / per_stage, (last + per_stage - 1) / per_stage);
 }
 
 // ------------------------------------------------------------------ weight gradients
@@ -1722,7 +1744,7 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
                 while (size < kSmallBlocks && 2 * size <= longest / 64 && clusters * size * 2 <= 2 * kNumSMs) size *= 2;
                 return launch_pdl(kern, dim3((unsigned)((grouped ? clusters : p.T) * size)), kThreads, smem, size, st, "adapter launch", p, (int)(grouped ? need : 0));
             }
-            constexpr int smem = NarrowShape<X8, R, LAY, VEC>::smem;
+            constexpr int smem = NarrowShape<X8, R>::smem;
             static std::atomic<uint64_t> configured{0};
             auto kern = lora_narrow_kernel<T, X8, R, LAY, VEC>;
             const qmm_status s = configure_once(configured, kern, smem, false, "adapter attributes");
@@ -1731,7 +1753,7 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
             int size = 1;                                  // blocks that share a tile's K: as many as run at once in all, 128 elements each at least
             // (528 blocks where 264 run at once: 24 us against 18.5 for 6000 x 2048 at r = 64)
             const int64_t most = tiles + (p.T < p.n ? p.T : p.n) / 2;
-            while (size < 8 && 2 * most * size <= NarrowShape<X8, R, LAY, VEC>::blocks * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
+            while (size < 8 && 2 * most * size <= (VEC ? NarrowShape<X8, R>::blocks : 2) * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
             return launch_pdl(kern, dim3((unsigned)(most_tiles(p.T, p.n) * size)), kThreads, smem, size, st, "adapter narrowing launch", p);
         };
         qmm_status s;
@@ -1745,7 +1767,7 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
         if (blocks + rest > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapters: %lld blocks are too many for one launch", (long long)(blocks + rest));
-        constexpr int smem = 2 * kTileRows * u_pitch<R> + (VEC ? WideShape<R, LAY>::stages * WideShape<R, LAY>::stage : 0);
+        constexpr int smem = 2 * kTileRows * u_pitch<R> + WideShape<R, LAY>::stages * WideShape<R, LAY>::stage;
         static std::atomic<uint64_t> configured{0};
         auto kern = lora_widen_kernel<T, R, LAY, VEC>;
         s = configure_once(configured, kern, smem, false, "adapter attributes");
