@@ -19,8 +19,8 @@ qmm_status launch_rms_norm_grad(int dtype, const void* dy, int64_t lddy, const v
                                 int64_t lddh, void* dx, int64_t lddx, float* dw, void* ws, cudaStream_t st);
 qmm_status launch_rows8_dequantize(int row8, const void* codes, int64_t ldc, const float* scales, int64_t rows, int K, int dtype, void* out, int64_t ldo, cudaStream_t st);
 
-qmm_status launch_lora_f16(const lora::LoraP& p, int r, bool x8, bool back, bool vec, cudaStream_t st);
-qmm_status launch_lora_bf16(const lora::LoraP& p, int r, bool x8, bool back, bool vec, cudaStream_t st);
+qmm_status launch_lora_f16(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st);
+qmm_status launch_lora_bf16(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st);
 qmm_status launch_lora_wgrad_f16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
 qmm_status launch_lora_wgrad_bf16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
 size_t expert_sort_workspace_bytes(int64_t P, int E);
@@ -111,6 +111,14 @@ static qmm_status check_lora_x(const char* who, const qmm_lora_args* a)
 }
 
 static uintptr_t pitch_bits(const void* p, int64_t ld, int size) { return p ? reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size) : 0; }
+
+// Lowest bits of the addresses and row pitches of the first product's rows and weights, of the second's (y0), and of its outputs with their width.
+struct LoraBits {
+    uintptr_t x, w1, y0, w2, y;
+    bool vx() const { return (x | w1) % 16 == 0; }
+    bool vy() const { return (y0 | w2 | y) % 16 == 0; }
+    int words() const { return (x % 4 == 0) | (w1 % 4 == 0) << 1 | (y0 % 4 == 0) << 2 | (w2 % 4 == 0) << 3; }
+};
 
 // The rows by adapter: the caller's plan, or one made in the workspace.
 static qmm_status lora_plan(const qmm_lora_args* a, const LoraLayout& l, char* ws, const int** order, const int** offsets, const int** units, cudaStream_t st)
@@ -254,11 +262,11 @@ qmm_status qmm_lora(const qmm_lora_args* a, void* ws, size_t ws_bytes, void* str
     const int *order = nullptr, *offsets = nullptr, *units = nullptr;
     if (!small) QMM_TRY(lora_plan(a, l, (char*)ws, &order, &offsets, &units, st));
     const bool x8 = a->x_scale != nullptr, same = a->Y0 == a->Y && a->ldy0 == a->ldy;
-    const uintptr_t bits = pitch_bits(a->X, a->ldx, x8 ? 1 : 2) | pitch_bits(a->A, a->K, 2) | pitch_bits(a->B, a->r, 2) |
-                           pitch_bits(a->Y0, a->ldy0, 2) | pitch_bits(a->Y, a->ldy, 2) | (uintptr_t)(a->N * 2);
+    const LoraBits b = {pitch_bits(a->X, a->ldx, x8 ? 1 : 2), pitch_bits(a->A, a->K, 2), pitch_bits(a->Y0, a->ldy0, 2), pitch_bits(a->B, a->r, 2),
+                        pitch_bits(a->Y, a->ldy, 2) | (uintptr_t)(a->N * 2)};
     const lora::LoraP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, a->idx, order, offsets, units, a->T, a->n, (int)a->K, (int)a->N, a->A, a->B, a->scale,
-                           a->Y0, a->ldy0, a->Y, a->ldy, a->S ? a->S : small ? nullptr : (float*)((char*)ws + l.s), 0, !same};
-    return a->dtype == QMM_F16 ? launch_lora_f16(p, a->r, x8, false, bits % 16 == 0, st) : launch_lora_bf16(p, a->r, x8, false, bits % 16 == 0, st);
+                           a->Y0, a->ldy0, a->Y, a->ldy, a->S ? a->S : small ? nullptr : (float*)((char*)ws + l.s), 0, !same, b.words()};
+    return a->dtype == QMM_F16 ? launch_lora_f16(p, a->r, x8, false, b.vx(), b.vy(), st) : launch_lora_bf16(p, a->r, x8, false, b.vx(), b.vy(), st);
 }
 
 qmm_status qmm_lora_grad(const qmm_lora_args* a, void* ws, size_t ws_bytes, void* stream)
@@ -290,21 +298,24 @@ qmm_status qmm_lora_grad(const qmm_lora_args* a, void* ws, size_t ws_bytes, void
     float* ds = (float*)((char*)ws + l.s);
     if (a->dX || a->dA) {
         const bool same = a->dX0 == a->dX && a->lddx0 == a->lddx;
-        const uintptr_t bits = pitch_bits(a->dY, a->lddy, 2) | pitch_bits(a->B, a->r, 2) | pitch_bits(a->A, a->K, 2) | pitch_bits(a->dX0, a->lddx0, 2) |
-                               pitch_bits(a->dX, a->lddx, 2) | (uintptr_t)(a->N * 2);
+        const LoraBits b = {pitch_bits(a->dY, a->lddy, 2), pitch_bits(a->B, a->r, 2), pitch_bits(a->dX0, a->lddx0, 2), pitch_bits(a->A, a->K, 2),
+                            pitch_bits(a->dX, a->lddx, 2) | (uintptr_t)(a->K * 2)};
+        const bool vx = b.vx() && a->N % 8 == 0;
         const lora::LoraP p = {a->dY, a->lddy, nullptr, 0, a->idx, order, offsets, units, a->T, a->n, (int)a->N, (int)a->K, a->B, a->A, a->scale, a->dX0, a->lddx0,
-                               a->dX, a->lddx, ds, 1, a->dX && !same};
-        QMM_TRY(half ? launch_lora_f16(p, a->r, false, true, bits % 16 == 0, st) : launch_lora_bf16(p, a->r, false, true, bits % 16 == 0, st));
+                               a->dX, a->lddx, ds, 1, a->dX && !same, b.words()};
+        QMM_TRY(half ? launch_lora_f16(p, a->r, false, true, vx, b.vy(), st) : launch_lora_bf16(p, a->r, false, true, vx, b.vy(), st));
     }
     if (a->dB) {
-        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, a->T, a->n, (int)a->N, a->dB, 0};
-        const bool vec = (pitch_bits(a->dY, a->lddy, 2) | (uintptr_t)(a->N * 2)) % 16 == 0;
+        const uintptr_t bits = pitch_bits(a->dY, a->lddy, 2);
+        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, a->T, a->n, (int)a->N, a->dB, bits % 4 == 0, 0};
+        const bool vec = (bits | (uintptr_t)(a->N * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, false, true, vec, st) : launch_lora_wgrad_bf16(p, a->r, false, true, vec, st));
     }
     if (a->dA) {
         const bool x8 = a->x_scale != nullptr;
-        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, a->T, a->n, (int)a->K, a->dA, a->dB != nullptr};
-        const bool vec = (pitch_bits(a->X, a->ldx, x8 ? 1 : 2) | (uintptr_t)(a->K * 2)) % 16 == 0;
+        const uintptr_t bits = pitch_bits(a->X, a->ldx, x8 ? 1 : 2);
+        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, a->T, a->n, (int)a->K, a->dA, bits % 4 == 0, a->dB != nullptr};
+        const bool vec = (bits | (uintptr_t)(a->K * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, x8, false, vec, st) : launch_lora_wgrad_bf16(p, a->r, x8, false, vec, st));
     }
     return QMM_OK;

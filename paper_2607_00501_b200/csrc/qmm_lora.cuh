@@ -556,7 +556,17 @@ struct LoraP {
     float* s;                                              // [T, R]
     int s_scaled;                                          // what s keeps: 0 the narrowing product, 1 that times scale
     int rest;                                              // rows without an adapter get y0 (0: they have it already)
+    int words;                                             // operands whose rows begin at whole words: 1 x, 2 w1, 4 y0, 8 w2
 };
+// A piece of 16 bytes of which `bytes` exist, by words: for rows that begin at whole words.  safe: any valid address.
+__device__ __forceinline__ void async_words(uint32_t to, const void* from, int bytes, const void* safe)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int n = min(max(bytes - 4 * i, 0), 4);
+        async4(to + 4 * i, n ? (const char*)from + 4 * i : safe, n);
+    }
+}
 
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
@@ -876,8 +886,8 @@ template <int R> __device__ __forceinline__ uint32_t piece_of_k(int k, int c)   
     return (uint32_t)(k * 2 * R + ((c ^ f) << 4));
 }
 
-// acc += tile . w1 over the stages [st0, st1) of K, rows[64] in shared memory.  VEC: whole pieces of 16 bytes, copied asynchronously; otherwise rows begin anywhere, and a
-// stage's pieces are put together in registers, which wait there during the products of the stage that is there.
+// acc += tile . w1 over the stages [st0, st1) of K, rows[64] in shared memory.  VEC: whole pieces of 16 bytes, copied asynchronously.  Otherwise rows begin at whole words, which
+// are copied one by one (p.words), or anywhere: then a stage's pieces are put together in registers, which wait there during the products of the stage that is there.
 template <typename T, bool X8, int R, int LAY, bool VEC>
 __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::MW][R / 8][4], const LoraP& p, const T* __restrict__ w1, const int* rows, uint8_t* smem, int st0,
                                               int st1)
@@ -911,6 +921,8 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
                 if constexpr (VEC) {
                     const int n = from[q] ? min(max(left * (X8 ? 1 : 2), 0), 16) : 0;
                     async16(to + x_at(q), n ? from[q] + (int64_t)kx * (X8 ? 1 : 2) : (const char*)p.x, n);
+                } else if (p.words & 1) {
+                    async_words(to + x_at(q), from[q] + (int64_t)kx * (X8 ? 1 : 2), from[q] ? left * (X8 ? 1 : 2) : 0, p.x);
                 } else if constexpr (X8) {
                     XPiece<T, true, false> a, b;
                     a.load(from[q], kx, left);
@@ -932,6 +944,8 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
                 if constexpr (VEC) {
                     const int n = k < p.K ? 16 : 0;
                     async16(to + w_at(i), n ? row + at : w1, n);
+                } else if (p.words & 2) {
+                    async_words(to + w_at(i), row + at, k < p.K ? 2 * ((LAY == 0 ? p.K : R) - at) : 0, w1);
                 } else {
                     uint32_t u[4];
                     load8<T, false>(row, at, k < p.K ? (LAY == 0 ? p.K : R) - at : 0, u);
@@ -945,13 +959,17 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
         if constexpr (!VEC) {
             if (st >= st1) return;
             uint8_t* to = smem + buf * S::stage;
+            if (!(p.words & 1)) {
 #pragma unroll
-            for (int q = 0; q < XN; ++q) *reinterpret_cast<uint4*>(to + x_at(q)) = held_x[q];
+                for (int q = 0; q < XN; ++q) *reinterpret_cast<uint4*>(to + x_at(q)) = held_x[q];
+            }
+            if (!(p.words & 2)) {
 #pragma unroll
-            for (int q = 0; q < WN; ++q) {
-                const int i = tid + q * kThreads;
-                if (16 * R < kThreads && i >= 16 * R) break;
-                *reinterpret_cast<uint4*>(to + w_at(i)) = held_w[q];
+                for (int q = 0; q < WN; ++q) {
+                    const int i = tid + q * kThreads;
+                    if (16 * R < kThreads && i >= 16 * R) break;
+                    *reinterpret_cast<uint4*>(to + w_at(i)) = held_w[q];
+                }
             }
         }
     };
@@ -1151,6 +1169,8 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
                 if constexpr (VEC) {
                     const bool in = left > 0 && from[q];
                     async16(at + y_place(fr + 16 * q, fc), in ? from[q] + n0 + 8 * fc : w2, in ? 16 : 0);
+                } else if (p.words & 4) {
+                    async_words(at + y_place(fr + 16 * q, fc), from[q] + n0 + 8 * fc, from[q] ? 2 * left : 0, w2);
                 } else {
                     uint32_t u[4];
                     load8<T, false, false>(from[q], n0 + 8 * fc, from[q] ? left : 0, u);
@@ -1166,6 +1186,8 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
                 if constexpr (VEC) {
                     const bool in = n < p.N;
                     async16(at + w_at(i), in ? row + col : w2, in ? 16 : 0);
+                } else if (p.words & 8) {
+                    async_words(at + w_at(i), row + col, n < p.N ? 2 * ((LAY == 0 ? R : p.N) - col) : 0, w2);
                 } else {
                     uint32_t u[4];
                     load8<T, false>(row, col, n < p.N ? (LAY == 0 ? R : p.N) - col : 0, u);
@@ -1179,13 +1201,17 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
         if constexpr (!VEC) {
             if (st >= s1) return;
             uint8_t* at = stages + buf * S::stage;
+            if (!(p.words & 4)) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(at + y_place(fr + 16 * q, fc)) = held_y[q];
+                for (int q = 0; q < 4; ++q) *reinterpret_cast<uint4*>(at + y_place(fr + 16 * q, fc)) = held_y[q];
+            }
+            if (!(p.words & 8)) {
 #pragma unroll
-            for (int q = 0; q < WN; ++q) {
-                const int i = tid + q * kThreads;
-                if (16 * R < kThreads && i >= 16 * R) break;
-                *reinterpret_cast<uint4*>(at + w_at(i)) = held_w[q];
+                for (int q = 0; q < WN; ++q) {
+                    const int i = tid + q * kThreads;
+                    if (16 * R < kThreads && i >= 16 * R) break;
+                    *reinterpret_cast<uint4*>(at + w_at(i)) = held_w[q];
+                }
             }
         }
     };
@@ -1339,6 +1365,7 @@ struct WgradP {
     const int *order, *offsets;
     int T, n, W;
     float* out;                                            // [n, R, W] or, TRANS, [n, W, R]
+    int words;                                             // v's rows begin at whole words
     int beside;                                            // this launch needs nothing of the one before it, which is the other weight gradient of the same call
 };
 
@@ -1427,6 +1454,8 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
             if constexpr (VEC) {
                 const int bytes = row ? min(max(vleft * es, 0), 16) : 0;
                 async16(to + v_place(vr + q * VS, vc), bytes ? row + (int64_t)vcol * es : p.v, bytes);
+            } else if (p.words) {
+                async_words(to + v_place(vr + q * VS, vc), row + (int64_t)vcol * es, row ? vleft * es : 0, p.v);
             } else if constexpr (!X8) {
                 load8<T, false>((const T*)row, vcol, row ? vleft : 0, held[q]);
             } else {
@@ -1445,10 +1474,10 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
             async4((uint32_t)__cvta_generic_to_shared(s_scale + buf * S::rows + tid), xrow >= 0 ? p.v_scale + xrow : p.v_scale, xrow >= 0 ? 4 : 0);
     };
     auto put_held = [&](int buf) {
-        if constexpr (!VEC) {
+        if (!VEC && !p.words) {
 #pragma unroll
             for (int q = 0; q < VN; ++q)
-                *reinterpret_cast<uint4*>(smem + buf * S::stage + v_place(vr + q * VS, vc)) = make_uint4(held[q][0], held[q][1], held[q][2], held[q][3]);
+                *reinterpret_cast<uint4*>(smem + buf * S::stage + v_place(vr + q * VS, vc)) = make_uint4(held[VEC ? 0 : q][0], held[VEC ? 0 : q][1], held[VEC ? 0 : q][2], held[VEC ? 0 : q][3]);
         }
     };
 
@@ -1722,13 +1751,14 @@ static int64_t most_tiles(int64_t T, int64_t n)
     return 2 * ((T + 127 * used) / 128);
 }
 
-template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const LoraP& p, int r, bool x8, cudaStream_t st)
+// vx, vy: x and w1, y and w2 have rows of whole 16-byte pieces.
+template <typename T, int LAY> static qmm_status launch_pair(const LoraP& p, int r, bool x8, bool vx, bool vy, cudaStream_t st)
 {
     return by_rank(r, [&](auto rank) {
         constexpr int R = decltype(rank)::value;
         constexpr int G = Wide<LAY>::cols;
-        auto narrowed = [&](auto e8) {
-            constexpr bool X8 = decltype(e8)::value;
+        auto narrowed = [&](auto e8, auto vec) {
+            constexpr bool X8 = decltype(e8)::value, VEC = decltype(vec)::value;
             if (p.T <= kSmallRows) {
                 constexpr int smem = (kWarps + kSmallBlocks) * 16 * R * 4 + 2 * 16 * u_pitch<R>;              // (at least the 4 KB of the counts)
                 static std::atomic<uint64_t> configured{0};
@@ -1756,10 +1786,13 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
             while (size < 8 && 2 * most * size <= (VEC ? NarrowShape<X8, R>::blocks : 2) * kNumSMs && p.K / (2 * size) >= 128) size *= 2;
             return launch_pdl(kern, dim3((unsigned)(most_tiles(p.T, p.n) * size)), kThreads, smem, size, st, "adapter narrowing launch", p);
         };
-        qmm_status s;
-        if constexpr (LAY == 0) s = x8 ? narrowed(std::true_type()) : narrowed(std::false_type());
-        else s = narrowed(std::false_type());
-        if (s != QMM_OK || p.T <= kSmallRows || !p.y) return s;
+        auto first = [&](auto vec) {
+            if constexpr (LAY == 0) return x8 ? narrowed(std::true_type(), vec) : narrowed(std::false_type(), vec);
+            else return narrowed(std::false_type(), vec);
+        };
+        const bool small = p.T <= kSmallRows, v1 = small ? vx && vy : vx;
+        const qmm_status s = v1 ? first(std::true_type()) : first(std::false_type());
+        if (s != QMM_OK || small || !p.y) return s;
         const int groups = (p.N + G - 1) / G;
         // column groups of a block: 1024 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns)
         int per_span = 1024 / G;
@@ -1767,12 +1800,16 @@ template <typename T, int LAY, bool VEC> static qmm_status launch_pair(const Lor
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
         if (blocks + rest > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapters: %lld blocks are too many for one launch", (long long)(blocks + rest));
-        constexpr int smem = 2 * kTileRows * u_pitch<R> + WideShape<R, LAY>::stages * WideShape<R, LAY>::stage;
-        static std::atomic<uint64_t> configured{0};
-        auto kern = lora_widen_kernel<T, R, LAY, VEC>;
-        s = configure_once(configured, kern, smem, false, "adapter attributes");
-        if (s != QMM_OK) return s;
-        return launch_pdl(kern, dim3((unsigned)(blocks + rest)), kThreads, smem, 1, st, "adapter widening launch", p, spans, per_span, (int)blocks);
+        auto widened = [&](auto vec) {
+            constexpr bool VEC = decltype(vec)::value;
+            constexpr int smem = 2 * kTileRows * u_pitch<R> + WideShape<R, LAY>::stages * WideShape<R, LAY>::stage;
+            static std::atomic<uint64_t> configured{0};
+            auto kern = lora_widen_kernel<T, R, LAY, VEC>;
+            const qmm_status c = configure_once(configured, kern, smem, false, "adapter attributes");
+            if (c != QMM_OK) return c;
+            return launch_pdl(kern, dim3((unsigned)(blocks + rest)), kThreads, smem, 1, st, "adapter widening launch", p, spans, per_span, (int)blocks);
+        };
+        return vy ? widened(std::true_type()) : widened(std::false_type());
     });
 }
 
@@ -1806,10 +1843,9 @@ template <typename T, bool TRANS, bool VEC> static qmm_status launch_wgrad(const
 
 // forward: both products of x with (A, B); backward: of dy with (B, A)
 #define QMM_LORA_TYPE(NAME, TYPE)                                                                                                                          \
-    qmm_status launch_lora_##NAME(const lora::LoraP& p, int r, bool x8, bool back, bool vec, cudaStream_t st)                                              \
+    qmm_status launch_lora_##NAME(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st)                                      \
     {                                                                                                                                                      \
-        if (back) return vec ? lora::launch_pair<TYPE, 1, true>(p, r, false, st) : lora::launch_pair<TYPE, 1, false>(p, r, false, st);                     \
-        return vec ? lora::launch_pair<TYPE, 0, true>(p, r, x8, st) : lora::launch_pair<TYPE, 0, false>(p, r, x8, st);                                     \
+        return back ? lora::launch_pair<TYPE, 1>(p, r, false, vx, vy, st) : lora::launch_pair<TYPE, 0>(p, r, x8, vx, vy, st);                              \
     }
 #define QMM_LORA_WGRAD_TYPE(NAME, TYPE)                                                                                                                    \
     qmm_status launch_lora_wgrad_##NAME(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st)                                      \
