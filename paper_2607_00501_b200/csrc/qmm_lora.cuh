@@ -54,11 +54,24 @@ template <typename T> __device__ __forceinline__ void mma16_first(float (&d)[4],
                      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
+__device__ __forceinline__ void mma8_tf32_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
 __device__ __forceinline__ void mma8_tf32(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// acc += d.  The tensor cores cut what does not fit a sum instead of rounding it; over a long chain of products into one accumulator that adds up (2048 rows: 2e-6 of the
+// result), so short chains are added up here, where every addition is rounded to nearest.
+__device__ __forceinline__ void add4(float (&acc)[4], const float (&d)[4])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[i] += d[i];
 }
 __device__ __forceinline__ uint32_t tf32(float v)
 {
@@ -1010,35 +1023,38 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
                 for (int i = 0; i < R / 8; ++i) {
                     const int r = 8 * i + g;
                     const uint4 q = *reinterpret_cast<const uint4*>(xs + S::xbytes + r * 2 * S::K + piece_in_row(r, 4 * c32 + t));
-                    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                    for (int m = 0; m < MW; ++m) {
+                        const uint32_t f0[4] = {a[m][0][0], a[m][1][0], a[m][0][1], a[m][1][1]}, f1[4] = {a[m][0][2], a[m][1][2], a[m][0][3], a[m][1][3]};
+                        float d[4];
+                        mma16_first<T>(d, f0, q.x, q.y);
+                        mma16<T>(d, f1, q.z, q.w);
+                        add4(acc[m][i], d);
+                    }
+                }
+            } else {                                       // fragments in the MMA's own order; accumulator tile i has ranks 8 i .. 8 i + 7
+                uint32_t a[MW][2][4];
+#pragma unroll
+                for (int m = 0; m < MW; ++m)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const int r = (rg * MW + m) * 16 + (lane & 15);
+                        ldmatrix4(a[m][j], xb + r * 2 * S::K + piece_in_row(r, 4 * c32 + 2 * j + (lane >> 4)));
+                    }
+#pragma unroll
+                for (int i = 0; i < R / 8; i += 2) {
+                    uint32_t b[2][4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) ldmatrix4t(b[j], wb + piece_of_k<R>(32 * c32 + 16 * j + (lane & 15), R == 8 ? 0 : i + (lane >> 4)));
 #pragma unroll
                     for (int m = 0; m < MW; ++m)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j) {
-                            const uint32_t f[4] = {a[m][0][2 * j], a[m][1][2 * j], a[m][0][2 * j + 1], a[m][1][2 * j + 1]};
-                            mma16<T>(acc[m][i], f, w[2 * j], w[2 * j + 1]);
+                        for (int h = 0; h < (R > 8 ? 2 : 1); ++h) {
+                            float d[4];
+                            mma16_first<T>(d, a[m][0], b[0][2 * h], b[0][2 * h + 1]);
+                            mma16<T>(d, a[m][1], b[1][2 * h], b[1][2 * h + 1]);
+                            add4(acc[m][i + h], d);
                         }
-                }
-            } else {                                       // fragments in the MMA's own order; accumulator tile i has ranks 8 i .. 8 i + 7
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    uint32_t a[MW][4];
-#pragma unroll
-                    for (int m = 0; m < MW; ++m) {
-                        const int r = (rg * MW + m) * 16 + (lane & 15);
-                        ldmatrix4(a[m], xb + r * 2 * S::K + piece_in_row(r, 4 * c32 + 2 * j + (lane >> 4)));
-                    }
-                    const int k = 32 * c32 + 16 * j + (lane & 15);
-#pragma unroll
-                    for (int i = 0; i < R / 8; i += 2) {
-                        uint32_t b[4];
-                        ldmatrix4t(b, wb + piece_of_k<R>(k, R == 8 ? 0 : i + (lane >> 4)));
-#pragma unroll
-                        for (int m = 0; m < MW; ++m) {
-                            mma16<T>(acc[m][i], a[m], b[0], b[1]);
-                            if constexpr (R > 8) mma16<T>(acc[m][i + 1], a[m], b[2], b[3]);
-                        }
-                    }
                 }
             }
         }
@@ -1529,78 +1545,74 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
     auto product = [&](int buf, int set) {
         const uint32_t vb = base + buf * S::stage;
         const uint8_t* pt = s_part + set * S::parts * S::part;
+        constexpr int TN = NT < 4 ? NT : 4;                // column tiles at a time
 #pragma unroll
         for (int k0 = 0; k0 < S::rows / RG; k0 += 16) {
             const int r0 = rg * (S::rows / RG) + k0;       // 16 rows of the stage
-            uint32_t b[NT][2];                             // pairs of rows (2 t, 2 t + 1) and (2 t + 8, 2 t + 9) of column g of the tile
-            if constexpr (!X8) {
 #pragma unroll
-                for (int i = 0; i < NT; i += 2) {
-                    uint32_t q[4];
-                    const int r = r0 + (lane & 15);
-                    ldmatrix4t(q, vb + v_place(r, cg * (WC / 8) + i + (lane >> 4)));
-                    b[i][0] = q[0], b[i][1] = q[1], b[i + 1][0] = q[2], b[i + 1][1] = q[3];
-                }
-            } else {                                       // tile i has column NT g + i at place g: NT codes of a row per lane
-                uint32_t x[4][(NT + 1) / 2];
+            for (int i0 = 0; i0 < NT; i0 += TN) {
+                uint32_t b[TN][2];                         // pairs of rows (2 t, 2 t + 1) and (2 t + 8, 2 t + 9) of column g of the tile
+                if constexpr (!X8) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int r = r0 + 2 * t + (q & 1) + 8 * (q >> 1), at = cg * WC + NT * g;
-                    const uint8_t* c = smem + buf * S::stage + v_place(r, at >> 4) + (at & 15);
-                    uint32_t w[2] = {0u, 0u};
-                    if constexpr (NT == 8) {
-                        const uint2 z = *reinterpret_cast<const uint2*>(c);
-                        w[0] = z.x, w[1] = z.y;
-                    } else if constexpr (NT == 4) {
-                        w[0] = *reinterpret_cast<const uint32_t*>(c);
-                    } else {
-                        w[0] = *reinterpret_cast<const unsigned short*>(c);
+                    for (int i = 0; i < TN; i += 2) {
+                        uint32_t q[4];
+                        const int r = r0 + (lane & 15);
+                        ldmatrix4t(q, vb + v_place(r, cg * (WC / 8) + i0 + i + (lane >> 4)));
+                        b[i][0] = q[0], b[i][1] = q[1], b[i + 1][0] = q[2], b[i + 1][1] = q[3];
                     }
-                    uint32_t lo, hi;
-                    values4<__nv_bfloat16>(w[0], p.int8, lo, hi);
-                    x[q][0] = lo;
-                    if constexpr (NT >= 4) x[q][1] = hi;
-                    if constexpr (NT == 8) {
-                        values4<__nv_bfloat16>(w[1], p.int8, lo, hi);
-                        x[q][2] = lo, x[q][3] = hi;
+                } else {                                   // tile i has column NT g + i at place g: TN codes of a row per lane
+                    uint32_t x[4][2];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const int r = r0 + 2 * t + (q & 1) + 8 * (q >> 1), at = cg * WC + NT * g + i0;
+                        const uint8_t* c = smem + buf * S::stage + v_place(r, at >> 4) + (at & 15);
+                        const uint32_t w = TN == 4 ? *reinterpret_cast<const uint32_t*>(c) : *reinterpret_cast<const unsigned short*>(c);
+                        values4<__nv_bfloat16>(w, p.int8, x[q][0], x[q][1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < TN; ++i) {
+                        b[i][0] = pair_of(x[0][i >> 1], x[1][i >> 1], i & 1);
+                        b[i][1] = pair_of(x[2][i >> 1], x[3][i >> 1], i & 1);
                     }
                 }
 #pragma unroll
-                for (int i = 0; i < NT; ++i) {
-                    b[i][0] = pair_of(x[0][i >> 1], x[1][i >> 1], i & 1);
-                    b[i][1] = pair_of(x[2][i >> 1], x[3][i >> 1], i & 1);
-                }
-            }
+                for (int m = 0; m < MT; ++m) {
+                    float d[TN][4];
+                    if constexpr (S::tf32) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) {
-                if constexpr (S::tf32) {
+                        for (int h = 0; h < 2; ++h) {      // rows 2 t + 8 h and the next: k = t and t + 4
+                            uint32_t f[2][4];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {          // rows 2 t + 8 h and the next: k = t and t + 4
-                        uint32_t f[2][4];
+                            for (int q = 0; q < 2; ++q)
 #pragma unroll
-                        for (int q = 0; q < 2; ++q)
+                                for (int e = 0; e < 2; ++e) {
+                                    const int j = 16 * m + g + 8 * e, r = r0 + 2 * t + 8 * h;
+                                    const uint2 z = *reinterpret_cast<const uint2*>(pt + q * S::part + j * 256 + (((r >> 2) ^ ((j & 7) << 1)) << 4) + (r & 3) * 4);
+                                    f[q][e] = z.x, f[q][2 + e] = z.y;
+                                }
 #pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const int j = 16 * m + g + 8 * e, r = r0 + 2 * t + 8 * h;
-                                const uint2 z = *reinterpret_cast<const uint2*>(pt + q * S::part + j * 256 + (((r >> 2) ^ ((j & 7) << 1)) << 4) + (r & 3) * 4);
-                                f[q][e] = z.x, f[q][2 + e] = z.y;
+                            for (int i = 0; i < TN; ++i) {
+                                const float2 x = Dt<__half>::up2(b[i][h]);
+                                if (h == 0) mma8_tf32_first(d[i], f[1], __float_as_uint(x.x), __float_as_uint(x.y));
+                                else mma8_tf32(d[i], f[1], __float_as_uint(x.x), __float_as_uint(x.y));
+                                mma8_tf32(d[i], f[0], __float_as_uint(x.x), __float_as_uint(x.y));
                             }
+                        }
+                    } else {
 #pragma unroll
-                        for (int i = 0; i < NT; ++i) {
-                            const float2 x = Dt<__half>::up2(b[i][h]);
-                            mma8_tf32(acc[m][i], f[1], __float_as_uint(x.x), __float_as_uint(x.y));
-                            mma8_tf32(acc[m][i], f[0], __float_as_uint(x.x), __float_as_uint(x.y));
+                        for (int q = 2; q >= 0; --q) {     // smallest part first
+                            uint32_t f[4];
+                            const int j = 16 * m + (lane & 15), c = (r0 >> 3) + (lane >> 4);
+                            ldmatrix4(f, part0 + set * S::parts * S::part + q * S::part + j * 128 + ((c ^ (j & 7)) << 4));
+#pragma unroll
+                            for (int i = 0; i < TN; ++i) {
+                                if (q == 2) mma16_first<__nv_bfloat16>(d[i], f, b[i][0], b[i][1]);
+                                else mma16<__nv_bfloat16>(d[i], f, b[i][0], b[i][1]);
+                            }
                         }
                     }
-                } else {
 #pragma unroll
-                    for (int q = 2; q >= 0; --q) {         // smallest part first
-                        uint32_t f[4];
-                        const int j = 16 * m + (lane & 15), c = (r0 >> 3) + (lane >> 4);
-                        ldmatrix4(f, part0 + set * S::parts * S::part + q * S::part + j * 128 + ((c ^ (j & 7)) << 4));
-#pragma unroll
-                        for (int i = 0; i < NT; ++i) mma16<__nv_bfloat16>(acc[m][i], f, b[i][0], b[i][1]);
-                    }
+                    for (int i = 0; i < TN; ++i) add4(acc[m][i0 + i], d[i]);
                 }
             }
         }

@@ -904,15 +904,14 @@ def lora(x: torch.Tensor, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, y
 
 def lora_grad(dy: torch.Tensor, x: torch.Tensor | None, s: torch.Tensor | None, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, dx0: torch.Tensor | None = None,
               scale: torch.Tensor | None = None, x_scale: torch.Tensor | None = None, plan: ExpertPlan | None = None, ws: torch.Tensor | None = None,
-              dx: torch.Tensor | None = None, da: torch.Tensor | None = None, db: torch.Tensor | None = None):
-    """(dx, da, db): dx [T, K] = dx0 (None: zeros) + the adapters' part, of dy's type; da, db fp32 in a's and b's shapes.  x: as in lora, 16-bit or 8-bit rows."""
+              dx: torch.Tensor | None | bool = None, da: torch.Tensor | None | bool = None, db: torch.Tensor | None | bool = None):
+    """(dx, da, db): dx [T, K] = dx0 (None: zeros) + the adapters' part, of dy's type; da, db fp32 in a's and b's shapes.  x: as in lora, 16-bit or 8-bit rows.
+    dx, da or db False: not wanted (da needs x, db needs s)."""
     T, n, r = dy.shape[0], a.shape[0], a.shape[1]
-    if dx is None:
-        dx = torch.empty((T, a.shape[2]), dtype=dy.dtype, device=dy.device)
-    if da is None:
-        da = torch.empty(a.shape, dtype=torch.float32, device=dy.device)
-    if db is None:
-        db = torch.empty(b.shape, dtype=torch.float32, device=dy.device)
+
+    def out(t, shape, dtype):
+        return None if t is False else torch.empty(shape, dtype=dtype, device=dy.device) if t is None else t
+    dx, da, db = out(dx, (T, a.shape[2]), dy.dtype), out(da, a.shape, torch.float32), out(db, b.shape, torch.float32)
     if ws is None:
         ws = torch.empty(lora_workspace_bytes(T, n, r), dtype=torch.uint8, device=dy.device)
     _check((_layer_ext or _layer()).lora_grad(x, x_scale, idx, a, b, scale, *_lora_plan(plan, T, n), s, dy, dx0, dx, da, db, ws))

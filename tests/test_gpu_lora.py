@@ -200,6 +200,23 @@ def test_parts_alone(qmm, T):
         assert torch.equal(out, want), which
 
 
+def test_what_is_not_wanted(qmm):
+    """False in place of a gradient: the others come alone, and what they do not need may be missing."""
+    p = Problem(qmm, "f16", 90, 128, 160, 3, 16, "dropped")
+    p.forward()
+    dx, da, db = (g.clone() for g in p.backward())
+    got = p.backward(dx=False, da=False)
+    assert got[:2] == (None, None) and torch.equal(got[2], db)
+    got = qmm.lora_grad(p.dy, None, None, p.idx, p.a, p.b, p.dx0, scale=p.scale, da=False, db=False)
+    assert got[1:] == (None, None) and torch.equal(got[0], dx)
+    got = qmm.lora_grad(p.dy, p.x, None, p.idx, p.a, p.b, scale=p.scale, dx=False, db=False)
+    assert torch.equal(got[1], da)
+    with pytest.raises(qmm.QmmError):
+        qmm.lora_grad(p.dy, p.x, None, p.idx, p.a, p.b)
+    with pytest.raises(AssertionError):
+        qmm.lora_grad(p.dy, None, p.s, p.idx, p.a, p.b)
+
+
 @pytest.mark.parametrize("dt", list(HALVES))
 @pytest.mark.parametrize("T,K,N,n,r", [(1, 160, 96, 1, 8), (70, 333, 263, 3, 16), (90, 512, 768, 4, 32), (300, 512, 520, 3, 64), (330, 257, 100, 2, 128), (1000, 128, 128, 20, 8),
                                        (40, 128, 64, 2, 128), (600, 96, 640, 2, 16)])
