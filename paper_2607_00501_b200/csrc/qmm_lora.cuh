@@ -869,7 +869,8 @@ __device__ __forceinline__ int find_part(const int* __restrict__ starts, int n, 
     return found;
 }
 
-// Rows of tile `tile` (64 of a unit of 128 of the sort): adapter, first sorted row, number of rows; false if there are none.
+// Rows of tile `tile` (64 of a unit of 128 of the sort): adapter, first sorted row, number of rows; false if there are none, as in every tile behind the last unit (which
+// counts to the last adapter, behind its rows).
 __device__ __forceinline__ bool tile_rows(const LoraP& p, int tile, int lane, int& a, int& first, int& count)
 {
     a = find_part(p.units, p.n, tile >> 1, lane);
@@ -1080,8 +1081,7 @@ __global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int rank = (int)cluster_rank(), size = (int)cluster_size();
     int a, first, count;
-    if (blockIdx.x / size >= 2 * __ldg(p.units + p.n)) return;                // (the whole cluster)
-    if (!tile_rows(p, blockIdx.x / size, lane, a, first, count)) return;
+    if (!tile_rows(p, blockIdx.x / size, lane, a, first, count)) return;      // (the whole cluster)
     if (tid < kTileRows) {
         const int r = tid < count ? __ldg(p.order + first + tid) : -1;
         rows[tid] = r >= 0 && r < p.T ? r : -1;
@@ -1138,10 +1138,10 @@ template <int R, int LAY> struct WideShape {
 __device__ __forceinline__ uint32_t y_place(int r, int c) { return (uint32_t)(r * 256 + ((c ^ ((r & 1) << 2)) << 4)); }
 
 // y = rn(y0 + back * (u . w2)) over the stages [s0, s1) of 128 columns.  y0 and w2 come by cp.async in whole pieces of rows; a warp takes one column group of a stage and MU of its
-// row tiles, and stores y from its fragments.
-template <typename T, int R, int LAY, bool VEC>
+// row tiles, and stores y from its fragments.  parts_of_s: what fills hi, lo and back, while the first stages are on their way.
+template <typename T, int R, int LAY, bool VEC, typename F>
 __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict__ w2, const int* rows, const uint8_t* hi, const uint8_t* lo, const float* back, uint8_t* stages,
-                                             int count, int s0, int s1)
+                                             int count, int s0, int s1, F parts_of_s)
 {
     using S = WideShape<R, LAY>;
     constexpr int G = Wide<LAY>::cols, GS = S::cols / G, MU = GS * 4 / kWarps, tiles = Wide<LAY>::tiles, steps = R < 16 ? 1 : R / 16;
@@ -1154,16 +1154,6 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
         const int r = rows[fr + 16 * q];
         from[q] = r >= 0 && p.y0 ? (const T*)p.y0 + (int64_t)r * p.ldy0 : nullptr;
     }
-    T* to[MU][2];
-    float factor[MU][2];
-#pragma unroll
-    for (int m = 0; m < MU; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int at = (m0 + m) * 16 + g + 8 * h, r = rows[at];
-            to[m][h] = r >= 0 ? (T*)p.y + (int64_t)r * p.ldy + cw * G + Wide<LAY>::own * t : nullptr;
-            factor[m][h] = back[at];
-        }
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(stages);
     constexpr int WN = 16 * R / kThreads ? 16 * R / kThreads : 1;             // pieces of w2 of a thread
     // piece i of w2.  LAY 0: row n = i / (R / 8) of 2 R bytes, at the row that its fragment has: column c of tile t of a group at 8 t + c.  LAY 1: rank i / 16, columns 8 (i % 16)
@@ -1236,6 +1226,18 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
         fetch(s0 + i, i);
         put(s0 + i, i);
     }
+    parts_of_s();
+    __syncthreads();
+    T* to[MU][2];
+    float factor[MU][2];
+#pragma unroll
+    for (int m = 0; m < MU; ++m)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = (m0 + m) * 16 + g + 8 * h, r = rows[at];
+            to[m][h] = r >= 0 ? (T*)p.y + (int64_t)r * p.ldy + cw * G + Wide<LAY>::own * t : nullptr;
+            factor[m][h] = back[at];
+        }
     int buf = 0;
     for (int st = s0; st < s1; ++st) {
         async_wait<S::stages - 2>();
@@ -1348,7 +1350,6 @@ __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R 
     }
     const int tile = blockIdx.x / spans, span = blockIdx.x - tile * spans;
     int a, first, count;
-    if (tile >= 2 * __ldg(p.units + p.n)) return;
     if (!tile_rows(p, tile, lane, a, first, count)) return;
     if (tid < kTileRows) {
         const int r = tid < count ? __ldg(p.order + first + tid) : -1;
@@ -1356,17 +1357,18 @@ __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R 
     }
     __syncthreads();
     const float sc = !p.s_scaled && p.scale ? __ldg(p.scale + a) : 1.0f;
-    for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
-        const int m = 4 * i / R, j = 4 * i % R, from = rows[m];
-        const float4 v = from >= 0 ? *reinterpret_cast<const float4*>(p.s + (int64_t)from * R + j) : make_float4(0.f, 0.f, 0.f, 0.f);
-        const float f[4] = {v.x * sc, v.y * sc, v.z * sc, v.w * sc};
-        put_u<T, R>(f, hi, lo, back, m, j);
-    }
-    __syncthreads();
+    auto parts_of_s = [&] {
+        for (int i = tid; i < kTileRows * R / 4; i += kThreads) {
+            const int m = 4 * i / R, j = 4 * i % R, from = rows[m];
+            const float4 v = from >= 0 ? *reinterpret_cast<const float4*>(p.s + (int64_t)from * R + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+            const float f[4] = {v.x * sc, v.y * sc, v.z * sc, v.w * sc};
+            put_u<T, R>(f, hi, lo, back, m, j);
+        }
+    };
     const T* w2 = (const T*)p.w2 + (int64_t)a * R * p.N;
     const int last = min((span + 1) * per_span, groups);
     constexpr int per_stage = WideShape<R, LAY>::cols / G;
-    widen_stages<T, R, LAY, VEC>(p, w2, rows, hi, lo, back, stages, count, span * per_span / per_stage, (last + per_stage - 1) / per_stage);
+    widen_stages<T, R, LAY, VEC>(p, w2, rows, hi, lo, back, stages, count, span * per_span / per_stage, (last + per_stage - 1) / per_stage, parts_of_s);
 }
 
 // ------------------------------------------------------------------ weight gradients
