@@ -553,7 +553,8 @@ qmm_status qmm_rows_dequantize(qmm_row_format fmt, const void* codes, int64_t ld
  *                  dA[a] = sum_t dS[t] x[t]^T,  dB[a] = scale[a] * sum_t dY[t] S[t]^T   (sums over the adapter's rows; fp32, in a fixed order)
  * A row without an adapter has Y = Y0 and dX = dX0, its row of S is neither written nor read; an adapter without rows has gradients 0.
  * X may be rows of 8 bits (x_format, x_scale as qmm_rms_norm and qmm_rows_quantize leave them), in the forward pass, in dA, or in both.
- * Accuracy: sums in fp32; S and dS enter the second products as two 16-bit parts (off by 2^-16 of the row's largest element at most).
+ * Accuracy: sums in fp32; S and dS enter the second products as two 16-bit parts (off by 2^-16 of the row's largest element at most)
+ * and the weight gradients as three bf16 or two tf32 parts (off by 2^-22 of themselves).
  *   order, offsets, units  of qmm_expert_sort(idx, T, 1, n), for callers that use one sort for many projections; NULL: the call
  *                          sorts in its workspace (up to 512 rows a forward pass needs none)
  *   Y0 may be Y, dX0 may be dX (in place); NULL counts as zeros.  Otherwise no output may overlap an input.

@@ -5,13 +5,15 @@
 //
 // The forward pass and dx are the same two products, a narrowing one over a row's K elements and a widening one over its N outputs, on weights laid out with either
 // axis contiguous ("LAY" below).  All of them move far more bytes than the tensor cores have work (r = 16: 16 multiply-adds per element read), so what counts is that x and
-// y pass through once, in wide accesses.  They therefore go from global memory straight into the fragments of mma.sync: which k (n) stands at which place of a
+// y pass through once, in wide accesses.  Few rows (lora_small_kernel): they go from global memory straight into the fragments of mma.sync; which k (n) stands at which place of a
 // fragment is free as long as both operands agree, and with the orders below a lane's share of a row is one 16-byte access, without shared memory or
-// transposition.  (tcgen05 would take x through shared memory and y through tensor memory for no gain: the products are 2 to 30 % of the time that the bytes take.)
+// transposition.  Many rows: stages of shared memory, copied asynchronously, so that more bytes are in flight than registers hold (2048 x 4096 x 28672: 85 us from registers,
+// 67 from stages).  The warp-level products' rate (540 TFLOP/s measured) leaves the products 2 to 30 % of the time that the bytes take, except in the weight gradients from r = 32
+// on; tcgen05 would take fp32 sums through tensor memory for a k or an n of 8 to 128, and s would still have to be split into parts by the warps.
 //
-// Sums are fp32.  s enters the widening product and the weight gradients as the sum of two 16-bit numbers (high and low part), so that no bits of it are
-// lost that matter beside fp32 sums; for fp16 the rows of s are scaled by a power of two first, or the product is one of tf32 halves (weight gradients), so that fp16's range
-// does not bound s.
+// Sums are fp32.  s enters the widening product as the sum of two 16-bit numbers (high and low part) and the weight gradients as three bf16 or two tf32 ones, so that no bits of
+// it are lost that matter beside fp32 sums; for fp16 the rows of s are scaled by a power of two first, or the product is one of tf32 halves (weight gradients), so that fp16's
+// range does not bound s.
 #pragma once
 
 #include "qmm_async.cuh"
@@ -662,6 +664,7 @@ template <typename T, bool VEC> __device__ __forceinline__ void copy_row(const L
     }
 }
 
+// Bound by latency: the adapter's rows, x and the weights, the meeting, y.  16 x 8192 x 2048 of 16 adapters 6.6 us on the GPU (5 MB: 0.8 us), 77 x 2048 x 2048 of five at r = 64 10 us.
 // Both products of up to 16 rows of one adapter by a cluster of blocks: each takes a share of K, the shares' sums meet through distributed shared memory, and each takes
 // a share of N.  One launch: for a decode step two, and a sort before them, would cost as much as all their work.
 //   groups 0: cluster b is there for row b; it does something if row b is the first, 17th, ... of its adapter's rows, and then takes 16 of them
@@ -1067,7 +1070,8 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
 }
 
 // The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
-// Bound by HBM (x once); w1 comes from L2.
+// Bound by HBM (x once; w1 comes from L2) and the fill of its stages: 8192 x 8192 bf16 at r = 32, 134 MB in 36 us (3.7 TB/s; 64 us without stages), 8192 x 2048 e4m3 16 us,
+// 2048 x 4096 fp16 at r = 16 11.5 us.
 template <typename T, bool X8, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2) lora_narrow_kernel(const LoraP p)
 {
@@ -1324,6 +1328,8 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
+// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 56 us (4.2 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 60 us (4.5); a copy in tiles of this shape reaches
+// 5.3 to 6.0 TB/s.  The rest is each block's chain of loads to its first rows, and the warps' waits for a stage.
 template <typename T, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
 {
@@ -1391,10 +1397,11 @@ struct WgradP {
 // cluster share the rows.  A warp has all R ranks of 64, 32 or 16 columns (R x columns = 2048 where R >= 32: 64 accumulators a lane), the warps of a column group share the stage's
 // rows.  k of the products is the row: v comes out of shared memory transposed (ldmatrix.trans; codes of 8 bits by words and byte permutes), s is brought into
 // [rank][row] once per stage, split into 16-bit or tf32 parts:
-//   bf16 products of three parts of s (all of its bits: with two, dA is off by 1.5e-6 beside an fp32 sum's 3e-7); fp16 rows: tf32 products of two parts, whose exponent
+//   bf16 products of three parts of s (all of its bits: with two, dA is off by 1.5e-6, with three by 1.6e-7); fp16 rows: tf32 products of two parts, whose exponent
 //   holds any s (a gradient's 1e-7 is below fp16's normal numbers).
 // The parts of a sum are added in a fixed order: warps, then blocks.
-// Bound by HBM where R <= 16; from R = 32 on by the warp-level tensor products of the parts (3 or 4 of them for each of s).
+// Bound by HBM where R <= 16; from R = 32 on by the adapter with the most rows, whose blocks' stages (1.7 us each, half of it warp-level tensor products of the parts, 3 or 4 for
+// each of s) follow one another: 8192 rows x 8192 at r = 32, 84 us with 3250 rows of the largest of four adapters; x 2048, four blocks for each column, 33 us.
 template <typename T, bool X8, int R> struct WgradShape {
     static constexpr bool tf32 = std::is_same<T, __half>::value && !X8;
     static constexpr int cols = 128, rows = 64, stages = R == 64 ? 2 : 3;      // (two blocks per SM up to R = 64)

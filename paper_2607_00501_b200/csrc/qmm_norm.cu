@@ -124,6 +124,8 @@ __device__ __forceinline__ uint32_t code8x2(float a, float b, int int8)
 }
 
 // A row by p.tpr threads, NV vectors of V elements each; blocks of several rows where a row needs fewer than the block's threads.
+// Bound by HBM: 8192 x 8192 bf16 with a residual into h and e4m3 rows, 470 MB in 77 us (6.1 TB/s); 8192 x 4096 into h and y, 268 MB in 48 us (5.6 TB/s).  With few rows bound by
+// the launch and two dependent loads: 4 x 2048 in 2.0 us.
 template <typename T, int V, int NV>
 __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
 {
@@ -284,6 +286,9 @@ __device__ __forceinline__ void block_sum2(float& a, float& b, float (*red)[64])
     }
 }
 
+//   dx = rstd (w dy - xhat mean(w dy xhat)) + dh, xhat = h rstd;   dw = sum over the rows of dy xhat
+// A block takes every gridDim.x-th row and keeps its share of dw in registers; the parts are added by rms_norm_dw_kernel.  Bound by HBM: 8192 x 4096 bf16 with dh, 268 MB in
+// 45 us (6.0 TB/s), straight into registers 77 us.
 // RING > 0: the rows of h, dy and dh come through shared memory, RING rows in flight (cp.async; a thread reads what it copied itself, so the rows need no
 // barrier).  RING 0: straight into registers, for rows that are not 16-byte aligned or too long for that.
 template <typename T, int V, int NV, int RING>
@@ -414,7 +419,8 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
     }
 }
 
-// The blocks' parts of dw in block order: 32 columns by 32 shares of the parts per block (all of a share's loads are in flight at once up to 512 parts).
+// The blocks' parts of dw in a fixed order: 32 columns by 32 shares of the parts per block (all of a share's loads are in flight at once up to 512 parts).  Bound by latency:
+// 592 parts of 4096 columns, 9.7 MB out of L2, 6.6 us; a thread for each column's parts took 16.5.
 constexpr int kColThreads = 1024;
 __global__ void __launch_bounds__(kColThreads) rms_norm_dw_kernel(const float* __restrict__ part, int parts, int K, float* __restrict__ dw)
 {
@@ -440,7 +446,7 @@ __global__ void __launch_bounds__(kColThreads) rms_norm_dw_kernel(const float* _
 
 // ------------------------------------------------------- 8-bit rows back to values
 
-// Thread = V codes of a row.
+// Thread = V codes of a row.  Bound by HBM: 8192 x 8192 into bf16, 201 MB in 35 us (5.7 TB/s; the measured copy rate is 6.6).
 template <typename T, int V>
 __global__ void __launch_bounds__(256) rows8_dequantize_kernel(const uint8_t* __restrict__ codes, int64_t ldc, const float* __restrict__ scales, int int8, int64_t rows, int nv,
                                                                T* __restrict__ out, int64_t ldo)
@@ -486,7 +492,12 @@ __global__ void __launch_bounds__(256) rows8_dequantize_kernel(const uint8_t* __
 static uintptr_t norm_bits(const void* p, int64_t ld, int size) { return p ? reinterpret_cast<uintptr_t>(p) | (uintptr_t)(ld * size) : 0; }
 
 // Threads per row and vectors per thread of a row of nv vectors.  Many rows: four vectors a thread keep more bytes in flight per warp and meet in fewer barriers;
-// few rows (less than a warp per scheduler): one vector a thread, for latency.
+// few rows (less than a warp per scheduler): one vector a thread, for latency.  In us, GPU time of the whole call:
+//                                          one    two   four  eight vectors
+//   4 x 2048 fp16                          2.0    2.1    2.6    5.2
+//   500 x 1001 fp32, with gradients       14.2   12.2    9.7   10.8        (rows that begin anywhere: single elements)
+//   8192 x 8192 bf16 to e4m3 and back      153    133    110    174
+//   8192 x 4096 bf16, with gradients       102     98    101    135
 struct NormShape {
     int tpr, per;
 };
