@@ -23,6 +23,7 @@ qmm_status launch_lora_f16(const lora::LoraP& p, int r, bool x8, bool back, bool
 qmm_status launch_lora_bf16(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st);
 qmm_status launch_lora_wgrad_f16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
 qmm_status launch_lora_wgrad_bf16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
+qmm_status launch_lora_join(int r, const int* units, int n, const lora::WgradParts& g0, const lora::WgradParts& g1, cudaStream_t st);
 size_t expert_sort_workspace_bytes(int64_t P, int E);
 qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int* place, int* offsets, int* units, void* ws, cudaStream_t st);
 
@@ -64,7 +65,7 @@ static qmm_status check_rows8(const char* who, int fmt, const void* codes, int64
 
 // Workspace of the adapters: a plan of the rows by adapter, where the caller brings none, and s or ds.
 struct LoraLayout {
-    size_t order, place, offsets, units, sort, s, total;
+    size_t order, place, offsets, units, sort, s, part, total;
 };
 static LoraLayout lora_layout(int64_t T, int n, int r)
 {
@@ -76,7 +77,8 @@ static LoraLayout lora_layout(int64_t T, int n, int r)
     l.units = up(l.offsets + (size_t)(n + 1) * 4);
     l.sort = up(l.units + (size_t)(n + 1) * 4);
     l.s = up(l.sort + expert_sort_workspace_bytes(T, n));
-    l.total = up(l.s + (size_t)T * r * 4);
+    l.part = up(l.s + (size_t)T * r * 4);
+    l.total = l.part + (T > lora::kSmallRows ? (size_t)lora::wgrad_blocks(r) * 2 * 128 * r * 4 : 0);         // sums of adapters that two blocks of a weight gradient share
     return l;
 }
 
@@ -305,20 +307,28 @@ qmm_status qmm_lora_grad(const qmm_lora_args* a, void* ws, size_t ws_bytes, void
                                a->dX, a->lddx, ds, 1, a->dX && !same, b.words()};
         QMM_TRY(half ? launch_lora_f16(p, a->r, false, true, vx, b.vy(), st) : launch_lora_bf16(p, a->r, false, true, vx, b.vy(), st));
     }
+    const int blocks = lora::wgrad_blocks(a->r);
+    const int of_b = a->dB ? lora::wgrad_share(blocks, a->T, a->N, half, a->dA ? a->K : 0, half && !a->x_scale) : 0;
+    const int of_a = a->dA ? lora::wgrad_share(blocks - of_b, a->T, a->K, half && !a->x_scale, 0, false) : 0;
+    float* const part_b = small ? nullptr : (float*)((char*)ws + l.part);
+    float* const part_a = small ? nullptr : part_b + (size_t)of_b * 2 * 128 * a->r;
     if (a->dB) {
         const uintptr_t bits = pitch_bits(a->dY, a->lddy, 2);
-        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, a->T, a->n, (int)a->N, a->dB, bits % 4 == 0, 0};
+        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, units, a->T, a->n, (int)a->N, a->dB, part_b, of_b, bits % 4 == 0, 0};
         const bool vec = (bits | (uintptr_t)(a->N * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, false, true, vec, st) : launch_lora_wgrad_bf16(p, a->r, false, true, vec, st));
     }
     if (a->dA) {
         const bool x8 = a->x_scale != nullptr;
         const uintptr_t bits = pitch_bits(a->X, a->ldx, x8 ? 1 : 2);
-        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, a->T, a->n, (int)a->K, a->dA, bits % 4 == 0, a->dB != nullptr};
+        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, units, a->T, a->n, (int)a->K, a->dA, part_a, of_a, bits % 4 == 0,
+                                 a->dB != nullptr};
         const bool vec = (bits | (uintptr_t)(a->K * 2)) % 16 == 0;
         QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, x8, false, vec, st) : launch_lora_wgrad_bf16(p, a->r, x8, false, vec, st));
     }
-    return QMM_OK;
+    if (small || !(a->dA || a->dB)) return QMM_OK;
+    const lora::WgradParts gb = {part_b, a->dB, (int)a->N, of_b, 1}, ga = {part_a, a->dA, (int)a->K, of_a, 0};
+    return launch_lora_join(a->r, units, a->n, of_b ? gb : ga, of_b ? ga : gb, st);
 }
 
 }  // extern "C"

@@ -243,6 +243,42 @@ def test_integers_are_exact(qmm, dt, T, K, N, n, r):
         assert torch.equal(da[e].double(), (ds * c)[t].T @ p.x64[t]) and torch.equal(db[e].double(), p.scale[e].double() * (p.dy.double()[t].T @ s[t])), e
 
 
+@pytest.mark.parametrize("dt", list(HALVES))
+@pytest.mark.parametrize("x8", [False, True])
+@pytest.mark.parametrize("T,K,N,n,r,kind", [(513, 64, 8, 1, 8, "one"), (4097, 136, 264, 5, 16, "skewed"), (2000, 72, 200, 1024, 8, "uniform"), (700, 130, 77, 1024, 16, "one"),
+                                            (3000, 256, 128, 3, 32, "none"), (20000, 2056, 136, 3, 32, "skewed"), (1500, 300, 133, 4, 128, "dropped"), (900, 101, 520, 6, 64, "uniform"),
+                                            (6000, 128, 1300, 40, 64, "skewed")])
+def test_rows_shared_by_blocks(qmm, dt, x8, T, K, N, n, r, kind):
+    """Many rows: the blocks of a weight gradient share all adapters' rows.  Integers, so that every sum is exact whoever adds what; a workspace of exactly the size asked for,
+    full of NaN, with other memory behind it."""
+    p = Problem(qmm, dt, T, K, N, n, r, kind)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+
+    def ints(shape, lo, hi, dtype):
+        return torch.randint(lo, hi + 1, shape, generator=gen, device="cuda").to(dtype)
+    ds_of = ints((T, r), -9, 9, torch.float32)
+    x = ints((T, K), -2, 2, torch.int8 if x8 else p.dtype)
+    xs = torch.tensor([0.5, 1.0, 2.0], device="cuda")[torch.arange(T, device="cuda") % 3] if x8 else None
+    dy, b = ints((T, N), -2, 2, p.dtype), torch.zeros_like(p.b)
+    b[:, : min(N, r)] = torch.eye(r, device="cuda", dtype=p.dtype)[: min(N, r)]             # ds = scale * the first elements of dy
+    scale = torch.tensor([0.5, 2.0, 1.0], device="cuda")[torch.arange(n, device="cuda") % 3]
+    need = qmm.lora_workspace_bytes(T, n, r)
+    buf = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    args = dict(scale=scale, x_scale=xs, ws=buf[:need])
+    _, da, db = qmm.lora_grad(dy, x, ds_of, p.idx, p.a, b, dx=False, **args)
+    one_a = qmm.lora_grad(dy, x, None, p.idx, p.a, b, dx=False, db=False, **args)[1]
+    one_b = qmm.lora_grad(dy, None, ds_of, p.idx, p.a, b, dx=False, da=False, scale=scale, ws=buf[:need])[2]
+    assert bool((buf[need:] == 255).all())
+    ds = torch.zeros(T, r, device="cuda", dtype=torch.float64)
+    ds[:, : min(N, r)] = dy[:, : min(N, r)].double()
+    xd = x.double() * (xs.double()[:, None] if x8 else 1.0)
+    for e in range(n):
+        t = torch.nonzero(p.idx == e)[:, 0]
+        want_a, want_b = scale[e].double() * ds[t].T @ xd[t], scale[e].double() * dy[t].double().T @ ds_of[t].double()
+        for got, want in ((da[e], want_a), (one_a[e], want_a), (db[e], want_b), (one_b[e], want_b)):
+            assert torch.equal(got.double(), want), "adapter %d of %d" % (e, n)
+
+
 @pytest.mark.parametrize("dt,std", [("f16", 2.0**-20), ("f16", 3e4), ("bf16", 1e-30), ("bf16", 1e30)])
 @pytest.mark.parametrize("T", [20, 300])
 def test_rows_far_from_one(qmm, dt, std, T):
