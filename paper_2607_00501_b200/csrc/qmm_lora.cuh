@@ -901,10 +901,12 @@ template <bool X8, int R> struct NarrowShape {
     static constexpr int RG = kTileRows / 16 / MW, KP = kWarps / RG;          // row groups x shares of K
     static constexpr int K = 128, chunks = K / 32 / KP;    // elements of a stage; 32-element chunks of a warp
     static constexpr int xbytes = kTileRows * K * (X8 ? 1 : 2), wbytes = K * R * 2, stage = xbytes + wbytes;
-    static constexpr int stages = R <= 64 ? 3 : 2;
+    static constexpr int stages = R == 32 ? 4 : R <= 64 ? 3 : 2;              // (r = 32: three 221.5 us instead of 219.7 for the call below)
     static constexpr int sums = KP * kTileRows * R * 4;
     static constexpr int smem = stages * stage > sums ? stages * stage : sums;
-    static constexpr int blocks = R <= 32 ? 3 : 2;         // per SM, as shared memory allows
+    // Per SM, as shared memory allows; r = 32 needs the registers more (8192 x 2048 x 8192 with gradients: 220 us with two, 235 with three), r = 16 the blocks (2048 x 4096 x 28672: 71
+    // and 67).
+    static constexpr int blocks = R <= 16 ? 3 : 2;
 };
 
 // Places of 16-byte pieces in a stage: conflict-free both for eight rows' pieces at one k (ldmatrix) and for two rows' four neighbouring ones.
@@ -1082,7 +1084,7 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
 }
 
 // The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
-// Bound by HBM (x once; w1 comes from L2) and the fill of its stages: 8192 x 8192 bf16 at r = 32, 134 MB in 36 us (3.7 TB/s; 64 us without stages), 8192 x 2048 e4m3 16 us,
+// Bound by HBM (x once; w1 comes from L2) and the fill of its stages: 8192 x 8192 bf16 at r = 32, 134 MB in 32 us (4.2 TB/s; 64 us without stages), 8192 x 2048 e4m3 14.4 us,
 // 2048 x 4096 fp16 at r = 16 11.5 us.
 template <typename T, bool X8, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2) lora_narrow_kernel(const LoraP p)
@@ -1147,8 +1149,9 @@ __global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2
 template <int R, int LAY> struct WideShape {
     static constexpr int cols = 128;
     static constexpr int ybytes = kTileRows * cols * 2, wbytes = cols * R * 2, stage = ybytes + wbytes;
-    static constexpr int stages = R <= 16 ? 3 : 2;
-    static constexpr int blocks = R <= 32 ? 3 : R <= 64 ? 2 : 1;              // per SM
+    static constexpr int stages = R <= 32 ? 3 : 2;
+    // Per SM: the products need the registers more than another block (three: 2048 x 4096 x 28672 at r = 16 67 us instead of 58, 8192 x 2048 x 8192 at r = 32 219 instead of 214).
+    static constexpr int blocks = R <= 64 ? 2 : 1;
 };
 // 16-byte piece c of row r of y0 lies at place c ^ 4 (r % 2), so that two rows' shares of a column group do not meet in a bank.
 __device__ __forceinline__ uint32_t y_place(int r, int c) { return (uint32_t)(r * 256 + ((c ^ ((r & 1) << 2)) << 4)); }
@@ -1340,7 +1343,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
-// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 56 us (4.2 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 60 us (4.5); a copy in tiles of this shape reaches
+// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 54 us (5.0); a copy in tiles of this shape reaches
 // 5.3 to 6.0 TB/s.  The rest is each block's chain of loads to its first rows, and the warps' waits for a stage.
 template <typename T, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
@@ -1940,8 +1943,9 @@ template <typename T, int LAY> static qmm_status launch_pair(const LoraP& p, int
         const qmm_status s = v1 ? first(std::true_type()) : first(std::false_type());
         if (s != QMM_OK || small || !p.y) return s;
         const int groups = (p.N + G - 1) / G;
-        // column groups of a block: 1024 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns)
-        int per_span = 1024 / G;
+        // column groups of a block: 2048 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns).  2048 x 4096 x 28672: 512 columns 68.6 us,
+        // 1024 58.5, 2048 58.0; 8192 x 2048 x 8192 with gradients 226.7, 213.9 and 211.6.
+        int per_span = 2048 / G;
         while (per_span > 256 / G && (int64_t)((p.T + kTileRows - 1) / kTileRows) * ((groups + per_span - 1) / per_span) < 2 * kNumSMs) per_span /= 2;
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
