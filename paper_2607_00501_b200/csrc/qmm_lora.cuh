@@ -8,7 +8,7 @@
 // y pass through once, in wide accesses.  Few rows (lora_small_kernel): they go from global memory straight into the fragments of mma.sync; which k (n) stands at which place of a
 // fragment is free as long as both operands agree, and with the orders below a lane's share of a row is one 16-byte access, without shared memory or
 // transposition.  Many rows: stages of shared memory, copied asynchronously, so that more bytes are in flight than registers hold (2048 x 4096 x 28672: 85 us from registers,
-// 67 from stages).  The warp-level products' rate (540 TFLOP/s measured) leaves the products 2 to 30 % of the time that the bytes take, except in the weight gradients from r = 32
+// 58 from stages).  The warp-level products' rate (540 TFLOP/s measured) leaves the products 2 to 30 % of the time that the bytes take, except in the weight gradients from r = 32
 // on; tcgen05 would take fp32 sums through tensor memory for a k or an n of 8 to 128, and s would still have to be split into parts by the warps.
 //
 // Sums are fp32.  s enters the widening product as the sum of two 16-bit numbers (high and low part) and the weight gradients as three bf16 or two tf32 ones, so that no bits of
@@ -1343,7 +1343,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
-// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 54 us (5.0); a copy in tiles of this shape reaches
+// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 55 us (4.9); a copy in tiles of this shape reaches
 // 5.3 to 6.0 TB/s.  The rest is each block's chain of loads to its first rows, and the warps' waits for a stage.
 template <typename T, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
@@ -1422,7 +1422,7 @@ struct WgradP {
 //   holds any s (a gradient's 1e-7 is below fp16's normal numbers).
 // The parts of a sum are added in a fixed order: warps, then blocks.
 // Bound by HBM where R <= 16; from R = 32 on by the warps' chains of barriers, splits and warp-level tensor products of the parts (3 or 4 for each of s), two blocks per SM:
-// 8192 rows, 8192 columns of bf16 and 2048 of e4m3 at r = 32: 90 us together (153 MB: 23 us; the products alone 32 us).
+// 8192 rows, 8192 columns of bf16 and 2048 of e4m3 at r = 32: 83 us together (153 MB: 23 us; the products alone 32 us).
 template <typename T, bool X8, int R> struct WgradShape {
     static constexpr bool tf32 = std::is_same<T, __half>::value && !X8;
     static constexpr int cols = 128, rows = 64, stages = R == 64 ? 2 : 3;      // (two blocks per SM up to R = 64)
