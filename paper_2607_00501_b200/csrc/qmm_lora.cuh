@@ -1343,7 +1343,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
-// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s), 8192 x 8192 bf16 at r = 32, 268 MB in 55 us (4.9); a copy in tiles of this shape reaches
+// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s) on rows used before, 57 on others, 8192 x 8192 bf16 at r = 32, 268 MB in 55 us (4.9); a copy in tiles of this shape reaches
 // 5.3 to 6.0 TB/s.  The rest is each block's chain of loads to its first rows, and the warps' waits for a stage.
 template <typename T, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)
@@ -1943,9 +1943,9 @@ template <typename T, int LAY> static qmm_status launch_pair(const LoraP& p, int
         const qmm_status s = v1 ? first(std::true_type()) : first(std::false_type());
         if (s != QMM_OK || small || !p.y) return s;
         const int groups = (p.N + G - 1) / G;
-        // column groups of a block: 2048 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns).  2048 x 4096 x 28672: 512 columns 68.6 us,
-        // 1024 58.5, 2048 58.0; 8192 x 2048 x 8192 with gradients 226.7, 213.9 and 211.6.
-        int per_span = 2048 / G;
+        // column groups of a block: 1024 columns, fewer where that leaves less than two blocks per SM (always whole stages of 128 columns).  2048 x 4096 x 28672, replayed on the same
+        // rows: 512 columns 68.6 us, 1024 58.5, 2048 58.0; on other rows from call to call 1024 68, 2048 78 (the last round is longer).
+        int per_span = 1024 / G;
         while (per_span > 256 / G && (int64_t)((p.T + kTileRows - 1) / kTileRows) * ((groups + per_span - 1) / per_span) < 2 * kNumSMs) per_span /= 2;
         const int spans = (groups + per_span - 1) / per_span;
         const int64_t blocks = most_tiles(p.T, p.n) * spans, rest = p.rest ? (int64_t)((p.T + kTileRows - 1) / kTileRows) * spans : 0;
