@@ -229,7 +229,7 @@ template <typename T> __device__ __forceinline__ double value64(const T* __restr
     return l > -INFINITY && c == c ? c : -INFINITY;
 }
 
-// The three places below take over where fp32 leaves something open, about one token in a thousand.  Their code is cold: what it takes is mostly its way into the instruction
+// The four places below take over where fp32 leaves something open, about one token in a thousand.  Their code is cold: what it takes is mostly its way into the instruction
 // cache, so loops stay rolled.
 
 // Open groups in 64 bits: sc holds the scores of 32 bits (shared memory).  false: a group's second and third are too near to one another as well.
@@ -270,6 +270,23 @@ template <typename T> __device__ __noinline__ bool open_groups_exactly(const T* 
 #pragma unroll 1
     for (int k = 0; k < p.groups; ++k) open |= (stay >> k & 1u) << (k << p.share);
     return true;
+}
+
+// Whether an expert behind the last one chosen (`last`: its key's upper bits, and in the bits `low` what the expert leaves of them) may be better than it.  Of one key's upper
+// bits any expert may be the best, so all that follow are looked at; those of the same logit and bias are in order.  m, per_z: of a softmax.
+template <typename T> __device__ __noinline__ bool overtaken(const T* __restrict__ row, unsigned last, unsigned low, float m, float per_z, const RouteP& p, int lane, float tie)
+{
+    auto score = [&](float l) { return p.sigmoid ? sigmoid_score(l) : expf(l - m) * per_z; };
+    const int at = (int)(low - (last & low));
+    const float v = route_logit(Dt<T>::up(row[at])), b = __ldg(p.bias + at), c = score(v) + b;
+    bool any = false;
+#pragma unroll 1
+    for (int e = lane; e < p.E; e += 32) {
+        const float l = route_logit(Dt<T>::up(row[e])), o = __ldg(p.bias + e), x = score(l) + o;
+        const unsigned k = l > -INFINITY && x > -INFINITY ? (route_key(x) & ~low) | (low - (unsigned)e) : 0u;
+        any |= k != 0u && k < last && !(c - x > tie) && !(l == v && o == b);
+    }
+    return __any_sync(0xFFFFFFFFu, any);
 }
 
 // The topk best of the candidates that the lanes hold (mine: the key's upper bits, and in the bits `low` what the expert leaves of them; 0: none), compared in 64 bits.  rest: the largest key that no lane holds.
@@ -434,16 +451,20 @@ __device__ __forceinline__ void route_one(const T* __restrict__ row, int64_t t, 
         if (sel >= 0) v = route_logit(Dt<T>::up(row[sel]));
         // Neighbours that agree in these bits (for 16-bit logits without a bias: are equal, and in order), or whose scores of 32 bits are nearer than these are exact, are
         // compared as logits, or in 64 bits, with eight that follow.  Equal logits and biases give equal scores there too.
-        bool near = false;
+        bool near = false, border = false;                 // border: the last one chosen is within reach of what follow's upper bits allow, whatever follow itself is
         if (next >= 0) {
             near = !(sizeof(T) == 2 && !p.bias) && (mine & ~low) == (follow & ~low);
             if (p.bias) {
                 const float l2 = route_logit(Dt<T>::up(row[next])), b1 = __ldg(p.bias + sel), b2 = __ldg(p.bias + next);
                 const float s1 = p.sigmoid ? sigmoid_score(v) : expf(v - m) * per_z, s2 = p.sigmoid ? sigmoid_score(l2) : expf(l2 - m) * per_z;
                 near = (near || !((s1 + b1) - (s2 + b2) > tie)) && !(v == l2 && b1 == b2);
+                border = lane == p.topk - 1 && !((s1 + b1) - route_unkey(follow | low) > tie);
             }
         }
-        if (__any_sync(0xFFFFFFFFu, near)) {
+        bool look = __any_sync(0xFFFFFFFFu, near || border);
+        if (look && p.bias && !__any_sync(0xFFFFFFFFu, near))
+            look = overtaken<T>(row, __shfl_sync(0xFFFFFFFFu, mine, p.topk - 1), low, m, per_z, p, lane, tie);
+        if (look) {
             unsigned rest;
             if (!p.bias) {                                 // the logits themselves decide: neighbours change places until they are in order
                 int e = mine ? (int)(low - (mine & low)) : 0x7FFFFFFF;

@@ -193,3 +193,55 @@ def test_route_into_the_experts(qmm):
     # the weights of a token add up to 2 whatever its logits, so the exact gradient of the logits is zero up to dy . x summed in 32 bits
     assert (dx.double() - gx).norm() / gx.norm() < 1e-5
     assert (dl.double() - gl).abs().max() < 64 * 2.0**-23 * (dy.abs() * x.abs()).sum(1).max() * 2
+
+
+def bucketed(E, sigmoid, T, topk, targets, seed):
+    """Logits and biases that bring the scores of `targets` (expert -> value) there, to within the roundings of the logits, topk - 1 others above and the rest far below."""
+    gen = torch.Generator().manual_seed(seed)
+    l = torch.randn(1, E, generator=gen)
+    want = 0.2 + 0.2 * torch.rand(E, generator=gen, dtype=torch.float64)
+    want[E - topk + 1:] = 0.8 + 0.01 * torch.arange(topk - 1)
+    for e, v in targets.items():
+        want[e] = v
+    bias = (want - ref.scores(l.double(), sigmoid)[0]).float()
+    noise = torch.zeros(T, E)
+    noise[:, list(targets)] = torch.randn(T, len(targets), generator=gen) * (1e-7 if sigmoid else 2e-8 * E)
+    return l + noise, bias
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,G", [(64, 1), (256, 1), (256, 8), (1024, 1)])
+@pytest.mark.parametrize("topk", [1, 5])
+def test_a_better_expert_behind_the_first_not_chosen(qmm, sigmoid, E, G, topk):
+    """The comparison's keys hold a score's upper bits alone.  Of one key's experts the lower index comes first: expert 20 stands before expert 40, whose score is the larger one and
+    within 1e-8 of expert 50's, across the border of two keys at 0.75."""
+    width = 2.0**-24 * 32 * max(1, E // 32)
+    l, bias = bucketed(E, sigmoid, 300 if E == 1024 else 1500, topk, {50: 0.75 + 1e-8, 20: 0.75 - 0.6 * width, 40: 0.75 - 1e-8}, E + topk)
+    check(qmm, l, topk, sigmoid, bias, G, min(G, 6), 2 if G > 1 else 1, True)
+    check(qmm, l.flip(1).contiguous(), topk, sigmoid, bias.flip(0).contiguous(), G, G, 1, False)
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E", [64, 256, 1024])
+@pytest.mark.parametrize("topk", [1, 2, 5])
+def test_equal_experts_before_a_better_one_of_the_same_key(qmm, sigmoid, E, topk):
+    """Experts 20 and 30 are equal to the last bit; expert 40 is better by a third of a key's width."""
+    width = 2.0**-24 * 32 * max(1, E // 32)
+    l, bias = bucketed(E, sigmoid, 50, topk, {40: 0.75 + 0.6 * width, 20: 0.75 + 0.3 * width}, E + topk)
+    l[:, 30], bias[30] = l[:, 20], bias[20]
+    if not sigmoid:                                        # (expert 30's share of the denominator is no longer what the biases were made for: the scores of the three move alike)
+        s = ref.scores(l[:1].double(), False)[0]
+        bias[40] = (0.75 + 0.6 * width - s[40]).float()
+        bias[[20, 30]] = (0.75 + 0.3 * width - s[20]).float()
+    idx = check(qmm, l, topk, sigmoid, bias, 1, 1, 1, True)[1].cpu()
+    assert (idx[:, topk - 1] == 40).all()
+
+
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,topk,G", [(64, 6, 1), (256, 8, 8), (1024, 32, 1)])
+def test_all_experts_equal_but_few(qmm, sigmoid, E, topk, G):
+    l, bias = torch.zeros(40, E), torch.full((E,), 0.125)
+    assert (check(qmm, l, topk, sigmoid, bias, G, G, 1, True)[1].cpu() == torch.arange(topk)).all()
+    l[20:, E - 3] = 1e-6                                   # one score is better by a few roundings, one by none
+    l[30:, E - 2] = 1e-9
+    check(qmm, l, topk, sigmoid, bias, G, G, 1, True)
