@@ -92,14 +92,18 @@ __device__ __forceinline__ void row_reduce(float& a, float& b, int threads, int 
     asm volatile("bar.sync %0, %1;" ::"r"(barrier), "r"(threads) : "memory");      // red may be written again
 }
 
-// 1 / sqrt(mean + eps) of a sum of squares; 64 bits where the squares were scaled by f^2 = 2^-128 or 2^128 to stay in fp32's range.
+// 1 / sqrt(mean + eps) of a sum of squares.
 __device__ __forceinline__ float rstd_of(float ss, int K, float eps) { return 1.0f / sqrtf(ss / (float)K + eps); }
-__device__ __forceinline__ float rstd_scaled(float ss, int K, float eps, bool small)
-{
-    return (float)(1.0 / sqrt((double)ss / K * (small ? 0x1p-128 : 0x1p128) + (double)eps));
-}
-// Sums of squares outside this range have lost values to fp32's ends and are formed again with scaled elements.
+// Sums of squares outside this range have lost values to fp32's ends and are formed again with scaled elements: by 2^64 in small rows, by 2^-80 in large ones, so that the sum
+// of 32768 squares of the type's largest number is 2^111.
 __device__ __forceinline__ bool off_range(float ss) { return !(ss < FLT_MAX) || ss < 0x1p-90f; }
+__device__ __forceinline__ float square_scale(bool small) { return small ? 0x1p64f : 0x1p-80f; }
+// Their rstd is up * the returned number: that of a large row alone would be below fp32's normal numbers.
+__device__ __forceinline__ float rstd_scaled(float ss, int K, float eps, bool small, float& up)
+{
+    up = small ? 1.0f : 0x1p-64f;
+    return (float)((small ? 1.0 : 0x1p64) / sqrt((double)ss / K * (small ? 0x1p-128 : 0x1p160) + (double)eps));
+}
 
 struct NormP {
     int64_t rows, ldx, ldr, ldh, ldy, ldc;
@@ -191,12 +195,12 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
             if (p.codes) amax = maxabs(amax, f * w[i].get(k));
         }
     row_reduce(ss, amax, tpr, 1 + group, tid, red + 2 * (group * (tpr >> 5)));
-    float rstd = 1.0f;
+    float rstd = 1.0f, up = 1.0f;                          // (the row's rstd is up * rstd; up is 1 but for the largest rows)
     if (p.norm) {
         rstd = rstd_of(ss, p.K, p.eps);
         if (off_range(ss)) {                               // (the same on every thread of the row)
             const bool small = ss < 1.0f;
-            const float f = small ? 0x1p64f : 0x1p-64f;
+            const float f = square_scale(small);
             float again = 0.0f, none = 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
@@ -206,7 +210,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
                     again = fmaf(e, e, again);
                 }
             row_reduce(again, none, tpr, 1 + group, tid, red + 2 * (group * (tpr >> 5)));
-            rstd = rstd_scaled(again, p.K, p.eps, small);
+            rstd = rstd_scaled(again, p.K, p.eps, small, up);
         }
     }
     if (p.y) {
@@ -215,7 +219,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
             const int v = tid + i * tpr;
             float f[V];
 #pragma unroll
-            for (int k = 0; k < V; ++k) f[k] = h[i].get(k) * rstd * w[i].get(k);
+            for (int k = 0; k < V; ++k) f[k] = h[i].get(k) * up * rstd * w[i].get(k);
             Piece<T, V> o;
             o.set(f);
             if (v < p.nv) o.store((T*)p.y + row * p.ldy + v * V);
@@ -225,7 +229,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(const NormP p)
         const float top = p.int8 ? 127.0f : 448.0f;
         const bool fine = amax < INFINITY, zero = amax < 0x1p-118f;         // (a NaN is neither)
         const float inv = fine && !zero ? top / amax : 0.0f;
-        if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7FC00000) : zero ? 0.0f : amax / top * rstd;
+        if (tid == 0) p.scales[row] = !fine ? __int_as_float(0x7FC00000) : zero ? 0.0f : amax / top * up * rstd;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int v = tid + i * tpr;
@@ -362,44 +366,59 @@ __global__ void __launch_bounds__(NV <= 4 ? 512 : 1024) rms_norm_grad_kernel(con
                 dot = fmaf(w[i].get(k) * dy[i].get(k), f, dot);
             }
         block_sum2(ss, dot, red);
-        float rstd = rstd_of(ss, p.K, p.eps), c = rstd * (rstd * dot / (float)p.K);        // rstd * mean(w dy xhat)
+        float rstd = rstd_of(ss, p.K, p.eps), c = rstd * (rstd * dot / (float)p.K), up = 1.0f;         // rstd * mean(w dy xhat); rstd and c are times up
         if (off_range(ss)) {                               // (the same on every thread)
             const bool small = ss < 1.0f;
-            const float f = small ? 0x1p64f : 0x1p-64f;
-            float again = 0.0f, dot2 = 0.0f;
+            const float f = square_scale(small);
+            float again = 0.0f, none = 0.0f, mean = 0.0f;
 #pragma unroll
             for (int i = 0; i < NV; ++i)
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
                     const float e = h[i].get(k) * f;
                     again = fmaf(e, e, again);
-                    dot2 = fmaf(w[i].get(k) * dy[i].get(k), e, dot2);
                 }
-            block_sum2(again, dot2, red);
-            rstd = rstd_scaled(again, p.K, p.eps, small);
-            c = rstd * (rstd / f * dot2 / (float)p.K);
-        }
+            block_sum2(again, none, red);
+            rstd = rstd_scaled(again, p.K, p.eps, small, up);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int v = tid + i * tpr;
-            Piece<T, V> dh;
-            dh.fill(0u);
-            if constexpr (RING > 0) {
-                if (p.dh) dh.load(reinterpret_cast<const T*>(ring + place(slot, 2, i)));
-            } else {
-                if (p.dh && v < p.nv) dh.load((const T*)p.dh + row * p.lddh + v * V);
-            }
-            float f[V];
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
-            for (int k = 0; k < V; ++k) {
-                const float xhat = h[i].get(k) * rstd;
-                f[k] = fmaf(rstd, w[i].get(k) * dy[i].get(k), fmaf(-c, xhat, dh.get(k)));
-                dw[i][k] = fmaf(dy[i].get(k), xhat, dw[i][k]);
-            }
-            Piece<T, V> o;
-            o.set(f);
-            if (p.dx && v < p.nv) o.store((T*)p.dx + row * p.lddx + v * V);
+                for (int k = 0; k < V; ++k) mean = fmaf(w[i].get(k) * dy[i].get(k), h[i].get(k) * up * rstd, mean);
+            block_sum2(mean, none, red);
+            c = rstd * (mean / (float)p.K);
         }
+        auto put = [&](auto largest) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int v = tid + i * tpr;
+                Piece<T, V> dh;
+                dh.fill(0u);
+                if constexpr (RING > 0) {
+                    if (p.dh) dh.load(reinterpret_cast<const T*>(ring + place(slot, 2, i)));
+                } else {
+                    if (p.dh && v < p.nv) dh.load((const T*)p.dh + row * p.lddh + v * V);
+                }
+                float f[V];
+#pragma unroll
+                for (int k = 0; k < V; ++k) {
+                    const float g = w[i].get(k) * dy[i].get(k);
+                    float xhat;
+                    if constexpr (decltype(largest)::value) {
+                        xhat = h[i].get(k) * up * rstd;
+                        f[k] = fmaf(up, fmaf(rstd, g, -c * xhat), dh.get(k));
+                    } else {
+                        xhat = h[i].get(k) * rstd;
+                        f[k] = fmaf(rstd, g, fmaf(-c, xhat, dh.get(k)));
+                    }
+                    dw[i][k] = fmaf(dy[i].get(k), xhat, dw[i][k]);
+                }
+                Piece<T, V> o;
+                o.set(f);
+                if (p.dx && v < p.nv) o.store((T*)p.dx + row * p.lddx + v * V);
+            }
+        };
+        if (up == 1.0f) put(std::false_type());
+        else put(std::true_type());
         if (RING > 0) slot = slot == RING - 1 ? 0 : slot + 1;
     }
     if (RING > 0) async_wait<0>();

@@ -231,3 +231,39 @@ def test_codes_at_halves_and_ends(qmm, kind):
     assert torch.equal(bits(codes), bits(want)) and torch.equal(scales.double(), want_s.float().double())
     zero = x.abs().amax(1) < 2.0**-118
     assert zero[4] and not bits(codes)[zero].any() and not scales[zero].any()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("K", [1, 300, 4096, 8191, 32768])
+@pytest.mark.parametrize("residual", [False, True])
+def test_largest_rows(qmm, dt, K, residual):
+    """Rows up to the end of the type's range: y, the 8-bit rows' scale and the gradients are numbers of ordinary size, or as small as rstd makes them."""
+    dtype, gen = ref.DTYPES[dt], gen_of(K)
+    x = rows(7, K, dtype, gen, 5e37)
+    top = torch.finfo(dtype).max
+    x[0] = top
+    x[1] = -top
+    x[2, : K // 2] = 0
+    x[3] = rows(1, K, dtype, gen, 5e36)[0]
+    x[4] = rows(1, K, dtype, gen, 1e20)[0]
+    x[5] = rows(1, K, dtype, gen, 1.0)[0]
+    r = None
+    if residual:
+        r = (x.double() * -0.25).to(dtype)
+    w = (0.2 + 0.5 * torch.rand(K, generator=gen, device="cuda")).to(dtype)
+    eps = float(torch.tensor(1e-6))
+    y, h = qmm.rms_norm(x, w, eps, residual=r)
+    assert torch.equal(h, ref.add(x, r))
+    check_y(y, h, w, eps)
+    assert bool((y.double().square().mean(1) > 0.03).all())
+    for kind in ref.ROW8.values():
+        codes, scales, h8 = qmm.rms_norm_rows(x, w, eps, residual=r, dtype=kind)
+        want, scale = ref.rows8(h8.float() * w.float(), kind, ref.norm(h, w, eps)[0])
+        assert torch.equal(codes.view(torch.uint8), want.view(torch.uint8))
+        assert bool(((scales.double() - scale).abs() <= (STAT + 2.0**-22) * scale + 2.0**-149).all())
+    for size in (1.0, 1e18, 1e30):                         # (larger dy: dx itself comes back to ordinary size)
+        dy = rows(7, K, dtype, gen, size)
+        dh = rows(7, K, dtype, gen, size * 1e-38) if residual else None
+        dx, dw = qmm.rms_norm_grad(dy, h, w, eps, dh=dh)
+        assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
+        check_grad(dx, dw, dy, h, w, eps, dh)
