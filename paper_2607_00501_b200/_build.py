@@ -16,7 +16,7 @@ EXT = os.path.join(HERE, "_qmm_py" + sysconfig.get_config_var("EXT_SUFFIX"))    
 LAYER_EXT = os.path.join(HERE, "_qmm_layer_py" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ("qmm_api.cu", "qmm_pack.cu", "qmm_gemv.cu", "qmm_gemm.cu", "qmm_gemm_small.cu", "qmm_moe.cu", "qmm_chain.cu",
            "qmm_mx_api.cu", "qmm_mx_quant.cu", "qmm_mx_gemm.cu", "qmm_expert.cu", "qmm_layer_api.cu", "qmm_router.cu", "qmm_norm.cu", "qmm_lora_f16.cu",
-           "qmm_lora_bf16.cu", "qmm_lora_grad_f16.cu", "qmm_lora_grad_bf16.cu")
+           "qmm_lora_bf16.cu", "qmm_lora_grad_f16.cu", "qmm_lora_grad_f16_rows8.cu", "qmm_lora_grad_bf16.cu", "qmm_lora_grad_bf16_rows8.cu")
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-lineinfo",
               "-Xcompiler", "-fPIC", "-DQMM_BUILD"]
 

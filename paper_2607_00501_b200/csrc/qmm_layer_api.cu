@@ -21,8 +21,10 @@ qmm_status launch_rows8_dequantize(int row8, const void* codes, int64_t ldc, con
 
 qmm_status launch_lora_f16(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st);
 qmm_status launch_lora_bf16(const lora::LoraP& p, int r, bool x8, bool back, bool vx, bool vy, cudaStream_t st);
-qmm_status launch_lora_wgrad_f16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
-qmm_status launch_lora_wgrad_bf16(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st);
+qmm_status launch_lora_wgrad_f16(const lora::WgradP& b, const lora::WgradP& a, int r, bool vb, bool va, cudaStream_t st);
+qmm_status launch_lora_wgrad_f16_rows8(const lora::WgradP& b, const lora::WgradP& a, int r, bool vb, bool va, cudaStream_t st);
+qmm_status launch_lora_wgrad_bf16(const lora::WgradP& b, const lora::WgradP& a, int r, bool vb, bool va, cudaStream_t st);
+qmm_status launch_lora_wgrad_bf16_rows8(const lora::WgradP& b, const lora::WgradP& a, int r, bool vb, bool va, cudaStream_t st);
 qmm_status launch_lora_join(int r, const int* units, int n, const lora::WgradParts& g0, const lora::WgradParts& g1, cudaStream_t st);
 size_t expert_sort_workspace_bytes(int64_t P, int E);
 qmm_status launch_expert_sort(const int* idx, int64_t P, int E, int* order, int* place, int* offsets, int* units, void* ws, cudaStream_t st);
@@ -312,21 +314,15 @@ qmm_status qmm_lora_grad(const qmm_lora_args* a, void* ws, size_t ws_bytes, void
     const int of_a = a->dA ? lora::wgrad_share(blocks - of_b, a->T, a->K, half && !a->x_scale, 0, false) : 0;
     float* const part_b = small ? nullptr : (float*)((char*)ws + l.part);
     float* const part_a = small ? nullptr : part_b + (size_t)of_b * 2 * 128 * a->r;
-    if (a->dB) {
-        const uintptr_t bits = pitch_bits(a->dY, a->lddy, 2);
-        const lora::WgradP p = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, units, a->T, a->n, (int)a->N, a->dB, part_b, of_b, bits % 4 == 0, 0};
-        const bool vec = (bits | (uintptr_t)(a->N * 2)) % 16 == 0;
-        QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, false, true, vec, st) : launch_lora_wgrad_bf16(p, a->r, false, true, vec, st));
-    }
-    if (a->dA) {
-        const bool x8 = a->x_scale != nullptr;
-        const uintptr_t bits = pitch_bits(a->X, a->ldx, x8 ? 1 : 2);
-        const lora::WgradP p = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, units, a->T, a->n, (int)a->K, a->dA, part_a, of_a, bits % 4 == 0,
-                                 a->dB != nullptr};
-        const bool vec = (bits | (uintptr_t)(a->K * 2)) % 16 == 0;
-        QMM_TRY(half ? launch_lora_wgrad_f16(p, a->r, x8, false, vec, st) : launch_lora_wgrad_bf16(p, a->r, x8, false, vec, st));
-    }
-    if (small || !(a->dA || a->dB)) return QMM_OK;
+    if (!a->dA && !a->dB) return QMM_OK;
+    const bool x8 = a->dA && a->x_scale;
+    const uintptr_t bits_b = a->dB ? pitch_bits(a->dY, a->lddy, 2) : 0, bits_a = a->dA ? pitch_bits(a->X, a->ldx, x8 ? 1 : 2) : 0;
+    const lora::WgradP pb = {a->dY, a->lddy, nullptr, 0, a->S, a->scale, order, offsets, units, a->T, a->n, (int)a->N, a->dB, part_b, of_b, bits_b % 4 == 0};
+    const lora::WgradP pa = {a->X, a->ldx, a->x_scale, a->x_format == QMM_ROW_INT8, ds, nullptr, order, offsets, units, a->T, a->n, (int)a->K, a->dA, part_a, of_a, bits_a % 4 == 0};
+    const bool vb = !a->dB || (bits_b | (uintptr_t)(a->N * 2)) % 16 == 0, va = !a->dA || (bits_a | (uintptr_t)(a->K * 2)) % 16 == 0;
+    if (half) QMM_TRY(x8 ? launch_lora_wgrad_f16_rows8(pb, pa, a->r, vb, va, st) : launch_lora_wgrad_f16(pb, pa, a->r, vb, va, st));
+    else QMM_TRY(x8 ? launch_lora_wgrad_bf16_rows8(pb, pa, a->r, vb, va, st) : launch_lora_wgrad_bf16(pb, pa, a->r, vb, va, st));
+    if (small) return QMM_OK;
     const lora::WgradParts gb = {part_b, a->dB, (int)a->N, of_b, 1}, ga = {part_a, a->dA, (int)a->K, of_a, 0};
     return launch_lora_join(a->r, units, a->n, of_b ? gb : ga, of_b ? ga : gb, st);
 }

@@ -1407,7 +1407,6 @@ struct WgradP {
     float* part;                                           // null: a cluster per adapter and 128 columns; else `blocks` share all rows, [blocks][2][R x 128] sums of shared adapters
     int blocks;
     int words;                                             // v's rows begin at whole words
-    int beside;                                            // this launch needs nothing of the one before it, which is the other weight gradient of the same call
 };
 
 // out[a] = sum over the adapter's rows of s (R) x v (W).  A block takes 128 columns of one adapter and 64 rows a stage, two or three stages in flight (cp.async).  Two forms:
@@ -1442,16 +1441,11 @@ template <typename T, bool X8, int R> struct WgradShape {
     static constexpr int smem = front + ahead * parts * part + stages * rows * 4;
 };
 
-template <typename T, bool X8, int R, bool TRANS, bool VEC>
-__global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(const WgradP p)
+// Block `block` of the `blocks` that work on one gradient.
+template <typename T, bool X8, int R, bool TRANS, bool VEC> __device__ __forceinline__ void wgrad(const WgradP& p, int block, int blocks, uint8_t* smem)
 {
-    // The next launch may begin once everything before this one is complete: the second weight gradient then runs beside the first, without waiting for it at its
-    // beginning, but at its end, so that what comes after it comes after both.
-    if (!p.beside) pdl_wait();
-    pdl_launch_dependents();
     using S = WgradShape<T, X8, R>;
     constexpr int MT = S::MT, NT = S::NT, WC = S::WC, RG = S::RG, RT = S::RT;
-    extern __shared__ __align__(16) uint8_t smem[];
     uint8_t* s_part = smem + S::front;
     float* s_scale = reinterpret_cast<float*>(s_part + S::ahead * S::parts * S::part);
     const uint32_t base = (uint32_t)__cvta_generic_to_shared(smem), part0 = base + S::front;
@@ -1466,12 +1460,12 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
     __shared__ int at_chunk, at_unit, at_left, seg_a, seg_col, seg_slot;      // seg_slot: -1, or where the segment's part goes
     if (p.part) {
         const int line = max(__ldg(p.units + p.n), 0);
-        const LineShares shares((int64_t)chunks * line, gridDim.x);
-        const int64_t from = shares.begin(blockIdx.x), to = shares.begin(blockIdx.x + 1);
+        const LineShares shares((int64_t)chunks * line, blocks);
+        const int64_t from = shares.begin(block), to = shares.begin(block + 1);
         if (to <= from) at_left = 0;
         else if (tid == 0) at_left = (int)(to - from), at_chunk = (int)(from / line), at_unit = (int)(from - from / line * line), seg_slot = -2;
         // adapters without rows
-        for (int64_t e = (int64_t)blockIdx.x * kWarps + warp; e < (int64_t)p.n * chunks; e += (int64_t)gridDim.x * kWarps) {
+        for (int64_t e = (int64_t)block * kWarps + warp; e < (int64_t)p.n * chunks; e += (int64_t)blocks * kWarps) {
             const int c = (int)(e / p.n), none = (int)(e - (int64_t)c * p.n);
             if (__ldg(p.units + none) != __ldg(p.units + none + 1)) continue;
             const int wide = min(S::cols, p.W - c * S::cols);
@@ -1677,7 +1671,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
             seg_slot = some == u1 - u0 ? -1 : slot == -2 ? 0 : 1;              // the block's first segment has the first place
         }
     } else {
-        const int64_t id = blockIdx.x / size;
+        const int64_t id = block / size;
         a = (int)(id / chunks), col0 = (int)(id - (int64_t)a * chunks) * S::cols;
         first = max(__ldg(p.offsets + a), 0), end = min(__ldg(p.offsets + a + 1), p.T);
         share_of(end > first ? (end - first + S::rows - 1) / S::rows : 0, rank, size, st0, st1);
@@ -1783,7 +1777,7 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
     if (slot < 0) {
         out = p.out + (TRANS ? ((int64_t)seg_a * p.W + seg_col) * R : (int64_t)seg_a * R * p.W + seg_col), wide = p.W - seg_col;
     } else {
-        out = p.part + ((int64_t)blockIdx.x * 2 + slot) * (R * S::cols), wide = pitch = S::cols;
+        out = p.part + ((int64_t)block * 2 + slot) * (R * S::cols), wide = pitch = S::cols;
     }
     if constexpr (TRANS) {                                 // [column][rank]
         for (int i = i0 + tid; i < i1; i += kThreads) {    // four ranks of one column
@@ -1815,7 +1809,18 @@ __global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(
         cluster_arrive();                                  // (a block's shared memory stays until the others have read it)
         cluster_wait();
     }
-    if (p.beside) pdl_wait();
+}
+
+// Both gradients as one grid, dB's blocks first: they run beside one another, behind one wait for all that they read.
+// VB, VA: dY's and X's rows are whole pieces of 16 bytes; X8: X has 8 bits.
+template <typename T, bool X8, int R, bool VB, bool VA>
+__global__ void __launch_bounds__(kThreads, R >= 128 ? 1 : 2) lora_wgrad_kernel(const __grid_constant__ WgradP b, const __grid_constant__ WgradP a, int of_b)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    extern __shared__ __align__(16) uint8_t smem[];
+    if ((int)blockIdx.x < of_b) wgrad<T, false, R, true, VB>(b, blockIdx.x, of_b, smem);
+    else wgrad<T, X8, R, false, VA>(a, blockIdx.x - of_b, gridDim.x - of_b, smem);
 }
 
 // What the blocks of one weight gradient left in parts.
@@ -1963,30 +1968,32 @@ template <typename T, int LAY> static qmm_status launch_pair(const LoraP& p, int
     });
 }
 
-template <typename T, bool TRANS, bool VEC> static qmm_status launch_wgrad(const WgradP& p, int r, bool x8, cudaStream_t st)
+// dB (b.out null: not wanted) and dA (a.out null).
+template <typename T, bool X8> static qmm_status launch_wgrads(const WgradP& b, const WgradP& a, int r, bool vb, bool va, cudaStream_t st)
 {
     return by_rank(r, [&](auto rank) {
         constexpr int R = decltype(rank)::value;
-        auto go = [&](auto e8) {
-            constexpr bool X8 = decltype(e8)::value;
-            using S = WgradShape<T, X8, R>;
-            constexpr int smem = S::smem;
+        using SB = WgradShape<T, false, R>;
+        using SA = WgradShape<T, X8, R>;
+        auto go = [&](auto vec_b, auto vec_a) {
+            constexpr int most = SB::smem > SA::smem ? SB::smem : SA::smem;
             static std::atomic<uint64_t> configured{0};
-            auto kern = lora_wgrad_kernel<T, X8, R, TRANS, VEC>;
-            const qmm_status s = configure_once(configured, kern, smem, false, "adapter gradient attributes");
+            auto kern = lora_wgrad_kernel<T, X8, R, decltype(vec_b)::value, decltype(vec_a)::value>;
+            const qmm_status s = configure_once(configured, kern, most, false, "adapter gradient attributes");
             if (s != QMM_OK) return s;
-            if (p.part) return launch_pdl(kern, dim3((unsigned)p.blocks), kThreads, smem, 1, st, "adapter gradient launch", p);
-            const int64_t columns = (int64_t)p.n * ((p.W + S::cols - 1) / S::cols);
+            const WgradP& any = b.out ? b : a;
+            const int smem = b.out ? most : SA::smem;
+            if (any.part) return launch_pdl(kern, dim3((unsigned)(b.blocks + a.blocks)), kThreads, smem, 1, st, "adapter gradient launch", b, a, b.blocks);
+            const int64_t of_b = b.out ? (int64_t)b.n * ((b.W + SB::cols - 1) / SB::cols) : 0, of_a = a.out ? (int64_t)a.n * ((a.W + SA::cols - 1) / SA::cols) : 0;
+            const int64_t columns = of_b + of_a;
             // blocks that share a column's rows: as many as make about two per SM in all, 128 rows each at least if one adapter had them all
             int size = 1;
-            while (size < 8 && columns * size < 3 * kNumSMs / 2 && (int64_t)p.T >= 256 * size) size *= 2;
+            while (size < 8 && columns * size < 3 * kNumSMs / 2 && (int64_t)any.T >= 256 * size) size *= 2;
             if (columns * size > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapter gradients: %lld blocks are too many for one launch", (long long)(columns * size));
-            return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", p);
+            return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", b, a, (int)(of_b * size));
         };
-        if constexpr (!TRANS)
-            return x8 ? go(std::true_type()) : go(std::false_type());
-        else
-            return go(std::false_type());
+        if (vb) return va ? go(std::true_type(), std::true_type()) : go(std::true_type(), std::false_type());
+        return va ? go(std::false_type(), std::true_type()) : go(std::false_type(), std::false_type());
     });
 }
 
@@ -2010,11 +2017,10 @@ static inline int wgrad_share(int blocks, int64_t T, int64_t W, bool tf32, int64
     {                                                                                                                                                      \
         return back ? lora::launch_pair<TYPE, 1>(p, r, false, vx, vy, st) : lora::launch_pair<TYPE, 0>(p, r, x8, vx, vy, st);                              \
     }
-#define QMM_LORA_WGRAD_TYPE(NAME, TYPE)                                                                                                                    \
-    qmm_status launch_lora_wgrad_##NAME(const lora::WgradP& p, int r, bool x8, bool trans, bool vec, cudaStream_t st)                                      \
+#define QMM_LORA_WGRAD_TYPE(NAME, TYPE, X8)                                                                                                                \
+    qmm_status launch_lora_wgrad_##NAME(const lora::WgradP& b, const lora::WgradP& a, int r, bool vb, bool va, cudaStream_t st)                            \
     {                                                                                                                                                      \
-        if (trans) return vec ? lora::launch_wgrad<TYPE, true, true>(p, r, false, st) : lora::launch_wgrad<TYPE, true, false>(p, r, false, st);            \
-        return vec ? lora::launch_wgrad<TYPE, false, true>(p, r, x8, st) : lora::launch_wgrad<TYPE, false, false>(p, r, x8, st);                           \
+        return lora::launch_wgrads<TYPE, X8>(b, a, r, vb, va, st);                                                                                         \
     }
 
 // The parts of one or two (g1.blocks > 0) weight gradients.

@@ -3,7 +3,7 @@
 
 namespace qmm {
 
-QMM_LORA_WGRAD_TYPE(bf16, __nv_bfloat16)
+QMM_LORA_WGRAD_TYPE(bf16, __nv_bfloat16, false)
 QMM_LORA_JOIN
 
 }  // namespace qmm

@@ -3,6 +3,6 @@
 
 namespace qmm {
 
-QMM_LORA_WGRAD_TYPE(f16, __half)
+QMM_LORA_WGRAD_TYPE(f16, __half, false)
 
 }  // namespace qmm

@@ -342,3 +342,30 @@ def test_no_rows(qmm):
     assert qmm.lora(x, idx, a, b, y).shape == (0, 16)
     dx, da, db = qmm.lora_grad(y, x, None, idx, a, b)
     assert dx.shape == (0, 32) and not da.any() and not db.any()
+
+
+@pytest.mark.parametrize("dt,x8", [("f16", None), ("bf16", None), ("bf16", "e4m3")])
+@pytest.mark.parametrize("T,K,N", [(300, 256, 136), (300, 131, 136), (300, 256, 77), (900, 256, 136), (900, 131, 136), (900, 256, 77)])
+def test_one_workspace_for_call_after_call(qmm, dt, x8, T, K, N):
+    """Calls on one workspace right behind one another, each with other rows of other adapters: both weight gradients read the sort and the dS of their own call.  Small integers: every
+    sum is exact, whoever adds what."""
+    n, r, calls = 5, 16, 12
+    p = Problem(qmm, dt, T, K, N, n, r, "uniform", x8=x8)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+
+    def ints(shape, lo, hi, dtype):
+        return torch.randint(lo, hi + 1, shape, generator=gen, device="cuda").to(dtype)
+    b = ints(p.b.shape, -1, 1, p.dtype)
+    ws = torch.full((qmm.lora_workspace_bytes(T, n, r),), 255, dtype=torch.uint8, device="cuda")
+    each = []
+    for _ in range(calls):
+        x = ints((T, K), -2, 2, torch.float32).to(ref.ROW8[x8] if x8 else p.dtype)
+        each.append((ints((T,), -1, n - 1, torch.int32), x, ints((T, N), -2, 2, p.dtype), ints((T, r), -9, 9, torch.float32)))
+    ones = torch.ones(T, device="cuda") if x8 else None
+    torch.cuda.synchronize()
+    got = [qmm.lora_grad(dy, x, s, idx, p.a, b, x_scale=ones, dx=False, ws=ws)[1:] for idx, x, dy, s in each]
+    for (idx, x, dy, s), (da, db) in zip(each, got):
+        for e in range(n):
+            t = torch.nonzero(idx == e)[:, 0]
+            ds = dy[t].double() @ b[e].double()
+            assert torch.equal(da[e].double(), ds.T @ x[t].double()) and torch.equal(db[e].double(), dy[t].double().T @ s[t].double())
