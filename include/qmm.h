@@ -511,7 +511,7 @@ qmm_status qmm_expert_route(qmm_dtype dtype, const void* logits, int64_t ld, int
 
 /* Gradient of the weights with respect to the logits, at the choice idx (which is constant; so is the bias):
  * dlogits [T, ldd] of type `dtype` is written whole.  dweights fp32 [T, topk]; what stands at dropped slots is not read
- * into the result.  dlogits may be logits.                                                            */
+ * into the result.  dlogits may be logits (ldd = ld).                                                 */
 qmm_status qmm_expert_route_grad(qmm_dtype dtype, const float* dweights, const void* logits, int64_t ld, const int32_t* idx, int32_t T, int32_t E,
                                  int32_t topk, qmm_scores scores, int32_t renormalize, float scale, void* dlogits, int64_t ldd, void* stream);
 

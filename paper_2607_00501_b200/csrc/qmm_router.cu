@@ -33,7 +33,9 @@ struct RouteP {
 // A logit as the rules read it: NaN counts as -inf, +inf as the largest finite value.
 __device__ __forceinline__ float route_logit(float v) { return v == v ? fminf(v, FLT_MAX) : -INFINITY; }
 
-template <typename T, int P> __device__ __forceinline__ void load_logits(const T* __restrict__ row, int E, int lane, int vec, float (&l)[P])
+// NC: nobody writes the row meanwhile (the gradient may take the logits' place).
+template <bool NC, typename V> __device__ __forceinline__ V load_as(const void* p) { return NC ? __ldg(reinterpret_cast<const V*>(p)) : *reinterpret_cast<const V*>(p); }
+template <typename T, int P, bool NC = true> __device__ __forceinline__ void load_logits(const T* row, int E, int lane, int vec, float (&l)[P])
 {
     constexpr int V = 16 / (int)sizeof(T) < P ? 16 / (int)sizeof(T) : P;     // elements per load
     if (vec && V > 1) {
@@ -43,13 +45,13 @@ template <typename T, int P> __device__ __forceinline__ void load_logits(const T
             if (e < E) {
                 uint32_t u[V * sizeof(T) / 4 ? V * sizeof(T) / 4 : 1];
                 if constexpr (V * sizeof(T) == 16) {
-                    const uint4 q = __ldg(reinterpret_cast<const uint4*>(row + e));
+                    const uint4 q = load_as<NC, uint4>(row + e);
                     u[0] = q.x, u[1] = q.y, u[2] = q.z, u[3] = q.w;
                 } else if constexpr (V * sizeof(T) == 8) {
-                    const uint2 q = __ldg(reinterpret_cast<const uint2*>(row + e));
+                    const uint2 q = load_as<NC, uint2>(row + e);
                     u[0] = q.x, u[1] = q.y;
                 } else if constexpr (V * sizeof(T) == 4) {
-                    u[0] = __ldg(reinterpret_cast<const uint32_t*>(row + e));
+                    u[0] = load_as<NC, uint32_t>(row + e);
                 }
 #pragma unroll
                 for (int k = 0; k < V; ++k) {
@@ -541,7 +543,7 @@ struct RouteGradP {
 // Bound by latency: a warp's row is 512 bytes, read, exchanged and written (16384 x 128 fp32: 18 MB in 10 us; the bytes take 2.8).
 template <typename T, int P>
 __global__ void __launch_bounds__(32 * kRouteWarps)
-expert_route_grad_kernel(const T* __restrict__ logits, const RouteGradP p, T* __restrict__ dlogits)
+expert_route_grad_kernel(const T* logits, const RouteGradP p, T* dlogits)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -561,7 +563,7 @@ expert_route_grad_kernel(const T* __restrict__ logits, const RouteGradP p, T* __
     }
     float d = 0.0f, m = 0.0f, z = 1.0f, dot = 0.0f, s = 0.0f, l[P];
     if (!p.sigmoid && !p.renorm) {
-        load_logits<T, P>(row, p.E, lane, p.vec > 1, l);
+        load_logits<T, P, false>(row, p.E, lane, p.vec > 1, l);
         m = -INFINITY;
 #pragma unroll
         for (int i = 0; i < P; ++i) m = fmaxf(m, l[i]);
@@ -604,6 +606,7 @@ expert_route_grad_kernel(const T* __restrict__ logits, const RouteGradP p, T* __
         d = full ? s * (sum - dot) : sum;
         if (last != lane) e = -1;
     }
+    __syncwarp();                                          // dlogits may be logits: the warp has read its row
     // the whole row, then the chosen ones over it (the same warp: its stores to an address stay in order)
     const float all = z > 0.0f ? -dot / z : 0.0f;          // (0: every expert masked)
     constexpr int V = 16 / (int)sizeof(T) < P ? 16 / (int)sizeof(T) : P;

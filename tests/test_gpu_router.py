@@ -245,3 +245,17 @@ def test_all_experts_equal_but_few(qmm, sigmoid, E, topk, G):
     l[20:, E - 3] = 1e-6                                   # one score is better by a few roundings, one by none
     l[30:, E - 2] = 1e-9
     check(qmm, l, topk, sigmoid, bias, G, G, 1, True)
+
+
+@pytest.mark.parametrize("dt", list(ref.DTYPES))
+@pytest.mark.parametrize("sigmoid,renorm", list(itertools.product((False, True), repeat=2)))
+@pytest.mark.parametrize("T,E,topk,pitch", [(1, 1, 1, 1), (50, 128, 8, 128), (50, 128, 8, 131), (33, 46, 7, 48), (40, 1024, 32, 1024), (40, 1023, 32, 1023)])
+def test_gradient_in_the_logits_place(qmm, dt, sigmoid, renorm, T, E, topk, pitch):
+    l = torch.full((T, pitch), 9.0, dtype=ref.DTYPES[dt], device="cuda")[:, :E]
+    l.copy_(logits_of(T, E, dt, "masked" if E > 1 else "plain", E))
+    scores = qmm.SIGMOID if sigmoid else qmm.SOFTMAX
+    idx, _ = qmm.expert_route(l, topk, scores, renormalize=renorm)
+    dw = torch.randn(T, topk, generator=torch.Generator().manual_seed(2)).cuda()
+    want = qmm.expert_route_grad(dw, l, idx, scores, renorm)
+    got = qmm.expert_route_grad(dw, l, idx, scores, renorm, out=l)
+    assert got is l and torch.equal(got, want)
