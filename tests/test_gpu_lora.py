@@ -369,3 +369,131 @@ def test_one_workspace_for_call_after_call(qmm, dt, x8, T, K, N):
             t = torch.nonzero(idx == e)[:, 0]
             ds = dy[t].double() @ b[e].double()
             assert torch.equal(da[e].double(), ds.T @ x[t].double()) and torch.equal(db[e].double(), dy[t].double().T @ s[t].double())
+
+
+# ---- the form for more than 512 rows, against the formulas
+
+@pytest.mark.parametrize("x8", [None, "e4m3", "int8"])
+@pytest.mark.parametrize("dt,K,N,r,pitch,off", [("bf16", 256, 512, 16, 8, 8), ("f16", 264, 136, 32, 16, 16), ("bf16", 256, 512, 64, 3, 1), ("f16", 200, 333, 8, 8, 8), ("bf16", 101, 104, 16, 7, 5),
+                                                ("bf16", 130, 258, 128, 2, 2), ("f16", 257, 131, 64, 4, 4)])
+def test_many_rows_with_gaps(qmm, dt, x8, K, N, r, pitch, off):
+    p = Problem(qmm, dt, 700, K, N, 3, r, "dropped", x8=x8, pitch=pitch, off=off)
+    p.check_forward(p.forward(), p.y0)
+    p.check_backward(*p.backward(), p.dx0)
+    for v in (p.out, p.dx):
+        gap = v.as_strided((v.shape[0] - 1, pitch), (v.stride(0), 1), v.storage_offset() + v.shape[1])
+        assert bool((gap == 7.0).all())
+
+
+@pytest.mark.parametrize("dt,r", [("f16", 16), ("bf16", 64)])
+@pytest.mark.parametrize("K,N", [(300, 520), (264, 1111), (1024, 256)])
+def test_many_rows_in_place_and_without_a_base(qmm, dt, r, K, N):
+    p = Problem(qmm, dt, 1100, K, N, 4, r, "dropped", scaled=False)
+    y0, dx0 = p.y0.clone(), p.dx0.clone()
+    y = p.forward(out=p.y0)
+    assert y is p.y0
+    p.check_forward(y, y0)
+    dx, da, db = p.backward(dx=p.dx0)
+    assert dx is p.dx0
+    p.check_backward(dx, da, db, dx0)
+    y = p.forward(y0=None)
+    p.check_forward(y, None)
+    p.check_backward(*p.backward(dx0=None), None)
+    p.check_forward(p.forward(s=None, y0=y0), y0, s=False)
+
+
+@pytest.mark.parametrize("dt", list(HALVES))
+@pytest.mark.parametrize("kind", ["dropped", "skewed"])
+@pytest.mark.parametrize("T,K,N,n,r", [(600, 512, 768, 4, 8), (700, 1024, 640, 5, 32), (1030, 640, 1024, 3, 64), (800, 1000, 2056, 6, 64), (513, 2048, 128, 2, 128), (2500, 136, 264, 70, 32)])
+def test_many_aligned_rows(qmm, dt, kind, T, K, N, n, r):
+    p = Problem(qmm, dt, T, K, N, n, r, kind)
+    p.check_forward(p.forward(), p.y0)
+    p.check_backward(*p.backward(), p.dx0)
+
+
+@pytest.mark.parametrize("dt", list(HALVES))
+@pytest.mark.parametrize("x8", list(ref.ROW8))
+@pytest.mark.parametrize("T,K,N,n,r", [(600, 264, 136, 3, 8), (900, 1024, 520, 5, 16), (1500, 1000, 304, 4, 32), (700, 2048, 256, 2, 64), (640, 260, 200, 3, 16), (520, 515, 130, 2, 64), (800, 72, 1000, 9, 128)])
+def test_many_rows_of_8_bits(qmm, dt, x8, T, K, N, n, r):
+    p = Problem(qmm, dt, T, K, N, n, r, "dropped", x8=x8)
+    p.check_forward(p.forward(), p.y0)
+    p.check_backward(*p.backward(), p.dx0)
+
+
+@pytest.mark.parametrize("dt,std", [("f16", 2.0**-20), ("f16", 3e4), ("bf16", 1e-30), ("bf16", 1e30)])
+@pytest.mark.parametrize("K,N,r", [(512, 256, 16), (333, 131, 64)])
+def test_many_rows_far_from_one(qmm, dt, std, K, N, r):
+    p = Problem(qmm, dt, 900, K, N, 2, r, "uniform", scaled=False)
+    p.x = (p.x.double() * std).clamp(-6e4 if dt == "f16" else -1e38, 6e4 if dt == "f16" else 1e38).to(p.dtype)
+    p.x64 = p.x.double()
+    p.b = (p.b.double() * max(1e-3, min(1e3, 1 / std))).to(p.dtype)
+    if dt == "f16":
+        p.a *= 8
+    p.check_forward(p.forward(), p.y0)
+    p.dy = (p.dy.double() * max(2.0**-12, min(1.0, std))).to(p.dtype)
+    p.check_backward(*p.backward(), p.dx0)
+
+
+@pytest.mark.parametrize("K,N,r", [(256, 320, 16), (256, 320, 64), (131, 77, 32)])
+def test_a_mixed_row_among_many_does_not_touch_the_others(qmm, K, N, r):
+    T = 900
+    p = Problem(qmm, "bf16", T, K, N, 3, r, "uniform")
+    y = p.forward().clone()
+    dx, da, db = (g.clone() for g in p.backward())
+    p.x[5, 7], p.x[9, 8] = float("inf"), float("nan")
+    p.dy[9, 3] = float("nan")
+    y2 = p.forward()
+    dx2, da2, db2 = p.backward()
+    others = torch.arange(T, device="cuda")
+    others = others[(others != 5) & (others != 9)]
+    assert torch.equal(y[others], y2[others]) and torch.equal(dx[others], dx2[others])
+    assert not torch.isfinite(y2[5]).any() and torch.isnan(y2[9]).all() and torch.isnan(dx2[9]).all()
+    for e in set(range(3)) - {int(p.idx[5]), int(p.idx[9])}:
+        assert torch.equal(da[e], da2[e]) and torch.equal(db[e], db2[e])
+
+
+# ---- the bits that the weight gradients keep
+
+@pytest.mark.parametrize("dt", list(HALVES))
+@pytest.mark.parametrize("T", [40, 600])
+@pytest.mark.parametrize("K,N,r", [(136, 136, 8), (131, 77, 16), (128, 264, 32), (264, 128, 64), (136, 200, 128)])
+def test_all_bits_of_s_reach_the_weight_gradients(qmm, dt, T, K, N, r):
+    """A row for each adapter, ones for x and dy: dB is s, dA is dS, with all their 24 bits (three bf16 parts) or 22 of them (two tf32 parts).  A sum of parts is cut 25 bits below
+    its largest one, which is 2^-24 for each of the three or four; 2^-22 covers both."""
+    dtype, gen = HALVES[dt], torch.Generator(device="cuda").manual_seed(T + K)
+    idx = torch.randperm(T, generator=gen, device="cuda").int()
+    s = (1 + torch.rand(T, r, generator=gen, device="cuda")) * torch.where(torch.rand(T, r, generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    x, a = torch.ones(T, K, dtype=dtype, device="cuda"), torch.zeros(T, r, K, dtype=dtype, device="cuda")
+    dy = torch.ones(T, N, dtype=dtype, device="cuda")
+    _, _, db = qmm.lora_grad(dy, x, s, idx, a, torch.zeros(T, N, r, dtype=dtype, device="cuda"), dx=False)
+    want = s[torch.argsort(idx.long())][:, None, :].double().expand(T, N, r)
+    assert bool(((db.double() - want).abs() <= 2.0**-22 * want.abs()).all())
+    # dS = b[0] + b[1] + ... of powers of two that add up to 24 bits without a rounding
+    b = torch.zeros(T, N, r, dtype=dtype, device="cuda")
+    bits = torch.randint(0, 2, (T, 23, r), generator=gen, device="cuda")
+    b[:, 0] = 1
+    b[:, 1:24] = (bits * 2.0 ** -torch.arange(1, 24, device="cuda")[None, :, None]).to(dtype)
+    want = b.double().sum(1)
+    _, da, _ = qmm.lora_grad(dy, x, s, idx, a, b, dx=False, db=False)
+    want = want[:, :, None].expand(T, r, K)
+    # the sum of dS on the tensor cores: at most two products of 32 elements, cut 25 bits below the largest
+    assert bool(((da.double() - want).abs() <= (2.0**-22 + 2.0**-23) * want.abs()).all())
+
+
+@pytest.mark.parametrize("dt", list(HALVES))
+@pytest.mark.parametrize("K,N,r", [(136, 136, 16), (131, 77, 32), (264, 264, 64), (128, 200, 128)])
+def test_sums_over_many_rows_are_rounded_to_nearest(qmm, dt, K, N, r):
+    """8192 rows of one adapter: a weight gradient is the sum of T / 16 = 512 short products at most, each addition rounded to nearest.  Partial sums of random signs grow with the
+    root of their length, so the roundings add up to 2^-24 / sqrt(3) sqrt(512 / 2) = 5.5e-7 of the result's norm; the products' own cuts (2^-24 for each of four, of a
+    part's size) add less than 2e-7.  Sums that are cut instead, all to one side, are off by 2e-6."""
+    T, dtype, gen = 8192, HALVES[dt], torch.Generator(device="cuda").manual_seed(K)
+    idx = torch.zeros(T, dtype=torch.int32, device="cuda")
+    x, dy = (torch.randn(T, w, generator=gen, device="cuda").to(dtype) for w in (K, N))
+    s = torch.randn(T, r, generator=gen, device="cuda")
+    b = torch.zeros(1, N, r, dtype=dtype, device="cuda")
+    b[0, : min(N, r)] = torch.eye(r, device="cuda", dtype=dtype)[: min(N, r)]               # dS: the first elements of dy, exactly
+    _, da, db = qmm.lora_grad(dy, x, s, idx, torch.zeros(1, r, K, dtype=dtype, device="cuda"), b, dx=False)
+    ds = torch.zeros(T, r, dtype=torch.float64, device="cuda")
+    ds[:, : min(N, r)] = dy[:, : min(N, r)].double()
+    for got, want in ((da[0], ds.T @ x.double()), (db[0], dy.double().T @ s.double())):
+        assert (got.double() - want).norm() <= 7.5e-7 * want.norm()

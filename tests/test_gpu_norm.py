@@ -267,3 +267,17 @@ def test_largest_rows(qmm, dt, K, residual):
         dx, dw = qmm.rms_norm_grad(dy, h, w, eps, dh=dh)
         assert torch.isfinite(dx).all() and torch.isfinite(dw).all()
         check_grad(dx, dw, dy, h, w, eps, dh)
+
+
+@pytest.mark.parametrize("dt", list(ref.DTYPES))
+@pytest.mark.parametrize("M,K", [(3, 64), (700, 1000), (700, 1001), (40, 16384), (5, 32768)])
+def test_gradient_in_the_place_of_what_comes_in(qmm, dt, M, K):
+    """dx over dh, and over dy."""
+    dtype, gen = ref.DTYPES[dt], gen_of(M + K)
+    h, dy, dh, w = rows(M, K, dtype, gen), rows(M, K, dtype, gen), rows(M, K, dtype, gen), rows(1, K, dtype, gen)[0]
+    want, dweight = qmm.rms_norm_grad(dy, h, w, dh=dh)
+    for place in (0, 1):
+        args = [dy.clone(), dh.clone()]
+        dx, dw = qmm.rms_norm_grad(args[0], h, w, dh=args[1], dx=args[place])
+        assert dx is args[place] and torch.equal(dx, want) and torch.equal(dw, dweight)
+        assert torch.equal(args[1 - place], (dy, dh)[1 - place])
