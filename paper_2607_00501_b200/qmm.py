@@ -871,6 +871,9 @@ def rows_dequantize(codes: torch.Tensor, scales: torch.Tensor, out: torch.Tensor
 
 # ---- low-rank adapters beside a shared projection
 
+LORA_ROWS_WITHOUT_WORKSPACE = 512                          # the library's bound: a forward pass of up to so many rows sorts nothing
+
+
 def lora_workspace_bytes(T: int, n: int, r: int) -> int:
     _counts(T, n, r)
     need = lib().qmm_lora_workspace_bytes(T, n, r)
@@ -896,7 +899,7 @@ def lora(x: torch.Tensor, idx: torch.Tensor, a: torch.Tensor, b: torch.Tensor, y
     T = x.shape[0]
     if out is None:
         out = torch.empty((T, b.shape[1]), dtype=b.dtype, device=x.device)
-    if ws is None and T > 512:
+    if ws is None and T > LORA_ROWS_WITHOUT_WORKSPACE:
         ws = torch.empty(lora_workspace_bytes(T, a.shape[0], a.shape[1]), dtype=torch.uint8, device=x.device)
     _check((_layer_ext or _layer()).lora(x, x_scale, idx, a, b, scale, *_lora_plan(plan, T, a.shape[0]), s, y0, out, ws))
     return out

@@ -71,6 +71,16 @@ def test_refusals_of_the_norm(L, a):
     assert L.qmm_rows_dequantize(1, a, 64, None, 2, 64, 0, a, 64, None) == 1 and L.qmm_rows_dequantize(3, a, 64, a, 2, 64, 0, a, 64, None) == 1
 
 
+def test_rows_without_a_workspace(L, a):
+    """The wrapper's bound is the library's: beyond it the workspace holds the blocks' parts, and a forward pass without one is refused."""
+    most = qmm.LORA_ROWS_WITHOUT_WORKSPACE
+    sizes = [qmm.lora_workspace_bytes(T, 1, 128) for T in range(2 * most)]
+    jumps = [T for T in range(2 * most - 1) if sizes[T + 1] - sizes[T] > 1 << 20]
+    assert jumps == [most]
+    q = qmm.LoraArgs(T=most + 1, n=1, r=128, K=64, N=32, X=a, ldx=64, idx=a, A=a, B=a, Y=a, ldy=32)
+    assert L.qmm_lora(ctypes.byref(q), None, 0, None) == 4
+
+
 def test_refusals_of_the_adapters(L, a):
     base = dict(T=600, n=4, r=16, dtype=0, K=64, N=32, X=a, ldx=64, idx=a, A=a, B=a, S=a, Y0=a, ldy0=32, Y=a, ldy=32, dY=a, lddy=32, dX0=a, lddx0=64, dX=a, lddx=64, dA=a, dB=a)
     need = qmm.lora_workspace_bytes(600, 4, 16)
