@@ -1413,7 +1413,8 @@ struct WgradP {
 //   few rows (kSmallRows): the blocks of a cluster share an adapter's rows and add their sums; nothing but one launch
 //   many rows: the line of all adapters' rows, once for each 128 columns, is cut into as many equal pieces as blocks run at once, so that adapters with many rows do not end last;
 //   what two blocks have of one adapter meets in the workspace, and a short launch adds it
-//   (500 x 1001 x 700 at r = 8, whole call with both passes: 38 us by clusters, 50 so; 1000 x 1000 x 1500 at r = 16: 52.7 and 49.9; 8192 x 2048 x 8192 at r = 32: 254 and 234)
+//   (both passes of 1000 x 1000 x 1500 at r = 16: by clusters 52.7 us, 49.9 so; 8192 x 2048 x 8192 at r = 32: 254 and 234; 500 x 1001 x 700 at r = 8: 38 and 50.  Measured when the
+//   two gradients were launches of their own.)
 // A warp has all R ranks of 64, 32 or 16 columns (R x columns = 2048 where R >= 32: 64 accumulators a lane), the warps of a column group share the stage's
 // rows.  k of the products is the row: v comes out of shared memory transposed (ldmatrix.trans; codes of 8 bits by words and byte permutes), s is brought into
 // [rank][row] once per stage, split into 16-bit or tf32 parts:
@@ -1988,9 +1989,10 @@ template <typename T, bool X8> static qmm_status launch_wgrads(const WgradP& b, 
             if (any.part) return launch_pdl(kern, dim3((unsigned)(b.blocks + a.blocks)), kThreads, smem, 1, st, "adapter gradient launch", b, a, b.blocks);
             const int64_t of_b = b.out ? (int64_t)b.n * ((b.W + SB::cols - 1) / SB::cols) : 0, of_a = a.out ? (int64_t)a.n * ((a.W + SA::cols - 1) / SA::cols) : 0;
             const int64_t columns = of_b + of_a;
-            // blocks that share a column's rows: as many as make about two per SM in all, 128 rows each at least if one adapter had them all
+            // blocks that share a column's rows: as many as make about two per SM in all, 128 rows each at least if one adapter had them all, 96 up to r = 16, where a stage's products
+            // are short (dS, dA and dB of 500 x 1001 x 700 at r = 8: 17.3 us with 96, 19.8 with 128; 390 x 512 x 2048 at r = 64: 29.2 and 27.2)
             int size = 1;
-            while (size < 8 && columns * size < 3 * kNumSMs / 2 && (int64_t)any.T >= 256 * size) size *= 2;
+            while (size < 8 && columns * size < 3 * kNumSMs / 2 && (int64_t)any.T >= (R <= 16 ? 192 : 256) * size) size *= 2;
             if (columns * size > 0x7FFFFFFF) return fail(QMM_ERR_UNSUPPORTED, "adapter gradients: %lld blocks are too many for one launch", (long long)(columns * size));
             return launch_pdl(kern, dim3((unsigned)(columns * size)), kThreads, smem, size, st, "adapter gradient launch", b, a, (int)(of_b * size));
         };
