@@ -573,7 +573,7 @@ struct LoraP {
     int rest;                                              // rows without an adapter get y0 (0: they have it already)
     int words;                                             // operands whose rows begin at whole words: 1 x, 2 w1, 4 y0, 8 w2
 };
-// A piece of 16 bytes of which `bytes` exist, by words: for rows that begin at whole words.  safe: any valid address.
+// A piece of 16 bytes of which `bytes` exist, by words: for rows that begin at whole words.  safe: any valid address of a whole word (a copy of no bytes needs an aligned one too).
 __device__ __forceinline__ void async_words(uint32_t to, const void* from, int bytes, const void* safe)
 {
 #pragma unroll
@@ -1195,7 +1195,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
                     const bool in = left > 0 && from[q];
                     async16(at + y_place(fr + 16 * q, fc), in ? from[q] + n0 + 8 * fc : w2, in ? 16 : 0);
                 } else if (p.words & 4) {
-                    async_words(at + y_place(fr + 16 * q, fc), from[q] + n0 + 8 * fc, from[q] ? 2 * left : 0, w2);
+                    async_words(at + y_place(fr + 16 * q, fc), from[q] + n0 + 8 * fc, from[q] ? 2 * left : 0, p.s);
                 } else {
                     uint32_t u[4];
                     load8<T, false, false>(from[q], n0 + 8 * fc, from[q] ? left : 0, u);

@@ -497,3 +497,22 @@ def test_sums_over_many_rows_are_rounded_to_nearest(qmm, dt, K, N, r):
     ds[:, : min(N, r)] = dy[:, : min(N, r)].double()
     for got, want in ((da[0], ds.T @ x.double()), (db[0], dy.double().T @ s.double())):
         assert (got.double() - want).norm() <= 7.5e-7 * want.norm()
+
+
+@pytest.mark.parametrize("dt,x8", [("f16", None), ("bf16", None), ("bf16", "int8")])
+@pytest.mark.parametrize("T", [40, 700])
+@pytest.mark.parametrize("K,N,r,off_a,off_b", [(256, 136, 16, 1, 1), (256, 136, 64, 2, 1), (130, 258, 8, 1, 2), (131, 77, 32, 3, 5), (264, 264, 128, 8, 1), (256, 512, 32, 1, 8)])
+def test_adapters_that_begin_at_any_element(qmm, dt, x8, T, K, N, r, off_a, off_b):
+    """A and B as contiguous pieces of larger tensors, beside rows that are aligned, rows of whole words, and no base at all."""
+    p = Problem(qmm, dt, T, K, N, 3, r, "dropped", x8=x8)
+
+    def at(t, off):
+        buf = torch.full((t.numel() + 16,), 7.0, dtype=t.dtype, device="cuda")
+        v = buf[off: off + t.numel()].view(t.shape)
+        v.copy_(t)
+        return v
+    p.a, p.b = at(p.a, off_a), at(p.b, off_b)
+    p.check_forward(p.forward(), p.y0)
+    p.check_backward(*p.backward(), p.dx0)
+    p.check_forward(p.forward(y0=None), None)
+    p.check_backward(*p.backward(dx0=None), None)
