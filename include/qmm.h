@@ -547,14 +547,15 @@ qmm_status qmm_rows_dequantize(qmm_row_format fmt, const void* codes, int64_t ld
 /* ---- low-rank adapters beside a shared projection ----
  *
  * Row t of X [T, K] belongs to adapter a = idx[t] of n (outside [0, n): to none).  Adapters lie one after the other, A [n, r, K]
- * and B [n, N, r], of X's type (QMM_F16 or QMM_BF16); r is 8, 16, 32, 64 or 128 (pad with zeros).
+ * and B [n, N, r], of X's type (QMM_F16 or QMM_BF16); r is 8, 16, 32, 64 or 128 (pad with zeros).  T <= 2^22, n <= 1024, K, N <= 2^20.
  *   qmm_lora       S[t] = A[a] x[t] (fp32),  Y[t] = Y0[t] + scale[a] * B[a] S[t]
  *   qmm_lora_grad  dS[t] = scale[a] * B[a]^T dY[t],  dX[t] = dX0[t] + A[a]^T dS[t],
  *                  dA[a] = sum_t dS[t] x[t]^T,  dB[a] = scale[a] * sum_t dY[t] S[t]^T   (sums over the adapter's rows; fp32, in a fixed order)
  * A row without an adapter has Y = Y0 and dX = dX0, its row of S is neither written nor read; an adapter without rows has gradients 0.
  * X may be rows of 8 bits (x_format, x_scale as qmm_rms_norm and qmm_rows_quantize leave them), in the forward pass, in dA, or in both.
  * Accuracy: sums in fp32; S and dS enter the second products as two 16-bit parts (off by 2^-16 of the row's largest element at most)
- * and the weight gradients as three bf16 or two tf32 parts (off by 2^-22 of themselves).
+ * and the weight gradients as three bf16 or two tf32 parts (off by 2^-22 of themselves).  A result that is infinite by the formulas
+ * may be NaN instead: the parts of an infinity are.
  *   order, offsets, units  of qmm_expert_sort(idx, T, 1, n), for callers that use one sort for many projections; NULL: the call
  *                          sorts in its workspace (up to 512 rows a forward pass needs none)
  *   Y0 may be Y, dX0 may be dX (in place); NULL counts as zeros.  Otherwise no output may overlap an input.

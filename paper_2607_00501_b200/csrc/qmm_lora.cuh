@@ -676,7 +676,8 @@ template <typename T, bool VEC> __device__ __forceinline__ void copy_row(const L
     }
 }
 
-// Bound by latency: the adapter's rows, x and the weights, the meeting, y.  16 x 8192 x 2048 of 16 adapters 6.6 us on the GPU (5 MB: 0.8 us), 77 x 2048 x 2048 of five at r = 64 10 us.
+// Bound by latency: the adapter's rows, x and the weights, the meeting (behind which the second product's weights are asked for where R > 32), y.  16 x 8192 x 2048 of 16 adapters 6.6 us
+// on the GPU (5 MB: 0.8 us), 77 x 2048 x 2048 of five at r = 64 10.2 us.
 // Both products of up to 16 rows of one adapter by a cluster of blocks: each takes a share of K, the shares' sums meet through distributed shared memory, and each takes
 // a share of N.  One launch: for a decode step two, and a sort before them, would cost as much as all their work.
 //   groups 0: cluster b is there for row b; it does something if row b is the first, 17th, ... of its adapter's rows, and then takes 16 of them
@@ -1084,8 +1085,8 @@ __device__ __forceinline__ void narrow_stages(float (&acc)[NarrowShape<X8, R>::M
 }
 
 // The narrowing product of tiles of 64 rows, a tile per cluster whose blocks share K.  -> s [T, R].
-// Bound by HBM (x once; w1 comes from L2) and the fill of its stages: 8192 x 8192 bf16 at r = 32, 134 MB in 32 us (4.2 TB/s; 64 us without stages), 8192 x 2048 e4m3 14.4 us,
-// 2048 x 4096 fp16 at r = 16 11.5 us.
+// Bound by HBM (x once; w1 comes from L2) and the fill of its stages: 8192 x 8192 bf16 at r = 32, 134 MB in 32 us (4.2 TB/s; 64 us without stages), 8192 x 2048 e4m3 14 to 16 us,
+// 2048 x 4096 fp16 at r = 16 12 us.
 template <typename T, bool X8, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? NarrowShape<X8, R>::blocks : 2) lora_narrow_kernel(const LoraP p)
 {
@@ -1343,7 +1344,7 @@ __device__ __forceinline__ void widen_stages(const LoraP& p, const T* __restrict
 }
 
 // The widening product: a block takes a tile of 64 rows and `span` column groups.  blockIdx.x = tile * spans + span; blocks from `tile_blocks` on copy the rows without an adapter.
-// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s) on rows used before, 57 on others, 8192 x 8192 bf16 at r = 32, 268 MB in 55 us (4.9); a copy in tiles of this shape reaches
+// Bound by HBM (y0 and y once): 2048 x 28672 fp16 at r = 16, 235 MB in 47 us (5.0 TB/s) on rows used before, 57 on others, 8192 x 8192 bf16 at r = 32, 268 MB in 55 to 58 us (4.9); a copy in tiles of this shape reaches
 // 5.3 to 6.0 TB/s.  The rest is each block's chain of loads to its first rows, and the warps' waits for a stage.
 template <typename T, int R, int LAY, bool VEC>
 __global__ void __launch_bounds__(kThreads, VEC ? WideShape<R, LAY>::blocks : R <= 64 ? 2 : 1) lora_widen_kernel(const LoraP p, int spans, int per_span, int tile_blocks)

@@ -512,8 +512,8 @@ __device__ __forceinline__ void route_one(const T* __restrict__ row, int64_t t, 
     }
 }
 
-// Bound by instruction issue and the latency of the warp's reductions where there are many tokens (16384 x 128 fp32: 15 us for 9.4 MB; the bytes take 1.4), by the launch and one
-// token's chain of them where there are few (4 x 128: 2.0 us; 2048 x 256 bf16 with a bias and groups 7.6).
+// Bound by the latency of a token's chain of reductions: with many tokens (16384 x 128 fp32: 12 us for 9.4 MB; the bytes take 1.4) issue slots are 45 % busy at 43 % of the
+// warps an SM can have, with few (4 x 128: 2.2 us; 2048 x 256 bf16 with a bias and groups 7.8) the launch and one chain are all there is.
 template <typename T, int P> __global__ void __launch_bounds__(32 * kRouteWarps, P <= 4 ? 8 : P == 8 ? 6 : 4) expert_route_kernel(const T* __restrict__ logits, const RouteP p)
 {
     pdl_launch_dependents();
@@ -540,7 +540,7 @@ struct RouteGradP {
 
 // One warp per token: lane j works out what flows into the logit of choice j; every other logit gets zero, or -s (g . s) where the weights are a softmax over all
 // experts.  Differences of g are summed instead of the difference of sums: sum_j p_j (g_i - g_j) loses nothing where one weight is nearly 1.
-// Bound by latency: a warp's row is 512 bytes, read, exchanged and written (16384 x 128 fp32: 18 MB in 10 us; the bytes take 2.8).
+// Bound by latency: a warp's row is 512 bytes, read, exchanged and written (16384 x 128 fp32, all of the four forms: 18 MB in 5.7 to 7.4 us; the bytes take 2.8).
 template <typename T, int P>
 __global__ void __launch_bounds__(32 * kRouteWarps)
 expert_route_grad_kernel(const T* logits, const RouteGradP p, T* dlogits)
