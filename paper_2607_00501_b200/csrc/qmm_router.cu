@@ -107,6 +107,17 @@ __device__ __forceinline__ float sigmoid_f(float l) { return l < kSigmoidEnd ? e
 // The same for comparisons: below -87 it is 0, which is nearer than they look.
 __device__ __forceinline__ float sigmoid_score(float l) { return __fdividef(1.0f, 1.0f + expf(-l)); }
 
+// Shares of the chosen scores in their sum.  v: the lane's chosen logit, -inf for none; top: the largest.  Scores relative to the largest one where exp(top) leaves fp32's range; a score
+// below that range beside a larger one is its ratio to that one, so that a share underflows only where it is below fp32 itself.
+__device__ __forceinline__ float chosen_share(float v, float top, bool there, int sigmoid, float least)
+{
+    float w = 0.0f;
+    if (there) w = sigmoid ? (top < kSigmoidEnd ? expf(v - top) : sigmoid_f(v)) : expf(v - top);
+    const float sum = fmaxf(warp_sum(w), least);
+    if (there) w = sigmoid && v < kSigmoidEnd && top >= kSigmoidEnd && top < 0.0f ? expf(v - top) * (expf(top) / sum) : w / sum;
+    return w;
+}
+
 // Order of fp64 values as unsigned numbers, as route_key; 0 is left for "none".
 __device__ __forceinline__ unsigned long long key_of(double v)
 {
@@ -500,11 +511,7 @@ __device__ __forceinline__ void route_one(const T* __restrict__ row, int64_t t, 
     if (!p.renorm) {
         if (sel >= 0) w = p.sigmoid ? sigmoid_f(v) : expf(v - m) * per_z;
     } else {
-        // weights relative to the largest chosen score: no underflow, whatever the logits
-        const float top = warp_max(v);
-        if (sel >= 0) w = p.sigmoid ? (top < kSigmoidEnd ? expf(v - top) : sigmoid_f(v)) : expf(v - top);
-        const float sum = warp_sum(w);
-        if (sel >= 0) w /= sum;
+        w = chosen_share(v, warp_max(v), sel >= 0, p.sigmoid, 0.0f);
     }
     if (lane < p.topk) {
         p.idx[(int64_t)t * p.topk + lane] = sel;
@@ -581,10 +588,7 @@ expert_route_grad_kernel(const T* logits, const RouteGradP p, T* dlogits)
     } else if (!p.renorm) {
         if (e >= 0) d = g * sigmoid_f(v) * sigmoid_f(-v);
     } else {
-        const float top = warp_max(v);
-        float w = 0.0f;
-        if (e >= 0) w = p.sigmoid ? (top < kSigmoidEnd ? expf(v - top) : sigmoid_f(v)) : expf(v - top);
-        w /= fmaxf(warp_sum(w), FLT_MIN);
+        const float w = chosen_share(v, warp_max(v), e >= 0, p.sigmoid, FLT_MIN);
         float sum = 0.0f;
         for (int j = 0; j < p.topk; ++j) sum = fmaf(__shfl_sync(0xFFFFFFFFu, w, j), g - __shfl_sync(0xFFFFFFFFu, g, j), sum);
         d = e >= 0 ? w * sum : 0.0f;

@@ -259,3 +259,28 @@ def test_gradient_in_the_logits_place(qmm, dt, sigmoid, renorm, T, E, topk, pitc
     want = qmm.expert_route_grad(dw, l, idx, scores, renorm)
     got = qmm.expert_route_grad(dw, l, idx, scores, renorm, out=l)
     assert got is l and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("E", [12, 256])
+def test_weights_of_chosen_scores_far_from_one_another(qmm, dt, E):
+    """Biases choose experts whose scores lie many orders below one: the weights are ratios of the scores, ordinary numbers where the smaller scores are none."""
+    sets = [(-44, -102, -60), (-75, -131, -110), (-1, -85, -70), (5, -86, -30), (-79, -81, -150), (-81, -85, -160), (-20, -87, -104), (0, -84, -80), (-10, -10, -95)]
+    l, bias = torch.full((len(sets), E), 3.0), torch.full((E,), -3.0)
+    bias[1:10:4] = torch.tensor([4.0, 3.0, 2.0])
+    for t, s in enumerate(sets):
+        l[t, 1:10:4] = torch.tensor(s, dtype=torch.float32) + (0.37 if dt == "f32" else 0.0)
+    l = l.to(ref.DTYPES[dt])
+    for scale in (1.5, -2.0):
+        idx, w = qmm.expert_route(l.cuda(), 3, qmm.SIGMOID, bias.cuda(), renormalize=True, scale=scale)
+        want_idx, want = ref.route(l, 3, True, bias, 1, 1, 1, True, scale)
+        assert torch.equal(idx.cpu().long(), want_idx) and torch.equal(want_idx, torch.tensor([[1, 5, 9]] * len(sets)))
+        # expf: 2 ulp, its argument's rounding of up to 2^-24 of 150, twice; half a dozen roundings; below fp32's normal numbers one of 2^-149, twice
+        tol = (2 * 150 + 32) * 2.0**-24 * want.abs() + 2.0**-147
+        assert bool(((w.cpu().double() - want).abs() <= tol).all())
+        dw = torch.tensor([[1.0, -2.0, 0.5]]).expand(len(sets), 3).contiguous()
+        got = qmm.expert_route_grad(dw.cuda(), l.cuda(), idx, qmm.SIGMOID, True, scale, out=torch.empty_like(l, device="cuda")).cpu().double()
+        p, g = want.abs() / abs(scale), scale * dw.double()
+        d = p * (p[:, None, :] * (g[:, :, None] - g[:, None, :])).sum(2) * torch.sigmoid(-l.double()[:, 1:10:4])
+        size = p * (p[:, None, :] * (g[:, :, None] - g[:, None, :]).abs()).sum(2)
+        assert bool(((got[:, 1:10:4] - d).abs() <= (4 * 150 + 64) * 2.0**-24 * size + ref.rounding(d, l.dtype) + 2.0**-146).all())
