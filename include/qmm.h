@@ -500,7 +500,7 @@ qmm_status qmm_expert_combine_grad(qmm_dtype dtype, const void* dy, int64_t lddy
  *   largest c (a missing second counts 0); the top_groups best stay, equal ones by lower group
  *   idx = the topk experts of the largest c among them, larger first, equal ones by lower expert
  *   weights = scale * s[idx], with `renormalize` divided by the sum of the chosen s before
- * Scores are compared as they are in 64 bits; without a bias experts are compared by their logits.  An expert whose
+ * Scores are compared as they are in 64 bits; without a bias experts, and groups where group_top is 1, by their logits.  An expert whose
  * logit or bias is -inf or NaN is never chosen: slots for which nothing is left have idx -1 (dropped by the
  * calls above) and weight 0.  A logit of +inf counts as the largest finite fp32.
  * 1 <= topk <= min(E, 32), E <= 1024, 1 <= groups <= 32, groups divides E, 1 <= top_groups <= groups.          */

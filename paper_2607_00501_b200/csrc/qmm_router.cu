@@ -336,8 +336,10 @@ template <typename T> __device__ __noinline__ int route_exactly(const T* __restr
 {
     const double none = -INFINITY;
     const Score64 q = score64_of(row, p, lane);
+    // without a bias the scores' order is that of the logits, which do not run into one another where scores do; sums of two scores are needed for groups alone
+    const bool by_logit = !p.bias && !(p.groups > 1 && p.group_top == 2);
 #pragma unroll 1
-    for (int e = lane; e < p.E; e += 32) sd[e] = value64(row, e, q, p);
+    for (int e = lane; e < p.E; e += 32) sd[e] = by_logit ? (double)route_logit(Dt<T>::up(row[e])) : value64(row, e, q, p);
     __syncwarp();
     if (p.groups > 1) {
         const double unused[1] = {none};
@@ -347,7 +349,7 @@ template <typename T> __device__ __noinline__ int route_exactly(const T* __restr
         for (int e = lane; e < p.E; e += 32)
             if (!(open >> (((e * p.per_inverse >> 20) << p.share) & 31) & 1u)) sd[e] = none;
     }
-    if (!p.bias)                                           // the scores' order is that of the logits
+    if (!p.bias && !by_logit)
 #pragma unroll 1
         for (int e = lane; e < p.E; e += 32)
             if (sd[e] > none) sd[e] = (double)route_logit(Dt<T>::up(row[e]));

@@ -284,3 +284,21 @@ def test_weights_of_chosen_scores_far_from_one_another(qmm, dt, E):
         d = p * (p[:, None, :] * (g[:, :, None] - g[:, None, :])).sum(2) * torch.sigmoid(-l.double()[:, 1:10:4])
         size = p * (p[:, None, :] * (g[:, :, None] - g[:, None, :]).abs()).sum(2)
         assert bool(((got[:, 1:10:4] - d).abs() <= (4 * 150 + 64) * 2.0**-24 * size + ref.rounding(d, l.dtype) + 2.0**-146).all())
+
+
+@pytest.mark.parametrize("dt", list(ref.DTYPES))
+@pytest.mark.parametrize("sigmoid", [False, True])
+@pytest.mark.parametrize("E,G,top,topk", [(21, 7, 6, 9), (64, 8, 5, 6), (256, 8, 4, 8), (96, 3, 2, 20)])
+def test_groups_by_logits_whose_scores_are_all_alike(qmm, dt, sigmoid, E, G, top, topk):
+    """Without a bias groups are valued by their largest logit: softmax scores beside one of 2000 are zero in 64 bits too, sigmoids of 45 are one.  Many equal logits, so that the
+    choice's end lies among them."""
+    gen = torch.Generator().manual_seed(E)
+    l = (torch.randn(80, E, generator=gen) * 3).round()
+    l[:, : E // 2] = torch.where(torch.rand(80, E // 2, generator=gen) < 0.7, 0.0, l[:, : E // 2])
+    if sigmoid:
+        l += 45
+    else:
+        l[torch.arange(80), torch.randint(0, E, (80,), generator=gen)] = 2000.0
+    l = l.to(ref.DTYPES[dt])
+    for renorm in (False, True):
+        check(qmm, l, topk, sigmoid, None, G, top, 1, renorm)
